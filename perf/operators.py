@@ -410,12 +410,17 @@ def _exact_stored(c, x):
     """What a cache of the case's type holds for float64 rows x."""
     if c["cache"] != "e4m3":
         return x.to(TYPES[c["cache"]]).double()
+
+    def two(k):  # 2^k for whole numbers (a power in 64 bits on the GPU may be off by a rounding)
+        return torch.ldexp(torch.ones(k.shape, device=k.device), k.int()).double()
+
     top = x.abs().amax(-1, keepdim=True)
-    k = torch.ceil(torch.log2(top / 448.0))
-    k = torch.clamp(torch.where(448.0 * 2.0 ** (k - 1) >= top, k - 1, k), -120, 120)  # (a logarithm just above a whole number)
-    y = x / 2.0 ** k
-    step = 2.0 ** (torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
-    return torch.round(y / step) * step * 2.0 ** k
+    k = torch.ceil(torch.log2(top / 448.0).clamp(min=-120))
+    k = torch.where(448.0 * two(k - 1) >= top, k - 1, k)  # (a logarithm just above a whole number)
+    k = torch.where(448.0 * two(k) < top, k + 1, k).clamp(min=-120)
+    y = x / two(k)
+    step = two(torch.frexp(y.abs().clamp(min=2.0 ** -6)).exponent - 4)
+    return torch.round(y / step) * step * two(k)
 
 
 def exact(case, seed):
