@@ -58,7 +58,7 @@ def listed():
         # a prompt chunk of a model without shared heads
         _base("attn", name="attn_chunk", B=2, T=1021, H=40, Hkv=40, p_lo=1500, p_hi=2500, mask="causal"),
         # 32-bit trees of a small model (64-wide heads), used to check a target
-        _base("attn", name="attn_tree_f32", B=4, T=13, H=4, Hkv=4, hd=64, p_lo=64, p_hi=1500, dtype="f32", cache="f32",
+        _base("attn", name="attn_tree_f32", B=4, T=13, H=4, Hkv=4, hd=64, rot=64, p_lo=64, p_hi=1500, dtype="f32", cache="f32",
               ragged=True),
     ]
 
