@@ -59,7 +59,8 @@ typedef enum {
     FE_ERR_DEVICE = -7       /* a device-side range check failed (token, page id) */
 } fe_status;
 
-typedef enum { FE_F32 = 0, FE_BF16 = 1 } fe_dtype;
+/* FE_E4M3 (8-bit floats with a scale per row) is a cache type of fe_target.h only. */
+typedef enum { FE_F32 = 0, FE_BF16 = 1, FE_E4M3 = 2 } fe_dtype;
 
 /* Shape of one drafter. Sec. 2.1 fixes the structure (N layers, shared frozen LM
  * head); the layer internals follow the LLaMA-style block EAGLE-3 uses. */

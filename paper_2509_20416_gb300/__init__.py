@@ -472,3 +472,8 @@ def fe_lm_head_topk_noalloc(h: Handle, hidden, B: int, top_k: int, temperature: 
                                         _dp(out["topk_id"]), _dp(out["topk_logit"]), _dp(out["topk_prob"]),
                                         _dp(out["lse"]), _stream(stream)), "fe_lm_head_topk_noalloc")
     return out
+
+
+from .target import (FE_E4M3, Cache, Target, alloc_cache, fe_cache_keep, fe_cache_read,  # noqa: E402,F401
+                     fe_cache_write, fe_rope, fe_target_free, fe_target_init, fe_target_status, fe_tree_attention,
+                     make_target_config)

@@ -1,0 +1,83 @@
+// Internal launch interface of the target-side operators (include/fe_target.h).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "fe_kernels.h"
+#include "fe_target.h"
+
+namespace fe {
+
+// Where a layer's cache rows lie. Row index (of head_dim elements, and of the scales) of
+// slot s of sequence b and head h: (b Hkv + h) max_seq + s, or, paged,
+// (table[b max_pages + s / page_size] Hkv + h) page_size + s % page_size.
+struct CacheView {
+    void *k, *v;
+    float *ks, *vs;
+    const int* table;
+    int n_pages, page_size, max_pages, max_seq, Hkv;
+};
+
+// rotation of rows: the table holds (cos, sin) [max_seq][rope_dim / 2]
+struct RopeView {
+    const float2* table;
+    int dim, interleaved, max_pos;
+};
+
+// fe_rope (cache_kind 0) and fe_cache_write (1: cache of the rows' type, 2: e4m3)
+struct RowsArgs {
+    int B, T, HA, HB;  // HA heads of rotated rows a; HB heads of rows b (fe_rope's k), or KV heads
+    fe_rows a_in, a_out, b_in, b_out;  // b_in: fe_rope's k or fe_cache_write's k
+    fe_rows v_in;
+    const int *pos, *start, *n_rows;
+    RopeView rope;
+    float dir;  // +1 forward, -1 the gradient: the sign of the sines
+    CacheView cache;
+    int* status;
+};
+
+struct ReadArgs {
+    int B, L;
+    const int *start, *n_rows;
+    CacheView cache;
+    fe_rows k_out, v_out;
+    int* status;
+};
+
+constexpr int kKeepMaxLayers = 64;  // per launch (the pointers travel as kernel arguments)
+
+struct KeepArgs {
+    int B, N, n_layers, row_bytes;
+    const int *path, *n_accept, *start;
+    CacheView cache;  // (its pointers are per layer, below)
+    fe_kv layer[kKeepMaxLayers];
+    int* status;
+};
+
+struct TreeAttnArgs {
+    int B, T, H, Hkv, G;
+    fe_rows q, out;
+    float* lse;
+    const int *prefix, *nodes;
+    const uint8_t* mask;
+    float scale;
+    CacheView cache;
+    float *part_o, *part_ml;  // per CTA two partial items: [2 G][rows][hd] sums, [2 G][rows][2] (max, sum)
+    int* status;
+    int q_vec, out_vec;  // rows of q / out on 16-byte boundaries
+};
+
+// rows of an attention item whose partial results the workspace holds, per CTA and slot
+constexpr int kAttnItemRows = 256;
+
+cudaError_t launch_rope_table(float2* table, int max_seq, int pairs, const double* inv_freq, double amplitude,
+                              cudaStream_t st);
+cudaError_t launch_rows(const RowsArgs& a, fe_dtype dtype, int hd, int cache_kind, cudaStream_t st);
+cudaError_t launch_cache_read(const ReadArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int hd, cudaStream_t st);
+cudaError_t launch_cache_keep(const KeepArgs& a, cudaStream_t st);
+cudaError_t tree_attn_prepare();
+cudaError_t launch_tree_attn(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int hd, int num_sms,
+                             cudaStream_t st);
+
+}  // namespace fe

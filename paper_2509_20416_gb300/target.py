@@ -1,0 +1,315 @@
+"""Python binding of the target-side operators (include/fe_target.h): rotary positions, the
+key/value cache's write, read and accepted-row moves, and attention of a draft tree over it.
+
+As the rest of the package, these functions only marshal arguments. Row tensors (queries,
+keys, values, outputs) are CUDA tensors [B, T, heads, head_dim] of the handle's type with any
+strides whose innermost dimension is contiguous, such as views of a fused projection; integer
+inputs are contiguous CUDA int32 tensors.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+from . import _check, _i32, _lib, _stream, _vp, FE_BF16, FE_F32
+
+FE_E4M3 = 2
+_DTYPES = {"f32": FE_F32, "bf16": FE_BF16, "e4m3": FE_E4M3}
+_TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
+
+_f32 = ctypes.c_float
+_i64 = ctypes.c_int64
+
+
+class fe_target_config(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("n_heads", "n_kv_heads", "head_dim", "max_batch", "max_seq", "page_size", "dtype",
+                                    "cache_dtype", "rope_dim", "rope_layout", "rope_scaling")] + \
+               [(n, _f32) for n in ("rope_theta", "rope_factor", "rope_low", "rope_high", "rope_orig")]
+
+
+class fe_rows(ctypes.Structure):
+    _fields_ = [("p", _vp), ("batch", _i64), ("token", _i64), ("head", _i64)]
+
+
+class fe_kv(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp)]
+
+
+class fe_pages(ctypes.Structure):
+    _fields_ = [("table", _vp), ("n_pages", _i32)]
+
+
+class fe_rope_args(ctypes.Structure):
+    _fields_ = [("B", _i32), ("T", _i32), ("q", fe_rows), ("k", fe_rows), ("q_out", fe_rows), ("k_out", fe_rows),
+                ("pos", _vp), ("backward", _i32)]
+
+
+class fe_cache_write_args(ctypes.Structure):
+    _fields_ = [("B", _i32), ("T", _i32), ("k", fe_rows), ("v", fe_rows), ("q", fe_rows), ("q_out", fe_rows),
+                ("pos", _vp), ("start", _vp), ("n_rows", _vp), ("cache", fe_kv), ("pages", fe_pages)]
+
+
+class fe_cache_read_args(ctypes.Structure):
+    _fields_ = [("B", _i32), ("L", _i32), ("start", _vp), ("n_rows", _vp), ("cache", fe_kv), ("pages", fe_pages),
+                ("k_out", fe_rows), ("v_out", fe_rows)]
+
+
+class fe_tree_attention_args(ctypes.Structure):
+    _fields_ = [("B", _i32), ("T", _i32), ("q", fe_rows), ("out", fe_rows), ("lse", _vp), ("prefix_len", _vp),
+                ("n_nodes", _vp), ("mask", _vp), ("scale", _f32), ("cache", fe_kv), ("pages", fe_pages)]
+
+
+class fe_cache_keep_args(ctypes.Structure):
+    _fields_ = [("B", _i32), ("N", _i32), ("n_layers", _i32), ("path", _vp), ("n_accept", _vp), ("start", _vp),
+                ("caches", ctypes.POINTER(fe_kv)), ("pages", fe_pages)]
+
+
+_lib.fe_target_init.argtypes = [ctypes.POINTER(fe_target_config), _vp, ctypes.POINTER(_vp)]
+_lib.fe_target_init.restype = ctypes.c_int
+_lib.fe_target_free.argtypes = [_vp]
+_lib.fe_target_free.restype = None
+_lib.fe_target_status.argtypes = [_vp, _vp]
+_lib.fe_target_status.restype = ctypes.c_int
+for _name in ("rope", "cache_write", "cache_read", "tree_attention", "cache_keep"):
+    _f = getattr(_lib, "fe_" + _name)
+    _f.argtypes = [_vp, ctypes.POINTER(globals()[f"fe_{_name}_args"]), _vp]
+    _f.restype = ctypes.c_int
+
+
+def make_target_config(cfg: dict) -> fe_target_config:
+    hd = cfg["head_dim"]
+    return fe_target_config(
+        cfg["n_heads"], cfg["n_kv_heads"], hd, cfg.get("max_batch", 1), cfg["max_seq"], cfg.get("page_size", 0),
+        _DTYPES[cfg["dtype"]], _DTYPES[cfg.get("cache_dtype", cfg["dtype"])], cfg.get("rope_dim", hd),
+        _LAYOUTS[cfg.get("rope_layout", "half")], _SCALINGS[cfg.get("rope_scaling", "none")], cfg["rope_theta"],
+        cfg.get("rope_factor", 1.0), cfg.get("rope_low", 0.0), cfg.get("rope_high", 0.0), cfg.get("rope_orig", 0.0))
+
+
+class Target:
+    """An initialised target-side handle (owns a fe_target*)."""
+
+    def __init__(self, ptr: int, cfg: dict):
+        self.ptr = ptr
+        self.cfg = dict(cfg)
+        self.H, self.Hkv, self.hd = cfg["n_heads"], cfg["n_kv_heads"], cfg["head_dim"]
+        self.dtype = _TORCH[cfg["dtype"]]
+        self.cache_name = cfg.get("cache_dtype", cfg["dtype"])
+        self.page_size, self.max_seq, self.max_batch = cfg.get("page_size", 0), cfg["max_seq"], cfg.get("max_batch", 1)
+
+    def __del__(self):
+        self.close()
+
+    def close(self):
+        if getattr(self, "ptr", None):
+            _lib.fe_target_free(self.ptr)
+            self.ptr = None
+
+
+def fe_target_init(cfg: dict, stream=None) -> Target:
+    """cfg: n_heads, n_kv_heads, head_dim, max_seq, dtype ("f32", "bf16"), rope_theta, and
+    optionally max_batch, page_size, cache_dtype ("f32", "bf16", "e4m3"; dtype), rope_dim
+    (head_dim), rope_layout ("half", "interleaved"), rope_scaling ("none", "linear", "ntk",
+    "bands", "yarn") with rope_factor, rope_low, rope_high and rope_orig."""
+    c = make_target_config(cfg)
+    out = _vp()
+    _check(_lib.fe_target_init(ctypes.byref(c), _stream(stream), ctypes.byref(out)), "fe_target_init")
+    return Target(out.value, cfg)
+
+
+def fe_target_free(t: Target) -> None:
+    t.close()
+
+
+def fe_target_status(t: Target, stream=None) -> int:
+    return int(_lib.fe_target_status(t.ptr, _stream(stream)))
+
+
+class Cache:
+    """The caches of a target's layers: k, v [layers, ...] tensors (or lists of one tensor per
+    layer) in the layout of fe_kv, with float32 scales for an e4m3 cache, and the page table
+    [B, ceil(max_seq / page_size)] that they share. The tensors stay the caller's; the
+    addresses are laid out once, here."""
+
+    def __init__(self, t: Target, k, v, k_scale=None, v_scale=None, page_table=None, n_pages: int = 0):
+        ps = t.page_size
+        rows = (n_pages, t.Hkv, ps) if ps else (t.max_batch, t.Hkv, t.max_seq)
+        types = (torch.float8_e4m3fn, torch.uint8) if t.cache_name == "e4m3" else (_TORCH[t.cache_name],)
+        n = len(k)
+        if n < 1 or len(v) != n:
+            raise ValueError("a cache needs k and v of the same number of layers")
+        scaled = t.cache_name == "e4m3"
+        if scaled and (k_scale is None or v_scale is None or len(k_scale) != n or len(v_scale) != n):
+            raise ValueError("an e4m3 cache needs k_scale and v_scale of every layer")
+        self.kv = (fe_kv * n)()
+        for i in range(n):
+            for x in (k[i], v[i]):
+                _cuda(x)
+                if tuple(x.shape) != rows + (t.hd,) or x.dtype not in types or not x.is_contiguous():
+                    raise ValueError(f"cache layer {i} must be a contiguous {types[0]} tensor of shape {rows + (t.hd,)}")
+            s = (None, None)
+            if scaled:
+                for x in (k_scale[i], v_scale[i]):
+                    _cuda(x)
+                    if tuple(x.shape) != rows or x.dtype != torch.float32 or not x.is_contiguous():
+                        raise ValueError(f"scales of cache layer {i} must be contiguous float32 of shape {rows}")
+                s = (k_scale[i].data_ptr(), v_scale[i].data_ptr())
+            self.kv[i] = fe_kv(k[i].data_ptr(), v[i].data_ptr(), *s)
+        self.n_layers, self.k, self.v, self.k_scale, self.v_scale = n, k, v, k_scale, v_scale
+        self.page_table, self.n_pages = page_table, n_pages
+        if ps:
+            if page_table is None or page_table.dim() != 2 or page_table.shape[1] != -(-t.max_seq // ps):
+                raise ValueError("a paged cache needs a page table [B, ceil(max_seq / page_size)]")
+            _ints(page_table, tuple(page_table.shape))
+        self.pages = fe_pages(page_table.data_ptr() if ps else None, n_pages)
+
+    def _layer(self, i: int) -> fe_kv:
+        if not 0 <= i < self.n_layers:
+            raise ValueError(f"layer {i} of a cache of {self.n_layers}")
+        return self.kv[i]
+
+    def _fits(self, B: int) -> None:
+        if self.page_table is not None and self.page_table.shape[0] < B:
+            raise ValueError("the page table has fewer rows than the call has sequences")
+
+    def tensors(self):
+        for x in (self.k, self.v, self.k_scale, self.v_scale, self.page_table):
+            if isinstance(x, torch.Tensor):
+                yield x
+            elif x is not None:
+                yield from x
+
+
+def alloc_cache(t: Target, n_layers: int, n_pages: int = 0, page_table=None, device="cuda") -> Cache:
+    """A zeroed cache of n_layers layers (paged: n_pages pages each, addressed by page_table)."""
+    rows = (n_layers,) + ((n_pages, t.Hkv, t.page_size) if t.page_size else (t.max_batch, t.Hkv, t.max_seq))
+    k, v = (torch.zeros(rows + (t.hd,), dtype=_TORCH[t.cache_name], device=device) for _ in range(2))
+    s = [torch.ones(rows, device=device) for _ in range(2)] if t.cache_name == "e4m3" else [None, None]
+    return Cache(t, k, v, *s, page_table=page_table, n_pages=n_pages)
+
+
+def _cuda(x) -> None:
+    if not x.is_cuda:
+        raise ValueError("buffers the kernels access must be CUDA tensors")
+
+
+def _ints(x, shape) -> int | None:
+    """The address of a contiguous CUDA int32 tensor of the given shape (None passes)."""
+    if x is None:
+        return None
+    _cuda(x)
+    if x.dtype != torch.int32 or tuple(x.shape) != shape or not x.is_contiguous():
+        raise ValueError(f"expected a contiguous int32 tensor of shape {shape}, got {x.dtype} {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _rows(t: Target, x, B: int, T: int, heads: int) -> fe_rows:
+    _cuda(x)
+    if x.dtype != t.dtype or tuple(x.shape) != (B, T, heads, t.hd) or x.stride(3) != 1:
+        raise ValueError(f"expected {t.dtype} rows {(B, T, heads, t.hd)} with contiguous elements, got {x.dtype} "
+                         f"{tuple(x.shape)} with strides {tuple(x.stride())}")
+    s = x.stride()
+    return fe_rows(x.data_ptr(), s[0], s[1], s[2])
+
+
+def _call(name: str, t: Target, args, stream, *tensors) -> None:
+    raw = _stream(stream)
+    # memory that PyTorch's allocator hands out belongs to the current stream: on another one,
+    # tell it that the tensors are in use there
+    if stream is not None and raw != torch.cuda.current_stream().cuda_stream:
+        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(raw)
+        for x in tensors:
+            if x is not None:
+                x.record_stream(s)
+    _check(getattr(_lib, name)(t.ptr, ctypes.byref(args), raw), name)
+
+
+def fe_rope(t: Target, q, k, pos, backward: bool = False, q_out=None, k_out=None, stream=None) -> tuple:
+    """Rotary positions (include/fe_target.h) of q [B, T, H, hd] and k [B, T, Hkv, hd] (either
+    may be None) at pos [B, T]; with backward, the gradient's rotation. Returns (q_out, k_out);
+    pass the inputs as outputs to rotate in place."""
+    B, T = int(pos.shape[0]), int(pos.shape[1])
+    a = fe_rope_args(B, T, pos=_ints(pos, (B, T)), backward=1 if backward else 0)
+    if q is not None:
+        a.q = _rows(t, q, B, T, t.H)
+        q_out = torch.empty((B, T, t.H, t.hd), dtype=t.dtype, device=q.device) if q_out is None else q_out
+        a.q_out = _rows(t, q_out, B, T, t.H)
+    if k is not None:
+        a.k = _rows(t, k, B, T, t.Hkv)
+        k_out = torch.empty((B, T, t.Hkv, t.hd), dtype=t.dtype, device=k.device) if k_out is None else k_out
+        a.k_out = _rows(t, k_out, B, T, t.Hkv)
+    _call("fe_rope", t, a, stream, q, k, q_out, k_out, pos)
+    return q_out, k_out
+
+
+def fe_cache_write(t: Target, cache: Cache, layer: int, k, v, start, n_rows=None, pos=None, q=None, q_out=None,
+                   stream=None):
+    """Rows k, v [B, T, Hkv, hd] into slots start[b] + i of a layer's cache, the keys rotated to
+    pos [B, T] if given, quantised if the cache is; with q [B, T, H, hd] also rotates the
+    queries into q_out, which is returned."""
+    B, T = int(k.shape[0]), int(k.shape[1])
+    cache._fits(B)
+    a = fe_cache_write_args(B, T, _rows(t, k, B, T, t.Hkv), _rows(t, v, B, T, t.Hkv), pos=_ints(pos, (B, T)),
+                            start=_ints(start, (B,)), n_rows=_ints(n_rows, (B,)), cache=cache._layer(layer),
+                            pages=cache.pages)
+    if q is not None:
+        a.q = _rows(t, q, B, T, t.H)
+        q_out = torch.empty((B, T, t.H, t.hd), dtype=t.dtype, device=q.device) if q_out is None else q_out
+        a.q_out = _rows(t, q_out, B, T, t.H)
+    _call("fe_cache_write", t, a, stream, k, v, start, n_rows, pos, q, q_out, *(cache.tensors() if stream else ()))
+    return q_out
+
+
+def fe_cache_read(t: Target, cache: Cache, layer: int, start, n_rows, L: int, k_out=None, v_out=None,
+                  stream=None) -> tuple:
+    """Slots start[b] .. start[b] + n_rows[b] - 1 of a layer's cache as rows k, v [B, L, Hkv, hd]
+    of the handle's type; rows past n_rows[b] are zero."""
+    B = int(start.shape[0])
+    cache._fits(B)
+    shape = (B, L, t.Hkv, t.hd)
+    k_out = torch.empty(shape, dtype=t.dtype, device=start.device) if k_out is None else k_out
+    v_out = torch.empty(shape, dtype=t.dtype, device=start.device) if v_out is None else v_out
+    a = fe_cache_read_args(B, L, _ints(start, (B,)), _ints(n_rows, (B,)), cache._layer(layer), cache.pages,
+                           _rows(t, k_out, B, L, t.Hkv), _rows(t, v_out, B, L, t.Hkv))
+    _call("fe_cache_read", t, a, stream, start, n_rows, k_out, v_out, *(cache.tensors() if stream else ()))
+    return k_out, v_out
+
+
+def fe_tree_attention(t: Target, cache: Cache, layer: int, q, prefix_len, mask=None, n_nodes=None,
+                      scale: float | None = None, out=None, lse=None, stream=None) -> tuple:
+    """Attention of q [B, T, H, hd]'s nodes over a layer's cache: every node sees the slots
+    before prefix_len[b], and slot prefix_len[b] + c where mask [B, T, T] (uint8) is set, or
+    c <= i without a mask (consecutive tokens, single-token decoding). scale: 1 / sqrt(hd)
+    unless given. Returns (out [B, T, H, hd], lse [B, T, H] float32)."""
+    B, T = int(q.shape[0]), int(q.shape[1])
+    cache._fits(B)
+    if out is None:
+        out = torch.empty((B, T, t.H, t.hd), dtype=t.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((B, T, t.H), dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or tuple(lse.shape) != (B, T, t.H) or not lse.is_contiguous() or not lse.is_cuda:
+        raise ValueError(f"lse must be a contiguous float32 CUDA tensor of shape {(B, T, t.H)}")
+    if mask is not None and (mask.dtype not in (torch.uint8, torch.bool) or tuple(mask.shape) != (B, T, T)
+                             or not mask.is_contiguous() or not mask.is_cuda):
+        raise ValueError(f"mask must be a contiguous uint8 CUDA tensor of shape {(B, T, T)}")
+    a = fe_tree_attention_args(B, T, _rows(t, q, B, T, t.H), _rows(t, out, B, T, t.H), lse.data_ptr(),
+                               _ints(prefix_len, (B,)), _ints(n_nodes, (B,)), None if mask is None else mask.data_ptr(),
+                               1.0 / math.sqrt(t.hd) if scale is None else float(scale), cache._layer(layer), cache.pages)
+    _call("fe_tree_attention", t, a, stream, q, prefix_len, n_nodes, mask, out, lse,
+          *(cache.tensors() if stream else ()))
+    return out, lse
+
+
+def fe_cache_keep(t: Target, cache: Cache, path, n_accept, start, stream=None) -> None:
+    """Move the accepted nodes' rows, slots start[b] + path[b][j] for j < n_accept[b], to slots
+    start[b] + 1 + j in every layer of the cache (path [B, N], n_accept [B], start [B])."""
+    B, N = int(path.shape[0]), int(path.shape[1])
+    if cache.page_table is None and B > t.max_batch:
+        raise ValueError("more sequences than the cache holds")
+    cache._fits(B)
+    a = fe_cache_keep_args(B, N, cache.n_layers, _ints(path, (B, N)), _ints(n_accept, (B,)), _ints(start, (B,)),
+                           cache.kv, cache.pages)
+    _call("fe_cache_keep", t, a, stream, path, n_accept, start, *(cache.tensors() if stream else ()))

@@ -161,3 +161,52 @@ def test_init_rejects_a_missing_layer_weight(lib):
     layers[1] = lib.fe_layer_weights(*([8] * 7))
     c.dtype = 7  # neither FE_F32 nor FE_BF16
     assert so.fe_draft_init(ctypes.byref(c), ctypes.byref(w), None, ctypes.byref(out)) == lib.FE_ERR_INVALID_ARG
+
+
+TARGET_CFG = dict(n_heads=8, n_kv_heads=2, head_dim=128, max_batch=2, max_seq=64, page_size=16, dtype="bf16",
+                  cache_dtype="e4m3", rope_theta=1e4, rope_factor=4.0, rope_low=1.0, rope_high=4.0, rope_orig=32.0)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(n_heads=0), "INVALID_ARG"), (dict(n_heads=7), "INVALID_ARG"), (dict(head_dim=0), "INVALID_ARG"),
+    (dict(max_batch=0), "INVALID_ARG"), (dict(max_batch=65536), "INVALID_ARG"), (dict(max_seq=0), "INVALID_ARG"),
+    (dict(max_seq=2**28 + 1), "INVALID_ARG"), (dict(page_size=-1), "INVALID_ARG"), (dict(rope_dim=0), "INVALID_ARG"),
+    (dict(rope_dim=7), "INVALID_ARG"), (dict(rope_dim=130), "INVALID_ARG"), (dict(rope_theta=1.0), "INVALID_ARG"),
+    (dict(rope_theta=float("nan")), "INVALID_ARG"), (dict(rope_scaling="linear", rope_factor=0.5), "INVALID_ARG"),
+    (dict(rope_scaling="ntk", rope_dim=2), "INVALID_ARG"), (dict(rope_scaling="bands", rope_high=1.0), "INVALID_ARG"),
+    (dict(rope_scaling="bands", rope_orig=0.0), "INVALID_ARG"), (dict(rope_scaling="yarn"), "INVALID_ARG"),
+    (dict(rope_scaling="yarn", rope_low=float("inf"), rope_high=1.0), "INVALID_ARG"),
+    (dict(head_dim=96), "UNSUPPORTED"), (dict(dtype="f32"), "UNSUPPORTED"), (dict(cache_dtype="f32"), "UNSUPPORTED"),
+])
+def test_target_init_rejects_configs_before_any_cuda_call(lib, change, code):
+    so = lib._lib
+    c = lib.make_target_config(dict(TARGET_CFG, **change))
+    out = ctypes.c_void_p()
+    assert so.fe_target_init(ctypes.byref(c), None, ctypes.byref(out)) == getattr(lib, "FE_ERR_" + code)
+    assert out.value is None
+
+
+def test_target_calls_reject_a_missing_handle_or_arguments(lib):
+    so = lib._lib
+    assert so.fe_target_init(None, None, None) == lib.FE_ERR_INVALID_ARG
+    assert so.fe_target_status(None, None) == lib.FE_ERR_INVALID_ARG
+    for f in (so.fe_rope, so.fe_cache_write, so.fe_cache_read, so.fe_tree_attention, so.fe_cache_keep):
+        assert f(None, None, None) == lib.FE_ERR_INVALID_ARG
+    so.fe_target_free(None)  # no-op
+
+
+def test_target_binding_rejects_wrong_tensors_before_the_library(lib):
+    """Host tensors, wrong types, shapes and strides raise ValueError before any library call."""
+    import torch
+    t = lib.Target(0, dict(TARGET_CFG, page_size=0, cache_dtype="bf16"))
+    q, k = torch.zeros(1, 3, 8, 128, dtype=torch.bfloat16), torch.zeros(1, 3, 2, 128, dtype=torch.bfloat16)
+    pos = torch.zeros(1, 3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="CUDA"):
+        lib.fe_rope(t, q, k, pos)
+    with pytest.raises(ValueError, match="CUDA"):
+        lib.Cache(t, [k], [k])
+    with pytest.raises(ValueError, match="same number of layers"):
+        lib.Cache(t, [k], [])
+    e = lib.Target(0, dict(TARGET_CFG, page_size=0))
+    with pytest.raises(ValueError, match="scale"):
+        lib.Cache(e, [k], [k])
