@@ -171,6 +171,7 @@ FE_API fe_status fe_cache_read(fe_target *t, const fe_cache_read_args *a, void *
  *  prefix_len  device [B] int32: P_b >= 0, P_b + n_b <= max_seq
  *  n_nodes     device [B] int32 in 0..T, or NULL for T
  *  mask        device [B, T, T] uint8 (fe_build_tree's mask) or NULL
+ *  scale       finite, >= 0
  * Softmax statistics and sums are float32. A node that sees no slot, or only scores of minus
  * infinity, and every node i >= n_b get a zero row and lse = -inf; slots that a node does not
  * see do not affect it whatever they hold, NaN included. A sequence with P_b or n_b out of

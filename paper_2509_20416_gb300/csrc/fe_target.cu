@@ -299,7 +299,8 @@ fe_status fe_cache_read(fe_target* t, const fe_cache_read_args* a, void* stream)
 
 fe_status fe_tree_attention(fe_target* t, const fe_tree_attention_args* a, void* stream) {
     if (!t || !a || !a->q.p || !a->out.p || !a->prefix_len || !shape_ok(t, a->B, a->T)) return FE_ERR_INVALID_ARG;
-    if (!kv_ok(t, a->cache) || !pages_ok(t, a->pages) || !isfinite(a->scale)) return FE_ERR_INVALID_ARG;
+    if (!kv_ok(t, a->cache) || !pages_ok(t, a->pages) || !isfinite(a->scale) || a->scale < 0.f)
+        return FE_ERR_INVALID_ARG;
     const fe_status dv = check_device(t);
     if (dv != FE_OK) return dv;
     const fe_target_config& c = t->cfg;

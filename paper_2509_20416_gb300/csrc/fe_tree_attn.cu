@@ -1,6 +1,7 @@
 // Attention of a draft tree's nodes (or of consecutive tokens) over the cache
 // (fe_tree_attention), and the join of items split between CTAs.
 #include "fe_tree_attn_simt.cuh"
+#include "fe_tree_attn_tc.cuh"
 
 namespace fe {
 
@@ -94,40 +95,56 @@ cudaError_t launch_join(const TreeAttnArgs& a, int ncta, cudaStream_t st) {
                     ncta);
 }
 
-template <typename QT, typename CT, int HD>
+template <int HD>
 cudaError_t launch_simt(const TreeAttnArgs& a, int num_sms, cudaStream_t st) {
-    const cudaError_t e = launch_k(tree_attn_simt_kernel<QT, CT, HD>, dim3(num_sms), dim3(kSimtThreads),
-                                   sizeof(SimtSmem<HD>), st, false, a);
+    const cudaError_t e = launch_k(tree_attn_simt_kernel<HD>, dim3(num_sms), dim3(kSimtThreads), sizeof(SimtSmem<HD>), st,
+                                   false, a);
     if (e != cudaSuccess) return e;
-    return launch_join<QT, HD, SimtPlan, kSimtRows>(a, num_sms, st);
+    return launch_join<float, HD, SimtPlan, kSimtRows>(a, num_sms, st);
 }
 
-template <typename QT, typename CT, int HD>
-cudaError_t prepare_simt() {
-    return cudaFuncSetAttribute(tree_attn_simt_kernel<QT, CT, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                (int)sizeof(SimtSmem<HD>));
+template <int HD, bool Q8, int MT>
+cudaError_t launch_tc(const TreeAttnArgs& a, int num_sms, cudaStream_t st) {
+    const cudaError_t e = launch_k(tree_attn_tc_kernel<HD, Q8, MT>, dim3(num_sms), dim3(TcShape<HD, Q8, MT>::kThreads),
+                                   tc_smem<HD, Q8, MT>(), st, false, a);
+    if (e != cudaSuccess) return e;
+    return launch_join<bf16_t, HD, TcPlan, kAttnItemRows>(a, num_sms, st);
+}
+
+template <typename K>
+cudaError_t allow_smem(K kern, size_t bytes) {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <int HD>
+cudaError_t prepare() {
+    cudaError_t e;
+    if ((e = allow_smem(tree_attn_simt_kernel<HD>, sizeof(SimtSmem<HD>))) != cudaSuccess) return e;
+    if ((e = allow_smem(tree_attn_tc_kernel<HD, false, 1>, tc_smem<HD, false, 1>())) != cudaSuccess) return e;
+    if ((e = allow_smem(tree_attn_tc_kernel<HD, false, 2>, tc_smem<HD, false, 2>())) != cudaSuccess) return e;
+    if ((e = allow_smem(tree_attn_tc_kernel<HD, true, 1>, tc_smem<HD, true, 1>())) != cudaSuccess) return e;
+    return allow_smem(tree_attn_tc_kernel<HD, true, 2>, tc_smem<HD, true, 2>());
+}
+
+template <int HD>
+cudaError_t launch_hd(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int num_sms, cudaStream_t st) {
+    if (dtype == FE_F32) return launch_simt<HD>(a, num_sms, st);
+    const bool one = (int64_t)a.T * a.G <= 128;  // every item fits one 128-row block: more tiles in flight
+    if (cache_dtype == FE_E4M3)
+        return one ? launch_tc<HD, true, 1>(a, num_sms, st) : launch_tc<HD, true, 2>(a, num_sms, st);
+    return one ? launch_tc<HD, false, 1>(a, num_sms, st) : launch_tc<HD, false, 2>(a, num_sms, st);
 }
 
 }  // namespace
 
 cudaError_t tree_attn_prepare() {
-    cudaError_t e;
-    if ((e = prepare_simt<float, float, 64>()) != cudaSuccess) return e;
-    if ((e = prepare_simt<float, float, 128>()) != cudaSuccess) return e;
-    if ((e = prepare_simt<bf16_t, bf16_t, 64>()) != cudaSuccess) return e;
-    if ((e = prepare_simt<bf16_t, bf16_t, 128>()) != cudaSuccess) return e;
-    if ((e = prepare_simt<bf16_t, e4m3_t, 64>()) != cudaSuccess) return e;
-    return prepare_simt<bf16_t, e4m3_t, 128>();
+    const cudaError_t e = prepare<64>();
+    return e != cudaSuccess ? e : prepare<128>();
 }
 
 cudaError_t launch_tree_attn(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int hd, int num_sms,
                              cudaStream_t st) {
-    if (dtype == FE_F32)
-        return hd == 128 ? launch_simt<float, float, 128>(a, num_sms, st) : launch_simt<float, float, 64>(a, num_sms, st);
-    if (cache_dtype == FE_E4M3)
-        return hd == 128 ? launch_simt<bf16_t, e4m3_t, 128>(a, num_sms, st)
-                         : launch_simt<bf16_t, e4m3_t, 64>(a, num_sms, st);
-    return hd == 128 ? launch_simt<bf16_t, bf16_t, 128>(a, num_sms, st) : launch_simt<bf16_t, bf16_t, 64>(a, num_sms, st);
+    return hd == 128 ? launch_hd<128>(a, dtype, cache_dtype, num_sms, st) : launch_hd<64>(a, dtype, cache_dtype, num_sms, st);
 }
 
 }  // namespace fe

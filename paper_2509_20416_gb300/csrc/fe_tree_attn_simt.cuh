@@ -22,28 +22,7 @@ struct SimtSmem {
     int odd[2];  // the tile holds a non-finite value in a node's row (one flag per tile parity)
 };
 
-// 4 floats of a cache row (CT: the cache type), column c a multiple of 4
-template <typename CT>
-__device__ __forceinline__ float4 cache_load4(const void* base, int64_t row, int hd, int c, const float* scale);
-template <>
-__device__ __forceinline__ float4 cache_load4<float>(const void* base, int64_t row, int hd, int c, const float*) {
-    return *reinterpret_cast<const float4*>((const float*)base + row * hd + c);
-}
-template <>
-__device__ __forceinline__ float4 cache_load4<bf16_t>(const void* base, int64_t row, int hd, int c, const float*) {
-    const uint2 u = *reinterpret_cast<const uint2*>((const bf16_t*)base + row * hd + c);
-    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
-                       __uint_as_float(u.y & 0xFFFF0000u));
-}
-template <>
-__device__ __forceinline__ float4 cache_load4<e4m3_t>(const void* base, int64_t row, int hd, int c, const float* scale) {
-    const uint32_t u = *reinterpret_cast<const uint32_t*>((const uint8_t*)base + row * hd + c);
-    const float s = scale[row];
-    const float2 a = e4m3x2_to_f32(u & 0xFFFF), b = e4m3x2_to_f32(u >> 16);
-    return make_float4(a.x * s, a.y * s, b.x * s, b.y * s);
-}
-
-template <typename QT, typename CT, int HD>
+template <int HD>
 __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const TreeAttnArgs a) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SimtSmem<HD>& sm = *reinterpret_cast<SimtSmem<HD>*>(smem_raw);
@@ -67,7 +46,7 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const Tree
             float x = 0.f;
             if (row < g.rows) {
                 const int node = row / a.G, head = g.h * a.G + row % a.G;
-                x = Storage<QT>::load((const QT*)a.q.p + g.b * a.q.batch + node * a.q.token + head * a.q.head, c);
+                x = ((const float*)a.q.p)[g.b * a.q.batch + node * a.q.token + head * a.q.head + c];
             }
             sm.q[r][c] = x * scale2;
         }
@@ -92,8 +71,8 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const Tree
                 int64_t row;
                 if (slot < g.end && cache_row(a.cache, g.b, slot, row, a.status)) {
                     row += g.h * head_step(a.cache);
-                    kk = cache_load4<CT>(a.cache.k, row, HD, c, a.cache.ks);
-                    vv = cache_load4<CT>(a.cache.v, row, HD, c, a.cache.vs);
+                    kk = *reinterpret_cast<const float4*>((const float*)a.cache.k + row * HD + c);
+                    vv = *reinterpret_cast<const float4*>((const float*)a.cache.v + row * HD + c);
                     if (slot >= g.s.P && !(finite_f32(vv.x) && finite_f32(vv.y) && finite_f32(vv.z) && finite_f32(vv.w)))
                         sm.odd[par] = 1;
                 }
@@ -195,13 +174,13 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const Tree
             if (row >= g.rows) continue;
             if (g.whole) {
                 const int node = row / a.G, head = g.h * a.G + row % a.G;
-                QT* o = (QT*)a.out.p + g.b * a.out.batch + node * a.out.token + head * a.out.head;
+                float* o = (float*)a.out.p + g.b * a.out.batch + node * a.out.token + head * a.out.head;
                 const float inv = sum[i] == 0.f ? 0.f : 1.0f / sum[i];
 #pragma unroll
                 for (int j = 0; j < NC; ++j)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        store_one(o + tx * 4 + 64 * j + k, sum[i] == 0.f ? 0.f : acc[i][j][k] * inv);
+                        o[tx * 4 + 64 * j + k] = sum[i] == 0.f ? 0.f : acc[i][j][k] * inv;
                 if (a.lse && tx == 0)
                     a.lse[((int64_t)g.b * a.T + node) * a.H + head] =
                         sum[i] == 0.f ? -INFINITY : mx[i] * 0.6931471805599453f + logf(sum[i]);
