@@ -99,9 +99,8 @@ typedef struct {
  *                     [n_pages, Hkv, page_size, hd], as in fe_draft.h, of the cache type
  *   k_scale, v_scale  FE_E4M3 only: float32 [max_batch, Hkv, max_seq] or
  *                     [n_pages, Hkv, page_size]; a row stands for its e4m3 numbers times its
- *                     scale. fe_cache_write stores power-of-two scales; the readers accept any
- *                     finite ones and round a product to bfloat16 (exact for powers of two
- *                     down to 2^-120) */
+ *                     scale, a power of two from 2^-120 to 2^120 (as fe_cache_write stores them),
+ *                     so every value is a bfloat16 number */
 typedef struct {
     void *k, *v;
     float *k_scale, *v_scale;
@@ -171,13 +170,14 @@ FE_API fe_status fe_cache_read(fe_target *t, const fe_cache_read_args *a, void *
  *  prefix_len  device [B] int32: P_b >= 0, P_b + n_b <= max_seq
  *  n_nodes     device [B] int32 in 0..T, or NULL for T
  *  mask        device [B, T, T] uint8 (fe_build_tree's mask) or NULL
- *  scale       finite, >= 0
+ *  scale       finite, > 0
  * Softmax statistics and sums are float32. A node that sees no slot, or only scores of minus
  * infinity, and every node i >= n_b get a zero row and lse = -inf; slots that a node does not
  * see do not affect it whatever they hold, NaN included. A sequence with P_b or n_b out of
  * range counts as n_b = 0 and sets FE_ERR_CAPACITY; a bad page id sets FE_ERR_DEVICE and its
  * rows count as zeros. The result does not depend on timing: the same call gives the same bits.
- * B in 1..max_batch, T >= 1. */
+ * B in 1..max_batch, T >= 1. FE_ERR_UNSUPPORTED for a shape whose work could pass 2^31 units of
+ * 64 rows x 64 slots (float32) or 128 x 128. */
 typedef struct {
     int32_t B, T;
     fe_rows q, out;

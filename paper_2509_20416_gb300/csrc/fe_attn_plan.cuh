@@ -40,10 +40,12 @@ __device__ __forceinline__ SeqLen seq_len(const PlanArgs& a, int b, bool* bad = 
     return s;
 }
 
-// ROWS rows an item, TN slots a tile; PAIR: an item of more than 128 rows costs two units a tile
+// ROWS rows an item, TN slots a tile; PAIR: an item of more than 128 rows costs two units a tile.
+// Units are counted in 32 bits (the launch refuses shapes that could pass 2^31): this runs once a
+// CTA before anything else can start, and short code is what it takes to be quick.
 template <int ROWS, int TN, bool PAIR>
 struct Plan {
-    __device__ __forceinline__ static int blocks(int rows) { return (rows + ROWS - 1) / ROWS; }
+    __host__ __device__ __forceinline__ static int blocks(int rows) { return (rows + ROWS - 1) / ROWS; }
     __device__ __forceinline__ static int weight(int rows, int m) { return PAIR && rows - m * ROWS > 128 ? 2 : 1; }
     // slots that block m's rows may see: [0, end)
     __device__ __forceinline__ static int end(const PlanArgs& a, SeqLen s, int m) {
@@ -52,78 +54,94 @@ struct Plan {
         return s.P + last / a.G + 1;
     }
     __device__ __forceinline__ static int tiles(const PlanArgs& a, SeqLen s, int m) {
-        return (end(a, s, m) + TN - 1) / TN;
+        return (int)((uint32_t)(end(a, s, m) + TN - 1) / TN);
     }
     // units of one KV head of a sequence
-    __device__ __forceinline__ static int64_t head_units(const PlanArgs& a, SeqLen s) {
+    __device__ __forceinline__ static int head_units(const PlanArgs& a, SeqLen s) {
         const int rows = s.n * a.G, nb = blocks(rows);
         if (nb == 0) return 0;
-        if (!a.causal) {  // every block but the last is full
-            return (int64_t)tiles(a, s, 0) * ((int64_t)(nb - 1) * weight(ROWS, 0) + weight(rows, nb - 1));
-        }
-        int64_t u = 0;
-        for (int m = 0; m < nb; ++m) u += (int64_t)tiles(a, s, m) * weight(rows, m);
+        if (!a.causal)  // every block but the last is full
+            return tiles(a, s, 0) * ((nb - 1) * weight(ROWS, 0) + weight(rows, nb - 1));
+        int u = 0;
+#pragma unroll 1
+        for (int m = 0; m < nb; ++m) u += tiles(a, s, m) * weight(rows, m);
         return u;
     }
-    // CTA c's first unit
-    __device__ __forceinline__ static int64_t begin(int64_t c, int64_t U, int G) { return c * U / G; }
-    // the CTA that owns the tile starting at unit s
-    __device__ __forceinline__ static int owner(int64_t s, int64_t U, int G) { return (int)(((s + 1) * G - 1) / U); }
-    // tiles of an item (first unit s0, weight w, nt tiles) that start in units [u0, u1)
-    __device__ __forceinline__ static int first_tile(int64_t s0, int w, int nt, int64_t u0) {
-        if (u0 <= s0) return 0;
-        const int64_t t = (u0 - s0 + w - 1) / w;
-        return t < nt ? (int)t : nt;
+    // first tile of an item (first unit s0, weight w = 1 or 2, nt tiles) that starts at unit u0 or later
+    __device__ __forceinline__ static int first_tile(int s0, int w, int nt, int u0) {
+        return u0 <= s0 ? 0 : min((u0 - s0 + w - 1) >> (w - 1), nt);
+    }
+    // whether every call of this shape keeps its units within 32 bits
+    static bool fits(int B, int Hkv, int64_t rows, int max_seq) {
+        const double u = 2.0 * B * Hkv * (double)((rows + ROWS - 1) / ROWS) * (double)(max_seq / TN + 1);
+        return u < 2147483647.0;
     }
 };
 
-// Sum of head_units * Hkv over all sequences; called by a whole warp.
-template <typename PL>
-__device__ __forceinline__ int64_t plan_total(const PlanArgs& a, bool* bad = nullptr) {
-    int64_t u = 0;
-    for (int b = threadIdx.x & 31; b < a.B; b += 32) u += PL::head_units(a, seq_len(a, b, bad));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
-    return u * a.Hkv;
-}
+// The line of U units cut into G CTAs: CTA c has the units [begin(c), begin(c + 1)), begin(c) =
+// floor(c U / G).
+struct Cut {
+    int q, r, G;
+    __device__ __forceinline__ Cut(int U, int ncta) : q(U / ncta), r(U - U / ncta * ncta), G(ncta) {}
+    __device__ __forceinline__ int begin(int c) const { return c * q + (int)((uint32_t)(c * r) / (uint32_t)G); }
+    // the last CTA whose begin is <= s: a guess in float32 (off by one at most), corrected
+    __device__ __forceinline__ int owner(int s) const {
+        int c = min((int)((float)s * (float)G / ((float)q * (float)G + (float)r)), G - 1);
+        while (c > 0 && begin(c) > s) --c;
+        while (c + 1 < G && begin(c + 1) <= s) ++c;
+        return c;
+    }
+};
 
-// A CTA's share of an item: tiles [t0, t1) of nt.
+// A CTA's share of an item: tiles [t0, t1).
 struct Segment {
     int b, h, m, rows, weight;
     SeqLen s;
-    int end, t0, t1, nt;
-    bool whole;  // the item has no other share
-    int slot;    // where its partial goes: 0 when an earlier CTA began the item, else 1
+    int end, t0, t1;
+    int whole;  // the item has no other share
+    int slot;   // where its partial goes: 0 when an earlier CTA began the item, else 1
 };
 
-// Walks a CTA's segments. Every lane of a warp holds the same state (init is collective).
+// Walks a CTA's segments; used by a whole warp, every lane holding the same state.
 template <typename PL>
 struct SegmentWalk {
-    int64_t u0, u1, pos;  // the CTA's units; first unit of the current item
+    int u0, u1, pos;  // the CTA's units; first unit of the current item
     int b, h, m;
     SeqLen s;
-    bool done;
 
     __device__ __forceinline__ void init(const PlanArgs& a, int cta, int ncta, bool* bad = nullptr) {
         const int lane = threadIdx.x & 31;
-        const int64_t U = plan_total<PL>(a, bad);
-        u0 = PL::begin(cta, U, ncta);
-        u1 = PL::begin(cta + 1, U, ncta);
-        done = u0 >= u1;
-        b = h = m = 0;
-        pos = 0;
+        // units of all sequences; the first 32 sequences' stay in registers
+        const SeqLen s0 = lane < a.B ? seq_len(a, lane, bad) : SeqLen{0, 0};
+        const int w0 = PL::head_units(a, s0);
+        int U = w0;
+#pragma unroll 1
+        for (int bb = lane + 32; bb < a.B; bb += 32) U += PL::head_units(a, seq_len(a, bb, bad));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
+        const Cut cut(U * a.Hkv, ncta);
+        u0 = cut.begin(cta);
+        u1 = cut.begin(cta + 1);
+        b = h = m = pos = 0;
         s = SeqLen{0, 0};
-        if (done) return;
-        // the sequence that holds unit u0: the last whose first unit is <= u0 (and has units)
-        int64_t base = 0;
+        if (u0 >= u1) {
+            b = a.B;
+            return;
+        }
+        // the sequence that holds unit u0: the first whose units end past it
+        int base = 0;
+#pragma unroll 1
         for (int b0 = 0; b0 < a.B; b0 += 32) {
-            const int bb = b0 + lane;
-            const SeqLen sl = bb < a.B ? seq_len(a, bb) : SeqLen{0, 0};
-            const int64_t hu = PL::head_units(a, sl), w = hu * a.Hkv;
-            int64_t inc = w;
+            SeqLen sl = s0;
+            int hu = w0;
+            if (b0) {
+                sl = b0 + lane < a.B ? seq_len(a, b0 + lane) : SeqLen{0, 0};
+                hu = PL::head_units(a, sl);
+            }
+            int inc = hu * a.Hkv;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+                const int v = __shfl_up_sync(0xffffffffu, inc, o);
                 if (lane >= o) inc += v;
             }
             const unsigned hit = __ballot_sync(0xffffffffu, base + inc > u0);
@@ -132,31 +150,23 @@ struct SegmentWalk {
                 b = b0 + l;
                 s.P = __shfl_sync(0xffffffffu, sl.P, l);
                 s.n = __shfl_sync(0xffffffffu, sl.n, l);
-                const int64_t head = __shfl_sync(0xffffffffu, hu, l);
-                pos = base + __shfl_sync(0xffffffffu, inc - w, l);
-                h = (int)((u0 - pos) / head);
+                const int head = __shfl_sync(0xffffffffu, hu, l);
+                pos = base + __shfl_sync(0xffffffffu, inc, l) - head * a.Hkv;
+                h = (u0 - pos) / head;
                 pos += h * head;
                 break;
             }
             base += __shfl_sync(0xffffffffu, inc, 31);
         }
-        m = 0;
-        while (true) {  // the block that holds u0
-            const int64_t w = units(a);
-            if (pos + w > u0) break;
-            pos += w;
-            ++m;
-        }
     }
-    __device__ __forceinline__ int64_t units(const PlanArgs& a) const {
-        return (int64_t)PL::tiles(a, s, m) * PL::weight(s.n * a.G, m);
-    }
-    // The next segment with at least one tile; false at the end.
+    // The next segment with at least one tile; false at the end. (The first call also skips the
+    // blocks of the item's head that lie before u0.)
     __device__ __forceinline__ bool next(const PlanArgs& a, Segment& g) {
-        while (!done) {
+#pragma unroll 1
+        while (b < a.B && pos < u1) {
             const int rows = s.n * a.G;
             bool got = false;
-            if (PL::blocks(rows) > 0) {
+            if (rows > 0) {
                 const int w = PL::weight(rows, m), nt = PL::tiles(a, s, m);
                 g.t0 = PL::first_tile(pos, w, nt, u0);
                 g.t1 = PL::first_tile(pos, w, nt, u1);
@@ -168,12 +178,11 @@ struct SegmentWalk {
                     g.rows = rows;
                     g.weight = w;
                     g.s = s;
-                    g.nt = nt;
                     g.end = PL::end(a, s, m);
                     g.whole = g.t0 == 0 && g.t1 == nt;
                     g.slot = g.t0 == 0 ? 1 : 0;
                 }
-                pos += (int64_t)nt * w;
+                pos += nt * w;
             }
             if (++m >= PL::blocks(rows)) {
                 m = 0;
@@ -182,7 +191,6 @@ struct SegmentWalk {
                     if (++b < a.B) s = seq_len(a, b);
                 }
             }
-            if (b >= a.B || pos >= u1) done = true;
             if (got) return true;
         }
         return false;

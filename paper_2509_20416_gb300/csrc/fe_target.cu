@@ -145,7 +145,7 @@ bool pages_ok(const fe_target* t, const fe_pages& p) { return t->cfg.page_size =
 
 bool shape_ok(const fe_target* t, int B, int T) {
     return B >= 1 && B <= t->cfg.max_batch && T >= 1 && T <= t->cfg.max_seq &&
-           (int64_t)B * T * (t->cfg.n_heads + t->cfg.n_kv_heads) <= 0x7FFFFFFF;
+           (int64_t)B * T * (t->cfg.n_heads + t->cfg.n_kv_heads) <= 1 << 30;
 }
 
 CacheView cache_view(const fe_target* t, const fe_kv& kv, const fe_pages& p) {
@@ -299,7 +299,7 @@ fe_status fe_cache_read(fe_target* t, const fe_cache_read_args* a, void* stream)
 
 fe_status fe_tree_attention(fe_target* t, const fe_tree_attention_args* a, void* stream) {
     if (!t || !a || !a->q.p || !a->out.p || !a->prefix_len || !shape_ok(t, a->B, a->T)) return FE_ERR_INVALID_ARG;
-    if (!kv_ok(t, a->cache) || !pages_ok(t, a->pages) || !isfinite(a->scale) || a->scale < 0.f)
+    if (!kv_ok(t, a->cache) || !pages_ok(t, a->pages) || !isfinite(a->scale) || a->scale <= 0.f)
         return FE_ERR_INVALID_ARG;
     const fe_status dv = check_device(t);
     if (dv != FE_OK) return dv;
@@ -324,6 +324,7 @@ fe_status fe_tree_attention(fe_target* t, const fe_tree_attention_args* a, void*
     r.status = t->status;
     r.q_vec = rows_16(a->q, es);
     r.out_vec = rows_16(a->out, es);
+    if (!tree_attn_fits(r, c.dtype)) return FE_ERR_UNSUPPORTED;
     FE_TRY(launch_tree_attn(r, c.dtype, c.cache_dtype, c.head_dim, t->num_sms, (cudaStream_t)stream));
     return FE_OK;
 }

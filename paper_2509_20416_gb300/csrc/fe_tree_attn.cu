@@ -14,15 +14,16 @@ namespace {
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
 template <typename QT, int HD, typename PL, int ROWS>
-__global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const TreeAttnArgs a, int ncta) {
+__global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a, int ncta) {
     const PlanArgs pa = plan_args(a);
     const int lane = threadIdx.x & 31;
     const int b = blockIdx.y;
     // schedule: total units, and the first unit of this sequence (lengths are the caller's and
     // do not depend on the attention kernel, so this runs before the wait)
-    int64_t U = 0, before = 0;
+    int U = 0, before = 0;
+#pragma unroll 1
     for (int bb = lane; bb < a.B; bb += 32) {
-        const int64_t u = PL::head_units(pa, seq_len(pa, bb)) * a.Hkv;
+        const int u = PL::head_units(pa, seq_len(pa, bb)) * a.Hkv;
         U += u;
         if (bb < b) before += u;
     }
@@ -33,7 +34,8 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const Tree
     }
     const SeqLen s = seq_len(pa, b);
     const int rows = s.n * a.G;
-    const int64_t head_units = PL::head_units(pa, s);
+    const int head_units = PL::head_units(pa, s);
+    const Cut cut(U, ncta);
     griddep_wait();
     for (int x = blockIdx.x * kJoinWarps + threadIdx.x / 32; x < a.T * a.H; x += gridDim.x * kJoinWarps) {
         const int node = x / a.H, head = x % a.H, h = head / a.G;
@@ -44,16 +46,17 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const Tree
         float mx = -INFINITY, sum = 0.f;
         if (node < s.n) {
             const int m = r / ROWS, w = PL::weight(rows, m), nt = PL::tiles(pa, s, m);
-            int64_t s0 = before + h * head_units;
+            int s0 = before + h * head_units;
             if (pa.causal) {
-                for (int k = 0; k < m; ++k) s0 += (int64_t)PL::tiles(pa, s, k) * PL::weight(rows, k);
+#pragma unroll 1
+                for (int k = 0; k < m; ++k) s0 += PL::tiles(pa, s, k) * PL::weight(rows, k);
             } else {
-                s0 += (int64_t)m * nt * PL::weight(ROWS, 0);
+                s0 += m * nt * PL::weight(ROWS, 0);
             }
-            const int c0 = PL::owner(s0, U, ncta), c1 = PL::owner(s0 + (int64_t)(nt - 1) * w, U, ncta);
+            const int c0 = cut.owner(s0), c1 = cut.owner(s0 + (nt - 1) * w);
             if (c0 == c1) continue;
             for (int c = c0; c <= c1; ++c) {
-                const int64_t u0 = PL::begin(c, U, ncta), u1 = PL::begin(c + 1, U, ncta);
+                const int u0 = cut.begin(c), u1 = cut.begin(c + 1);
                 const int t0 = PL::first_tile(s0, w, nt, u0);
                 if (t0 >= PL::first_tile(s0, w, nt, u1)) continue;  // no tile starts in this CTA's units
                 const int64_t pr = ((int64_t)c * 2 + (t0 == 0 ? 1 : 0)) * kAttnItemRows + (r - m * ROWS);
@@ -140,6 +143,12 @@ cudaError_t launch_hd(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtyp
 cudaError_t tree_attn_prepare() {
     const cudaError_t e = prepare<64>();
     return e != cudaSuccess ? e : prepare<128>();
+}
+
+bool tree_attn_fits(const TreeAttnArgs& a, fe_dtype dtype) {
+    const int64_t rows = (int64_t)a.T * a.G;
+    return dtype == FE_F32 ? SimtPlan::fits(a.B, a.Hkv, rows, a.cache.max_seq)
+                           : TcPlan::fits(a.B, a.Hkv, rows, a.cache.max_seq);
 }
 
 cudaError_t launch_tree_attn(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int hd, int num_sms,

@@ -23,7 +23,7 @@ struct SimtSmem {
 };
 
 template <int HD>
-__global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const TreeAttnArgs a) {
+__global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __grid_constant__ TreeAttnArgs a) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SimtSmem<HD>& sm = *reinterpret_cast<SimtSmem<HD>*>(smem_raw);
     const int t = threadIdx.x, tx = t & 15, ty = t >> 4;

@@ -43,15 +43,23 @@ template <int HD, bool Q8, int MT>
 struct TcShape {
     static constexpr int kTileBytes = kTcTile * HD * 2;  // also a query block's
     static constexpr int kRawBytes = kTcTile * HD;
-    static constexpr int kSlots = Q8 ? 4 : 7 - MT;           // tiles in flight
-    static constexpr int kRawSlots = Q8 ? (MT == 1 ? 4 : 2) : 0;
-    static constexpr int kThreads = Q8 ? 448 : 416;
-    static constexpr int kData = MT * kTileBytes + kSlots * kTileBytes + kRawSlots * kRawBytes;
+    static constexpr int kSlots = !Q8 && MT == 1 ? 5 : 4;  // tiles in flight
+    static constexpr int kRawSlots = Q8 ? (MT == 1 ? 3 : 2) : 0;
+    // the epilogue's staging, 2 KB a warp: its own where there is room, else the queries' buffer,
+    // whose next load then waits for the epilogue
+    static constexpr bool kStageInQ = Q8 && MT == 2 && HD == 128;
+    static constexpr int kStageBytes = kStageInQ ? 0 : 8 * 2048;
+    static constexpr int kThreads = Q8 ? 512 : 480;
+    static constexpr int kReaders = Q8 ? 15 : 14;  // warps that read the segments
+    static constexpr int kData = MT * kTileBytes + kSlots * kTileBytes + kRawSlots * kRawBytes + kStageBytes;
 };
 
+constexpr int kTcSegs = 4;  // segments planned ahead
+
 struct TcState {
-    uint64_t full[6], empty[6], rawfull[4], rawempty[4], qfull, qempty, sfull[2], pfull[2], odone, ofree, mlfull, mlfree,
-        drain;
+    uint64_t full[6], empty[6], rawfull[4], rawempty[4], segfull[kTcSegs], segempty[kTcSegs], qfull, qempty, sfull[2],
+        pfull[2], odone, ofree, mlfull, mlfree, drain[2];
+    Segment seg[kTcSegs];  // weight 0: no more
     uint32_t tmem;
     int abort;
     int odd[8];        // by segment: non-finite value elements were set aside
@@ -59,15 +67,19 @@ struct TcState {
 };
 
 template <int HD, bool Q8, int MT>
-constexpr int tc_smem() { return 1024 + TcShape<HD, Q8, MT>::kData + (int)sizeof(TcState); }
+constexpr int tc_smem() {
+    constexpr int bytes = 1024 + TcShape<HD, Q8, MT>::kData + (int)sizeof(TcState);
+    static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
+    return bytes;
+}
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// one arrival on `bar` once all cp.async of this thread so far are complete
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -97,8 +109,13 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// A bounded wait (mbar_wait_abortable) whose slow part is one call, not a copy at every place.
+__device__ __noinline__ bool tc_wait_slow(uint64_t* bar, uint32_t parity, int* status, int* abort) {
+    return mbar_wait_abortable(bar, parity, status, abort);
+}
+
 // The slots of [s0, s0 + 32) that node `node` sees, as bits.
-__device__ __forceinline__ uint32_t seen_bits(const TreeAttnArgs& a, const Segment& g, int node, int s0) {
+__device__ __noinline__ uint32_t seen_bits(const TreeAttnArgs& a, const Segment& g, int node, int s0) {
     const int P = g.s.P;
     auto ones = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
     if (!a.mask) return ones(min(P + node + 1, g.end) - s0);
@@ -148,7 +165,7 @@ __device__ __forceinline__ void load_q(const TreeAttnArgs& a, const Segment& g, 
         src = (const bf16_t*)a.q.p + g.b * a.q.batch + (int64_t)(r0 / a.G) * a.q.token +
               (int64_t)(g.h * a.G + r0 % a.G) * a.q.head;
     const int c = lane % CH;
-#pragma unroll 4
+#pragma unroll 1
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = i * RP + lane / CH;
         const bf16_t* p = (const bf16_t*)__shfl_sync(0xffffffffu, (unsigned long long)src, r);
@@ -170,12 +187,13 @@ template <int HD>
 __device__ __forceinline__ void load_tile(const void* base, const RowInfo& x, unsigned char* dst, int w, int lane) {
     constexpr int CH = HD / 8, RP = 32 / CH;
     const int c = lane % CH;
-#pragma unroll
+    const unsigned long long mine = x.row < 0 ? 0ull : (unsigned long long)base + (unsigned long long)x.row * (HD * 2);
+    const uint32_t d = smem_u32(dst) + (c >> 3) * 16384 + w * 4096;
+#pragma unroll 4
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = i * RP + lane / CH;
-        const int64_t row = __shfl_sync(0xffffffffu, x.row, r);
-        const char* src = (const char*)base + ((row < 0 ? 0 : row) * HD + c * 8) * 2;
-        cp_async16(smem_u32(dst + (c >> 3) * 16384 + sw128_offset(w * 32 + r, c & 7)), src, row >= 0);
+        const unsigned long long src = __shfl_sync(0xffffffffu, mine, r);
+        cp_async16(d + sw128_offset(r, c & 7), (const void*)((src ? src : (unsigned long long)base) + c * 16), src != 0);
     }
 }
 
@@ -185,7 +203,7 @@ __device__ __forceinline__ bool scrub_tile(unsigned char* tile, int first, int w
     constexpr int CH = HD / 8, RP = 32 / CH;
     const int c = lane % CH;
     bool odd = false;
-#pragma unroll 4
+#pragma unroll 1
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = w * 32 + i * RP + lane / CH;
         if (r < first) continue;
@@ -205,96 +223,236 @@ __device__ __forceinline__ bool scrub_tile(unsigned char* tile, int first, int w
     return odd;
 }
 
-// One tile of e4m3 rows, converted: raw [128][HD] bytes to bf16 values number * scale (exact for
-// power-of-two scales). Rows without a cache row become zero; in rows from `first` on, so do
-// non-finite elements (returns whether there were any).
+// Four e4m3 numbers to bfloat16, times 2^-120: their 7 magnitude bits are moved to where
+// bfloat16 keeps the low 4 exponent and high 3 fraction bits (subnormals to subnormals). Exact;
+// the NaN codes come out as 480 and are looked for by the caller.
+__device__ __forceinline__ void e4m3x4_to_bf16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    const uint32_t a = __byte_perm(w, 0, 0x1404), b = __byte_perm(w, 0, 0x3424);
+    lo = ((a >> 4) & 0x07F007F0u) | (a & 0x80008000u);
+    hi = ((b >> 4) & 0x07F007F0u) | (b & 0x80008000u);
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// What a row's numbers (times 2^-120) are multiplied by, as packed bfloat16: its scale 2^c times
+// 2^120, in two factors (the second is 1 up to c = 7), so that neither overflows.
+__device__ __forceinline__ uint2 scale_factors(float scale) {
+    const int e = (int)(__float_as_uint(scale) >> 23) - 127 + 120, e1 = min(max(e, 0), 127), e2 = min(e - e1, 127);
+    const uint32_t f1 = (uint32_t)(e1 + 127) << 7, f2 = (uint32_t)(max(e2, 0) + 127) << 7;
+    return make_uint2(f1 | f1 << 16, f2 | f2 << 16);
+}
+
+// One tile of e4m3 rows, converted: raw [128][HD] bytes to the bfloat16 values they stand for
+// (number * scale, exact). Rows without a cache row become zero; in rows from `first` on, so do
+// NaN elements (returns whether there were any).
 template <int HD>
-__device__ __forceinline__ bool convert_tile(const unsigned char* raw, int64_t row_of_lane, float scale_of_lane, int first,
+__device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_row, float scale, int first,
                                              unsigned char* dst, int w, int lane) {
     constexpr int CH = HD / 16, RP = 32 / CH;
     const int c = lane % CH;
+    const uint2 mine = has_row ? scale_factors(scale) : make_uint2(0, 0);
     bool odd = false;
-#pragma unroll 4
+    // lanes of a row's second 64 columns store their two chunks in the other order, so that eight
+    // lanes store into different banks
+    unsigned char* base = dst + (c >> 2) * 16384 + w * 4096;
+    const int swap = c >> 2, c0 = 2 * (c & 3) + swap, c1 = 2 * (c & 3) + 1 - swap;
+#pragma unroll 2
     for (int i = 0; i < 32 / RP; ++i) {
-        const int rr = i * RP + lane / CH, r = w * 32 + rr;
-        const bool valid = __shfl_sync(0xffffffffu, row_of_lane, rr) >= 0;
-        const float s = __shfl_sync(0xffffffffu, scale_of_lane, rr);
-        uint4 u = *reinterpret_cast<const uint4*>(raw + r * HD + c * 16);
-        if (!valid) u = make_uint4(0, 0, 0, 0);
+        const int r = i * RP + lane / CH;
+        const uint32_t f1 = __shfl_sync(0xffffffffu, mine.x, r), f2 = __shfl_sync(0xffffffffu, mine.y, r);
+        uint4 u = *reinterpret_cast<const uint4*>(raw + (w * 32 + r) * HD + c * 16);
+        if (f1 == 0) u = make_uint4(0, 0, 0, 0);
         const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-        uint32_t o[8];
+        uint32_t o[8], nan = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float2 f = e4m3x2_to_f32(in[e / 2] >> (16 * (e & 1)));
-            o[e] = pack_bf16(f.x * s, f.y * s);
+        for (int e = 0; e < 4; ++e) {
+            nan |= (in[e] & 0x7F7F7F7Fu) + 0x01010101u;
+            e4m3x4_to_bf16(in[e], o[2 * e], o[2 * e + 1]);
         }
-        if (!valid) {  // (0 times a stale scale may be NaN)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = 0;
-        } else if (r >= first) {
+        for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], f1);
+        if (f2 != 0x3F803F80u && f1 != 0) {  // a scale above 2^7
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if ((o[e] & 0x7F80u) == 0x7F80u) { o[e] &= 0xffff0000u; odd = true; }
-                if ((o[e] & 0x7F800000u) == 0x7F800000u) { o[e] &= 0x0000ffffu; odd = true; }
-            }
+            for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], f2);
         }
-        // two 16-byte chunks; lanes of the upper half of a 128-byte-row pair go in the other order,
-        // so that eight lanes store into different banks
-        unsigned char* base = dst + (c >> 2) * 16384;
-        const int c0 = 2 * (c & 3);
+        if (nan & 0x80808080u) {
+            const bool node = w * 32 + r >= first;
+            odd |= node;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if ((in[e / 4] >> (8 * (e & 3)) & 0x7Fu) == 0x7Fu) {
+                    const uint32_t m = e & 1 ? 0xFFFF0000u : 0x0000FFFFu;
+                    o[e / 2] = (o[e / 2] & ~m) | (node ? 0u : 0x7FC07FC0u & m);
+                }
+        }
         const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
-        const bool swap = (c >> 2) != 0;
-        *reinterpret_cast<uint4*>(base + sw128_offset(r, swap ? c0 + 1 : c0)) = swap ? hi : lo;
-        *reinterpret_cast<uint4*>(base + sw128_offset(r, swap ? c0 : c0 + 1)) = swap ? lo : hi;
+        *reinterpret_cast<uint4*>(base + sw128_offset(r, c0)) = swap ? hi : lo;
+        *reinterpret_cast<uint4*>(base + sw128_offset(r, c1)) = swap ? lo : hi;
     }
     return odd;
+}
+
+// 16 TMEM columns, not waited for; then the wait, which the values pass through
+__device__ __forceinline__ void tc_ld16_start(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tc_ld16_wait(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
+
+// packed pairs of floats: d = a * b + c and a + b, elementwise
+__device__ __forceinline__ uint64_t pair_f32(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+__device__ __forceinline__ uint64_t fma_x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+// A row of 128 scores x at TMEM columns ts: 2^(scale2 x + shift) as packed bfloat16 in pk, their
+// float32 sum in z; returns the largest x. The next 16 columns load while 16 are worked on.
+__device__ __forceinline__ float softmax_row(uint32_t ts, float scale2, float shift, uint32_t (&pk)[kTcTile / 2], float& z) {
+    const uint64_t sc = pair_f32(__float_as_uint(scale2), __float_as_uint(scale2));
+    const uint64_t sh = pair_f32(__float_as_uint(shift), __float_as_uint(shift));
+    uint32_t x[2][16];
+    uint64_t z2[2] = {0, 0};
+    float mx = -INFINITY;
+    tc_ld16_start(ts, x[0]);
+#pragma unroll
+    for (int c = 0; c < kTcTile / 16; ++c) {
+        uint32_t* v = x[c & 1];
+        tc_ld16_wait(v);
+        if (c + 1 < kTcTile / 16) tc_ld16_start(ts + 16 * (c + 1), x[(c + 1) & 1]);
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            mx = fmaxf(mx, fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
+            const uint64_t y = fma_x2(pair_f32(v[e], v[e + 1]), sc, sh);
+            const float p0 = ex2_approx(__uint_as_float((uint32_t)y)), p1 = ex2_approx(__uint_as_float((uint32_t)(y >> 32)));
+            z2[(e >> 1) & 1] = add_x2(z2[(e >> 1) & 1], pair_f32(__float_as_uint(p0), __float_as_uint(p1)));
+            pk[8 * c + e / 2] = pack_bf16(p0, p1);
+        }
+    }
+    const uint64_t zz = add_x2(z2[0], z2[1]);
+    z = __uint_as_float((uint32_t)zz) + __uint_as_float((uint32_t)(zz >> 32));
+    return mx;
 }
 
 // Ring positions of a segment's tiles. They are loaded in the order of their first use:
 // K0 K1 V0 K2 V1 ... K(n-1) V(n-2) V(n-1).
 __device__ __forceinline__ int pos_k(int t) { return t == 0 ? 0 : 2 * t - 1; }
 __device__ __forceinline__ int pos_v(int t, int n) { return t < n - 1 ? 2 * t + 2 : 2 * n - 1; }
+__device__ __forceinline__ bool tile_is_value(int l, int n) { return l == 2 * n - 1 || (l > 0 && !(l & 1)); }
+__device__ __forceinline__ int tile_number(int l, int n) {
+    return l == 0 ? 0 : l == 2 * n - 1 ? n - 1 : l & 1 ? (l + 1) / 2 : (l - 2) / 2;
+}
+
+// For a row that sees non-finite value elements (which the loaders set to zero): the result in
+// their columns is the sum of p times them alone, since what is finite does not change an infinity
+// or NaN. dst: the row's place in the output (bfloat16) or the partial results (float32).
+template <int HD, bool Q8>
+__device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segment& g, int node, int head, float m, void* dst) {
+    const bf16_t* q = (const bf16_t*)a.q.p + g.b * a.q.batch + (int64_t)node * a.q.token + (int64_t)head * a.q.head;
+#pragma unroll 1
+    for (int e = 0; e < HD; ++e) {
+        float t = 0.f;
+        bool any = false;
+#pragma unroll 1
+        for (int s = max(g.s.P, g.t0 * kTcTile); s < min(g.end, g.t1 * kTcTile); ++s) {
+            const RowInfo x = row_info<Q8>(a, g, s / kTcTile, s % kTcTile);
+            if (x.row < 0) continue;
+            auto at = [&](const void* p, float sc, int k) {
+                if (Q8) return e4m3x2_to_f32(((const uint8_t*)p)[x.row * HD + k]).x * sc;
+                return Storage<bf16_t>::load((const bf16_t*)p, x.row * HD + k);
+            };
+            const float v = at(a.cache.v, x.vs, e);
+            if (finite_f32(v) || !(seen_bits(a, g, node, s) & 1u)) continue;
+            float dot = 0.f;
+#pragma unroll 1
+            for (int k = 0; k < HD; ++k) dot = fmaf(Storage<bf16_t>::load(q, k), at(a.cache.k, x.ks, k), dot);
+            t += exp2f(dot * (a.scale * kLog2e) - (m == -INFINITY ? 0.f : m)) * v;
+            any = true;
+        }
+        if (!any) continue;
+        if (g.whole) store_one((bf16_t*)dst + e, t);
+        else ((float*)dst)[e] = t;
+    }
+}
+
+// A position in the ring of tiles: slot and phase, moved on by small steps without division.
+template <int S>
+struct RingPos {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void skip(int d) {
+        slot += d;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)  // (d <= 2 S)
+            if (slot >= S) {
+                slot -= S;
+                phase ^= 1u;
+            }
+    }
+    __device__ __forceinline__ void skip_long(int d) {
+        phase ^= (uint32_t)((slot + d) / S) & 1u;
+        slot = (slot + d) % S;
+    }
+};
 
 // ---- the kernel -----------------------------------------------------------------------------------
 template <int HD, bool Q8, int MT>
-__global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1) tree_attn_tc_kernel(const TreeAttnArgs a) {
+__global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
+    tree_attn_tc_kernel(const __grid_constant__ TreeAttnArgs a) {
     using SH = TcShape<HD, Q8, MT>;
     constexpr int S = SH::kSlots, RS = Q8 ? SH::kRawSlots : 1, TB = SH::kTileBytes;
     extern __shared__ unsigned char dsm_raw[];
     unsigned char* qbuf = (unsigned char*)(((uintptr_t)dsm_raw + 1023) & ~(uintptr_t)1023);
     unsigned char* ring = qbuf + MT * TB;
     unsigned char* rawring = ring + S * TB;
+    unsigned char* stages = SH::kStageInQ ? qbuf : rawring + SH::kRawSlots * SH::kRawBytes;
     TcState& st = *reinterpret_cast<TcState*>(qbuf + SH::kData);
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-    const PlanArgs pa = plan_args(a);
     griddep_launch_dependents();
-
-    bool bad = false;
-    SegmentWalk<TcPlan> walk;
-    walk.init(pa, blockIdx.x, gridDim.x, &bad);
-    if (bad && blockIdx.x == 0 && warp == 0) atomicOr(a.status, ST_CAPACITY);
-    if (walk.done) return;  // (the same in every warp)
 
     if (t == 0) {
         for (int i = 0; i < S; ++i) {
             mbar_init(&st.full[i], 128);
-            mbar_init(&st.empty[i], 1);
+            mbar_init(&st.empty[i], MT);  // (a tile that one stream alone used is released twice by it)
         }
         for (int i = 0; i < RS; ++i) {
             mbar_init(&st.rawfull[i], 1);
             mbar_init(&st.rawempty[i], 128);
         }
+        for (int i = 0; i < kTcSegs; ++i) {
+            mbar_init(&st.segfull[i], 1);
+            mbar_init(&st.segempty[i], SH::kReaders);
+        }
         mbar_init(&st.qfull, 128);
-        mbar_init(&st.qempty, 1);
+        mbar_init(&st.qempty, SH::kStageInQ ? 10 : 2);  // both streams' score products (and epilogues)
         for (int i = 0; i < 2; ++i) {
             mbar_init(&st.sfull[i], 1);
             mbar_init(&st.pfull[i], 4);
+            mbar_init(&st.drain[i], 1);
         }
-        mbar_init(&st.odone, 1);
+        mbar_init(&st.odone, 2);
         mbar_init(&st.ofree, 8);
         mbar_init(&st.mlfull, 4);
         mbar_init(&st.mlfree, 4);
-        mbar_init(&st.drain, 1);
         st.abort = 0;
         for (int i = 0; i < 8; ++i) st.odd[i] = 0;
         mbar_fence_init();
@@ -304,165 +462,186 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1) tree_attn_tc
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = st.tmem;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_abortable(bar, parity & 1u, a.status, &st.abort); };
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+        return mbar_try_wait(bar, parity & 1u) || tc_wait_slow(bar, parity & 1u, a.status, &st.abort);
+    };
+    // the next planned segment; false at the end (or after a failed wait)
+    uint32_t seg = 0;  // segments taken
+    auto next = [&](Segment& g) -> bool {
+        const int k = seg % kTcSegs;
+        if (!wait(&st.segfull[k], seg / kTcSegs)) return false;
+        g = st.seg[k];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&st.segempty[k]);
+        ++seg;
+        return g.weight != 0;
+    };
     Segment g;
+    bool ok = true;
 
     if (warp >= 8 && warp < 12) {  // ---- loaders
         const int w = warp - 8;
-        uint32_t i = 0, sig = 0;  // tiles issued, tiles announced
-        uint32_t qpos = 0xffffffffu;  // the tile whose group also brings the queries
-        uint32_t seg = 0;
-        bool ok = true;
-        // announce tiles up to (not including) `upto`, whose copies are complete
-        auto announce = [&](uint32_t upto) {
-            if (sig == upto) return;
-            fence_async_proxy();
-            for (; sig != upto; ++sig) {
-                if (sig == qpos) mbar_arrive(&st.qfull);
-                mbar_arrive(&st.full[sig % S]);
-            }
-        };
-        auto slot_free = [&]() -> bool {
-            if (i < (uint32_t)S) return true;
-            uint64_t* e = &st.empty[i % S];
-            const uint32_t par = (i / S - 1) & 1u;
-            if (!Q8 && !mbar_try_wait(e, par)) {
-                // everything is in flight or in use: announce what is here before blocking
-                cp_async_wait<0>();
-                announce(i);
-            }
-            return wait(e, par);
-        };
-        while (ok && walk.next(pa, g)) {
-            if (seg > 0) {  // the queries' buffer is free once the last segment's scores are done
-                if (!mbar_try_wait(&st.qempty, (seg - 1) & 1u)) {
-                    cp_async_wait<0>();
-                    announce(i);
-                }
-                if (!(ok = wait(&st.qempty, seg - 1))) break;
-            }
+        RingPos<S> pos;
+        RingPos<RS> rpos;
+        bool reuse = false;  // the ring has been filled once
+        while (ok && next(g)) {
+            // the queries' buffer is free once the last segment's scores (and epilogue) are done
+            if (seg > 1 && !(ok = wait(&st.qempty, seg - 2))) break;
             const int nt = g.t1 - g.t0;
-            RowInfo x0 = row_info<Q8>(a, g, g.t0, w * 32 + lane), x1 = row_info<Q8>(a, g, g.t0 + 1, w * 32 + lane), x2 = x1;
+            // what the lane knows of its rows in tiles t, t + 1, t + 2 (addresses and scales are
+            // fetched a tile ahead of their use)
+            RowInfo x0 = row_info<Q8>(a, g, g.t0, w * 32 + lane), x1 = x0, x2 = x0;
             for (int b = 0; b < g.weight; ++b) load_q<HD>(a, g, b, qbuf + b * TB, w, lane);
-            qpos = i;
-            // key or value tile tt (from this segment's first) of the rows in x
-            auto load = [&](bool val, int tt, const RowInfo& x) {
-                unsigned char* dst = ring + (i % S) * TB;
+            if (a.q_vec) {
+                cp_async_arrive(&st.qfull);
+            } else {
+                fence_async_proxy();
+                mbar_arrive(&st.qfull);
+            }
+#pragma unroll 1
+            for (int l = 0; l < 2 * nt; ++l) {  // K0 K1 V0 K2 V1 ...
+                const bool val = tile_is_value(l, nt);
+                const int tt = tile_number(l, nt);
+                if (!val) {
+                    x0 = x1;
+                    x1 = l == 0 ? x0 : x2;
+                    x2 = row_info<Q8>(a, g, g.t0 + tt + 1, w * 32 + lane);
+                }
+                // (a key tile tt is loaded with x1's rows; the value tile loaded after it is tt - 1,
+                // the last one tt)
+                const RowInfo& x = !val || tt == nt - 1 ? x1 : x0;
+                unsigned char* dst = ring + pos.slot * TB;
+                uint64_t* full = &st.full[pos.slot];
                 const int first = g.s.P - (g.t0 + tt) * kTcTile;  // first row of the tile that is a node's
                 if constexpr (Q8) {
-                    const uint32_t rs = i % RS;
-                    if (i == qpos) {  // (the queries' copies)
-                        cp_async_commit();
-                        cp_async_wait<0>();
-                    }
-                    if (!(ok = wait(&st.rawfull[rs], i / RS)) || !(ok = slot_free())) return;
-                    const bool odd = convert_tile<HD>(rawring + rs * SH::kRawBytes, x.row, val ? x.vs : x.ks,
+                    if (!(ok = wait(&st.rawfull[rpos.slot], rpos.phase))) break;
+                }
+                if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
+                if constexpr (Q8) {
+                    const bool odd = convert_tile<HD>(rawring + rpos.slot * SH::kRawBytes, x.row >= 0, val ? x.vs : x.ks,
                                                       val ? first : kTcTile, dst, w, lane);
-                    if (odd) st.odd[seg & 7] = 1;
-                    mbar_arrive(&st.rawempty[rs]);
-                    ++i;
-                    announce(i);
+                    if (odd) st.odd[(seg - 1) & 7] = 1;
+                    fence_async_proxy();
+                    mbar_arrive(&st.rawempty[rpos.slot]);
+                    mbar_arrive(full);
+                    rpos.skip(1);
                 } else {
-                    if (!(ok = slot_free())) return;
                     load_tile<HD>(val ? a.cache.v : a.cache.k, x, dst, w, lane);
-                    cp_async_commit();
-                    ++i;
                     if (val && first < kTcTile) {
-                        cp_async_wait<0>();
-                        if (scrub_tile<HD>(dst, first, w, lane)) st.odd[seg & 7] = 1;
-                        announce(i);
+                        cp_async_wait_all();
+                        if (scrub_tile<HD>(dst, first, w, lane)) st.odd[(seg - 1) & 7] = 1;
+                        fence_async_proxy();
+                        mbar_arrive(full);
                     } else {
-                        cp_async_wait<2>();
-                        if (i - sig > 2) announce(i - 2);
+                        // (the copies' writes are ordered before the MMA's reads by the MMA thread's
+                        // proxy fence: a fence here would wait for the copies)
+                        cp_async_arrive(full);
                     }
                 }
-            };
-            load(false, 0, x0);
-            for (int tt = 0; tt < nt && ok; ++tt) {
-                if (tt + 1 < nt) {
-                    x2 = row_info<Q8>(a, g, g.t0 + tt + 2, w * 32 + lane);
-                    load(false, tt + 1, x1);
-                    if (!ok) break;
-                }
-                load(true, tt, x0);
-                x0 = x1;
-                x1 = x2;
+                pos.skip(1);
+                reuse |= pos.slot == 0;
             }
-            ++seg;
         }
-        cp_async_wait<0>();
-        if (ok) announce(i);
-    } else if (warp == 12) {  // ---- MMA issuer
+        cp_async_wait_all();
+    } else if (warp == 12 || warp == 13) {  // ---- MMA issuers, one thread per stream
+        const int gs = warp - 12;
         const uint32_t id_qk = idesc_bf16_f32(128, kTcTile);
         const uint32_t id_pv = idesc_bf16_f32(128, HD) | (1u << 16);  // B is MN-major
-        uint32_t base = 0, seg = 0, np[2] = {0, 0};
-        bool ok = true;
-        while (walk.next(pa, g)) {
+        const uint32_t ts = tmem + gs * 128, to = tmem + 256 + gs * 128;
+        const uint64_t ring_d = sw128_desc(smem_u32(ring)), ring_mn = sw128_desc_mn(smem_u32(ring), 16384);
+        RingPos<S> base;
+        uint32_t np = 0;
+        while (next(g)) {
             if (lane == 0 && ok) {
                 const int nt = g.t1 - g.t0;
                 const bool pair = g.weight == 2;
-                const int n = pair ? 2 * nt : nt;
-                auto qk = [&](int j) {
-                    const int gs = j & 1, tt = pair ? j >> 1 : j;
-                    const uint32_t p = base + pos_k(tt);
-                    if (j == 0 && !(ok = wait(&st.qfull, seg))) return;
-                    if (!(ok = wait(&st.full[p % S], p / S))) return;
-                    tc_fence_after();
-                    const uint32_t qa = smem_u32(qbuf + (pair ? gs * TB : 0)), ka = smem_u32(ring + (p % S) * TB);
+                const int step = pair ? 1 : 2, first = pair ? 0 : gs;
+                const uint64_t qd = sw128_desc(smem_u32(qbuf + (pair ? gs * TB : 0)));
+                const bool twice = MT == 2 && !pair;
+                RingPos<S> kp = base, vp = base;
+                kp.skip(first ? pos_k(first) : 0);
+                vp.skip(pos_v(first, nt));
+                if (first < nt) ok = wait(&st.qfull, seg - 1);
+#pragma unroll 1
+                for (int tt = first - step; tt < nt && ok; tt += step) {  // O += P V of tile tt, S = Q K^T of the next
+                    if (tt >= first) {
+                        if (!(ok = wait(&st.pfull[gs], np))) break;
+                        ++np;
+                        if (tt == first && seg > 1 && !(ok = wait(&st.ofree, seg - 2))) break;
+                        if (!(ok = wait(&st.full[vp.slot], vp.phase))) break;
+                        fence_async_proxy();
+                        tc_fence_after();
+                        const uint64_t vd = ring_mn + (uint32_t)(vp.slot * (TB / 16));
 #pragma unroll
-                    for (int k = 0; k < HD / 16; ++k)
-                        tc_mma(tmem + gs * 128, sw128_desc(qa + (k >> 2) * 16384) + 2 * (k & 3),
-                               sw128_desc(ka + (k >> 2) * 16384) + 2 * (k & 3), id_qk, k ? 1u : 0u);
-                    if (!pair || gs == 1) tc_commit(&st.empty[p % S]);
-                    tc_commit(&st.sfull[gs]);
-                    if (j == n - 1) tc_commit(&st.qempty);
-                };
-                qk(0);
-                if (ok && n > 1) qk(1);
-                for (int j = 0; j < n && ok; ++j) {
-                    const int gs = j & 1, tt = pair ? j >> 1 : j;
-                    const uint32_t p = base + pos_v(tt, nt);
-                    if (!(ok = wait(&st.pfull[gs], np[gs]))) break;
-                    ++np[gs];
-                    if (j == 0 && seg > 0 && !(ok = wait(&st.ofree, seg - 1))) break;
-                    if (!(ok = wait(&st.full[p % S], p / S))) break;
-                    tc_fence_after();
-                    const uint32_t va = smem_u32(ring + (p % S) * TB);
+                        for (int k = 0; k < kTcTile / 16; ++k)
+                            tc_mma_ts(to, ts + k * 8, vd + k * 128, id_pv, tt > first || k ? 1u : 0u);
+                        tc_commit(&st.empty[vp.slot]);
+                        if (twice) tc_commit(&st.empty[vp.slot]);
+                        vp.skip(pos_v(min(tt + step, nt - 1), nt) - pos_v(tt, nt));
+                    }
+                    if (tt + step < nt) {
+                        if (!(ok = wait(&st.full[kp.slot], kp.phase))) break;
+                        fence_async_proxy();
+                        tc_fence_after();
+                        const uint64_t kd = ring_d + (uint32_t)(kp.slot * (TB / 16));
 #pragma unroll
-                    for (int k = 0; k < kTcTile / 16; ++k)
-                        tc_mma_ts(tmem + 256 + gs * 128, tmem + gs * 128 + k * 8, sw128_desc_mn(va + k * 2048, 16384), id_pv,
-                                  j > 1 || k ? 1u : 0u);
-                    if (!pair || gs == 1) tc_commit(&st.empty[p % S]);
-                    if (j + 2 < n) qk(j + 2);
+                        for (int k = 0; k < HD / 16; ++k)  // 32 bytes a step, 16384 to the next 64 columns
+                            tc_mma(ts, qd + (k >> 2) * 1024 + 2 * (k & 3), kd + (k >> 2) * 1024 + 2 * (k & 3), id_qk, k ? 1u : 0u);
+                        tc_commit(&st.sfull[gs]);
+                        tc_commit(&st.empty[kp.slot]);
+                        if (twice) tc_commit(&st.empty[kp.slot]);
+                        kp.skip(2 * step - (tt + step == 0));
+                    }
                 }
-                if (ok) tc_commit(&st.odone);
-                base += 2 * nt;
+                if (ok) {
+                    tc_commit(&st.qempty);
+                    tc_commit(&st.odone);
+                }
+                base.skip_long(2 * nt);
             }
-            ++seg;
             __syncwarp();
         }
         // every MMA issued has finished reading shared memory and TMEM before the CTA ends
         if (lane == 0) {
-            tc_commit(&st.drain);
-            mbar_wait(&st.drain, 0, a.status, 100000000LL);
+            tc_commit(&st.drain[gs]);
+            mbar_wait(&st.drain[gs], 0, a.status, 100000000LL);
         }
         __syncwarp();
-    } else if (Q8 && warp == 13) {  // ---- raw rows of an e4m3 cache
+    } else if (warp == 14) {  // ---- the plan
+        const PlanArgs pa = plan_args(a);
+        bool bad = false;
+        SegmentWalk<TcPlan> walk;
+        walk.init(pa, blockIdx.x, gridDim.x, &bad);
+        if (bad && blockIdx.x == 0) atomicOr(a.status, ST_CAPACITY);
+        for (uint32_t n = 0; ok; ++n) {
+            g.weight = 0;
+            const bool more = walk.next(pa, g);
+            const int k = n % kTcSegs;
+            if (n >= kTcSegs && !(ok = wait(&st.segempty[k], n / kTcSegs - 1))) break;
+            if (lane == 0) {
+                if (!more) g.weight = 0;
+                st.seg[k] = g;
+                mbar_arrive(&st.segfull[k]);
+            }
+            __syncwarp();
+            if (!more) break;
+        }
+    } else if (Q8 && warp == 15) {  // ---- raw rows of an e4m3 cache
+        RingPos<RS> pos;
         uint32_t i = 0;
-        bool ok = true;
-        while (ok && walk.next(pa, g)) {
+        while (ok && next(g)) {
             const int nt = g.t1 - g.t0;
-            for (int l = 0; l < 2 * nt && ok; ++l, ++i) {
-                const bool val = l == 2 * nt - 1 || (l > 0 && !(l & 1));
-                const int tt = l == 0 ? 0 : l == 2 * nt - 1 ? nt - 1 : val ? (l - 2) / 2 : (l + 1) / 2;
-                const uint32_t rs = i % RS;
-                if (i >= (uint32_t)RS && !(ok = wait(&st.rawempty[rs], i / RS - 1))) break;
+#pragma unroll 1
+            for (int l = 0; l < 2 * nt; ++l, ++i) {
+                const bool val = tile_is_value(l, nt);
+                const int tt = tile_number(l, nt);
+                if (i >= (uint32_t)RS && !(ok = wait(&st.rawempty[pos.slot], pos.phase ^ 1u))) break;
                 const int s0 = (g.t0 + tt) * kTcTile, s1 = min(s0 + kTcTile, g.end);
                 const int ps = a.cache.page_size ? a.cache.page_size : a.cache.max_seq;
                 const int p0 = s0 / ps, np = (s1 - 1) / ps - p0 + 1;
-                // a lane's runs: pages p0 + lane, + 32, ...
+                // a lane's runs of rows: pages p0 + lane, + 32, ...
                 auto run = [&](int k, int& from, int& rows, int64_t& row) -> bool {
-                    const int lo = max(s0, (p0 + k) * ps), hi = min((int64_t)s1, (int64_t)(p0 + k + 1) * ps);
+                    const int lo = max(s0, (p0 + k) * ps), hi = (int)min((int64_t)s1, (int64_t)(p0 + k + 1) * ps);
                     from = lo - s0;
                     rows = hi - lo;
                     if (!cache_row(a.cache, g.b, lo, row, a.status)) return false;
@@ -471,16 +650,20 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1) tree_attn_tc
                 };
                 int from, rows, bytes = 0;
                 int64_t row;
+#pragma unroll 1
                 for (int k = lane; k < np; k += 32)
                     if (run(k, from, rows, row)) bytes += rows * HD;
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) bytes += __shfl_xor_sync(0xffffffffu, bytes, o);
-                if (lane == 0) mbar_arrive_expect_tx(&st.rawfull[rs], bytes);
+                uint64_t* full = &st.rawfull[pos.slot];
+                if (lane == 0) mbar_arrive_expect_tx(full, bytes);
                 __syncwarp();
-                unsigned char* dst = rawring + rs * SH::kRawBytes;
+                unsigned char* dst = rawring + pos.slot * SH::kRawBytes;
                 const char* src = (const char*)(val ? a.cache.v : a.cache.k);
+#pragma unroll 1
                 for (int k = lane; k < np; k += 32)
-                    if (run(k, from, rows, row)) bulk_g2s(dst + from * HD, src + row * HD, rows * HD, &st.rawfull[rs]);
+                    if (run(k, from, rows, row)) bulk_g2s(dst + from * HD, src + row * HD, rows * HD, full);
+                pos.skip(1);
             }
         }
         // leave with no copy in flight: the last tiles have landed
@@ -490,49 +673,57 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1) tree_attn_tc
         const uint32_t lanes = (uint32_t)(wl * 32) << 16;
         const uint32_t ts = tmem + gs * 128 + lanes, to = tmem + 256 + gs * 128 + lanes;
         const float scale2 = a.scale * kLog2e;
-        uint32_t ns = 0, nj = 0, seg = 0;  // score blocks taken, joins, segments
-        bool ok = true;
-        while (walk.next(pa, g)) {
+        uint32_t ns = 0, nj = 0;  // score blocks taken, joins of the streams
+        while (ok && next(g)) {
             const int nt = g.t1 - g.t0;
             const bool pair = g.weight == 2;
             const int row = g.m * kAttnItemRows + (pair ? gs * 128 : 0) + wl * 32 + lane;  // of the item's head
             const int node = row / a.G;
             const bool live = row < g.rows;
-            const bool idle = g.m * kAttnItemRows + (pair ? gs * 128 : 0) + wl * 32 >= g.rows;  // the whole warp
+            const bool idle = row - lane >= g.rows;  // the whole warp
             float m = -INFINITY, sum = 0.f;  // reference maximum (log2 units), sum of 2^(s - m)
-            for (int tt = pair ? 0 : gs; tt < nt && ok; tt += pair ? 1 : 2) {
+#pragma unroll 1
+            for (int tt = pair ? 0 : gs; tt < nt; tt += pair ? 1 : 2) {
                 const int tile = g.t0 + tt;
                 if (!(ok = wait(&st.sfull[gs], ns))) break;
                 ++ns;
                 tc_fence_after();
                 if (!idle) {
-                    const bool tail = (tile + 1) * kTcTile > g.s.P;  // some slots need the mask
-                    uint32_t see[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
-                    if (tail) {
+                    if ((tile + 1) * kTcTile > g.s.P) {  // some slots are nodes': hidden scores become -inf
+#pragma unroll 1
+                        for (int c = 0; c < kTcTile; c += 32) {
+                            const uint32_t see = live ? seen_bits(a, g, node, tile * kTcTile + c) : 0u;
+                            uint32_t x[32];
+                            tc_ld32(ts + c, reinterpret_cast<float*>(x));
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) see[c] = live ? seen_bits(a, g, node, tile * kTcTile + 32 * c) : 0u;
-                    }
-                    float mx = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float s[32];
-                        tc_ld32(ts + 32 * c, s);
-                        if (tail) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) s[e] = see[c] >> e & 1u ? s[e] : -INFINITY;
+                            for (int e = 0; e < 32; ++e) x[e] = see >> e & 1u ? x[e] : 0xFF800000u;
+                            tc_st16(ts + c, x);
+                            tc_st16(ts + c + 16, x + 16);
                         }
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) mx = fmaxf(mx, s[e]);
+                        tc_wait_st();
                     }
-                    mx = mx == -INFINITY ? -INFINITY : mx * scale2;
-                    const bool first = tt < 2 && (tt == 0 || !pair);
-                    if (first) {
-                        m = mx;
-                    } else if (__any_sync(0xffffffffu, mx > m + 8.f)) {
+                    if (tt < 2 && (tt == 0 || !pair)) {  // the stream's first tile: its own maximum
+                        float mx = -INFINITY;
+#pragma unroll 1
+                        for (int c = 0; c < kTcTile; c += 32) {
+                            float x[32];
+                            tc_ld32(ts + c, x);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) mx = fmaxf(mx, x[e]);
+                        }
+                        m = mx * scale2;
+                    }
+                    uint32_t pk[kTcTile / 2];  // the row's probabilities
+                    float z;
+#pragma unroll 1
+                    while (true) {  // twice at most: again if the maximum has outgrown the reference
+                        const float ms = m == -INFINITY ? 0.f : m;
+                        const float mx = softmax_row(ts, scale2, -ms, pk, z) * scale2;
+                        if (!__any_sync(0xffffffffu, mx > m + 8.f)) break;
                         const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
                         sum *= f;
                         m = mn;
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < HD; c += 16) {
                             float o[16];
                             uint32_t u[16];
@@ -542,27 +733,9 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1) tree_attn_tc
                             tc_st16(to + c, u);
                         }
                     }
-                    const float ms = m == -INFINITY ? 0.f : m;
-                    float z0 = 0.f, z1 = 0.f;
+                    sum += z;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float s[32];
-                        uint32_t u[16];
-                        tc_ld32(ts + 32 * c, s);
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float p0 = ex2_approx(fmaf(s[e], scale2, -ms)), p1 = ex2_approx(fmaf(s[e + 1], scale2, -ms));
-                            if (tail) {
-                                p0 = see[c] >> e & 1u ? p0 : 0.f;
-                                p1 = see[c] >> (e + 1) & 1u ? p1 : 0.f;
-                            }
-                            z0 += p0;
-                            z1 += p1;
-                            u[e / 2] = pack_bf16(p0, p1);
-                        }
-                        tc_st16(ts + 16 * c, u);
-                    }
-                    sum += z0 + z1;
+                    for (int c = 0; c < kTcTile / 2; c += 16) tc_st16(ts + c, pk + c);
                     tc_wait_st();
                 }
                 tc_fence_before();
@@ -570,105 +743,116 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1) tree_attn_tc
                 if (lane == 0) mbar_arrive(&st.pfull[gs]);
             }
             // ---- the segment's result
-            ok = ok && wait(&st.odone, seg);
-            if (ok) {
-                tc_fence_after();
-                float f0 = 1.f, f1 = 0.f;  // weights of this stream's block, and of stream 1's (alternating)
-                const bool join = !pair && nt > 1;
-                if (join && gs == 1) {
-                    if (nj > 0 && !(ok = wait(&st.mlfree, nj - 1))) break;
-                    st.ml[wl * 32 + lane] = make_float2(m, sum);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&st.mlfull);
-                } else if (join) {
-                    if (!(ok = wait(&st.mlfull, nj))) break;
-                    const float2 o = st.ml[wl * 32 + lane];
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&st.mlfree);
-                    const float mn = fmaxf(m, o.x), ms = mn == -INFINITY ? 0.f : mn;
-                    f0 = exp2f(m - ms);
-                    f1 = exp2f(o.x - ms);
-                    sum = sum * f0 + o.y * f1;
-                    m = mn;
+            if (!ok || !(ok = wait(&st.odone, seg - 1))) break;
+            tc_fence_after();
+            float f0 = 1.f, f1 = 0.f;  // weights of this stream's block, and of stream 1's (alternating)
+            const bool join = !pair && nt > 1;
+            if (join && gs == 1) {
+                if (nj > 0 && !(ok = wait(&st.mlfree, nj - 1))) break;
+                st.ml[wl * 32 + lane] = make_float2(m, sum);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&st.mlfull);
+            } else if (join) {
+                if (!(ok = wait(&st.mlfull, nj))) break;
+                const float2 o = st.ml[wl * 32 + lane];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&st.mlfree);
+                const float mn = fmaxf(m, o.x), ms = mn == -INFINITY ? 0.f : mn;
+                f0 = exp2f(m - ms);
+                f1 = exp2f(o.x - ms);
+                sum = sum * f0 + o.y * f1;
+                m = mn;
+            }
+            nj += join;
+            if (!idle && (pair || gs == 0)) {
+                // rows leave through shared memory, 16 columns at a time, so that a warp writes whole
+                // sectors: the lanes' rows as addresses of the output or of the partial
+                unsigned char* stage = stages + warp * (SH::kStageInQ ? MT * TB / 8 : 2048);
+                const int head = g.h * a.G + row % a.G;
+                const int64_t pr = ((int64_t)blockIdx.x * 2 + g.slot) * kAttnItemRows + (row - g.m * kAttnItemRows);
+                const unsigned long long mine =
+                    !live ? 0ull
+                    : g.whole ? (unsigned long long)((bf16_t*)a.out.p + g.b * a.out.batch + (int64_t)node * a.out.token +
+                                                     (int64_t)head * a.out.head)
+                              : (unsigned long long)(a.part_o + pr * HD);
+                if (g.whole) {  // (zero sums: a row that sees nothing; its block may hold anything)
+                    f0 = sum == 0.f ? 0.f : f0 / sum;
+                    f1 = sum == 0.f ? 0.f : f1 / sum;
                 }
-                nj += join;
-                if (!idle && (pair || gs == 0)) {
-                    const bool odd = *(volatile int*)&st.odd[seg & 7] != 0;
-                    const int head = g.h * a.G + row % a.G;
-                    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-                    const int64_t pr = ((int64_t)blockIdx.x * 2 + g.slot) * kAttnItemRows + (row - g.m * kAttnItemRows);
+                const bool zero = g.whole && sum == 0.f;
 #pragma unroll 1
-                    for (int c = 0; c < HD; c += 32) {
-                        float o[32];
-                        tc_ld32(to + c, o);
-                        if (join) {
-                            float p[32];
-                            tc_ld32(to + 128 + c, p);
-                            // (a stream without any visible slot has zero sums: its block counts for nothing)
+                for (int c = 0; c < HD; c += 16) {
+                    float o[16];
+                    tc_ld16(to + c, o);
+                    if (join) {
+                        float p[16];
+                        tc_ld16(to + 128 + c, p);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = o[e] * f0 + p[e] * f1;
-                        }
-                        if (live && odd) {  // terms of non-finite value elements, for the nodes that see them
-                            const bf16_t* q = (const bf16_t*)a.q.p + g.b * a.q.batch + (int64_t)node * a.q.token +
-                                              (int64_t)head * a.q.head;
-                            for (int s = max(g.s.P, g.t0 * kTcTile); s < min(g.end, g.t1 * kTcTile); ++s) {
-                                const RowInfo x = row_info<Q8>(a, g, s / kTcTile, s % kTcTile);
-                                if (x.row < 0 || !(seen_bits(a, g, node, s) & 1u)) continue;
-                                auto at = [&](const void* p, float sc, int e) {
-                                    if (Q8) {
-                                        const float f = e4m3x2_to_f32(((const uint8_t*)p)[x.row * HD + e]).x;
-                                        return bf16_to_f32((uint16_t)pack_bf16(f * sc, 0.f));
-                                    }
-                                    return Storage<bf16_t>::load((const bf16_t*)p, x.row * HD + e);
-                                };
-                                bool any = false;
-                                for (int e = 0; e < 32; ++e) any |= !finite_f32(at(a.cache.v, x.vs, c + e));
-                                if (!any) continue;
-                                float dot = 0.f;
-                                for (int e = 0; e < HD; ++e) dot = fmaf(Storage<bf16_t>::load(q, e), at(a.cache.k, x.ks, e), dot);
-                                const float p = exp2f(dot * scale2 - (m == -INFINITY ? 0.f : m));
+                        for (int e = 0; e < 16; ++e) o[e] = o[e] * f0 + p[e] * f1;
+                    } else if (g.whole) {
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    const float v = at(a.cache.v, x.vs, c + e);
-                                    if (!finite_f32(v)) o[e] += p * v;
+                        for (int e = 0; e < 16; ++e) o[e] *= f0;
+                    }
+                    if (zero) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = 0.f;
+                    }
+                    // chunk k of row l lies at 16 (k ^ l / 4 or l / 2) of the row's bytes: no bank conflicts
+                    __syncwarp();
+                    if (g.whole) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            *reinterpret_cast<uint4*>(stage + lane * 32 + ((k ^ (lane >> 2)) & 1) * 16) = pack16<bf16_t>(o + 8 * k);
+                        __syncwarp();
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {  // two lanes a row
+                            const int r = k * 16 + lane / 2, h = lane & 1;
+                            bf16_t* dst = (bf16_t*)__shfl_sync(0xffffffffu, mine, r);
+                            const uint4 v = *reinterpret_cast<const uint4*>(stage + r * 32 + ((h ^ (r >> 2)) & 1) * 16);
+                            if (dst) {
+                                dst += c + 8 * h;
+                                if (a.out_vec) {
+                                    *reinterpret_cast<uint4*>(dst) = v;
+                                } else {
+                                    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) dst[e].bits = (uint16_t)(x[e / 2] >> (16 * (e & 1)));
                                 }
                             }
                         }
-                        if (live && g.whole) {
-                            bf16_t* dst = (bf16_t*)a.out.p + g.b * a.out.batch + (int64_t)node * a.out.token +
-                                          (int64_t)head * a.out.head + c;
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = sum == 0.f ? 0.f : o[e] * inv;
-                            if (a.out_vec) {
-#pragma unroll
-                                for (int e = 0; e < 32; e += 8) *reinterpret_cast<uint4*>(dst + e) = pack16<bf16_t>(o + e);
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) store_one(dst + e, o[e]);
-                            }
-                        } else if (live) {
-                            float4* dst = reinterpret_cast<float4*>(a.part_o + pr * HD + c);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) dst[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                        }
+                        for (int k = 0; k < 4; ++k)
+                            *reinterpret_cast<float4*>(stage + lane * 64 + ((k ^ (lane >> 1)) & 3) * 16) =
+                                make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
                         __syncwarp();
-                    }
-                    if (live) {
-                        if (!g.whole)
-                            *reinterpret_cast<float2*>(a.part_ml + 2 * pr) = make_float2(m, sum);
-                        else if (a.lse)
-                            a.lse[((int64_t)g.b * a.T + node) * a.H + head] =
-                                sum == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(sum);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {  // four lanes a row
+                            const int r = k * 8 + lane / 4, h = lane & 3;
+                            float* dst = (float*)__shfl_sync(0xffffffffu, mine, r);
+                            const float4 v = *reinterpret_cast<const float4*>(stage + r * 64 + ((h ^ (r >> 1)) & 3) * 16);
+                            if (dst) *reinterpret_cast<float4*>(dst + c + 4 * h) = v;
+                        }
                     }
                 }
-                tc_fence_before();
                 __syncwarp();
-                // (the loaders are at most two segments ahead, the other stream at most one behind)
-                if (gs == 0 && wl == 0 && lane == 0) st.odd[(seg + 4) & 7] = 0;
-                if (lane == 0) mbar_arrive(&st.ofree);
+                if (live) {
+                    if (!g.whole)
+                        *reinterpret_cast<float2*>(a.part_ml + 2 * pr) = make_float2(m, sum);
+                    else if (a.lse)
+                        a.lse[((int64_t)g.b * a.T + node) * a.H + head] =
+                            sum == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(sum);
+                    if (*(volatile int*)&st.odd[(seg - 1) & 7]) put_odd_columns<HD, Q8>(a, g, node, head, m, (void*)mine);
+                }
             }
-            ++seg;
-            if (!ok) break;
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                // (the loaders are at most two segments ahead, the other stream at most one behind)
+                if (warp == 0) st.odd[(seg + 3) & 7] = 0;
+                mbar_arrive(&st.ofree);
+                if (SH::kStageInQ) mbar_arrive(&st.qempty);
+            }
         }
     }
     tc_fence_before();
