@@ -102,37 +102,34 @@ struct Segment {
     int slot;   // where its partial goes: 0 when an earlier CTA began the item, else 1
 };
 
-// Walks a CTA's segments; used by a whole warp, every lane holding the same state.
+// Where CTA c's units begin: the cut of the line and the item that holds unit cut.begin(c).
+// Found by a whole warp together, every lane with the same result.
 template <typename PL>
-struct SegmentWalk {
-    int u0, u1, pos;  // the CTA's units; first unit of the current item
-    int b, h, m;
+struct Place {
+    Cut cut;
+    bool found;  // false: no unit at or past the beginning
+    int b, h, m, s0;  // the item and its first unit
     SeqLen s;
 
-    __device__ __forceinline__ void init(const PlanArgs& a, int cta, int ncta, bool* bad = nullptr) {
+    __device__ __forceinline__ static Place find(const PlanArgs& a, int c, int ncta, bool* bad = nullptr) {
         const int lane = threadIdx.x & 31;
         // units of all sequences; the first 32 sequences' stay in registers
-        const SeqLen s0 = lane < a.B ? seq_len(a, lane, bad) : SeqLen{0, 0};
-        const int w0 = PL::head_units(a, s0);
+        const SeqLen sl0 = lane < a.B ? seq_len(a, lane, bad) : SeqLen{0, 0};
+        const int w0 = PL::head_units(a, sl0);
         int U = w0;
 #pragma unroll 1
         for (int bb = lane + 32; bb < a.B; bb += 32) U += PL::head_units(a, seq_len(a, bb, bad));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
-        const Cut cut(U * a.Hkv, ncta);
-        u0 = cut.begin(cta);
-        u1 = cut.begin(cta + 1);
-        b = h = m = pos = 0;
-        s = SeqLen{0, 0};
-        if (u0 >= u1) {
-            b = a.B;
-            return;
-        }
+        U *= a.Hkv;
+        Place p{Cut(U, ncta), false, 0, 0, 0, 0, SeqLen{0, 0}};
+        const int u0 = p.cut.begin(c);
+        if (u0 >= U) return p;
         // the sequence that holds unit u0: the first whose units end past it
         int base = 0;
 #pragma unroll 1
         for (int b0 = 0; b0 < a.B; b0 += 32) {
-            SeqLen sl = s0;
+            SeqLen sl = sl0;
             int hu = w0;
             if (b0) {
                 sl = b0 + lane < a.B ? seq_len(a, b0 + lane) : SeqLen{0, 0};
@@ -147,20 +144,47 @@ struct SegmentWalk {
             const unsigned hit = __ballot_sync(0xffffffffu, base + inc > u0);
             if (hit) {
                 const int l = __ffs(hit) - 1;
-                b = b0 + l;
-                s.P = __shfl_sync(0xffffffffu, sl.P, l);
-                s.n = __shfl_sync(0xffffffffu, sl.n, l);
+                p.found = true;
+                p.b = b0 + l;
+                p.s.P = __shfl_sync(0xffffffffu, sl.P, l);
+                p.s.n = __shfl_sync(0xffffffffu, sl.n, l);
                 const int head = __shfl_sync(0xffffffffu, hu, l);
-                pos = base + __shfl_sync(0xffffffffu, inc, l) - head * a.Hkv;
-                h = (u0 - pos) / head;
-                pos += h * head;
+                p.s0 = base + __shfl_sync(0xffffffffu, inc, l) - head * a.Hkv;
+                p.h = (u0 - p.s0) / head;
+                p.s0 += p.h * head;
                 break;
             }
             base += __shfl_sync(0xffffffffu, inc, 31);
         }
+        // the block of the head
+#pragma unroll 1
+        while (true) {
+            const int w = PL::tiles(a, p.s, p.m) * PL::weight(p.s.n * a.G, p.m);
+            if (p.s0 + w > u0) return p;
+            p.s0 += w;
+            ++p.m;
+        }
     }
-    // The next segment with at least one tile; false at the end. (The first call also skips the
-    // blocks of the item's head that lie before u0.)
+};
+
+// Walks a CTA's segments; used by a whole warp, every lane holding the same state.
+template <typename PL>
+struct SegmentWalk {
+    int u0, u1, pos;  // the CTA's units; first unit of the current item
+    int b, h, m;
+    SeqLen s;
+
+    __device__ __forceinline__ void init(const PlanArgs& a, int cta, int ncta, bool* bad = nullptr) {
+        const Place<PL> p = Place<PL>::find(a, cta, ncta, bad);
+        u0 = p.cut.begin(cta);
+        u1 = p.cut.begin(cta + 1);
+        b = p.found ? p.b : a.B;
+        h = p.h;
+        m = p.m;
+        pos = p.s0;
+        s = p.s;
+    }
+    // The next segment with at least one tile; false at the end.
     __device__ __forceinline__ bool next(const PlanArgs& a, Segment& g) {
 #pragma unroll 1
         while (b < a.B && pos < u1) {

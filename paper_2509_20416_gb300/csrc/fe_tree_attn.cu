@@ -8,94 +8,91 @@ namespace fe {
 namespace {
 
 // ---- the join ------------------------------------------------------------------------------
-// One warp per row (b, node, head): if the row's item was split, sum its partials in CTA order,
-// sum_c 2^(m_c - m) (o_c, l_c) with m the largest m_c, and write the row; rows without any item
-// (nodes past n_b) get zeros and -inf. Rows of whole items were written by the attention kernel.
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
+// Sums the partial results of items split between CTAs, sum_c 2^(m_c - m) (o_c, l_c) with m the
+// largest m_c, in CTA order, and writes their rows; also fills the rows of nodes past n_b with
+// zeros and -inf. Only G - 1 places can split an item, so block x looks at the one between CTAs x
+// and x + 1, and takes the item there if CTA x is the item's first; blocks y share its rows, a
+// warp per row. Bound by the latency of the schedule and of two dependent reads; launched so that
+// the schedule (which needs only the caller's lengths) is worked out before the attention ends.
+constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinShares = 8;
 
 template <typename QT, int HD, typename PL, int ROWS>
 __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a, int ncta) {
+    constexpr int E = HD / 32;  // columns of a lane
     const PlanArgs pa = plan_args(a);
-    const int lane = threadIdx.x & 31;
-    const int b = blockIdx.y;
-    // schedule: total units, and the first unit of this sequence (lengths are the caller's and
-    // do not depend on the attention kernel, so this runs before the wait)
-    int U = 0, before = 0;
-#pragma unroll 1
-    for (int bb = lane; bb < a.B; bb += 32) {
-        const int u = PL::head_units(pa, seq_len(pa, bb)) * a.Hkv;
-        U += u;
-        if (bb < b) before += u;
-    }
+    const int lane = threadIdx.x & 31, wid = blockIdx.y * kJoinWarps + threadIdx.x / 32;
+    const Place<PL> w = Place<PL>::find(pa, blockIdx.x + 1, ncta);
+    griddep_wait();  // (on every path: this kernel's end stands for the attention's too)
+    // rows of nodes past n_b
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+        const int n = seq_len(pa, b).n;
+        if (n == a.T) continue;
+        for (int x = n * a.H + wid; x < a.T * a.H; x += kJoinShares * kJoinWarps) {
+            QT* dst = (QT*)a.out.p + b * a.out.batch + (int64_t)(x / a.H) * a.out.token + (int64_t)(x % a.H) * a.out.head;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        U += __shfl_xor_sync(0xffffffffu, U, o);
-        before += __shfl_xor_sync(0xffffffffu, before, o);
+            for (int e = 0; e < E; ++e) store_one(dst + lane * E + e, 0.f);
+            if (a.lse && lane == 0) a.lse[(int64_t)b * a.T * a.H + x] = -INFINITY;
+        }
     }
-    const SeqLen s = seq_len(pa, b);
-    const int rows = s.n * a.G;
-    const int head_units = PL::head_units(pa, s);
-    const Cut cut(U, ncta);
-    griddep_wait();
-    for (int x = blockIdx.x * kJoinWarps + threadIdx.x / 32; x < a.T * a.H; x += gridDim.x * kJoinWarps) {
-        const int node = x / a.H, head = x % a.H, h = head / a.G;
-        const int r = node * a.G + head % a.G;
-        float o[HD / 32];
+    if (!w.found) return;
+    const int rows = w.s.n * a.G, nrow = min(ROWS, rows - w.m * ROWS);
+    const int wt = PL::weight(rows, w.m), nt = PL::tiles(pa, w.s, w.m);
+    if (w.s0 >= w.cut.begin(blockIdx.x + 1)) return;  // the item starts there: not split
+    if (w.cut.owner(w.s0) != (int)blockIdx.x) return;  // an earlier block's item
+    const int c1 = w.cut.owner(w.s0 + (nt - 1) * wt);
+    if (c1 == (int)blockIdx.x) return;
+    for (int r = wid; r < nrow; r += kJoinShares * kJoinWarps) {
+        // the partials' row of contributor c, or -1 if no tile starts in c's units
+        auto part = [&](int c) -> int64_t {
+            const int t0 = PL::first_tile(w.s0, wt, nt, w.cut.begin(c));
+            if (c > c1 || t0 >= PL::first_tile(w.s0, wt, nt, w.cut.begin(c + 1))) return -1;
+            return ((int64_t)c * 2 + (t0 == 0 ? 1 : 0)) * kAttnItemRows + r;
+        };
+        float mx = -INFINITY;
+        for (int c = blockIdx.x + lane; c <= c1; c += 32) {
+            const int64_t p = part(c);
+            if (p >= 0) mx = fmaxf(mx, __ldcg(a.part_ml + 2 * p));
+        }
+        mx = warp_max(mx);
+        const float ms = mx == -INFINITY ? 0.f : mx;
+        float o[E], sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < HD / 32; ++e) o[e] = 0.f;
-        float mx = -INFINITY, sum = 0.f;
-        if (node < s.n) {
-            const int m = r / ROWS, w = PL::weight(rows, m), nt = PL::tiles(pa, s, m);
-            int s0 = before + h * head_units;
-            if (pa.causal) {
-#pragma unroll 1
-                for (int k = 0; k < m; ++k) s0 += PL::tiles(pa, s, k) * PL::weight(rows, k);
-            } else {
-                s0 += m * nt * PL::weight(ROWS, 0);
-            }
-            const int c0 = cut.owner(s0), c1 = cut.owner(s0 + (nt - 1) * w);
-            if (c0 == c1) continue;
-            for (int c = c0; c <= c1; ++c) {
-                const int u0 = cut.begin(c), u1 = cut.begin(c + 1);
-                const int t0 = PL::first_tile(s0, w, nt, u0);
-                if (t0 >= PL::first_tile(s0, w, nt, u1)) continue;  // no tile starts in this CTA's units
-                const int64_t pr = ((int64_t)c * 2 + (t0 == 0 ? 1 : 0)) * kAttnItemRows + (r - m * ROWS);
-                const float pm = __ldcg(a.part_ml + 2 * pr), pl = __ldcg(a.part_ml + 2 * pr + 1);
-                const float* po = a.part_o + pr * HD + lane * (HD / 32);
-                float v[HD / 32];
-                if constexpr (HD == 128) {
-                    const float4 f = __ldcg(reinterpret_cast<const float4*>(po));
-                    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
+        for (int c0 = blockIdx.x; c0 <= c1; c0 += 32) {
+            const int64_t p = part(c0 + lane);
+            const float2 ml = p >= 0 ? __ldcg(reinterpret_cast<const float2*>(a.part_ml + 2 * p)) : make_float2(-INFINITY, 0.f);
+            const float f = exp2f(ml.x - ms);
+            const int n = min(32, c1 - c0 + 1);
+#pragma unroll 4
+            for (int k = 0; k < n; ++k) {
+                const int64_t pk = __shfl_sync(0xffffffffu, p, k);
+                const float fk = __shfl_sync(0xffffffffu, f, k), lk = __shfl_sync(0xffffffffu, ml.y, k);
+                if (pk < 0) continue;
+                const float* src = a.part_o + pk * HD + lane * E;
+                sum += lk * fk;
+                if constexpr (E == 4) {
+                    const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
+                    o[0] += v.x * fk; o[1] += v.y * fk; o[2] += v.z * fk; o[3] += v.w * fk;
                 } else {
-                    const float2 f = __ldcg(reinterpret_cast<const float2*>(po));
-                    v[0] = f.x; v[1] = f.y;
+                    const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
+                    o[0] += v.x * fk; o[1] += v.y * fk;
                 }
-                const float mn = fmaxf(mx, pm), ms = mn == -INFINITY ? 0.f : mn;
-                const float f0 = exp2f(mx - ms), f1 = exp2f(pm - ms);
-                mx = mn;
-                sum = sum * f0 + pl * f1;
-#pragma unroll
-                for (int e = 0; e < HD / 32; ++e) o[e] = o[e] * f0 + v[e] * f1;
             }
         }
+        const int row = w.m * ROWS + r, node = row / a.G, head = w.h * a.G + row % a.G;
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        QT* dst = (QT*)a.out.p + b * a.out.batch + node * a.out.token + head * a.out.head + lane * (HD / 32);
+        QT* dst = (QT*)a.out.p + w.b * a.out.batch + (int64_t)node * a.out.token + (int64_t)head * a.out.head + lane * E;
 #pragma unroll
-        for (int e = 0; e < HD / 32; ++e) store_one(dst + e, sum == 0.f ? 0.f : o[e] * inv);
+        for (int e = 0; e < E; ++e) store_one(dst + e, sum == 0.f ? 0.f : o[e] * inv);
         if (a.lse && lane == 0)
-            a.lse[((int64_t)b * a.T + node) * a.H + head] =
+            a.lse[((int64_t)w.b * a.T + node) * a.H + head] =
                 sum == 0.f ? -INFINITY : mx * 0.6931471805599453f + logf(sum);
     }
 }
 
 template <typename QT, int HD, typename PL, int ROWS>
 cudaError_t launch_join(const TreeAttnArgs& a, int ncta, cudaStream_t st) {
-    const int64_t rows = (int64_t)a.T * a.H;
-    int64_t gx = (rows + kJoinWarps - 1) / kJoinWarps;
-    const int64_t most = (152 * 8 + a.B - 1) / a.B;  // about one resident wave over all sequences
-    if (gx > most) gx = most;
-    return launch_k(tree_attn_join_kernel<QT, HD, PL, ROWS>, dim3((unsigned)gx, a.B), dim3(kJoinThreads), 0, st, true, a,
-                    ncta);
+    return launch_k(tree_attn_join_kernel<QT, HD, PL, ROWS>, dim3(ncta, kJoinShares), dim3(kJoinThreads), 0, st, true, a, ncta);
 }
 
 template <int HD>

@@ -13,7 +13,8 @@
 // every key/value tile; a smaller one gives both streams the same rows, on alternate tiles, and
 // adds their results at the end. While one stream's softmax runs on the CUDA cores, the tensor
 // cores work on the other's products.
-//   warps 0-3, 4-7   softmax of stream 0, 1: thread = row (TMEM lane)
+//   warps 0-3, 4-7   softmax of stream 0, 1: thread = row (TMEM lane); they also load the queries, the
+//                    next segment's while this one's last product runs, and write the results
 //   warps 8-11       loaders: rows from the cache into 128-byte-swizzled tiles of 128 slots (K and
 //                    V alike, [slot][hd]), by cp.async, or converted from e4m3 on the way
 //   warp 12          issues the MMAs: S = Q K^T (K-major operands), O += P V with P (bfloat16)
@@ -21,7 +22,8 @@
 //   warp 13          e4m3: bulk copies of the raw rows (runs of rows are contiguous in a page)
 // The softmax keeps a reference maximum per row and rescales O only when the maximum has grown by
 // more than 2^8 (the probabilities then stay below 2^8, where bfloat16 is as precise as below 1):
-// after the first tiles that is rare, and it saves a pass over O per tile. Sums and statistics
+// after the first tiles that is rare; it saves a pass over O per tile and a pass over the scores
+// for their maximum. Sums and statistics
 // are float32; probabilities are rounded to bfloat16 for the second product, which costs 2^-9 of
 // each on average and is what the 16-bit tensor path offers.
 // Values in slots that a row does not see meet a zero probability, but 0 x NaN is NaN: the loaders
@@ -58,17 +60,17 @@ constexpr int kTcSegs = 4;  // segments planned ahead
 
 struct TcState {
     uint64_t full[6], empty[6], rawfull[4], rawempty[4], segfull[kTcSegs], segempty[kTcSegs], qfull, qempty, sfull[2],
-        pfull[2], odone, ofree, mlfull, mlfree, drain[2];
+        pfull[2], odone, ofree, mlfull, mlfree, drain[2], turn[2];
     Segment seg[kTcSegs];  // weight 0: no more
     uint32_t tmem;
     int abort;
     int odd[8];        // by segment: non-finite value elements were set aside
-    float2 ml[128];    // stream 1's (maximum, sum) for the join of the two streams
+    float2 ml[2][128];  // the streams' (maximum, sum), for their join
 };
 
 template <int HD, bool Q8, int MT>
 constexpr int tc_smem() {
-    constexpr int bytes = 1024 + TcShape<HD, Q8, MT>::kData + (int)sizeof(TcState);
+    constexpr int bytes = TcShape<HD, Q8, MT>::kData + (int)sizeof(TcState);
     static_assert(bytes <= 227 * 1024, "shared memory of a CTA");
     return bytes;
 }
@@ -82,6 +84,13 @@ __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// true in one lane of a converged warp (the same lane every time)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 
 // MN-major operand block of 128 K-rows x hd: 128-byte-swizzled atoms of 8 rows x 64 elements,
 // 1024 bytes between 8-row groups (K), `half` bytes between 64-element groups (MN)
@@ -155,29 +164,30 @@ __device__ __forceinline__ RowInfo row_info(const TreeAttnArgs& a, const Segment
     return x;
 }
 
-// Query rows of block `blk` into a swizzled K-major tile (rows past the item's are zero).
+// A warp's 32 query rows (rows r0 ..) into rows w * 32 .. of a swizzled K-major tile; rows past
+// the item's are zero.
 template <int HD>
-__device__ __forceinline__ void load_q(const TreeAttnArgs& a, const Segment& g, int blk, unsigned char* dst, int w, int lane) {
+__device__ __forceinline__ void load_q(const TreeAttnArgs& a, const Segment& g, int r0, unsigned char* dst, int w, int lane) {
     constexpr int CH = HD / 8, RP = 32 / CH;  // 16-byte chunks a row, rows a warp access
-    const int r0 = g.m * kAttnItemRows + blk * 128 + w * 32 + lane;
-    const bf16_t* src = nullptr;
-    if (r0 < g.rows)
-        src = (const bf16_t*)a.q.p + g.b * a.q.batch + (int64_t)(r0 / a.G) * a.q.token +
-              (int64_t)(g.h * a.G + r0 % a.G) * a.q.head;
-    const int c = lane % CH;
-#pragma unroll 1
+    const int c = lane % CH, row = r0 + lane;
+    unsigned long long mine = 0;
+    if (row < g.rows)
+        mine = (unsigned long long)((const bf16_t*)a.q.p + g.b * a.q.batch + (int64_t)(row / a.G) * a.q.token +
+                                    (int64_t)(g.h * a.G + row % a.G) * a.q.head);
+    const uint32_t d = smem_u32(dst) + (c >> 3) * 16384 + w * 4096;
+#pragma unroll 2
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = i * RP + lane / CH;
-        const bf16_t* p = (const bf16_t*)__shfl_sync(0xffffffffu, (unsigned long long)src, r);
-        unsigned char* d = dst + (c >> 3) * 16384 + sw128_offset(w * 32 + r, c & 7);
+        const unsigned long long src = __shfl_sync(0xffffffffu, mine, r);
         if (a.q_vec) {
-            cp_async16(smem_u32(d), p ? p + c * 8 : (const bf16_t*)a.q.p, p != nullptr);
+            cp_async16(d + sw128_offset(r, c & 7), (const void*)((src ? src : (unsigned long long)a.q.p) + (src ? c * 16 : 0)), src != 0);
         } else {
             uint32_t x[4] = {0, 0, 0, 0};
+            const bf16_t* p = (const bf16_t*)src;
             if (p)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = (uint32_t)p[c * 8 + 2 * e].bits | (uint32_t)p[c * 8 + 2 * e + 1].bits << 16;
-            *reinterpret_cast<uint4*>(d) = make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4*>(dst + (c >> 3) * 16384 + w * 4096 + sw128_offset(r, c & 7)) = make_uint4(x[0], x[1], x[2], x[3]);
         }
     }
 }
@@ -259,10 +269,11 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_
     // lanes store into different banks
     unsigned char* base = dst + (c >> 2) * 16384 + w * 4096;
     const int swap = c >> 2, c0 = 2 * (c & 3) + swap, c1 = 2 * (c & 3) + 1 - swap;
-#pragma unroll 2
+    const bool big = __any_sync(0xffffffffu, mine.y != 0x3F803F80u && mine.x != 0);  // some scale above 2^7
+#pragma unroll 1
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = i * RP + lane / CH;
-        const uint32_t f1 = __shfl_sync(0xffffffffu, mine.x, r), f2 = __shfl_sync(0xffffffffu, mine.y, r);
+        const uint32_t f1 = __shfl_sync(0xffffffffu, mine.x, r);
         uint4 u = *reinterpret_cast<const uint4*>(raw + (w * 32 + r) * HD + c * 16);
         if (f1 == 0) u = make_uint4(0, 0, 0, 0);
         const uint32_t in[4] = {u.x, u.y, u.z, u.w};
@@ -274,7 +285,8 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], f1);
-        if (f2 != 0x3F803F80u && f1 != 0) {  // a scale above 2^7
+        if (big) {
+            const uint32_t f2 = __shfl_sync(0xffffffffu, mine.y, r);
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], f2);
         }
@@ -295,7 +307,7 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_
     return odd;
 }
 
-// 16 TMEM columns, not waited for; then the wait, which the values pass through
+// TMEM columns, not waited for; then the wait, which the values pass through
 __device__ __forceinline__ void tc_ld16_start(uint32_t taddr, uint32_t* r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
@@ -311,6 +323,32 @@ __device__ __forceinline__ void tc_ld16_wait(uint32_t* r) {
                  :
                  : "memory");
 }
+__device__ __forceinline__ void tc_ld32_start(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tc_ld32_wait(uint32_t* r) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                   "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                   "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :
+                 : "memory");
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 
 // packed pairs of floats: d = a * b + c and a + b, elementwise
 __device__ __forceinline__ uint64_t pair_f32(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
@@ -325,32 +363,74 @@ __device__ __forceinline__ uint64_t add_x2(uint64_t a, uint64_t b) {
     return d;
 }
 
-// A row of 128 scores x at TMEM columns ts: 2^(scale2 x + shift) as packed bfloat16 in pk, their
-// float32 sum in z; returns the largest x. The next 16 columns load while 16 are worked on.
-__device__ __forceinline__ float softmax_row(uint32_t ts, float scale2, float shift, uint32_t (&pk)[kTcTile / 2], float& z) {
+// One row's softmax of a tile, in one pass over its 128 scores x at TMEM columns ts: 2^(scale2 x - m)
+// as packed bfloat16 over the first 64 columns (32 scores become 16 columns, always behind what is
+// still to be read), their float32 sum added to `sum`. m is the row's reference maximum; when some
+// row of the warp has outgrown it by more than 2^8, the warp moves to new references on the spot,
+// rescaling the sums, the columns written so far and, unless this is the stream's first tile, O.
+// A loop with a short body: the CTA's roles share the instruction caches, and unrolled rows made
+// every one of them wait for fetches.
+template <int HD>
+__device__ __forceinline__ void softmax_row(uint32_t ts, uint32_t to, float scale2, bool first, float& m, float& sum) {
     const uint64_t sc = pair_f32(__float_as_uint(scale2), __float_as_uint(scale2));
-    const uint64_t sh = pair_f32(__float_as_uint(shift), __float_as_uint(shift));
-    uint32_t x[2][16];
-    uint64_t z2[2] = {0, 0};
-    float mx = -INFINITY;
-    tc_ld16_start(ts, x[0]);
+    uint32_t x[32];
+    uint64_t z[2] = {0, 0};
+    tc_ld32_start(ts, x);
+#pragma unroll 1
+    for (int c = 0; c < kTcTile; c += 32) {
+        tc_ld32_wait(x);
+        float mx = __uint_as_float(x[0]), my = __uint_as_float(x[1]);
 #pragma unroll
-    for (int c = 0; c < kTcTile / 16; ++c) {
-        uint32_t* v = x[c & 1];
-        tc_ld16_wait(v);
-        if (c + 1 < kTcTile / 16) tc_ld16_start(ts + 16 * (c + 1), x[(c + 1) & 1]);
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            mx = fmaxf(mx, fmaxf(__uint_as_float(v[e]), __uint_as_float(v[e + 1])));
-            const uint64_t y = fma_x2(pair_f32(v[e], v[e + 1]), sc, sh);
-            const float p0 = ex2_approx(__uint_as_float((uint32_t)y)), p1 = ex2_approx(__uint_as_float((uint32_t)(y >> 32)));
-            z2[(e >> 1) & 1] = add_x2(z2[(e >> 1) & 1], pair_f32(__float_as_uint(p0), __float_as_uint(p1)));
-            pk[8 * c + e / 2] = pack_bf16(p0, p1);
+        for (int e = 2; e < 30; e += 4) {
+            mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+            my = max3(my, __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
         }
+        mx = max3(mx, __uint_as_float(x[30]), __uint_as_float(x[31]));
+        mx = fmaxf(mx, my) * scale2;
+        if (__any_sync(0xffffffffu, mx > m + 8.f)) {
+            const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
+            const uint64_t ff = pair_f32(__float_as_uint(f), __float_as_uint(f));
+            z[0] = fma_x2(z[0], ff, 0);
+            z[1] = fma_x2(z[1], ff, 0);
+            sum *= f;
+            m = mn;
+#pragma unroll 1
+            for (int k = 0; k < c / 2; k += 16) {
+                uint32_t u[16];
+                tc_ld16_start(ts + k, u);
+                tc_ld16_wait(u);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    u[e] = pack_bf16(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xFFFF0000u) * f);
+                tc_st16(ts + k, u);
+            }
+            if (!first) {
+#pragma unroll 1
+                for (int k = 0; k < HD; k += 16) {
+                    uint32_t u[16];
+                    tc_ld16_start(to + k, u);
+                    tc_ld16_wait(u);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * f);
+                    tc_st16(to + k, u);
+                }
+            }
+        }
+        const float shift = m == -INFINITY ? 0.f : -m;
+        const uint64_t sh = pair_f32(__float_as_uint(shift), __float_as_uint(shift));
+        uint32_t pk[16];
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const uint64_t y = fma_x2(pair_f32(x[e], x[e + 1]), sc, sh);
+            const float p0 = ex2_approx(__uint_as_float((uint32_t)y)), p1 = ex2_approx(__uint_as_float((uint32_t)(y >> 32)));
+            z[(e >> 1) & 1] = add_x2(z[(e >> 1) & 1], pair_f32(__float_as_uint(p0), __float_as_uint(p1)));
+            pk[e / 2] = pack_bf16(p0, p1);
+        }
+        if (c + 32 < kTcTile) tc_ld32_start(ts + c + 32, x);
+        tc_st16(ts + c / 2, pk);
     }
-    const uint64_t zz = add_x2(z2[0], z2[1]);
-    z = __uint_as_float((uint32_t)zz) + __uint_as_float((uint32_t)(zz >> 32));
-    return mx;
+    const uint64_t zz = add_x2(z[0], z[1]);
+    sum += __uint_as_float((uint32_t)zz) + __uint_as_float((uint32_t)(zz >> 32));
 }
 
 // Ring positions of a segment's tiles. They are loaded in the order of their first use:
@@ -366,10 +446,11 @@ __device__ __forceinline__ int tile_number(int l, int n) {
 // their columns is the sum of p times them alone, since what is finite does not change an infinity
 // or NaN. dst: the row's place in the output (bfloat16) or the partial results (float32).
 template <int HD, bool Q8>
-__device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segment& g, int node, int head, float m, void* dst) {
+__device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segment& g, int node, int head, float m, void* dst, int e0,
+                                             int e1) {
     const bf16_t* q = (const bf16_t*)a.q.p + g.b * a.q.batch + (int64_t)node * a.q.token + (int64_t)head * a.q.head;
 #pragma unroll 1
-    for (int e = 0; e < HD; ++e) {
+    for (int e = e0; e < e1; ++e) {
         float t = 0.f;
         bool any = false;
 #pragma unroll 1
@@ -420,14 +501,17 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     tree_attn_tc_kernel(const __grid_constant__ TreeAttnArgs a) {
     using SH = TcShape<HD, Q8, MT>;
     constexpr int S = SH::kSlots, RS = Q8 ? SH::kRawSlots : 1, TB = SH::kTileBytes;
-    extern __shared__ unsigned char dsm_raw[];
-    unsigned char* qbuf = (unsigned char*)(((uintptr_t)dsm_raw + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) unsigned char qbuf[];
     unsigned char* ring = qbuf + MT * TB;
     unsigned char* rawring = ring + S * TB;
     unsigned char* stages = SH::kStageInQ ? qbuf : rawring + SH::kRawSlots * SH::kRawBytes;
     TcState& st = *reinterpret_cast<TcState*>(qbuf + SH::kData);
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     griddep_launch_dependents();
+    if (smem_u32(qbuf) & 1023u) {  // (dynamic memory alone starts on a 1024-byte boundary)
+        if (t == 0) atomicOr(a.status, ST_DEVICE);
+        return;
+    }
 
     if (t == 0) {
         for (int i = 0; i < S; ++i) {
@@ -442,17 +526,18 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             mbar_init(&st.segfull[i], 1);
             mbar_init(&st.segempty[i], SH::kReaders);
         }
-        mbar_init(&st.qfull, 128);
-        mbar_init(&st.qempty, SH::kStageInQ ? 10 : 2);  // both streams' score products (and epilogues)
+        mbar_init(&st.qfull, 256);
+        mbar_init(&st.qempty, 2);  // both streams' score products
         for (int i = 0; i < 2; ++i) {
             mbar_init(&st.sfull[i], 1);
             mbar_init(&st.pfull[i], 4);
             mbar_init(&st.drain[i], 1);
+            mbar_init(&st.turn[i], 1);
         }
         mbar_init(&st.odone, 2);
         mbar_init(&st.ofree, 8);
-        mbar_init(&st.mlfull, 4);
-        mbar_init(&st.mlfree, 4);
+        mbar_init(&st.mlfull, 8);
+        mbar_init(&st.mlfree, 8);
         st.abort = 0;
         for (int i = 0; i < 8; ++i) st.odd[i] = 0;
         mbar_fence_init();
@@ -485,19 +570,10 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         RingPos<RS> rpos;
         bool reuse = false;  // the ring has been filled once
         while (ok && next(g)) {
-            // the queries' buffer is free once the last segment's scores (and epilogue) are done
-            if (seg > 1 && !(ok = wait(&st.qempty, seg - 2))) break;
             const int nt = g.t1 - g.t0;
             // what the lane knows of its rows in tiles t, t + 1, t + 2 (addresses and scales are
             // fetched a tile ahead of their use)
             RowInfo x0 = row_info<Q8>(a, g, g.t0, w * 32 + lane), x1 = x0, x2 = x0;
-            for (int b = 0; b < g.weight; ++b) load_q<HD>(a, g, b, qbuf + b * TB, w, lane);
-            if (a.q_vec) {
-                cp_async_arrive(&st.qfull);
-            } else {
-                fence_async_proxy();
-                mbar_arrive(&st.qfull);
-            }
 #pragma unroll 1
             for (int l = 0; l < 2 * nt; ++l) {  // K0 K1 V0 K2 V1 ...
                 const bool val = tile_is_value(l, nt);
@@ -549,64 +625,92 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         const uint32_t id_pv = idesc_bf16_f32(128, HD) | (1u << 16);  // B is MN-major
         const uint32_t ts = tmem + gs * 128, to = tmem + 256 + gs * 128;
         const uint64_t ring_d = sw128_desc(smem_u32(ring)), ring_mn = sw128_desc_mn(smem_u32(ring), 16384);
+        // The streams take turns: a stream's P V and next Q K^T are issued together and run while the
+        // other's softmax does. (Issued side by side, both streams' products end together and then
+        // both softmaxes compete.) The warp runs as one, and one lane issues.
         RingPos<S> base;
-        uint32_t np = 0;
-        while (next(g)) {
-            if (lane == 0 && ok) {
-                const int nt = g.t1 - g.t0;
-                const bool pair = g.weight == 2;
-                const int step = pair ? 1 : 2, first = pair ? 0 : gs;
-                const uint64_t qd = sw128_desc(smem_u32(qbuf + (pair ? gs * TB : 0)));
-                const bool twice = MT == 2 && !pair;
-                RingPos<S> kp = base, vp = base;
-                kp.skip(first ? pos_k(first) : 0);
-                vp.skip(pos_v(first, nt));
-                if (first < nt) ok = wait(&st.qfull, seg - 1);
+        uint32_t np = 0, turn = 0;
+        while (ok && next(g)) {
+            const int nt = g.t1 - g.t0;
+            const bool pair = g.weight == 2;
+            const int step = pair ? 1 : 2, first = pair ? 0 : gs;
+            const uint64_t qd = sw128_desc(smem_u32(qbuf + (pair ? gs * TB : 0)));
+            const bool twice = MT == 2 && !pair;
+            RingPos<S> kp = base, vp = base;
+            kp.skip(first ? pos_k(first) : 0);
+            vp.skip(pos_v(first, nt));
+            if (first < nt) ok = wait(&st.qfull, seg - 1);
+            bool qdone = false;
+            // (both streams make the same number of rounds, the last of stream 1 may be empty)
 #pragma unroll 1
-                for (int tt = first - step; tt < nt && ok; tt += step) {  // O += P V of tile tt, S = Q K^T of the next
-                    if (tt >= first) {
-                        if (!(ok = wait(&st.pfull[gs], np))) break;
-                        ++np;
-                        if (tt == first && seg > 1 && !(ok = wait(&st.ofree, seg - 2))) break;
-                        if (!(ok = wait(&st.full[vp.slot], vp.phase))) break;
-                        fence_async_proxy();
-                        tc_fence_after();
-                        const uint64_t vd = ring_mn + (uint32_t)(vp.slot * (TB / 16));
+            for (int t0 = -step; t0 < nt && ok; t0 += step) {  // O += P V of tile tt, S = Q K^T of the next
+                const int tt = t0 + first;
+                const bool pv = t0 >= 0 && tt < nt, qk = tt + step < nt;
+                if (pv) {
+                    ok = ok && wait(&st.pfull[gs], np);
+                    ++np;
+                    if (t0 == 0 && seg > 1) ok = ok && wait(&st.ofree, seg - 2);
+                    ok = ok && wait(&st.full[vp.slot], vp.phase);
+                }
+                // a stream's turn; its K tile is waited for before the products if it is there already
+                if (gs == 1 || turn > 0) ok = ok && wait(&st.turn[gs], gs == 1 ? turn : turn - 1);
+                ++turn;
+                bool kthere = qk && mbar_try_wait(&st.full[kp.slot], kp.phase);
+                if (!__all_sync(0xffffffffu, ok)) {
+                    ok = false;
+                    break;
+                }
+                kthere = __all_sync(0xffffffffu, kthere);
+                fence_async_proxy();
+                tc_fence_after();
+                const bool leader = elect_one();
+                if (pv && leader) {
+                    const uint64_t vd = ring_mn + (uint32_t)(vp.slot * (TB / 16));
 #pragma unroll
-                        for (int k = 0; k < kTcTile / 16; ++k)
-                            tc_mma_ts(to, ts + k * 8, vd + k * 128, id_pv, tt > first || k ? 1u : 0u);
-                        tc_commit(&st.empty[vp.slot]);
-                        if (twice) tc_commit(&st.empty[vp.slot]);
-                        vp.skip(pos_v(min(tt + step, nt - 1), nt) - pos_v(tt, nt));
-                    }
-                    if (tt + step < nt) {
-                        if (!(ok = wait(&st.full[kp.slot], kp.phase))) break;
-                        fence_async_proxy();
-                        tc_fence_after();
+                    for (int k = 0; k < kTcTile / 16; ++k)
+                        tc_mma_ts(to, ts + k * 8, vd + k * 128, id_pv, t0 > 0 || k ? 1u : 0u);
+                }
+                if (qk && !kthere) {
+                    ok = __all_sync(0xffffffffu, wait(&st.full[kp.slot], kp.phase));
+                    if (!ok) break;
+                    fence_async_proxy();
+                    tc_fence_after();
+                }
+                if (leader) {
+                    if (qk) {
                         const uint64_t kd = ring_d + (uint32_t)(kp.slot * (TB / 16));
 #pragma unroll
                         for (int k = 0; k < HD / 16; ++k)  // 32 bytes a step, 16384 to the next 64 columns
                             tc_mma(ts, qd + (k >> 2) * 1024 + 2 * (k & 3), kd + (k >> 2) * 1024 + 2 * (k & 3), id_qk, k ? 1u : 0u);
                         tc_commit(&st.sfull[gs]);
+                    }
+                    mbar_arrive(&st.turn[gs ^ 1]);
+                    if (qk) {
                         tc_commit(&st.empty[kp.slot]);
                         if (twice) tc_commit(&st.empty[kp.slot]);
-                        kp.skip(2 * step - (tt + step == 0));
+                        if (tt + 2 * step >= nt) tc_commit(&st.qempty);
+                    }
+                    if (pv) {
+                        tc_commit(&st.empty[vp.slot]);
+                        if (twice) tc_commit(&st.empty[vp.slot]);
                     }
                 }
-                if (ok) {
-                    tc_commit(&st.qempty);
-                    tc_commit(&st.odone);
-                }
-                base.skip_long(2 * nt);
+                __syncwarp();
+                if (pv) vp.skip(pos_v(min(tt + step, nt - 1), nt) - pos_v(tt, nt));
+                if (qk) kp.skip(2 * step - (tt + step == 0));
+                qdone |= qk;
+            }
+            if (ok && elect_one()) {
+                if (!qdone) tc_commit(&st.qempty);
+                tc_commit(&st.odone);
             }
             __syncwarp();
+            base.skip_long(2 * nt);
         }
         // every MMA issued has finished reading shared memory and TMEM before the CTA ends
-        if (lane == 0) {
-            tc_commit(&st.drain[gs]);
-            mbar_wait(&st.drain[gs], 0, a.status, 100000000LL);
-        }
+        if (elect_one()) tc_commit(&st.drain[gs]);
         __syncwarp();
+        mbar_wait(&st.drain[gs], 0, a.status, 100000000LL);
     } else if (warp == 14) {  // ---- the plan
         const PlanArgs pa = plan_args(a);
         bool bad = false;
@@ -674,7 +778,23 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         const uint32_t ts = tmem + gs * 128 + lanes, to = tmem + 256 + gs * 128 + lanes;
         const float scale2 = a.scale * kLog2e;
         uint32_t ns = 0, nj = 0;  // score blocks taken, joins of the streams
-        while (ok && next(g)) {
+        // the warp's part of segment s's queries: rows of its own block, or half of the only one
+        auto queries = [&](const Segment& s) {
+            if (s.weight == 2 || gs == 0)
+                load_q<HD>(a, s, s.m * kAttnItemRows + gs * 128 + wl * 32, qbuf + gs * TB, wl, lane);
+            if (a.q_vec) {
+                cp_async_arrive(&st.qfull);
+            } else {
+                fence_async_proxy();
+                mbar_arrive(&st.qfull);
+            }
+        };
+        Segment g2;  // the segment after this one, once its queries are on their way
+        bool more = next(g2);
+        if (more) queries(g2);
+        while (more) {
+            g = g2;
+            const uint32_t cur = seg - 1;  // this segment's number
             const int nt = g.t1 - g.t0;
             const bool pair = g.weight == 2;
             const int row = g.m * kAttnItemRows + (pair ? gs * 128 : 0) + wl * 32 + lane;  // of the item's head
@@ -702,59 +822,32 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         }
                         tc_wait_st();
                     }
-                    if (tt < 2 && (tt == 0 || !pair)) {  // the stream's first tile: its own maximum
-                        float mx = -INFINITY;
-#pragma unroll 1
-                        for (int c = 0; c < kTcTile; c += 32) {
-                            float x[32];
-                            tc_ld32(ts + c, x);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) mx = fmaxf(mx, x[e]);
-                        }
-                        m = mx * scale2;
-                    }
-                    uint32_t pk[kTcTile / 2];  // the row's probabilities
-                    float z;
-#pragma unroll 1
-                    while (true) {  // twice at most: again if the maximum has outgrown the reference
-                        const float ms = m == -INFINITY ? 0.f : m;
-                        const float mx = softmax_row(ts, scale2, -ms, pk, z) * scale2;
-                        if (!__any_sync(0xffffffffu, mx > m + 8.f)) break;
-                        const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
-                        sum *= f;
-                        m = mn;
-#pragma unroll 1
-                        for (int c = 0; c < HD; c += 16) {
-                            float o[16];
-                            uint32_t u[16];
-                            tc_ld16(to + c, o);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(o[e] * f);
-                            tc_st16(to + c, u);
-                        }
-                    }
-                    sum += z;
-#pragma unroll
-                    for (int c = 0; c < kTcTile / 2; c += 16) tc_st16(ts + c, pk + c);
+                    softmax_row<HD>(ts, to, scale2, tt < 2 && (tt == 0 || !pair), m, sum);
                     tc_wait_st();
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&st.pfull[gs]);
             }
+            // the next segment's queries may come once this one's scores are all done
+            if (!ok) break;
+            more = next(g2);
+            if (more && !SH::kStageInQ) {
+                if (!(ok = wait(&st.qempty, cur))) break;
+                queries(g2);
+            }
             // ---- the segment's result
-            if (!ok || !(ok = wait(&st.odone, seg - 1))) break;
+            if (!(ok = wait(&st.odone, cur))) break;
             tc_fence_after();
-            float f0 = 1.f, f1 = 0.f;  // weights of this stream's block, and of stream 1's (alternating)
+            float f0 = 1.f, f1 = 0.f;  // weights of this stream's block, and of the other's (alternating)
             const bool join = !pair && nt > 1;
-            if (join && gs == 1) {
+            if (join) {
                 if (nj > 0 && !(ok = wait(&st.mlfree, nj - 1))) break;
-                st.ml[wl * 32 + lane] = make_float2(m, sum);
+                st.ml[gs][wl * 32 + lane] = make_float2(m, sum);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&st.mlfull);
-            } else if (join) {
                 if (!(ok = wait(&st.mlfull, nj))) break;
-                const float2 o = st.ml[wl * 32 + lane];
+                const float2 o = st.ml[gs ^ 1][wl * 32 + lane];
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&st.mlfree);
                 const float mn = fmaxf(m, o.x), ms = mn == -INFINITY ? 0.f : mn;
@@ -764,10 +857,11 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 m = mn;
             }
             nj += join;
-            if (!idle && (pair || gs == 0)) {
+            // (a joined block's columns are shared out between the streams' warps)
+            if (!idle && (pair || join || gs == 0)) {
                 // rows leave through shared memory, 16 columns at a time, so that a warp writes whole
                 // sectors: the lanes' rows as addresses of the output or of the partial
-                unsigned char* stage = stages + warp * (SH::kStageInQ ? MT * TB / 8 : 2048);
+                unsigned char* stage = stages + warp * (SH::kStageInQ ? TB / 4 : 2048);
                 const int head = g.h * a.G + row % a.G;
                 const int64_t pr = ((int64_t)blockIdx.x * 2 + g.slot) * kAttnItemRows + (row - g.m * kAttnItemRows);
                 const unsigned long long mine =
@@ -780,15 +874,20 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     f1 = sum == 0.f ? 0.f : f1 / sum;
                 }
                 const bool zero = g.whole && sum == 0.f;
+                const uint32_t other = tmem + 256 + (gs ^ 1) * 128 + lanes;
 #pragma unroll 1
-                for (int c = 0; c < HD; c += 16) {
+                for (int c = join && gs ? HD / 2 : 0; c < (join && !gs ? HD / 2 : HD); c += 16) {
+                    uint32_t u[16], v[16];
                     float o[16];
-                    tc_ld16(to + c, o);
-                    if (join) {
-                        float p[16];
-                        tc_ld16(to + 128 + c, p);
+                    tc_ld16_start(to + c, u);
+                    if (join) tc_ld16_start(other + c, v);
+                    tc_ld16_wait(u);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = o[e] * f0 + p[e] * f1;
+                    for (int e = 0; e < 16; ++e) o[e] = __uint_as_float(u[e]);
+                    if (join) {
+                        tc_ld16_wait(v);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) o[e] = o[e] * f0 + __uint_as_float(v[e]) * f1;
                     } else if (g.whole) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) o[e] *= f0;
@@ -808,13 +907,13 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         for (int k = 0; k < 2; ++k) {  // two lanes a row
                             const int r = k * 16 + lane / 2, h = lane & 1;
                             bf16_t* dst = (bf16_t*)__shfl_sync(0xffffffffu, mine, r);
-                            const uint4 v = *reinterpret_cast<const uint4*>(stage + r * 32 + ((h ^ (r >> 2)) & 1) * 16);
+                            const uint4 y = *reinterpret_cast<const uint4*>(stage + r * 32 + ((h ^ (r >> 2)) & 1) * 16);
                             if (dst) {
                                 dst += c + 8 * h;
                                 if (a.out_vec) {
-                                    *reinterpret_cast<uint4*>(dst) = v;
+                                    *reinterpret_cast<uint4*>(dst) = y;
                                 } else {
-                                    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+                                    const uint32_t x[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                                     for (int e = 0; e < 8; ++e) dst[e].bits = (uint16_t)(x[e / 2] >> (16 * (e & 1)));
                                 }
@@ -830,28 +929,34 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         for (int k = 0; k < 4; ++k) {  // four lanes a row
                             const int r = k * 8 + lane / 4, h = lane & 3;
                             float* dst = (float*)__shfl_sync(0xffffffffu, mine, r);
-                            const float4 v = *reinterpret_cast<const float4*>(stage + r * 64 + ((h ^ (r >> 1)) & 3) * 16);
-                            if (dst) *reinterpret_cast<float4*>(dst + c + 4 * h) = v;
+                            const float4 y = *reinterpret_cast<const float4*>(stage + r * 64 + ((h ^ (r >> 1)) & 3) * 16);
+                            if (dst) *reinterpret_cast<float4*>(dst + c + 4 * h) = y;
                         }
                     }
                 }
                 __syncwarp();
-                if (live) {
+                if (live && (pair || gs == 0)) {
                     if (!g.whole)
                         *reinterpret_cast<float2*>(a.part_ml + 2 * pr) = make_float2(m, sum);
                     else if (a.lse)
                         a.lse[((int64_t)g.b * a.T + node) * a.H + head] =
                             sum == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(sum);
-                    if (*(volatile int*)&st.odd[(seg - 1) & 7]) put_odd_columns<HD, Q8>(a, g, node, head, m, (void*)mine);
                 }
+                if (live && *(volatile int*)&st.odd[cur & 7])
+                    put_odd_columns<HD, Q8>(a, g, node, head, m, (void*)mine, join && gs ? HD / 2 : 0, join && !gs ? HD / 2 : HD);
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                // (the loaders are at most two segments ahead, the other stream at most one behind)
-                if (warp == 0) st.odd[(seg + 3) & 7] = 0;
+                // (the next segment's first value tile is not released yet, so the ring lets the loaders
+                // be at most three segments ahead; the other stream is at most one behind)
+                if (warp == 0) st.odd[(cur + 4) & 7] = 0;
                 mbar_arrive(&st.ofree);
-                if (SH::kStageInQ) mbar_arrive(&st.qempty);
+            }
+            if (SH::kStageInQ && more) {
+                // the buffer held this segment's staged rows
+                if (!(ok = wait(&st.ofree, cur))) break;
+                queries(g2);
             }
         }
     }
