@@ -41,10 +41,13 @@ __device__ __forceinline__ SeqLen seq_len(const PlanArgs& a, int b, bool* bad = 
 }
 
 // ROWS rows an item, TN slots a tile; PAIR: an item of more than 128 rows costs two units a tile.
+// An item begins with OVER units that hold no tile: what starting and finishing it costs a CTA, in
+// units, so that a CTA with many short items does not end after one with few long ones.
 // Units are counted in 32 bits (the launch refuses shapes that could pass 2^31): this runs once a
 // CTA before anything else can start, and short code is what it takes to be quick.
-template <int ROWS, int TN, bool PAIR>
+template <int ROWS, int TN, bool PAIR, int OVER>
 struct Plan {
+    static constexpr int kOver = OVER;
     __host__ __device__ __forceinline__ static int blocks(int rows) { return (rows + ROWS - 1) / ROWS; }
     __device__ __forceinline__ static int weight(int rows, int m) { return PAIR && rows - m * ROWS > 128 ? 2 : 1; }
     // slots that block m's rows may see: [0, end)
@@ -61,19 +64,22 @@ struct Plan {
         const int rows = s.n * a.G, nb = blocks(rows);
         if (nb == 0) return 0;
         if (!a.causal)  // every block but the last is full
-            return tiles(a, s, 0) * ((nb - 1) * weight(ROWS, 0) + weight(rows, nb - 1));
-        int u = 0;
+            return nb * OVER + tiles(a, s, 0) * ((nb - 1) * weight(ROWS, 0) + weight(rows, nb - 1));
+        int u = nb * OVER;
 #pragma unroll 1
         for (int m = 0; m < nb; ++m) u += tiles(a, s, m) * weight(rows, m);
         return u;
     }
-    // first tile of an item (first unit s0, weight w = 1 or 2, nt tiles) that starts at unit u0 or later
+    // units of an item of nt tiles of weight w = 1 or 2; the unit where tile t starts
+    __device__ __forceinline__ static int units(int w, int nt) { return OVER + w * nt; }
+    __device__ __forceinline__ static int tile_unit(int s0, int w, int t) { return s0 + OVER + w * t; }
+    // first tile of an item with first unit s0 that starts at unit u0 or later
     __device__ __forceinline__ static int first_tile(int s0, int w, int nt, int u0) {
-        return u0 <= s0 ? 0 : min((u0 - s0 + w - 1) >> (w - 1), nt);
+        return u0 <= s0 + OVER ? 0 : min((u0 - s0 - OVER + w - 1) >> (w - 1), nt);
     }
     // whether every call of this shape keeps its units within 32 bits
     static bool fits(int B, int Hkv, int64_t rows, int max_seq) {
-        const double u = 2.0 * B * Hkv * (double)((rows + ROWS - 1) / ROWS) * (double)(max_seq / TN + 1);
+        const double u = 2.0 * B * Hkv * (double)((rows + ROWS - 1) / ROWS) * (double)(max_seq / TN + 1 + OVER);
         return u < 2147483647.0;
     }
 };
@@ -113,12 +119,14 @@ struct Place {
 
     __device__ __forceinline__ static Place find(const PlanArgs& a, int c, int ncta, bool* bad = nullptr) {
         const int lane = threadIdx.x & 31;
-        // units of all sequences; the first 32 sequences' stay in registers
-        const SeqLen sl0 = lane < a.B ? seq_len(a, lane, bad) : SeqLen{0, 0};
-        const int w0 = PL::head_units(a, sl0);
-        int U = w0;
+        SeqLen sl;
+        int hu = 0, U = 0;
 #pragma unroll 1
-        for (int bb = lane + 32; bb < a.B; bb += 32) U += PL::head_units(a, seq_len(a, bb, bad));
+        for (int b0 = (a.B - 1) & ~31; b0 >= 0; b0 -= 32) {  // (ends with the first 32's in sl and hu)
+            sl = b0 + lane < a.B ? seq_len(a, b0 + lane, bad) : SeqLen{0, 0};
+            hu = PL::head_units(a, sl);
+            U += hu;
+        }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
         U *= a.Hkv;
@@ -129,8 +137,6 @@ struct Place {
         int base = 0;
 #pragma unroll 1
         for (int b0 = 0; b0 < a.B; b0 += 32) {
-            SeqLen sl = sl0;
-            int hu = w0;
             if (b0) {
                 sl = b0 + lane < a.B ? seq_len(a, b0 + lane) : SeqLen{0, 0};
                 hu = PL::head_units(a, sl);
@@ -159,7 +165,7 @@ struct Place {
         // the block of the head
 #pragma unroll 1
         while (true) {
-            const int w = PL::tiles(a, p.s, p.m) * PL::weight(p.s.n * a.G, p.m);
+            const int w = PL::units(PL::weight(p.s.n * a.G, p.m), PL::tiles(a, p.s, p.m));
             if (p.s0 + w > u0) return p;
             p.s0 += w;
             ++p.m;
@@ -206,7 +212,7 @@ struct SegmentWalk {
                     g.whole = g.t0 == 0 && g.t1 == nt;
                     g.slot = g.t0 == 0 ? 1 : 0;
                 }
-                pos += nt * w;
+                pos += PL::units(w, nt);
             }
             if (++m >= PL::blocks(rows)) {
                 m = 0;

@@ -66,6 +66,8 @@ struct TreeAttnArgs {
     float *part_o, *part_ml;  // per CTA two partial items: [2 G][rows][hd] sums, [2 G][rows][2] (max, sum)
     int* status;
     int q_vec, out_vec;  // rows of q / out on 16-byte boundaries
+    int box_rows;        // cache rows of a TMA box (0: no tensor maps)
+    int q_tma;           // the queries come by TMA too
 };
 
 // rows of an attention item whose partial results the workspace holds, per CTA and slot

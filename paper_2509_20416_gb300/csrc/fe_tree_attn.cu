@@ -38,8 +38,8 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __gr
     const int rows = w.s.n * a.G, nrow = min(ROWS, rows - w.m * ROWS);
     const int wt = PL::weight(rows, w.m), nt = PL::tiles(pa, w.s, w.m);
     if (w.s0 >= w.cut.begin(blockIdx.x + 1)) return;  // the item starts there: not split
-    if (w.cut.owner(w.s0) != (int)blockIdx.x) return;  // an earlier block's item
-    const int c1 = w.cut.owner(w.s0 + (nt - 1) * wt);
+    if (w.cut.owner(PL::tile_unit(w.s0, wt, 0)) != (int)blockIdx.x) return;  // an earlier block's item
+    const int c1 = w.cut.owner(PL::tile_unit(w.s0, wt, nt - 1));
     if (c1 == (int)blockIdx.x) return;
     for (int r = wid; r < nrow; r += kJoinShares * kJoinWarps) {
         // the partials' row of contributor c, or -1 if no tile starts in c's units
@@ -103,10 +103,75 @@ cudaError_t launch_simt(const TreeAttnArgs& a, int num_sms, cudaStream_t st) {
     return launch_join<float, HD, SimtPlan, kSimtRows>(a, num_sms, st);
 }
 
+// cuTensorMapEncodeTiled, looked up once (the library does not link the driver)
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess) return (EncodeTiled) nullptr;
+        return r == cudaDriverEntryPointSuccess ? (EncodeTiled)p : nullptr;
+    }();
+    return fn;
+}
+
+// Rows of a TMA box: a bfloat16 cache's tiles of 128 slots come in boxes that lie inside one page
+// and fill whole 8-row swizzle groups; 0 where no such box exists (pages of other sizes, caches of
+// less than a tile), and the loaders' copies do it all.
+int tma_box_rows(const CacheView& c, int groups) {
+    if (groups <= 0) return 0;
+    if (c.page_size == 0) return c.max_seq >= kTcTile ? kTcTile : 0;
+    int b = kTcTile;
+    while (c.page_size % b) b /= 2;
+    return b >= 8 ? b : 0;
+}
+
+// The cache as [groups][rows][hd], rows of a page or sequence, groups = (pages or sequences) x heads
+bool make_map(CUtensorMap* map, const void* base, int hd, int rows, int groups, int box_rows) {
+    const cuuint64_t dims[3] = {(cuuint64_t)hd, (cuuint64_t)rows, (cuuint64_t)groups};
+    const cuuint64_t strides[2] = {(cuuint64_t)hd * 2, (cuuint64_t)rows * hd * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+    const EncodeTiled encode = encode_tiled();
+    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The queries as [B][T][H][hd]; a block of 128 rows is a box of G heads and 128 / G nodes, where G
+// is a power of two and the strides are what a map can hold (whole 16 bytes, as they mostly are).
+bool make_q_map(CUtensorMap* map, const TreeAttnArgs& a, int hd) {
+    if (!a.q_vec || a.G > 128 || 128 % a.G) return false;
+    cuuint64_t strides[3] = {(cuuint64_t)a.q.head * 2, (cuuint64_t)a.q.token * 2, (cuuint64_t)a.q.batch * 2};
+    const cuuint64_t dims[4] = {(cuuint64_t)hd, (cuuint64_t)a.H, (cuuint64_t)a.T, (cuuint64_t)a.B};
+    for (int i = 0; i < 3; ++i) {
+        if (dims[i + 1] == 1) strides[i] = (cuuint64_t)hd * 2;  // (an extent of 1: the stride is not used)
+        if ((int64_t)strides[i] <= 0 || strides[i] >= (cuuint64_t)1 << 40) return false;
+    }
+    const cuuint32_t box[4] = {64, (cuuint32_t)a.G, (cuuint32_t)(128 / a.G), 1}, step[4] = {1, 1, 1, 1};
+    const EncodeTiled encode = encode_tiled();
+    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, a.q.p, dims, strides, box, step,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int HD, bool Q8, int MT>
-cudaError_t launch_tc(const TreeAttnArgs& a, int num_sms, cudaStream_t st) {
+cudaError_t launch_tc(const TreeAttnArgs& args, int num_sms, cudaStream_t st) {
+    TreeAttnArgs a = args;
+    CUtensorMap kmap{}, vmap{}, qmap{};
+    a.q_tma = make_q_map(&qmap, a, HD);
+    if (!Q8) {
+        const CacheView& c = a.cache;
+        const int64_t groups = (int64_t)(c.page_size ? c.n_pages : a.B) * a.Hkv;
+        a.box_rows = tma_box_rows(c, groups < 0x7FFFFFFF ? (int)groups : 0);
+        const int rows = c.page_size ? c.page_size : c.max_seq;
+        if (a.box_rows && !(make_map(&kmap, c.k, HD, rows, (int)groups, a.box_rows) &&
+                            make_map(&vmap, c.v, HD, rows, (int)groups, a.box_rows)))
+            return cudaErrorInvalidValue;
+    }
     const cudaError_t e = launch_k(tree_attn_tc_kernel<HD, Q8, MT>, dim3(num_sms), dim3(TcShape<HD, Q8, MT>::kThreads),
-                                   tc_smem<HD, Q8, MT>(), st, false, a);
+                                   tc_smem<HD, Q8, MT>(), st, false, a, kmap, vmap, qmap);
     if (e != cudaSuccess) return e;
     return launch_join<bf16_t, HD, TcPlan, kAttnItemRows>(a, num_sms, st);
 }

@@ -13,7 +13,7 @@
 namespace fe {
 
 constexpr int kSimtRows = 64, kSimtTile = 64, kSimtThreads = 256;
-using SimtPlan = Plan<kSimtRows, kSimtTile, false>;
+using SimtPlan = Plan<kSimtRows, kSimtTile, false, 1>;
 
 template <int HD>
 struct SimtSmem {

@@ -17,9 +17,12 @@
 //                    next segment's while this one's last product runs, and write the results
 //   warps 8-11       loaders: rows from the cache into 128-byte-swizzled tiles of 128 slots (K and
 //                    V alike, [slot][hd]), by cp.async, or converted from e4m3 on the way
-//   warp 12          issues the MMAs: S = Q K^T (K-major operands), O += P V with P (bfloat16)
-//                    read from TMEM over S's own columns and V as the MN-major operand
-//   warp 13          e4m3: bulk copies of the raw rows (runs of rows are contiguous in a page)
+//   warps 12, 13     issue the MMAs of stream 0, 1: S = Q K^T (K-major operands), O += P V with P
+//                    (bfloat16) read from TMEM over S's own columns and V as the MN-major operand
+//   warp 14          plans: the CTA's segments (shares of items), a few ahead of their use
+//   warp 15          TMA: whole bfloat16 tiles of prefix slots, in boxes of a page's rows (the loaders
+//                    then fetch only the tiles that reach into the nodes' rows; all of them where the
+//                    pages' size has no such box); e4m3: bulk copies of the raw rows
 // The softmax keeps a reference maximum per row and rescales O only when the maximum has grown by
 // more than 2^8 (the probabilities then stay below 2^8, where bfloat16 is as precise as below 1):
 // after the first tiles that is rare; it saves a pass over O per tile and a pass over the scores
@@ -31,6 +34,8 @@
 // adds their terms to the rows that do see them.
 #pragma once
 
+#include <cuda.h>
+
 #include "fe_attn_plan.cuh"
 #include "fe_stream.cuh"
 #include "fe_tc.cuh"
@@ -38,7 +43,7 @@
 namespace fe {
 
 constexpr int kTcTile = 128;
-using TcPlan = Plan<kAttnItemRows, kTcTile, true>;
+using TcPlan = Plan<kAttnItemRows, kTcTile, true, 4>;
 
 // MT: 128-row query blocks a CTA must hold (1 when no item has more than 128 rows)
 template <int HD, bool Q8, int MT>
@@ -51,8 +56,8 @@ struct TcShape {
     // whose next load then waits for the epilogue
     static constexpr bool kStageInQ = Q8 && MT == 2 && HD == 128;
     static constexpr int kStageBytes = kStageInQ ? 0 : 8 * 2048;
-    static constexpr int kThreads = Q8 ? 512 : 480;
-    static constexpr int kReaders = Q8 ? 15 : 14;  // warps that read the segments
+    static constexpr int kThreads = 512;
+    static constexpr int kReaders = 15;  // warps that read the segments
     static constexpr int kData = MT * kTileBytes + kSlots * kTileBytes + kRawSlots * kRawBytes + kStageBytes;
 };
 
@@ -84,6 +89,26 @@ __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// arrive on `bar` n times
+__device__ __forceinline__ void mbar_arrive_n(uint64_t* bar, uint32_t n) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
+}
+
+// one box of a 3-D tensor map to shared memory, its bytes counted on `bar`
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+        : "memory");
+}
 
 // true in one lane of a converged warp (the same lane every time)
 __device__ __forceinline__ bool elect_one() {
@@ -123,22 +148,38 @@ __device__ __noinline__ bool tc_wait_slow(uint64_t* bar, uint32_t parity, int* s
     return mbar_wait_abortable(bar, parity, status, abort);
 }
 
-// The slots of [s0, s0 + 32) that node `node` sees, as bits.
-__device__ __noinline__ uint32_t seen_bits(const TreeAttnArgs& a, const Segment& g, int node, int s0) {
+// The slots of [s0, s0 + 128) that node `node` sees, as bits (x: the first 64).
+__device__ __noinline__ ulonglong2 seen_bits(const TreeAttnArgs& a, const Segment& g, int node, int s0) {
     const int P = g.s.P;
-    auto ones = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
-    if (!a.mask) return ones(min(P + node + 1, g.end) - s0);
-    uint32_t w = ones(P - s0);
-    const uint8_t* row = a.mask + ((int64_t)g.b * a.T + node) * a.T - P + s0;
-    const int lo = max(P - s0, 0), hi = min(g.end - s0, 32);
-    for (int j0 = lo; j0 < hi; j0 += 8) {  // eight loads at a time
-        uint8_t v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = j0 + k < hi ? row[j0 + k] : 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) w |= v[k] ? 1u << ((j0 + k) & 31) : 0u;
+    auto ones = [](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; };
+    if (!a.mask) {
+        const int n = min(P + node + 1, g.end) - s0;
+        return make_ulonglong2(ones(n), ones(n - 64));
     }
-    return w;
+    const int lo = max(P - s0, 0), hi = min(g.end - s0, kTcTile);  // the nodes' slots in the tile
+    // their bytes, in aligned words (the first and last may hold up to three neighbouring bytes)
+    const uint8_t* row = a.mask + ((int64_t)g.b * a.T + node) * a.T - P + s0;  // slot s0's byte
+    ulonglong2 w = make_ulonglong2(0ull, 0ull);
+    int c = lo - (int)((uintptr_t)(row + lo) & 3);  // a word's first slot
+#pragma unroll 1
+    for (; c < hi; c += 32) {
+        uint32_t v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c + 4 * k < hi ? *reinterpret_cast<const uint32_t*>(row + c + 4 * k) : 0u;
+        uint32_t bits = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {  // bytes that are not zero
+            const uint32_t z = (((v[k] & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | v[k]) >> 7 & 0x01010101u;
+            bits |= (z * 0x01020408u >> 24) << (4 * k);
+        }
+        const unsigned long long b = bits;
+        if (c < 0) w.x |= b >> -c;
+        else if (c < 64) w.x |= b << c;
+        else w.y |= b << (c - 64);
+        if (c > 32 && c < 64) w.y |= b >> (64 - c);
+    }
+    // (bits below the first node's slot came from neighbouring bytes: those slots are the prefix's)
+    return make_ulonglong2((w.x & ones(hi)) | ones(lo), (w.y & ones(hi - 64)) | ones(lo - 64));
 }
 
 // ---- loaders ------------------------------------------------------------------------------------
@@ -167,7 +208,7 @@ __device__ __forceinline__ RowInfo row_info(const TreeAttnArgs& a, const Segment
 // A warp's 32 query rows (rows r0 ..) into rows w * 32 .. of a swizzled K-major tile; rows past
 // the item's are zero.
 template <int HD>
-__device__ __forceinline__ void load_q(const TreeAttnArgs& a, const Segment& g, int r0, unsigned char* dst, int w, int lane) {
+__device__ __noinline__ void load_q(const TreeAttnArgs& a, const Segment& g, int r0, unsigned char* dst, int w, int lane) {
     constexpr int CH = HD / 8, RP = 32 / CH;  // 16-byte chunks a row, rows a warp access
     const int c = lane % CH, row = r0 + lane;
     unsigned long long mine = 0;
@@ -363,30 +404,57 @@ __device__ __forceinline__ uint64_t add_x2(uint64_t a, uint64_t b) {
     return d;
 }
 
+__device__ __forceinline__ float max32(const uint32_t* x) {
+    float mx = __uint_as_float(x[0]), my = __uint_as_float(x[1]);
+#pragma unroll
+    for (int e = 2; e < 30; e += 4) {
+        mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+        my = max3(my, __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
+    }
+    mx = max3(mx, __uint_as_float(x[30]), __uint_as_float(x[31]));
+    return fmaxf(mx, my);
+}
+
+// The rows of a warp move to references grown by log2(1 / f): the np packed columns of probabilities
+// written so far at ts and the no columns of O at `to` times f. (Rare, hence a call.)
+__device__ __noinline__ void rescale_row(uint32_t ts, int np, uint32_t to, int no, float f) {
+    uint32_t u[16];
+#pragma unroll 1
+    for (int k = 0; k < np; k += 16) {
+        tc_ld16_start(ts + k, u);
+        tc_ld16_wait(u);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            u[e] = pack_bf16(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xFFFF0000u) * f);
+        tc_st16(ts + k, u);
+    }
+#pragma unroll 1
+    for (int k = 0; k < no; k += 16) {
+        tc_ld16_start(to + k, u);
+        tc_ld16_wait(u);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * f);
+        tc_st16(to + k, u);
+    }
+}
+
 // One row's softmax of a tile, in one pass over its 128 scores x at TMEM columns ts: 2^(scale2 x - m)
 // as packed bfloat16 over the first 64 columns (32 scores become 16 columns, always behind what is
 // still to be read), their float32 sum added to `sum`. m is the row's reference maximum; when some
-// row of the warp has outgrown it by more than 2^8, the warp moves to new references on the spot,
-// rescaling the sums, the columns written so far and, unless this is the stream's first tile, O.
-// A loop with a short body: the CTA's roles share the instruction caches, and unrolled rows made
-// every one of them wait for fetches.
+// row of the warp has outgrown it by more than 2^8, the warp moves to new references on the spot.
+// Bound by the exponentials (16 a clock and SM), in whose shade the next 32 scores are loaded and
+// their maximum taken. A loop with a short body: the CTA's roles share the instruction caches, and
+// unrolled rows made every one of them wait for fetches.
 template <int HD>
 __device__ __forceinline__ void softmax_row(uint32_t ts, uint32_t to, float scale2, bool first, float& m, float& sum) {
     const uint64_t sc = pair_f32(__float_as_uint(scale2), __float_as_uint(scale2));
-    uint32_t x[32];
+    uint32_t x[32], y[32];
     uint64_t z[2] = {0, 0};
     tc_ld32_start(ts, x);
+    tc_ld32_wait(x);
+    float mx = max32(x) * scale2;
 #pragma unroll 1
     for (int c = 0; c < kTcTile; c += 32) {
-        tc_ld32_wait(x);
-        float mx = __uint_as_float(x[0]), my = __uint_as_float(x[1]);
-#pragma unroll
-        for (int e = 2; e < 30; e += 4) {
-            mx = max3(mx, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
-            my = max3(my, __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
-        }
-        mx = max3(mx, __uint_as_float(x[30]), __uint_as_float(x[31]));
-        mx = fmaxf(mx, my) * scale2;
         if (__any_sync(0xffffffffu, mx > m + 8.f)) {
             const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
             const uint64_t ff = pair_f32(__float_as_uint(f), __float_as_uint(f));
@@ -394,40 +462,29 @@ __device__ __forceinline__ void softmax_row(uint32_t ts, uint32_t to, float scal
             z[1] = fma_x2(z[1], ff, 0);
             sum *= f;
             m = mn;
-#pragma unroll 1
-            for (int k = 0; k < c / 2; k += 16) {
-                uint32_t u[16];
-                tc_ld16_start(ts + k, u);
-                tc_ld16_wait(u);
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    u[e] = pack_bf16(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xFFFF0000u) * f);
-                tc_st16(ts + k, u);
-            }
-            if (!first) {
-#pragma unroll 1
-                for (int k = 0; k < HD; k += 16) {
-                    uint32_t u[16];
-                    tc_ld16_start(to + k, u);
-                    tc_ld16_wait(u);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * f);
-                    tc_st16(to + k, u);
-                }
-            }
+            rescale_row(ts, c / 2, to, first ? 0 : HD, f);
         }
         const float shift = m == -INFINITY ? 0.f : -m;
         const uint64_t sh = pair_f32(__float_as_uint(shift), __float_as_uint(shift));
         uint32_t pk[16];
+        auto exps = [&](int e0) {
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) {
-            const uint64_t y = fma_x2(pair_f32(x[e], x[e + 1]), sc, sh);
-            const float p0 = ex2_approx(__uint_as_float((uint32_t)y)), p1 = ex2_approx(__uint_as_float((uint32_t)(y >> 32)));
-            z[(e >> 1) & 1] = add_x2(z[(e >> 1) & 1], pair_f32(__float_as_uint(p0), __float_as_uint(p1)));
-            pk[e / 2] = pack_bf16(p0, p1);
-        }
-        if (c + 32 < kTcTile) tc_ld32_start(ts + c + 32, x);
+            for (int e = e0; e < e0 + 16; e += 2) {
+                const uint64_t v = fma_x2(pair_f32(x[e], x[e + 1]), sc, sh);
+                const float p0 = ex2_approx(__uint_as_float((uint32_t)v)), p1 = ex2_approx(__uint_as_float((uint32_t)(v >> 32)));
+                z[(e >> 1) & 1] = add_x2(z[(e >> 1) & 1], pair_f32(__float_as_uint(p0), __float_as_uint(p1)));
+                pk[e / 2] = pack_bf16(p0, p1);
+            }
+        };
+        // (past the last column the first ones are loaded again, and not used)
+        tc_ld32_start(ts + (c + 32) % kTcTile, y);
+        exps(0);
+        tc_ld32_wait(y);
+        exps(16);
+        mx = max32(y) * scale2;
         tc_st16(ts + c / 2, pk);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = y[e];
     }
     const uint64_t zz = add_x2(z[0], z[1]);
     sum += __uint_as_float((uint32_t)zz) + __uint_as_float((uint32_t)(zz >> 32));
@@ -462,7 +519,7 @@ __device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segmen
                 return Storage<bf16_t>::load((const bf16_t*)p, x.row * HD + k);
             };
             const float v = at(a.cache.v, x.vs, e);
-            if (finite_f32(v) || !(seen_bits(a, g, node, s) & 1u)) continue;
+            if (finite_f32(v) || !(seen_bits(a, g, node, s).x & 1ull)) continue;
             float dot = 0.f;
 #pragma unroll 1
             for (int k = 0; k < HD; ++k) dot = fmaf(Storage<bf16_t>::load(q, k), at(a.cache.k, x.ks, k), dot);
@@ -473,6 +530,11 @@ __device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segmen
         if (g.whole) store_one((bf16_t*)dst + e, t);
         else ((float*)dst)[e] = t;
     }
+}
+
+// Whether tile t of the segment (from its first) comes by TMA: a whole tile of prefix slots.
+__device__ __forceinline__ bool by_tma(const TreeAttnArgs& a, const Segment& g, int t) {
+    return a.box_rows > 0 && (g.t0 + t + 1) * kTcTile <= g.s.P;
 }
 
 // A position in the ring of tiles: slot and phase, moved on by small steps without division.
@@ -498,7 +560,8 @@ struct RingPos {
 // ---- the kernel -----------------------------------------------------------------------------------
 template <int HD, bool Q8, int MT>
 __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
-    tree_attn_tc_kernel(const __grid_constant__ TreeAttnArgs a) {
+    tree_attn_tc_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ CUtensorMap kmap,
+                        const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap) {
     using SH = TcShape<HD, Q8, MT>;
     constexpr int S = SH::kSlots, RS = Q8 ? SH::kRawSlots : 1, TB = SH::kTileBytes;
     extern __shared__ __align__(1024) unsigned char qbuf[];
@@ -573,7 +636,9 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             const int nt = g.t1 - g.t0;
             // what the lane knows of its rows in tiles t, t + 1, t + 2 (addresses and scales are
             // fetched a tile ahead of their use)
-            RowInfo x0 = row_info<Q8>(a, g, g.t0, w * 32 + lane), x1 = x0, x2 = x0;
+            RowInfo x0{-1, 0.f, 0.f};
+            if (!by_tma(a, g, 0)) x0 = row_info<Q8>(a, g, g.t0, w * 32 + lane);
+            RowInfo x1 = x0, x2 = x0;
 #pragma unroll 1
             for (int l = 0; l < 2 * nt; ++l) {  // K0 K1 V0 K2 V1 ...
                 const bool val = tile_is_value(l, nt);
@@ -581,7 +646,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 if (!val) {
                     x0 = x1;
                     x1 = l == 0 ? x0 : x2;
-                    x2 = row_info<Q8>(a, g, g.t0 + tt + 1, w * 32 + lane);
+                    if (!by_tma(a, g, tt + 1)) x2 = row_info<Q8>(a, g, g.t0 + tt + 1, w * 32 + lane);
                 }
                 // (a key tile tt is loaded with x1's rows; the value tile loaded after it is tt - 1,
                 // the last one tt)
@@ -592,7 +657,14 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 if constexpr (Q8) {
                     if (!(ok = wait(&st.rawfull[rpos.slot], rpos.phase))) break;
                 }
+                // (every slot's release is waited for, also of tiles that come by TMA: a barrier's phase is
+                // one bit, and a role that skipped one could take an older release for the one it needs)
                 if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
+                if (!Q8 && by_tma(a, g, tt)) {
+                    pos.skip(1);
+                    reuse |= pos.slot == 0;
+                    continue;
+                }
                 if constexpr (Q8) {
                     const bool odd = convert_tile<HD>(rawring + rpos.slot * SH::kRawBytes, x.row >= 0, val ? x.vs : x.ks,
                                                       val ? first : kTcTile, dst, w, lane);
@@ -717,7 +789,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         SegmentWalk<TcPlan> walk;
         walk.init(pa, blockIdx.x, gridDim.x, &bad);
         if (bad && blockIdx.x == 0) atomicOr(a.status, ST_CAPACITY);
-        for (uint32_t n = 0; ok; ++n) {
+        uint32_t n = 0;
+        for (; ok; ++n) {
             g.weight = 0;
             const bool more = walk.next(pa, g);
             const int k = n % kTcSegs;
@@ -729,7 +802,22 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             }
             __syncwarp();
             if (!more) break;
+            if (a.q_tma) {  // the queries, once the buffer's last ones (and what was staged there) are done with
+                if (n > 0 && !(ok = SH::kStageInQ ? wait(&st.ofree, n - 1) : wait(&st.qempty, n - 1))) break;
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(&st.qfull, g.weight * TB);
+                    mbar_arrive_n(&st.qfull, 255);  // in the place of the softmax warps' 256 arrivals
+                    const int per = 128 / a.G;  // nodes of a block; its rows are their heads of this KV head
+                    for (int b = 0; b < g.weight; ++b)
+                        for (int half = 0; half < HD / 64; ++half)
+                            tma_load_4d(smem_u32(qbuf) + b * TB + half * 16384, &qmap, half * 64, g.h * a.G,
+                                        (2 * g.m + b) * per, g.b, &st.qfull);
+                }
+                __syncwarp();
+            }
         }
+        // (after a failed wait: leave with no copy in flight)
+        if (!ok && a.q_tma && n > 0) mbar_wait(&st.qfull, (n - 1) & 1u, a.status, 100000000LL);
     } else if (Q8 && warp == 15) {  // ---- raw rows of an e4m3 cache
         RingPos<RS> pos;
         uint32_t i = 0;
@@ -772,6 +860,59 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         }
         // leave with no copy in flight: the last tiles have landed
         for (uint32_t j = i > (uint32_t)RS ? i - RS : 0; j < i; ++j) mbar_wait(&st.rawfull[j % RS], (j / RS) & 1u, a.status);
+    } else if (!Q8 && warp == 15) {  // ---- whole tiles by TMA
+        RingPos<S> pos;
+        bool reuse = false;
+        uint32_t sent = 0;  // by slot: used here, and (from bit 8) the phase of its last use
+        while (ok && a.box_rows > 0 && next(g)) {
+            const int nt = g.t1 - g.t0;
+            // a lane's box of every tile: rows box * br .. of the tile, columns half * 64 ..
+            const int br = a.box_rows, boxes = kTcTile / br, box = lane % boxes, half = lane / boxes;
+            // where tile t's box lies: its page's (or sequence's) place in the map; fetched a tile ahead
+            auto place = [&](int t) -> int {
+                if (!a.cache.page_size) return g.b * a.Hkv + g.h;
+                if (!by_tma(a, g, t) || g.t0 + t >= g.t1) return 0;
+                const int lp = ((g.t0 + t) * kTcTile + box * br) / a.cache.page_size;
+                const int pg = a.cache.table[(int64_t)g.b * a.cache.max_pages + lp];
+                if (pg >= 0 && pg < a.cache.n_pages) return pg * a.Hkv + g.h;
+                atomicOr(a.status, ST_DEVICE);
+                return a.cache.n_pages * a.Hkv;  // past the pool: the box reads as zeros
+            };
+            int z0 = place(0), z1 = z0, z2 = z0;  // of tiles t, t + 1, t + 2, as the loaders'
+#pragma unroll 1
+            for (int l = 0; l < 2 * nt; ++l) {
+                const bool val = tile_is_value(l, nt);
+                const int tt = tile_number(l, nt);
+                if (!val) {
+                    z0 = z1;
+                    z1 = l == 0 ? z0 : z2;
+                    z2 = place(tt + 1);
+                }
+                if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;  // (of every tile, as the loaders)
+                if (by_tma(a, g, tt)) {
+                    uint64_t* full = &st.full[pos.slot];
+                    if (lane == 0) {  // in the place of the loaders' 128 arrivals
+                        mbar_arrive_expect_tx(full, TB);
+                        mbar_arrive_n(full, 127);
+                    }
+                    __syncwarp();
+                    sent = (sent & ~(0x100u << pos.slot)) | 1u << pos.slot | pos.phase << (8 + pos.slot);
+                    if (half < HD / 64) {
+                        const int slot = (g.t0 + tt) * kTcTile + box * br;
+                        const int y = a.cache.page_size ? slot % a.cache.page_size : slot;
+                        tma_load_3d(smem_u32(ring) + pos.slot * TB + half * 16384 + box * br * 128, val ? &vmap : &kmap, half * 64, y,
+                                    !val || tt == nt - 1 ? z1 : z0, full);
+                    }
+                }
+                pos.skip(1);
+                reuse |= pos.slot == 0;
+            }
+        }
+        while (a.box_rows <= 0 && next(g)) {}
+        // (after a failed wait: leave with no copy in flight. Otherwise every tile has been used.)
+        if (!ok)
+            for (int k = 0; k < S; ++k)
+                if (sent >> k & 1u) mbar_wait(&st.full[k], sent >> (8 + k) & 1u, a.status, 100000000LL);
     } else if (warp < 8) {  // ---- softmax
         const int gs = warp >> 2, wl = warp & 3;
         const uint32_t lanes = (uint32_t)(wl * 32) << 16;
@@ -780,6 +921,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         uint32_t ns = 0, nj = 0;  // score blocks taken, joins of the streams
         // the warp's part of segment s's queries: rows of its own block, or half of the only one
         auto queries = [&](const Segment& s) {
+            if (a.q_tma) return;  // (the planner's)
             if (s.weight == 2 || gs == 0)
                 load_q<HD>(a, s, s.m * kAttnItemRows + gs * 128 + wl * 32, qbuf + gs * TB, wl, lane);
             if (a.q_vec) {
@@ -805,18 +947,23 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
 #pragma unroll 1
             for (int tt = pair ? 0 : gs; tt < nt; tt += pair ? 1 : 2) {
                 const int tile = g.t0 + tt;
+                const bool tail = (tile + 1) * kTcTile > g.s.P;  // some slots are nodes'
+                ulonglong2 see = make_ulonglong2(0ull, 0ull);
+                if (tail && live) see = seen_bits(a, g, node, tile * kTcTile);  // (while the scores are on their way)
+                __syncwarp();
                 if (!(ok = wait(&st.sfull[gs], ns))) break;
                 ++ns;
                 tc_fence_after();
                 if (!idle) {
-                    if ((tile + 1) * kTcTile > g.s.P) {  // some slots are nodes': hidden scores become -inf
+                    if (tail) {  // hidden scores become -inf
 #pragma unroll 1
                         for (int c = 0; c < kTcTile; c += 32) {
-                            const uint32_t see = live ? seen_bits(a, g, node, tile * kTcTile + c) : 0u;
+                            const uint32_t bits = (uint32_t)((c < 64 ? see.x : see.y) >> (c & 32));
                             uint32_t x[32];
-                            tc_ld32(ts + c, reinterpret_cast<float*>(x));
+                            tc_ld32_start(ts + c, x);
+                            tc_ld32_wait(x);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = see >> e & 1u ? x[e] : 0xFF800000u;
+                            for (int e = 0; e < 32; ++e) x[e] = bits >> e & 1u ? x[e] : 0xFF800000u;
                             tc_st16(ts + c, x);
                             tc_st16(ts + c + 16, x + 16);
                         }
@@ -832,7 +979,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             // the next segment's queries may come once this one's scores are all done
             if (!ok) break;
             more = next(g2);
-            if (more && !SH::kStageInQ) {
+            if (more && !SH::kStageInQ && !a.q_tma) {
                 if (!(ok = wait(&st.qempty, cur))) break;
                 queries(g2);
             }
@@ -869,69 +1016,60 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     : g.whole ? (unsigned long long)((bf16_t*)a.out.p + g.b * a.out.batch + (int64_t)node * a.out.token +
                                                      (int64_t)head * a.out.head)
                               : (unsigned long long)(a.part_o + pr * HD);
-                if (g.whole) {  // (zero sums: a row that sees nothing; its block may hold anything)
-                    f0 = sum == 0.f ? 0.f : f0 / sum;
-                    f1 = sum == 0.f ? 0.f : f1 / sum;
-                }
+                // o = f0 u + f1 v with v the other stream's block; alone, a block counts half twice.
+                // Zero sums: a row that sees nothing, whose block may hold anything.
+                const float norm = (g.whole ? sum == 0.f ? 0.f : 1.f / sum : 1.f) * (join ? 1.f : 0.5f);
+                f0 *= norm;
+                f1 = join ? f1 * norm : f0;
                 const bool zero = g.whole && sum == 0.f;
-                const uint32_t other = tmem + 256 + (gs ^ 1) * 128 + lanes;
+                unsigned long long rows[4];  // the rows that this lane stores parts of
+#pragma unroll
+                for (int k = 0; k < 4; ++k) rows[k] = __shfl_sync(0xffffffffu, mine, 8 * k + lane / 4);
+                const bool vec = a.out_vec;
+                const uint32_t other = join ? tmem + 256 + (gs ^ 1) * 128 + lanes : to;
 #pragma unroll 1
                 for (int c = join && gs ? HD / 2 : 0; c < (join && !gs ? HD / 2 : HD); c += 16) {
                     uint32_t u[16], v[16];
-                    float o[16];
                     tc_ld16_start(to + c, u);
-                    if (join) tc_ld16_start(other + c, v);
+                    tc_ld16_start(other + c, v);
                     tc_ld16_wait(u);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = __uint_as_float(u[e]);
-                    if (join) {
-                        tc_ld16_wait(v);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = o[e] * f0 + __uint_as_float(v[e]) * f1;
-                    } else if (g.whole) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] *= f0;
-                    }
-                    if (zero) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] = 0.f;
-                    }
-                    // chunk k of row l lies at 16 (k ^ l / 4 or l / 2) of the row's bytes: no bank conflicts
+                    tc_ld16_wait(v);
                     __syncwarp();
+                    // chunk k of row l lies at 16 (k ^ l / 2) of the row's 64 bytes: no bank conflicts
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            o[e] = zero ? 0.f : __uint_as_float(u[4 * k + e]) * f0 + __uint_as_float(v[4 * k + e]) * f1;
+                        *reinterpret_cast<float4*>(stage + lane * 64 + ((k ^ (lane >> 1)) & 3) * 16) = make_float4(o[0], o[1], o[2], o[3]);
+                    }
+                    __syncwarp();
+                    float4 y[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {  // four lanes a row
+                        const int r = 8 * k + lane / 4;
+                        y[k] = *reinterpret_cast<const float4*>(stage + r * 64 + (((lane & 3) ^ (r >> 1)) & 3) * 16);
+                    }
                     if (g.whole) {
 #pragma unroll
-                        for (int k = 0; k < 2; ++k)
-                            *reinterpret_cast<uint4*>(stage + lane * 32 + ((k ^ (lane >> 2)) & 1) * 16) = pack16<bf16_t>(o + 8 * k);
-                        __syncwarp();
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {  // two lanes a row
-                            const int r = k * 16 + lane / 2, h = lane & 1;
-                            bf16_t* dst = (bf16_t*)__shfl_sync(0xffffffffu, mine, r);
-                            const uint4 y = *reinterpret_cast<const uint4*>(stage + r * 32 + ((h ^ (r >> 2)) & 1) * 16);
-                            if (dst) {
-                                dst += c + 8 * h;
-                                if (a.out_vec) {
-                                    *reinterpret_cast<uint4*>(dst) = y;
-                                } else {
-                                    const uint32_t x[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e) dst[e].bits = (uint16_t)(x[e / 2] >> (16 * (e & 1)));
-                                }
+                        for (int k = 0; k < 4; ++k) {
+                            const uint2 w = make_uint2(pack_bf16(y[k].x, y[k].y), pack_bf16(y[k].z, y[k].w));
+                            bf16_t* d = (bf16_t*)rows[k] + c + 4 * (lane & 3);
+                            if (!rows[k]) continue;
+                            if (vec) {
+                                *reinterpret_cast<uint2*>(d) = w;
+                            } else {
+                                d[0].bits = (uint16_t)w.x;
+                                d[1].bits = (uint16_t)(w.x >> 16);
+                                d[2].bits = (uint16_t)w.y;
+                                d[3].bits = (uint16_t)(w.y >> 16);
                             }
                         }
                     } else {
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            *reinterpret_cast<float4*>(stage + lane * 64 + ((k ^ (lane >> 1)) & 3) * 16) =
-                                make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-                        __syncwarp();
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {  // four lanes a row
-                            const int r = k * 8 + lane / 4, h = lane & 3;
-                            float* dst = (float*)__shfl_sync(0xffffffffu, mine, r);
-                            const float4 y = *reinterpret_cast<const float4*>(stage + r * 64 + ((h ^ (r >> 1)) & 3) * 16);
-                            if (dst) *reinterpret_cast<float4*>(dst + c + 4 * h) = y;
-                        }
+                            if (rows[k]) *reinterpret_cast<float4*>((float*)rows[k] + c + 4 * (lane & 3)) = y[k];
                     }
                 }
                 __syncwarp();
@@ -953,7 +1091,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 if (warp == 0) st.odd[(cur + 4) & 7] = 0;
                 mbar_arrive(&st.ofree);
             }
-            if (SH::kStageInQ && more) {
+            if (SH::kStageInQ && more && !a.q_tma) {
                 // the buffer held this segment's staged rows
                 if (!(ok = wait(&st.ofree, cur))) break;
                 queries(g2);
