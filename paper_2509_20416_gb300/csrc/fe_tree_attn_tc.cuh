@@ -296,6 +296,22 @@ __device__ __forceinline__ uint2 scale_factors(float scale) {
     return make_uint2(f1 | f1 << 16, f2 | f2 << 16);
 }
 
+// What convert_tile's straight path leaves out: zeros where there is no row, the second factor of
+// scales above 2^7, NaN codes (to NaN, or to zero in a node's value row, which is reported).
+__device__ __forceinline__ bool convert_rare(const uint32_t (&in)[4], uint32_t f1, uint32_t f2, bool node, uint32_t (&o)[8]) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = f1 == 0 ? 0u : mul_bf16x2(o[e], f2);
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (f1 != 0 && (in[e / 4] >> (8 * (e & 3)) & 0x7Fu) == 0x7Fu) {
+            const uint32_t m = e & 1 ? 0xFFFF0000u : 0x0000FFFFu;
+            o[e / 2] = (o[e / 2] & ~m) | (node ? 0u : 0x7FC07FC0u & m);
+            odd |= node;
+        }
+    return odd;
+}
+
 // One tile of e4m3 rows, converted: raw [128][HD] bytes to the bfloat16 values they stand for
 // (number * scale, exact). Rows without a cache row become zero; in rows from `first` on, so do
 // NaN elements (returns whether there were any).
@@ -311,13 +327,16 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_
     unsigned char* base = dst + (c >> 2) * 16384 + w * 4096;
     const int swap = c >> 2, c0 = 2 * (c & 3) + swap, c1 = 2 * (c & 3) + 1 - swap;
     const bool big = __any_sync(0xffffffffu, mine.y != 0x3F803F80u && mine.x != 0);  // some scale above 2^7
+    // a step converts RP rows; the next step's numbers load meanwhile
+    const unsigned char* src = raw + (w * 32 + lane / CH) * HD + c * 16;
+    uint4 u = *reinterpret_cast<const uint4*>(src);
 #pragma unroll 1
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = i * RP + lane / CH;
         const uint32_t f1 = __shfl_sync(0xffffffffu, mine.x, r);
-        uint4 u = *reinterpret_cast<const uint4*>(raw + (w * 32 + r) * HD + c * 16);
-        if (f1 == 0) u = make_uint4(0, 0, 0, 0);
         const uint32_t in[4] = {u.x, u.y, u.z, u.w};
+        src += RP * HD;
+        if (i + 1 < 32 / RP) u = *reinterpret_cast<const uint4*>(src);
         uint32_t o[8], nan = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -326,21 +345,8 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], f1);
-        if (big) {
-            const uint32_t f2 = __shfl_sync(0xffffffffu, mine.y, r);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], f2);
-        }
-        if (nan & 0x80808080u) {
-            const bool node = w * 32 + r >= first;
-            odd |= node;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if ((in[e / 4] >> (8 * (e & 3)) & 0x7Fu) == 0x7Fu) {
-                    const uint32_t m = e & 1 ? 0xFFFF0000u : 0x0000FFFFu;
-                    o[e / 2] = (o[e / 2] & ~m) | (node ? 0u : 0x7FC07FC0u & m);
-                }
-        }
+        // rows without a cache row (f1 = 0), NaN codes, large scales: rare
+        if (__any_sync(0xffffffffu, (nan & 0x80808080u) != 0 || f1 == 0) || big) odd |= convert_rare(in, f1, __shfl_sync(0xffffffffu, mine.y, r), w * 32 + r >= first, o);
         const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
         *reinterpret_cast<uint4*>(base + sw128_offset(r, c0)) = swap ? hi : lo;
         *reinterpret_cast<uint4*>(base + sw128_offset(r, c1)) = swap ? lo : hi;
