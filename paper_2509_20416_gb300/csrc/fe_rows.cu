@@ -42,57 +42,34 @@ struct Share {
     }
 };
 
-template <typename ST, bool FAST>
-__device__ __forceinline__ void load_share(const ST* row, int e0, int e1, float* x) {
-    constexpr int V = Vec16<ST>::kN;
-    if (FAST) {
-        const uint4 a = *reinterpret_cast<const uint4*>(row + e0), b = *reinterpret_cast<const uint4*>(row + e1);
-        Vec16<ST>::widen(a, x);
-        Vec16<ST>::widen(b, x + V);
-    } else {
+// A lane's V pairs, (x[e], x[V + e]) or neighbours, by the angles whose (cos, sin) are t.
+template <int V, bool NEIGHBOURS>
+__device__ __forceinline__ void rotate_pairs(float* x, const float2* t) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            x[j] = Storage<ST>::load(row, e0 + j);
-            x[V + j] = Storage<ST>::load(row, e1 + j);
-        }
+    for (int e = 0; e < V; ++e) {
+        float& a = x[NEIGHBOURS ? 2 * e : e];
+        float& b = x[NEIGHBOURS ? 2 * e + 1 : V + e];
+        const float ya = a * t[e].x - b * t[e].y, yb = b * t[e].x + a * t[e].y;
+        a = ya;
+        b = yb;
     }
 }
 
-// Rotate a lane's elements x (loaded from `row`) to the position whose table row is `cs`.
-template <typename ST, bool FAST>
-__device__ __forceinline__ void rotate_share(const ST* row, int u, int e0, int e1, const RopeView& r, const float2* cs,
-                                             float dir, float* x) {
+// The same element by element, each partner read from the row itself.
+template <typename ST>
+__device__ __forceinline__ void rotate_elements(const ST* row, int e0, int e1, const RopeView& r, const float2* cs, float dir,
+                                                float* x) {
     constexpr int V = Vec16<ST>::kN;
-    if (FAST) {
-        if (u >= r.dim / (2 * V)) return;
-        float2 t[V];
+    const int half = r.dim / 2;
 #pragma unroll
-        for (int j = 0; j < V / 2; ++j) {
-            const float4 f = __ldg(reinterpret_cast<const float4*>(cs + V * u) + j);
-            t[2 * j] = make_float2(f.x, f.y * dir);
-            t[2 * j + 1] = make_float2(f.z, f.w * dir);
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {  // pair j of this unit: (x[j], x[V + j]), or neighbours
-            const int ia = r.interleaved ? 2 * j : j, ib = r.interleaved ? 2 * j + 1 : V + j;
-            float& a = x[ia];
-            float& b = x[ib];
-            const float ya = a * t[j].x - b * t[j].y, yb = b * t[j].x + a * t[j].y;
-            a = ya;
-            b = yb;
-        }
-    } else {
-        const int half = r.dim / 2;
-#pragma unroll
-        for (int j = 0; j < 2 * V; ++j) {
-            const int e = j < V ? e0 + j : e1 + j - V;
-            if (e >= r.dim) continue;
-            const bool first = r.interleaved ? !(e & 1) : e < half;
-            const int pe = r.interleaved ? e ^ 1 : first ? e + half : e - half;
-            const float2 t = __ldg(cs + (r.interleaved ? e >> 1 : first ? e : e - half));
-            const float p = Storage<ST>::load(row, pe), s = t.y * dir;
-            x[j] = first ? x[j] * t.x - p * s : x[j] * t.x + p * s;
-        }
+    for (int j = 0; j < 2 * V; ++j) {
+        const int e = j < V ? e0 + j : e1 + j - V;
+        if (e >= r.dim) continue;
+        const bool first = r.interleaved ? !(e & 1) : e < half;
+        const int pe = r.interleaved ? e ^ 1 : first ? e + half : e - half;
+        const float2 t = __ldg(cs + (r.interleaved ? e >> 1 : first ? e : e - half));
+        const float p = Storage<ST>::load(row, pe), s = t.y * dir;
+        x[j] = first ? x[j] * t.x - p * s : x[j] * t.x + p * s;
     }
 }
 
@@ -119,110 +96,144 @@ __device__ __forceinline__ int scale_exp(float m) {
 }
 __device__ __forceinline__ float pow2(int c) { return __uint_as_float((uint32_t)(c + 127) << 23); }
 
-// One group per job: a token's two rotated heads (2 j, 2 j + 1), or a KV head's key and value
-// rows. Two rows a lane keep 64 bytes in flight, and a key and its value share one address.
+// A group's row, 2 V elements a lane, to e4m3 at `out` and its scale.
+template <int HD, int V>
+__device__ __forceinline__ void quantise_share(const float* x, unsigned lanes, int e0, int e1, uint8_t* out, float* scale,
+                                               bool first_lane) {
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2 * V; ++e) m = fmaxf(m, finite_f32(x[e]) ? fabsf(x[e]) : 0.f);
+#pragma unroll
+    for (int o = HD / (2 * V) / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, o));
+    const int c = scale_exp(m);
+    const float inv = pow2(-c);
+    uint32_t w[V / 2];
+#pragma unroll
+    for (int e = 0; e < 2 * V; e += 4) {
+        float y[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z)  // (a non-finite element becomes NaN)
+            y[z] = finite_f32(x[e + z]) ? x[e + z] * inv : __uint_as_float(0x7FC00000u);
+        w[e / 4] = f32x2_to_e4m3(y[0], y[1]) | (f32x2_to_e4m3(y[2], y[3]) << 16);
+    }
+    if (V == 8) {
+        *reinterpret_cast<uint2*>(out + e0) = make_uint2(w[0], w[1]);
+        *reinterpret_cast<uint2*>(out + e1) = make_uint2(w[V / 4], w[V / 4 + 1]);
+    } else {
+        *reinterpret_cast<uint32_t*>(out + e0) = w[0];
+        *reinterpret_cast<uint32_t*>(out + e1) = w[V / 4];
+    }
+    if (first_lane) *scale = pow2(c);
+}
+
+// One group per job: four of a token's rotated heads, or two KV heads' key and value rows. Four rows
+// a lane keep 128 bytes in flight (about what the memory's latency takes at two blocks an SM) and
+// share the token's table row and address arithmetic. (Two rows a lane with 64-bit index divisions
+// moved 2.5 TB/s at 32 thousand tokens of 64 + 8 heads.)
 template <typename ST, int HD, int CACHE, bool FAST>
-__global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(kRowThreads) rows_kernel(const __grid_constant__ RowsArgs a) {
     constexpr int V = Vec16<ST>::kN, GL = HD / (2 * V);
-    const int ja = (a.HA + 1) / 2, jb = CACHE ? a.HB : (a.HB + 1) / 2, J = ja + jb;
-    const int64_t group = (int64_t)blockIdx.x * (kRowThreads / GL) + threadIdx.x / GL;
+    const uint32_t ja = (a.HA + 3) / 4, jb = CACHE ? (a.HB + 1) / 2 : (a.HB + 3) / 4, J = ja + jb;
+    const uint32_t group = blockIdx.x * (kRowThreads / GL) + threadIdx.x / GL;
     const int u = threadIdx.x % GL;
-    const bool live = group < (int64_t)a.B * a.T * J;
-    const int64_t token = live ? group / J : 0;
-    const int j = (int)(group - token * J), b = (int)(token / a.T), i = (int)(token - (int64_t)b * a.T);
+    if (group >= (uint32_t)(a.B * a.T) * J) return;  // (whole groups: the shuffles below stay inside one)
+    const uint32_t token = group / J;
+    const int j = (int)(group - token * J), b = (int)(token / (uint32_t)a.T), i = (int)(token - (uint32_t)b * a.T);
     const Share<V> sh(u, a.rope);
     // the group's lanes of the warp: they take every branch below together
     const unsigned lanes = ((1u << GL) - 1u) << ((threadIdx.x & 31) / GL * GL);
 
-    const bool kv = CACHE && live && j >= ja;
-    const ST* src[2] = {nullptr, nullptr};
-    ST* dst[2] = {nullptr, nullptr};
-    bool rot[2] = {true, true};
+    int pos = 0;
+    if (a.pos) {
+        pos = a.pos[token];
+        if (pos < 0 || pos >= a.rope.max_pos) {
+            if (u == 0) atomicOr(a.status, ST_CAPACITY);
+            return;
+        }
+    }
+    const bool kv = CACHE && j >= (int)ja;
+    const ST* src[4];
     int64_t crow = 0;
-    if (live) {
-        int pos = 0;
-        bool pos_ok = true;
-        if (a.pos) {
-            pos = a.pos[token];
-            pos_ok = pos >= 0 && pos < a.rope.max_pos;
-            if (!pos_ok && u == 0) atomicOr(a.status, ST_CAPACITY);
-        } else {
-            rot[0] = false;
+    int h0, heads;  // the job's first head, of how many
+    const fe_rows& out = !CACHE && j >= (int)ja ? a.b_out : a.a_out;
+    if (kv) {
+        h0 = 2 * (j - (int)ja);
+        heads = a.HB;
+        const int n = a.n_rows ? a.n_rows[b] : a.T;
+        if (n < 0 || n > a.T) {
+            if (u == 0) atomicOr(a.status, ST_DEVICE);
+            return;
         }
-        if (kv) {
-            const int h = j - ja;
-            const int n = a.n_rows ? a.n_rows[b] : a.T;
-            if ((n < 0 || n > a.T) && u == 0) atomicOr(a.status, ST_DEVICE);
-            rot[1] = false;
-            if (pos_ok && i < n && n <= a.T && cache_row(a.cache, b, (int64_t)a.start[b] + i, crow, a.status)) {
-                crow += h * head_step(a.cache);
-                src[0] = (const ST*)a.b_in.p + b * a.b_in.batch + i * a.b_in.token + h * a.b_in.head;
-                src[1] = (const ST*)a.v_in.p + b * a.v_in.batch + i * a.v_in.token + h * a.v_in.head;
-                if (CACHE == 1) {
-                    dst[0] = (ST*)a.cache.k + crow * HD;
-                    dst[1] = (ST*)a.cache.v + crow * HD;
-                }
-            }
-        } else if (pos_ok) {
-            const bool second = !CACHE && j >= ja;
-            const fe_rows &in = second ? a.b_in : a.a_in, &out = second ? a.b_out : a.a_out;
-            const int heads = second ? a.HB : a.HA;
+        if (i >= n || !cache_row(a.cache, b, (int64_t)a.start[b] + i, crow, a.status)) return;
+        const ST* k = (const ST*)a.b_in.p + b * a.b_in.batch + i * a.b_in.token + h0 * a.b_in.head;
+        const ST* v = (const ST*)a.v_in.p + b * a.v_in.batch + i * a.v_in.token + h0 * a.v_in.head;
+        const bool two = h0 + 1 < heads;
+        src[0] = k;
+        src[1] = v;
+        src[2] = two ? k + a.b_in.head : nullptr;
+        src[3] = two ? v + a.v_in.head : nullptr;
+    } else {
+        const bool second = !CACHE && j >= (int)ja;
+        const fe_rows& in = second ? a.b_in : a.a_in;
+        h0 = 4 * (second ? j - (int)ja : j);
+        heads = second ? a.HB : a.HA;
+        const ST* p = (const ST*)in.p + b * in.batch + i * in.token + h0 * in.head;
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int h = 2 * (second ? j - ja : j) + r;
-                if (h >= heads) continue;
-                src[r] = (const ST*)in.p + b * in.batch + i * in.token + h * in.head;
-                dst[r] = (ST*)out.p + b * out.batch + i * out.token + h * out.head;
+        for (int r = 0; r < 4; ++r) src[r] = h0 + r < heads ? p + r * in.head : nullptr;
+    }
+    uint4 raw[4][2];
+    if (FAST) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (src[r]) {
+                raw[r][0] = *reinterpret_cast<const uint4*>(src[r] + sh.e0);
+                raw[r][1] = *reinterpret_cast<const uint4*>(src[r] + sh.e1);
             }
+    }
+    // the table row of this position: cosines and sines of the lane's V pairs
+    const float2* cs = a.rope.table + (int64_t)pos * (a.rope.dim / 2);
+    const bool turns = a.pos && (!FAST || u < a.rope.dim / (2 * V));
+    float2 t[V];
+    if (FAST && turns) {
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) {
+            const float4 f = __ldg(reinterpret_cast<const float4*>(cs + V * u) + e);
+            t[2 * e] = make_float2(f.x, f.y * a.dir);
+            t[2 * e + 1] = make_float2(f.z, f.w * a.dir);
         }
-        // (the table row of a skipped position is never read: src stays null)
-        const float2* cs = a.rope.table + (int64_t)pos * (a.rope.dim / 2);
-        float x[2][2 * V];
+    }
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
-            if (src[r]) load_share<ST, FAST>(src[r], sh.e0, sh.e1, x[r]);
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-            if (src[r] && rot[r]) rotate_share<ST, FAST>(src[r], u, sh.e0, sh.e1, a.rope, cs, a.dir, x[r]);
-        if (CACHE == 2 && kv) {
-            // (src is set for both rows or none, alike in the group's lanes)
-            if (src[0]) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    float m = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) m = fmaxf(m, finite_f32(x[r][e]) ? fabsf(x[r][e]) : 0.f);
-#pragma unroll
-                    for (int o = GL / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(lanes, m, o));
-                    const int c = scale_exp(m);
-                    const float inv = pow2(-c);
-                    uint8_t* out = (uint8_t*)(r ? a.cache.v : a.cache.k) + crow * HD;
-                    uint32_t w[V / 2];
-#pragma unroll
-                    for (int e = 0; e < 2 * V; e += 4) {
-                        float y[4];
-#pragma unroll
-                        for (int z = 0; z < 4; ++z)  // (a non-finite element becomes NaN)
-                            y[z] = finite_f32(x[r][e + z]) ? x[r][e + z] * inv : __uint_as_float(0x7FC00000u);
-                        w[e / 4] = f32x2_to_e4m3(y[0], y[1]) | (f32x2_to_e4m3(y[2], y[3]) << 16);
-                    }
-                    if (V == 8) {
-                        *reinterpret_cast<uint2*>(out + sh.e0) = make_uint2(w[0], w[1]);
-                        *reinterpret_cast<uint2*>(out + sh.e1) = make_uint2(w[V / 4], w[V / 4 + 1]);
-                    } else {
-                        *reinterpret_cast<uint32_t*>(out + sh.e0) = w[0];
-                        *reinterpret_cast<uint32_t*>(out + sh.e1) = w[V / 4];
-                    }
-                    if (u == 0) (r ? a.cache.vs : a.cache.ks)[crow] = pow2(c);
-                }
+    for (int r = 0; r < 4; ++r) {
+        if (!src[r]) continue;
+        float x[2 * V];
+        const bool value = kv && (r & 1);
+        if (FAST) {
+            Vec16<ST>::widen(raw[r][0], x);
+            Vec16<ST>::widen(raw[r][1], x + V);
+            if (turns && !value) {
+                if (a.rope.interleaved) rotate_pairs<V, true>(x, t);
+                else rotate_pairs<V, false>(x, t);
             }
         } else {
-            // in place and element-wise, a lane's partners are other lanes' elements: all lanes
-            // of the group read before any writes
-            if (!FAST) __syncwarp(lanes);
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
-                if (dst[r]) store_share<ST, FAST>(dst[r], sh.e0, sh.e1, x[r]);
+            for (int e = 0; e < V; ++e) {
+                x[e] = Storage<ST>::load(src[r], sh.e0 + e);
+                x[V + e] = Storage<ST>::load(src[r], sh.e1 + e);
+            }
+            if (turns && !value) rotate_elements<ST>(src[r], sh.e0, sh.e1, a.rope, cs, a.dir, x);
+            // in place, a lane's partners are other lanes' elements: all of the group read before any writes
+            __syncwarp(lanes);
+        }
+        if (CACHE && kv) {
+            const int64_t row = crow + (h0 + (r >> 1)) * head_step(a.cache);
+            if (CACHE == 2) {
+                quantise_share<HD, V>(x, lanes, sh.e0, sh.e1, (uint8_t*)(value ? a.cache.v : a.cache.k) + row * HD,
+                                      (value ? a.cache.vs : a.cache.ks) + row, u == 0);
+            } else {
+                store_share<ST, FAST>((ST*)(value ? a.cache.v : a.cache.k) + row * HD, sh.e0, sh.e1, x);
+            }
+        } else {
+            store_share<ST, FAST>((ST*)out.p + b * out.batch + i * out.token + (h0 + r) * out.head, sh.e0, sh.e1, x);
         }
     }
 }
@@ -231,14 +242,14 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const RowsArgs a) {
 // One group of HD / 16 lanes (e4m3) or HD es / 16 lanes per (sequence, row, head): the key and
 // the value row, one 16-byte load each.
 template <typename ST, int HD, bool Q8, bool FAST>
-__global__ void __launch_bounds__(kRowThreads) read_kernel(const ReadArgs a) {
+__global__ void __launch_bounds__(kRowThreads) read_kernel(const __grid_constant__ ReadArgs a) {
     constexpr int V = Q8 ? 16 : Vec16<ST>::kN, GL = HD / V;
-    const int64_t group = (int64_t)blockIdx.x * (kRowThreads / GL) + threadIdx.x / GL;
+    const uint32_t group = blockIdx.x * (kRowThreads / GL) + threadIdx.x / GL;
     const int u = threadIdx.x % GL;
-    const int Hkv = a.cache.Hkv;
-    if (group >= (int64_t)a.B * a.L * Hkv) return;
-    const int64_t row = group / Hkv;
-    const int h = (int)(group - row * Hkv), b = (int)(row / a.L), i = (int)(row - (int64_t)b * a.L);
+    const uint32_t Hkv = a.cache.Hkv;
+    if (group >= (uint32_t)a.B * a.L * Hkv) return;
+    const uint32_t row = group / Hkv;
+    const int h = (int)(group - row * Hkv), b = (int)(row / (uint32_t)a.L), i = (int)(row - (uint32_t)b * a.L);
     const int n = a.n_rows[b];
     if ((n < 0 || n > a.L) && u == 0) atomicOr(a.status, ST_DEVICE);
     uint4 raw[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
@@ -375,7 +386,7 @@ cudaError_t launch_rows_t(const RowsArgs& a, int cache_kind, cudaStream_t st) {
     constexpr int V = Vec16<ST>::kN, GL = HD / (2 * V), es = Storage<ST>::kBytes;
     const bool fast = a.rope.dim % (2 * V) == 0 && rows_aligned(a.a_in, es) && rows_aligned(a.a_out, es) &&
                       rows_aligned(a.b_in, es) && rows_aligned(a.b_out, es) && rows_aligned(a.v_in, es);
-    const int64_t J = (a.HA + 1) / 2 + (cache_kind ? a.HB : (a.HB + 1) / 2);
+    const int64_t J = (a.HA + 3) / 4 + (cache_kind ? (a.HB + 1) / 2 : (a.HB + 3) / 4);
     const int64_t groups = (int64_t)a.B * a.T * J;
     const int pb = kRowThreads / GL;
     auto go = [&](auto k) { return launch_groups(k, groups, pb, a, st); };

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 import torch
 
@@ -31,42 +32,23 @@ class fe_target_config(ctypes.Structure):
                [(n, _f32) for n in ("rope_theta", "rope_factor", "rope_low", "rope_high", "rope_orig")]
 
 
-class fe_rows(ctypes.Structure):
-    _fields_ = [("p", _vp), ("batch", _i64), ("token", _i64), ("head", _i64)]
-
-
 class fe_kv(ctypes.Structure):
     _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp)]
 
 
-class fe_pages(ctypes.Structure):
-    _fields_ = [("table", _vp), ("n_pages", _i32)]
-
-
-class fe_rope_args(ctypes.Structure):
-    _fields_ = [("B", _i32), ("T", _i32), ("q", fe_rows), ("k", fe_rows), ("q_out", fe_rows), ("k_out", fe_rows),
-                ("pos", _vp), ("backward", _i32)]
-
-
-class fe_cache_write_args(ctypes.Structure):
-    _fields_ = [("B", _i32), ("T", _i32), ("k", fe_rows), ("v", fe_rows), ("q", fe_rows), ("q_out", fe_rows),
-                ("pos", _vp), ("start", _vp), ("n_rows", _vp), ("cache", fe_kv), ("pages", fe_pages)]
-
-
-class fe_cache_read_args(ctypes.Structure):
-    _fields_ = [("B", _i32), ("L", _i32), ("start", _vp), ("n_rows", _vp), ("cache", fe_kv), ("pages", fe_pages),
-                ("k_out", fe_rows), ("v_out", fe_rows)]
-
-
-class fe_tree_attention_args(ctypes.Structure):
-    _fields_ = [("B", _i32), ("T", _i32), ("q", fe_rows), ("out", fe_rows), ("lse", _vp), ("prefix_len", _vp),
-                ("n_nodes", _vp), ("mask", _vp), ("scale", _f32), ("cache", fe_kv), ("pages", fe_pages)]
-
-
-class fe_cache_keep_args(ctypes.Structure):
-    _fields_ = [("B", _i32), ("N", _i32), ("n_layers", _i32), ("path", _vp), ("n_accept", _vp), ("start", _vp),
-                ("caches", ctypes.POINTER(fe_kv)), ("pages", fe_pages)]
-
+# The calls' argument structs (include/fe_target.h), packed in one step: filling ctypes structures
+# field by field would cost more than a small kernel takes. rows: p and three strides; kv: k, v,
+# k_scale, v_scale; pages: table, n_pages.
+_ROWS, _KV, _PAGES = "Pqqq", "PPPP", "Pi4x"
+_ARGS = {
+    "fe_rope": "ii" + 4 * _ROWS + "Pi4x",
+    "fe_cache_write": "ii" + 4 * _ROWS + "PPP" + _KV + _PAGES,
+    "fe_cache_read": "iiPP" + _KV + _PAGES + 2 * _ROWS,
+    "fe_tree_attention": "ii" + 2 * _ROWS + "PPPPf4x" + _KV + _PAGES,
+    "fe_cache_keep": "iii4xPPPP" + _PAGES,
+}
+_PACK = {name: struct.Struct("@" + fmt).pack for name, fmt in _ARGS.items()}
+_NONE = (0, 0, 0, 0)  # rows not given
 
 _lib.fe_target_init.argtypes = [ctypes.POINTER(fe_target_config), _vp, ctypes.POINTER(_vp)]
 _lib.fe_target_init.restype = ctypes.c_int
@@ -74,10 +56,11 @@ _lib.fe_target_free.argtypes = [_vp]
 _lib.fe_target_free.restype = None
 _lib.fe_target_status.argtypes = [_vp, _vp]
 _lib.fe_target_status.restype = ctypes.c_int
-for _name in ("rope", "cache_write", "cache_read", "tree_attention", "cache_keep"):
-    _f = getattr(_lib, "fe_" + _name)
-    _f.argtypes = [_vp, ctypes.POINTER(globals()[f"fe_{_name}_args"]), _vp]
+for _name in _ARGS:
+    _f = getattr(_lib, _name)
+    _f.argtypes = [_vp, ctypes.c_char_p, _vp]
     _f.restype = ctypes.c_int
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
 def make_target_config(cfg: dict) -> fe_target_config:
@@ -99,6 +82,7 @@ class Target:
         self.dtype = _TORCH[cfg["dtype"]]
         self.cache_name = cfg.get("cache_dtype", cfg["dtype"])
         self.page_size, self.max_seq, self.max_batch = cfg.get("page_size", 0), cfg["max_seq"], cfg.get("max_batch", 1)
+        self.scale = 1.0 / math.sqrt(self.hd)
 
     def __del__(self):
         self.close()
@@ -145,6 +129,7 @@ class Cache:
         if scaled and (k_scale is None or v_scale is None or len(k_scale) != n or len(v_scale) != n):
             raise ValueError("an e4m3 cache needs k_scale and v_scale of every layer")
         self.kv = (fe_kv * n)()
+        self.rows = []  # each layer's four addresses
         for i in range(n):
             for x in (k[i], v[i]):
                 _cuda(x)
@@ -157,19 +142,22 @@ class Cache:
                     if tuple(x.shape) != rows or x.dtype != torch.float32 or not x.is_contiguous():
                         raise ValueError(f"scales of cache layer {i} must be contiguous float32 of shape {rows}")
                 s = (k_scale[i].data_ptr(), v_scale[i].data_ptr())
-            self.kv[i] = fe_kv(k[i].data_ptr(), v[i].data_ptr(), *s)
+            self.rows.append((k[i].data_ptr(), v[i].data_ptr()) + tuple(x or 0 for x in s))
+            self.kv[i] = fe_kv(*self.rows[-1])
         self.n_layers, self.k, self.v, self.k_scale, self.v_scale = n, k, v, k_scale, v_scale
         self.page_table, self.n_pages = page_table, n_pages
         if ps:
             if page_table is None or page_table.dim() != 2 or page_table.shape[1] != -(-t.max_seq // ps):
                 raise ValueError("a paged cache needs a page table [B, ceil(max_seq / page_size)]")
             _ints(page_table, tuple(page_table.shape))
-        self.pages = fe_pages(page_table.data_ptr() if ps else None, n_pages)
+        self.pages = (page_table.data_ptr() if ps else 0, n_pages)
 
-    def _layer(self, i: int) -> fe_kv:
+    def _layer(self, i: int, B: int) -> tuple:
+        """Addresses of layer i's buffers and of the page table, for a call of B sequences."""
         if not 0 <= i < self.n_layers:
             raise ValueError(f"layer {i} of a cache of {self.n_layers}")
-        return self.kv[i]
+        self._fits(B)
+        return self.rows[i] + self.pages
 
     def _fits(self, B: int) -> None:
         if self.page_table is not None and self.page_table.shape[0] < B:
@@ -196,52 +184,61 @@ def _cuda(x) -> None:
         raise ValueError("buffers the kernels access must be CUDA tensors")
 
 
-def _ints(x, shape) -> int | None:
-    """The address of a contiguous CUDA int32 tensor of the given shape (None passes)."""
+def _ints(x, shape) -> int:
+    """The address of a contiguous CUDA int32 tensor of the given shape (0 for None)."""
     if x is None:
-        return None
+        return 0
     _cuda(x)
-    if x.dtype != torch.int32 or tuple(x.shape) != shape or not x.is_contiguous():
+    if x.dtype != torch.int32 or x.shape != shape or not x.is_contiguous():
         raise ValueError(f"expected a contiguous int32 tensor of shape {shape}, got {x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
 
 
-def _rows(t: Target, x, B: int, T: int, heads: int) -> fe_rows:
+def _rows(t: Target, x, shape) -> tuple:
+    """A row tensor's address and strides."""
     _cuda(x)
-    if x.dtype != t.dtype or tuple(x.shape) != (B, T, heads, t.hd) or x.stride(3) != 1:
-        raise ValueError(f"expected {t.dtype} rows {(B, T, heads, t.hd)} with contiguous elements, got {x.dtype} "
-                         f"{tuple(x.shape)} with strides {tuple(x.stride())}")
     s = x.stride()
-    return fe_rows(x.data_ptr(), s[0], s[1], s[2])
+    if x.dtype != t.dtype or x.shape != shape or s[3] != 1:
+        raise ValueError(f"expected {t.dtype} rows {tuple(shape)} with contiguous elements, got {x.dtype} {tuple(x.shape)} "
+                         f"with strides {tuple(s)}")
+    return x.data_ptr(), s[0], s[1], s[2]
 
 
-def _call(name: str, t: Target, args, stream, *tensors) -> None:
-    raw = _stream(stream)
-    # memory that PyTorch's allocator hands out belongs to the current stream: on another one,
-    # tell it that the tensors are in use there
-    if stream is not None and raw != torch.cuda.current_stream().cuda_stream:
-        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(raw)
-        for x in tensors:
-            if x is not None:
-                x.record_stream(s)
-    _check(getattr(_lib, name)(t.ptr, ctypes.byref(args), raw), name)
+def _call(name: str, t: Target, stream, tensors, *args) -> None:
+    """Pack the arguments and call the library. Memory that PyTorch's allocator hands out belongs
+    to the current stream: on another one, the allocator is told that `tensors` are in use there."""
+    if stream is None and _raw_stream is not None:
+        raw = _raw_stream(torch.cuda.current_device())
+    else:
+        raw = _stream(stream)
+        if stream is not None and raw != torch.cuda.current_stream().cuda_stream:
+            s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(raw)
+            for x in tensors():
+                if x is not None:
+                    x.record_stream(s)
+    code = getattr(_lib, name)(t.ptr, _PACK[name](*args), raw)
+    if code:
+        _check(code, name)
 
 
 def fe_rope(t: Target, q, k, pos, backward: bool = False, q_out=None, k_out=None, stream=None) -> tuple:
     """Rotary positions (include/fe_target.h) of q [B, T, H, hd] and k [B, T, Hkv, hd] (either
     may be None) at pos [B, T]; with backward, the gradient's rotation. Returns (q_out, k_out);
     pass the inputs as outputs to rotate in place."""
-    B, T = int(pos.shape[0]), int(pos.shape[1])
-    a = fe_rope_args(B, T, pos=_ints(pos, (B, T)), backward=1 if backward else 0)
+    B, T = pos.shape
+    qr = kr = qo = ko = _NONE
     if q is not None:
-        a.q = _rows(t, q, B, T, t.H)
-        q_out = torch.empty((B, T, t.H, t.hd), dtype=t.dtype, device=q.device) if q_out is None else q_out
-        a.q_out = _rows(t, q_out, B, T, t.H)
+        shape = (B, T, t.H, t.hd)
+        qr = _rows(t, q, shape)
+        q_out = q.new_empty(shape) if q_out is None else q_out
+        qo = _rows(t, q_out, shape)
     if k is not None:
-        a.k = _rows(t, k, B, T, t.Hkv)
-        k_out = torch.empty((B, T, t.Hkv, t.hd), dtype=t.dtype, device=k.device) if k_out is None else k_out
-        a.k_out = _rows(t, k_out, B, T, t.Hkv)
-    _call("fe_rope", t, a, stream, q, k, q_out, k_out, pos)
+        shape = (B, T, t.Hkv, t.hd)
+        kr = _rows(t, k, shape)
+        k_out = k.new_empty(shape) if k_out is None else k_out
+        ko = _rows(t, k_out, shape)
+    _call("fe_rope", t, stream, lambda: (q, k, q_out, k_out, pos), B, T, *qr, *kr, *qo, *ko, _ints(pos, (B, T)),
+          1 if backward else 0)
     return q_out, k_out
 
 
@@ -250,16 +247,17 @@ def fe_cache_write(t: Target, cache: Cache, layer: int, k, v, start, n_rows=None
     """Rows k, v [B, T, Hkv, hd] into slots start[b] + i of a layer's cache, the keys rotated to
     pos [B, T] if given, quantised if the cache is; with q [B, T, H, hd] also rotates the
     queries into q_out, which is returned."""
-    B, T = int(k.shape[0]), int(k.shape[1])
-    cache._fits(B)
-    a = fe_cache_write_args(B, T, _rows(t, k, B, T, t.Hkv), _rows(t, v, B, T, t.Hkv), pos=_ints(pos, (B, T)),
-                            start=_ints(start, (B,)), n_rows=_ints(n_rows, (B,)), cache=cache._layer(layer),
-                            pages=cache.pages)
+    B, T = k.shape[:2]
+    shape = (B, T, t.Hkv, t.hd)
+    qr = qo = _NONE
     if q is not None:
-        a.q = _rows(t, q, B, T, t.H)
-        q_out = torch.empty((B, T, t.H, t.hd), dtype=t.dtype, device=q.device) if q_out is None else q_out
-        a.q_out = _rows(t, q_out, B, T, t.H)
-    _call("fe_cache_write", t, a, stream, k, v, start, n_rows, pos, q, q_out, *(cache.tensors() if stream else ()))
+        qshape = (B, T, t.H, t.hd)
+        qr = _rows(t, q, qshape)
+        q_out = q.new_empty(qshape) if q_out is None else q_out
+        qo = _rows(t, q_out, qshape)
+    _call("fe_cache_write", t, stream, lambda: (k, v, start, n_rows, pos, q, q_out, *cache.tensors()), B, T,
+          *_rows(t, k, shape), *_rows(t, v, shape), *qr, *qo, _ints(pos, (B, T)), _ints(start, (B,)), _ints(n_rows, (B,)),
+          *cache._layer(layer, B))
     return q_out
 
 
@@ -267,14 +265,12 @@ def fe_cache_read(t: Target, cache: Cache, layer: int, start, n_rows, L: int, k_
                   stream=None) -> tuple:
     """Slots start[b] .. start[b] + n_rows[b] - 1 of a layer's cache as rows k, v [B, L, Hkv, hd]
     of the handle's type; rows past n_rows[b] are zero."""
-    B = int(start.shape[0])
-    cache._fits(B)
+    B = start.shape[0]
     shape = (B, L, t.Hkv, t.hd)
     k_out = torch.empty(shape, dtype=t.dtype, device=start.device) if k_out is None else k_out
     v_out = torch.empty(shape, dtype=t.dtype, device=start.device) if v_out is None else v_out
-    a = fe_cache_read_args(B, L, _ints(start, (B,)), _ints(n_rows, (B,)), cache._layer(layer), cache.pages,
-                           _rows(t, k_out, B, L, t.Hkv), _rows(t, v_out, B, L, t.Hkv))
-    _call("fe_cache_read", t, a, stream, start, n_rows, k_out, v_out, *(cache.tensors() if stream else ()))
+    _call("fe_cache_read", t, stream, lambda: (start, n_rows, k_out, v_out, *cache.tensors()), B, L, _ints(start, (B,)),
+          _ints(n_rows, (B,)), *cache._layer(layer, B), *_rows(t, k_out, shape), *_rows(t, v_out, shape))
     return k_out, v_out
 
 
@@ -284,32 +280,28 @@ def fe_tree_attention(t: Target, cache: Cache, layer: int, q, prefix_len, mask=N
     before prefix_len[b], and slot prefix_len[b] + c where mask [B, T, T] (uint8) is set, or
     c <= i without a mask (consecutive tokens, single-token decoding). scale: 1 / sqrt(hd)
     unless given. Returns (out [B, T, H, hd], lse [B, T, H] float32)."""
-    B, T = int(q.shape[0]), int(q.shape[1])
-    cache._fits(B)
+    B, T = q.shape[:2]
+    shape = (B, T, t.H, t.hd)
+    qr = _rows(t, q, shape)
     if out is None:
-        out = torch.empty((B, T, t.H, t.hd), dtype=t.dtype, device=q.device)
+        out = q.new_empty(shape)
     if lse is None:
         lse = torch.empty((B, T, t.H), dtype=torch.float32, device=q.device)
-    elif lse.dtype != torch.float32 or tuple(lse.shape) != (B, T, t.H) or not lse.is_contiguous() or not lse.is_cuda:
+    elif lse.dtype != torch.float32 or lse.shape != (B, T, t.H) or not lse.is_contiguous() or not lse.is_cuda:
         raise ValueError(f"lse must be a contiguous float32 CUDA tensor of shape {(B, T, t.H)}")
-    if mask is not None and (mask.dtype not in (torch.uint8, torch.bool) or tuple(mask.shape) != (B, T, T)
+    if mask is not None and (mask.dtype not in (torch.uint8, torch.bool) or mask.shape != (B, T, T)
                              or not mask.is_contiguous() or not mask.is_cuda):
         raise ValueError(f"mask must be a contiguous uint8 CUDA tensor of shape {(B, T, T)}")
-    a = fe_tree_attention_args(B, T, _rows(t, q, B, T, t.H), _rows(t, out, B, T, t.H), lse.data_ptr(),
-                               _ints(prefix_len, (B,)), _ints(n_nodes, (B,)), None if mask is None else mask.data_ptr(),
-                               1.0 / math.sqrt(t.hd) if scale is None else float(scale), cache._layer(layer), cache.pages)
-    _call("fe_tree_attention", t, a, stream, q, prefix_len, n_nodes, mask, out, lse,
-          *(cache.tensors() if stream else ()))
+    _call("fe_tree_attention", t, stream, lambda: (q, prefix_len, n_nodes, mask, out, lse, *cache.tensors()), B, T, *qr,
+          *_rows(t, out, shape), lse.data_ptr(), _ints(prefix_len, (B,)), _ints(n_nodes, (B,)),
+          0 if mask is None else mask.data_ptr(), t.scale if scale is None else float(scale), *cache._layer(layer, B))
     return out, lse
 
 
 def fe_cache_keep(t: Target, cache: Cache, path, n_accept, start, stream=None) -> None:
     """Move the accepted nodes' rows, slots start[b] + path[b][j] for j < n_accept[b], to slots
     start[b] + 1 + j in every layer of the cache (path [B, N], n_accept [B], start [B])."""
-    B, N = int(path.shape[0]), int(path.shape[1])
-    if cache.page_table is None and B > t.max_batch:
-        raise ValueError("more sequences than the cache holds")
+    B, N = path.shape
     cache._fits(B)
-    a = fe_cache_keep_args(B, N, cache.n_layers, _ints(path, (B, N)), _ints(n_accept, (B,)), _ints(start, (B,)),
-                           cache.kv, cache.pages)
-    _call("fe_cache_keep", t, a, stream, path, n_accept, start, *(cache.tensors() if stream else ()))
+    _call("fe_cache_keep", t, stream, lambda: (path, n_accept, start, *cache.tensors()), B, N, cache.n_layers,
+          _ints(path, (B, N)), _ints(n_accept, (B,)), _ints(start, (B,)), ctypes.addressof(cache.kv), *cache.pages)

@@ -210,3 +210,44 @@ def test_target_binding_rejects_wrong_tensors_before_the_library(lib):
     e = lib.Target(0, dict(TARGET_CFG, page_size=0))
     with pytest.raises(ValueError, match="scale"):
         lib.Cache(e, [k], [k])
+
+
+def test_packed_arguments_match_the_header(lib, tmp_path):
+    """The binding packs the target calls' arguments by a format string; its size and the offset of
+    every member must be the C compiler's."""
+    import struct
+    import subprocess
+    from paper_2509_20416_gb300 import target
+    members = {
+        "fe_rope": ["B", "q", "k", "q_out", "k_out", "pos", "backward"],
+        "fe_cache_write": ["B", "k", "v", "q", "q_out", "pos", "start", "n_rows", "cache", "pages"],
+        "fe_cache_read": ["B", "start", "n_rows", "cache", "pages", "k_out", "v_out"],
+        "fe_tree_attention": ["B", "q", "out", "lse", "prefix_len", "n_nodes", "mask", "scale", "cache", "pages"],
+        "fe_cache_keep": ["B", "path", "n_accept", "start", "caches", "pages"],
+    }
+    # format characters before each member
+    before = {
+        "fe_rope": [0, 2, 6, 10, 14, 18, 19],
+        "fe_cache_write": [0, 2, 6, 10, 14, 18, 19, 20, 21, 25],
+        "fe_cache_read": [0, 2, 3, 4, 8, 11, 15],
+        "fe_tree_attention": [0, 2, 6, 10, 11, 12, 13, 14, 16, 20],
+        "fe_cache_keep": [0, 4, 5, 6, 7, 8],
+    }
+    src = ['#include <stdio.h>', '#include <stddef.h>', '#include "fe_target.h"', 'int main(void) {']
+    for f, ms in members.items():
+        src.append(f'printf("{f} %zu", sizeof({f}_args));')
+        src += [f'printf(" %zu", offsetof({f}_args, {m}));' for m in ms]
+        src.append('printf("\\n");')
+    src.append('return 0; }')
+    c = tmp_path / "offsets.c"
+    c.write_text("\n".join(src))
+    exe = str(tmp_path / "offsets")
+    subprocess.run(["gcc", "-I" + os.path.join(ROOT, "include"), str(c), "-o", exe], check=True)
+    for line in subprocess.run([exe], check=True, capture_output=True, text=True).stdout.splitlines():
+        f, size, *offsets = line.split()
+        fmt = target._ARGS[f]
+        parts = re.findall(r"\d*[a-zA-Z]", fmt)  # one per value or padding
+        assert struct.calcsize("@" + fmt) == int(size), f
+        for n, off in zip(before[f], offsets):
+            head = "@" + "".join(parts[:n]) + ("0P" if parts[n:n + 1] == ["P"] else "")
+            assert struct.calcsize(head) == int(off), (f, n)

@@ -517,7 +517,6 @@ def test_cache_past_32_bit_offsets(fe):
 
 
 def test_calls_refuse_bad_arguments(fe):
-    import ctypes
     from paper_2509_20416_gb300 import target as tg
     c = ref.config(max_seq=64, cache_dtype="e4m3")
     t = fe.fe_target_init(c)
@@ -546,7 +545,8 @@ def test_calls_refuse_bad_arguments(fe):
         with pytest.raises(ValueError):
             call()
     # a cache off the 16-byte grid is refused by the library itself
-    args = tg.fe_tree_attention_args(2, 4, tg._rows(t, q, 2, 4, 8), tg._rows(t, q, 2, 4, 8), None, s.data_ptr(), None, None,
-                                     1.0, tg.fe_kv(store.k.data_ptr() + 8, store.v.data_ptr(), 16, 16), store.pages)
-    assert fe._lib.fe_tree_attention(t.ptr, ctypes.byref(args), None) == fe.FE_ERR_INVALID_ARG
+    rows_q = tg._rows(t, q, q.shape)
+    args = tg._PACK["fe_tree_attention"](2, 4, *rows_q, *rows_q, 0, s.data_ptr(), 0, 0, 1.0, store.k.data_ptr() + 8,
+                                         store.v.data_ptr(), store.k_scale.data_ptr(), store.v_scale.data_ptr(), 0, 0)
+    assert fe._lib.fe_tree_attention(t.ptr, args, None) == fe.FE_ERR_INVALID_ARG
     assert fe.fe_target_status(t) == fe.FE_OK
