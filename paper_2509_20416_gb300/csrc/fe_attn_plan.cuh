@@ -19,6 +19,9 @@ struct PlanArgs {
     int B, T, Hkv, G, max_seq;
     const int *prefix, *nodes;
     bool causal;
+    // Set by Place::find: short items, no more of them than CTAs, are not split (joining a split
+    // costs about as much as six tiles); every item then counts as one unit, and CTA c has item c.
+    bool whole = false;
 };
 
 __device__ __forceinline__ PlanArgs plan_args(const TreeAttnArgs& a) {
@@ -62,7 +65,7 @@ struct Plan {
     // units of one KV head of a sequence
     __device__ __forceinline__ static int head_units(const PlanArgs& a, SeqLen s) {
         const int rows = s.n * a.G, nb = blocks(rows);
-        if (nb == 0) return 0;
+        if (a.whole || nb == 0) return nb;
         if (!a.causal)  // every block but the last is full
             return nb * OVER + tiles(a, s, 0) * ((nb - 1) * weight(ROWS, 0) + weight(rows, nb - 1));
         int u = nb * OVER;
@@ -71,10 +74,13 @@ struct Plan {
         return u;
     }
     // units of an item of nt tiles of weight w = 1 or 2; the unit where tile t starts
-    __device__ __forceinline__ static int units(int w, int nt) { return OVER + w * nt; }
-    __device__ __forceinline__ static int tile_unit(int s0, int w, int t) { return s0 + OVER + w * t; }
+    __device__ __forceinline__ static int units(const PlanArgs& a, int w, int nt) { return a.whole ? 1 : OVER + w * nt; }
+    __device__ __forceinline__ static int tile_unit(const PlanArgs& a, int s0, int w, int t) {
+        return a.whole ? s0 : s0 + OVER + w * t;
+    }
     // first tile of an item with first unit s0 that starts at unit u0 or later
-    __device__ __forceinline__ static int first_tile(int s0, int w, int nt, int u0) {
+    __device__ __forceinline__ static int first_tile(const PlanArgs& a, int s0, int w, int nt, int u0) {
+        if (a.whole) return u0 <= s0 ? 0 : nt;
         return u0 <= s0 + OVER ? 0 : min((u0 - s0 - OVER + w - 1) >> (w - 1), nt);
     }
     // whether every call of this shape keeps its units within 32 bits
@@ -117,20 +123,31 @@ struct Place {
     int b, h, m, s0;  // the item and its first unit
     SeqLen s;
 
-    __device__ __forceinline__ static Place find(const PlanArgs& a, int c, int ncta, bool* bad = nullptr) {
+    __device__ __forceinline__ static Place find(PlanArgs& a, int c, int ncta, bool* bad = nullptr) {
         const int lane = threadIdx.x & 31;
         SeqLen sl;
-        int hu = 0, U = 0;
+        int hu = 0, U = 0, items = 0;
 #pragma unroll 1
         for (int b0 = (a.B - 1) & ~31; b0 >= 0; b0 -= 32) {  // (ends with the first 32's in sl and hu)
             sl = b0 + lane < a.B ? seq_len(a, b0 + lane, bad) : SeqLen{0, 0};
             hu = PL::head_units(a, sl);
             U += hu;
+            items += PL::blocks(sl.n * a.G);
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) U += __shfl_xor_sync(0xffffffffu, U, o);
+        for (int o = 16; o > 0; o >>= 1) {
+            U += __shfl_xor_sync(0xffffffffu, U, o);
+            items += __shfl_xor_sync(0xffffffffu, items, o);
+        }
         U *= a.Hkv;
-        Place p{Cut(U, ncta), false, 0, 0, 0, 0, SeqLen{0, 0}};
+        items *= a.Hkv;
+        a.whole = items <= ncta && U <= items * (PL::kOver + 6);
+        if (a.whole) {
+            U = items;
+            hu = PL::blocks(sl.n * a.G);
+        }
+        Place p{Cut(U, a.whole ? max(items, 1) : ncta), false, 0, 0, 0, 0, SeqLen{0, 0}};
+        if (c >= p.cut.G) return p;
         const int u0 = p.cut.begin(c);
         if (u0 >= U) return p;
         // the sequence that holds unit u0: the first whose units end past it
@@ -165,7 +182,7 @@ struct Place {
         // the block of the head
 #pragma unroll 1
         while (true) {
-            const int w = PL::units(PL::weight(p.s.n * a.G, p.m), PL::tiles(a, p.s, p.m));
+            const int w = PL::units(a, PL::weight(p.s.n * a.G, p.m), PL::tiles(a, p.s, p.m));
             if (p.s0 + w > u0) return p;
             p.s0 += w;
             ++p.m;
@@ -180,7 +197,7 @@ struct SegmentWalk {
     int b, h, m;
     SeqLen s;
 
-    __device__ __forceinline__ void init(const PlanArgs& a, int cta, int ncta, bool* bad = nullptr) {
+    __device__ __forceinline__ void init(PlanArgs& a, int cta, int ncta, bool* bad = nullptr) {
         const Place<PL> p = Place<PL>::find(a, cta, ncta, bad);
         u0 = p.cut.begin(cta);
         u1 = p.cut.begin(cta + 1);
@@ -198,8 +215,8 @@ struct SegmentWalk {
             bool got = false;
             if (rows > 0) {
                 const int w = PL::weight(rows, m), nt = PL::tiles(a, s, m);
-                g.t0 = PL::first_tile(pos, w, nt, u0);
-                g.t1 = PL::first_tile(pos, w, nt, u1);
+                g.t0 = PL::first_tile(a, pos, w, nt, u0);
+                g.t1 = PL::first_tile(a, pos, w, nt, u1);
                 got = g.t0 < g.t1;
                 if (got) {
                     g.b = b;
@@ -212,7 +229,7 @@ struct SegmentWalk {
                     g.whole = g.t0 == 0 && g.t1 == nt;
                     g.slot = g.t0 == 0 ? 1 : 0;
                 }
-                pos += PL::units(w, nt);
+                pos += PL::units(a, w, nt);
             }
             if (++m >= PL::blocks(rows)) {
                 m = 0;

@@ -19,7 +19,7 @@ constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinShares = 
 template <typename QT, int HD, typename PL, int ROWS>
 __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a, int ncta) {
     constexpr int E = HD / 32;  // columns of a lane
-    const PlanArgs pa = plan_args(a);
+    PlanArgs pa = plan_args(a);
     const int lane = threadIdx.x & 31, wid = blockIdx.y * kJoinWarps + threadIdx.x / 32;
     const Place<PL> w = Place<PL>::find(pa, blockIdx.x + 1, ncta);
     griddep_wait();  // (on every path: this kernel's end stands for the attention's too)
@@ -34,18 +34,18 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __gr
             if (a.lse && lane == 0) a.lse[(int64_t)b * a.T * a.H + x] = -INFINITY;
         }
     }
-    if (!w.found) return;
+    if (!w.found || pa.whole) return;
     const int rows = w.s.n * a.G, nrow = min(ROWS, rows - w.m * ROWS);
     const int wt = PL::weight(rows, w.m), nt = PL::tiles(pa, w.s, w.m);
     if (w.s0 >= w.cut.begin(blockIdx.x + 1)) return;  // the item starts there: not split
-    if (w.cut.owner(PL::tile_unit(w.s0, wt, 0)) != (int)blockIdx.x) return;  // an earlier block's item
-    const int c1 = w.cut.owner(PL::tile_unit(w.s0, wt, nt - 1));
+    if (w.cut.owner(PL::tile_unit(pa, w.s0, wt, 0)) != (int)blockIdx.x) return;  // an earlier block's item
+    const int c1 = w.cut.owner(PL::tile_unit(pa, w.s0, wt, nt - 1));
     if (c1 == (int)blockIdx.x) return;
     for (int r = wid; r < nrow; r += kJoinShares * kJoinWarps) {
         // the partials' row of contributor c, or -1 if no tile starts in c's units
         auto part = [&](int c) -> int64_t {
-            const int t0 = PL::first_tile(w.s0, wt, nt, w.cut.begin(c));
-            if (c > c1 || t0 >= PL::first_tile(w.s0, wt, nt, w.cut.begin(c + 1))) return -1;
+            const int t0 = PL::first_tile(pa, w.s0, wt, nt, w.cut.begin(c));
+            if (c > c1 || t0 >= PL::first_tile(pa, w.s0, wt, nt, w.cut.begin(c + 1))) return -1;
             return ((int64_t)c * 2 + (t0 == 0 ? 1 : 0)) * kAttnItemRows + r;
         };
         float mx = -INFINITY;

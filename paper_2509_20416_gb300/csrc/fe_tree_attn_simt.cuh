@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __gr
     SimtSmem<HD>& sm = *reinterpret_cast<SimtSmem<HD>*>(smem_raw);
     const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
     constexpr int NC = HD / 64;  // groups of four output columns per thread
-    const PlanArgs pa = plan_args(a);
+    PlanArgs pa = plan_args(a);
     griddep_launch_dependents();
     bool bad = false;
     SegmentWalk<SimtPlan> walk;

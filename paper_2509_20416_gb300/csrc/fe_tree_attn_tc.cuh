@@ -790,7 +790,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         __syncwarp();
         mbar_wait(&st.drain[gs], 0, a.status, 100000000LL);
     } else if (warp == 14) {  // ---- the plan
-        const PlanArgs pa = plan_args(a);
+        PlanArgs pa = plan_args(a);
         bool bad = false;
         SegmentWalk<TcPlan> walk;
         walk.init(pa, blockIdx.x, gridDim.x, &bad);

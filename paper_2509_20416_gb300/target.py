@@ -230,12 +230,12 @@ def fe_rope(t: Target, q, k, pos, backward: bool = False, q_out=None, k_out=None
     if q is not None:
         shape = (B, T, t.H, t.hd)
         qr = _rows(t, q, shape)
-        q_out = q.new_empty(shape) if q_out is None else q_out
+        q_out = torch.empty(shape, dtype=t.dtype, device=q.device) if q_out is None else q_out
         qo = _rows(t, q_out, shape)
     if k is not None:
         shape = (B, T, t.Hkv, t.hd)
         kr = _rows(t, k, shape)
-        k_out = k.new_empty(shape) if k_out is None else k_out
+        k_out = torch.empty(shape, dtype=t.dtype, device=k.device) if k_out is None else k_out
         ko = _rows(t, k_out, shape)
     _call("fe_rope", t, stream, lambda: (q, k, q_out, k_out, pos), B, T, *qr, *kr, *qo, *ko, _ints(pos, (B, T)),
           1 if backward else 0)
@@ -253,7 +253,7 @@ def fe_cache_write(t: Target, cache: Cache, layer: int, k, v, start, n_rows=None
     if q is not None:
         qshape = (B, T, t.H, t.hd)
         qr = _rows(t, q, qshape)
-        q_out = q.new_empty(qshape) if q_out is None else q_out
+        q_out = torch.empty(qshape, dtype=t.dtype, device=q.device) if q_out is None else q_out
         qo = _rows(t, q_out, qshape)
     _call("fe_cache_write", t, stream, lambda: (k, v, start, n_rows, pos, q, q_out, *cache.tensors()), B, T,
           *_rows(t, k, shape), *_rows(t, v, shape), *qr, *qo, _ints(pos, (B, T)), _ints(start, (B,)), _ints(n_rows, (B,)),
@@ -284,7 +284,7 @@ def fe_tree_attention(t: Target, cache: Cache, layer: int, q, prefix_len, mask=N
     shape = (B, T, t.H, t.hd)
     qr = _rows(t, q, shape)
     if out is None:
-        out = q.new_empty(shape)
+        out = torch.empty(shape, dtype=t.dtype, device=q.device)
     if lse is None:
         lse = torch.empty((B, T, t.H), dtype=torch.float32, device=q.device)
     elif lse.dtype != torch.float32 or lse.shape != (B, T, t.H) or not lse.is_contiguous() or not lse.is_cuda:
