@@ -131,7 +131,7 @@ __device__ __forceinline__ void quantise_share(const float* x, unsigned lanes, i
 // share the token's table row and address arithmetic. (Two rows a lane with 64-bit index divisions
 // moved 2.5 TB/s at 32 thousand tokens of 64 + 8 heads.)
 template <typename ST, int HD, int CACHE, bool FAST>
-__global__ void __launch_bounds__(kRowThreads) rows_kernel(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(kRowThreads, 3) rows_kernel(const __grid_constant__ RowsArgs a) {
     constexpr int V = Vec16<ST>::kN, GL = HD / (2 * V);
     const uint32_t ja = (a.HA + 3) / 4, jb = CACHE ? (a.HB + 1) / 2 : (a.HB + 3) / 4, J = ja + jb;
     const uint32_t group = blockIdx.x * (kRowThreads / GL) + threadIdx.x / GL;
@@ -297,71 +297,77 @@ __global__ void __launch_bounds__(kRowThreads) read_kernel(const __grid_constant
 }
 
 // ---- keep --------------------------------------------------------------------------------------
-// One warp per (layer, sequence, KV head). A lane carries one 16-byte column of the key or value
-// rows along the path: since path is increasing with path[j] >= j + 1, slot 1 + j is written only
-// after the last read of it when the moves go in order, so eight loads at a time may go before
-// their eight stores. Nothing crosses lanes.
+// One warp per (group of layers, sequence, KV head). The lanes first work out the path's rows, one
+// node each (its slot's and its new slot's cache rows: two page lookups side by side), then carry
+// 16-byte columns of the key and value rows along the path, layer after layer: since path is
+// increasing with path[j] >= j + 1, slot 1 + j is written only after the last read of it when the
+// moves go in order, so eight loads go before their eight stores. Bound by three dependent reads
+// (path, page table, rows); four layers a warp, where there are enough warps, share the first two.
 __global__ void __launch_bounds__(kRowThreads) keep_kernel(const __grid_constant__ KeepArgs a) {
-    const int64_t w = (int64_t)blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32;
+    const uint32_t w = blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32;
     const int lane = threadIdx.x & 31;
-    const int Hkv = a.cache.Hkv;
-    if (w >= (int64_t)a.n_layers * a.B * Hkv) return;
-    const int h = (int)(w % Hkv);
-    const int b = (int)(w / Hkv % a.B);
-    const fe_kv& L = a.layer[w / Hkv / a.B];
+    const uint32_t Hkv = a.cache.Hkv, groups = (a.n_layers + a.layers_per_warp - 1) / a.layers_per_warp;
+    if (w >= groups * a.B * Hkv) return;
+    const int h = (int)(w % Hkv), b = (int)(w / Hkv % a.B), l0 = (int)(w / Hkv / a.B) * a.layers_per_warp;
+    const int l1 = min(l0 + a.layers_per_warp, a.n_layers);
     const int n = a.n_accept[b];
     const int* path = a.path + (int64_t)b * a.N;
-    const int64_t start = a.start[b];
+    const int64_t start = a.start[b], hs = h * head_step(a.cache);
     if (n <= 0 || n > a.N) {
         if (n != 0 && lane == 0) atomicOr(a.status, ST_DEVICE);
         return;
     }
-    // every slot and page of the path is checked before the first move
-    int bad = 0;
-    for (int j = lane; j <= n; j += 32) {
-        int64_t row;
-        if (j < n) {
-            const int p = path[j];
-            if (p < 1 || (j > 0 && path[j - 1] >= p)) {
-                atomicOr(a.status, ST_DEVICE);
-                bad = 1;
-            } else if (!cache_row(a.cache, b, start + p, row, a.status)) {
-                bad = 1;
-            }
-        }
-        if (j > 0 && !cache_row(a.cache, b, start + j, row, a.status)) bad = 1;
-    }
+    // the rows of node path[j] (from) and of its new slot (to); false if the path or a slot is bad
+    auto rows_of = [&](int j, int64_t& from, int64_t& to) -> bool {
+        const int p = path[j], before = j > 0 ? path[j - 1] : 0;
+        bool ok = p > before;
+        if (!ok) atomicOr(a.status, ST_DEVICE);
+        ok = ok && cache_row(a.cache, b, start + p, from, a.status);
+        return cache_row(a.cache, b, start + 1 + j, to, a.status) && ok;
+    };
+    int64_t from = 0, to = 0;
+    // every node, and the root's slot, is checked before the first move
+    bool bad = false;
+    int64_t root;
+    if (lane == 0 && !cache_row(a.cache, b, start, root, a.status)) bad = true;
+    for (int j = lane; j < n; j += 32)
+        if (!rows_of(j, from, to)) bad = true;
     if (__any_sync(0xffffffffu, bad)) return;
-    const int64_t hs = h * head_step(a.cache);
-    const int rv = a.row_bytes / 16;
-    const bool scaled = L.k_scale != nullptr;
-    for (int it = lane; it < 2 * rv + (scaled ? 2 : 0); it += 32) {
-        const bool sc = it >= 2 * rv;
-        const bool val = sc ? it > 2 * rv : it >= rv;
-        char* base = (char*)(val ? L.v : L.k) + (it - (val ? rv : 0)) * 16;
-        float* sbase = val ? L.v_scale : L.k_scale;
-        for (int j0 = 0; j0 < n; j0 += 8) {
-            uint4 x[8];
-            int64_t to[8];
+    const int rv = a.row_bytes / 16, parts = 2 * rv + (a.layer[0].k_scale ? 2 : 0);
+    for (int j0 = 0; j0 < n; j0 += 8) {
+        if (n > 32 && j0 % 32 == 0 && j0 + lane < n) rows_of(j0 + lane, from, to);  // (up to 32 are at hand from the check)
+        int64_t f[8], d[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                to[k] = -1;
-                if (j0 + k >= n) continue;
-                int64_t from = 0;
-                cache_row(a.cache, b, start + path[j0 + k], from, a.status);
-                cache_row(a.cache, b, start + 1 + j0 + k, to[k], a.status);
-                if (from == to[k]) {
-                    to[k] = -1;
-                    continue;
+        for (int k = 0; k < 8; ++k) {
+            f[k] = __shfl_sync(0xffffffffu, from, (j0 + k) & 31) + hs;
+            d[k] = __shfl_sync(0xffffffffu, to, (j0 + k) & 31) + hs;
+            if (j0 + k >= n || f[k] == d[k]) d[k] = -1;
+        }
+        for (int it = lane; it < parts; it += 32) {
+            const bool sc = it >= 2 * rv, val = sc ? it > 2 * rv : it >= rv;
+            const int col = (it - (val ? rv : 0)) * 16;
+#pragma unroll 1
+            for (int l = l0; l < l1; ++l) {
+                const fe_kv& L = a.layer[l];
+                if (!sc) {
+                    char* base = (char*)(val ? L.v : L.k) + col;
+                    uint4 x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (d[k] >= 0) x[k] = *reinterpret_cast<const uint4*>(base + f[k] * a.row_bytes);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (d[k] >= 0) *reinterpret_cast<uint4*>(base + d[k] * a.row_bytes) = x[k];
+                } else {
+                    float* base = val ? L.v_scale : L.k_scale;
+                    float x[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (d[k] >= 0) x[k] = base[f[k]];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (d[k] >= 0) base[d[k]] = x[k];
                 }
-                if (sc) x[k].x = __float_as_uint(sbase[from + hs]);
-                else x[k] = *reinterpret_cast<const uint4*>(base + (from + hs) * a.row_bytes);
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if (to[k] < 0) continue;
-                if (sc) sbase[to[k] + hs] = __uint_as_float(x[k].x);
-                else *reinterpret_cast<uint4*>(base + (to[k] + hs) * a.row_bytes) = x[k];
             }
         }
     }
@@ -429,8 +435,11 @@ cudaError_t launch_cache_read(const ReadArgs& a, fe_dtype dtype, fe_dtype cache_
     return hd == 128 ? launch_read_t<bf16_t, 128, false>(a, st) : launch_read_t<bf16_t, 64, false>(a, st);
 }
 
-cudaError_t launch_cache_keep(const KeepArgs& a, cudaStream_t st) {
-    const int64_t warps = (int64_t)a.n_layers * a.B * a.cache.Hkv;
+cudaError_t launch_cache_keep(const KeepArgs& args, cudaStream_t st) {
+    KeepArgs a = args;
+    const int64_t one = (int64_t)a.n_layers * a.B * a.cache.Hkv;
+    a.layers_per_warp = one >= 152 * 32 ? 4 : 1;  // (half an SM's warps, at least, with one layer each)
+    const int64_t warps = (int64_t)((a.n_layers + a.layers_per_warp - 1) / a.layers_per_warp) * a.B * a.cache.Hkv;
     return launch_groups(keep_kernel, warps, kRowThreads / 32, a, st);
 }
 

@@ -45,10 +45,10 @@ struct ReadArgs {
     int* status;
 };
 
-constexpr int kKeepMaxLayers = 64;  // per launch (the pointers travel as kernel arguments)
+constexpr int kKeepMaxLayers = 128;  // per launch (the pointers travel as kernel arguments)
 
 struct KeepArgs {
-    int B, N, n_layers, row_bytes;
+    int B, N, n_layers, row_bytes, layers_per_warp;
     const int *path, *n_accept, *start;
     CacheView cache;  // (its pointers are per layer, below)
     fe_kv layer[kKeepMaxLayers];

@@ -252,7 +252,7 @@ def test_cache_keep(fe, dtype, cache, hd, page):
     t = fe.fe_target_init(c)
     g = gen(page + hd)
     table, n_pages = ref.paged(c, 5, g)
-    store = ref.random_cache(fe, t, c, g, layers=67, table=table, n_pages=n_pages)
+    store = ref.random_cache(fe, t, c, g, layers=131, table=table, n_pages=n_pages)
     path = torch.tensor([[1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11], [2, 3, 5, 8, 9, 20, 21, 22, 30, 31, 33],
                          [40, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0], [-1] * 11, [3, 9, 10, 11, 12, 30, 31, 32, 33, 50, 52]],
                         dtype=torch.int32)
@@ -264,7 +264,7 @@ def test_cache_keep(fe, dtype, cache, hd, page):
     raw = lambda x: x.view(torch.uint8) if x.dtype == torch.float8_e4m3fn else x
     for m, was in old.items():
         now = getattr(store, m)
-        for layer in (0, 1, 63, 66):
+        for layer in (0, 1, 127, 130):
             for b in range(5):
                 want, got = slots_of(c, raw(was[layer]), b, table).clone(), slots_of(c, raw(now[layer]), b, table)
                 src = slots_of(c, raw(was[layer]), b, table)
