@@ -128,15 +128,18 @@ int tma_box_rows(const CacheView& c, int groups) {
     return b >= 8 ? b : 0;
 }
 
-// The cache as [groups][rows][hd], rows of a page or sequence, groups = (pages or sequences) x heads
-bool make_map(CUtensorMap* map, const void* base, int hd, int rows, int groups, int box_rows) {
+// The cache as [groups][rows][hd], rows of a page or sequence, groups = (pages or sequences) x
+// heads; boxes of 64 bfloat16 or hd e4m3 elements, swizzled over their bytes
+bool make_map(CUtensorMap* map, const void* base, bool e4m3, int hd, int rows, int groups, int box_rows) {
+    const cuuint64_t es = e4m3 ? 1 : 2;
     const cuuint64_t dims[3] = {(cuuint64_t)hd, (cuuint64_t)rows, (cuuint64_t)groups};
-    const cuuint64_t strides[2] = {(cuuint64_t)hd * 2, (cuuint64_t)rows * hd * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
+    const cuuint64_t strides[2] = {(cuuint64_t)hd * es, (cuuint64_t)rows * hd * es};
+    const cuuint32_t box[3] = {e4m3 ? (cuuint32_t)hd : 64u, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
     const EncodeTiled encode = encode_tiled();
-    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
-                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode && encode(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                            const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            box[0] * es == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The queries as [B][T][H][hd]; a block of 128 rows is a box of G heads and 128 / G nodes, where G
@@ -161,15 +164,13 @@ cudaError_t launch_tc(const TreeAttnArgs& args, int num_sms, cudaStream_t st) {
     TreeAttnArgs a = args;
     CUtensorMap kmap{}, vmap{}, qmap{};
     a.q_tma = make_q_map(&qmap, a, HD);
-    if (!Q8) {
-        const CacheView& c = a.cache;
-        const int64_t groups = (int64_t)(c.page_size ? c.n_pages : a.B) * a.Hkv;
-        a.box_rows = tma_box_rows(c, groups < 0x7FFFFFFF ? (int)groups : 0);
-        const int rows = c.page_size ? c.page_size : c.max_seq;
-        if (a.box_rows && !(make_map(&kmap, c.k, HD, rows, (int)groups, a.box_rows) &&
-                            make_map(&vmap, c.v, HD, rows, (int)groups, a.box_rows)))
-            return cudaErrorInvalidValue;
-    }
+    const CacheView& c = a.cache;
+    const int64_t groups = (int64_t)(c.page_size ? c.n_pages : a.B) * a.Hkv;
+    a.box_rows = tma_box_rows(c, groups < 0x7FFFFFFF ? (int)groups : 0);
+    const int rows = c.page_size ? c.page_size : c.max_seq;
+    if (a.box_rows && !(make_map(&kmap, c.k, Q8, HD, rows, (int)groups, a.box_rows) &&
+                        (Q8 || make_map(&vmap, c.v, false, HD, rows, (int)groups, a.box_rows))))
+        return cudaErrorInvalidValue;
     const cudaError_t e = launch_k(tree_attn_tc_kernel<HD, Q8, MT>, dim3(num_sms), dim3(TcShape<HD, Q8, MT>::kThreads),
                                    tc_smem<HD, Q8, MT>(), st, false, a, kmap, vmap, qmap);
     if (e != cudaSuccess) return e;

@@ -43,34 +43,41 @@
 namespace fe {
 
 constexpr int kTcTile = 128;
+// Key tiles whose scales are at hand. A softmax still reads tile t's when the loaders may be at tile
+// t + 1 + kKeySlots (the other stream's products may be one tile further).
+constexpr int kTcScales = 8;
 using TcPlan = Plan<kAttnItemRows, kTcTile, true, 4>;
 
 // MT: 128-row query blocks a CTA must hold (1 when no item has more than 128 rows)
 template <int HD, bool Q8, int MT>
 struct TcShape {
-    static constexpr int kTileBytes = kTcTile * HD * 2;  // also a query block's
-    static constexpr int kRawBytes = kTcTile * HD;
-    static constexpr int kSlots = !Q8 && MT == 1 ? 5 : 4;  // tiles in flight
+    static constexpr int kTileBytes = kTcTile * HD * 2;  // bfloat16 tile; also a query block's
+    static constexpr int kRawBytes = kTcTile * HD;       // e4m3 tile
+    // tiles in flight: bfloat16 keys and values in one ring; e4m3 keys as they are, raw values, and
+    // converted values in three
+    static constexpr int kSlots = Q8 ? 2 : MT == 1 ? 5 : 4;
+    static constexpr int kKeySlots = Q8 ? 3 : 0;
     static constexpr int kRawSlots = Q8 ? (MT == 1 ? 3 : 2) : 0;
-    // the epilogue's staging, 2 KB a warp: its own where there is room, else the queries' buffer,
-    // whose next load then waits for the epilogue
-    static constexpr bool kStageInQ = Q8 && MT == 2 && HD == 128;
-    static constexpr int kStageBytes = kStageInQ ? 0 : 8 * 2048;
+    // the epilogue's staging: 16 columns of a warp's rows, or 8 where there is no room for more
+    static constexpr int kStageCols = Q8 && MT == 2 ? 8 : 16;
+    static constexpr int kStageBytes = 8 * 32 * kStageCols * 4;
+    static constexpr int kScaleBytes = Q8 ? kTcScales * kTcTile * 4 : 0;  // the key tiles' scales
     static constexpr int kThreads = 512;
     static constexpr int kReaders = 15;  // warps that read the segments
-    static constexpr int kData = MT * kTileBytes + kSlots * kTileBytes + kRawSlots * kRawBytes + kStageBytes;
+    static constexpr int kData = MT * kTileBytes + kSlots * kTileBytes + (kKeySlots + kRawSlots) * kRawBytes + kStageBytes + kScaleBytes;
 };
 
 constexpr int kTcSegs = 4;  // segments planned ahead
 
 struct TcState {
-    uint64_t full[6], empty[6], rawfull[4], rawempty[4], segfull[kTcSegs], segempty[kTcSegs], qfull, qempty, sfull[2],
+    uint64_t full[6], empty[6], kfull[4], kempty[4], rawfull[4], rawempty[4], segfull[kTcSegs], segempty[kTcSegs], qfull, qempty, qready, sfull[2],
         pfull[2], odone, ofree, mlfull, mlfree, drain[2], turn[2];
     Segment seg[kTcSegs];  // weight 0: no more
     uint32_t tmem;
     int abort;
     int odd[8];        // by segment: non-finite value elements were set aside
     float2 ml[2][128];  // the streams' (maximum, sum), for their join
+    float qs[2][2][128];  // e4m3: scales of the query rows [segment parity][block]
 };
 
 template <int HD, bool Q8, int MT>
@@ -121,6 +128,24 @@ __device__ __forceinline__ bool elect_one() {
 // 1024 bytes between 8-row groups (K), `half` bytes between 64-element groups (MN)
 __device__ __forceinline__ uint64_t sw128_desc_mn(uint32_t smem_addr, uint32_t half) {
     return sw128_desc(smem_addr) | ((uint64_t)(half >> 4) << 16);
+}
+
+// e4m3 operands: the key tile's descriptor (64-byte swizzle for 64-wide heads: mode 4, 512 bytes
+// between 8-row groups), the instruction descriptor (float32 from e4m3 and e4m3, K-major) and one
+// M x N x 32 step
+template <int HD>
+__device__ __forceinline__ uint64_t key_desc(uint32_t smem_addr) {
+    if (HD == 128) return sw128_desc(smem_addr);
+    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | (uint64_t)(512u >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)4 << 61;
+}
+constexpr uint32_t idesc_e4m3_f32(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
+__device__ __forceinline__ void tc_mma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
 }
 
 // D[tmem] (+)= A[tmem, bf16 pairs] * B[smem desc], one M x N x 16 step
@@ -248,6 +273,27 @@ __device__ __forceinline__ void load_tile(const void* base, const RowInfo& x, un
     }
 }
 
+// Byte offset of 16-byte chunk c of row r in an e4m3 key tile: K-major rows of HD bytes, 128-byte
+// swizzled, or 64-byte swizzled for 64-wide heads
+template <int HD>
+__device__ __forceinline__ uint32_t key_offset(int r, int c) {
+    return HD == 128 ? sw128_offset(r, c) : (uint32_t)(r * 64 + ((c ^ (r >> 1 & 3)) << 4));
+}
+
+// one key tile of e4m3 rows as they are
+template <int HD>
+__device__ __forceinline__ void load_key_tile(const void* base, const RowInfo& x, unsigned char* dst, int w, int lane) {
+    constexpr int CH = HD / 16, RP = 32 / CH;
+    const int c = lane % CH;
+    const unsigned long long mine = x.row < 0 ? 0ull : (unsigned long long)base + (unsigned long long)x.row * HD;
+#pragma unroll 2
+    for (int i = 0; i < 32 / RP; ++i) {
+        const int r = i * RP + lane / CH;
+        const unsigned long long src = __shfl_sync(0xffffffffu, mine, r);
+        cp_async16(smem_u32(dst) + key_offset<HD>(w * 32 + r, c), (const void*)((src ? src : (unsigned long long)base) + c * 16), src != 0);
+    }
+}
+
 // Zero the non-finite elements of a lane's own chunks of a value tile, in rows from `first` on.
 template <int HD>
 __device__ __forceinline__ bool scrub_tile(unsigned char* tile, int first, int w, int lane) {
@@ -370,6 +416,14 @@ __device__ __forceinline__ void tc_ld16_wait(uint32_t* r) {
                  :
                  : "memory");
 }
+__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+        : "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tc_ld32_start(uint32_t taddr, uint32_t* r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
@@ -402,6 +456,11 @@ __device__ __forceinline__ uint64_t pair_f32(uint32_t lo, uint32_t hi) { return 
 __device__ __forceinline__ uint64_t fma_x2(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t d;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul_x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
 __device__ __forceinline__ uint64_t add_x2(uint64_t a, uint64_t b) {
@@ -451,13 +510,30 @@ __device__ __noinline__ void rescale_row(uint32_t ts, int np, uint32_t to, int n
 // Bound by the exponentials (16 a clock and SM), in whose shade the next 32 scores are loaded and
 // their maximum taken. A loop with a short body: the CTA's roles share the instruction caches, and
 // unrolled rows made every one of them wait for fetches.
-template <int HD>
-__device__ __forceinline__ void softmax_row(uint32_t ts, uint32_t to, float scale2, bool first, float& m, float& sum) {
+// With e4m3 keys (Q8) the scores still lack their keys' scales, ks (shared memory).
+template <int HD, bool Q8>
+__device__ __forceinline__ void softmax_row(uint32_t ts, uint32_t to, float scale2, bool first, const float* ks, float& m,
+                                            float& sum) {
     const uint64_t sc = pair_f32(__float_as_uint(scale2), __float_as_uint(scale2));
     uint32_t x[32], y[32];
     uint64_t z[2] = {0, 0};
+    auto scale32 = [&](uint32_t* v, int c) {
+        if constexpr (Q8) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+                const float4 f = *reinterpret_cast<const float4*>(ks + c + e);
+                const uint64_t a = mul_x2(pair_f32(v[e], v[e + 1]), pair_f32(__float_as_uint(f.x), __float_as_uint(f.y)));
+                const uint64_t b = mul_x2(pair_f32(v[e + 2], v[e + 3]), pair_f32(__float_as_uint(f.z), __float_as_uint(f.w)));
+                v[e] = (uint32_t)a;
+                v[e + 1] = (uint32_t)(a >> 32);
+                v[e + 2] = (uint32_t)b;
+                v[e + 3] = (uint32_t)(b >> 32);
+            }
+        }
+    };
     tc_ld32_start(ts, x);
     tc_ld32_wait(x);
+    scale32(x, 0);
     float mx = max32(x) * scale2;
 #pragma unroll 1
     for (int c = 0; c < kTcTile; c += 32) {
@@ -487,6 +563,7 @@ __device__ __forceinline__ void softmax_row(uint32_t ts, uint32_t to, float scal
         exps(0);
         tc_ld32_wait(y);
         exps(16);
+        scale32(y, (c + 32) % kTcTile);
         mx = max32(y) * scale2;
         tc_st16(ts + c / 2, pk);
 #pragma unroll
@@ -538,6 +615,60 @@ __device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segmen
     }
 }
 
+// A query row, for the e4m3 product with keys as they are: q = 2^c (hi + lo), hi the e4m3 rounding
+// of q / 2^c with the smallest c that fits the row's largest magnitude under 448, lo that of the
+// rest. A bfloat16 number's 8 significant bits are two times e4m3's 4, so the split is exact down
+// to 2^-10 of the row's scale (2^-18 of its largest element), and costs the tensor cores nothing:
+// two products at twice the rate. In place: the 64 bytes of elements 32 k .. become their 32 hi
+// and 32 lo bytes. Returns 2^c.
+template <int HD>
+__device__ __forceinline__ float split_query_row(unsigned char* block, int row) {
+    auto chunk = [&](int c) { return reinterpret_cast<uint4*>(block + (c >> 3) * 16384 + sw128_offset(row, c & 7)); };
+    float m = 0.f;
+#pragma unroll 1
+    for (int c = 0; c < HD / 8; ++c) {
+        float x[8];
+        Vec16<bf16_t>::widen(*chunk(c), x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_f32(x[e]) ? fabsf(x[e]) : 0.f);
+    }
+    const uint32_t u = __float_as_uint(m);
+    const int c2 = max((int)(u >> 23) - 135 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0), -100);
+    const float inv = __uint_as_float((uint32_t)(127 - c2) << 23);
+#pragma unroll 1
+    for (int k = 0; k < HD / 32; ++k) {
+        uint4 v[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = *chunk(4 * k + c);
+        uint32_t hi[8], lo[8];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float x[8];
+            Vec16<bf16_t>::widen(v[c], x);
+#pragma unroll
+            for (int e = 0; e < 8; e += 4) {
+                uint32_t h[2], l[2];
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const float a = x[e + 2 * z], b = x[e + 2 * z + 1];
+                    const float y0 = finite_f32(a) ? a * inv : __uint_as_float(0x7FC00000u);
+                    const float y1 = finite_f32(b) ? b * inv : __uint_as_float(0x7FC00000u);
+                    h[z] = f32x2_to_e4m3(y0, y1);
+                    const float2 f = e4m3x2_to_f32(h[z]);
+                    l[z] = f32x2_to_e4m3(y0 - f.x, y1 - f.y);
+                }
+                hi[2 * c + e / 4] = h[0] | h[1] << 16;
+                lo[2 * c + e / 4] = l[0] | l[1] << 16;
+            }
+        }
+        *chunk(4 * k) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *chunk(4 * k + 1) = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+        *chunk(4 * k + 2) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        *chunk(4 * k + 3) = make_uint4(lo[4], lo[5], lo[6], lo[7]);
+    }
+    return __uint_as_float((uint32_t)(127 + c2) << 23);
+}
+
 // Whether tile t of the segment (from its first) comes by TMA: a whole tile of prefix slots.
 __device__ __forceinline__ bool by_tma(const TreeAttnArgs& a, const Segment& g, int t) {
     return a.box_rows > 0 && (g.t0 + t + 1) * kTcTile <= g.s.P;
@@ -569,11 +700,13 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     tree_attn_tc_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ CUtensorMap kmap,
                         const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap) {
     using SH = TcShape<HD, Q8, MT>;
-    constexpr int S = SH::kSlots, RS = Q8 ? SH::kRawSlots : 1, TB = SH::kTileBytes;
+    constexpr int S = SH::kSlots, KS = Q8 ? SH::kKeySlots : 1, RS = Q8 ? SH::kRawSlots : 1, TB = SH::kTileBytes;
     extern __shared__ __align__(1024) unsigned char qbuf[];
     unsigned char* ring = qbuf + MT * TB;
-    unsigned char* rawring = ring + S * TB;
-    unsigned char* stages = SH::kStageInQ ? qbuf : rawring + SH::kRawSlots * SH::kRawBytes;
+    unsigned char* keyring = ring + S * TB;  // (e4m3)
+    unsigned char* rawring = keyring + SH::kKeySlots * SH::kRawBytes;
+    unsigned char* stages = rawring + SH::kRawSlots * SH::kRawBytes;
+    float* key_scales = (float*)(stages + SH::kStageBytes);
     TcState& st = *reinterpret_cast<TcState*>(qbuf + SH::kData);
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     griddep_launch_dependents();
@@ -587,6 +720,10 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             mbar_init(&st.full[i], 128);
             mbar_init(&st.empty[i], MT);  // (a tile that one stream alone used is released twice by it)
         }
+        for (int i = 0; i < KS; ++i) {
+            mbar_init(&st.kfull[i], 129);  // the loaders (scales) and the TMA warp (keys)
+            mbar_init(&st.kempty[i], MT);
+        }
         for (int i = 0; i < RS; ++i) {
             mbar_init(&st.rawfull[i], 1);
             mbar_init(&st.rawempty[i], 128);
@@ -597,6 +734,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         }
         mbar_init(&st.qfull, 256);
         mbar_init(&st.qempty, 2);  // both streams' score products
+        mbar_init(&st.qready, 8);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&st.sfull[i], 1);
             mbar_init(&st.pfull[i], 4);
@@ -636,14 +774,16 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     if (warp >= 8 && warp < 12) {  // ---- loaders
         const int w = warp - 8;
         RingPos<S> pos;
+        RingPos<KS> kpos;
         RingPos<RS> rpos;
-        bool reuse = false;  // the ring has been filled once
+        bool reuse = false, kreuse = false;  // the rings have been filled once
+        uint32_t tiles = 0;  // key tiles so far
         while (ok && next(g)) {
             const int nt = g.t1 - g.t0;
             // what the lane knows of its rows in tiles t, t + 1, t + 2 (addresses and scales are
             // fetched a tile ahead of their use)
             RowInfo x0{-1, 0.f, 0.f};
-            if (!by_tma(a, g, 0)) x0 = row_info<Q8>(a, g, g.t0, w * 32 + lane);
+            if (Q8 || !by_tma(a, g, 0)) x0 = row_info<Q8>(a, g, g.t0, w * 32 + lane);
             RowInfo x1 = x0, x2 = x0;
 #pragma unroll 1
             for (int l = 0; l < 2 * nt; ++l) {  // K0 K1 V0 K2 V1 ...
@@ -652,7 +792,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 if (!val) {
                     x0 = x1;
                     x1 = l == 0 ? x0 : x2;
-                    if (!by_tma(a, g, tt + 1)) x2 = row_info<Q8>(a, g, g.t0 + tt + 1, w * 32 + lane);
+                    if (Q8 || !by_tma(a, g, tt + 1)) x2 = row_info<Q8>(a, g, g.t0 + tt + 1, w * 32 + lane);
                 }
                 // (a key tile tt is loaded with x1's rows; the value tile loaded after it is tt - 1,
                 // the last one tt)
@@ -661,6 +801,19 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 uint64_t* full = &st.full[pos.slot];
                 const int first = g.s.P - (g.t0 + tt) * kTcTile;  // first row of the tile that is a node's
                 if constexpr (Q8) {
+                    if (!val) {  // the rows' scales; the rows themselves where TMA cannot fetch them
+                        if (kreuse && !(ok = wait(&st.kempty[kpos.slot], kpos.phase ^ 1u))) break;
+                        key_scales[(tiles++ % kTcScales) * kTcTile + w * 32 + lane] = x.row >= 0 ? x.ks : 1.f;
+                        if (a.box_rows > 0) {
+                            mbar_arrive(&st.kfull[kpos.slot]);
+                        } else {
+                            load_key_tile<HD>(a.cache.k, x, keyring + kpos.slot * SH::kRawBytes, w, lane);
+                            cp_async_arrive(&st.kfull[kpos.slot]);
+                        }
+                        kpos.skip(1);
+                        kreuse |= kpos.slot == 0;
+                        continue;
+                    }
                     if (!(ok = wait(&st.rawfull[rpos.slot], rpos.phase))) break;
                 }
                 // (every slot's release is waited for, also of tiles that come by TMA: a barrier's phase is
@@ -672,8 +825,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     continue;
                 }
                 if constexpr (Q8) {
-                    const bool odd = convert_tile<HD>(rawring + rpos.slot * SH::kRawBytes, x.row >= 0, val ? x.vs : x.ks,
-                                                      val ? first : kTcTile, dst, w, lane);
+                    const bool odd = convert_tile<HD>(rawring + rpos.slot * SH::kRawBytes, x.row >= 0, x.vs, first, dst, w, lane);
                     if (odd) st.odd[(seg - 1) & 7] = 1;
                     fence_async_proxy();
                     mbar_arrive(&st.rawempty[rpos.slot]);
@@ -699,14 +851,20 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         cp_async_wait_all();
     } else if (warp == 12 || warp == 13) {  // ---- MMA issuers, one thread per stream
         const int gs = warp - 12;
-        const uint32_t id_qk = idesc_bf16_f32(128, kTcTile);
+        const uint32_t id_qk = Q8 ? idesc_e4m3_f32(128, kTcTile) : idesc_bf16_f32(128, kTcTile);
         const uint32_t id_pv = idesc_bf16_f32(128, HD) | (1u << 16);  // B is MN-major
         const uint32_t ts = tmem + gs * 128, to = tmem + 256 + gs * 128;
         const uint64_t ring_d = sw128_desc(smem_u32(ring)), ring_mn = sw128_desc_mn(smem_u32(ring), 16384);
         // The streams take turns: a stream's P V and next Q K^T are issued together and run while the
         // other's softmax does. (Issued side by side, both streams' products end together and then
         // both softmaxes compete.) The warp runs as one, and one lane issues.
+        const uint64_t key_d = key_desc<HD>(smem_u32(keyring));
+        // keys and values: positions in one ring, or (e4m3) in a ring each
+        constexpr int KR = Q8 ? KS : S;
+        uint64_t* const kfull = Q8 ? st.kfull : st.full;
+        uint64_t* const kempty = Q8 ? st.kempty : st.empty;
         RingPos<S> base;
+        RingPos<KR> kbase;
         uint32_t np = 0, turn = 0;
         while (ok && next(g)) {
             const int nt = g.t1 - g.t0;
@@ -714,10 +872,11 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             const int step = pair ? 1 : 2, first = pair ? 0 : gs;
             const uint64_t qd = sw128_desc(smem_u32(qbuf + (pair ? gs * TB : 0)));
             const bool twice = MT == 2 && !pair;
-            RingPos<S> kp = base, vp = base;
-            kp.skip(first ? pos_k(first) : 0);
-            vp.skip(pos_v(first, nt));
-            if (first < nt) ok = wait(&st.qfull, seg - 1);
+            RingPos<KR> kp = kbase;
+            RingPos<S> vp = base;
+            kp.skip(Q8 ? first : pos_k(first));
+            vp.skip(Q8 ? first : pos_v(first, nt));
+            if (first < nt) ok = wait(Q8 ? &st.qready : &st.qfull, seg - 1);
             bool qdone = false;
             // (both streams make the same number of rounds, the last of stream 1 may be empty)
 #pragma unroll 1
@@ -733,7 +892,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 // a stream's turn; its K tile is waited for before the products if it is there already
                 if (gs == 1 || turn > 0) ok = ok && wait(&st.turn[gs], gs == 1 ? turn : turn - 1);
                 ++turn;
-                bool kthere = qk && mbar_try_wait(&st.full[kp.slot], kp.phase);
+                bool kthere = qk && mbar_try_wait(&kfull[kp.slot], kp.phase);
                 if (!__all_sync(0xffffffffu, ok)) {
                     ok = false;
                     break;
@@ -749,13 +908,19 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         tc_mma_ts(to, ts + k * 8, vd + k * 128, id_pv, t0 > 0 || k ? 1u : 0u);
                 }
                 if (qk && !kthere) {
-                    ok = __all_sync(0xffffffffu, wait(&st.full[kp.slot], kp.phase));
+                    ok = __all_sync(0xffffffffu, wait(&kfull[kp.slot], kp.phase));
                     if (!ok) break;
                     fence_async_proxy();
                     tc_fence_after();
                 }
                 if (leader) {
-                    if (qk) {
+                    if (qk && Q8) {
+                        const uint64_t kd = key_d + (uint32_t)(kp.slot * (SH::kRawBytes / 16));
+#pragma unroll
+                        for (int k = 0; k < HD / 16; ++k)  // 32 elements' hi, then their lo part, with the same keys
+                            tc_mma_e4m3(ts, qd + (k >> 2) * 1024 + 2 * (k & 3), kd + 2 * (k >> 1), id_qk, k ? 1u : 0u);
+                        tc_commit(&st.sfull[gs]);
+                    } else if (qk) {
                         const uint64_t kd = ring_d + (uint32_t)(kp.slot * (TB / 16));
 #pragma unroll
                         for (int k = 0; k < HD / 16; ++k)  // 32 bytes a step, 16384 to the next 64 columns
@@ -764,8 +929,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     }
                     mbar_arrive(&st.turn[gs ^ 1]);
                     if (qk) {
-                        tc_commit(&st.empty[kp.slot]);
-                        if (twice) tc_commit(&st.empty[kp.slot]);
+                        tc_commit(&kempty[kp.slot]);
+                        if (twice) tc_commit(&kempty[kp.slot]);
                         if (tt + 2 * step >= nt) tc_commit(&st.qempty);
                     }
                     if (pv) {
@@ -774,8 +939,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     }
                 }
                 __syncwarp();
-                if (pv) vp.skip(pos_v(min(tt + step, nt - 1), nt) - pos_v(tt, nt));
-                if (qk) kp.skip(2 * step - (tt + step == 0));
+                if (pv) vp.skip(Q8 ? step : pos_v(min(tt + step, nt - 1), nt) - pos_v(tt, nt));
+                if (qk) kp.skip(Q8 ? step : 2 * step - (tt + step == 0));
                 qdone |= qk;
             }
             if (ok && elect_one()) {
@@ -783,7 +948,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 tc_commit(&st.odone);
             }
             __syncwarp();
-            base.skip_long(2 * nt);
+            base.skip_long(Q8 ? nt : 2 * nt);
+            kbase.skip_long(Q8 ? nt : 2 * nt);
         }
         // every MMA issued has finished reading shared memory and TMEM before the CTA ends
         if (elect_one()) tc_commit(&st.drain[gs]);
@@ -808,8 +974,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             }
             __syncwarp();
             if (!more) break;
-            if (a.q_tma) {  // the queries, once the buffer's last ones (and what was staged there) are done with
-                if (n > 0 && !(ok = SH::kStageInQ ? wait(&st.ofree, n - 1) : wait(&st.qempty, n - 1))) break;
+            if (a.q_tma) {  // the queries, once the buffer's last ones are done with
+                if (n > 0 && !(ok = wait(&st.qempty, n - 1))) break;
                 if (lane == 0) {
                     mbar_arrive_expect_tx(&st.qfull, g.weight * TB);
                     mbar_arrive_n(&st.qfull, 255);  // in the place of the softmax warps' 256 arrivals
@@ -824,17 +990,48 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         }
         // (after a failed wait: leave with no copy in flight)
         if (!ok && a.q_tma && n > 0) mbar_wait(&st.qfull, (n - 1) & 1u, a.status, 100000000LL);
-    } else if (Q8 && warp == 15) {  // ---- raw rows of an e4m3 cache
+    } else if (Q8 && warp == 15) {  // ---- an e4m3 cache's keys (TMA) and raw values (bulk copies)
+        RingPos<KS> kpos;
         RingPos<RS> pos;
-        uint32_t i = 0;
+        bool kreuse = false;
+        uint32_t i = 0, ktiles = 0;
         while (ok && next(g)) {
             const int nt = g.t1 - g.t0;
+            const int br = a.box_rows > 0 ? a.box_rows : kTcTile, boxes = kTcTile / br;
 #pragma unroll 1
-            for (int l = 0; l < 2 * nt; ++l, ++i) {
-                const bool val = tile_is_value(l, nt);
+            for (int l = 0; l < 2 * nt; ++l) {
                 const int tt = tile_number(l, nt);
-                if (i >= (uint32_t)RS && !(ok = wait(&st.rawempty[pos.slot], pos.phase ^ 1u))) break;
                 const int s0 = (g.t0 + tt) * kTcTile, s1 = min(s0 + kTcTile, g.end);
+                if (!tile_is_value(l, nt)) {
+                    if (kreuse && !(ok = wait(&st.kempty[kpos.slot], kpos.phase ^ 1u))) break;
+                    uint64_t* full = &st.kfull[kpos.slot];
+                    if (a.box_rows > 0) {
+                        if (lane == 0) mbar_arrive_expect_tx(full, SH::kRawBytes);
+                        __syncwarp();
+                        if (lane < boxes) {  // a box of rows a lane; boxes past the item's end read as zeros, or hidden rows
+                            const int slot = s0 + lane * br;
+                            int y = slot, z = g.b * a.Hkv + g.h;
+                            if (a.cache.page_size) {
+                                const int lp = slot / a.cache.page_size;
+                                y = slot - lp * a.cache.page_size;
+                                z = a.cache.n_pages * a.Hkv;  // past the pool
+                                if (slot < g.end) {
+                                    const int pg = a.cache.table[(int64_t)g.b * a.cache.max_pages + lp];
+                                    if (pg >= 0 && pg < a.cache.n_pages) z = pg * a.Hkv + g.h;
+                                    else atomicOr(a.status, ST_DEVICE);
+                                }
+                            }
+                            tma_load_3d(smem_u32(keyring) + kpos.slot * SH::kRawBytes + lane * br * HD, &kmap, 0, y, z, full);
+                        }
+                    } else if (lane == 0) {
+                        mbar_arrive(full);
+                    }
+                    ++ktiles;
+                    kpos.skip(1);
+                    kreuse |= kpos.slot == 0;
+                    continue;
+                }
+                if (i >= (uint32_t)RS && !(ok = wait(&st.rawempty[pos.slot], pos.phase ^ 1u))) break;
                 const int ps = a.cache.page_size ? a.cache.page_size : a.cache.max_seq;
                 const int p0 = s0 / ps, np = (s1 - 1) / ps - p0 + 1;
                 // a lane's runs of rows: pages p0 + lane, + 32, ...
@@ -846,26 +1043,36 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     row += g.h * head_step(a.cache);
                     return true;
                 };
-                int from, rows, bytes = 0;
-                int64_t row;
+                // the first round's runs stay at hand; more than 32 pages are looked up again
+                int from = 0, rows = 0, bytes = 0;
+                int64_t row = 0;
+                const bool mine = lane < np && run(lane, from, rows, row);
+                if (mine) bytes = rows * HD;
+                int f2, r2;
+                int64_t w2;
 #pragma unroll 1
-                for (int k = lane; k < np; k += 32)
-                    if (run(k, from, rows, row)) bytes += rows * HD;
+                for (int k = lane + 32; k < np; k += 32)
+                    if (run(k, f2, r2, w2)) bytes += r2 * HD;
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) bytes += __shfl_xor_sync(0xffffffffu, bytes, o);
                 uint64_t* full = &st.rawfull[pos.slot];
                 if (lane == 0) mbar_arrive_expect_tx(full, bytes);
                 __syncwarp();
                 unsigned char* dst = rawring + pos.slot * SH::kRawBytes;
-                const char* src = (const char*)(val ? a.cache.v : a.cache.k);
+                const char* src = (const char*)a.cache.v;
+                if (mine) bulk_g2s(dst + from * HD, src + row * HD, rows * HD, full);
 #pragma unroll 1
-                for (int k = lane; k < np; k += 32)
-                    if (run(k, from, rows, row)) bulk_g2s(dst + from * HD, src + row * HD, rows * HD, full);
+                for (int k = lane + 32; k < np; k += 32)
+                    if (run(k, f2, r2, w2)) bulk_g2s(dst + f2 * HD, src + w2 * HD, r2 * HD, full);
                 pos.skip(1);
+                ++i;
             }
         }
         // leave with no copy in flight: the last tiles have landed
         for (uint32_t j = i > (uint32_t)RS ? i - RS : 0; j < i; ++j) mbar_wait(&st.rawfull[j % RS], (j / RS) & 1u, a.status);
+        if (!ok && a.box_rows > 0)
+            for (uint32_t j = ktiles > (uint32_t)KS ? ktiles - KS : 0; j < ktiles; ++j)
+                mbar_wait(&st.kfull[j % KS], (j / KS) & 1u, a.status, 100000000LL);
     } else if (!Q8 && warp == 15) {  // ---- whole tiles by TMA
         RingPos<S> pos;
         bool reuse = false;
@@ -937,10 +1144,27 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 mbar_arrive(&st.qfull);
             }
         };
+        // e4m3: the warp's rows of segment number n's queries (as they have arrived) split for the product
+        auto split = [&](const Segment& s, uint32_t n) -> bool {
+            if constexpr (Q8) {
+                if (!wait(&st.qfull, n)) return false;
+                if (s.weight == 2 || gs == 0) {
+                    st.qs[n & 1][gs][wl * 32 + lane] = split_query_row<HD>(qbuf + gs * TB, wl * 32 + lane);
+                    fence_async_proxy();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&st.qready);
+            }
+            return true;
+        };
+        uint32_t ktile = 0;  // the segment's first key tile (of kTcScales)
         Segment g2;  // the segment after this one, once its queries are on their way
         bool more = next(g2);
-        if (more) queries(g2);
-        while (more) {
+        if (more) {
+            queries(g2);
+            ok = split(g2, 0);
+        }
+        while (more && ok) {
             g = g2;
             const uint32_t cur = seg - 1;  // this segment's number
             const int nt = g.t1 - g.t0;
@@ -975,7 +1199,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         }
                         tc_wait_st();
                     }
-                    softmax_row<HD>(ts, to, scale2, tt < 2 && (tt == 0 || !pair), m, sum);
+                    softmax_row<HD, Q8>(ts, to, Q8 ? scale2 * st.qs[cur & 1][pair ? gs : 0][wl * 32 + lane] : scale2,
+                                        tt < 2 && (tt == 0 || !pair), key_scales + (ktile + tt) % kTcScales * kTcTile, m, sum);
                     tc_wait_st();
                 }
                 tc_fence_before();
@@ -985,10 +1210,12 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             // the next segment's queries may come once this one's scores are all done
             if (!ok) break;
             more = next(g2);
-            if (more && !SH::kStageInQ && !a.q_tma) {
+            if (more && !a.q_tma) {
                 if (!(ok = wait(&st.qempty, cur))) break;
                 queries(g2);
             }
+            if (more && !(ok = split(g2, cur + 1))) break;
+            ktile += nt;
             // ---- the segment's result
             if (!(ok = wait(&st.odone, cur))) break;
             tc_fence_after();
@@ -1012,9 +1239,10 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             nj += join;
             // (a joined block's columns are shared out between the streams' warps)
             if (!idle && (pair || join || gs == 0)) {
-                // rows leave through shared memory, 16 columns at a time, so that a warp writes whole
+                // rows leave through shared memory, 8 or 16 columns at a time, so that a warp writes whole
                 // sectors: the lanes' rows as addresses of the output or of the partial
-                unsigned char* stage = stages + warp * (SH::kStageInQ ? TB / 4 : 2048);
+                constexpr int CW = SH::kStageCols, K4 = CW / 4;  // columns a round; 16-byte chunks, and lanes, of a row
+                unsigned char* stage = stages + warp * (32 * CW * 4);
                 const int head = g.h * a.G + row % a.G;
                 const int64_t pr = ((int64_t)blockIdx.x * 2 + g.slot) * kAttnItemRows + (row - g.m * kAttnItemRows);
                 const unsigned long long mine =
@@ -1028,40 +1256,45 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 f0 *= norm;
                 f1 = join ? f1 * norm : f0;
                 const bool zero = g.whole && sum == 0.f;
-                unsigned long long rows[4];  // the rows that this lane stores parts of
+                unsigned long long rows[K4];  // the rows that this lane stores parts of
 #pragma unroll
-                for (int k = 0; k < 4; ++k) rows[k] = __shfl_sync(0xffffffffu, mine, 8 * k + lane / 4);
+                for (int k = 0; k < K4; ++k) rows[k] = __shfl_sync(0xffffffffu, mine, 32 / K4 * k + lane / K4);
                 const bool vec = a.out_vec;
                 const uint32_t other = join ? tmem + 256 + (gs ^ 1) * 128 + lanes : to;
 #pragma unroll 1
-                for (int c = join && gs ? HD / 2 : 0; c < (join && !gs ? HD / 2 : HD); c += 16) {
-                    uint32_t u[16], v[16];
-                    tc_ld16_start(to + c, u);
-                    tc_ld16_start(other + c, v);
-                    tc_ld16_wait(u);
-                    tc_ld16_wait(v);
+                for (int c = join && gs ? HD / 2 : 0; c < (join && !gs ? HD / 2 : HD); c += CW) {
+                    uint32_t u[CW], v[CW];
+                    if constexpr (CW == 16) {
+                        tc_ld16_start(to + c, u);
+                        tc_ld16_start(other + c, v);
+                        tc_ld16_wait(u);
+                        tc_ld16_wait(v);
+                    } else {
+                        tc_ld8(to + c, u);
+                        tc_ld8(other + c, v);
+                    }
                     __syncwarp();
-                    // chunk k of row l lies at 16 (k ^ l / 2) of the row's 64 bytes: no bank conflicts
+                    // chunk k of row l lies at 16 (k ^ l / 2) (or l / 4) of the row's bytes: no bank conflicts
+                    auto place = [&](int r, int k) { return r * (CW * 4) + ((k ^ (r >> (CW == 16 ? 1 : 2))) & (K4 - 1)) * 16; };
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                    for (int k = 0; k < K4; ++k) {
                         float o[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             o[e] = zero ? 0.f : __uint_as_float(u[4 * k + e]) * f0 + __uint_as_float(v[4 * k + e]) * f1;
-                        *reinterpret_cast<float4*>(stage + lane * 64 + ((k ^ (lane >> 1)) & 3) * 16) = make_float4(o[0], o[1], o[2], o[3]);
+                        *reinterpret_cast<float4*>(stage + place(lane, k)) = make_float4(o[0], o[1], o[2], o[3]);
                     }
                     __syncwarp();
-                    float4 y[4];
+                    float4 y[K4];
+                    const int col = c + 4 * (lane % K4);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {  // four lanes a row
-                        const int r = 8 * k + lane / 4;
-                        y[k] = *reinterpret_cast<const float4*>(stage + r * 64 + (((lane & 3) ^ (r >> 1)) & 3) * 16);
-                    }
+                    for (int k = 0; k < K4; ++k)  // K4 lanes a row
+                        y[k] = *reinterpret_cast<const float4*>(stage + place(32 / K4 * k + lane / K4, lane % K4));
                     if (g.whole) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
+                        for (int k = 0; k < K4; ++k) {
                             const uint2 w = make_uint2(pack_bf16(y[k].x, y[k].y), pack_bf16(y[k].z, y[k].w));
-                            bf16_t* d = (bf16_t*)rows[k] + c + 4 * (lane & 3);
+                            bf16_t* d = (bf16_t*)rows[k] + col;
                             if (!rows[k]) continue;
                             if (vec) {
                                 *reinterpret_cast<uint2*>(d) = w;
@@ -1074,8 +1307,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         }
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (rows[k]) *reinterpret_cast<float4*>((float*)rows[k] + c + 4 * (lane & 3)) = y[k];
+                        for (int k = 0; k < K4; ++k)
+                            if (rows[k]) *reinterpret_cast<float4*>((float*)rows[k] + col) = y[k];
                     }
                 }
                 __syncwarp();
@@ -1096,11 +1329,6 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 // be at most three segments ahead; the other stream is at most one behind)
                 if (warp == 0) st.odd[(cur + 4) & 7] = 0;
                 mbar_arrive(&st.ofree);
-            }
-            if (SH::kStageInQ && more && !a.q_tma) {
-                // the buffer held this segment's staged rows
-                if (!(ok = wait(&st.ofree, cur))) break;
-                queries(g2);
             }
         }
     }
