@@ -342,48 +342,66 @@ __device__ __forceinline__ uint2 scale_factors(float scale) {
     return make_uint2(f1 | f1 << 16, f2 | f2 << 16);
 }
 
-// What convert_tile's straight path leaves out: zeros where there is no row, the second factor of
-// scales above 2^7, NaN codes (to NaN, or to zero in a node's value row, which is reported).
-__device__ __forceinline__ bool convert_rare(const uint32_t (&in)[4], uint32_t f1, uint32_t f2, bool node, uint32_t (&o)[8]) {
+// A lane's 16 numbers of a row, as two 16-byte chunks of a bfloat16 tile. Lanes of a row's second 64
+// columns store their chunks in the other order, so that eight lanes store into different banks.
+template <int HD>
+__device__ __forceinline__ void store_converted(unsigned char* dst, int row, int c, const uint32_t (&o)[8]) {
+    unsigned char* base = dst + (c >> 2) * 16384;
+    const int swap = c >> 2, c0 = 2 * (c & 3) + swap, c1 = 2 * (c & 3) + 1 - swap;
+    const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
+    *reinterpret_cast<uint4*>(base + sw128_offset(row, c0)) = swap ? hi : lo;
+    *reinterpret_cast<uint4*>(base + sw128_offset(row, c1)) = swap ? lo : hi;
+}
+
+// The warp's rows of a tile once more, with what convert_tile's loop leaves out: the second factor
+// of scales above 2^7, NaN codes (to NaN, or in rows from `first` on to zero: returns whether there
+// were any).
+template <int HD>
+__device__ __noinline__ bool convert_rare(const unsigned char* raw, uint2 mine, int first, unsigned char* dst, int w, int lane) {
+    constexpr int CH = HD / 16, RP = 32 / CH;
+    const int c = lane % CH;
     bool odd = false;
+#pragma unroll 1
+    for (int i = 0; i < 32 / RP; ++i) {
+        const int r = i * RP + lane / CH, row = w * 32 + r;
+        const uint32_t f1 = __shfl_sync(0xffffffffu, mine.x, r), f2 = __shfl_sync(0xffffffffu, mine.y, r);
+        const uint4 u = *reinterpret_cast<const uint4*>(raw + row * HD + c * 16);
+        const uint32_t in[4] = {u.x, u.y, u.z, u.w};
+        uint32_t o[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = f1 == 0 ? 0u : mul_bf16x2(o[e], f2);
+        for (int e = 0; e < 4; ++e) e4m3x4_to_bf16(in[e], o[2 * e], o[2 * e + 1]);
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-        if (f1 != 0 && (in[e / 4] >> (8 * (e & 3)) & 0x7Fu) == 0x7Fu) {
-            const uint32_t m = e & 1 ? 0xFFFF0000u : 0x0000FFFFu;
-            o[e / 2] = (o[e / 2] & ~m) | (node ? 0u : 0x7FC07FC0u & m);
-            odd |= node;
-        }
+        for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(mul_bf16x2(o[e], f1), f2);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (f1 != 0 && (in[e / 4] >> (8 * (e & 3)) & 0x7Fu) == 0x7Fu) {
+                const uint32_t m = e & 1 ? 0xFFFF0000u : 0x0000FFFFu;
+                o[e / 2] = (o[e / 2] & ~m) | (row >= first ? 0u : 0x7FC07FC0u & m);
+                odd |= row >= first;
+            }
+        store_converted<HD>(dst, row, c, o);
+    }
     return odd;
 }
 
-// One tile of e4m3 rows, converted: raw [128][HD] bytes to the bfloat16 values they stand for
-// (number * scale, exact). Rows without a cache row become zero; in rows from `first` on, so do
-// NaN elements (returns whether there were any).
+// One value tile of e4m3 rows, converted: raw [128][HD] bytes to the bfloat16 values they stand for
+// (number * scale, exact); rows without a cache row become zero (their factor is zero). The loop
+// has no branches; what it leaves out is looked for along the way and rarely found (convert_rare).
 template <int HD>
 __device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_row, float scale, int first,
                                              unsigned char* dst, int w, int lane) {
     constexpr int CH = HD / 16, RP = 32 / CH;
     const int c = lane % CH;
-    const uint2 mine = has_row ? scale_factors(scale) : make_uint2(0, 0);
-    bool odd = false;
-    // lanes of a row's second 64 columns store their two chunks in the other order, so that eight
-    // lanes store into different banks
-    unsigned char* base = dst + (c >> 2) * 16384 + w * 4096;
-    const int swap = c >> 2, c0 = 2 * (c & 3) + swap, c1 = 2 * (c & 3) + 1 - swap;
-    const bool big = __any_sync(0xffffffffu, mine.y != 0x3F803F80u && mine.x != 0);  // some scale above 2^7
-    // a step converts RP rows; the next step's numbers load meanwhile
+    const uint2 mine = has_row ? scale_factors(scale) : make_uint2(0, 0x3F803F80u);
     const unsigned char* src = raw + (w * 32 + lane / CH) * HD + c * 16;
-    uint4 u = *reinterpret_cast<const uint4*>(src);
-#pragma unroll 1
+    uint32_t nan = 0;
+#pragma unroll 2
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = i * RP + lane / CH;
         const uint32_t f1 = __shfl_sync(0xffffffffu, mine.x, r);
+        const uint4 u = *reinterpret_cast<const uint4*>(src + i * RP * HD);
         const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-        src += RP * HD;
-        if (i + 1 < 32 / RP) u = *reinterpret_cast<const uint4*>(src);
-        uint32_t o[8], nan = 0;
+        uint32_t o[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             nan |= (in[e] & 0x7F7F7F7Fu) + 0x01010101u;
@@ -391,13 +409,10 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = mul_bf16x2(o[e], f1);
-        // rows without a cache row (f1 = 0), NaN codes, large scales: rare
-        if (__any_sync(0xffffffffu, (nan & 0x80808080u) != 0 || f1 == 0) || big) odd |= convert_rare(in, f1, __shfl_sync(0xffffffffu, mine.y, r), w * 32 + r >= first, o);
-        const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
-        *reinterpret_cast<uint4*>(base + sw128_offset(r, c0)) = swap ? hi : lo;
-        *reinterpret_cast<uint4*>(base + sw128_offset(r, c1)) = swap ? lo : hi;
+        store_converted<HD>(dst, w * 32 + r, c, o);
     }
-    return odd;
+    if (!__any_sync(0xffffffffu, (nan & 0x80808080u) != 0 || mine.y != 0x3F803F80u)) return false;
+    return convert_rare<HD>(raw, mine, first, dst, w, lane);
 }
 
 // TMEM columns, not waited for; then the wait, which the values pass through
@@ -771,8 +786,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     Segment g;
     bool ok = true;
 
-    if (warp >= 8 && warp < 12) {  // ---- loaders
-        const int w = warp - 8;
+    if (Q8 && warp >= 8 && warp < 12) {  // ---- loaders of an e4m3 cache: key scales, value conversion
+        const int w = warp - 8, r = w * 32 + lane;  // the lane's row of every tile
         RingPos<S> pos;
         RingPos<KS> kpos;
         RingPos<RS> rpos;
@@ -780,66 +795,71 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         uint32_t tiles = 0;  // key tiles so far
         while (ok && next(g)) {
             const int nt = g.t1 - g.t0;
-            // what the lane knows of its rows in tiles t, t + 1, t + 2 (addresses and scales are
-            // fetched a tile ahead of their use)
-            RowInfo x0{-1, 0.f, 0.f};
-            if (Q8 || !by_tma(a, g, 0)) x0 = row_info<Q8>(a, g, g.t0, w * 32 + lane);
-            RowInfo x1 = x0, x2 = x0;
+            // the row's place and scales in tiles tt and tt + 1; the next tile's are fetched a tile ahead
+            RowInfo x1 = row_info<Q8>(a, g, g.t0, r);
+            float vs = 0.f;
+            bool has = false;
+#pragma unroll 1
+            for (int tt = -1; tt < nt; ++tt) {  // K0 (K1 V0) (K2 V1) ...
+                const float vs1 = x1.vs;
+                const bool has1 = x1.row >= 0;
+                if (tt + 1 < nt) {  // the rows' scales; the rows themselves where TMA cannot fetch them
+                    if (kreuse && !(ok = wait(&st.kempty[kpos.slot], kpos.phase ^ 1u))) break;
+                    key_scales[(tiles++ % kTcScales) * kTcTile + r] = has1 ? x1.ks : 1.f;
+                    if (a.box_rows > 0) {
+                        mbar_arrive(&st.kfull[kpos.slot]);
+                    } else {
+                        load_key_tile<HD>(a.cache.k, x1, keyring + kpos.slot * SH::kRawBytes, w, lane);
+                        cp_async_arrive(&st.kfull[kpos.slot]);
+                    }
+                    kpos.skip(1);
+                    kreuse |= kpos.slot == 0;
+                    x1 = row_info<Q8>(a, g, g.t0 + tt + 2, r);
+                }
+                if (tt >= 0) {
+                    if (!(ok = wait(&st.rawfull[rpos.slot], rpos.phase))) break;
+                    if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
+                    // (the MMA warp's proxy fence orders the tile's writes before the product's reads)
+                    if (convert_tile<HD>(rawring + rpos.slot * SH::kRawBytes, has, vs, g.s.P - (g.t0 + tt) * kTcTile,
+                                         ring + pos.slot * TB, w, lane))
+                        st.odd[(seg - 1) & 7] = 1;
+                    mbar_arrive(&st.rawempty[rpos.slot]);
+                    mbar_arrive(&st.full[pos.slot]);
+                    rpos.skip(1);
+                    pos.skip(1);
+                    reuse |= pos.slot == 0;
+                }
+                vs = vs1;
+                has = has1;
+            }
+        }
+        cp_async_wait_all();
+    } else if (warp >= 8 && warp < 12) {  // ---- loaders of a bfloat16 cache: what TMA does not fetch
+        const int w = warp - 8;
+        RingPos<S> pos;
+        bool reuse = false;  // the ring has been filled once
+        while (ok && next(g)) {
+            const int nt = g.t1 - g.t0;
 #pragma unroll 1
             for (int l = 0; l < 2 * nt; ++l) {  // K0 K1 V0 K2 V1 ...
                 const bool val = tile_is_value(l, nt);
                 const int tt = tile_number(l, nt);
-                if (!val) {
-                    x0 = x1;
-                    x1 = l == 0 ? x0 : x2;
-                    if (Q8 || !by_tma(a, g, tt + 1)) x2 = row_info<Q8>(a, g, g.t0 + tt + 1, w * 32 + lane);
-                }
-                // (a key tile tt is loaded with x1's rows; the value tile loaded after it is tt - 1,
-                // the last one tt)
-                const RowInfo& x = !val || tt == nt - 1 ? x1 : x0;
                 unsigned char* dst = ring + pos.slot * TB;
                 uint64_t* full = &st.full[pos.slot];
-                const int first = g.s.P - (g.t0 + tt) * kTcTile;  // first row of the tile that is a node's
-                if constexpr (Q8) {
-                    if (!val) {  // the rows' scales; the rows themselves where TMA cannot fetch them
-                        if (kreuse && !(ok = wait(&st.kempty[kpos.slot], kpos.phase ^ 1u))) break;
-                        key_scales[(tiles++ % kTcScales) * kTcTile + w * 32 + lane] = x.row >= 0 ? x.ks : 1.f;
-                        if (a.box_rows > 0) {
-                            mbar_arrive(&st.kfull[kpos.slot]);
-                        } else {
-                            load_key_tile<HD>(a.cache.k, x, keyring + kpos.slot * SH::kRawBytes, w, lane);
-                            cp_async_arrive(&st.kfull[kpos.slot]);
-                        }
-                        kpos.skip(1);
-                        kreuse |= kpos.slot == 0;
-                        continue;
-                    }
-                    if (!(ok = wait(&st.rawfull[rpos.slot], rpos.phase))) break;
-                }
                 // (every slot's release is waited for, also of tiles that come by TMA: a barrier's phase is
                 // one bit, and a role that skipped one could take an older release for the one it needs)
                 if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
-                if (!Q8 && by_tma(a, g, tt)) {
-                    pos.skip(1);
-                    reuse |= pos.slot == 0;
-                    continue;
-                }
-                if constexpr (Q8) {
-                    const bool odd = convert_tile<HD>(rawring + rpos.slot * SH::kRawBytes, x.row >= 0, x.vs, first, dst, w, lane);
-                    if (odd) st.odd[(seg - 1) & 7] = 1;
-                    fence_async_proxy();
-                    mbar_arrive(&st.rawempty[rpos.slot]);
-                    mbar_arrive(full);
-                    rpos.skip(1);
-                } else {
+                if (!by_tma(a, g, tt)) {
+                    const RowInfo x = row_info<Q8>(a, g, g.t0 + tt, w * 32 + lane);
                     load_tile<HD>(val ? a.cache.v : a.cache.k, x, dst, w, lane);
+                    const int first = g.s.P - (g.t0 + tt) * kTcTile;  // first row of the tile that is a node's
                     if (val && first < kTcTile) {
                         cp_async_wait_all();
                         if (scrub_tile<HD>(dst, first, w, lane)) st.odd[(seg - 1) & 7] = 1;
                         fence_async_proxy();
                         mbar_arrive(full);
                     } else {
-                        // (the copies' writes are ordered before the MMA's reads by the MMA thread's
+                        // (the copies' writes are ordered before the MMA's reads by the MMA warp's
                         // proxy fence: a fence here would wait for the copies)
                         cp_async_arrive(full);
                     }
@@ -1145,12 +1165,12 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             }
         };
         // e4m3: the warp's rows of segment number n's queries (as they have arrived) split for the product
+        // (the MMA warps' proxy fence orders these writes before their reads)
         auto split = [&](const Segment& s, uint32_t n) -> bool {
             if constexpr (Q8) {
                 if (!wait(&st.qfull, n)) return false;
                 if (s.weight == 2 || gs == 0) {
                     st.qs[n & 1][gs][wl * 32 + lane] = split_query_row<HD>(qbuf + gs * TB, wl * 32 + lane);
-                    fence_async_proxy();
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&st.qready);
