@@ -193,12 +193,15 @@ struct Place {
 // Walks a CTA's segments; used by a whole warp, every lane holding the same state.
 template <typename PL>
 struct SegmentWalk {
+    Cut cut;
     int u0, u1, pos;  // the CTA's units; first unit of the current item
     int b, h, m;
     SeqLen s;
 
+    __device__ __forceinline__ SegmentWalk() : cut(0, 1) {}
     __device__ __forceinline__ void init(PlanArgs& a, int cta, int ncta, bool* bad = nullptr) {
         const Place<PL> p = Place<PL>::find(a, cta, ncta, bad);
+        cut = p.cut;
         u0 = p.cut.begin(cta);
         u1 = p.cut.begin(cta + 1);
         b = p.found ? p.b : a.B;
@@ -206,6 +209,22 @@ struct SegmentWalk {
         m = p.m;
         pos = p.s0;
         s = p.s;
+    }
+    // What the join has to know of this CTA; after the last next(), with the last segment and whether
+    // some segment's slot was 0.
+    __device__ __forceinline__ SplitDesc desc(const PlanArgs& a, bool any, const Segment& g, bool continues) const {
+        SplitDesc d{};
+        d.has0 = continues;
+        d.last = -1;
+        if (any && !g.whole && g.slot == 1) {  // an item begins here and goes on
+            const int nt = PL::tiles(a, g.s, g.m), w = g.weight, p = pos - PL::units(a, w, nt);  // (pos: past the item)
+            d.b = g.b;
+            d.h = g.h;
+            d.m = g.m;
+            d.rows = g.rows;
+            d.last = cut.owner(PL::tile_unit(a, p, w, nt - 1));
+        }
+        return d;
     }
     // The next segment with at least one tile; false at the end.
     __device__ __forceinline__ bool next(const PlanArgs& a, Segment& g) {

@@ -16,6 +16,7 @@ struct fe_target {
     float2* rope = nullptr;
     float *part_o = nullptr, *part_ml = nullptr;
     int* status = nullptr;
+    SplitDesc* split = nullptr;
 };
 
 namespace {
@@ -109,6 +110,7 @@ void release(fe_target* t) {
     cudaFree(t->part_o);
     cudaFree(t->part_ml);
     cudaFree(t->status);
+    cudaFree(t->split);
     delete t;
 }
 
@@ -123,6 +125,7 @@ fe_status build(fe_target* t, cudaStream_t st) {
     FE_TRY(cudaMalloc((void**)&t->part_o, rows * c.head_dim * sizeof(float)));
     FE_TRY(cudaMalloc((void**)&t->part_ml, rows * 2 * sizeof(float)));
     FE_TRY(cudaMalloc((void**)&t->status, sizeof(int)));
+    FE_TRY(cudaMalloc((void**)&t->split, t->num_sms * sizeof(SplitDesc)));
     FE_TRY(cudaMemsetAsync(t->status, 0, sizeof(int), st));
     double amplitude = 1.0;
     const std::vector<double> f = rope_freqs(c, &amplitude);
@@ -319,6 +322,7 @@ fe_status fe_tree_attention(fe_target* t, const fe_tree_attention_args* a, void*
     r.mask = a->mask;
     r.scale = a->scale;
     r.cache = cache_view(t, a->cache, a->pages);
+    r.split = t->split;
     r.part_o = t->part_o;
     r.part_ml = t->part_ml;
     r.status = t->status;

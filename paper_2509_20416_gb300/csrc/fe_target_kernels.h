@@ -55,6 +55,12 @@ struct KeepArgs {
     int* status;
 };
 
+// What an attention CTA leaves for the join of split items: the item that it begins and that goes
+// on to CTA `last` (-1: none), and whether it holds a share of an item begun before it.
+struct SplitDesc {
+    int b, h, m, rows, last, has0, pad[2];
+};
+
 struct TreeAttnArgs {
     int B, T, H, Hkv, G;
     fe_rows q, out;
@@ -63,6 +69,7 @@ struct TreeAttnArgs {
     const uint8_t* mask;
     float scale;
     CacheView cache;
+    SplitDesc* split;         // [G], of every attention CTA
     float *part_o, *part_ml;  // per CTA two partial items: [2 G][rows][hd] sums, [2 G][rows][2] (max, sum)
     int* status;
     int q_vec, out_vec;  // rows of q / out on 16-byte boundaries

@@ -10,43 +10,49 @@ namespace {
 // ---- the join ------------------------------------------------------------------------------
 // Sums the partial results of items split between CTAs, sum_c 2^(m_c - m) (o_c, l_c) with m the
 // largest m_c, in CTA order, and writes their rows; also fills the rows of nodes past n_b with
-// zeros and -inf. Only G - 1 places can split an item, so block x looks at the one between CTAs x
-// and x + 1, and takes the item there if CTA x is the item's first; blocks y share its rows, a
-// warp per row. Bound by the latency of the schedule and of two dependent reads; launched so that
-// the schedule (which needs only the caller's lengths) is worked out before the attention ends.
+// zeros and -inf. At most one item begins in a CTA and goes on in the next: blocks x look at the
+// one that attention CTA x noted (SplitDesc), blocks y share its rows, a warp per row. Bound by
+// latency: its launch, which the attention's registers keep from overlapping, and three dependent
+// reads.
 constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinShares = 8;
 
-template <typename QT, int HD, typename PL, int ROWS>
-__global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a, int ncta) {
-    constexpr int E = HD / 32;  // columns of a lane
-    PlanArgs pa = plan_args(a);
-    const int lane = threadIdx.x & 31, wid = blockIdx.y * kJoinWarps + threadIdx.x / 32;
-    const Place<PL> w = Place<PL>::find(pa, blockIdx.x + 1, ncta);
-    griddep_wait();  // (on every path: this kernel's end stands for the attention's too)
-    // rows of nodes past n_b
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-        const int n = seq_len(pa, b).n;
-        if (n == a.T) continue;
-        for (int x = n * a.H + wid; x < a.T * a.H; x += kJoinShares * kJoinWarps) {
-            QT* dst = (QT*)a.out.p + b * a.out.batch + (int64_t)(x / a.H) * a.out.token + (int64_t)(x % a.H) * a.out.head;
+// Rows of sequence b's nodes from n on: zeros, -inf.
+template <typename QT, int HD>
+__device__ __forceinline__ void fill_rows(const TreeAttnArgs& a, int b, int n, int wid) {
+    constexpr int E = HD / 32;
+    const int lane = threadIdx.x & 31;
+    for (int x = n * a.H + wid; x < a.T * a.H; x += kJoinShares * kJoinWarps) {
+        QT* dst = (QT*)a.out.p + b * a.out.batch + (int64_t)(x / a.H) * a.out.token + (int64_t)(x % a.H) * a.out.head;
 #pragma unroll
-            for (int e = 0; e < E; ++e) store_one(dst + lane * E + e, 0.f);
-            if (a.lse && lane == 0) a.lse[(int64_t)b * a.T * a.H + x] = -INFINITY;
+        for (int e = 0; e < E; ++e) store_one(dst + lane * E + e, 0.f);
+        if (a.lse && lane == 0) a.lse[(int64_t)b * a.T * a.H + x] = -INFINITY;
+    }
+}
+
+template <typename QT, int HD, int ROWS>
+__global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a) {
+    constexpr int E = HD / 32;  // columns of a lane
+    const int lane = threadIdx.x & 31, wid = blockIdx.y * kJoinWarps + threadIdx.x / 32;
+    griddep_wait();
+    // rows of nodes past n_b
+    if (a.nodes) {
+        const PlanArgs pa = plan_args(a);
+        for (int b = blockIdx.x; b < a.B; b += gridDim.x) fill_rows<QT, HD>(a, b, seq_len(pa, b).n, wid);
+    } else {
+        for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+            const int P = a.prefix[b];  // (a sequence out of range has no nodes)
+            if (P < 0 || (int64_t)P + a.T > a.cache.max_seq) fill_rows<QT, HD>(a, b, 0, wid);
         }
     }
-    if (!w.found || pa.whole) return;
-    const int rows = w.s.n * a.G, nrow = min(ROWS, rows - w.m * ROWS);
-    const int wt = PL::weight(rows, w.m), nt = PL::tiles(pa, w.s, w.m);
-    if (w.s0 >= w.cut.begin(blockIdx.x + 1)) return;  // the item starts there: not split
-    if (w.cut.owner(PL::tile_unit(pa, w.s0, wt, 0)) != (int)blockIdx.x) return;  // an earlier block's item
-    const int c1 = w.cut.owner(PL::tile_unit(pa, w.s0, wt, nt - 1));
-    if (c1 == (int)blockIdx.x) return;
+    const SplitDesc w = a.split[blockIdx.x];
+    const int c0 = blockIdx.x, c1 = w.last;
+    if (c1 <= c0) return;
+    const int nrow = min(ROWS, w.rows - w.m * ROWS);
     for (int r = wid; r < nrow; r += kJoinShares * kJoinWarps) {
         // the partials' row of contributor c, or -1 if no tile starts in c's units
         auto part = [&](int c) -> int64_t {
-            const int t0 = PL::first_tile(pa, w.s0, wt, nt, w.cut.begin(c));
-            if (c > c1 || t0 >= PL::first_tile(pa, w.s0, wt, nt, w.cut.begin(c + 1))) return -1;
-            return ((int64_t)c * 2 + (t0 == 0 ? 1 : 0)) * kAttnItemRows + r;
+            if (c > c1 || (c > c0 && !a.split[c].has0)) return -1;
+            return ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * kAttnItemRows + r;
         };
         float mx = -INFINITY;
         for (int c = blockIdx.x + lane; c <= c1; c += 32) {
@@ -90,9 +96,9 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __gr
     }
 }
 
-template <typename QT, int HD, typename PL, int ROWS>
+template <typename QT, int HD, int ROWS>
 cudaError_t launch_join(const TreeAttnArgs& a, int ncta, cudaStream_t st) {
-    return launch_k(tree_attn_join_kernel<QT, HD, PL, ROWS>, dim3(ncta, kJoinShares), dim3(kJoinThreads), 0, st, true, a, ncta);
+    return launch_k(tree_attn_join_kernel<QT, HD, ROWS>, dim3(ncta, kJoinShares), dim3(kJoinThreads), 0, st, true, a);
 }
 
 template <int HD>
@@ -100,7 +106,7 @@ cudaError_t launch_simt(const TreeAttnArgs& a, int num_sms, cudaStream_t st) {
     const cudaError_t e = launch_k(tree_attn_simt_kernel<HD>, dim3(num_sms), dim3(kSimtThreads), sizeof(SimtSmem<HD>), st,
                                    false, a);
     if (e != cudaSuccess) return e;
-    return launch_join<float, HD, SimtPlan, kSimtRows>(a, num_sms, st);
+    return launch_join<float, HD, kSimtRows>(a, num_sms, st);
 }
 
 // cuTensorMapEncodeTiled, looked up once (the library does not link the driver)
@@ -174,7 +180,7 @@ cudaError_t launch_tc(const TreeAttnArgs& args, int num_sms, cudaStream_t st) {
     const cudaError_t e = launch_k(tree_attn_tc_kernel<HD, Q8, MT>, dim3(num_sms), dim3(TcShape<HD, Q8, MT>::kThreads),
                                    tc_smem<HD, Q8, MT>(), st, false, a, kmap, vmap, qmap);
     if (e != cudaSuccess) return e;
-    return launch_join<bf16_t, HD, TcPlan, kAttnItemRows>(a, num_sms, st);
+    return launch_join<bf16_t, HD, kAttnItemRows>(a, num_sms, st);
 }
 
 template <typename K>

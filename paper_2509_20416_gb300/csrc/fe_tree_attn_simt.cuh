@@ -38,7 +38,10 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __gr
     if (t < 2) sm.odd[t] = 0;
 
     Segment g;
+    bool any = false, continues = false;
     while (walk.next(pa, g)) {
+        any = true;
+        continues |= !g.whole && g.slot == 0;
         const int r0 = g.m * kSimtRows;
         __syncthreads();  // the previous segment's readers of sm.q are done
         for (int e = t; e < kSimtRows * HD; e += kSimtThreads) {
@@ -197,6 +200,7 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __gr
             }
         }
     }
+    if (t == 0) a.split[blockIdx.x] = walk.desc(pa, any, g, continues);
 }
 
 }  // namespace fe

@@ -982,9 +982,11 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         walk.init(pa, blockIdx.x, gridDim.x, &bad);
         if (bad && blockIdx.x == 0) atomicOr(a.status, ST_CAPACITY);
         uint32_t n = 0;
+        bool continues = false;
         for (; ok; ++n) {
-            g.weight = 0;
             const bool more = walk.next(pa, g);
+            continues |= more && !g.whole && g.slot == 0;
+            if (!more && lane == 0) a.split[blockIdx.x] = walk.desc(pa, n > 0, g, continues);
             const int k = n % kTcSegs;
             if (n >= kTcSegs && !(ok = wait(&st.segempty[k], n / kTcSegs - 1))) break;
             if (lane == 0) {
