@@ -11,10 +11,33 @@ namespace {
 // Sums the partial results of items split between CTAs, sum_c 2^(m_c - m) (o_c, l_c) with m the
 // largest m_c, in CTA order, and writes their rows; also fills the rows of nodes past n_b with
 // zeros and -inf. At most one item begins in a CTA and goes on in the next: blocks x look at the
-// one that attention CTA x noted (SplitDesc), blocks y share its rows, a warp per row. Bound by
-// latency: its launch, which the attention's registers keep from overlapping, and three dependent
-// reads.
-constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinShares = 8;
+// one that attention CTA x noted (SplitDesc), blocks y share its rows, four to a warp, so that the
+// four rows' reads are under way together. Bound by latency: its launch, which the attention's
+// registers keep from overlapping, and three dependent reads (a row a warp took 20 us where 150
+// items of 196 rows were split, four take 8).
+constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinShares = 16;
+
+__device__ __forceinline__ void store_four(bf16_t* p, float a, float b, float c, float d, bool aligned) {
+    const uint2 w = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
+    if (aligned) {
+        *reinterpret_cast<uint2*>(p) = w;
+    } else {
+        p[0].bits = (uint16_t)w.x;
+        p[1].bits = (uint16_t)(w.x >> 16);
+        p[2].bits = (uint16_t)w.y;
+        p[3].bits = (uint16_t)(w.y >> 16);
+    }
+}
+__device__ __forceinline__ void store_four(float* p, float a, float b, float c, float d, bool aligned) {
+    if (aligned) {
+        *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+    } else {
+        p[0] = a;
+        p[1] = b;
+        p[2] = c;
+        p[3] = d;
+    }
+}
 
 // Rows of sequence b's nodes from n on: zeros, -inf.
 template <typename QT, int HD>
@@ -48,49 +71,62 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __gr
     const int c0 = blockIdx.x, c1 = w.last;
     if (c1 <= c0) return;
     const int nrow = min(ROWS, w.rows - w.m * ROWS);
-    for (int r = wid; r < nrow; r += kJoinShares * kJoinWarps) {
+    constexpr int GL = 8, NV = HD / (4 * GL);  // lanes of a row, float4 of a lane (4 columns each, GL apart)
+    const int l = lane % GL;
+    const unsigned group = 0xFFu << (lane / GL * GL);
+    for (int r = wid * (32 / GL) + lane / GL; r < nrow; r += kJoinShares * kJoinWarps * (32 / GL)) {
         // the partials' row of contributor c, or -1 if no tile starts in c's units
         auto part = [&](int c) -> int64_t {
             if (c > c1 || (c > c0 && !a.split[c].has0)) return -1;
             return ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * kAttnItemRows + r;
         };
         float mx = -INFINITY;
-        for (int c = blockIdx.x + lane; c <= c1; c += 32) {
+        for (int c = c0 + l; c <= c1; c += GL) {
             const int64_t p = part(c);
             if (p >= 0) mx = fmaxf(mx, __ldcg(a.part_ml + 2 * p));
         }
-        mx = warp_max(mx);
-        const float ms = mx == -INFINITY ? 0.f : mx;
-        float o[E], sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.f;
-        for (int c0 = blockIdx.x; c0 <= c1; c0 += 32) {
-            const int64_t p = part(c0 + lane);
+        for (int o = GL / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(group, mx, o));
+        const float ms = mx == -INFINITY ? 0.f : mx;
+        float4 o[NV];
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < NV; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int b0 = c0; b0 <= c1; b0 += GL) {
+            const int64_t p = part(b0 + l);
             const float2 ml = p >= 0 ? __ldcg(reinterpret_cast<const float2*>(a.part_ml + 2 * p)) : make_float2(-INFINITY, 0.f);
             const float f = exp2f(ml.x - ms);
-            const int n = min(32, c1 - c0 + 1);
-#pragma unroll 4
+            const int n = min(GL, c1 - b0 + 1);
+#pragma unroll 2
             for (int k = 0; k < n; ++k) {
-                const int64_t pk = __shfl_sync(0xffffffffu, p, k);
-                const float fk = __shfl_sync(0xffffffffu, f, k), lk = __shfl_sync(0xffffffffu, ml.y, k);
+                const int from = lane / GL * GL + k;
+                const int64_t pk = __shfl_sync(group, p, from);
+                const float fk = __shfl_sync(group, f, from), lk = __shfl_sync(group, ml.y, from);
                 if (pk < 0) continue;
-                const float* src = a.part_o + pk * HD + lane * E;
+                const float4* src = reinterpret_cast<const float4*>(a.part_o + pk * HD) + l;
+                float4 v[NV];
+#pragma unroll
+                for (int e = 0; e < NV; ++e) v[e] = __ldcg(src + GL * e);
                 sum += lk * fk;
-                if constexpr (E == 4) {
-                    const float4 v = __ldcg(reinterpret_cast<const float4*>(src));
-                    o[0] += v.x * fk; o[1] += v.y * fk; o[2] += v.z * fk; o[3] += v.w * fk;
-                } else {
-                    const float2 v = __ldcg(reinterpret_cast<const float2*>(src));
-                    o[0] += v.x * fk; o[1] += v.y * fk;
+#pragma unroll
+                for (int e = 0; e < NV; ++e) {
+                    o[e].x += v[e].x * fk;
+                    o[e].y += v[e].y * fk;
+                    o[e].z += v[e].z * fk;
+                    o[e].w += v[e].w * fk;
                 }
             }
         }
         const int row = w.m * ROWS + r, node = row / a.G, head = w.h * a.G + row % a.G;
         const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        QT* dst = (QT*)a.out.p + w.b * a.out.batch + (int64_t)node * a.out.token + (int64_t)head * a.out.head + lane * E;
+        QT* dst = (QT*)a.out.p + w.b * a.out.batch + (int64_t)node * a.out.token + (int64_t)head * a.out.head;
 #pragma unroll
-        for (int e = 0; e < E; ++e) store_one(dst + e, sum == 0.f ? 0.f : o[e] * inv);
-        if (a.lse && lane == 0)
+        for (int e = 0; e < NV; ++e) {
+            const bool none = sum == 0.f;
+            store_four(dst + 4 * (l + GL * e), none ? 0.f : o[e].x * inv, none ? 0.f : o[e].y * inv, none ? 0.f : o[e].z * inv,
+                       none ? 0.f : o[e].w * inv, a.out_vec);
+        }
+        if (a.lse && l == 0)
             a.lse[((int64_t)w.b * a.T + node) * a.H + head] =
                 sum == 0.f ? -INFINITY : mx * 0.6931471805599453f + logf(sum);
     }

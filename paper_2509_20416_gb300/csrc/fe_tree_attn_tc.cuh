@@ -725,6 +725,16 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     TcState& st = *reinterpret_cast<TcState*>(qbuf + SH::kData);
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     griddep_launch_dependents();
+    // what takes long and needs nothing goes first: the schedule, and the tensor maps' descriptors
+    PlanArgs pa = plan_args(a);
+    bool bad = false;
+    SegmentWalk<TcPlan> walk;
+    if (warp == 14) walk.init(pa, blockIdx.x, gridDim.x, &bad);
+    if (warp == 15 && lane < 3) {
+        const CUtensorMap* map = lane == 0 ? &kmap : lane == 1 ? &vmap : &qmap;
+        if (lane == 2 ? a.q_tma : a.box_rows > 0 && (lane == 0 || !Q8))
+            asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+    }
     if (smem_u32(qbuf) & 1023u) {  // (dynamic memory alone starts on a 1024-byte boundary)
         if (t == 0) atomicOr(a.status, ST_DEVICE);
         return;
@@ -976,10 +986,6 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         __syncwarp();
         mbar_wait(&st.drain[gs], 0, a.status, 100000000LL);
     } else if (warp == 14) {  // ---- the plan
-        PlanArgs pa = plan_args(a);
-        bool bad = false;
-        SegmentWalk<TcPlan> walk;
-        walk.init(pa, blockIdx.x, gridDim.x, &bad);
         if (bad && blockIdx.x == 0) atomicOr(a.status, ST_CAPACITY);
         uint32_t n = 0;
         bool continues = false;
