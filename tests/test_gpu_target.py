@@ -434,6 +434,38 @@ def test_attention_score_ranges(fe, dtype, cache):
         check_attention(c, store, None, q, plen, torch.tensor([T]), None, out, lse)
 
 
+@pytest.mark.parametrize("T,P", [(5, 300), (70, 300)])
+def test_attention_over_e4m3_of_every_scale(fe, T, P):
+    """Value and key rows of very large and very small scale (factors beyond one bfloat16 multiply),
+    NaN numbers in the prefix, queries of every size and a NaN query."""
+    B, H, Hkv, hd = 1, 6, 2, 128
+    c = ref.config(cache_dtype="e4m3", n_heads=H, n_kv_heads=Hkv, head_dim=hd, max_batch=B, max_seq=P + T + 1)
+    t = fe.fe_target_init(c)
+    g = gen(T)
+    store = ref.random_cache(fe, t, c, g)
+    for h, shift in ((0, 12), (1, -60)):  # one head's rows far above 2^7, one's far below
+        store.v_scale[0, 0, h] *= 2.0 ** shift
+        store.k_scale[0, 0, h] *= 2.0 ** (-shift)
+    store.v_scale[0, 0, 1, 40:60] *= 2.0 ** 30
+    q = torch.randn(B, T, H, hd, generator=g)
+    q[:, :, :3] *= 2.0 ** 12
+    q[:, :, 3:] *= 2.0 ** -60
+    q[:, 1] *= 0.0
+    q = q.to(torch.bfloat16).cuda()
+    plen, n = torch.tensor([P], dtype=torch.int32), torch.tensor([T])
+    out, lse = fe.fe_tree_attention(t, store, 0, q, plen.cuda())
+    check_attention(c, store, None, q, plen, n, None, out, lse)
+    store.v[0, 0, 0, 7, 11] = math.nan
+    q[0, 2, 4, 9] = math.nan
+    out2, lse2 = fe.fe_tree_attention(t, store, 0, q, plen.cuda())
+    assert torch.isnan(out2[:, :, :3, 11]).all() and torch.isnan(out2[0, 2, 4]).all() and torch.isnan(lse2[0, 2, 4])
+    same = torch.ones_like(out2, dtype=torch.bool)
+    same[:, :, :3, 11] = False
+    same[0, 2, 4] = False
+    assert torch.equal(out2[same], out[same])
+    assert fe.fe_target_status(t) == fe.FE_OK
+
+
 def test_attention_strided_output_scale_and_stream(fe):
     c = ref.config(max_batch=2, max_seq=600, page_size=16, cache_dtype="e4m3")
     t = fe.fe_target_init(c)
