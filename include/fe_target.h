@@ -99,7 +99,8 @@ typedef struct {
  *                     [n_pages, Hkv, page_size, hd], as in fe_draft.h, of the cache type
  *   k_scale, v_scale  FE_E4M3 only: float32 [max_batch, Hkv, max_seq] or
  *                     [n_pages, Hkv, page_size]; a row stands for its e4m3 numbers times its
- *                     scale, a power of two from 2^-120 to 2^120 (as fe_cache_write stores them),
+ *                     scale, a power of two from 2^-120 to 2^120 (as fe_cache_write stores them;
+ *                     in slots that no node sees anything, as in the rows themselves),
  *                     so every value is a bfloat16 number */
 typedef struct {
     void *k, *v;

@@ -209,15 +209,19 @@ __device__ __noinline__ ulonglong2 seen_bits(const TreeAttnArgs& a, const Segmen
 
 // ---- loaders ------------------------------------------------------------------------------------
 // What a lane knows of its row (32 w + lane) of a tile: the cache row, or -1 for a slot past the
-// item's end (or with a bad page id); and the row's scales.
+// item's end (or with a bad page id); and the row's scales. A node's row may be hidden from all and
+// hold anything. A NaN or infinity among its scales would spread through a masked score or a zero
+// probability: outside of 2^-120 .. 2^120 a key's scale becomes 1 and the value row (bad) zeros.
 struct RowInfo {
     int64_t row;
     float ks, vs;
+    bool bad;
 };
+__device__ __forceinline__ bool valid_scale(float x) { return __float_as_uint(x) - (7u << 23) <= 240u << 23; }
 
 template <bool Q8>
 __device__ __forceinline__ RowInfo row_info(const TreeAttnArgs& a, const Segment& g, int tile, int r) {
-    RowInfo x{-1, 0.f, 0.f};
+    RowInfo x{-1, 0.f, 0.f, false};
     const int64_t slot = (int64_t)tile * kTcTile + r;
     int64_t row;
     if (tile < g.t1 && slot < g.end && cache_row(a.cache, g.b, slot, row, a.status)) {
@@ -225,6 +229,10 @@ __device__ __forceinline__ RowInfo row_info(const TreeAttnArgs& a, const Segment
         if (Q8) {
             x.ks = a.cache.ks[x.row];
             x.vs = a.cache.vs[x.row];
+            if (slot >= g.s.P) {
+                if (!valid_scale(x.ks)) x.ks = 1.f;
+                x.bad = !valid_scale(x.vs);
+            }
         }
     }
     return x;
@@ -812,7 +820,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
 #pragma unroll 1
             for (int tt = -1; tt < nt; ++tt) {  // K0 (K1 V0) (K2 V1) ...
                 const float vs1 = x1.vs;
-                const bool has1 = x1.row >= 0;
+                const bool has1 = x1.row >= 0, ok1 = has1 && !x1.bad;
                 if (tt + 1 < nt) {  // the rows' scales; the rows themselves where TMA cannot fetch them
                     if (kreuse && !(ok = wait(&st.kempty[kpos.slot], kpos.phase ^ 1u))) break;
                     key_scales[(tiles++ % kTcScales) * kTcTile + r] = has1 ? x1.ks : 1.f;
@@ -840,7 +848,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     reuse |= pos.slot == 0;
                 }
                 vs = vs1;
-                has = has1;
+                has = ok1;
             }
         }
         cp_async_wait_all();

@@ -407,6 +407,29 @@ def test_hidden_slots_do_not_matter(fe, dtype, cache, T, P):
     check_attention(c, store, None, q, plen, n, mask, out, lse)
 
 
+@pytest.mark.parametrize("scale", [math.nan, math.inf, -math.inf, 0.0, 3e38, -1.0, 1e-40])
+def test_hidden_rows_with_any_scale(fe, scale):
+    """A row that no node sees may hold any scale: branches whose rows were never written."""
+    B, T, H, Hkv, hd, P = 2, 40, 8, 2, 128, (129, 700)
+    c = ref.config(dtype="bf16", cache_dtype="e4m3", n_heads=H, n_kv_heads=Hkv, head_dim=hd, max_batch=B, max_seq=800)
+    t = fe.fe_target_init(c)
+    g = gen(T)
+    store = ref.random_cache(fe, t, c, g)
+    mask = tree_masks(g, B, T)
+    mask[:, 5, :] = 0
+    mask[:, :, 5] = 0
+    n = torch.full((B,), T, dtype=torch.int32)
+    q = rows(g, "bf16", B, T, H, hd)
+    plen = torch.tensor(P, dtype=torch.int32)
+    want = fe.fe_tree_attention(t, store, 0, q, plen.cuda(), mask=mask.cuda())
+    for b in range(B):
+        store.k_scale[0, b, :, P[b] + 5] = scale
+        store.v_scale[0, b, :, P[b] + 5] = scale
+    got = fe.fe_tree_attention(t, store, 0, q, plen.cuda(), mask=mask.cuda())
+    assert fe.fe_target_status(t) == fe.FE_OK
+    assert torch.isfinite(want[0]).all() and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "e4m3")])
 def test_attention_score_ranges(fe, dtype, cache):
     """Scores far apart (one slot takes all), all alike, very negative, and a growing maximum."""
