@@ -19,8 +19,8 @@ struct PlanArgs {
     int B, T, Hkv, G, max_seq;
     const int *prefix, *nodes;
     bool causal;
-    // Set by Place::find: short items, no more of them than CTAs, are not split (joining a split
-    // costs about as much as six tiles); every item then counts as one unit, and CTA c has item c.
+    // Set by Place::find: short items (of JOIN tiles at most, on average), no more of them than CTAs,
+    // are not split; every item then counts as one unit, and CTA c has item c.
     bool whole = false;
 };
 
@@ -45,12 +45,13 @@ __device__ __forceinline__ SeqLen seq_len(const PlanArgs& a, int b, bool* bad = 
 
 // ROWS rows an item, TN slots a tile; PAIR: an item of more than 128 rows costs two units a tile.
 // An item begins with OVER units that hold no tile: what starting and finishing it costs a CTA, in
-// units, so that a CTA with many short items does not end after one with few long ones.
+// units, so that a CTA with many short items does not end after one with few long ones. JOIN: about
+// how many tiles joining a split costs.
 // Units are counted in 32 bits (the launch refuses shapes that could pass 2^31): this runs once a
 // CTA before anything else can start, and short code is what it takes to be quick.
-template <int ROWS, int TN, bool PAIR, int OVER>
+template <int ROWS, int TN, bool PAIR, int OVER, int JOIN>
 struct Plan {
-    static constexpr int kOver = OVER;
+    static constexpr int kOver = OVER, kJoin = JOIN;
     __host__ __device__ __forceinline__ static int blocks(int rows) { return (rows + ROWS - 1) / ROWS; }
     __device__ __forceinline__ static int weight(int rows, int m) { return PAIR && rows - m * ROWS > 128 ? 2 : 1; }
     // slots that block m's rows may see: [0, end)
@@ -141,7 +142,7 @@ struct Place {
         }
         U *= a.Hkv;
         items *= a.Hkv;
-        a.whole = items <= ncta && U <= items * (PL::kOver + 6);
+        a.whole = items <= ncta && U <= items * (PL::kOver + PL::kJoin);
         if (a.whole) {
             U = items;
             hu = PL::blocks(sl.n * a.G);

@@ -125,7 +125,7 @@ fe_status build(fe_target* t, cudaStream_t st) {
     FE_TRY(cudaMalloc((void**)&t->part_o, rows * c.head_dim * sizeof(float)));
     FE_TRY(cudaMalloc((void**)&t->part_ml, rows * 2 * sizeof(float)));
     FE_TRY(cudaMalloc((void**)&t->status, sizeof(int)));
-    FE_TRY(cudaMalloc((void**)&t->split, t->num_sms * sizeof(SplitDesc)));
+    FE_TRY(cudaMalloc((void**)&t->split, (size_t)t->num_sms * kAttnCtasPerSm * sizeof(SplitDesc)));
     FE_TRY(cudaMemsetAsync(t->status, 0, sizeof(int), st));
     double amplitude = 1.0;
     const std::vector<double> f = rope_freqs(c, &amplitude);

@@ -72,4 +72,8 @@ template <> __device__ __forceinline__ uint4 pack16<bf16_t>(const float* f) {
 __device__ __forceinline__ void store_one(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_one(bf16_t* p, float v) { p->bits = (uint16_t)pack_bf16(v, 0.f); }
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+
 }  // namespace fe

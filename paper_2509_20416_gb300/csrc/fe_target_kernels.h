@@ -70,7 +70,8 @@ struct TreeAttnArgs {
     float scale;
     CacheView cache;
     SplitDesc* split;         // [G], of every attention CTA
-    float *part_o, *part_ml;  // per CTA two partial items: [2 G][rows][hd] sums, [2 G][rows][2] (max, sum)
+    int part_rows;            // rows of a partial item in the workspace: per CTA two items,
+    float *part_o, *part_ml;  // [2 G][part_rows][hd] sums, [2 G][part_rows][2] (max, sum)
     int* status;
     int q_vec, out_vec;  // rows of q / out on 16-byte boundaries
     int box_rows;        // cache rows of a TMA box (0: no tensor maps)
@@ -79,6 +80,7 @@ struct TreeAttnArgs {
 
 // rows of an attention item whose partial results the workspace holds, per CTA and slot
 constexpr int kAttnItemRows = 256;
+constexpr int kAttnCtasPerSm = 2;  // at most (with items of at most 128 rows each then)
 
 cudaError_t launch_rope_table(float2* table, int max_seq, int pairs, const double* inv_freq, double amplitude,
                               cudaStream_t st);

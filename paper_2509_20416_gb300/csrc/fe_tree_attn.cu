@@ -15,7 +15,7 @@ namespace {
 // four rows' reads are under way together. Bound by latency: its launch, which the attention's
 // registers keep from overlapping, and three dependent reads (a row a warp took 20 us where 150
 // items of 196 rows were split, four take 8).
-constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinShares = 16;
+constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinRows = 4 * kJoinWarps;
 
 __device__ __forceinline__ void store_four(bf16_t* p, float a, float b, float c, float d, bool aligned) {
     const uint2 w = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
@@ -44,7 +44,7 @@ template <typename QT, int HD>
 __device__ __forceinline__ void fill_rows(const TreeAttnArgs& a, int b, int n, int wid) {
     constexpr int E = HD / 32;
     const int lane = threadIdx.x & 31;
-    for (int x = n * a.H + wid; x < a.T * a.H; x += kJoinShares * kJoinWarps) {
+    for (int x = n * a.H + wid; x < a.T * a.H; x += gridDim.y * kJoinWarps) {
         QT* dst = (QT*)a.out.p + b * a.out.batch + (int64_t)(x / a.H) * a.out.token + (int64_t)(x % a.H) * a.out.head;
 #pragma unroll
         for (int e = 0; e < E; ++e) store_one(dst + lane * E + e, 0.f);
@@ -54,7 +54,6 @@ __device__ __forceinline__ void fill_rows(const TreeAttnArgs& a, int b, int n, i
 
 template <typename QT, int HD, int ROWS>
 __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __grid_constant__ TreeAttnArgs a) {
-    constexpr int E = HD / 32;  // columns of a lane
     const int lane = threadIdx.x & 31, wid = blockIdx.y * kJoinWarps + threadIdx.x / 32;
     griddep_wait();
     // rows of nodes past n_b
@@ -71,14 +70,14 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __gr
     const int c0 = blockIdx.x, c1 = w.last;
     if (c1 <= c0) return;
     const int nrow = min(ROWS, w.rows - w.m * ROWS);
-    constexpr int GL = 8, NV = HD / (4 * GL);  // lanes of a row, float4 of a lane (4 columns each, GL apart)
+    constexpr int GL = 32 * kJoinWarps / kJoinRows, NV = HD / (4 * GL);  // lanes of a row, float4 of a lane (4 columns each, GL apart)
     const int l = lane % GL;
     const unsigned group = 0xFFu << (lane / GL * GL);
-    for (int r = wid * (32 / GL) + lane / GL; r < nrow; r += kJoinShares * kJoinWarps * (32 / GL)) {
+    for (int r = wid * (32 / GL) + lane / GL; r < nrow; r += gridDim.y * kJoinRows) {
         // the partials' row of contributor c, or -1 if no tile starts in c's units
         auto part = [&](int c) -> int64_t {
             if (c > c1 || (c > c0 && !a.split[c].has0)) return -1;
-            return ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * kAttnItemRows + r;
+            return ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * a.part_rows + r;
         };
         float mx = -INFINITY;
         for (int c = c0 + l; c <= c1; c += GL) {
@@ -134,15 +133,20 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __gr
 
 template <typename QT, int HD, int ROWS>
 cudaError_t launch_join(const TreeAttnArgs& a, int ncta, cudaStream_t st) {
-    return launch_k(tree_attn_join_kernel<QT, HD, ROWS>, dim3(ncta, kJoinShares), dim3(kJoinThreads), 0, st, true, a);
+    const int rows = (int)min((int64_t)a.T * a.G, (int64_t)ROWS);  // of an item
+    return launch_k(tree_attn_join_kernel<QT, HD, ROWS>, dim3(ncta, (rows + kJoinRows - 1) / kJoinRows), dim3(kJoinThreads), 0, st, true, a);
 }
 
-template <int HD>
-cudaError_t launch_simt(const TreeAttnArgs& a, int num_sms, cudaStream_t st) {
-    const cudaError_t e = launch_k(tree_attn_simt_kernel<HD>, dim3(num_sms), dim3(kSimtThreads), sizeof(SimtSmem<HD>), st,
-                                   false, a);
+template <int HD, int NI>
+cudaError_t launch_simt(const TreeAttnArgs& args, int num_sms, cudaStream_t st) {
+    using SM = SimtSmem<HD, NI>;
+    static_assert(SM::kCtas * 64 <= kAttnItemRows && SM::kCtas <= kAttnCtasPerSm, "the workspace's rows and notes");
+    TreeAttnArgs a = args;
+    a.part_rows = 64;
+    const int grid = num_sms * SM::kCtas;
+    const cudaError_t e = launch_k(tree_attn_simt_kernel<HD, NI>, dim3(grid), dim3(kSimtThreads), sizeof(SM), st, false, a);
     if (e != cudaSuccess) return e;
-    return launch_join<float, HD, kSimtRows>(a, num_sms, st);
+    return launch_join<float, HD, 16 * NI>(a, grid, st);
 }
 
 // cuTensorMapEncodeTiled, looked up once (the library does not link the driver)
@@ -204,6 +208,7 @@ bool make_q_map(CUtensorMap* map, const TreeAttnArgs& a, int hd) {
 template <int HD, bool Q8, int MT>
 cudaError_t launch_tc(const TreeAttnArgs& args, int num_sms, cudaStream_t st) {
     TreeAttnArgs a = args;
+    a.part_rows = kAttnItemRows;
     CUtensorMap kmap{}, vmap{}, qmap{};
     a.q_tma = make_q_map(&qmap, a, HD);
     const CacheView& c = a.cache;
@@ -227,7 +232,9 @@ cudaError_t allow_smem(K kern, size_t bytes) {
 template <int HD>
 cudaError_t prepare() {
     cudaError_t e;
-    if ((e = allow_smem(tree_attn_simt_kernel<HD>, sizeof(SimtSmem<HD>))) != cudaSuccess) return e;
+    if ((e = allow_smem(tree_attn_simt_kernel<HD, 1>, sizeof(SimtSmem<HD, 1>))) != cudaSuccess) return e;
+    if ((e = allow_smem(tree_attn_simt_kernel<HD, 2>, sizeof(SimtSmem<HD, 2>))) != cudaSuccess) return e;
+    if ((e = allow_smem(tree_attn_simt_kernel<HD, 4>, sizeof(SimtSmem<HD, 4>))) != cudaSuccess) return e;
     if ((e = allow_smem(tree_attn_tc_kernel<HD, false, 1>, tc_smem<HD, false, 1>())) != cudaSuccess) return e;
     if ((e = allow_smem(tree_attn_tc_kernel<HD, false, 2>, tc_smem<HD, false, 2>())) != cudaSuccess) return e;
     if ((e = allow_smem(tree_attn_tc_kernel<HD, true, 1>, tc_smem<HD, true, 1>())) != cudaSuccess) return e;
@@ -236,8 +243,12 @@ cudaError_t prepare() {
 
 template <int HD>
 cudaError_t launch_hd(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int num_sms, cudaStream_t st) {
-    if (dtype == FE_F32) return launch_simt<HD>(a, num_sms, st);
-    const bool one = (int64_t)a.T * a.G <= 128;  // every item fits one 128-row block: more tiles in flight
+    const int64_t rows = (int64_t)a.T * a.G;
+    if (dtype == FE_F32)
+        return rows <= 16   ? launch_simt<HD, 1>(a, num_sms, st)
+               : rows <= 32 ? launch_simt<HD, 2>(a, num_sms, st)
+                            : launch_simt<HD, 4>(a, num_sms, st);
+    const bool one = rows <= 128;  // every item fits one 128-row block: more tiles in flight
     if (cache_dtype == FE_E4M3)
         return one ? launch_tc<HD, true, 1>(a, num_sms, st) : launch_tc<HD, true, 2>(a, num_sms, st);
     return one ? launch_tc<HD, false, 1>(a, num_sms, st) : launch_tc<HD, false, 2>(a, num_sms, st);
@@ -252,7 +263,8 @@ cudaError_t tree_attn_prepare() {
 
 bool tree_attn_fits(const TreeAttnArgs& a, fe_dtype dtype) {
     const int64_t rows = (int64_t)a.T * a.G;
-    return dtype == FE_F32 ? SimtPlan::fits(a.B, a.Hkv, rows, a.cache.max_seq)
+    // (the float32 variants of fewer rows hold all of an item's)
+    return dtype == FE_F32 ? SimtPlan<4>::fits(a.B, a.Hkv, rows, a.cache.max_seq)
                            : TcPlan::fits(a.B, a.Hkv, rows, a.cache.max_seq);
 }
 

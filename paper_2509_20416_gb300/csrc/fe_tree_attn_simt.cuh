@@ -1,50 +1,71 @@
 // Attention over the cache on the CUDA cores, in float32 throughout: float32 targets have no
 // tensor-core path that keeps their precision (bf16 and tf32 operands drop 13 to 16 bits).
 //
-// A CTA of 256 threads holds 64 query rows and walks tiles of 64 slots: thread (ty, tx) of a
-// 16 x 16 grid owns rows ty + 16 i and, of each tile's scores, slots tx + 16 j, then of the
-// outputs four consecutive columns tx 4 + 64 j. Scores, the running maximum and sum, and the
-// outputs stay in registers; keys, values and the tile's probabilities pass through shared
-// memory, padded so that the 16 rows a warp reads at once fall into different banks.
+// A CTA of 256 threads holds 16 NI query rows (NI = 1, 2 or 4, the fewest that hold an item's) and
+// walks tiles of 64 slots: thread (ty, tx) of a 16 x 16 grid owns rows ty + 16 i and, of each tile's
+// scores, slots tx + 16 j, then of the outputs four consecutive columns tx 4 + 64 j. Scores, the
+// running maximum and sum, and the outputs stay in registers; keys, values and the tile's
+// probabilities pass through shared memory, padded so that the 16 rows a warp reads at once fall
+// into different banks. Meanwhile the next tile's rows arrive (cp.async) in a second buffer, or,
+// where two CTAs fit an SM only with one buffer, the other CTA works. With 64 rows bound by the
+// float32 units (8192 clocks a tile of 128-wide heads), with 16 by shared memory (4096) and latency.
 #pragma once
 
 #include "fe_attn_plan.cuh"
 
 namespace fe {
 
-constexpr int kSimtRows = 64, kSimtTile = 64, kSimtThreads = 256;
-using SimtPlan = Plan<kSimtRows, kSimtTile, false, 1>;
-
-template <int HD>
+constexpr int kSimtTile = 64, kSimtThreads = 256;
+template <int NI>
+using SimtPlan = Plan<16 * NI, kSimtTile, false, 1, 2>;
+template <int HD, int NI>
 struct SimtSmem {
     static constexpr int kPad = HD + 4;
-    float q[kSimtRows][kPad], k[kSimtTile][kPad], v[kSimtTile][HD], p[kSimtRows][kSimtTile + 4];
-    int odd[2];  // the tile holds a non-finite value in a node's row (one flag per tile parity)
+    static constexpr int kBufs = HD == 128 && NI <= 2 ? 1 : 2, kCtas = HD == 128 && NI == 4 ? 1 : 2;  // CTAs an SM
+    float q[16 * NI][kPad], k[kBufs][kSimtTile][kPad], v[kBufs][kSimtTile][HD], p[16 * NI][kSimtTile + 4];
+    int odd[2];  // by the tile's parity in the walk: it holds a non-finite value in a node's row
 };
 
-template <int HD>
-__global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __grid_constant__ TreeAttnArgs a) {
+template <int HD, int NI>
+__global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_attn_simt_kernel(const __grid_constant__ TreeAttnArgs a) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    SimtSmem<HD>& sm = *reinterpret_cast<SimtSmem<HD>*>(smem_raw);
+    SimtSmem<HD, NI>& sm = *reinterpret_cast<SimtSmem<HD, NI>*>(smem_raw);
     const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
     constexpr int NC = HD / 64;  // groups of four output columns per thread
+    constexpr bool kTwo = SimtSmem<HD, NI>::kBufs == 2;
     PlanArgs pa = plan_args(a);
     griddep_launch_dependents();
     bool bad = false;
-    SegmentWalk<SimtPlan> walk;
+    SegmentWalk<SimtPlan<NI>> walk;
     walk.init(pa, blockIdx.x, gridDim.x, &bad);
     if (bad && blockIdx.x == 0) atomicOr(a.status, ST_CAPACITY);
     const float scale2 = a.scale * kLog2e;
     if (t < 2) sm.odd[t] = 0;
+    __syncthreads();
 
     Segment g;
     bool any = false, continues = false;
+    int buf = 0, par = 0;
     while (walk.next(pa, g)) {
         any = true;
         continues |= !g.whole && g.slot == 0;
-        const int r0 = g.m * kSimtRows;
-        __syncthreads();  // the previous segment's readers of sm.q are done
-        for (int e = t; e < kSimtRows * HD; e += kSimtThreads) {
+        const int r0 = g.m * 16 * NI;
+        // a thread's 16-byte chunks of a tile's keys and values, into buffer `to`
+        auto load = [&](int tile, int to) {
+#pragma unroll 1
+            for (int e = t; e < kSimtTile * (HD / 4); e += kSimtThreads) {
+                const int r = e / (HD / 4), c = e % (HD / 4) * 4;
+                const int64_t slot = (int64_t)tile * kSimtTile + r;
+                int64_t row = 0;
+                const bool ok = slot < g.end && cache_row(a.cache, g.b, slot, row, a.status);
+                if (ok) row += g.h * head_step(a.cache);
+                cp_async16(smem_u32(&sm.k[to][r][c]), (const float*)a.cache.k + row * HD + c, ok);
+                cp_async16(smem_u32(&sm.v[to][r][c]), (const float*)a.cache.v + row * HD + c, ok);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        if (kTwo) load(g.t0, buf);  // (the last reads of sm were before the barrier that ended the last tile)
+        for (int e = t; e < 16 * NI * HD; e += kSimtThreads) {
             const int r = e / HD, c = e % HD, row = r0 + r;
             float x = 0.f;
             if (row < g.rows) {
@@ -53,9 +74,9 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __gr
             }
             sm.q[r][c] = x * scale2;
         }
-        float mx[4], sum[4], acc[4][NC][4];
+        float mx[NI], sum[NI], acc[NI][NC][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < NI; ++i) {
             mx[i] = -INFINITY;
             sum[i] = 0.f;
 #pragma unroll
@@ -63,40 +84,38 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __gr
 #pragma unroll
                 for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
         }
-        for (int tile = g.t0; tile < g.t1; ++tile) {
-            const int par = tile & 1;
-            __syncthreads();  // the previous tile's readers of k, v, p are done
-            if (t == 0) sm.odd[par ^ 1] = 0;
-            for (int e = t; e < kSimtTile * (HD / 4); e += kSimtThreads) {
-                const int r = e / (HD / 4), c = e % (HD / 4) * 4;
-                const int64_t slot = (int64_t)tile * kSimtTile + r;
-                float4 kk = make_float4(0.f, 0.f, 0.f, 0.f), vv = kk;
-                int64_t row;
-                if (slot < g.end && cache_row(a.cache, g.b, slot, row, a.status)) {
-                    row += g.h * head_step(a.cache);
-                    kk = *reinterpret_cast<const float4*>((const float*)a.cache.k + row * HD + c);
-                    vv = *reinterpret_cast<const float4*>((const float*)a.cache.v + row * HD + c);
-                    if (slot >= g.s.P && !(finite_f32(vv.x) && finite_f32(vv.y) && finite_f32(vv.z) && finite_f32(vv.w)))
+        for (int tile = g.t0; tile < g.t1; ++tile, buf ^= kTwo, par ^= 1) {
+            if (kTwo && tile + 1 < g.t1) {
+                load(tile + 1, buf ^ 1);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            } else {
+                if (!kTwo) load(tile, buf);
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            }
+            if ((tile + 1) * kSimtTile > g.s.P) {  // the thread's own chunks of nodes' value rows
+#pragma unroll 1
+                for (int e = t; e < kSimtTile * (HD / 4); e += kSimtThreads) {
+                    const int r = e / (HD / 4), c = e % (HD / 4) * 4;
+                    const float4 x = *reinterpret_cast<const float4*>(&sm.v[buf][r][c]);
+                    if (tile * kSimtTile + r >= g.s.P && !(finite_f32(x.x) && finite_f32(x.y) && finite_f32(x.z) && finite_f32(x.w)))
                         sm.odd[par] = 1;
                 }
-                *reinterpret_cast<float4*>(&sm.k[r][c]) = kk;
-                *reinterpret_cast<float4*>(&sm.v[r][c]) = vv;
             }
             __syncthreads();
-            float s[4][4];
+            float s[NI][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < NI; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 4
             for (int c = 0; c < HD; c += 4) {
-                float4 q4[4], k4[4];
+                float4 q4[NI], k4[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) q4[i] = *reinterpret_cast<const float4*>(&sm.q[ty + 16 * i][c]);
+                for (int i = 0; i < NI; ++i) q4[i] = *reinterpret_cast<const float4*>(&sm.q[ty + 16 * i][c]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][c]);
+                for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(&sm.k[buf][tx + 16 * j][c]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < NI; ++i)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         s[i][j] = fmaf(q4[i].x, k4[j].x, s[i][j]);
@@ -107,7 +126,7 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __gr
             }
             const bool odd = sm.odd[par] != 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < NI; ++i) {
                 const int node = (r0 + ty + 16 * i) / a.G;
                 bool see[4];
                 float m = -INFINITY;
@@ -141,38 +160,46 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __gr
             }
             __syncwarp();  // a row's probabilities come from its own half warp
             if (!odd) {
-#pragma unroll 4
-                for (int c = 0; c < kSimtTile; ++c) {
-                    float4 v4[NC];
+#pragma unroll 2
+                for (int c = 0; c < kSimtTile; c += 4) {
+                    float4 p4[NI];
 #pragma unroll
-                    for (int j = 0; j < NC; ++j) v4[j] = *reinterpret_cast<const float4*>(&sm.v[c][tx * 4 + 64 * j]);
+                    for (int i = 0; i < NI; ++i) p4[i] = *reinterpret_cast<const float4*>(&sm.p[ty + 16 * i][c]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p = sm.p[ty + 16 * i][c];
+                    for (int u = 0; u < 4; ++u) {
+                        float4 v4[NC];
 #pragma unroll
-                        for (int j = 0; j < NC; ++j) {
-                            acc[i][j][0] = fmaf(p, v4[j].x, acc[i][j][0]);
-                            acc[i][j][1] = fmaf(p, v4[j].y, acc[i][j][1]);
-                            acc[i][j][2] = fmaf(p, v4[j].z, acc[i][j][2]);
-                            acc[i][j][3] = fmaf(p, v4[j].w, acc[i][j][3]);
+                        for (int j = 0; j < NC; ++j) v4[j] = *reinterpret_cast<const float4*>(&sm.v[buf][c + u][tx * 4 + 64 * j]);
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) {
+                            const float p = u == 0 ? p4[i].x : u == 1 ? p4[i].y : u == 2 ? p4[i].z : p4[i].w;
+#pragma unroll
+                            for (int j = 0; j < NC; ++j) {
+                                acc[i][j][0] = fmaf(p, v4[j].x, acc[i][j][0]);
+                                acc[i][j][1] = fmaf(p, v4[j].y, acc[i][j][1]);
+                                acc[i][j][2] = fmaf(p, v4[j].z, acc[i][j][2]);
+                                acc[i][j][3] = fmaf(p, v4[j].w, acc[i][j][3]);
+                            }
                         }
                     }
                 }
             } else {
                 for (int c = 0; c < kSimtTile; ++c)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < NI; ++i) {
                         const float p = sm.p[ty + 16 * i][c];
                         if (p == -1.f) continue;
 #pragma unroll
                         for (int j = 0; j < NC; ++j)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) acc[i][j][k] = fmaf(p, sm.v[c][tx * 4 + 64 * j + k], acc[i][j][k]);
+                            for (int k = 0; k < 4; ++k) acc[i][j][k] = fmaf(p, sm.v[buf][c][tx * 4 + 64 * j + k], acc[i][j][k]);
                     }
             }
+            __syncthreads();  // this buffer's (and p's) readers are done
+            if (t == 0) sm.odd[par] = 0;  // (set again two tiles on, a barrier later)
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < NI; ++i) {
             const int r = ty + 16 * i, row = r0 + r;
             if (row >= g.rows) continue;
             if (g.whole) {
@@ -188,7 +215,7 @@ __global__ void __launch_bounds__(kSimtThreads) tree_attn_simt_kernel(const __gr
                     a.lse[((int64_t)g.b * a.T + node) * a.H + head] =
                         sum[i] == 0.f ? -INFINITY : mx[i] * 0.6931471805599453f + logf(sum[i]);
             } else {
-                const int64_t pr = ((int64_t)blockIdx.x * 2 + g.slot) * kAttnItemRows + r;
+                const int64_t pr = ((int64_t)blockIdx.x * 2 + g.slot) * a.part_rows + r;
 #pragma unroll
                 for (int j = 0; j < NC; ++j)
                     *reinterpret_cast<float4*>(a.part_o + pr * HD + tx * 4 + 64 * j) =

@@ -46,7 +46,7 @@ constexpr int kTcTile = 128;
 // Key tiles whose scales are at hand. A softmax still reads tile t's when the loaders may be at tile
 // t + 1 + kKeySlots (the other stream's products may be one tile further).
 constexpr int kTcScales = 8;
-using TcPlan = Plan<kAttnItemRows, kTcTile, true, 4>;
+using TcPlan = Plan<kAttnItemRows, kTcTile, true, 4, 6>;
 
 // MT: 128-row query blocks a CTA must hold (1 when no item has more than 128 rows)
 template <int HD, bool Q8, int MT>
@@ -87,9 +87,6 @@ constexpr int tc_smem() {
     return bytes;
 }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // one arrival on `bar` once all cp.async of this thread so far are complete
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
