@@ -70,7 +70,7 @@ struct TcShape {
 constexpr int kTcSegs = 4;  // segments planned ahead
 
 struct TcState {
-    uint64_t full[6], empty[6], kfull[4], kempty[4], rawfull[4], rawempty[4], segfull[kTcSegs], segempty[kTcSegs], qfull, qempty, qready, sfull[2],
+    uint64_t full[6], empty[6], landed[6], kfull[4], kempty[4], rawfull[4], rawempty[4], segfull[kTcSegs], segempty[kTcSegs], qfull, qempty, qready, sfull[2],
         pfull[2], odone, ofree, mlfull, mlfree, drain[2], turn[2];
     Segment seg[kTcSegs];  // weight 0: no more
     uint32_t tmem;
@@ -306,21 +306,22 @@ __device__ __forceinline__ bool scrub_tile(unsigned char* tile, int first, int w
     const int c = lane % CH;
     bool odd = false;
 #pragma unroll 1
-    for (int i = 0; i < 32 / RP; ++i) {
+    for (int i = max(first - w * 32, 0) / RP; i < 32 / RP; ++i) {
         const int r = w * 32 + i * RP + lane / CH;
-        if (r < first) continue;
-        uint32_t* d = reinterpret_cast<uint32_t*>(tile + (c >> 3) * 16384 + sw128_offset(r, c & 7));
+        uint4* d = reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + sw128_offset(r, c & 7));
+        const uint4 x = *d;
+        uint32_t u[4] = {x.x, x.y, x.z, x.w};
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= (u[e] & 0x7F80u) == 0x7F80u || (u[e] & 0x7F800000u) == 0x7F800000u;
+        if (!any || r < first) continue;
+        odd = true;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint32_t u = d[e];
-            uint32_t keep = 0xffffffffu;
-            if ((u & 0x7F80u) == 0x7F80u) keep &= 0xffff0000u;
-            if ((u & 0x7F800000u) == 0x7F800000u) keep &= 0x0000ffffu;
-            if (keep != 0xffffffffu) {
-                d[e] = u & keep;
-                odd = true;
-            }
+            if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xffff0000u;
+            if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0x0000ffffu;
         }
+        *d = make_uint4(u[0], u[1], u[2], u[3]);
     }
     return odd;
 }
@@ -689,11 +690,6 @@ __device__ __forceinline__ float split_query_row(unsigned char* block, int row) 
     return __uint_as_float((uint32_t)(127 + c2) << 23);
 }
 
-// Whether tile t of the segment (from its first) comes by TMA: a whole tile of prefix slots.
-__device__ __forceinline__ bool by_tma(const TreeAttnArgs& a, const Segment& g, int t) {
-    return a.box_rows > 0 && (g.t0 + t + 1) * kTcTile <= g.s.P;
-}
-
 // A position in the ring of tiles: slot and phase, moved on by small steps without division.
 template <int S>
 struct RingPos {
@@ -748,6 +744,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     if (t == 0) {
         for (int i = 0; i < S; ++i) {
             mbar_init(&st.full[i], 128);
+            mbar_init(&st.landed[i], 1);
             mbar_init(&st.empty[i], MT);  // (a tile that one stream alone used is released twice by it)
         }
         for (int i = 0; i < KS; ++i) {
@@ -849,10 +846,12 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             }
         }
         cp_async_wait_all();
-    } else if (warp >= 8 && warp < 12) {  // ---- loaders of a bfloat16 cache: what TMA does not fetch
+    } else if (warp >= 8 && warp < 12) {  // ---- loaders of a bfloat16 cache
         const int w = warp - 8;
         RingPos<S> pos;
-        bool reuse = false;  // the ring has been filled once
+        bool reuse = false;       // the ring has been filled once
+        uint32_t landed = 0;      // by slot: the phase of landed[] that comes next
+        const bool tma = a.box_rows > 0;
         while (ok && next(g)) {
             const int nt = g.t1 - g.t0;
 #pragma unroll 1
@@ -861,13 +860,23 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 const int tt = tile_number(l, nt);
                 unsigned char* dst = ring + pos.slot * TB;
                 uint64_t* full = &st.full[pos.slot];
-                // (every slot's release is waited for, also of tiles that come by TMA: a barrier's phase is
-                // one bit, and a role that skipped one could take an older release for the one it needs)
-                if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
-                if (!by_tma(a, g, tt)) {
+                const int first = g.s.P - (g.t0 + tt) * kTcTile;  // first row of the tile that is a node's
+                if (tma) {  // what TMA brings is looked through where it may hold what nobody sees
+                    if (val && first < kTcTile) {
+                        if (!(ok = wait(&st.landed[pos.slot], landed >> pos.slot))) break;
+                        landed ^= 1u << pos.slot;
+                        if (scrub_tile<HD>(dst, first, w, lane)) {
+                            st.odd[(seg - 1) & 7] = 1;
+                            fence_async_proxy();
+                        }
+                        mbar_arrive(full);
+                    }
+                } else {
+                    // (every slot's release is waited for: a barrier's phase is one bit, and a role that
+                    // skipped one could take an older release for the one it needs)
+                    if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
                     const RowInfo x = row_info<Q8>(a, g, g.t0 + tt, w * 32 + lane);
                     load_tile<HD>(val ? a.cache.v : a.cache.k, x, dst, w, lane);
-                    const int first = g.s.P - (g.t0 + tt) * kTcTile;  // first row of the tile that is a node's
                     if (val && first < kTcTile) {
                         cp_async_wait_all();
                         if (scrub_tile<HD>(dst, first, w, lane)) st.odd[(seg - 1) & 7] = 1;
@@ -1106,10 +1115,11 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         if (!ok && a.box_rows > 0)
             for (uint32_t j = ktiles > (uint32_t)KS ? ktiles - KS : 0; j < ktiles; ++j)
                 mbar_wait(&st.kfull[j % KS], (j / KS) & 1u, a.status, 100000000LL);
-    } else if (!Q8 && warp == 15) {  // ---- whole tiles by TMA
+    } else if (!Q8 && warp == 15) {  // ---- a bfloat16 cache's tiles by TMA
         RingPos<S> pos;
         bool reuse = false;
-        uint32_t sent = 0;  // by slot: used here, and (from bit 8) the phase of its last use
+        uint32_t sent = 0;  // by slot: used; from bit 8 its last use's phase; from bit 16: on landed[]
+        uint32_t landed = 0;  // by slot: the phase of landed[] that comes next
         while (ok && a.box_rows > 0 && next(g)) {
             const int nt = g.t1 - g.t0;
             // a lane's box of every tile: rows box * br .. of the tile, columns half * 64 ..
@@ -1117,8 +1127,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             // where tile t's box lies: its page's (or sequence's) place in the map; fetched a tile ahead
             auto place = [&](int t) -> int {
                 if (!a.cache.page_size) return g.b * a.Hkv + g.h;
-                if (!by_tma(a, g, t) || g.t0 + t >= g.t1) return 0;
-                const int lp = ((g.t0 + t) * kTcTile + box * br) / a.cache.page_size;
+                const int slot = (g.t0 + t) * kTcTile + box * br, lp = slot / a.cache.page_size;
+                if (g.t0 + t >= g.t1 || slot >= g.end) return a.cache.n_pages * a.Hkv;
                 const int pg = a.cache.table[(int64_t)g.b * a.cache.max_pages + lp];
                 if (pg >= 0 && pg < a.cache.n_pages) return pg * a.Hkv + g.h;
                 atomicOr(a.status, ST_DEVICE);
@@ -1134,21 +1144,24 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     z1 = l == 0 ? z0 : z2;
                     z2 = place(tt + 1);
                 }
-                if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;  // (of every tile, as the loaders)
-                if (by_tma(a, g, tt)) {
-                    uint64_t* full = &st.full[pos.slot];
-                    if (lane == 0) {  // in the place of the loaders' 128 arrivals
-                        mbar_arrive_expect_tx(full, TB);
-                        mbar_arrive_n(full, 127);
-                    }
-                    __syncwarp();
-                    sent = (sent & ~(0x100u << pos.slot)) | 1u << pos.slot | pos.phase << (8 + pos.slot);
-                    if (half < HD / 64) {
-                        const int slot = (g.t0 + tt) * kTcTile + box * br;
-                        const int y = a.cache.page_size ? slot % a.cache.page_size : slot;
-                        tma_load_3d(smem_u32(ring) + pos.slot * TB + half * 16384 + box * br * 128, val ? &vmap : &kmap, half * 64, y,
-                                    !val || tt == nt - 1 ? z1 : z0, full);
-                    }
+                if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
+                // (rows past the item's end are zeros or whatever the cache holds: hidden from everyone, and
+                // the loaders look through the values of tiles with nodes)
+                const bool look = val && (g.t0 + tt + 1) * kTcTile > g.s.P;
+                uint64_t* full = look ? &st.landed[pos.slot] : &st.full[pos.slot];
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(full, TB);
+                    if (!look) mbar_arrive_n(full, 127);  // in the place of the loaders' 128 arrivals
+                }
+                __syncwarp();
+                const uint32_t phase = look ? landed >> pos.slot & 1u : pos.phase;
+                sent = (sent & ~(0x10100u << pos.slot)) | 1u << pos.slot | phase << (8 + pos.slot) | (uint32_t)look << (16 + pos.slot);
+                landed ^= (uint32_t)look << pos.slot;
+                if (half < HD / 64) {
+                    const int slot = (g.t0 + tt) * kTcTile + box * br;
+                    const int y = a.cache.page_size ? slot % a.cache.page_size : slot;
+                    tma_load_3d(smem_u32(ring) + pos.slot * TB + half * 16384 + box * br * 128, val ? &vmap : &kmap, half * 64, y,
+                                !val || tt == nt - 1 ? z1 : z0, full);
                 }
                 pos.skip(1);
                 reuse |= pos.slot == 0;
@@ -1158,7 +1171,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         // (after a failed wait: leave with no copy in flight. Otherwise every tile has been used.)
         if (!ok)
             for (int k = 0; k < S; ++k)
-                if (sent >> k & 1u) mbar_wait(&st.full[k], sent >> (8 + k) & 1u, a.status, 100000000LL);
+                if (sent >> k & 1u) mbar_wait(sent >> (16 + k) & 1u ? &st.landed[k] : &st.full[k], sent >> (8 + k) & 1u, a.status, 100000000LL);
     } else if (warp < 8) {  // ---- softmax
         const int gs = warp >> 2, wl = warp & 3;
         const uint32_t lanes = (uint32_t)(wl * 32) << 16;
@@ -1213,12 +1226,13 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 const bool tail = (tile + 1) * kTcTile > g.s.P;  // some slots are nodes'
                 ulonglong2 see = make_ulonglong2(0ull, 0ull);
                 if (tail && live) see = seen_bits(a, g, node, tile * kTcTile);  // (while the scores are on their way)
-                __syncwarp();
+                // (of a long causal run, most tiles are seen whole by all of the warp's rows)
+                const bool hide = tail && __any_sync(0xffffffffu, live && (see.x & see.y) != ~0ull);
                 if (!(ok = wait(&st.sfull[gs], ns))) break;
                 ++ns;
                 tc_fence_after();
                 if (!idle) {
-                    if (tail) {  // hidden scores become -inf
+                    if (hide) {  // hidden scores become -inf
 #pragma unroll 1
                         for (int c = 0; c < kTcTile; c += 32) {
                             const uint32_t bits = (uint32_t)((c < 64 ? see.x : see.y) >> (c & 32));
