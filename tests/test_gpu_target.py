@@ -407,6 +407,39 @@ def test_hidden_slots_do_not_matter(fe, dtype, cache, T, P):
     check_attention(c, store, None, q, plen, n, mask, out, lse)
 
 
+@pytest.mark.parametrize("page", [0, 3, 16, 128, 256])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "e4m3")])
+def test_what_lies_past_the_end_does_not_matter(fe, dtype, cache, causal, page):
+    """Slots from P + n on and the pool's other pages may hold anything, their page ids too."""
+    B, T, H, Hkv, P, ragged = 4, 150, 8, 4, (0, 100, 129, 511), (150, 3, 127, 0)
+    c = ref.config(dtype=dtype, cache_dtype=cache, n_heads=H, n_kv_heads=Hkv, head_dim=64, page_size=page, max_batch=B, max_seq=896)
+    t = fe.fe_target_init(c)
+    g = gen(page)
+    table, n_pages = ref.paged(c, B, g)
+    store = ref.random_cache(fe, t, c, g, table=table, n_pages=n_pages)
+    q, mask = rows(g, dtype, B, T, H, 64), None if causal else tree_masks(g, B, T).cuda()
+    plen, n = torch.tensor(P, dtype=torch.int32).cuda(), torch.tensor(ragged, dtype=torch.int32).cuda()
+    want = fe.fe_tree_attention(t, store, 0, q, plen, n_nodes=n, mask=mask)
+    kept = [x[0].clone() for x in (store.k, store.v, store.k_scale, store.v_scale) if x is not None]
+    for x, y in zip([x[0] for x in (store.k, store.v, store.k_scale, store.v_scale) if x is not None], kept):
+        x.fill_(math.nan)
+        for b in range(B):
+            end = P[b] + ragged[b]
+            if not page:
+                x[b, :, :end] = y[b, :, :end]
+                continue
+            for s in range(0, end, page):
+                pg, rows_ = int(table[b, s // page]), min(page, end - s)
+                x[pg, :, :rows_] = y[pg, :, :rows_]
+    if page:
+        for b in range(B):
+            table[b, (P[b] + ragged[b] + page - 1) // page:] = -7
+    got = fe.fe_tree_attention(t, store, 0, q, plen, n_nodes=n, mask=mask)
+    assert fe.fe_target_status(t) == fe.FE_OK
+    assert torch.isfinite(want[0]).all() and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("scale", [math.nan, math.inf, -math.inf, 0.0, 3e38, -1.0, 1e-40])
 def test_hidden_rows_with_any_scale(fe, scale):
     """A row that no node sees may hold any scale: branches whose rows were never written."""
