@@ -206,13 +206,14 @@ __device__ __noinline__ ulonglong2 seen_bits(const TreeAttnArgs& a, const Segmen
 
 // ---- loaders ------------------------------------------------------------------------------------
 // What a lane knows of its row (32 w + lane) of a tile: the cache row, or -1 for a slot past the
-// item's end (or with a bad page id); and the row's scales. A node's row may be hidden from all and
-// hold anything. A NaN or infinity among its scales would spread through a masked score or a zero
-// probability: outside of 2^-120 .. 2^120 a key's scale becomes 1 and the value row (bad) zeros.
+// item's end (or with a bad page id); the row's scales; and whether it is a node's. A node's row may
+// be hidden from all and hold anything. A NaN or infinity among its scales would spread through a
+// masked score or a zero probability: unless valid_scale, a key's scale becomes 1 and a value row
+// zeros. (Looked at where they are used: here it would wait for the loads.)
 struct RowInfo {
     int64_t row;
     float ks, vs;
-    bool bad;
+    bool node;
 };
 __device__ __forceinline__ bool valid_scale(float x) { return __float_as_uint(x) - (7u << 23) <= 240u << 23; }
 
@@ -226,10 +227,7 @@ __device__ __forceinline__ RowInfo row_info(const TreeAttnArgs& a, const Segment
         if (Q8) {
             x.ks = a.cache.ks[x.row];
             x.vs = a.cache.vs[x.row];
-            if (slot >= g.s.P) {
-                if (!valid_scale(x.ks)) x.ks = 1.f;
-                x.bad = !valid_scale(x.vs);
-            }
+            x.node = slot >= g.s.P;
         }
     }
     return x;
@@ -690,6 +688,13 @@ __device__ __forceinline__ float split_query_row(unsigned char* block, int row) 
     return __uint_as_float((uint32_t)(127 + c2) << 23);
 }
 
+// Whether a tile of a bfloat16 cache comes by TMA: all do where a box holds 32 rows or more; of
+// smaller pages' the loaders bring the values, except those to look through.
+constexpr int kWideBox = 32;
+__device__ __forceinline__ bool by_tma(const TreeAttnArgs& a, const Segment& g, int tt, bool val) {
+    return a.box_rows >= kWideBox || (a.box_rows > 0 && (!val || (g.t0 + tt + 1) * kTcTile > g.s.P));
+}
+
 // A position in the ring of tiles: slot and phase, moved on by small steps without division.
 template <int S>
 struct RingPos {
@@ -814,10 +819,10 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
 #pragma unroll 1
             for (int tt = -1; tt < nt; ++tt) {  // K0 (K1 V0) (K2 V1) ...
                 const float vs1 = x1.vs;
-                const bool has1 = x1.row >= 0, ok1 = has1 && !x1.bad;
+                const bool has1 = x1.row >= 0, ok1 = has1 && (!x1.node || valid_scale(vs1));
                 if (tt + 1 < nt) {  // the rows' scales; the rows themselves where TMA cannot fetch them
                     if (kreuse && !(ok = wait(&st.kempty[kpos.slot], kpos.phase ^ 1u))) break;
-                    key_scales[(tiles++ % kTcScales) * kTcTile + r] = has1 ? x1.ks : 1.f;
+                    key_scales[(tiles++ % kTcScales) * kTcTile + r] = has1 && (!x1.node || valid_scale(x1.ks)) ? x1.ks : 1.f;
                     if (a.box_rows > 0) {
                         mbar_arrive(&st.kfull[kpos.slot]);
                     } else {
@@ -851,7 +856,6 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         RingPos<S> pos;
         bool reuse = false;       // the ring has been filled once
         uint32_t landed = 0;      // by slot: the phase of landed[] that comes next
-        const bool tma = a.box_rows > 0;
         while (ok && next(g)) {
             const int nt = g.t1 - g.t0;
 #pragma unroll 1
@@ -861,7 +865,10 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 unsigned char* dst = ring + pos.slot * TB;
                 uint64_t* full = &st.full[pos.slot];
                 const int first = g.s.P - (g.t0 + tt) * kTcTile;  // first row of the tile that is a node's
-                if (tma) {  // what TMA brings is looked through where it may hold what nobody sees
+                // (where the loaders fill slots, every slot's release is waited for: a barrier's phase is one
+                // bit, and a role that skipped one could take an older release for the one it needs)
+                if (a.box_rows < kWideBox && reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
+                if (by_tma(a, g, tt, val)) {  // what TMA brings is looked through where it may hold what nobody sees
                     if (val && first < kTcTile) {
                         if (!(ok = wait(&st.landed[pos.slot], landed >> pos.slot))) break;
                         landed ^= 1u << pos.slot;
@@ -872,9 +879,6 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         mbar_arrive(full);
                     }
                 } else {
-                    // (every slot's release is waited for: a barrier's phase is one bit, and a role that
-                    // skipped one could take an older release for the one it needs)
-                    if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
                     const RowInfo x = row_info<Q8>(a, g, g.t0 + tt, w * 32 + lane);
                     load_tile<HD>(val ? a.cache.v : a.cache.k, x, dst, w, lane);
                     if (val && first < kTcTile) {
@@ -1145,6 +1149,11 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                     z2 = place(tt + 1);
                 }
                 if (reuse && !(ok = wait(&st.empty[pos.slot], pos.phase ^ 1u))) break;
+                if (!by_tma(a, g, tt, val)) {
+                    pos.skip(1);
+                    reuse |= pos.slot == 0;
+                    continue;
+                }
                 // (rows past the item's end are zeros or whatever the cache holds: hidden from everyone, and
                 // the loaders look through the values of tiles with nodes)
                 const bool look = val && (g.t0 + tt + 1) * kTcTile > g.s.P;
