@@ -931,22 +931,23 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             for (int t0 = -step; t0 < nt && ok; t0 += step) {  // O += P V of tile tt, S = Q K^T of the next
                 const int tt = t0 + first;
                 const bool pv = t0 >= 0 && tt < nt, qk = tt + step < nt;
+                // the tiles first (K only if it is there already), with the proxy fence that they need; the
+                // probabilities, which are what is late as a rule, and the stream's turn after it
+                if (pv) ok = ok && wait(&st.full[vp.slot], vp.phase);
+                bool kthere = qk && mbar_try_wait(&kfull[kp.slot], kp.phase);
+                kthere = __all_sync(0xffffffffu, kthere);
+                fence_async_proxy();
                 if (pv) {
+                    if (t0 == 0 && seg > 1) ok = ok && wait(&st.ofree, seg - 2);
                     ok = ok && wait(&st.pfull[gs], np);
                     ++np;
-                    if (t0 == 0 && seg > 1) ok = ok && wait(&st.ofree, seg - 2);
-                    ok = ok && wait(&st.full[vp.slot], vp.phase);
                 }
-                // a stream's turn; its K tile is waited for before the products if it is there already
                 if (gs == 1 || turn > 0) ok = ok && wait(&st.turn[gs], gs == 1 ? turn : turn - 1);
                 ++turn;
-                bool kthere = qk && mbar_try_wait(&kfull[kp.slot], kp.phase);
                 if (!__all_sync(0xffffffffu, ok)) {
                     ok = false;
                     break;
                 }
-                kthere = __all_sync(0xffffffffu, kthere);
-                fence_async_proxy();
                 tc_fence_after();
                 const bool leader = elect_one();
                 if (pv && leader) {
