@@ -175,9 +175,9 @@ RowsArgs rows_args(const fe_target* t) {
     return r;
 }
 
-bool rows_16(const fe_rows& r, int es) {
-    const int v = 16 / es;
-    return ((uintptr_t)r.p & 15) == 0 && r.batch % v == 0 && r.token % v == 0 && r.head % v == 0;
+bool rows_on(int bytes, const fe_rows& r, int es) {
+    const int v = bytes / es;
+    return ((uintptr_t)r.p & (bytes - 1)) == 0 && r.batch % v == 0 && r.token % v == 0 && r.head % v == 0;
 }
 
 }  // namespace
@@ -326,8 +326,8 @@ fe_status fe_tree_attention(fe_target* t, const fe_tree_attention_args* a, void*
     r.part_o = t->part_o;
     r.part_ml = t->part_ml;
     r.status = t->status;
-    r.q_vec = rows_16(a->q, es);
-    r.out_vec = rows_16(a->out, es);
+    r.q_vec = rows_on(16, a->q, es);
+    r.out_vec = rows_on(32, a->out, es) ? 2 : rows_on(16, a->out, es);
     if (!tree_attn_fits(r, c.dtype)) return FE_ERR_UNSUPPORTED;
     FE_TRY(launch_tree_attn(r, c.dtype, c.cache_dtype, c.head_dim, t->num_sms, (cudaStream_t)stream));
     return FE_OK;

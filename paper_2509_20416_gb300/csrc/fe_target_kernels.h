@@ -71,9 +71,9 @@ struct TreeAttnArgs {
     CacheView cache;
     SplitDesc* split;         // [G], of every attention CTA
     int part_rows;            // rows of a partial item in the workspace: per CTA two items,
-    float *part_o, *part_ml;  // [2 G][part_rows][hd] sums, [2 G][part_rows][2] (max, sum)
+    float *part_o, *part_ml;  // sums [2 G][hd / 4][part_rows][4], (max, sum) [2 G][part_rows][2]
     int* status;
-    int q_vec, out_vec;  // rows of q / out on 16-byte boundaries
+    int q_vec, out_vec;  // rows of q / out on 16-byte boundaries (out: 2 on 32-byte ones)
     int box_rows;        // cache rows of a TMA box (0: no tensor maps)
     int q_tma;           // the queries come by TMA too
 };

@@ -15,7 +15,7 @@ namespace {
 // four rows' reads are under way together. Bound by latency: its launch, which the attention's
 // registers keep from overlapping, and three dependent reads (a row a warp took 20 us where 150
 // items of 196 rows were split, four take 8).
-constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32, kJoinRows = 4 * kJoinWarps;
+constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32;
 
 __device__ __forceinline__ void store_four(bf16_t* p, float a, float b, float c, float d, bool aligned) {
     const uint2 w = make_uint2(pack_bf16(a, b), pack_bf16(c, d));
@@ -69,72 +69,53 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attn_join_kernel(const __gr
     const SplitDesc w = a.split[blockIdx.x];
     const int c0 = blockIdx.x, c1 = w.last;
     if (c1 <= c0) return;
-    const int nrow = min(ROWS, w.rows - w.m * ROWS);
-    constexpr int GL = 32 * kJoinWarps / kJoinRows, NV = HD / (4 * GL);  // lanes of a row, float4 of a lane (4 columns each, GL apart)
-    const int l = lane % GL;
-    const unsigned group = 0xFFu << (lane / GL * GL);
-    for (int r = wid * (32 / GL) + lane / GL; r < nrow; r += gridDim.y * kJoinRows) {
-        // the partials' row of contributor c, or -1 if no tile starts in c's units
-        auto part = [&](int c) -> int64_t {
-            if (c > c1 || (c > c0 && !a.split[c].has0)) return -1;
-            return ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * a.part_rows + r;
-        };
-        float mx = -INFINITY;
-        for (int c = c0 + l; c <= c1; c += GL) {
-            const int64_t p = part(c);
-            if (p >= 0) mx = fmaxf(mx, __ldcg(a.part_ml + 2 * p));
+    const int r = wid / (HD / 16) * 32 + lane, col = wid % (HD / 16) * 16;
+    if (r >= min(ROWS, w.rows - w.m * ROWS)) return;
+    // contributor c's partial (a share of the item in which no tile starts has none: what lies there is
+    // read all the same, ahead of the flag, and not used)
+    auto slot = [&](int c) { return (int64_t)c * 2 + (c == c0 ? 1 : 0); };
+    auto has = [&](int c) { return c == c0 || __ldcg(&a.split[c].has0) != 0; };
+    float4 o[4];
+    float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.part_ml + 2 * (slot(c) * a.part_rows + r)));
+        const float4* src = reinterpret_cast<const float4*>(a.part_o + slot(c) * a.part_rows * HD) + (int64_t)(col / 4) * a.part_rows + r;
+        float4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __ldcg(src + e * a.part_rows);
+        const bool mine = has(c);
+        const float mn = mine ? fmaxf(mx, ml.x) : mx, ms = mn == -INFINITY ? 0.f : mn;
+        const float f = exp2f(mx - ms), g = exp2f(ml.x - ms);
+        mx = mn;
+        if (!mine) continue;
+        sum = sum * f + ml.y * g;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[e].x = o[e].x * f + v[e].x * g;
+            o[e].y = o[e].y * f + v[e].y * g;
+            o[e].z = o[e].z * f + v[e].z * g;
+            o[e].w = o[e].w * f + v[e].w * g;
         }
-#pragma unroll
-        for (int o = GL / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(group, mx, o));
-        const float ms = mx == -INFINITY ? 0.f : mx;
-        float4 o[NV];
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < NV; ++e) o[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int b0 = c0; b0 <= c1; b0 += GL) {
-            const int64_t p = part(b0 + l);
-            const float2 ml = p >= 0 ? __ldcg(reinterpret_cast<const float2*>(a.part_ml + 2 * p)) : make_float2(-INFINITY, 0.f);
-            const float f = exp2f(ml.x - ms);
-            const int n = min(GL, c1 - b0 + 1);
-#pragma unroll 2
-            for (int k = 0; k < n; ++k) {
-                const int from = lane / GL * GL + k;
-                const int64_t pk = __shfl_sync(group, p, from);
-                const float fk = __shfl_sync(group, f, from), lk = __shfl_sync(group, ml.y, from);
-                if (pk < 0) continue;
-                const float4* src = reinterpret_cast<const float4*>(a.part_o + pk * HD) + l;
-                float4 v[NV];
-#pragma unroll
-                for (int e = 0; e < NV; ++e) v[e] = __ldcg(src + GL * e);
-                sum += lk * fk;
-#pragma unroll
-                for (int e = 0; e < NV; ++e) {
-                    o[e].x += v[e].x * fk;
-                    o[e].y += v[e].y * fk;
-                    o[e].z += v[e].z * fk;
-                    o[e].w += v[e].w * fk;
-                }
-            }
-        }
-        const int row = w.m * ROWS + r, node = row / a.G, head = w.h * a.G + row % a.G;
-        const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-        QT* dst = (QT*)a.out.p + w.b * a.out.batch + (int64_t)node * a.out.token + (int64_t)head * a.out.head;
-#pragma unroll
-        for (int e = 0; e < NV; ++e) {
-            const bool none = sum == 0.f;
-            store_four(dst + 4 * (l + GL * e), none ? 0.f : o[e].x * inv, none ? 0.f : o[e].y * inv, none ? 0.f : o[e].z * inv,
-                       none ? 0.f : o[e].w * inv, a.out_vec);
-        }
-        if (a.lse && l == 0)
-            a.lse[((int64_t)w.b * a.T + node) * a.H + head] =
-                sum == 0.f ? -INFINITY : mx * 0.6931471805599453f + logf(sum);
     }
+    const int row = w.m * ROWS + r, node = row / a.G, head = w.h * a.G + row % a.G;
+    const bool none = sum == 0.f;
+    const float inv = none ? 0.f : 1.0f / sum;
+    QT* dst = (QT*)a.out.p + w.b * a.out.batch + (int64_t)node * a.out.token + (int64_t)head * a.out.head + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        store_four(dst + 4 * e, none ? 0.f : o[e].x * inv, none ? 0.f : o[e].y * inv, none ? 0.f : o[e].z * inv,
+                   none ? 0.f : o[e].w * inv, a.out_vec);
+    if (a.lse && col == 0)
+        a.lse[((int64_t)w.b * a.T + node) * a.H + head] = none ? -INFINITY : mx * 0.6931471805599453f + logf(sum);
 }
 
 template <typename QT, int HD, int ROWS>
 cudaError_t launch_join(const TreeAttnArgs& a, int ncta, cudaStream_t st) {
     const int rows = (int)min((int64_t)a.T * a.G, (int64_t)ROWS);  // of an item
-    return launch_k(tree_attn_join_kernel<QT, HD, ROWS>, dim3(ncta, (rows + kJoinRows - 1) / kJoinRows), dim3(kJoinThreads), 0, st, true, a);
+    return launch_k(tree_attn_join_kernel<QT, HD, ROWS>, dim3(ncta, ((rows + 31) / 32 * (HD / 16) + kJoinWarps - 1) / kJoinWarps), dim3(kJoinThreads), 0, st, true, a);
 }
 
 template <int HD, int NI>

@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
                 const int64_t pr = ((int64_t)blockIdx.x * 2 + g.slot) * a.part_rows + r;
 #pragma unroll
                 for (int j = 0; j < NC; ++j)
-                    *reinterpret_cast<float4*>(a.part_o + pr * HD + tx * 4 + 64 * j) =
+                    *reinterpret_cast<float4*>(a.part_o + (pr - r) * HD + ((tx + 16 * j) * a.part_rows + r) * 4) =
                         make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
                 if (tx == 0) {
                     a.part_ml[2 * pr] = mx[i];

@@ -58,20 +58,17 @@ struct TcShape {
     static constexpr int kSlots = Q8 ? 2 : MT == 1 ? 5 : 4;
     static constexpr int kKeySlots = Q8 ? 3 : 0;
     static constexpr int kRawSlots = Q8 ? (MT == 1 ? 3 : 2) : 0;
-    // the epilogue's staging: 16 columns of a warp's rows, or 8 where there is no room for more
-    static constexpr int kStageCols = Q8 && MT == 2 ? 8 : 16;
-    static constexpr int kStageBytes = 8 * 32 * kStageCols * 4;
     static constexpr int kScaleBytes = Q8 ? kTcScales * kTcTile * 4 : 0;  // the key tiles' scales
     static constexpr int kThreads = 512;
     static constexpr int kReaders = 15;  // warps that read the segments
-    static constexpr int kData = MT * kTileBytes + kSlots * kTileBytes + (kKeySlots + kRawSlots) * kRawBytes + kStageBytes + kScaleBytes;
+    static constexpr int kData = MT * kTileBytes + kSlots * kTileBytes + (kKeySlots + kRawSlots) * kRawBytes + kScaleBytes;
 };
 
 constexpr int kTcSegs = 4;  // segments planned ahead
 
 struct TcState {
     uint64_t full[6], empty[6], landed[6], kfull[4], kempty[4], rawfull[4], rawempty[4], segfull[kTcSegs], segempty[kTcSegs], qfull, qempty, qready, sfull[2],
-        pfull[2], odone, ofree, mlfull, mlfree, drain[2], turn[2];
+        pfull[2], odone[2], ofree, mlfull, mlfree, drain[2], turn[2];
     Segment seg[kTcSegs];  // weight 0: no more
     uint32_t tmem;
     int abort;
@@ -162,6 +159,11 @@ __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -630,7 +632,7 @@ __device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segmen
         }
         if (!any) continue;
         if (g.whole) store_one((bf16_t*)dst + e, t);
-        else ((float*)dst)[e] = t;
+        else ((float*)dst)[e / 4 * (4 * kAttnItemRows) + e % 4] = t;
     }
 }
 
@@ -726,8 +728,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     unsigned char* ring = qbuf + MT * TB;
     unsigned char* keyring = ring + S * TB;  // (e4m3)
     unsigned char* rawring = keyring + SH::kKeySlots * SH::kRawBytes;
-    unsigned char* stages = rawring + SH::kRawSlots * SH::kRawBytes;
-    float* key_scales = (float*)(stages + SH::kStageBytes);
+    float* key_scales = (float*)(rawring + SH::kRawSlots * SH::kRawBytes);
     TcState& st = *reinterpret_cast<TcState*>(qbuf + SH::kData);
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     griddep_launch_dependents();
@@ -772,8 +773,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             mbar_init(&st.pfull[i], 4);
             mbar_init(&st.drain[i], 1);
             mbar_init(&st.turn[i], 1);
+            mbar_init(&st.odone[i], 1);
         }
-        mbar_init(&st.odone, 2);
         mbar_init(&st.ofree, 8);
         mbar_init(&st.mlfull, 8);
         mbar_init(&st.mlfree, 8);
@@ -994,7 +995,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             }
             if (ok && elect_one()) {
                 if (!qdone) tc_commit(&st.qempty);
-                tc_commit(&st.odone);
+                tc_commit(&st.odone[gs]);
             }
             __syncwarp();
             base.skip_long(Q8 ? nt : 2 * nt);
@@ -1274,7 +1275,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             if (more && !(ok = split(g2, cur + 1))) break;
             ktile += nt;
             // ---- the segment's result
-            if (!(ok = wait(&st.odone, cur))) break;
+            if (!(ok = wait(&st.odone[gs], cur))) break;
+            if (!pair && !(ok = wait(&st.odone[gs ^ 1], cur))) break;
             tc_fence_after();
             float f0 = 1.f, f1 = 0.f;  // weights of this stream's block, and of the other's (alternating)
             const bool join = !pair && nt > 1;
@@ -1296,79 +1298,56 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             nj += join;
             // (a joined block's columns are shared out between the streams' warps)
             if (!idle && (pair || join || gs == 0)) {
-                // rows leave through shared memory, 8 or 16 columns at a time, so that a warp writes whole
-                // sectors: the lanes' rows as addresses of the output or of the partial
-                constexpr int CW = SH::kStageCols, K4 = CW / 4;  // columns a round; 16-byte chunks, and lanes, of a row
-                unsigned char* stage = stages + warp * (32 * CW * 4);
+                // A lane's row leaves 16 columns at a time, as whole sectors: of the output's row, or of the
+                // partial's, where a warp's 32 rows of 4 columns are 512 bytes in a row.
                 const int head = g.h * a.G + row % a.G;
                 const int64_t pr = ((int64_t)blockIdx.x * 2 + g.slot) * kAttnItemRows + (row - g.m * kAttnItemRows);
-                const unsigned long long mine =
-                    !live ? 0ull
-                    : g.whole ? (unsigned long long)((bf16_t*)a.out.p + g.b * a.out.batch + (int64_t)node * a.out.token +
-                                                     (int64_t)head * a.out.head)
-                              : (unsigned long long)(a.part_o + pr * HD);
-                // o = f0 u + f1 v with v the other stream's block; alone, a block counts half twice.
+                float* part = a.part_o + ((int64_t)blockIdx.x * 2 + g.slot) * (kAttnItemRows * HD) + (row - g.m * kAttnItemRows) * 4;
+                bf16_t* dst = (bf16_t*)a.out.p + g.b * a.out.batch + (int64_t)node * a.out.token + (int64_t)head * a.out.head;
+                // o = f0 u + f1 v with v the other stream's block.
                 // Zero sums: a row that sees nothing, whose block may hold anything.
-                const float norm = (g.whole ? sum == 0.f ? 0.f : 1.f / sum : 1.f) * (join ? 1.f : 0.5f);
+                const float norm = g.whole ? sum == 0.f ? 0.f : 1.f / sum : 1.f;
                 f0 *= norm;
-                f1 = join ? f1 * norm : f0;
+                f1 *= norm;
                 const bool zero = g.whole && sum == 0.f;
-                unsigned long long rows[K4];  // the rows that this lane stores parts of
-#pragma unroll
-                for (int k = 0; k < K4; ++k) rows[k] = __shfl_sync(0xffffffffu, mine, 32 / K4 * k + lane / K4);
-                const bool vec = a.out_vec;
-                const uint32_t other = join ? tmem + 256 + (gs ^ 1) * 128 + lanes : to;
 #pragma unroll 1
-                for (int c = join && gs ? HD / 2 : 0; c < (join && !gs ? HD / 2 : HD); c += CW) {
-                    uint32_t u[CW], v[CW];
-                    if constexpr (CW == 16) {
-                        tc_ld16_start(to + c, u);
-                        tc_ld16_start(other + c, v);
+                for (int c = join && gs ? HD / 2 : 0; c < (join && !gs ? HD / 2 : HD); c += 16) {
+                    uint32_t u[16];
+                    tc_ld16_start(to + c, u);
+                    if (join) {
+                        uint32_t v[16];
+                        tc_ld16_start(tmem + 256 + (gs ^ 1) * 128 + lanes + c, v);
                         tc_ld16_wait(u);
                         tc_ld16_wait(v);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            u[e] = __float_as_uint(fmaf(__uint_as_float(v[e]), f1, __uint_as_float(u[e]) * f0));
                     } else {
-                        tc_ld8(to + c, u);
-                        tc_ld8(other + c, v);
+                        tc_ld16_wait(u);
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) u[e] = __float_as_uint(__uint_as_float(u[e]) * f0);
                     }
-                    __syncwarp();
-                    // chunk k of row l lies at 16 (k ^ l / 2) (or l / 4) of the row's bytes: no bank conflicts
-                    auto place = [&](int r, int k) { return r * (CW * 4) + ((k ^ (r >> (CW == 16 ? 1 : 2))) & (K4 - 1)) * 16; };
+                    if (!live) continue;
+                    if (!g.whole) {
 #pragma unroll
-                    for (int k = 0; k < K4; ++k) {
-                        float o[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            o[e] = zero ? 0.f : __uint_as_float(u[4 * k + e]) * f0 + __uint_as_float(v[4 * k + e]) * f1;
-                        *reinterpret_cast<float4*>(stage + place(lane, k)) = make_float4(o[0], o[1], o[2], o[3]);
+                        for (int e = 0; e < 16; e += 4)
+                            *reinterpret_cast<uint4*>(part + (c + e) * kAttnItemRows) = make_uint4(u[e], u[e + 1], u[e + 2], u[e + 3]);
+                        continue;
                     }
-                    __syncwarp();
-                    float4 y[K4];
-                    const int col = c + 4 * (lane % K4);
+                    uint32_t w[8];
 #pragma unroll
-                    for (int k = 0; k < K4; ++k)  // K4 lanes a row
-                        y[k] = *reinterpret_cast<const float4*>(stage + place(32 / K4 * k + lane / K4, lane % K4));
-                    if (g.whole) {
-#pragma unroll
-                        for (int k = 0; k < K4; ++k) {
-                            const uint2 w = make_uint2(pack_bf16(y[k].x, y[k].y), pack_bf16(y[k].z, y[k].w));
-                            bf16_t* d = (bf16_t*)rows[k] + col;
-                            if (!rows[k]) continue;
-                            if (vec) {
-                                *reinterpret_cast<uint2*>(d) = w;
-                            } else {
-                                d[0].bits = (uint16_t)w.x;
-                                d[1].bits = (uint16_t)(w.x >> 16);
-                                d[2].bits = (uint16_t)w.y;
-                                d[3].bits = (uint16_t)(w.y >> 16);
-                            }
-                        }
+                    for (int e = 0; e < 8; ++e)
+                        w[e] = zero ? 0u : pack_bf16(__uint_as_float(u[2 * e]), __uint_as_float(u[2 * e + 1]));
+                    if (a.out_vec == 2) {
+                        st_global_32(dst + c, w);
+                    } else if (a.out_vec) {
+                        *reinterpret_cast<uint4*>(dst + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4*>(dst + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
                     } else {
 #pragma unroll
-                        for (int k = 0; k < K4; ++k)
-                            if (rows[k]) *reinterpret_cast<float4*>((float*)rows[k] + col) = y[k];
+                        for (int e = 0; e < 16; ++e) dst[c + e].bits = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
                     }
                 }
-                __syncwarp();
                 if (live && (pair || gs == 0)) {
                     if (!g.whole)
                         *reinterpret_cast<float2*>(a.part_ml + 2 * pr) = make_float2(m, sum);
@@ -1377,7 +1356,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                             sum == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(sum);
                 }
                 if (live && *(volatile int*)&st.odd[cur & 7])
-                    put_odd_columns<HD, Q8>(a, g, node, head, m, (void*)mine, join && gs ? HD / 2 : 0, join && !gs ? HD / 2 : HD);
+                    put_odd_columns<HD, Q8>(a, g, node, head, m, g.whole ? (void*)dst : (void*)part, join && gs ? HD / 2 : 0, join && !gs ? HD / 2 : HD);
             }
             tc_fence_before();
             __syncwarp();
