@@ -349,14 +349,21 @@ __device__ __forceinline__ uint2 scale_factors(float scale) {
 }
 
 // A lane's 16 numbers of a row, as two 16-byte chunks of a bfloat16 tile. Lanes of a row's second 64
-// columns store their chunks in the other order, so that eight lanes store into different banks.
+// columns take their two halves in the other order, so that eight lanes store into different banks.
+__device__ __forceinline__ void raw_words(const unsigned char* src, int c, uint32_t (&w)[4]) {
+    const uint4 u = *reinterpret_cast<const uint4*>(src);
+    const bool swap = c >> 2;
+    w[0] = swap ? u.z : u.x;
+    w[1] = swap ? u.w : u.y;
+    w[2] = swap ? u.x : u.z;
+    w[3] = swap ? u.y : u.w;
+}
 template <int HD>
 __device__ __forceinline__ void store_converted(unsigned char* dst, int row, int c, const uint32_t (&o)[8]) {
     unsigned char* base = dst + (c >> 2) * 16384;
     const int swap = c >> 2, c0 = 2 * (c & 3) + swap, c1 = 2 * (c & 3) + 1 - swap;
-    const uint4 lo = make_uint4(o[0], o[1], o[2], o[3]), hi = make_uint4(o[4], o[5], o[6], o[7]);
-    *reinterpret_cast<uint4*>(base + sw128_offset(row, c0)) = swap ? hi : lo;
-    *reinterpret_cast<uint4*>(base + sw128_offset(row, c1)) = swap ? lo : hi;
+    *reinterpret_cast<uint4*>(base + sw128_offset(row, c0)) = make_uint4(o[0], o[1], o[2], o[3]);
+    *reinterpret_cast<uint4*>(base + sw128_offset(row, c1)) = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
 // The warp's rows of a tile once more, with what convert_tile's loop leaves out: the second factor
@@ -371,9 +378,8 @@ __device__ __noinline__ bool convert_rare(const unsigned char* raw, uint2 mine, 
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = i * RP + lane / CH, row = w * 32 + r;
         const uint32_t f1 = __shfl_sync(0xffffffffu, mine.x, r), f2 = __shfl_sync(0xffffffffu, mine.y, r);
-        const uint4 u = *reinterpret_cast<const uint4*>(raw + row * HD + c * 16);
-        const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-        uint32_t o[8];
+        uint32_t in[4], o[8];
+        raw_words(raw + row * HD + c * 16, c, in);
 #pragma unroll
         for (int e = 0; e < 4; ++e) e4m3x4_to_bf16(in[e], o[2 * e], o[2 * e + 1]);
 #pragma unroll
@@ -401,13 +407,12 @@ __device__ __forceinline__ bool convert_tile(const unsigned char* raw, bool has_
     const uint2 mine = has_row ? scale_factors(scale) : make_uint2(0, 0x3F803F80u);
     const unsigned char* src = raw + (w * 32 + lane / CH) * HD + c * 16;
     uint32_t nan = 0;
-#pragma unroll 2
+#pragma unroll 1
     for (int i = 0; i < 32 / RP; ++i) {
         const int r = i * RP + lane / CH;
         const uint32_t f1 = __shfl_sync(0xffffffffu, mine.x, r);
-        const uint4 u = *reinterpret_cast<const uint4*>(src + i * RP * HD);
-        const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-        uint32_t o[8];
+        uint32_t in[4], o[8];
+        raw_words(src + i * RP * HD, c, in);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             nan |= (in[e] & 0x7F7F7F7Fu) + 0x01010101u;
