@@ -13,25 +13,38 @@
 // every key/value tile; a smaller one gives both streams the same rows, on alternate tiles, and
 // adds their results at the end. While one stream's softmax runs on the CUDA cores, the tensor
 // cores work on the other's products.
-//   warps 0-3, 4-7   softmax of stream 0, 1: thread = row (TMEM lane); they also load the queries, the
-//                    next segment's while this one's last product runs, and write the results
-//   warps 8-11       loaders: rows from the cache into 128-byte-swizzled tiles of 128 slots (K and
-//                    V alike, [slot][hd]), by cp.async, or converted from e4m3 on the way
+//   warps 0-3, 4-7   softmax of stream 0, 1: thread = row (TMEM lane); they also load the queries
+//                    that TMA cannot, the next segment's while this one's last product runs, split
+//                    them for e4m3 keys, and write the results
+//   warps 8-11       loaders. bfloat16: values of tiles with nodes are looked through where TMA put
+//                    them, tiles that TMA does not bring come by cp.async. e4m3: a tile's key scales,
+//                    and values converted to bfloat16 [slot][hd]
 //   warps 12, 13     issue the MMAs of stream 0, 1: S = Q K^T (K-major operands), O += P V with P
 //                    (bfloat16) read from TMEM over S's own columns and V as the MN-major operand
-//   warp 14          plans: the CTA's segments (shares of items), a few ahead of their use
-//   warp 15          TMA: whole bfloat16 tiles of prefix slots, in boxes of a page's rows (the loaders
-//                    then fetch only the tiles that reach into the nodes' rows; all of them where the
-//                    pages' size has no such box); e4m3: bulk copies of the raw rows
+//   warp 14          plans: the CTA's segments (shares of items), a few ahead of their use, and their
+//                    queries by TMA where heads and strides allow
+//   warp 15          TMA: tiles in boxes of a page's rows into the rings; e4m3 values by bulk copies
+// e4m3 keys go to the tensor cores as they are, with queries as two e4m3 parts (split_query_row);
+// their scales are applied to the scores.
+//
 // The softmax keeps a reference maximum per row and rescales O only when the maximum has grown by
-// more than 2^8 (the probabilities then stay below 2^8, where bfloat16 is as precise as below 1):
-// after the first tiles that is rare; it saves a pass over O per tile and a pass over the scores
-// for their maximum. Sums and statistics
-// are float32; probabilities are rounded to bfloat16 for the second product, which costs 2^-9 of
-// each on average and is what the 16-bit tensor path offers.
+// more than 2^12: after the first tiles that is rare, and it saves a pass over O per tile and a pass
+// over the scores for their maximum. The probabilities then stay below 2^12, where floating point is
+// as precise as below 1, and sums over a long cache are far from overflow. (81 nodes over 131k e4m3
+// slots: 362 us with 2^8, 353 with 2^12, 354 with 2^16 or 2^24.) Sums and statistics are float32;
+// probabilities are rounded to bfloat16 for the second product, which costs 2^-9 of each at most and
+// is what the 16-bit tensor path offers.
 // Values in slots that a row does not see meet a zero probability, but 0 x NaN is NaN: the loaders
-// zero the non-finite elements of nodes' value rows and flag the segment, whose epilogue then
-// adds their terms to the rows that do see them.
+// zero the non-finite elements of nodes' value rows (and of what lies past the item's end) and flag
+// the segment, whose epilogue then adds their terms to the rows that do see them.
+//
+// What bounds it (GB300, 128-wide heads): 32 sequences over 256 to 4096 bfloat16 slots, 8 KV heads,
+// 17 nodes x 4 heads: 66 us, 4.5 TB/s (pages of 16: 75); 49 x 4 rows: 90 us, 645 TFLOP/s. 81 nodes x
+// 64 heads over 131k slots: bfloat16 303 us, 1150 TFLOP/s; e4m3 353 us, 985 TFLOP/s. The long ones
+// are bound by a stream's chain, softmax (1300 clocks a tile, 1024 of them exponentials; with key
+// scales 2200 and more) after product after softmax, of which two are in flight; the products alone
+// need 2048 of the 3200 clocks that a tile pair takes. The short ones pay 7 us of start (schedule,
+// first tile, cold instruction caches) and an epilogue of 2 us a share of an item.
 #pragma once
 
 #include <cuda.h>
@@ -43,6 +56,7 @@
 namespace fe {
 
 constexpr int kTcTile = 128;
+constexpr float kRescale = 12.f;  // log2 of the growth of a row's maximum that its block is rescaled for
 // Key tiles whose scales are at hand. A softmax still reads tile t's when the loaders may be at tile
 // t + 1 + kKeySlots (the other stream's products may be one tile further).
 constexpr int kTcScales = 8;
@@ -532,7 +546,7 @@ __device__ __noinline__ void rescale_row(uint32_t ts, int np, uint32_t to, int n
 // One row's softmax of a tile, in one pass over its 128 scores x at TMEM columns ts: 2^(scale2 x - m)
 // as packed bfloat16 over the first 64 columns (32 scores become 16 columns, always behind what is
 // still to be read), their float32 sum added to `sum`. m is the row's reference maximum; when some
-// row of the warp has outgrown it by more than 2^8, the warp moves to new references on the spot.
+// row of the warp has outgrown it by more than 2^12, the warp moves to new references on the spot.
 // Bound by the exponentials (16 a clock and SM), in whose shade the next 32 scores are loaded and
 // their maximum taken. A loop with a short body: the CTA's roles share the instruction caches, and
 // unrolled rows made every one of them wait for fetches.
@@ -563,7 +577,7 @@ __device__ __forceinline__ void softmax_row(uint32_t ts, uint32_t to, float scal
     float mx = max32(x) * scale2;
 #pragma unroll 1
     for (int c = 0; c < kTcTile; c += 32) {
-        if (__any_sync(0xffffffffu, mx > m + 8.f)) {
+        if (__any_sync(0xffffffffu, mx > m + kRescale)) {
             const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
             const uint64_t ff = pair_f32(__float_as_uint(f), __float_as_uint(f));
             z[0] = fma_x2(z[0], ff, 0);
