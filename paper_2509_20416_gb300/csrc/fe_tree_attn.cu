@@ -11,10 +11,11 @@ namespace {
 // Sums the partial results of items split between CTAs, sum_c 2^(m_c - m) (o_c, l_c) with m the
 // largest m_c, in CTA order, and writes their rows; also fills the rows of nodes past n_b with
 // zeros and -inf. At most one item begins in a CTA and goes on in the next: blocks x look at the
-// one that attention CTA x noted (SplitDesc), blocks y share its rows, four to a warp, so that the
-// four rows' reads are under way together. Bound by latency: its launch, which the attention's
-// registers keep from overlapping, and three dependent reads (a row a warp took 20 us where 150
-// items of 196 rows were split, four take 8).
+// one that attention CTA x noted (SplitDesc), blocks y share its rows and columns: a lane has 16
+// columns of a row, as the partials lie (four columns of a warp's 32 rows are 512 bytes in a row).
+// One pass, four contributors' reads under way at a time, the sums rescaled as their maximum grows.
+// Bound by latency: its launch, which the attention's registers keep from overlapping, and two
+// dependent reads (150 items of 196 rows: a row a warp took 20 us, this 8).
 constexpr int kJoinThreads = 128, kJoinWarps = kJoinThreads / 32;
 
 __device__ __forceinline__ void store_four(bf16_t* p, float a, float b, float c, float d, bool aligned) {

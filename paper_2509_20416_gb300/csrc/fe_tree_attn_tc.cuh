@@ -32,7 +32,7 @@
 // over the scores for their maximum. The probabilities then stay below 2^12, where floating point is
 // as precise as below 1, and sums over a long cache are far from overflow. (81 nodes over 131k e4m3
 // slots: 362 us with 2^8, 353 with 2^12, 354 with 2^16 or 2^24.) Sums and statistics are float32;
-// probabilities are rounded to bfloat16 for the second product, which costs 2^-9 of each at most and
+// probabilities are rounded to bfloat16 for the second product, which costs up to 2^-8 of each and
 // is what the 16-bit tensor path offers.
 // Values in slots that a row does not see meet a zero probability, but 0 x NaN is NaN: the loaders
 // zero the non-finite elements of nodes' value rows (and of what lies past the item's end) and flag
