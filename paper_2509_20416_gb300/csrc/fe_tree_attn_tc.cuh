@@ -60,7 +60,11 @@ constexpr float kRescale = 12.f;  // log2 of the growth of a row's maximum that 
 // Key tiles whose scales are at hand. A softmax still reads tile t's when the loaders may be at tile
 // t + 1 + kKeySlots (the other stream's products may be one tile further).
 constexpr int kTcScales = 8;
-using TcPlan = Plan<kAttnItemRows, kTcTile, true, 4, 6>;
+// What an item's start and finish cost, in tiles of 128 rows: 4, and 6 where the queries are split too
+// (e4m3, 32 x 49 nodes: 111 us with 4, 104 with 6, 105 with 8; bfloat16, 4096 causal tokens: 220 us
+// with 4, 224 with 6, 228 with 8).
+template <bool Q8>
+using TcPlan = Plan<kAttnItemRows, kTcTile, true, Q8 ? 6 : 4, 6>;
 
 // MT: 128-row query blocks a CTA must hold (1 when no item has more than 128 rows)
 template <int HD, bool Q8, int MT>
@@ -754,7 +758,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     // what takes long and needs nothing goes first: the schedule, and the tensor maps' descriptors
     PlanArgs pa = plan_args(a);
     bool bad = false;
-    SegmentWalk<TcPlan> walk;
+    SegmentWalk<TcPlan<Q8>> walk;
     if (warp == 14) walk.init(pa, blockIdx.x, gridDim.x, &bad);
     if (warp == 15 && lane < 3) {
         const CUtensorMap* map = lane == 0 ? &kmap : lane == 1 ? &vmap : &qmap;
