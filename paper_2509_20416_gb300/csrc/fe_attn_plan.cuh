@@ -46,11 +46,12 @@ __device__ __forceinline__ SeqLen seq_len(const PlanArgs& a, int b, bool* bad = 
 // ROWS rows an item, TN slots a tile; PAIR: an item of more than 128 rows costs two units a tile.
 // An item begins with OVER units that hold no tile: what starting and finishing it costs a CTA, in
 // units, so that a CTA with many short items does not end after one with few long ones. JOIN: about
-// how many tiles joining a split costs (one token over 199 float32 slots, 8 items of 4 tiles: 36 us
+// how many tiles joining a split costs. TAIL: what a tile that reaches into the nodes' slots costs an
+// item of two units a tile besides (masks, values to look through). (one token over 199 float32 slots, 8 items of 4 tiles: 36 us
 // whole, 20 split).
 // Units are counted in 32 bits (the launch refuses shapes that could pass 2^31): this runs once a
 // CTA before anything else can start, and short code is what it takes to be quick.
-template <int ROWS, int TN, bool PAIR, int OVER, int JOIN>
+template <int ROWS, int TN, bool PAIR, int OVER, int JOIN, int TAIL>
 struct Plan {
     static constexpr int kOver = OVER, kJoin = JOIN;
     __host__ __device__ __forceinline__ static int blocks(int rows) { return (rows + ROWS - 1) / ROWS; }
@@ -68,26 +69,39 @@ struct Plan {
     __device__ __forceinline__ static int head_units(const PlanArgs& a, SeqLen s) {
         const int rows = s.n * a.G, nb = blocks(rows);
         if (a.whole || nb == 0) return nb;
-        if (!a.causal)  // every block but the last is full
-            return nb * OVER + tiles(a, s, 0) * ((nb - 1) * weight(ROWS, 0) + weight(rows, nb - 1));
+        if (!a.causal) {  // every block but the last is full
+            const int full = weight(ROWS, 0), last = weight(rows, nb - 1), nt = tiles(a, s, 0);
+            return nb * OVER + nt * ((nb - 1) * full + last) + tail(s, nt) * ((nb - 1) * (full - 1) + last - 1);
+        }
         int u = nb * OVER;
 #pragma unroll 1
-        for (int m = 0; m < nb; ++m) u += tiles(a, s, m) * weight(rows, m);
+        for (int m = 0; m < nb; ++m) {
+            const int w = weight(rows, m), nt = tiles(a, s, m);
+            u += nt * w + tail(s, nt) * (w - 1);
+        }
         return u;
     }
+    // what the first t tiles' share in the nodes' slots costs besides, for an item of weight 2
+    __device__ __forceinline__ static int tail(SeqLen s, int t) { return TAIL ? TAIL * max(t - s.P / TN, 0) : 0; }
     // units of an item of nt tiles of weight w = 1 or 2; the unit where tile t starts
-    __device__ __forceinline__ static int units(const PlanArgs& a, int w, int nt) { return a.whole ? 1 : OVER + w * nt; }
-    __device__ __forceinline__ static int tile_unit(const PlanArgs& a, int s0, int w, int t) {
-        return a.whole ? s0 : s0 + OVER + w * t;
+    __device__ __forceinline__ static int units(const PlanArgs& a, SeqLen s, int w, int nt) {
+        return a.whole ? 1 : OVER + w * nt + tail(s, nt) * (w - 1);
+    }
+    __device__ __forceinline__ static int tile_unit(const PlanArgs& a, SeqLen s, int s0, int w, int t) {
+        return a.whole ? s0 : s0 + OVER + w * t + tail(s, t) * (w - 1);
     }
     // first tile of an item with first unit s0 that starts at unit u0 or later
-    __device__ __forceinline__ static int first_tile(const PlanArgs& a, int s0, int w, int nt, int u0) {
+    __device__ __forceinline__ static int first_tile(const PlanArgs& a, SeqLen s, int s0, int w, int nt, int u0) {
         if (a.whole) return u0 <= s0 ? 0 : nt;
-        return u0 <= s0 + OVER ? 0 : min((u0 - s0 - OVER + w - 1) >> (w - 1), nt);
+        const int d = u0 - s0 - OVER, tp = s.P / TN;
+        if (d <= 0) return 0;
+        int t = (d + w - 1) >> (w - 1);
+        if (TAIL && w == 2 && t > tp) t = tp + (d - 2 * tp + 1 + TAIL) / (2 + TAIL);
+        return min(t, nt);
     }
     // whether every call of this shape keeps its units within 32 bits
     static bool fits(int B, int Hkv, int64_t rows, int max_seq) {
-        const double u = 2.0 * B * Hkv * (double)((rows + ROWS - 1) / ROWS) * (double)(max_seq / TN + 1 + OVER);
+        const double u = (2.0 + TAIL) * B * Hkv * (double)((rows + ROWS - 1) / ROWS) * (double)(max_seq / TN + 1 + OVER);
         return u < 2147483647.0;
     }
 };
@@ -184,7 +198,7 @@ struct Place {
         // the block of the head
 #pragma unroll 1
         while (true) {
-            const int w = PL::units(a, PL::weight(p.s.n * a.G, p.m), PL::tiles(a, p.s, p.m));
+            const int w = PL::units(a, p.s, PL::weight(p.s.n * a.G, p.m), PL::tiles(a, p.s, p.m));
             if (p.s0 + w > u0) return p;
             p.s0 += w;
             ++p.m;
@@ -219,12 +233,12 @@ struct SegmentWalk {
         d.has0 = continues;
         d.last = -1;
         if (any && !g.whole && g.slot == 1) {  // an item begins here and goes on
-            const int nt = PL::tiles(a, g.s, g.m), w = g.weight, p = pos - PL::units(a, w, nt);  // (pos: past the item)
+            const int nt = PL::tiles(a, g.s, g.m), w = g.weight, p = pos - PL::units(a, g.s, w, nt);  // (pos: past the item)
             d.b = g.b;
             d.h = g.h;
             d.m = g.m;
             d.rows = g.rows;
-            d.last = cut.owner(PL::tile_unit(a, p, w, nt - 1));
+            d.last = cut.owner(PL::tile_unit(a, g.s, p, w, nt - 1));
         }
         return d;
     }
@@ -236,8 +250,8 @@ struct SegmentWalk {
             bool got = false;
             if (rows > 0) {
                 const int w = PL::weight(rows, m), nt = PL::tiles(a, s, m);
-                g.t0 = PL::first_tile(a, pos, w, nt, u0);
-                g.t1 = PL::first_tile(a, pos, w, nt, u1);
+                g.t0 = PL::first_tile(a, s, pos, w, nt, u0);
+                g.t1 = PL::first_tile(a, s, pos, w, nt, u1);
                 got = g.t0 < g.t1;
                 if (got) {
                     g.b = b;
@@ -250,7 +264,7 @@ struct SegmentWalk {
                     g.whole = g.t0 == 0 && g.t1 == nt;
                     g.slot = g.t0 == 0 ? 1 : 0;
                 }
-                pos += PL::units(a, w, nt);
+                pos += PL::units(a, s, w, nt);
             }
             if (++m >= PL::blocks(rows)) {
                 m = 0;

@@ -62,9 +62,11 @@ constexpr float kRescale = 12.f;  // log2 of the growth of a row's maximum that 
 constexpr int kTcScales = 8;
 // What an item's start and finish cost, in tiles of 128 rows: 4, and 6 where the queries are split too
 // (e4m3, 32 x 49 nodes: 111 us with 4, 104 with 6, 105 with 8; bfloat16, 4096 causal tokens: 220 us
-// with 4, 224 with 6, 228 with 8).
+// with 4, 224 with 6, 228 with 8). And what a tile with nodes costs two streams besides: half a tile's
+// time over bfloat16 (2 x 1021 causal tokens: 125 us without, 121 with), nothing over e4m3, whose
+// values all pass the loaders (139 us without, 141 with).
 template <bool Q8>
-using TcPlan = Plan<kAttnItemRows, kTcTile, true, Q8 ? 6 : 4, 6>;
+using TcPlan = Plan<kAttnItemRows, kTcTile, true, Q8 ? 6 : 4, 6, Q8 ? 0 : 1>;
 
 // MT: 128-row query blocks a CTA must hold (1 when no item has more than 128 rows)
 template <int HD, bool Q8, int MT>
