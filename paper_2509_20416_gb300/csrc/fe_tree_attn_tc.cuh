@@ -75,10 +75,11 @@ struct TcShape {
     static constexpr int kRawBytes = kTcTile * HD;       // e4m3 tile
     // tiles in flight: bfloat16 keys and values in one ring; e4m3 keys as they are, raw values, and
     // converted values in three
-    static constexpr int kSlots = Q8 ? 2 : MT == 1 ? 5 : 4;
+    static constexpr int kSlots = Q8 ? 2 : MT == 1 ? 6 : 5;
     static constexpr int kKeySlots = Q8 ? 3 : 0;
     static constexpr int kRawSlots = Q8 ? (MT == 1 ? 3 : 2) : 0;
-    static constexpr int kScaleBytes = Q8 ? kTcScales * kTcTile * 4 : 0;  // the key tiles' scales
+    // the key tiles' scales, and the query rows' [segment parity][block][row]
+    static constexpr int kScaleBytes = Q8 ? (kTcScales + 4) * kTcTile * 4 : 0;
     static constexpr int kThreads = 512;
     static constexpr int kReaders = 15;  // warps that read the segments
     static constexpr int kData = MT * kTileBytes + kSlots * kTileBytes + (kKeySlots + kRawSlots) * kRawBytes + kScaleBytes;
@@ -94,7 +95,6 @@ struct TcState {
     int abort;
     int odd[8];        // by segment: non-finite value elements were set aside
     float2 ml[2][128];  // the streams' (maximum, sum), for their join
-    float qs[2][2][128];  // e4m3: scales of the query rows [segment parity][block]
 };
 
 template <int HD, bool Q8, int MT>
@@ -319,31 +319,46 @@ __device__ __forceinline__ void load_key_tile(const void* base, const RowInfo& x
     }
 }
 
-// Zero the non-finite elements of a lane's own chunks of a value tile, in rows from `first` on.
+// Zero the non-finite elements of a lane's own chunks of a value tile, in rows from `first` on;
+// whether there were any. Looking comes first, by a short loop (exponent bits all ones carry into
+// the sign bit); the repair is rare.
 template <int HD>
-__device__ __forceinline__ bool scrub_tile(unsigned char* tile, int first, int w, int lane) {
+__device__ __noinline__ bool repair_tile(unsigned char* tile, int first, int w, int lane) {
     constexpr int CH = HD / 8, RP = 32 / CH;
     const int c = lane % CH;
     bool odd = false;
 #pragma unroll 1
-    for (int i = max(first - w * 32, 0) / RP; i < 32 / RP; ++i) {
+    for (int i = 0; i < 32 / RP; ++i) {
         const int r = w * 32 + i * RP + lane / CH;
-        uint4* d = reinterpret_cast<uint4*>(tile + (c >> 3) * 16384 + sw128_offset(r, c & 7));
-        const uint4 x = *d;
-        uint32_t u[4] = {x.x, x.y, x.z, x.w};
-        bool any = false;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) any |= (u[e] & 0x7F80u) == 0x7F80u || (u[e] & 0x7F800000u) == 0x7F800000u;
-        if (!any || r < first) continue;
-        odd = true;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if ((u[e] & 0x7F80u) == 0x7F80u) u[e] &= 0xffff0000u;
-            if ((u[e] & 0x7F800000u) == 0x7F800000u) u[e] &= 0x0000ffffu;
+        uint32_t* d = reinterpret_cast<uint32_t*>(tile + (c >> 3) * 16384 + sw128_offset(r, c & 7));
+#pragma unroll 1
+        for (int e = 0; e < 4 && r >= first; ++e) {
+            uint32_t u = d[e];
+            if ((u & 0x7F80u) == 0x7F80u) u &= 0xffff0000u;
+            if ((u & 0x7F800000u) == 0x7F800000u) u &= 0x0000ffffu;
+            if (u != d[e]) {
+                d[e] = u;
+                odd = true;
+            }
         }
-        *d = make_uint4(u[0], u[1], u[2], u[3]);
     }
     return odd;
+}
+template <int HD>
+__device__ __forceinline__ bool scrub_tile(unsigned char* tile, int first, int w, int lane) {
+    constexpr int CH = HD / 8, RP = 32 / CH;
+    const int c = lane % CH;
+    const unsigned char* src = tile + (c >> 3) * 16384;
+    uint32_t any = 0;
+#pragma unroll 4
+    for (int i = 0; i < 32 / RP; ++i) {
+        const uint4 x = *reinterpret_cast<const uint4*>(src + sw128_offset(w * 32 + i * RP + lane / CH, c & 7));
+        any |= (x.x & 0x7F807F80u) + 0x00800080u;
+        any |= (x.y & 0x7F807F80u) + 0x00800080u;
+        any |= (x.z & 0x7F807F80u) + 0x00800080u;
+        any |= (x.w & 0x7F807F80u) + 0x00800080u;
+    }
+    return (any & 0x80008000u) != 0 && repair_tile<HD>(tile, first, w, lane);
 }
 
 // Four e4m3 numbers to bfloat16, times 2^-120: their 7 magnitude bits are moved to where
@@ -754,6 +769,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     unsigned char* keyring = ring + S * TB;  // (e4m3)
     unsigned char* rawring = keyring + SH::kKeySlots * SH::kRawBytes;
     float* key_scales = (float*)(rawring + SH::kRawSlots * SH::kRawBytes);
+    float* query_scales = key_scales + kTcScales * kTcTile;
     TcState& st = *reinterpret_cast<TcState*>(qbuf + SH::kData);
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     griddep_launch_dependents();
@@ -1232,7 +1248,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             if constexpr (Q8) {
                 if (!wait(&st.qfull, n)) return false;
                 if (s.weight == 2 || gs == 0) {
-                    st.qs[n & 1][gs][wl * 32 + lane] = split_query_row<HD>(qbuf + gs * TB, wl * 32 + lane);
+                    query_scales[((n & 1) * 2 + gs) * 128 + wl * 32 + lane] = split_query_row<HD>(qbuf + gs * TB, wl * 32 + lane);
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&st.qready);
@@ -1282,7 +1298,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         }
                         tc_wait_st();
                     }
-                    softmax_row<HD, Q8>(ts, to, Q8 ? scale2 * st.qs[cur & 1][pair ? gs : 0][wl * 32 + lane] : scale2,
+                    softmax_row<HD, Q8>(ts, to, Q8 ? scale2 * query_scales[((cur & 1) * 2 + (pair ? gs : 0)) * 128 + wl * 32 + lane] : scale2,
                                         tt < 2 && (tt == 0 || !pair), key_scales + (ktile + tt) % kTcScales * kTcTile, m, sum);
                     tc_wait_st();
                 }
