@@ -39,11 +39,11 @@
 // the segment, whose epilogue then adds their terms to the rows that do see them.
 //
 // What bounds it (GB300, 128-wide heads): 32 sequences over 256 to 4096 bfloat16 slots, 8 KV heads,
-// 17 nodes x 4 heads: 66 us, 4.5 TB/s (pages of 16: 75); 49 x 4 rows: 90 us, 645 TFLOP/s. 81 nodes x
-// 64 heads over 131k slots: bfloat16 303 us, 1150 TFLOP/s; e4m3 353 us, 985 TFLOP/s. The long ones
+// 17 nodes x 4 heads: 67 us, 4.4 TB/s (pages of 16: 75); 49 x 4 rows: 87 us, 660 TFLOP/s. 81 nodes x
+// 64 heads over 131k slots: bfloat16 297 us, 1170 TFLOP/s; e4m3 351 us, 990 TFLOP/s. The long ones
 // are bound by a stream's chain, softmax (1300 clocks a tile, 1024 of them exponentials; with key
 // scales 2200 and more) after product after softmax, of which two are in flight; the products alone
-// need 2048 of the 3200 clocks that a tile pair takes. The short ones pay 7 us of start (schedule,
+// need 2048 of the 3150 clocks that a tile pair takes. The short ones pay 7 us of start (schedule,
 // first tile, cold instruction caches) and an epilogue of 2 us a share of an item.
 #pragma once
 
@@ -61,10 +61,11 @@ constexpr float kRescale = 12.f;  // log2 of the growth of a row's maximum that 
 // t + 1 + kKeySlots (the other stream's products may be one tile further).
 constexpr int kTcScales = 8;
 // What an item's start and finish cost, in tiles of 128 rows: 4, and 6 where the queries are split too
-// (e4m3, 32 x 49 nodes: 111 us with 4, 104 with 6, 105 with 8; bfloat16, 4096 causal tokens: 220 us
-// with 4, 224 with 6, 228 with 8). And what a tile with nodes costs two streams besides: half a tile's
-// time over bfloat16 (2 x 1021 causal tokens: 125 us without, 121 with), nothing over e4m3, whose
-// values all pass the loaders (139 us without, 141 with).
+// (e4m3, 32 x 49 nodes: 111 us with 4, 104 with 6, 105 with 8; bfloat16, 2 x 1021 causal tokens: 112
+// us with 4 or 5; 3 x 700: 69 us with 4, 71 with 5). And what a tile with nodes costs two streams
+// besides: half a tile's time over bfloat16 (3 x 700 causal tokens: 74 us without, 69 with; 4096 from
+// an empty cache: 169 without, 173 with), nothing over e4m3, whose values all pass the loaders (139
+// us without, 141 with, 2 x 1021 tokens).
 template <bool Q8>
 using TcPlan = Plan<kAttnItemRows, kTcTile, true, Q8 ? 6 : 4, 6, Q8 ? 0 : 1>;
 
