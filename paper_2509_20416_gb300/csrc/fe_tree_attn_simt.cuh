@@ -7,11 +7,13 @@
 // running maximum and sum, and the outputs stay in registers; keys, values and the tile's
 // probabilities pass through shared memory, padded so that the 16 rows a warp reads at once fall
 // into different banks. Meanwhile the next tile's rows arrive (cp.async) in a second buffer, or,
-// where two CTAs fit an SM only with one buffer, the other CTA works. With 64 rows bound by the
-// float32 units (8192 clocks a tile of 128-wide heads), with 16 by shared memory (4096) and latency.
+// where two CTAs fit an SM only with one buffer, the other CTA works. Products go two columns to an
+// instruction (packed float32 pairs). With 64 rows bound by shared memory: a tile of 128-wide heads
+// needs 8192 clocks of products and takes 22 thousand, as a warp gets its 16-byte operands at 4 clocks a load,
+// eight loads for 64 products of a thread; with 16 rows by the same and by latency.
 // Fewer rows take fewer operations and leave room for the second CTA: 32 sequences over 256 to 4096
 // slots, 128-wide heads, 16 rows an item: 467 us with 64 rows a CTA, 357 with 16; 36 rows (64 a CTA)
-// 655 us, 16 TFLOP/s. 64-wide heads, one CTA an SM or two: 402 or 320 us at 36 rows, 22 or 24 us for
+// 631 us, 16 TFLOP/s. 64-wide heads, one CTA an SM or two: 402 or 320 us at 36 rows, 22 or 24 us for
 // 16 short items.
 #pragma once
 
@@ -78,7 +80,8 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
             }
             sm.q[r][c] = x * scale2;
         }
-        float mx[NI], sum[NI], acc[NI][NC][4];
+        float mx[NI], sum[NI];
+        uint64_t acc[NI][NC][2];  // pairs of columns
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
             mx[i] = -INFINITY;
@@ -86,7 +89,7 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
 #pragma unroll
             for (int j = 0; j < NC; ++j)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
+                for (int k = 0; k < 2; ++k) acc[i][j][k] = 0;
         }
         for (int tile = g.t0; tile < g.t1; ++tile, buf ^= kTwo, par ^= 1) {
             if (kTwo && tile + 1 < g.t1) {
@@ -107,26 +110,28 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
             }
             __syncthreads();
             float s[NI][4];
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
-#pragma unroll 4
-            for (int c = 0; c < HD; c += 4) {
-                float4 q4[NI], k4[4];
-#pragma unroll
-                for (int i = 0; i < NI; ++i) q4[i] = *reinterpret_cast<const float4*>(&sm.q[ty + 16 * i][c]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const float4*>(&sm.k[buf][tx + 16 * j][c]);
+            {
+                uint64_t s2[NI][4];  // even and odd columns' sums
 #pragma unroll
                 for (int i = 0; i < NI; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s[i][j] = fmaf(q4[i].x, k4[j].x, s[i][j]);
-                        s[i][j] = fmaf(q4[i].y, k4[j].y, s[i][j]);
-                        s[i][j] = fmaf(q4[i].z, k4[j].z, s[i][j]);
-                        s[i][j] = fmaf(q4[i].w, k4[j].w, s[i][j]);
-                    }
+                    for (int j = 0; j < 4; ++j) s2[i][j] = 0;
+#pragma unroll 4
+                for (int c = 0; c < HD; c += 4) {
+                    ulonglong2 q4[NI], k4[4];
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) q4[i] = *reinterpret_cast<const ulonglong2*>(&sm.q[ty + 16 * i][c]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) k4[j] = *reinterpret_cast<const ulonglong2*>(&sm.k[buf][tx + 16 * j][c]);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s2[i][j] = fma_x2(q4[i].y, k4[j].y, fma_x2(q4[i].x, k4[j].x, s2[i][j]));
+                }
+#pragma unroll
+                for (int i = 0; i < NI; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[i][j] = low_f32(s2[i][j]) + high_f32(s2[i][j]);
             }
             const bool odd = sm.odd[par] != 0;
 #pragma unroll
@@ -160,7 +165,7 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
 #pragma unroll
                 for (int j = 0; j < NC; ++j)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[i][j][k] *= f;
+                    for (int k = 0; k < 2; ++k) acc[i][j][k] = mul_x2(acc[i][j][k], pair_f32(f));
             }
             __syncwarp();  // a row's probabilities come from its own half warp
             if (!odd) {
@@ -171,18 +176,16 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
                     for (int i = 0; i < NI; ++i) p4[i] = *reinterpret_cast<const float4*>(&sm.p[ty + 16 * i][c]);
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
-                        float4 v4[NC];
+                        ulonglong2 v4[NC];
 #pragma unroll
-                        for (int j = 0; j < NC; ++j) v4[j] = *reinterpret_cast<const float4*>(&sm.v[buf][c + u][tx * 4 + 64 * j]);
+                        for (int j = 0; j < NC; ++j) v4[j] = *reinterpret_cast<const ulonglong2*>(&sm.v[buf][c + u][tx * 4 + 64 * j]);
 #pragma unroll
                         for (int i = 0; i < NI; ++i) {
-                            const float p = u == 0 ? p4[i].x : u == 1 ? p4[i].y : u == 2 ? p4[i].z : p4[i].w;
+                            const uint64_t p = pair_f32(u == 0 ? p4[i].x : u == 1 ? p4[i].y : u == 2 ? p4[i].z : p4[i].w);
 #pragma unroll
                             for (int j = 0; j < NC; ++j) {
-                                acc[i][j][0] = fmaf(p, v4[j].x, acc[i][j][0]);
-                                acc[i][j][1] = fmaf(p, v4[j].y, acc[i][j][1]);
-                                acc[i][j][2] = fmaf(p, v4[j].z, acc[i][j][2]);
-                                acc[i][j][3] = fmaf(p, v4[j].w, acc[i][j][3]);
+                                acc[i][j][0] = fma_x2(p, v4[j].x, acc[i][j][0]);
+                                acc[i][j][1] = fma_x2(p, v4[j].y, acc[i][j][1]);
                             }
                         }
                     }
@@ -196,7 +199,8 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
 #pragma unroll
                         for (int j = 0; j < NC; ++j)
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) acc[i][j][k] = fmaf(p, sm.v[buf][c][tx * 4 + 64 * j + k], acc[i][j][k]);
+                            for (int k = 0; k < 2; ++k)
+                                acc[i][j][k] = fma_x2(pair_f32(p), *reinterpret_cast<const uint64_t*>(&sm.v[buf][c][tx * 4 + 64 * j + 2 * k]), acc[i][j][k]);
                     }
             }
             __syncthreads();  // this buffer's (and p's) readers are done
@@ -214,7 +218,7 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
                 for (int j = 0; j < NC; ++j)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        o[tx * 4 + 64 * j + k] = sum[i] == 0.f ? 0.f : acc[i][j][k] * inv;
+                        o[tx * 4 + 64 * j + k] = sum[i] == 0.f ? 0.f : (k & 1 ? high_f32(acc[i][j][k / 2]) : low_f32(acc[i][j][k / 2])) * inv;
                 if (a.lse && tx == 0)
                     a.lse[((int64_t)g.b * a.T + node) * a.H + head] =
                         sum[i] == 0.f ? -INFINITY : mx[i] * 0.6931471805599453f + logf(sum[i]);
@@ -223,7 +227,7 @@ __global__ void __launch_bounds__(kSimtThreads, SimtSmem<HD, NI>::kCtas) tree_at
 #pragma unroll
                 for (int j = 0; j < NC; ++j)
                     *reinterpret_cast<float4*>(a.part_o + (pr - r) * HD + ((tx + 16 * j) * a.part_rows + r) * 4) =
-                        make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+                        make_float4(low_f32(acc[i][j][0]), high_f32(acc[i][j][0]), low_f32(acc[i][j][1]), high_f32(acc[i][j][1]));
                 if (tx == 0) {
                     a.part_ml[2 * pr] = mx[i];
                     a.part_ml[2 * pr + 1] = sum[i];
