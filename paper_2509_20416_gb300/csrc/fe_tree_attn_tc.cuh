@@ -40,7 +40,7 @@
 //
 // What bounds it (GB300, 128-wide heads): 32 sequences over 256 to 4096 bfloat16 slots, 8 KV heads,
 // 17 nodes x 4 heads: 67 us, 4.4 TB/s (pages of 16: 75); 49 x 4 rows: 87 us, 660 TFLOP/s. 81 nodes x
-// 64 heads over 131k slots: bfloat16 297 us, 1170 TFLOP/s; e4m3 351 us, 990 TFLOP/s. The long ones
+// 64 heads over 131k slots: bfloat16 297 us, 1170 TFLOP/s; e4m3 356 us, 977 TFLOP/s. The long ones
 // are bound by a stream's chain, softmax (1300 clocks a tile, 1024 of them exponentials; with key
 // scales 2200 and more) after product after softmax, of which two are in flight; the products alone
 // need 2048 of the 3150 clocks that a tile pair takes. The short ones pay 7 us of start (schedule,
@@ -1254,6 +1254,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             const int node = row / a.G;
             const bool live = row < g.rows;
             const bool idle = row - lane >= g.rows;  // the whole warp
+            const float* qscale = query_scales + ((cur & 1) * 2 + (pair ? gs : 0)) * 128 + wl * 32 + lane;
             float m = -INFINITY, sum = 0.f;  // reference maximum (log2 units), sum of 2^(s - m)
 #pragma unroll 1
             for (int tt = pair ? 0 : gs; tt < nt; tt += pair ? 1 : 2) {
@@ -1281,7 +1282,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         }
                         tc_wait_st();
                     }
-                    softmax_row<HD, Q8>(ts, to, Q8 ? scale2 * query_scales[((cur & 1) * 2 + (pair ? gs : 0)) * 128 + wl * 32 + lane] : scale2,
+                    softmax_row<HD, Q8>(ts, to, Q8 ? scale2 * *qscale : scale2,
                                         tt < 2 && (tt == 0 || !pair), key_scales + (ktile + tt) % kTcScales * kTcTile, m, sum);
                     tc_wait_st();
                 }
