@@ -525,9 +525,12 @@ __device__ __forceinline__ float max32(const uint32_t* x) {
 }
 
 // The rows of a warp move to references grown by log2(1 / f): the np packed columns of probabilities
-// written so far at ts and the no columns of O at `to` times f. (Rare, hence a call.)
+// written so far at ts and the no columns of O at `to` times f. (Rare, hence a call.) TMEM loads are
+// not ordered behind stores without a wait, and both may just have been stored: the probabilities by
+// the softmax's last step, and everything by a rescaling one step earlier.
 __device__ __noinline__ void rescale_row(uint32_t ts, int np, uint32_t to, int no, float f) {
     uint32_t u[16];
+    tc_wait_st();
 #pragma unroll 1
     for (int k = 0; k < np; k += 16) {
         tc_ld16_start(ts + k, u);
