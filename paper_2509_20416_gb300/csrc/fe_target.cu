@@ -127,6 +127,7 @@ fe_status build(fe_target* t, cudaStream_t st) {
     FE_TRY(cudaMalloc((void**)&t->status, sizeof(int)));
     FE_TRY(cudaMalloc((void**)&t->split, (size_t)t->num_sms * kAttnCtasPerSm * sizeof(SplitDesc)));
     FE_TRY(cudaMemsetAsync(t->status, 0, sizeof(int), st));
+    FE_TRY(cudaMemsetAsync(t->split, 0, (size_t)t->num_sms * kAttnCtasPerSm * sizeof(SplitDesc), st));
     double amplitude = 1.0;
     const std::vector<double> f = rope_freqs(c, &amplitude);
     double* df = nullptr;

@@ -763,6 +763,8 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     PlanArgs pa = plan_args(a);
     bool bad = false;
     SegmentWalk<TcPlan<Q8>> walk;
+    // (nothing to join, until the planner has come to its end: a CTA that gives up leaves no old note)
+    if (warp == 14 && lane == 0) a.split[blockIdx.x] = SplitDesc{0, 0, 0, 0, -1, 0, {0, 0}};
     if (warp == 14) walk.init(pa, blockIdx.x, gridDim.x, &bad);
     if (warp == 15 && lane < 3) {
         const CUtensorMap* map = lane == 0 ? &kmap : lane == 1 ? &vmap : &qmap;
