@@ -188,9 +188,10 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&w)[8]) {
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// A bounded wait (mbar_wait_abortable) whose slow part is one call, not a copy at every place.
+// A warp's bounded wait (mbar_wait_abortable) whose slow part is one call, not a copy at every place.
+// It has failed if it failed in any lane.
 __device__ __noinline__ bool tc_wait_slow(uint64_t* bar, uint32_t parity, int* status, int* abort) {
-    return mbar_wait_abortable(bar, parity, status, abort);
+    return __all_sync(0xffffffffu, mbar_wait_abortable(bar, parity, status, abort));
 }
 
 // The slots of [s0, s0 + 128) that node `node` sees, as bits (x: the first 64).
@@ -816,8 +817,10 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = st.tmem;
+    // Whole warps wait together and agree on the outcome: a warp of which some lanes gave up would not
+    // meet again at the warp-wide instructions that follow.
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-        return mbar_try_wait(bar, parity & 1u) || tc_wait_slow(bar, parity & 1u, a.status, &st.abort);
+        return __all_sync(0xffffffffu, mbar_try_wait(bar, parity & 1u)) || tc_wait_slow(bar, parity & 1u, a.status, &st.abort);
     };
     // the next planned segment; false at the end (or after a failed wait)
     uint32_t seg = 0;  // segments taken
