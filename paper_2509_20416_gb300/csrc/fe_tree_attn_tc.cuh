@@ -835,6 +835,9 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     };
     Segment g;
     bool ok = true;
+    // What a role that issues bulk copies has issued, for the wait at the end: where waits have failed,
+    // nobody else may have waited for the last of them.
+    uint32_t sent = 0;
 
     if (Q8 && warp >= 8 && warp < 12) {  // ---- loaders of an e4m3 cache: key scales, value conversion
         const int w = warp - 8, r = w * 32 + lane;  // the lane's row of every tile
@@ -1068,8 +1071,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 __syncwarp();
             }
         }
-        // (after a failed wait: leave with no copy in flight)
-        if (!ok && a.q_tma && n > 0) mbar_wait(&st.qfull, (n - 1) & 1u, a.status, 100000000LL);
+        sent = a.q_tma ? n : 0;
     } else if (Q8 && warp == 15) {  // ---- an e4m3 cache's keys (TMA) and raw values (bulk copies)
         RingPos<KS> kpos;
         RingPos<RS> pos;
@@ -1150,13 +1152,11 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         }
         // leave with no copy in flight: the last tiles have landed
         for (uint32_t j = i > (uint32_t)RS ? i - RS : 0; j < i; ++j) mbar_wait(&st.rawfull[j % RS], (j / RS) & 1u, a.status);
-        if (!ok && a.box_rows > 0)
-            for (uint32_t j = ktiles > (uint32_t)KS ? ktiles - KS : 0; j < ktiles; ++j)
-                mbar_wait(&st.kfull[j % KS], (j / KS) & 1u, a.status, 100000000LL);
+        sent = a.box_rows > 0 ? ktiles : 0;
     } else if (!Q8 && warp == 15) {  // ---- a bfloat16 cache's tiles by TMA
         RingPos<S> pos;
         bool reuse = false;
-        uint32_t sent = 0;  // by slot: used; from bit 8 its last use's phase; from bit 16: on landed[]
+        // (sent, by slot: used; from bit 8 its last use's phase; from bit 16: on landed[])
         uint32_t landed = 0;  // by slot: the phase of landed[] that comes next
         while (ok && a.box_rows > 0 && next(g)) {
             const int nt = g.t1 - g.t0;
@@ -1211,10 +1211,6 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             }
         }
         while (a.box_rows <= 0 && next(g)) {}
-        // (after a failed wait: leave with no copy in flight. Otherwise every tile has been used.)
-        if (!ok)
-            for (int k = 0; k < S; ++k)
-                if (sent >> k & 1u) mbar_wait(sent >> (16 + k) & 1u ? &st.landed[k] : &st.full[k], sent >> (8 + k) & 1u, a.status, 100000000LL);
     } else if (warp < 8) {  // ---- softmax
         const int gs = warp >> 2, wl = warp & 3;
         const uint32_t lanes = (uint32_t)(wl * 32) << 16;
@@ -1400,11 +1396,25 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                 mbar_arrive(&st.ofree);
             }
         }
+        cp_async_wait_all();
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     if (warp == 12) tc_dealloc(tmem, 512);
+    // Leave with no copy in flight. (Otherwise every copy has been waited for and used.)
+    if (*(volatile int*)&st.abort && sent) {
+        constexpr int64_t kLimit = 100000000;  // ns
+        if (warp == 14) {
+            mbar_wait(&st.qfull, (sent - 1) & 1u, a.status, kLimit);
+        } else if (Q8) {
+            for (uint32_t j = sent > (uint32_t)KS ? sent - KS : 0; j < sent; ++j)
+                mbar_wait(&st.kfull[j % KS], (j / KS) & 1u, a.status, kLimit);
+        } else {
+            for (int k = 0; k < S; ++k)
+                if (sent >> k & 1u) mbar_wait(sent >> (16 + k) & 1u ? &st.landed[k] : &st.full[k], sent >> (8 + k) & 1u, a.status, kLimit);
+        }
+    }
 }
 
 }  // namespace fe
