@@ -99,10 +99,10 @@ struct Plan {
         if (TAIL && w == 2 && t > tp) t = tp + (d - 2 * tp + 1 + TAIL) / (2 + TAIL);
         return min(t, nt);
     }
-    // whether every call of this shape keeps its units within 32 bits
-    static bool fits(int B, int Hkv, int64_t rows, int max_seq) {
-        const double u = (2.0 + TAIL) * B * Hkv * (double)((rows + ROWS - 1) / ROWS) * (double)(max_seq / TN + 1 + OVER);
-        return u < 2147483647.0;
+    // whether every call of T nodes with G heads to a KV head keeps its units within 32 bits
+    static bool fits(int B, int Hkv, int T, int G, int max_seq) {
+        const double items = (double)B * Hkv * (double)(((int64_t)T * G + ROWS - 1) / ROWS);
+        return items * (2.0 * (max_seq / TN + 1 + OVER) + TAIL * (T / TN + 2.0)) < 2147483647.0;
     }
 };
 
@@ -278,5 +278,26 @@ struct SegmentWalk {
         return false;
     }
 };
+
+// ---- the kernels' schedules ------------------------------------------------------------------
+constexpr int kTcTile = 128, kSimtTile = 64;
+
+// What an item's start and finish cost, in tiles of 128 rows: 4, and 6 where the queries are split too
+// (e4m3, 32 x 49 nodes: 111 us with 4, 104 with 6, 105 with 8; bfloat16, 2 x 1021 causal tokens: 112
+// us with 4 or 5; 3 x 700: 69 us with 4, 71 with 5). And what a tile with nodes costs two streams
+// besides: half a tile's time over bfloat16 (3 x 700 causal tokens: 74 us without, 69 with; 4096 from
+// an empty cache: 169 without, 173 with), nothing over e4m3, whose values all pass the loaders (139
+// us without, 141 with, 2 x 1021 tokens).
+template <bool Q8>
+using TcPlan = Plan<kAttnItemRows, kTcTile, true, Q8 ? 6 : 4, 6, Q8 ? 0 : 1>;
+// The float32 kernel's, of 16 NI rows an item.
+template <int NI>
+using SimtPlan = Plan<16 * NI, kSimtTile, false, 1, 2, 0>;
+
+// Whether the schedule that a call runs on can count the work of every call of its shape.
+inline bool attn_plan_fits(fe_dtype dtype, fe_dtype cache_dtype, int B, int Hkv, int T, int G, int max_seq) {
+    if (dtype == FE_F32) return SimtPlan<4>::fits(B, Hkv, T, G, max_seq);  // (the variants of fewer rows hold all of an item's)
+    return cache_dtype == FE_E4M3 ? TcPlan<true>::fits(B, Hkv, T, G, max_seq) : TcPlan<false>::fits(B, Hkv, T, G, max_seq);
+}
 
 }  // namespace fe

@@ -329,7 +329,7 @@ fe_status fe_tree_attention(fe_target* t, const fe_tree_attention_args* a, void*
     r.status = t->status;
     r.q_vec = rows_on(16, a->q, es);
     r.out_vec = rows_on(32, a->out, es) ? 2 : rows_on(16, a->out, es);
-    if (!tree_attn_fits(r, c.dtype)) return FE_ERR_UNSUPPORTED;
+    if (!tree_attn_fits(r, c.dtype, c.cache_dtype)) return FE_ERR_UNSUPPORTED;
     FE_TRY(launch_tree_attn(r, c.dtype, c.cache_dtype, c.head_dim, t->num_sms, (cudaStream_t)stream));
     return FE_OK;
 }

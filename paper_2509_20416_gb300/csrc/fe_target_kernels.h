@@ -89,7 +89,7 @@ cudaError_t launch_cache_read(const ReadArgs& a, fe_dtype dtype, fe_dtype cache_
 cudaError_t launch_cache_keep(const KeepArgs& a, cudaStream_t st);
 cudaError_t tree_attn_prepare();
 // whether the schedule can count the work of every call of this shape
-bool tree_attn_fits(const TreeAttnArgs& a, fe_dtype dtype);
+bool tree_attn_fits(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype);
 cudaError_t launch_tree_attn(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int hd, int num_sms,
                              cudaStream_t st);
 

@@ -140,11 +140,8 @@ cudaError_t tree_attn_prepare() {
     return e != cudaSuccess ? e : prepare<128>();
 }
 
-bool tree_attn_fits(const TreeAttnArgs& a, fe_dtype dtype) {
-    const int64_t rows = (int64_t)a.T * a.G;
-    // (the float32 variants of fewer rows hold all of an item's)
-    return dtype == FE_F32 ? SimtPlan<4>::fits(a.B, a.Hkv, rows, a.cache.max_seq)
-                           : TcPlan<true>::fits(a.B, a.Hkv, rows, a.cache.max_seq);
+bool tree_attn_fits(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype) {
+    return attn_plan_fits(dtype, cache_dtype, a.B, a.Hkv, a.T, a.G, a.cache.max_seq);
 }
 
 cudaError_t launch_tree_attn(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int hd, int num_sms,

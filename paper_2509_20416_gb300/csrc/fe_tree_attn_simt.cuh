@@ -21,9 +21,7 @@
 
 namespace fe {
 
-constexpr int kSimtTile = 64, kSimtThreads = 256;
-template <int NI>
-using SimtPlan = Plan<16 * NI, kSimtTile, false, 1, 2, 0>;
+constexpr int kSimtThreads = 256;
 template <int HD, int NI>
 struct SimtSmem {
     static constexpr int kPad = HD + 4;

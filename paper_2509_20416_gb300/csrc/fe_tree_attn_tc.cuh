@@ -55,20 +55,10 @@
 
 namespace fe {
 
-constexpr int kTcTile = 128;
 constexpr float kRescale = 12.f;  // log2 of the growth of a row's maximum that its block is rescaled for
 // Key tiles whose scales are at hand. A softmax still reads tile t's when the loaders may be at tile
 // t + 1 + kKeySlots (the other stream's products may be one tile further).
 constexpr int kTcScales = 8;
-// What an item's start and finish cost, in tiles of 128 rows: 4, and 6 where the queries are split too
-// (e4m3, 32 x 49 nodes: 111 us with 4, 104 with 6, 105 with 8; bfloat16, 2 x 1021 causal tokens: 112
-// us with 4 or 5; 3 x 700: 69 us with 4, 71 with 5). And what a tile with nodes costs two streams
-// besides: half a tile's time over bfloat16 (3 x 700 causal tokens: 74 us without, 69 with; 4096 from
-// an empty cache: 169 without, 173 with), nothing over e4m3, whose values all pass the loaders (139
-// us without, 141 with, 2 x 1021 tokens).
-template <bool Q8>
-using TcPlan = Plan<kAttnItemRows, kTcTile, true, Q8 ? 6 : 4, 6, Q8 ? 0 : 1>;
-
 // MT: 128-row query blocks a CTA must hold (1 when no item has more than 128 rows)
 template <int HD, bool Q8, int MT>
 struct TcShape {
