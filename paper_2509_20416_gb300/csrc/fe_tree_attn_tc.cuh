@@ -620,9 +620,10 @@ __device__ __forceinline__ int tile_number(int l, int n) {
     return l == 0 ? 0 : l == 2 * n - 1 ? n - 1 : l & 1 ? (l + 1) / 2 : (l - 2) / 2;
 }
 
-// For a row that sees non-finite value elements (which the loaders set to zero): the result in
-// their columns is the sum of p times them alone, since what is finite does not change an infinity
-// or NaN. dst: the row's place in the output (bfloat16) or the partial results (float32).
+// For a row that sees non-finite value elements of nodes (which the loaders set to zero): the sum of
+// p times them is added to the result in their columns. That may hold an infinity or NaN of the
+// prefix already; what is finite does not change one. dst: the row's place in the output (bfloat16)
+// or the partial results (float32), where this thread has just written the rest.
 template <int HD, bool Q8>
 __device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segment& g, int node, int head, float m, void* dst, int e0,
                                              int e1) {
@@ -648,8 +649,8 @@ __device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segmen
             any = true;
         }
         if (!any) continue;
-        if (g.whole) store_one((bf16_t*)dst + e, t);
-        else ((float*)dst)[e / 4 * (4 * kAttnItemRows) + e % 4] = t;
+        if (g.whole) store_one((bf16_t*)dst + e, Storage<bf16_t>::load((const bf16_t*)dst, e) + t);
+        else ((float*)dst)[e / 4 * (4 * kAttnItemRows) + e % 4] += t;
     }
 }
 
@@ -1374,7 +1375,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                         a.lse[((int64_t)g.b * a.T + node) * a.H + head] =
                             sum == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(sum);
                 }
-                if (live && *(volatile int*)&st.odd[cur & 7])
+                if (live && !zero && *(volatile int*)&st.odd[cur & 7])
                     put_odd_columns<HD, Q8>(a, g, node, head, m, g.whole ? (void*)dst : (void*)part, join && gs ? HD / 2 : 0, join && !gs ? HD / 2 : HD);
             }
             tc_fence_before();

@@ -109,3 +109,63 @@ def test_join_stays_within_the_grid(join):
         size = (w[..., None] * o.abs()).sum(0) / (w * l).sum(0)[:, None]
         assert ((out[:, 1].double() - want).abs() <= 2.0 ** -19 * size).all()
         assert ((lse[:, 1].double() - (m.amax(0) * math.log(2) + torch.log((w * l).sum(0)))).abs() <= 2.0 ** -19).all()
+
+
+def classes(x):
+    """0 finite, 1 NaN, 2 +inf, 3 -inf."""
+    return torch.isnan(x) * 1 + (x == math.inf) * 2 + (x == -math.inf) * 3
+
+
+def check_classes(c, store, q, P, n, mask, out, lse):
+    """Outputs and log-sum-exps are finite, NaN, +inf or -inf exactly where the 64-bit form's are."""
+    H, Hkv, hd = c["n_heads"], c["n_kv_heads"], c["head_dim"]
+    G = H // Hkv
+    for b in range(q.shape[0]):
+        nb, Pb = int(n[b]), int(P[b])
+        see = torch.ones(nb, Pb + nb, dtype=torch.bool, device="cuda")
+        see[:, Pb:] = (mask[b, :nb, :nb].cuda() != 0) if mask is not None else torch.ones(nb, nb, device="cuda").tril().bool()
+        for h in range(Hkv):
+            k, v = ref.cache_rows(c, store, 0, b, h, Pb + nb)
+            for gq in range(G):
+                o, l, _, _ = ref.attend(q[b, :nb, h * G + gq], k, v, see, 1 / math.sqrt(hd))
+                assert torch.equal(classes(out[b, :nb, h * G + gq]), classes(o)), (b, h, gq)
+                assert torch.equal(classes(lse[b, :nb, h * G + gq]), classes(l)), (b, h, gq)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("T,P", [(9, [40, 90]), (40, [100, 300]), (70, [3000]), (140, [10, 700])])
+def test_infinities_of_prefix_and_nodes_meet(fe, dtype, cache, T, P):
+    """Values of +inf, -inf and NaN in the prefix and in nodes that some nodes see, in the same column
+    and in different ones: opposite infinities and NaN give NaN, alone they stay what they are."""
+    B, H, Hkv, hd = len(P), 4, 2, 128
+    c = ref.config(dtype=dtype, cache_dtype=cache, n_heads=H, n_kv_heads=Hkv, head_dim=hd, max_batch=B, max_seq=max(P) + T + 1)
+    t = fe.fe_target_init(c)
+    g = gen(T)
+    store = ref.random_cache(fe, t, c, g)
+    inf, nan = (math.inf, math.nan) if cache != "e4m3" else (math.nan, math.nan)
+    near, far = [p - 1 for p in P], [p // 7 for p in P]  # prefix slots: the nodes' tile as a rule, and an early one
+    for b in range(B):
+        v = store.v[0, b]
+        # columns: prefix alone (0-3), nodes alone (8-10), both (16-23)
+        for h in range(Hkv):
+            for col, slot, x in ((0, near[b], inf), (1, far[b], -inf), (2, near[b], nan), (3, far[b], nan),
+                                 (8, P[b] + 1, inf), (9, P[b] + 3, -inf), (10, P[b] + 4, nan),
+                                 (16, near[b], inf), (16, P[b] + 1, -inf), (17, far[b], inf), (17, P[b] + 3, -inf),
+                                 (18, near[b], nan), (18, P[b] + 1, -inf), (19, far[b], -inf), (19, P[b] + 1, -inf),
+                                 (20, far[b], nan), (20, P[b] + 4, inf), (21, P[b] + 1, inf), (21, P[b] + 3, -inf),
+                                 (22, near[b], inf), (22, P[b] + 4, nan), (23, near[b], inf), (23, P[b] + 3, inf)):
+                v[h, slot, col + 64 * h] = x
+    # every second node sees node 1, every third node 3, every fifth node 4
+    mask = torch.zeros(B, T, T, dtype=torch.uint8)
+    i = torch.arange(T)
+    for node, every in ((1, 2), (3, 3), (4, 5)):
+        mask[:, i % every == 0, node] = 1
+    mask[:, i, i] |= torch.tensor([0 if j in (1, 3, 4) else 1 for j in range(T)], dtype=torch.uint8)
+    # scores stay small: no probability rounds to zero
+    q = (0.3 * torch.randn(B, T, H, hd, generator=g)).to(ref.DT[dtype]).cuda()
+    plen = torch.tensor(P, dtype=torch.int32)
+    out, lse = fe.fe_tree_attention(t, store, 0, q, plen.cuda(), mask=mask.cuda())
+    assert fe.fe_target_status(t) == fe.FE_OK
+    assert torch.isnan(out).any() and (cache == "e4m3" or torch.isinf(out).any())
+    check_classes(c, store, q, P, [T] * B, mask, out, lse)
+    check_attention(c, store, None, q, plen, torch.tensor([T] * B), mask, out, lse)
