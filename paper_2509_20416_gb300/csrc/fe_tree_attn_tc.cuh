@@ -620,35 +620,96 @@ __device__ __forceinline__ int tile_number(int l, int n) {
     return l == 0 ? 0 : l == 2 * n - 1 ? n - 1 : l & 1 ? (l + 1) / 2 : (l - 2) / 2;
 }
 
-// For a row that sees non-finite value elements of nodes (which the loaders set to zero): the sum of
-// p times them is added to the result in their columns. That may hold an infinity or NaN of the
-// prefix already; what is finite does not change one. dst: the row's place in the output (bfloat16)
-// or the partial results (float32), where this thread has just written the rest.
+// Whether 16 bytes of a cache row hold an infinity or NaN; element e of them: 0 finite, 1 NaN, 2 +inf, 3 -inf
+template <bool Q8>
+__device__ __forceinline__ bool odd_chunk(uint4 u) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint32_t any = 0;  // (a NaN code's low bits, or an exponent of ones, carry into the bit above)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) any |= Q8 ? (w[k] & 0x7F7F7F7Fu) + 0x01010101u : ((w[k] & 0x7F807F80u) + 0x00800080u);
+    return (any & 0x80808080u) != 0 && (Q8 || (any & 0x80008000u) != 0);
+}
+template <bool Q8>
+__device__ __forceinline__ int odd_kind(uint4 u, int e) {
+    const int k = Q8 ? e >> 2 : e >> 1;
+    const uint32_t w = k == 0 ? u.x : k == 1 ? u.y : k == 2 ? u.z : u.w;
+    if (Q8) return (w >> (8 * (e & 3)) & 0x7Fu) == 0x7Fu ? 1 : 0;
+    const uint32_t x = w >> (16 * (e & 1)) & 0xFFFFu;
+    return (x & 0x7F80u) != 0x7F80u ? 0 : x & 0x7Fu ? 1 : x & 0x8000u ? 3 : 2;
+}
+
+// For a row that sees non-finite value elements of nodes (which the loaders set to zero): they are
+// added to the result in their columns, which become that infinity, or NaN where a NaN, infinities
+// of both signs or a probability of exactly zero (a score of -inf) are among them. What they are
+// multiplied by does not matter otherwise, so the values are only looked through, each once a row
+// and until all columns are NaN: this takes about as long as the row's nodes have value bytes, and a
+// prompt whose values are all NaN keeps no other role waiting. The result may hold an infinity or
+// NaN of the prefix already. dst: the row's place in the output (bfloat16) or the partial results
+// (float32), where this thread has just written the rest.
 template <int HD, bool Q8>
-__device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segment& g, int node, int head, float m, void* dst, int e0,
-                                             int e1) {
+__device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segment& g, int node, int head, void* dst, int e0, int e1) {
+    constexpr int E = Q8 ? 16 : 8, CH = HD / E;          // elements of 16 bytes, chunks of a row
+    constexpr int AT = CH / 2 < 4 ? CH / 2 : 4;  // chunks loaded at a time (of half a row or all of it)
     const bf16_t* q = (const bf16_t*)a.q.p + g.b * a.q.batch + (int64_t)node * a.q.token + (int64_t)head * a.q.head;
+    unsigned long long kind[3][2] = {{0, 0}, {0, 0}, {0, 0}};  // columns with a NaN, a +inf, a -inf
+    // a score of -inf takes an infinity in the key or the query (e4m3 makes NaN of either)
+    int odd_q = -1;
+    auto minus_inf = [&](int64_t row) -> bool {
+        if (Q8) return false;
+        const uint4* k = reinterpret_cast<const uint4*>(a.cache.k) + row * CH;
+        bool odd = false;
+#pragma unroll 4
+        for (int c = 0; c < CH; ++c) odd |= odd_chunk<Q8>(k[c]);
+        if (odd_q < 0) {
+            odd_q = 0;
+#pragma unroll 1
+            for (int e = 0; e < HD; ++e) odd_q |= !finite_f32(Storage<bf16_t>::load(q, e));
+        }
+        if (!odd && !odd_q) return false;
+        float dot = 0.f;
+#pragma unroll 1
+        for (int e = 0; e < HD; ++e) dot = fmaf(Storage<bf16_t>::load(q, e), Storage<bf16_t>::load((const bf16_t*)k, e), dot);
+        return dot == -INFINITY;
+    };
+#pragma unroll 1
+    for (int tile = max(g.s.P / kTcTile, g.t0); tile < g.t1; ++tile) {
+        const int s0 = tile * kTcTile;
+        const ulonglong2 see = seen_bits(a, g, node, s0);
+#pragma unroll 1
+        for (int r = max(g.s.P - s0, 0); r < min(g.end - s0, kTcTile); ++r) {
+            if (!((r < 64 ? see.x >> r : see.y >> (r - 64)) & 1ull)) continue;
+            const RowInfo x = row_info<Q8>(a, g, tile, r);
+            if (x.row < 0) continue;
+            const uint4* v = reinterpret_cast<const uint4*>(a.cache.v) + x.row * CH;
+            int none = -1;  // the slot's probability is zero (-1: not looked at)
+#pragma unroll 1
+            for (int c = e0 / E; c < e1 / E; c += AT) {
+                uint4 u[AT];
+                bool odd = false;
+#pragma unroll
+                for (int k = 0; k < AT; ++k) u[k] = v[c + k];
+#pragma unroll
+                for (int k = 0; k < AT; ++k) odd |= odd_chunk<Q8>(u[k]);
+                if (!odd) continue;
+                if (none < 0) none = minus_inf(x.row);
+#pragma unroll
+                for (int i = 0; i < AT * E; ++i) {
+                    const int k = odd_kind<Q8>(u[i / E], i % E), e = c * E + i;
+                    if (k) kind[none ? 0 : k - 1][e >> 6] |= 1ull << (e & 63);
+                }
+            }
+            if (__popcll(kind[0][0]) + __popcll(kind[0][1]) == e1 - e0) {
+                tile = g.t1;
+                break;
+            }
+        }
+    }
 #pragma unroll 1
     for (int e = e0; e < e1; ++e) {
-        float t = 0.f;
-        bool any = false;
-#pragma unroll 1
-        for (int s = max(g.s.P, g.t0 * kTcTile); s < min(g.end, g.t1 * kTcTile); ++s) {
-            const RowInfo x = row_info<Q8>(a, g, s / kTcTile, s % kTcTile);
-            if (x.row < 0) continue;
-            auto at = [&](const void* p, float sc, int k) {
-                if (Q8) return e4m3x2_to_f32(((const uint8_t*)p)[x.row * HD + k]).x * sc;
-                return Storage<bf16_t>::load((const bf16_t*)p, x.row * HD + k);
-            };
-            const float v = at(a.cache.v, x.vs, e);
-            if (finite_f32(v) || !(seen_bits(a, g, node, s).x & 1ull)) continue;
-            float dot = 0.f;
-#pragma unroll 1
-            for (int k = 0; k < HD; ++k) dot = fmaf(Storage<bf16_t>::load(q, k), at(a.cache.k, x.ks, k), dot);
-            t += exp2f(dot * (a.scale * kLog2e) - (m == -INFINITY ? 0.f : m)) * v;
-            any = true;
-        }
-        if (!any) continue;
+        auto has = [&](int k) { return (kind[k][e >> 6] >> (e & 63) & 1ull) != 0; };
+        const bool nan = has(0), pos = has(1), neg = has(2);
+        if (!nan && !pos && !neg) continue;
+        const float t = nan || (pos && neg) ? __uint_as_float(0x7FC00000u) : pos ? INFINITY : -INFINITY;
         if (g.whole) store_one((bf16_t*)dst + e, Storage<bf16_t>::load((const bf16_t*)dst, e) + t);
         else ((float*)dst)[e / 4 * (4 * kAttnItemRows) + e % 4] += t;
     }
@@ -1376,7 +1437,7 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
                             sum == 0.f ? -INFINITY : m * 0.6931471805599453f + logf(sum);
                 }
                 if (live && !zero && *(volatile int*)&st.odd[cur & 7])
-                    put_odd_columns<HD, Q8>(a, g, node, head, m, g.whole ? (void*)dst : (void*)part, join && gs ? HD / 2 : 0, join && !gs ? HD / 2 : HD);
+                    put_odd_columns<HD, Q8>(a, g, node, head, g.whole ? (void*)dst : (void*)part, join && gs ? HD / 2 : 0, join && !gs ? HD / 2 : HD);
             }
             tc_fence_before();
             __syncwarp();

@@ -169,3 +169,49 @@ def test_infinities_of_prefix_and_nodes_meet(fe, dtype, cache, T, P):
     assert torch.isnan(out).any() and (cache == "e4m3" or torch.isinf(out).any())
     check_classes(c, store, q, P, [T] * B, mask, out, lse)
     check_attention(c, store, None, q, plen, torch.tensor([T] * B), mask, out, lse)
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_a_prompt_of_non_finite_values_takes_no_time(fe, dtype, cache, value):
+    """A chunk whose values are all NaN, or all infinite (NaN in an e4m3 cache): right by kind, and in
+    some milliseconds at most, far below the two seconds after which a wait inside the kernel runs
+    out. (A pass over all slots for each of a row's columns took half a second.)"""
+    T, P, H, hd = 600, 70, 2, 128
+    c = ref.config(dtype=dtype, cache_dtype=cache, n_heads=H, n_kv_heads=1, head_dim=hd, max_batch=1, max_seq=P + T)
+    t = fe.fe_target_init(c)
+    g = gen(T)
+    store = ref.random_cache(fe, t, c, g)
+    q = (0.3 * torch.randn(1, T, H, hd, generator=g)).to(ref.DT[dtype]).cuda()
+    plen = torch.tensor([P], dtype=torch.int32).cuda()
+    fe.fe_tree_attention(t, store, 0, q, plen)
+    store.v[0, 0, :, P:] = math.nan if cache == "e4m3" else value
+    store.v[0, 0, :, P + 100:P + 300, 5] = 1.0  # (finite, alone of their rows)
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    out, lse = fe.fe_tree_attention(t, store, 0, q, plen)
+    end.record()
+    assert fe.fe_target_status(t) == fe.FE_OK
+    check_classes(c, store, q, [P], [T], None, out, lse)
+    assert begin.elapsed_time(end) < 50.0
+
+
+@pytest.mark.parametrize("dtype,cache", [("f32", "f32"), ("bf16", "bf16")])
+def test_an_infinite_value_at_probability_zero(fe, dtype, cache):
+    """A node whose key makes a score of -inf has probability zero: its infinite values give NaN, as
+    zero times infinity does, and its finite ones nothing."""
+    T, P, hd = 33, 20, 64
+    c = ref.config(dtype=dtype, n_heads=2, n_kv_heads=1, head_dim=hd, max_batch=1, max_seq=P + T)
+    t = fe.fe_target_init(c)
+    g = gen(T)
+    store = ref.random_cache(fe, t, c, g)
+    q = (0.3 * torch.randn(1, T, 2, hd, generator=g)).abs().to(ref.DT[dtype]).cuda()
+    store.k[0, 0, 0, P + 3, 7] = -math.inf
+    store.v[0, 0, 0, P + 3, 1] = math.inf
+    store.v[0, 0, 0, P + 4, 2] = -math.inf
+    plen = torch.tensor([P], dtype=torch.int32)
+    out, lse = fe.fe_tree_attention(t, store, 0, q, plen.cuda())
+    assert fe.fe_target_status(t) == fe.FE_OK
+    assert torch.isnan(out[0, 3:, :, 1]).all() and (out[0, 4:, :, 2] == -math.inf).all()
+    check_classes(c, store, q, [P], [T], None, out, lse)
+    check_attention(c, store, None, q, plen, torch.tensor([T]), None, out, lse)
