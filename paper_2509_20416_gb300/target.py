@@ -4,7 +4,8 @@ key/value cache's write, read and accepted-row moves, and attention of a draft t
 As the rest of the package, these functions only marshal arguments. Row tensors (queries,
 keys, values, outputs) are CUDA tensors [B, T, heads, head_dim] of the handle's type with any
 strides whose innermost dimension is contiguous, such as views of a fused projection; integer
-inputs are contiguous CUDA int32 tensors.
+inputs are contiguous CUDA int32 tensors. `stream` (a torch stream or a raw handle) is where a call
+runs, the current stream unless given; ordering it with others is the caller's.
 """
 from __future__ import annotations
 
@@ -204,18 +205,40 @@ def _rows(t: Target, x, shape) -> tuple:
     return x.data_ptr(), s[0], s[1], s[2]
 
 
-def _call(name: str, t: Target, stream, tensors, *args) -> None:
-    """Pack the arguments and call the library. Memory that PyTorch's allocator hands out belongs
-    to the current stream: on another one, the allocator is told that `tensors` are in use there."""
-    if stream is None and _raw_stream is not None:
-        raw = _raw_stream(torch.cuda.current_device())
+def _side(stream):
+    """The stream of a call as PyTorch's object; None for the current stream."""
+    if stream is None:
+        return None
+    raw = _stream(stream)
+    if raw == torch.cuda.current_stream().cuda_stream:
+        return None
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
+
+
+def _empty(shape, dtype, device, side):
+    """A new output. Memory that PyTorch's allocator hands out belongs to a stream: kernels queued
+    there may still use it, and another stream must not write it yet. So an output is allocated on
+    the stream that writes it, and the current one, where the caller holds it, is noted as a user."""
+    if side is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(side):
+        x = torch.empty(shape, dtype=dtype, device=device)
+    x.record_stream(torch.cuda.current_stream())
+    return x
+
+
+def _call(name: str, t: Target, side, tensors, *args) -> None:
+    """Pack the arguments and call the library, on the current stream or on `side`: there, the
+    allocator is told that `tensors` are in use."""
+    if side is None:
+        raw = _raw_stream(torch.cuda.current_device()) if _raw_stream is not None else _stream(None)
     else:
-        raw = _stream(stream)
-        if stream is not None and raw != torch.cuda.current_stream().cuda_stream:
-            s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(raw)
-            for x in tensors():
-                if x is not None:
-                    x.record_stream(s)
+        raw = side.cuda_stream
+        for x in tensors():
+            if x is not None:
+                x.record_stream(side)
     code = getattr(_lib, name)(t.ptr, _PACK[name](*args), raw)
     if code:
         _check(code, name)
@@ -226,18 +249,19 @@ def fe_rope(t: Target, q, k, pos, backward: bool = False, q_out=None, k_out=None
     may be None) at pos [B, T]; with backward, the gradient's rotation. Returns (q_out, k_out);
     pass the inputs as outputs to rotate in place."""
     B, T = pos.shape
+    side = _side(stream)
     qr = kr = qo = ko = _NONE
     if q is not None:
         shape = (B, T, t.H, t.hd)
         qr = _rows(t, q, shape)
-        q_out = torch.empty(shape, dtype=t.dtype, device=q.device) if q_out is None else q_out
+        q_out = _empty(shape, t.dtype, q.device, side) if q_out is None else q_out
         qo = _rows(t, q_out, shape)
     if k is not None:
         shape = (B, T, t.Hkv, t.hd)
         kr = _rows(t, k, shape)
-        k_out = torch.empty(shape, dtype=t.dtype, device=k.device) if k_out is None else k_out
+        k_out = _empty(shape, t.dtype, k.device, side) if k_out is None else k_out
         ko = _rows(t, k_out, shape)
-    _call("fe_rope", t, stream, lambda: (q, k, q_out, k_out, pos), B, T, *qr, *kr, *qo, *ko, _ints(pos, (B, T)),
+    _call("fe_rope", t, side, lambda: (q, k, q_out, k_out, pos), B, T, *qr, *kr, *qo, *ko, _ints(pos, (B, T)),
           1 if backward else 0)
     return q_out, k_out
 
@@ -249,13 +273,14 @@ def fe_cache_write(t: Target, cache: Cache, layer: int, k, v, start, n_rows=None
     queries into q_out, which is returned."""
     B, T = k.shape[:2]
     shape = (B, T, t.Hkv, t.hd)
+    side = _side(stream)
     qr = qo = _NONE
     if q is not None:
         qshape = (B, T, t.H, t.hd)
         qr = _rows(t, q, qshape)
-        q_out = torch.empty(qshape, dtype=t.dtype, device=q.device) if q_out is None else q_out
+        q_out = _empty(qshape, t.dtype, q.device, side) if q_out is None else q_out
         qo = _rows(t, q_out, qshape)
-    _call("fe_cache_write", t, stream, lambda: (k, v, start, n_rows, pos, q, q_out, *cache.tensors()), B, T,
+    _call("fe_cache_write", t, side, lambda: (k, v, start, n_rows, pos, q, q_out, *cache.tensors()), B, T,
           *_rows(t, k, shape), *_rows(t, v, shape), *qr, *qo, _ints(pos, (B, T)), _ints(start, (B,)), _ints(n_rows, (B,)),
           *cache._layer(layer, B))
     return q_out
@@ -266,10 +291,11 @@ def fe_cache_read(t: Target, cache: Cache, layer: int, start, n_rows, L: int, k_
     """Slots start[b] .. start[b] + n_rows[b] - 1 of a layer's cache as rows k, v [B, L, Hkv, hd]
     of the handle's type; rows past n_rows[b] are zero."""
     B = start.shape[0]
+    side = _side(stream)
     shape = (B, L, t.Hkv, t.hd)
-    k_out = torch.empty(shape, dtype=t.dtype, device=start.device) if k_out is None else k_out
-    v_out = torch.empty(shape, dtype=t.dtype, device=start.device) if v_out is None else v_out
-    _call("fe_cache_read", t, stream, lambda: (start, n_rows, k_out, v_out, *cache.tensors()), B, L, _ints(start, (B,)),
+    k_out = _empty(shape, t.dtype, start.device, side) if k_out is None else k_out
+    v_out = _empty(shape, t.dtype, start.device, side) if v_out is None else v_out
+    _call("fe_cache_read", t, side, lambda: (start, n_rows, k_out, v_out, *cache.tensors()), B, L, _ints(start, (B,)),
           _ints(n_rows, (B,)), *cache._layer(layer, B), *_rows(t, k_out, shape), *_rows(t, v_out, shape))
     return k_out, v_out
 
@@ -283,16 +309,17 @@ def fe_tree_attention(t: Target, cache: Cache, layer: int, q, prefix_len, mask=N
     B, T = q.shape[:2]
     shape = (B, T, t.H, t.hd)
     qr = _rows(t, q, shape)
+    side = _side(stream)
     if out is None:
-        out = torch.empty(shape, dtype=t.dtype, device=q.device)
+        out = _empty(shape, t.dtype, q.device, side)
     if lse is None:
-        lse = torch.empty((B, T, t.H), dtype=torch.float32, device=q.device)
+        lse = _empty((B, T, t.H), torch.float32, q.device, side)
     elif lse.dtype != torch.float32 or lse.shape != (B, T, t.H) or not lse.is_contiguous() or not lse.is_cuda:
         raise ValueError(f"lse must be a contiguous float32 CUDA tensor of shape {(B, T, t.H)}")
     if mask is not None and (mask.dtype not in (torch.uint8, torch.bool) or mask.shape != (B, T, T)
                              or not mask.is_contiguous() or not mask.is_cuda):
         raise ValueError(f"mask must be a contiguous uint8 CUDA tensor of shape {(B, T, T)}")
-    _call("fe_tree_attention", t, stream, lambda: (q, prefix_len, n_nodes, mask, out, lse, *cache.tensors()), B, T, *qr,
+    _call("fe_tree_attention", t, side, lambda: (q, prefix_len, n_nodes, mask, out, lse, *cache.tensors()), B, T, *qr,
           *_rows(t, out, shape), lse.data_ptr(), _ints(prefix_len, (B,)), _ints(n_nodes, (B,)),
           0 if mask is None else mask.data_ptr(), t.scale if scale is None else float(scale), *cache._layer(layer, B))
     return out, lse
@@ -303,5 +330,5 @@ def fe_cache_keep(t: Target, cache: Cache, path, n_accept, start, stream=None) -
     start[b] + 1 + j in every layer of the cache (path [B, N], n_accept [B], start [B])."""
     B, N = path.shape
     cache._fits(B)
-    _call("fe_cache_keep", t, stream, lambda: (path, n_accept, start, *cache.tensors()), B, N, cache.n_layers,
+    _call("fe_cache_keep", t, _side(stream), lambda: (path, n_accept, start, *cache.tensors()), B, N, cache.n_layers,
           _ints(path, (B, N)), _ints(n_accept, (B,)), _ints(start, (B,)), ctypes.addressof(cache.kv), *cache.pages)

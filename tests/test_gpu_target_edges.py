@@ -215,3 +215,37 @@ def test_an_infinite_value_at_probability_zero(fe, dtype, cache):
     assert torch.isnan(out[0, 3:, :, 1]).all() and (out[0, 4:, :, 2] == -math.inf).all()
     check_classes(c, store, q, [P], [T], None, out, lse)
     check_attention(c, store, None, q, plen, torch.tensor([T]), None, out, lse)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("call", ["rope", "write", "read", "attention"])
+def test_new_outputs_on_another_stream_are_not_written_early(fe, call, handle):
+    """Memory just freed on the current stream, which kernels queued there still write, is not handed
+    out as the output of a call that runs at once on another stream."""
+    T, H, hd = 256, 64, 128
+    c = ref.config(n_heads=H, n_kv_heads=H, max_batch=1, max_seq=512)
+    t = fe.fe_target_init(c)
+    g = gen(1)
+    store = ref.random_cache(fe, t, c, g)
+    q, k = (torch.randn(1, T, H, hd, generator=g).bfloat16().cuda() for _ in range(2))
+    pos = torch.arange(T, dtype=torch.int32)[None].cuda()
+    zero, n = torch.zeros(1, dtype=torch.int32).cuda(), torch.full((1,), T, dtype=torch.int32).cuda()
+    run = {"rope": lambda **kw: fe.fe_rope(t, q, None, pos, **kw)[0],
+           "write": lambda **kw: fe.fe_cache_write(t, store, 0, k, k, zero, pos=pos, q=q, **kw),
+           "read": lambda **kw: fe.fe_cache_read(t, store, 0, zero, n, T, **kw)[0],
+           "attention": lambda **kw: fe.fe_tree_attention(t, store, 0, q, zero, **kw)[0]}[call]
+    want = run().clone()
+    other = torch.full_like(want, 3.0)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    freed = torch.empty_like(want)
+    torch.cuda._sleep(400_000_000)
+    freed.copy_(other)  # (runs after the pause)
+    del freed
+    got = run(stream=s.cuda_stream if handle else s)
+    s.synchronize()
+    assert not torch.cuda.current_stream().query()  # the pause is still going on
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    assert fe.fe_target_status(t) == fe.FE_OK
