@@ -223,10 +223,12 @@ fe_status fe_target_status(fe_target* t, void* stream) {
     const fe_status dv = check_device(t);
     if (dv != FE_OK) return dv;
     cudaStream_t st = (cudaStream_t)stream;
+    // (on `st` itself: the default stream is not ordered with it, so that a clear there could come after
+    // the next call's errors, and it may have long work of others queued)
     int v = 0;
+    FE_TRY(cudaMemcpyAsync(&v, t->status, sizeof(int), cudaMemcpyDeviceToHost, st));
+    FE_TRY(cudaMemsetAsync(t->status, 0, sizeof(int), st));
     FE_TRY(cudaStreamSynchronize(st));
-    FE_TRY(cudaMemcpy(&v, t->status, sizeof(int), cudaMemcpyDeviceToHost));
-    FE_TRY(cudaMemset(t->status, 0, sizeof(int)));
     if (v & ST_TIMEOUT) return FE_ERR_TIMEOUT;
     if (v & ST_CAPACITY) return FE_ERR_CAPACITY;
     if (v & ST_DEVICE) return FE_ERR_DEVICE;

@@ -249,3 +249,25 @@ def test_new_outputs_on_another_stream_are_not_written_early(fe, call, handle):
     torch.cuda.synchronize()
     assert torch.equal(got, want)
     assert fe.fe_target_status(t) == fe.FE_OK
+
+
+def test_status_is_read_and_cleared_on_its_own_stream(fe):
+    """fe_target_status(stream) neither waits for another stream's work, the default stream's
+    included, nor clears an error of a call that follows it on the same stream."""
+    c = ref.config(max_batch=1, max_seq=32)
+    t = fe.fe_target_init(c)
+    store = fe.alloc_cache(t, 1)
+    k = torch.zeros(1, 1, 2, 128, dtype=torch.bfloat16, device="cuda")
+    bad, good = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (99, 3))
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400_000_000)
+    fe.fe_cache_write(t, store, 0, k, k, bad, stream=s)
+    assert fe.fe_target_status(t, stream=s) == fe.FE_ERR_CAPACITY
+    for _ in range(20):
+        fe.fe_cache_write(t, store, 0, k, k, good, stream=s)
+        assert fe.fe_target_status(t, stream=s) == fe.FE_OK
+        fe.fe_cache_write(t, store, 0, k, k, bad, stream=s)
+        assert fe.fe_target_status(t, stream=s) == fe.FE_ERR_CAPACITY
+    assert not torch.cuda.current_stream().query()  # the default stream's pause is still going on
+    torch.cuda.synchronize()
