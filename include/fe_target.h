@@ -134,7 +134,8 @@ FE_API fe_status fe_rope(fe_target *t, const fe_rope_args *a, void *stream);
  *            float32: an FE_E4M3 cache rounds once), and, when q.p is set, q [B, T, H, hd] is
  *            rotated into q_out as by fe_rope (all T rows). Without pos the keys are stored as
  *            they are and q must be NULL.
- *  start     device [B] int32; n_rows device [B] int32 in 0..T, or NULL for T
+ *  start     device [B] int32; n_rows device [B] int32 in 0..T, or NULL for T. Rows from n_rows[b]
+ *            on are not looked at, their positions only for q
  * FE_E4M3: each row of a head gets the scale 2^c with the smallest c >= -120 for which no
  * finite element exceeds 448 times it, and each element / 2^c is rounded to e4m3 (ties to
  * even); a NaN or infinite element is stored as e4m3's NaN. Rows whose slot lies outside

@@ -144,15 +144,23 @@ __global__ void __launch_bounds__(kRowThreads, 3) rows_kernel(const __grid_const
     // the group's lanes of the warp: they take every branch below together
     const unsigned lanes = ((1u << GL) - 1u) << ((threadIdx.x & 31) / GL * GL);
 
+    const bool kv = CACHE && j >= (int)ja;
     int pos = 0;
+    if (a.pos) pos = a.pos[token];
+    if (kv) {  // (a row past n_rows[b] is none: its position may be anything)
+        const int n = a.n_rows ? a.n_rows[b] : a.T;
+        if (n < 0 || n > a.T) {
+            if (u == 0) atomicOr(a.status, ST_DEVICE);
+            return;
+        }
+        if (i >= n) return;
+    }
     if (a.pos) {
-        pos = a.pos[token];
         if (pos < 0 || pos >= a.rope.max_pos) {
             if (u == 0) atomicOr(a.status, ST_CAPACITY);
             return;
         }
     }
-    const bool kv = CACHE && j >= (int)ja;
     const ST* src[4];
     int64_t crow = 0;
     int h0, heads;  // the job's first head, of how many
@@ -160,12 +168,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) rows_kernel(const __grid_const
     if (kv) {
         h0 = 2 * (j - (int)ja);
         heads = a.HB;
-        const int n = a.n_rows ? a.n_rows[b] : a.T;
-        if (n < 0 || n > a.T) {
-            if (u == 0) atomicOr(a.status, ST_DEVICE);
-            return;
-        }
-        if (i >= n || !cache_row(a.cache, b, (int64_t)a.start[b] + i, crow, a.status)) return;
+        if (!cache_row(a.cache, b, (int64_t)a.start[b] + i, crow, a.status)) return;
         const ST* k = (const ST*)a.b_in.p + b * a.b_in.batch + i * a.b_in.token + h0 * a.b_in.head;
         const ST* v = (const ST*)a.v_in.p + b * a.v_in.batch + i * a.v_in.token + h0 * a.v_in.head;
         const bool two = h0 + 1 < heads;

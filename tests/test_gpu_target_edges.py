@@ -271,3 +271,27 @@ def test_status_is_read_and_cleared_on_its_own_stream(fe):
         assert fe.fe_target_status(t, stream=s) == fe.FE_ERR_CAPACITY
     assert not torch.cuda.current_stream().query()  # the default stream's pause is still going on
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+def test_positions_of_rows_that_are_not_written(fe, dtype, cache):
+    """Without queries, the positions of rows from n_rows[b] on (padding of ragged trees) may be
+    anything; a bad position of a row that is written is reported, and that row skipped."""
+    c = ref.config(dtype=dtype, cache_dtype=cache, max_batch=2, max_seq=64)
+    t = fe.fe_target_init(c)
+    store = fe.alloc_cache(t, 1)
+    k = torch.randn(2, 5, 2, 128, generator=gen(1)).to(ref.DT[dtype]).cuda()
+    start, n = torch.tensor([7, 20], dtype=torch.int32).cuda(), torch.tensor([2, 4], dtype=torch.int32).cuda()
+    pos = torch.tensor([[7, 8, -1, 64, 2**31 - 1], [20, 21, 22, 21, -9]], dtype=torch.int32).cuda()
+    fe.fe_cache_write(t, store, 0, k, k, start, n_rows=n, pos=pos)
+    assert fe.fe_target_status(t) == fe.FE_OK
+    written = (store.v[0].float() != 0).any(-1).nonzero().tolist()
+    assert written == [[0, h, s] for h in range(2) for s in (7, 8)] + [[1, h, s] for h in range(2) for s in (20, 21, 22, 23)]
+    store.v.zero_()
+    pos[0, 1] = -1
+    fe.fe_cache_write(t, store, 0, k, k, start, n_rows=n, pos=pos)
+    assert fe.fe_target_status(t) == fe.FE_ERR_CAPACITY
+    written = (store.v[0].float() != 0).any(-1).nonzero().tolist()
+    assert written == [[0, h, 7] for h in range(2)] + [[1, h, s] for h in range(2) for s in (20, 21, 22, 23)]
+    fe.fe_cache_write(t, store, 0, k, k, start, n_rows=torch.tensor([-1, 6], dtype=torch.int32).cuda(), pos=pos.clamp(0, 9))
+    assert fe.fe_target_status(t) == fe.FE_ERR_DEVICE
