@@ -5,7 +5,8 @@ As the rest of the package, these functions only marshal arguments. Row tensors 
 keys, values, outputs) are CUDA tensors [B, T, heads, head_dim] of the handle's type with any
 strides whose innermost dimension is contiguous, such as views of a fused projection; integer
 inputs are contiguous CUDA int32 tensors. `stream` (a torch stream or a raw handle) is where a call
-runs, the current stream unless given; ordering it with others is the caller's.
+runs, the current stream unless given; ordering it with others is the caller's. fe_rope takes part
+in autograd; the results of the cache and the attention over it, which serve, carry no graph.
 """
 from __future__ import annotations
 
@@ -247,7 +248,11 @@ def _call(name: str, t: Target, side, tensors, *args) -> None:
 def fe_rope(t: Target, q, k, pos, backward: bool = False, q_out=None, k_out=None, stream=None) -> tuple:
     """Rotary positions (include/fe_target.h) of q [B, T, H, hd] and k [B, T, Hkv, hd] (either
     may be None) at pos [B, T]; with backward, the gradient's rotation. Returns (q_out, k_out);
-    pass the inputs as outputs to rotate in place."""
+    pass the inputs as outputs to rotate in place. Where autograd records, new outputs on the
+    current stream are differentiable in q and k."""
+    if torch.is_grad_enabled() and q_out is None and k_out is None and _side(stream) is None \
+            and any(x is not None and x.requires_grad for x in (q, k)):
+        return _Rotation.apply(t, pos, backward, q, k)
     B, T = pos.shape
     side = _side(stream)
     qr = kr = qo = ko = _NONE
@@ -264,6 +269,25 @@ def fe_rope(t: Target, q, k, pos, backward: bool = False, q_out=None, k_out=None
     _call("fe_rope", t, side, lambda: (q, k, q_out, k_out, pos), B, T, *qr, *kr, *qo, *ko, _ints(pos, (B, T)),
           1 if backward else 0)
     return q_out, k_out
+
+
+class _Rotation(torch.autograd.Function):
+    """fe_rope under autograd: a rotation's gradient is its transpose."""
+
+    @staticmethod
+    def forward(ctx, t, pos, backward, q, k):
+        ctx.t, ctx.turn = t, backward
+        ctx.save_for_backward(pos)
+        ctx.set_materialize_grads(False)
+        return fe_rope(t, q, k, pos, backward)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        dq, dk = (x if x is None or x.stride(3) == 1 else x.contiguous()
+                  for x in (d if need else None for d, need in zip((dq, dk), ctx.needs_input_grad[3:])))
+        if dq is None and dk is None:
+            return None, None, None, None, None
+        return None, None, None, *fe_rope(ctx.t, dq, dk, *ctx.saved_tensors, not ctx.turn)
 
 
 def fe_cache_write(t: Target, cache: Cache, layer: int, k, v, start, n_rows=None, pos=None, q=None, q_out=None,

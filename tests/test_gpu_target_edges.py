@@ -295,3 +295,55 @@ def test_positions_of_rows_that_are_not_written(fe, dtype, cache):
     assert written == [[0, h, 7] for h in range(2)] + [[1, h, s] for h in range(2) for s in (20, 21, 22, 23)]
     fe.fe_cache_write(t, store, 0, k, k, start, n_rows=torch.tensor([-1, 6], dtype=torch.int32).cuda(), pos=pos.clamp(0, 9))
     assert fe.fe_target_status(t) == fe.FE_ERR_DEVICE
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout,scaling", [("half", "none"), ("interleaved", "yarn")])
+def test_rope_under_autograd(fe, dtype, layout, scaling):
+    """Rotations of tensors that require gradients are differentiable: the gradient is the transposed
+    rotation, checked against its 64-bit form (the bound of test_gpu_target.py: 4 * 2^-24 of amplitude
+    * (|a| + |b|), and u |y|) and, for float32, against differences. The map is linear, so a central
+    difference of sum(y g) has no error but its roundings: with x and x + d rounded to float32 and
+    sums in 64 bits, each y is off by 4 * 2^-24 (|a| + |b|) amp + 2^-24 |y| on either side."""
+    c = ref.config(dtype=dtype, rope_layout=layout, rope_scaling=scaling, rope_dim=96, rope_factor=4.0, rope_orig=128.0,
+                   rope_low=32.0, rope_high=1.0)
+    t = fe.fe_target_init(c)
+    g, u = gen(5), ref.UNIT[dtype]
+    B, T, dt = 2, 7, ref.DT[dtype]
+    leaf = [torch.randn(B, T, n, 128, generator=g).to(dt).cuda().requires_grad_() for n in (8, 2)]
+    pos = torch.randint(0, 512, (B, T), generator=g, dtype=torch.int32).cuda()
+    grads = [torch.randn(B, T, n, 128, generator=g).to(dt).cuda() for n in (8, 2)]
+    out = fe.fe_rope(t, *leaf, pos)
+    plain = fe.fe_rope(t, *(x.detach() for x in leaf), pos)
+    assert all(o.requires_grad and torch.equal(o, p) for o, p in zip(out, plain))
+    got = torch.autograd.grad(out, leaf, grads)
+    for x, d in zip(got, grads):
+        want, mag = ref.rotate(c, d, pos, backward=True)
+        assert ((x.double() - want).abs() <= 4 * 2.0 ** -24 * mag + u * want.abs()).all()
+    # one input alone; a gradient with strides of zero; the gradient's own gradient
+    k = leaf[1]
+    none, ko = fe.fe_rope(t, None, k, pos)
+    assert none is None
+    ones, _ = ref.rotate(c, torch.ones_like(k), pos, backward=True)
+    dk, = torch.autograd.grad(ko.sum(), k)
+    assert ((dk.double() - ones).abs() <= (8 * 2.0 ** -24 * 2 * 1.2 + u * ones.abs())).all()
+    w = grads[1].clone().requires_grad_()
+    dk, = torch.autograd.grad(fe.fe_rope(t, None, k, pos)[1], k, w, create_graph=True)
+    back, = torch.autograd.grad(dk, w, grads[1])
+    assert torch.equal(back, fe.fe_rope(t, None, grads[1], pos)[1])
+    # q's graph only: k stays outside it
+    qo, ko = fe.fe_rope(t, leaf[0], k.detach(), pos)
+    dq, = torch.autograd.grad(qo, leaf[0], grads[0])
+    assert torch.equal(dq, got[0])
+    with torch.no_grad():
+        assert not fe.fe_rope(t, *leaf, pos)[0].requires_grad
+    if dtype == "f32":
+        for x, d, dx, n in zip(leaf, grads, got, range(2)):
+            e = torch.randn(x.shape, generator=g).cuda()
+            a, b = (x + e).detach(), (x - e).detach()
+            ya, yb = (fe.fe_rope(t, *((z, None) if n == 0 else (None, z)), pos)[n] for z in (a, b))
+            diff = ((ya.double() - yb.double()) * d.double()).sum()
+            want = ((a.double() - b.double()) * dx.double()).sum()
+            tol = sum(((5 * 2.0 ** -24 * ref.rotate(c, z, pos)[1]) * d.double().abs()).sum() for z in (a, b)) \
+                + ((a - b).double().abs() * (5 * 2.0 ** -24 * ref.rotate(c, d, pos, backward=True)[1])).sum()
+            assert (diff - want).abs() <= tol
