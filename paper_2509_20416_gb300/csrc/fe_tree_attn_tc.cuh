@@ -180,9 +180,11 @@ __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sy
 
 // A warp's bounded wait (mbar_wait_abortable) whose slow part is one call, not a copy at every place.
 // It has failed if it failed in any lane.
-__device__ __noinline__ bool tc_wait_slow(uint64_t* bar, uint32_t parity, int* status, int* abort) {
-    return __all_sync(0xffffffffu, mbar_wait_abortable(bar, parity, status, abort));
+__device__ __noinline__ bool tc_wait_slow(uint64_t* bar, uint32_t parity, int* status, int* abort, int64_t budget_ns) {
+    return __all_sync(0xffffffffu, mbar_wait_abortable(bar, parity, status, abort, 0, budget_ns));
 }
+// What a wait is allowed besides, for each tile that it lasts: several times a tile's time.
+constexpr int64_t kTileBudgetNs = 20000;
 
 // The slots of [s0, s0 + 128) that node `node` sees, as bits (x: the first 64).
 __device__ __noinline__ ulonglong2 seen_bits(const TreeAttnArgs& a, const Segment& g, int node, int s0) {
@@ -871,8 +873,9 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
     const uint32_t tmem = st.tmem;
     // Whole warps wait together and agree on the outcome: a warp of which some lanes gave up would not
     // meet again at the warp-wide instructions that follow.
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-        return __all_sync(0xffffffffu, mbar_try_wait(bar, parity & 1u)) || tc_wait_slow(bar, parity & 1u, a.status, &st.abort);
+    auto wait = [&](uint64_t* bar, uint32_t parity, int tiles = 0) {
+        return __all_sync(0xffffffffu, mbar_try_wait(bar, parity & 1u)) ||
+               tc_wait_slow(bar, parity & 1u, a.status, &st.abort, kWaitBudgetNs + tiles * kTileBudgetNs);
     };
     // the next planned segment; false at the end (or after a failed wait)
     uint32_t seg = 0;  // segments taken
@@ -1094,14 +1097,16 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
         mbar_wait(&st.drain[gs], 0, a.status, 100000000LL);
     } else if (warp == 14) {  // ---- the plan
         if (bad && blockIdx.x == 0) atomicOr(a.status, ST_CAPACITY);
+        // It alone waits for as long as a whole segment takes, which may have two million tiles.
         uint32_t n = 0;
+        int longest = 0;  // tiles of a segment so far
         bool continues = false;
         for (; ok; ++n) {
             const bool more = walk.next(pa, g);
             continues |= more && !g.whole && g.slot == 0;
             if (!more && lane == 0) a.split[blockIdx.x] = walk.desc(pa, n > 0, g, continues);
             const int k = n % kTcSegs;
-            if (n >= kTcSegs && !(ok = wait(&st.segempty[k], n / kTcSegs - 1))) break;
+            if (n >= kTcSegs && !(ok = wait(&st.segempty[k], n / kTcSegs - 1, longest))) break;
             if (lane == 0) {
                 if (!more) g.weight = 0;
                 st.seg[k] = g;
@@ -1109,8 +1114,10 @@ __global__ void __launch_bounds__(TcShape<HD, Q8, MT>::kThreads, 1)
             }
             __syncwarp();
             if (!more) break;
+            const int before = longest;  // (of the segments that a wait here may last)
+            longest = max(longest, g.t1 - g.t0);
             if (a.q_tma) {  // the queries, once the buffer's last ones are done with
-                if (n > 0 && !(ok = wait(&st.qempty, n - 1))) break;
+                if (n > 0 && !(ok = wait(&st.qempty, n - 1, before))) break;
                 if (lane == 0) {
                     mbar_arrive_expect_tx(&st.qfull, g.weight * TB);
                     mbar_arrive_n(&st.qfull, 255);  // in the place of the softmax warps' 256 arrivals
