@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import target_ref as ref
-from test_gpu_target import check_attention, gen
+from test_gpu_target import check_attention, gen, tree_masks
 
 pytestmark = pytest.mark.gpu
 
@@ -347,3 +347,86 @@ def test_rope_under_autograd(fe, dtype, layout, scaling):
             tol = sum(((5 * 2.0 ** -24 * ref.rotate(c, z, pos)[1]) * d.double().abs()).sum() for z in (a, b)) \
                 + ((a - b).double().abs() * (5 * 2.0 ** -24 * ref.rotate(c, d, pos, backward=True)[1])).sum()
             assert (diff - want).abs() <= tol
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("page", [0, 16])
+def test_calls_captured_in_a_graph(fe, dtype, cache, page):
+    """A step's calls captured once and replayed on new inputs, lengths and counts give the bits of
+    direct calls."""
+    B, T, H, Hkv, hd = 3, 21, 8, 2, 128
+    c = ref.config(dtype=dtype, cache_dtype=cache, n_heads=H, n_kv_heads=Hkv, head_dim=hd, page_size=page, max_batch=B, max_seq=512)
+    t = fe.fe_target_init(c)
+    g = gen(page)
+    table, n_pages = ref.paged(c, B, g)
+    store, twin = (ref.random_cache(fe, t, c, gen(page + 1), layers=2, table=table, n_pages=n_pages) for _ in range(2))
+    qkv = torch.zeros(B, T, H + 2 * Hkv, hd, dtype=ref.DT[dtype], device="cuda")
+    q, k, v = qkv.split([H, Hkv, Hkv], 2)
+    ints = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    start, n, pos, path, acc = ints(B), ints(B), ints(B, T), ints(B, 3), ints(B)
+    mask = torch.zeros(B, T, T, dtype=torch.uint8, device="cuda")
+
+    def step(cache):
+        r = fe.fe_cache_write(t, cache, 1, k, v, start, n_rows=n, pos=pos, q=q)
+        out, lse = fe.fe_tree_attention(t, cache, 1, r, start, mask=mask, n_nodes=n)
+        fe.fe_cache_keep(t, cache, path, acc, start)
+        return r, out, lse, *fe.fe_cache_read(t, cache, 1, start, n, T)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(store)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(store)
+    for x in ("k", "v", "k_scale", "v_scale"):  # (the warm-up wrote a row)
+        if getattr(store, x) is not None:
+            getattr(store, x).view(torch.uint8).copy_(getattr(twin, x).view(torch.uint8))
+    for i in range(3):
+        P = torch.randint(0, 512 - T, (B,), generator=g, dtype=torch.int32)
+        for to, x in ((qkv, torch.randn(qkv.shape, generator=g)), (start, P), (n, torch.randint(4, T + 1, (B,), generator=g)),
+                      (pos, P[:, None] + torch.arange(T)), (mask, tree_masks(g, B, T)), (path, torch.tensor([[1, 2, 3]] * B)),
+                      (acc, torch.randint(0, 4, (B,), generator=g))):
+            to.copy_(x.to(to.dtype))
+        graph.replay()
+        want = step(twin)
+        assert fe.fe_target_status(t) == fe.FE_OK
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want)), i
+        assert torch.equal(store.k.view(torch.uint8), twin.k.view(torch.uint8))
+
+
+@pytest.mark.parametrize("size", [2.0 ** 5, 2.0 ** 10, 2.0 ** 14])
+@pytest.mark.parametrize("T", [6, 50])
+def test_queries_with_an_outlier_over_e4m3(fe, T, size):
+    """One element of a query row far above the rest, met by small key elements. Over e4m3 a query
+    element is exact down to 2^-10 of the scale 2^c, the smallest with the row's largest magnitude
+    below 448 times it, and off by 2^-10 2^c at most; a score by f = scale 2^-10 2^c sum |k|. So every
+    probability carries a relative error below e + exp(2 f) - 1 (e as in test_gpu_target.py), and the
+    log-sum-exp one of f."""
+    H, Hkv, hd, P = 4, 2, 128, 300
+    c = ref.config(cache_dtype="e4m3", n_heads=H, n_kv_heads=Hkv, head_dim=hd, max_batch=1, max_seq=P + T)
+    t = fe.fe_target_init(c)
+    g = gen(T)
+    store = ref.random_cache(fe, t, c, g)
+    for name in ("k", "v"):
+        x = torch.randn(Hkv, P + T, hd, generator=g)
+        if name == "k":
+            x[..., 77] *= 2.0 ** -8
+        fill(store, name, x, "e4m3")
+    q = torch.randn(1, T, H, hd, generator=g)
+    q[..., 77] = size * torch.sign(q[..., 77])
+    q = q.bfloat16().cuda()
+    scale = 1 / math.sqrt(hd)
+    out, lse = fe.fe_tree_attention(t, store, 0, q, torch.tensor([P], dtype=torch.int32).cuda())
+    assert fe.fe_target_status(t) == fe.FE_OK
+    see = torch.ones(T, P + T, device="cuda").tril(P).bool()
+    for h in range(Hkv):
+        k, v = ref.cache_rows(c, store, 0, 0, h, P + T)
+        for i in range(h * 2, h * 2 + 2):
+            o, l, mag, A = ref.attend(q[0, :, i], k, v, see, scale)
+            c2 = torch.ceil(torch.log2(q[0, :, i].double().abs().amax(-1) / 448))
+            f = scale * 2.0 ** -10 * torch.exp2(c2) * k.abs().sum(-1).amax()
+            e = 2 * (hd + 4) * 2.0 ** -24 * A + 2.0 ** -20
+            tol = ((e + torch.expm1(2 * f))[:, None] + 1.01 * 2.0 ** -8) * mag + 2.0 ** -8 * o.abs()
+            assert ((out[0, :, i].double() - o).abs() <= tol).all()
+            assert ((lse[0, :, i].double() - l).abs() <= e + f + 2.0 ** -23 * l.abs()).all()
