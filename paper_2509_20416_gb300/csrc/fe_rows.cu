@@ -305,9 +305,10 @@ __global__ void __launch_bounds__(kRowThreads) read_kernel(const __grid_constant
 // node each (its slot's and its new slot's cache rows: two page lookups side by side), then carry
 // 16-byte columns of the key and value rows along the path, layer after layer: since path is
 // increasing with path[j] >= j + 1, slot 1 + j is written only after the last read of it when the
-// moves go in order, so eight loads go before their eight stores. Bound by three dependent reads
-// (path, page table, rows); four layers a warp, where there are enough warps, share the first two.
-// 80 layers of one sequence: 5 us; 32 layers of 32 sequences, 7 rows each at most: 10 us.
+// moves go in order, so eight loads go before their eight stores. Bound by latency: three dependent
+// reads (path, page table, rows), and with four layers a warp, which where there are enough warps
+// share the first two, the layers' moves one after another. 80 layers of one sequence: 5 us; 32
+// layers of 32 sequences, 7 rows each at most: 10 us.
 __global__ void __launch_bounds__(kRowThreads) keep_kernel(const __grid_constant__ KeepArgs a) {
     const uint32_t w = blockIdx.x * (kRowThreads / 32) + threadIdx.x / 32;
     const int lane = threadIdx.x & 31;
@@ -419,9 +420,9 @@ cudaError_t launch_read_t(const ReadArgs& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_rope_table(float2* table, int max_seq, int pairs, const double* inv_freq, double amplitude,
-                              cudaStream_t st) {
+                              int num_sms, cudaStream_t st) {
     const int64_t n = (int64_t)max_seq * pairs;
-    const int blocks = (int)((n + 255) / 256 < 152 * 8 ? (n + 255) / 256 : 152 * 8);
+    const int blocks = (int)((n + 255) / 256 < num_sms * 8 ? (n + 255) / 256 : num_sms * 8);
     rope_table_kernel<<<blocks, 256, 0, st>>>(table, max_seq, pairs, inv_freq, amplitude);
     return cudaGetLastError();
 }
@@ -440,10 +441,10 @@ cudaError_t launch_cache_read(const ReadArgs& a, fe_dtype dtype, fe_dtype cache_
     return hd == 128 ? launch_read_t<bf16_t, 128, false>(a, st) : launch_read_t<bf16_t, 64, false>(a, st);
 }
 
-cudaError_t launch_cache_keep(const KeepArgs& args, cudaStream_t st) {
+cudaError_t launch_cache_keep(const KeepArgs& args, int num_sms, cudaStream_t st) {
     KeepArgs a = args;
     const int64_t one = (int64_t)a.n_layers * a.B * a.cache.Hkv;
-    a.layers_per_warp = one >= 152 * 32 ? 4 : 1;  // (half an SM's warps, at least, with one layer each)
+    a.layers_per_warp = one >= num_sms * 32 ? 4 : 1;  // (half an SM's warps, at least, with one layer each)
     const int64_t warps = (int64_t)((a.n_layers + a.layers_per_warp - 1) / a.layers_per_warp) * a.B * a.cache.Hkv;
     return launch_groups(keep_kernel, warps, kRowThreads / 32, a, st);
 }

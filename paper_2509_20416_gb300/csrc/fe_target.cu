@@ -133,7 +133,7 @@ fe_status build(fe_target* t, cudaStream_t st) {
     double* df = nullptr;
     FE_TRY(cudaMalloc((void**)&df, f.size() * sizeof(double)));
     cudaError_t e = cudaMemcpyAsync(df, f.data(), f.size() * sizeof(double), cudaMemcpyHostToDevice, st);
-    if (e == cudaSuccess) e = launch_rope_table(t->rope, c.max_seq, pairs, df, amplitude, st);
+    if (e == cudaSuccess) e = launch_rope_table(t->rope, c.max_seq, pairs, df, amplitude, t->num_sms, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     cudaFree(df);
     FE_TRY(e);
@@ -361,7 +361,7 @@ fe_status fe_cache_keep(fe_target* t, const fe_cache_keep_args* a, void* stream)
             r.layer[i] = a->caches[l0 + i];
             if (c.cache_dtype != FE_E4M3) r.layer[i].k_scale = r.layer[i].v_scale = nullptr;
         }
-        FE_TRY(launch_cache_keep(r, (cudaStream_t)stream));
+        FE_TRY(launch_cache_keep(r, t->num_sms, (cudaStream_t)stream));
     }
     return FE_OK;
 }

@@ -6,8 +6,6 @@
 
 namespace fe {
 
-struct e4m3_t { uint8_t bits; };
-
 // The row index of (sequence b, head 0, slot); the head's row is + h * head_step(). False for
 // a slot outside [0, max_seq) or a page id outside the pool.
 __device__ __forceinline__ bool cache_row(const CacheView& c, int b, int64_t slot, int64_t& row, int* status) {

@@ -83,10 +83,10 @@ constexpr int kAttnItemRows = 256;
 constexpr int kAttnCtasPerSm = 2;  // at most (with items of at most 128 rows each then)
 
 cudaError_t launch_rope_table(float2* table, int max_seq, int pairs, const double* inv_freq, double amplitude,
-                              cudaStream_t st);
+                              int num_sms, cudaStream_t st);
 cudaError_t launch_rows(const RowsArgs& a, fe_dtype dtype, int hd, int cache_kind, cudaStream_t st);
 cudaError_t launch_cache_read(const ReadArgs& a, fe_dtype dtype, fe_dtype cache_dtype, int hd, cudaStream_t st);
-cudaError_t launch_cache_keep(const KeepArgs& a, cudaStream_t st);
+cudaError_t launch_cache_keep(const KeepArgs& a, int num_sms, cudaStream_t st);
 cudaError_t tree_attn_prepare();
 // whether the schedule can count the work of every call of this shape
 bool tree_attn_fits(const TreeAttnArgs& a, fe_dtype dtype, fe_dtype cache_dtype);
