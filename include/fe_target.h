@@ -173,13 +173,17 @@ FE_API fe_status fe_cache_read(fe_target *t, const fe_cache_read_args *a, void *
  *  n_nodes     device [B] int32 in 0..T, or NULL for T
  *  mask        device [B, T, T] uint8 (fe_build_tree's mask) or NULL
  *  scale       finite, > 0
- * Softmax statistics and sums are float32. A node that sees no slot, or only scores of minus
- * infinity, and every node i >= n_b get a zero row and lse = -inf; slots that a node does not
- * see do not affect it whatever they hold, NaN included. A sequence with P_b or n_b out of
- * range counts as n_b = 0 and sets FE_ERR_CAPACITY; a bad page id sets FE_ERR_DEVICE and its
- * rows count as zeros. The result does not depend on timing: the same call gives the same bits.
- * B in 1..max_batch, T >= 1. FE_ERR_UNSUPPORTED for a shape whose work could pass 2^31 units of
- * 64 rows x 64 slots (float32) or 128 x 128. */
+ * Softmax statistics and sums are float32. FE_BF16 handles round the probabilities to bfloat16 (up
+ * to 2^-8 of each) for the product with the values. Over an FE_E4M3 cache they take a query
+ * element exactly from 2^-9 of its row's largest on and to 2^-17 of the largest below that, and a
+ * row with a non-finite element as NaN. An FE_F32 handle keeps 32 bits throughout. A node that
+ * sees no slot, or only scores of minus infinity, and every node i >= n_b get a zero row and lse =
+ * -inf; slots that a node does not see do not affect it whatever they hold, NaN included. A
+ * sequence with P_b or n_b out of range counts as n_b = 0 and sets FE_ERR_CAPACITY; a bad page id
+ * sets FE_ERR_DEVICE and its rows count as zeros. The result does not depend on timing: the same
+ * call gives the same bits.
+ * B in 1..max_batch, T >= 1. FE_ERR_UNSUPPORTED for a shape whose work could pass 2^31 units, of 64
+ * rows x 64 slots (float32) or 128 x 128 (where slots are nodes' a half more, over bfloat16). */
 typedef struct {
     int32_t B, T;
     fe_rows q, out;

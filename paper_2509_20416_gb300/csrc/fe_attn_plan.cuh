@@ -46,9 +46,10 @@ __device__ __forceinline__ SeqLen seq_len(const PlanArgs& a, int b, bool* bad = 
 // ROWS rows an item, TN slots a tile; PAIR: an item of more than 128 rows costs two units a tile.
 // An item begins with OVER units that hold no tile: what starting and finishing it costs a CTA, in
 // units, so that a CTA with many short items does not end after one with few long ones. JOIN: about
-// how many tiles joining a split costs. TAIL: what a tile that reaches into the nodes' slots costs an
-// item of two units a tile besides (masks, values to look through). (one token over 199 float32 slots, 8 items of 4 tiles: 36 us
-// whole, 20 split).
+// how many tiles joining a split costs: items of that many on average, no more of them than CTAs, are
+// not split. Above it splitting pays (one token over 199 float32 slots, 8 items of 4 tiles of 64: 20 us
+// split, 36 whole). TAIL: what a tile that reaches into the nodes' slots costs an item of two units a
+// tile besides (masks, values to look through).
 // Units are counted in 32 bits (the launch refuses shapes that could pass 2^31): this runs once a
 // CTA before anything else can start, and short code is what it takes to be quick.
 template <int ROWS, int TN, bool PAIR, int OVER, int JOIN, int TAIL>

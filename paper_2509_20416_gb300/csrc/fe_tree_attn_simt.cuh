@@ -1,5 +1,6 @@
-// Attention over the cache on the CUDA cores, in float32 throughout: float32 targets have no
-// tensor-core path that keeps their precision (bf16 and tf32 operands drop 13 to 16 bits).
+// Attention over the cache on the CUDA cores, in float32 throughout. (One bfloat16 or tf32 operand
+// drops 13 to 16 bits; three bfloat16 parts a number, six products, would keep them on the tensor
+// cores and have not been tried.)
 //
 // A CTA of 256 threads holds 16 NI query rows (NI = 1, 2 or 4, the fewest that hold an item's) and
 // walks tiles of 64 slots: thread (ty, tx) of a 16 x 16 grid owns rows ty + 16 i and, of each tile's

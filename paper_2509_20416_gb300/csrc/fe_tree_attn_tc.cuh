@@ -31,20 +31,25 @@
 // more than 2^12: after the first tiles that is rare, and it saves a pass over O per tile and a pass
 // over the scores for their maximum. The probabilities then stay below 2^12, where floating point is
 // as precise as below 1, and sums over a long cache are far from overflow. (81 nodes over 131k e4m3
-// slots: 362 us with 2^8, 353 with 2^12, 354 with 2^16 or 2^24.) Sums and statistics are float32;
-// probabilities are rounded to bfloat16 for the second product, which costs up to 2^-8 of each and
-// is what the 16-bit tensor path offers.
+// slots: 362 us with 2^8, 353 with 2^12, 354 with 2^16 or 2^24.) Sums and statistics are float32.
+// The probabilities are rounded to bfloat16 for the second product, up to 2^-8 of each and without a
+// bias: outputs are off by 2.3e-3 of their size against 64 bits, by 1.7e-3 from their own rounding
+// alone. Two parts a probability would double that product, half of the tensor cores' work. A row's
+// sum is that of the unrounded ones: the log-sum-exp needs it to 32 bits. 2^x is ex2.approx's, off
+// by up to 2^-22.
 // Values in slots that a row does not see meet a zero probability, but 0 x NaN is NaN: the loaders
 // zero the non-finite elements of nodes' value rows (and of what lies past the item's end) and flag
 // the segment, whose epilogue then adds their terms to the rows that do see them.
 //
 // What bounds it (GB300, 128-wide heads): 32 sequences over 256 to 4096 bfloat16 slots, 8 KV heads,
-// 17 nodes x 4 heads: 67 us, 4.4 TB/s (pages of 16: 75); 49 x 4 rows: 87 us, 660 TFLOP/s. 81 nodes x
-// 64 heads over 131k slots: bfloat16 297 us, 1170 TFLOP/s; e4m3 356 us, 977 TFLOP/s. The long ones
-// are bound by a stream's chain, softmax (1300 clocks a tile, 1024 of them exponentials; with key
-// scales 2200 and more) after product after softmax, of which two are in flight; the products alone
-// need 2048 of the 3150 clocks that a tile pair takes. The short ones pay 7 us of start (schedule,
-// first tile, cold instruction caches) and an epilogue of 2 us a share of an item.
+// 17 nodes x 4 heads: 67 us, 4.4 TB/s (pages of 16: 77); 49 x 4 rows: 86 us, 660 TFLOP/s. 81 nodes x
+// 64 heads over 131k slots: bfloat16 299 us, 1160 TFLOP/s; e4m3 361 us, 960 TFLOP/s. The long ones
+// are bound by a stream's chain, softmax (1300 clocks a tile; with key scales 2700) after product
+// after softmax, of which two are in flight; the products alone need 2048 of the 3150 clocks that a
+// tile pair takes. No pipe of the softmax is near its limit: over 2 x 1021 tokens the exponentials' is
+// used to 26 % (32 a clock and SM: 512 clocks a tile), the integer pipe to 35 %, the issue slots to
+// 43 %. The short ones pay 7 us of start (schedule, first tile, cold instruction caches) and an
+// epilogue of 2 us a share of an item.
 #pragma once
 
 #include <cuda.h>
@@ -471,14 +476,6 @@ __device__ __forceinline__ void tc_ld16_wait(uint32_t* r) {
                  :
                  : "memory");
 }
-__device__ __forceinline__ void tc_ld8(uint32_t taddr, uint32_t* r) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-        : "r"(taddr)
-        : "memory");
-}
 __device__ __forceinline__ void tc_ld32_start(uint32_t taddr, uint32_t* r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
@@ -547,8 +544,8 @@ __device__ __noinline__ void rescale_row(uint32_t ts, int np, uint32_t to, int n
 // as packed bfloat16 over the first 64 columns (32 scores become 16 columns, always behind what is
 // still to be read), their float32 sum added to `sum`. m is the row's reference maximum; when some
 // row of the warp has outgrown it by more than 2^12, the warp moves to new references on the spot.
-// Bound by the exponentials (16 a clock and SM), in whose shade the next 32 scores are loaded and
-// their maximum taken. A loop with a short body: the CTA's roles share the instruction caches, and
+// Bound by latency: the next 32 scores load under the exponentials of these (512 of a tile's 1300
+// clocks), their maximum follows. A loop with a short body: the CTA's roles share the instruction caches, and
 // unrolled rows made every one of them wait for fetches.
 // With e4m3 keys (Q8) the scores still lack their keys' scales, ks (shared memory).
 template <int HD, bool Q8>
@@ -719,9 +716,11 @@ __device__ __noinline__ void put_odd_columns(const TreeAttnArgs& a, const Segmen
 
 // A query row, for the e4m3 product with keys as they are: q = 2^c (hi + lo), hi the e4m3 rounding
 // of q / 2^c with the smallest c that fits the row's largest magnitude under 448, lo that of the
-// rest. A bfloat16 number's 8 significant bits are two times e4m3's 4, so the split is exact down
-// to 2^-10 of the row's scale (2^-18 of its largest element), and costs the tensor cores nothing:
-// two products at twice the rate. In place: the 64 bytes of elements 32 k .. become their 32 hi
+// rest. A bfloat16 number's 8 significant bits are two times e4m3's 4, so the split is exact for
+// elements from 2^c / 4 on (2^-9 of the row's largest is always that); smaller ones end at e4m3's
+// last place and are off by up to 2^(c - 10), 2^-17 of the largest, where bfloat16 held more. It costs
+// the tensor cores nothing: two products at twice the rate. (Keys converted to bfloat16 would meet
+// queries as they are: 423 us where this took 390, 81 nodes over 131k slots.) In place: the 64 bytes of elements 32 k .. become their 32 hi
 // and 32 lo bytes. Returns 2^c.
 template <int HD>
 __device__ __forceinline__ float split_query_row(unsigned char* block, int row) {
