@@ -240,7 +240,7 @@ def test_new_outputs_on_another_stream_are_not_written_early(fe, call, handle):
     torch.cuda.synchronize()
     torch.cuda.empty_cache()
     freed = torch.empty_like(want)
-    torch.cuda._sleep(400_000_000)
+    torch.cuda._sleep(1_000_000_000)
     freed.copy_(other)  # (runs after the pause)
     del freed
     got = run(stream=s.cuda_stream if handle else s)
@@ -260,8 +260,10 @@ def test_status_is_read_and_cleared_on_its_own_stream(fe):
     k = torch.zeros(1, 1, 2, 128, dtype=torch.bfloat16, device="cuda")
     bad, good = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (99, 3))
     s = torch.cuda.Stream()
+    fe.fe_cache_write(t, store, 0, k, k, good)  # (a first launch loads its kernel, which may wait for others)
+    assert fe.fe_target_status(t) == fe.FE_OK
     torch.cuda.synchronize()
-    torch.cuda._sleep(400_000_000)
+    torch.cuda._sleep(1_000_000_000)
     fe.fe_cache_write(t, store, 0, k, k, bad, stream=s)
     assert fe.fe_target_status(t, stream=s) == fe.FE_ERR_CAPACITY
     for _ in range(20):
