@@ -27,8 +27,8 @@
 // e4m3 keys go to the tensor cores as they are, with queries as two e4m3 parts (split_query_row);
 // their scales are applied to the scores.
 //
-// The softmax keeps a reference maximum per row and rescales O only when the maximum has grown by
-// more than 2^12: after the first tiles that is rare, and it saves a pass over O per tile and a pass
+// The softmax keeps a reference per row, its maximum rounded up to a whole power of two, and rescales O
+// (exactly, therefore) only when the maximum has grown by more than 2^12: after the first tiles that is rare, and it saves a pass over O per tile and a pass
 // over the scores for their maximum. The probabilities then stay below 2^12, where floating point is
 // as precise as below 1, and sums over a long cache are far from overflow. (81 nodes over 131k e4m3
 // slots: 362 us with 2^8, 353 with 2^12, 354 with 2^16 or 2^24.) Sums and statistics are float32.
@@ -542,8 +542,10 @@ __device__ __noinline__ void rescale_row(uint32_t ts, int np, uint32_t to, int n
 
 // One row's softmax of a tile, in one pass over its 128 scores x at TMEM columns ts: 2^(scale2 x - m)
 // as packed bfloat16 over the first 64 columns (32 scores become 16 columns, always behind what is
-// still to be read), their float32 sum added to `sum`. m is the row's reference maximum; when some
-// row of the warp has outgrown it by more than 2^12, the warp moves to new references on the spot.
+// still to be read), their float32 sum added to `sum`. m is the row's reference, its maximum rounded
+// up to a whole number; when some row of the warp has outgrown it by more than 2^12, the warp moves to
+// new references on the spot. They differ by whole numbers, so what has been written is scaled by a
+// power of two and not rounded again.
 // Bound by latency: the next 32 scores load under the exponentials of these (512 of a tile's 1300
 // clocks), their maximum follows. A loop with a short body: the CTA's roles share the instruction caches, and
 // unrolled rows made every one of them wait for fetches.
@@ -575,7 +577,8 @@ __device__ __forceinline__ void softmax_row(uint32_t ts, uint32_t to, float scal
 #pragma unroll 1
     for (int c = 0; c < kTcTile; c += 32) {
         if (__any_sync(0xffffffffu, mx > m + kRescale)) {
-            const float mn = fmaxf(m, mx), f = mn == -INFINITY ? 1.f : exp2f(m - mn);
+            const float mn = fmaxf(m, ceilf(mx)), d = mn == -INFINITY ? 0.f : m - mn;  // (whole, or -inf)
+            const float f = d < -126.f ? 0.f : __uint_as_float((uint32_t)(127 + (int)d) << 23);
             const uint64_t ff = pair_f32(__float_as_uint(f), __float_as_uint(f));
             z[0] = fma_x2(z[0], ff, 0);
             z[1] = fma_x2(z[1], ff, 0);

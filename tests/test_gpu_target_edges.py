@@ -432,3 +432,29 @@ def test_queries_with_an_outlier_over_e4m3(fe, T, size):
             tol = ((e + torch.expm1(2 * f))[:, None] + 1.01 * 2.0 ** -8) * mag + 2.0 ** -8 * o.abs()
             assert ((out[0, :, i].double() - o).abs() <= tol).all()
             assert ((lse[0, :, i].double() - l).abs() <= e + f + 2.0 ** -23 * l.abs()).all()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+@pytest.mark.parametrize("T", [30, 90])
+def test_probabilities_are_rounded_once(fe, cache, T):
+    """A slot at the start of a tile in which the maximum then grows three times by 2^13 to 2^20: its
+    probability is all that half of the columns see. It may be off by one rounding to bfloat16, as in
+    test_gpu_target.py's bound, however often the row's reference moves."""
+    H, Hkv, hd, P = 8, 2, 128, 128
+    c = ref.config(cache_dtype=cache, n_heads=H, n_kv_heads=Hkv, head_dim=hd, max_batch=1, max_seq=P + T)
+    t = fe.fe_target_init(c)
+    g = gen(T)
+    store = ref.random_cache(fe, t, c, g)
+    k = torch.zeros(Hkv, P + T, hd)
+    k[:, torch.arange(P), torch.arange(P) // 32] = 1.0
+    v = torch.randn(Hkv, P + T, hd, generator=g)
+    v[:, 1:, :64] = 0.0
+    fill(store, "k", k, cache)
+    fill(store, "v", v, cache)
+    q = torch.zeros(1, T, H, hd)
+    q[..., :4] = (9 + 5 * torch.rand(1, T, H, 4, generator=g)).cumsum(-1)
+    q = q.bfloat16().cuda()
+    plen = torch.tensor([P], dtype=torch.int32)
+    out, lse = fe.fe_tree_attention(t, store, 0, q, plen.cuda(), scale=1.0)
+    assert fe.fe_target_status(t) == fe.FE_OK
+    check_attention(c, store, None, q, plen, torch.tensor([T]), None, out, lse, scale=1.0)
