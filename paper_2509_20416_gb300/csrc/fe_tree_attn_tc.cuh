@@ -27,23 +27,23 @@
 // e4m3 keys go to the tensor cores as they are, with queries as two e4m3 parts (split_query_row);
 // their scales are applied to the scores.
 //
-// The softmax keeps a reference per row, its maximum rounded up to a whole power of two, and rescales O
-// (exactly, therefore) only when the maximum has grown by more than 2^12: after the first tiles that is rare, and it saves a pass over O per tile and a pass
-// over the scores for their maximum. The probabilities then stay below 2^12, where floating point is
-// as precise as below 1, and sums over a long cache are far from overflow. (81 nodes over 131k e4m3
-// slots: 362 us with 2^8, 353 with 2^12, 354 with 2^16 or 2^24.) Sums and statistics are float32.
-// The probabilities are rounded to bfloat16 for the second product, up to 2^-8 of each and without a
-// bias: outputs are off by 2.3e-3 of their size against 64 bits, by 1.7e-3 from their own rounding
-// alone. Two parts a probability would double that product, half of the tensor cores' work. A row's
-// sum is that of the unrounded ones: the log-sum-exp needs it to 32 bits. 2^x is ex2.approx's, off
-// by up to 2^-22.
+// The softmax keeps a reference per row, its maximum rounded up to a whole power of two, and rescales
+// O (exactly, therefore) only when the maximum has grown by more than 2^12: after the first tiles that
+// is rare, and it saves a pass over O per tile and a pass over the scores for their maximum. The
+// probabilities then stay below 2^12, where floating point is as precise as below 1, and sums over a
+// long cache are far from overflow. (81 nodes over 131k e4m3 slots: 362 us with 2^8, 353 with 2^12,
+// 354 with 2^16 or 2^24.) Sums and statistics are float32. The probabilities are rounded to bfloat16
+// for the second product, up to 2^-8 of each and without a bias: outputs are off by 2.3e-3 of their
+// size against 64 bits, by 1.7e-3 from their own rounding alone. Two parts a probability would double
+// that product, half of the tensor cores' work. A row's sum is that of the unrounded ones: the log-
+// sum-exp needs it to 32 bits. 2^x is ex2.approx's, off by up to 2^-22.
 // Values in slots that a row does not see meet a zero probability, but 0 x NaN is NaN: the loaders
 // zero the non-finite elements of nodes' value rows (and of what lies past the item's end) and flag
 // the segment, whose epilogue then adds their terms to the rows that do see them.
 //
 // What bounds it (GB300, 128-wide heads): 32 sequences over 256 to 4096 bfloat16 slots, 8 KV heads,
 // 17 nodes x 4 heads: 67 us, 4.4 TB/s (pages of 16: 77); 49 x 4 rows: 86 us, 660 TFLOP/s. 81 nodes x
-// 64 heads over 131k slots: bfloat16 299 us, 1160 TFLOP/s; e4m3 361 us, 960 TFLOP/s. The long ones
+// 64 heads over 131k slots: bfloat16 299 us, 1160 TFLOP/s; e4m3 358 us, 972 TFLOP/s. The long ones
 // are bound by a stream's chain, softmax (1300 clocks a tile; with key scales 2700) after product
 // after softmax, of which two are in flight; the products alone need 2048 of the 3150 clocks that a
 // tile pair takes. No pipe of the softmax is near its limit: over 2 x 1021 tokens the exponentials' is
