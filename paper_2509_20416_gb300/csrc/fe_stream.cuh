@@ -94,13 +94,13 @@ __device__ inline StreamSmem carve_stream_smem(unsigned char* smem, int D, int x
 // wall-clock budget (then raises the flag and records ST_TIMEOUT). With sleep_ns > 0 the
 // thread sleeps (up to sleep_ns per try) instead of spinning.
 __device__ __forceinline__ bool mbar_wait_abortable(uint64_t* bar, uint32_t parity, int* status, int* abort,
-                                                    uint32_t sleep_ns = 0, int64_t budget_ns = kWaitBudgetNs) {
+                                                    uint32_t sleep_ns = 0) {
     if (mbar_try_wait(bar, parity)) return true;
     const uint64_t t0 = globaltimer_ns();
     while (true) {
         if (sleep_ns ? mbar_try_wait_sleep(bar, parity, sleep_ns) : mbar_try_wait(bar, parity)) return true;
         if (*(volatile int*)abort) return false;
-        if ((int64_t)(globaltimer_ns() - t0) > budget_ns) {
+        if ((int64_t)(globaltimer_ns() - t0) > kWaitBudgetNs) {
             atomicOr(status, ST_TIMEOUT);
             *(volatile int*)abort = 1;
             return false;

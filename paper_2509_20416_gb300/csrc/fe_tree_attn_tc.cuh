@@ -183,10 +183,19 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&w)[8]) {
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// A warp's bounded wait (mbar_wait_abortable) whose slow part is one call, not a copy at every place.
+// The slow part of a warp's bounded wait, one call, not a copy at every place: until the phase is
+// complete, another role gives up, or the time is over (which it then tells the others and the host).
 // It has failed if it failed in any lane.
 __device__ __noinline__ bool tc_wait_slow(uint64_t* bar, uint32_t parity, int* status, int* abort, int64_t budget_ns) {
-    return __all_sync(0xffffffffu, mbar_wait_abortable(bar, parity, status, abort, 0, budget_ns));
+    const uint64_t t0 = globaltimer_ns();
+    bool done = false;
+    while (!(done = mbar_try_wait(bar, parity)) && !*(volatile int*)abort) {
+        if ((int64_t)(globaltimer_ns() - t0) > budget_ns) {
+            atomicOr(status, ST_TIMEOUT);
+            *(volatile int*)abort = 1;
+        }
+    }
+    return __all_sync(0xffffffffu, done);
 }
 // What a wait is allowed besides, for each tile that it lasts: several times a tile's time.
 constexpr int64_t kTileBudgetNs = 20000;
