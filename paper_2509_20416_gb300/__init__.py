@@ -477,3 +477,5 @@ def fe_lm_head_topk_noalloc(h: Handle, hidden, B: int, top_k: int, temperature: 
 from .target import (FE_E4M3, Cache, Target, alloc_cache, fe_cache_keep, fe_cache_read,  # noqa: E402,F401
                      fe_cache_write, fe_rope, fe_target_free, fe_target_init, fe_target_status, fe_tree_attention,
                      make_target_config)
+from .layer import (fe_block_norm, fe_block_norm_backward, fe_gated_ffn, fe_gated_ffn_backward, fe_project,  # noqa: E402,F401
+                    fe_project_backward, fe_token_logprobs, fe_token_logprobs_backward)

@@ -1,0 +1,116 @@
+// Gradients of activations, and sums over rows (fe_project_backward, fe_gated_ffn_backward): bound
+// by memory traffic. A warp takes a strip of columns, 16 bytes a lane, of every eighth row of its
+// CTA's part of the rows, so that a column's sum stays in a register until the part is done; the
+// parts' sums are added in order by a second kernel.
+#include "fe_layer_common.cuh"
+
+namespace fe {
+
+namespace {
+
+constexpr int kGradWarps = 8;
+
+template <typename T>
+__global__ void __launch_bounds__(kGradWarps * 32) act_grad_kernel(const __grid_constant__ ActGradArgs a) {
+    constexpr int V = Vec16<T>::kN;
+    __shared__ float sums[kGradWarps][32][V + 1];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int n = (blockIdx.x * 32 + lane) * V, have = a.N - n;
+    const int64_t r0 = a.M * blockIdx.y / a.parts, r1 = a.M * (blockIdx.y + 1) / a.parts;
+    float sum[V] = {};
+    if (have > 0) {
+#pragma unroll 2
+        for (int64_t r = r0 + warp; r < r1; r += kGradWarps) {
+            float d[V], z[V], u[V];
+            load_row<T, V>((const T*)a.dout.p + r * a.dout.row + n, have, a.vec, d);
+            if (a.pre.p) load_row<T, V>((const T*)a.pre.p + r * a.pre.row + n, have, a.vec, z);
+            if (a.gated) {
+                load_row<T, V>((const T*)a.pre2.p + r * a.pre2.row + n, have, a.vec, u);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float v, dv;
+                    act_both(a.act, z[i], v, dv);
+                    z[i] = d[i] * v;
+                    d[i] = d[i] * u[i] * dv;
+                }
+                store_row<T, V>((T*)a.d2.p + r * a.d2.row + n, have, a.vec, z);
+            } else if (a.act != FE_ACT_NONE) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float v, dv;
+                    act_both(a.act, z[i], v, dv);
+                    d[i] *= dv;
+                }
+            }
+            if (a.d1.p) store_row<T, V>((T*)a.d1.p + r * a.d1.row + n, have, a.vec, d);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] += d[i];
+        }
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int i = 0; i < V; ++i) sums[warp][lane][i] = sum[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * V; i += kGradWarps * 32) {
+        const int c = blockIdx.x * 32 * V + i;
+        if (c >= a.N) break;
+        float s = 0.f;
+        for (int w = 0; w < kGradWarps; ++w) s += sums[w][i / V][i % V];
+        a.part[(int64_t)blockIdx.y * a.N + c] = s;
+    }
+}
+
+// a warp's lanes take neighbouring columns, the warps of a CTA every eighth part
+template <typename T>
+__global__ void __launch_bounds__(kGradWarps * 32)
+    sum_parts_kernel(const float* part, int64_t parts, int64_t groups, int64_t n, T* out, int64_t out_row) {
+    __shared__ float sums[kGradWarps][32];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    for (int64_t g = blockIdx.y; g < groups; g += gridDim.y) {
+        float s = 0.f;
+        if (c < n) {
+            const float* p = part + g * parts * n + c;
+#pragma unroll 8
+            for (int64_t i = warp; i < parts; i += kGradWarps) s += p[i * n];
+        }
+        sums[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0 && c < n) {
+            s = 0.f;
+#pragma unroll
+            for (int w = 0; w < kGradWarps; ++w) s += sums[w][lane];
+            store_one(out + g * out_row + c, s);
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T>
+cudaError_t launch_grad(const ActGradArgs& a, cudaStream_t st) {
+    const int strip = 32 * Vec16<T>::kN;
+    return launch_k(act_grad_kernel<T>, dim3((a.N + strip - 1) / strip, a.parts), dim3(kGradWarps * 32), 0, st, false, a);
+}
+
+}  // namespace
+
+int act_grad_parts(int64_t M, int N, fe_dtype dtype, int num_sms) {
+    const int strip = dtype == FE_F32 ? 128 : 256;
+    const int64_t strips = (N + strip - 1) / strip, most = (M + kGradWarps - 1) / kGradWarps;
+    const int64_t want = (num_sms * 8 + strips - 1) / strips;  // eight CTAs an SM
+    return (int)(want < most ? want : most);
+}
+
+cudaError_t launch_act_grad(const ActGradArgs& a, fe_dtype dtype, cudaStream_t st) {
+    return dtype == FE_F32 ? launch_grad<float>(a, st) : launch_grad<bf16_t>(a, st);
+}
+
+cudaError_t launch_sum_parts(const float* part, int64_t parts, int64_t groups, int64_t n, void* out, int64_t out_row,
+                             fe_dtype dtype, cudaStream_t st) {
+    const dim3 grid((unsigned)((n + 31) / 32), (unsigned)(groups < 65535 ? groups : 65535)), block(kGradWarps * 32);
+    if (dtype == FE_F32)
+        return launch_k(sum_parts_kernel<float>, grid, block, 0, st, false, part, parts, groups, n, (float*)out, out_row);
+    return launch_k(sum_parts_kernel<bf16_t>, grid, block, 0, st, false, part, parts, groups, n, (bf16_t*)out, out_row);
+}
+
+}  // namespace fe

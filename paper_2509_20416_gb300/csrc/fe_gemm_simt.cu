@@ -1,0 +1,201 @@
+// Matrix products on the CUDA cores: float32 throughout, any size, stride and alignment, either
+// operand with its summed index as columns or as rows (fe_layer.h's products and their gradients).
+//
+// A CTA of 256 threads makes a BM x BN tile, a thread BM/16 x BN/16 of it in registers: per step of
+// the summed index it reads (BM + BN) / 16 floats from shared memory for BM BN / 256 products. The
+// products go in pairs of columns (fma.rn.f32x2). Slices of 16 steps alternate between two buffers;
+// the next slice's loads are in flight while a slice is multiplied.
+#include "fe_layer_common.cuh"
+
+namespace fe {
+
+namespace {
+
+constexpr int kBK = 16;
+
+// One operand's slice of R rows (tile rows) x 16 steps. Stored by rows (summed index contiguous) a
+// thread takes runs of 4 steps of a row, stored by steps (T) runs of 4 rows of a step.
+template <typename T, int R, bool STEPS>
+struct Slice {
+    static constexpr int kRuns = R * kBK / 4 / 256;
+    float v[kRuns][4];
+
+    // row_of(i): the row of the stored matrix for tile row i, -1 outside (BY ROWS); for STEPS tile rows
+    // are columns from r0 on, rows of them
+    __device__ __forceinline__ void load(const fe_mat& m, int64_t r0, int64_t rows, int k0, int K, bool vec, int split,
+                                         const fe_mat& second) {
+#pragma unroll
+        for (int i = 0; i < kRuns; ++i) {
+            const int u = threadIdx.x + i * 256;
+            if (!STEPS) {
+                const int r = u / (kBK / 4), k = k0 + u % (kBK / 4) * 4;
+                // gated tiles: their second half takes the same rows of the second matrix
+                const bool two = split > 0 && r >= split;
+                const int64_t row = r0 + (two ? r - split : r);
+                const T* p = (const T*)(two ? second.p : m.p) + row * (two ? second.row : m.row) + k;
+                run(p, row < rows ? K - k : 0, vec, v[i]);
+            } else {
+                const int k = u / (R / 4), r = u % (R / 4) * 4;
+                const T* p = (const T*)m.p + (int64_t)(k0 + k) * m.row + r0 + r;
+                const int64_t left = rows - r0 - r;
+                run(p, k0 + k < K ? (left < 4 ? (int)left : 4) : 0, vec, v[i]);
+            }
+        }
+    }
+    __device__ __forceinline__ static void run(const T* p, int have, bool vec, float* f) {
+        if (vec && have >= 4) {
+            if (sizeof(T) == 4) {
+                const float4 x = *reinterpret_cast<const float4*>(p);
+                f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(p);
+                f[0] = __uint_as_float(x.x << 16), f[1] = __uint_as_float(x.x & 0xFFFF0000u);
+                f[2] = __uint_as_float(x.y << 16), f[3] = __uint_as_float(x.y & 0xFFFF0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = i < have ? load_one(p + i) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void store(float (*s)[R + 4]) const {
+#pragma unroll
+        for (int i = 0; i < kRuns; ++i) {
+            const int u = threadIdx.x + i * 256;
+            if (!STEPS) {
+                const int r = u / (kBK / 4), k = u % (kBK / 4) * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[k + e][r] = v[i][e];
+            } else {
+                const int k = u / (R / 4), r = u % (R / 4) * 4;
+                *reinterpret_cast<float4*>(&s[k][r]) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+            }
+        }
+    }
+};
+
+template <int N>
+__device__ __forceinline__ void read_run(const float* s, float* f) {
+    if constexpr (N == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(s);
+        f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w;
+    } else {
+        const float2 x = *reinterpret_cast<const float2*>(s);
+        f[0] = x.x, f[1] = x.y;
+    }
+}
+
+template <typename T, int BM, int BN, bool AT, bool BT>
+__global__ void __launch_bounds__(256) gemm_simt_kernel(const __grid_constant__ GemmArgs g, int a_vec, int b_vec) {
+    constexpr int HM = BM / 32, HN = BN / 32;  // a thread's rows and columns: HM and HN in each half of the tile
+    __shared__ float As[2][kBK][BM + 4], Bs[2][kBK][BN + 4];
+    const int width = g.gated ? BN / 2 : BN;  // columns of the result in a tile
+    const int64_t nt = (g.N + width - 1) / width, mt = (g.M + BM - 1) / BM;
+    int64_t t = blockIdx.x;
+    const int prob = t >= nt * mt;
+    if (prob) t -= nt * mt;
+    const int64_t m0 = t / nt * BM;
+    const int n0 = (int)(t % nt) * width;
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    uint64_t acc[2 * HM][HN];
+#pragma unroll
+    for (int i = 0; i < 2 * HM; ++i)
+#pragma unroll
+        for (int j = 0; j < HN; ++j) acc[i][j] = 0;
+    const int slices = (g.K + kBK - 1) / kBK, all = slices * g.segs;
+    Slice<T, BM, AT> a;
+    Slice<T, BN, BT> b;
+    const auto fetch = [&](int s) {
+        const int seg = s >= slices;
+        const int k0 = (s - seg * slices) * kBK;
+        a.load(g.a[seg + prob], m0, g.M, k0, g.K, a_vec, 0, g.a[0]);
+        b.load(g.b[seg], n0, g.N, k0, g.K, b_vec, g.gated ? width : 0, g.b[1]);
+    };
+    fetch(0);
+    a.store(As[0]);
+    b.store(Bs[0]);
+    __syncthreads();
+    for (int s = 0; s < all; ++s) {
+        if (s + 1 < all) fetch(s + 1);
+        const float(*sa)[BM + 4] = As[s & 1];
+        const float(*sb)[BN + 4] = Bs[s & 1];
+#pragma unroll
+        for (int k = 0; k < kBK; ++k) {
+            float av[2 * HM], bv[2 * HN];
+            read_run<HM>(&sa[k][ty * HM], av);
+            read_run<HM>(&sa[k][BM / 2 + ty * HM], av + HM);
+            read_run<HN>(&sb[k][tx * HN], bv);
+            read_run<HN>(&sb[k][BN / 2 + tx * HN], bv + HN);
+#pragma unroll
+            for (int i = 0; i < 2 * HM; ++i) {
+                const uint64_t ai = pair_f32(av[i]);
+#pragma unroll
+                for (int j = 0; j < HN; ++j)
+                    acc[i][j] = fma_x2(ai, pair_f32(__float_as_uint(bv[2 * j]), __float_as_uint(bv[2 * j + 1])), acc[i][j]);
+            }
+        }
+        if (s + 1 < all) {
+            a.store(As[(s + 1) & 1]);
+            b.store(Bs[(s + 1) & 1]);
+            __syncthreads();
+        }
+    }
+    Finish e = g.e;
+    if (prob) {
+        e.out = g.out2;
+        e.out_row = g.out2_row;
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * HM; ++i) {
+        const int64_t m = m0 + (i < HM ? ty * HM + i : BM / 2 + ty * HM + i - HM);
+        if (m >= g.M) continue;
+        float z[2 * HN];
+#pragma unroll
+        for (int j = 0; j < HN; ++j) {
+            z[2 * j] = low_f32(acc[i][j]);
+            z[2 * j + 1] = high_f32(acc[i][j]);
+        }
+        if (g.gated) {
+            epilogue_gated<T, HN>(e, m, n0 + tx * HN, g.N, z, z + HN);
+        } else {
+            epilogue_plain<T, HN>(e, m, n0 + tx * HN, g.N, z);
+            epilogue_plain<T, HN>(e, m, n0 + BN / 2 + tx * HN, g.N, z + HN);
+        }
+    }
+}
+
+// runs of 4 elements on their own boundary
+bool runs_of_4(const fe_mat& m, int es) { return ((uintptr_t)m.p & (4 * es - 1)) == 0 && m.row % 4 == 0; }
+
+template <typename T, int BM, int BN, bool AT, bool BT>
+cudaError_t launch_tile(const GemmArgs& g, cudaStream_t st) {
+    const int es = sizeof(T), width = g.gated ? BN / 2 : BN;
+    const int64_t tiles = ((g.M + BM - 1) / BM) * ((g.N + width - 1) / width) * (g.twice ? 2 : 1);
+    if (tiles > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
+    const int na = g.segs == 2 || g.twice ? 2 : 1, nb = g.segs == 2 || g.gated ? 2 : 1;
+    bool av = true, bv = true;
+    for (int i = 0; i < na; ++i) av = av && runs_of_4(g.a[i], es);
+    for (int i = 0; i < nb; ++i) bv = bv && runs_of_4(g.b[i], es);
+    return launch_k(gemm_simt_kernel<T, BM, BN, AT, BT>, dim3((unsigned)tiles), dim3(256), 0, st, false, g, (int)av, (int)bv);
+}
+
+template <typename T, bool AT, bool BT>
+cudaError_t launch_layout(const GemmArgs& g, int num_sms, cudaStream_t st) {
+    const int64_t big = ((g.M + 127) / 128) * ((g.N + (g.gated ? 63 : 127)) / (g.gated ? 64 : 128)) * (g.twice ? 2 : 1);
+    // too few large tiles to occupy the GPU: a quarter of the size
+    if (big < num_sms || g.M <= 64) return launch_tile<T, 64, 64, AT, BT>(g, st);
+    return launch_tile<T, 128, 128, AT, BT>(g, st);
+}
+
+template <typename T>
+cudaError_t launch_type(const GemmArgs& g, int num_sms, cudaStream_t st) {
+    if (g.a_t) return launch_layout<T, true, true>(g, num_sms, st);  // (a weight's gradient: both by steps)
+    return g.b_t ? launch_layout<T, false, true>(g, num_sms, st) : launch_layout<T, false, false>(g, num_sms, st);
+}
+
+}  // namespace
+
+cudaError_t launch_gemm_simt(const GemmArgs& g, fe_dtype dtype, int num_sms, cudaStream_t st) {
+    return dtype == FE_F32 ? launch_type<float>(g, num_sms, st) : launch_type<bf16_t>(g, num_sms, st);
+}
+
+}  // namespace fe

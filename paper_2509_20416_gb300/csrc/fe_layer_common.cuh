@@ -1,0 +1,134 @@
+// Device helpers shared by the dense operators: activations and the products' epilogue.
+#pragma once
+
+#include "fe_layer_kernels.h"
+#include "fe_target_common.cuh"
+
+namespace fe {
+
+__device__ __forceinline__ float load_one(const float* p) { return *p; }
+__device__ __forceinline__ float load_one(const bf16_t* p) { return bf16_to_f32(p->bits); }
+
+// 1 / (1 + e^-x); 0 and 1 at the ends
+__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+
+constexpr float kGeluA = 1.5957691216057308f;   // 2 sqrt(2 / pi)
+constexpr float kGeluB = 0.07135481627260025f;  // kGeluA * 0.044715
+
+// (1 + tanh(u)) / 2 = sigmoid(2 u). Past |z| = 12 the cube adds nothing to a sigmoid that is 0 or 1
+// in float32, and a square that overflows would make the gradient's 0 times it NaN.
+__device__ __forceinline__ float act_value(int act, float z) {
+    switch (act) {
+        case FE_ACT_RELU: return z < 0.f ? 0.f : z;
+        case FE_ACT_SILU: return z * sigmoid(z);
+        case FE_ACT_GELU: {
+            const float c = fminf(fmaxf(z, -12.f), 12.f);
+            const float s = sigmoid(c * (kGeluA + kGeluB * c * c));
+            return (z < -12.f && z > -INFINITY) ? 0.f : z * s;
+        }
+        default: return z;
+    }
+}
+
+// act(z) and act'(z)
+__device__ __forceinline__ void act_both(int act, float z, float& v, float& dv) {
+    switch (act) {
+        case FE_ACT_RELU:
+            v = z < 0.f ? 0.f : z;
+            dv = z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
+            return;
+        case FE_ACT_SILU: {
+            const float s = sigmoid(z);
+            v = z * s;
+            dv = s * (1.f + z * (1.f - s));
+            return;
+        }
+        case FE_ACT_GELU: {
+            const float c = fminf(fmaxf(z, -12.f), 12.f);
+            const float s = sigmoid(c * (kGeluA + kGeluB * c * c));
+            v = (z < -12.f && z > -INFINITY) ? 0.f : z * s;
+            dv = s + c * s * (1.f - s) * (kGeluA + 3.f * kGeluB * c * c);
+            if (z != z) dv = z;
+            return;
+        }
+        default:
+            v = z;
+            dv = 1.f;
+    }
+}
+
+// N consecutive elements of a row (N a multiple of 16 bytes where vec, else any) from and to floats;
+// elements from `have` on are left out
+template <typename T, int N>
+__device__ __forceinline__ void load_row(const T* p, int have, bool vec, float* f) {
+    constexpr int V = Vec16<T>::kN;
+    if (N % V == 0 && vec && have >= N) {
+#pragma unroll
+        for (int i = 0; i < N / V; ++i) Vec16<T>::widen(reinterpret_cast<const uint4*>(p)[i], f + i * V);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = i < have ? load_one(p + i) : 0.f;
+    }
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T* p, int have, bool vec, const float* f) {
+    constexpr int V = Vec16<T>::kN;
+    if (N % V == 0 && vec && have >= N) {
+#pragma unroll
+        for (int i = 0; i < N / V; ++i) reinterpret_cast<uint4*>(p)[i] = pack16<T>(f + i * V);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < have) store_one(p + i, f[i]);
+    }
+}
+
+// NV columns of row m from column n on, of a plain product z (overwritten)
+template <typename T, int NV>
+__device__ __forceinline__ void epilogue_plain(const Finish& e, int64_t m, int n, int N, float* z) {
+    const int have = N - n;
+    if (have <= 0) return;
+    float t[NV];
+    if (e.bias) {
+        load_row<T, NV>((const T*)e.bias + n, have, e.vec, t);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) z[i] += t[i];
+    }
+    if (e.pre) store_row<T, NV>((T*)e.pre + m * e.pre_row + n, have, e.vec, z);
+    if (e.act != FE_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) z[i] = act_value(e.act, z[i]);
+    }
+    if (e.res) {
+        load_row<T, NV>((const T*)e.res + m * e.res_row + n, have, e.vec, t);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) z[i] += t[i];
+    }
+    store_row<T, NV>((T*)e.out + m * e.out_row + n, have, e.vec, z);
+}
+
+// the same of a gated pair of products g and u (g is overwritten)
+template <typename T, int NV>
+__device__ __forceinline__ void epilogue_gated(const Finish& e, int64_t m, int n, int N, float* g, const float* u) {
+    const int have = N - n;
+    if (have <= 0) return;
+    if (e.pre) {
+        store_row<T, NV>((T*)e.pre + m * e.pre_row + n, have, e.vec, g);
+        store_row<T, NV>((T*)e.pre2 + m * e.pre2_row + n, have, e.vec, u);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) g[i] = act_value(e.act, g[i]) * u[i];
+    store_row<T, NV>((T*)e.out + m * e.out_row + n, have, e.vec, g);
+}
+
+// the sum of v over the CTA's threads, in the same order every time; buf: a float per warp
+__device__ __forceinline__ float cta_sum(float v, float* buf) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    v = warp_sum(v);
+    if (lane == 0) buf[warp] = v;
+    __syncthreads();
+    v = lane < warps ? buf[lane] : 0.f;
+    return warp_sum(v);
+}
+
+}  // namespace fe

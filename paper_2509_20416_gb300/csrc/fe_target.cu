@@ -6,43 +6,14 @@
 #include <new>
 #include <vector>
 
-#include "fe_target_kernels.h"
+#include "fe_layer_kernels.h"
+#include "fe_target_handle.h"
+
+#define FE_SOURCE "fe_target.cu"
 
 using namespace fe;
 
-struct fe_target {
-    fe_target_config cfg;
-    int device = 0, num_sms = 0;
-    float2* rope = nullptr;
-    float *part_o = nullptr, *part_ml = nullptr;
-    int* status = nullptr;
-    SplitDesc* split = nullptr;
-};
-
 namespace {
-
-fe_status fail(cudaError_t e, const char* what) {
-    char buf[200];
-    snprintf(buf, sizeof(buf), "%s (fe_target.cu): %s", what, cudaGetErrorString(e));
-    set_error_detail(buf);
-    return e == cudaErrorMemoryAllocation ? FE_ERR_OOM : FE_ERR_CUDA;
-}
-
-#define FE_TRY(call)                                   \
-    do {                                               \
-        cudaError_t _e = (call);                       \
-        if (_e != cudaSuccess) return fail(_e, #call); \
-    } while (0)
-
-fe_status check_device(const fe_target* t) {
-    int dev = -1;
-    FE_TRY(cudaGetDevice(&dev));
-    if (dev == t->device) return FE_OK;
-    char buf[128];
-    snprintf(buf, sizeof(buf), "the current CUDA device (%d) is not the handle's device (%d)", dev, t->device);
-    set_error_detail(buf);
-    return FE_ERR_INVALID_ARG;
-}
 
 bool valid_config(const fe_target_config* c) {
     if (!c) return false;
@@ -119,6 +90,7 @@ fe_status build(fe_target* t, cudaStream_t st) {
     FE_TRY(cudaGetDevice(&t->device));
     FE_TRY(cudaDeviceGetAttribute(&t->num_sms, cudaDevAttrMultiProcessorCount, t->device));
     FE_TRY(tree_attn_prepare());
+    FE_TRY(layer_prepare());
     const int pairs = c.rope_dim / 2;
     const size_t rows = (size_t)t->num_sms * 2 * kAttnItemRows;
     FE_TRY(cudaMalloc((void**)&t->rope, (size_t)c.max_seq * pairs * sizeof(float2)));
