@@ -46,7 +46,7 @@ typedef enum { FE_ACT_NONE = 0, FE_ACT_RELU = 1, FE_ACT_SILU = 2, FE_ACT_GELU = 
 
 /* out [M, N] = act(x [M, K] w [N, K]^T + bias [N]) + residual [M, N].
  *  bias, residual  may be absent; out may be the residual itself (the same p and row)
- *  pre             [M, N] or absent: x w^T + bias, which the gradient of an activation needs
+ *  pre             float32 [M, N] or absent: x w^T + bias, which the gradient of an activation needs
  * M >= 0 up to 2^30; N, K in 1..2^24. */
 typedef struct {
     int64_t M;
@@ -61,8 +61,8 @@ typedef struct {
 FE_API int64_t fe_project_work(const fe_target *t, const fe_project_args *a);
 FE_API fe_status fe_project(fe_target *t, const fe_project_args *a, void *stream);
 
-/* Gradients of fe_project for dout [M, N] (the residual's is dout itself): with dz = dout act'(pre),
- * rounded to the handle's type where act is not NONE,
+/* Gradients of fe_project for dout [M, N] (the residual's is dout itself), pre as fe_project stored it:
+ * with dz = dout act'(pre), rounded to the handle's type where act is not NONE,
  *   dx [M, K] = dz w,  dw [N, K] = dz^T x,  dbias [N] = sum over rows of dz;
  * each may be absent. w is read for dx, x for dw, pre for act != NONE. */
 typedef struct {
@@ -78,8 +78,8 @@ typedef struct {
 FE_API int64_t fe_project_backward_work(const fe_target *t, const fe_project_backward_args *a);
 FE_API fe_status fe_project_backward(fe_target *t, const fe_project_backward_args *a, void *stream);
 
-/* out [M, F] = act(x [M, K] w_gate [F, K]^T) * (x w_up [F, K]^T). gate_pre and up_pre [M, F]: both
- * or none of the two products, which the gradient needs. Sizes as for fe_project. */
+/* out [M, F] = act(x [M, K] w_gate [F, K]^T) * (x w_up [F, K]^T). gate_pre and up_pre: both or none of
+ * the two products, float32 [M, F], which the gradient needs. Sizes as for fe_project. */
 typedef struct {
     int64_t M;
     int32_t F, K;
@@ -91,15 +91,17 @@ typedef struct {
 FE_API int64_t fe_gated_ffn_work(const fe_target *t, const fe_gated_ffn_args *a);
 FE_API fe_status fe_gated_ffn(fe_target *t, const fe_gated_ffn_args *a, void *stream);
 
-/* Gradients of fe_gated_ffn for dout [M, F]: with dg = dout up act'(gate) and du = dout act(gate)
- * (gate, up: the two products), rounded to the handle's type,
- *   dx [M, K] = dg w_gate + du w_up,  dw_gate [F, K] = dg^T x,  dw_up [F, K] = du^T x;
- * dx may be absent, and the weights' gradients (both or none). */
+/* Gradients of fe_gated_ffn, for dh [M, F]: dout itself, or, with w_down [N, F], dout [M, N] w_down (the
+ * gradient of a block h w_down^T, without a rounding in between). With dg = dh up act'(gate) and du =
+ * dh act(gate) (gate, up: the two products as stored), rounded to the handle's type,
+ *   dx [M, K] = dg w_gate + du w_up,  dw_gate [F, K] = dg^T x,  dw_up [F, K] = du^T x,
+ *   dw_down [N, F] = dout^T h with h = act(gate) up, rounded as fe_gated_ffn's result;
+ * each may be absent, the first two weights' both or none. */
 typedef struct {
     int64_t M;
-    int32_t F, K;
-    fe_mat x, w_gate, w_up, dout, gate_pre, up_pre;
-    fe_mat dx, dw_gate, dw_up;
+    int32_t F, K, N;
+    fe_mat x, w_gate, w_up, w_down, dout, gate_pre, up_pre;
+    fe_mat dx, dw_gate, dw_up, dw_down;
     fe_act act;
     void *work;
     int64_t work_bytes;

@@ -23,9 +23,9 @@ __global__ void __launch_bounds__(kGradWarps * 32) act_grad_kernel(const __grid_
         for (int64_t r = r0 + warp; r < r1; r += kGradWarps) {
             float d[V], z[V], u[V];
             load_row<T, V>((const T*)a.dout.p + r * a.dout.row + n, have, a.vec, d);
-            if (a.pre.p) load_row<T, V>((const T*)a.pre.p + r * a.pre.row + n, have, a.vec, z);
+            if (a.pre.p) load_row<float, V>((const float*)a.pre.p + r * a.pre.row + n, have, a.vec, z);
             if (a.gated) {
-                load_row<T, V>((const T*)a.pre2.p + r * a.pre2.row + n, have, a.vec, u);
+                load_row<float, V>((const float*)a.pre2.p + r * a.pre2.row + n, have, a.vec, u);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     float v, dv;

@@ -88,7 +88,7 @@ template <typename T, int BM, int BN, bool AT, bool BT>
 __global__ void __launch_bounds__(256) gemm_simt_kernel(const __grid_constant__ GemmArgs g, int a_vec, int b_vec) {
     constexpr int HM = BM / 32, HN = BN / 32;  // a thread's rows and columns: HM and HN in each half of the tile
     __shared__ float As[2][kBK][BM + 4], Bs[2][kBK][BN + 4];
-    const int width = g.gated ? BN / 2 : BN;  // columns of the result in a tile
+    const int width = g.e.kind == FINISH_GATED ? BN / 2 : BN;  // columns of the result in a tile
     const int64_t nt = (g.N + width - 1) / width, mt = (g.M + BM - 1) / BM;
     int64_t t = blockIdx.x;
     const int prob = t >= nt * mt;
@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(256) gemm_simt_kernel(const __grid_constant__ 
         const int seg = s >= slices;
         const int k0 = (s - seg * slices) * kBK;
         a.load(g.a[seg + prob], m0, g.M, k0, g.K, a_vec, 0, g.a[0]);
-        b.load(g.b[seg], n0, g.N, k0, g.K, b_vec, g.gated ? width : 0, g.b[1]);
+        b.load(g.b[seg], n0, g.N, k0, g.K, b_vec, g.e.kind == FINISH_GATED ? width : 0, g.b[1]);
     };
     fetch(0);
     a.store(As[0]);
@@ -141,8 +141,8 @@ __global__ void __launch_bounds__(256) gemm_simt_kernel(const __grid_constant__ 
     }
     Finish e = g.e;
     if (prob) {
-        e.out = g.out2;
-        e.out_row = g.out2_row;
+        e.out = e.out2;
+        e.out_row = e.out2_row;
     }
 #pragma unroll
     for (int i = 0; i < 2 * HM; ++i) {
@@ -154,11 +154,11 @@ __global__ void __launch_bounds__(256) gemm_simt_kernel(const __grid_constant__ 
             z[2 * j] = low_f32(acc[i][j]);
             z[2 * j + 1] = high_f32(acc[i][j]);
         }
-        if (g.gated) {
+        if (e.kind == FINISH_GATED) {
             epilogue_gated<T, HN>(e, m, n0 + tx * HN, g.N, z, z + HN);
         } else {
-            epilogue_plain<T, HN>(e, m, n0 + tx * HN, g.N, z);
-            epilogue_plain<T, HN>(e, m, n0 + BN / 2 + tx * HN, g.N, z + HN);
+            epilogue_one<T, HN>(e, m, n0 + tx * HN, g.N, z);
+            epilogue_one<T, HN>(e, m, n0 + BN / 2 + tx * HN, g.N, z + HN);
         }
     }
 }
@@ -168,10 +168,10 @@ bool runs_of_4(const fe_mat& m, int es) { return ((uintptr_t)m.p & (4 * es - 1))
 
 template <typename T, int BM, int BN, bool AT, bool BT>
 cudaError_t launch_tile(const GemmArgs& g, cudaStream_t st) {
-    const int es = sizeof(T), width = g.gated ? BN / 2 : BN;
+    const int es = sizeof(T), width = g.e.kind == FINISH_GATED ? BN / 2 : BN;
     const int64_t tiles = ((g.M + BM - 1) / BM) * ((g.N + width - 1) / width) * (g.twice ? 2 : 1);
     if (tiles > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
-    const int na = g.segs == 2 || g.twice ? 2 : 1, nb = g.segs == 2 || g.gated ? 2 : 1;
+    const int na = g.segs == 2 || g.twice ? 2 : 1, nb = g.segs == 2 || g.e.kind == FINISH_GATED ? 2 : 1;
     bool av = true, bv = true;
     for (int i = 0; i < na; ++i) av = av && runs_of_4(g.a[i], es);
     for (int i = 0; i < nb; ++i) bv = bv && runs_of_4(g.b[i], es);
@@ -180,22 +180,17 @@ cudaError_t launch_tile(const GemmArgs& g, cudaStream_t st) {
 
 template <typename T, bool AT, bool BT>
 cudaError_t launch_layout(const GemmArgs& g, int num_sms, cudaStream_t st) {
-    const int64_t big = ((g.M + 127) / 128) * ((g.N + (g.gated ? 63 : 127)) / (g.gated ? 64 : 128)) * (g.twice ? 2 : 1);
+    const int64_t big = ((g.M + 127) / 128) * ((g.N + (g.e.kind == FINISH_GATED ? 63 : 127)) / (g.e.kind == FINISH_GATED ? 64 : 128)) * (g.twice ? 2 : 1);
     // too few large tiles to occupy the GPU: a quarter of the size
     if (big < num_sms || g.M <= 64) return launch_tile<T, 64, 64, AT, BT>(g, st);
     return launch_tile<T, 128, 128, AT, BT>(g, st);
 }
 
-template <typename T>
-cudaError_t launch_type(const GemmArgs& g, int num_sms, cudaStream_t st) {
-    if (g.a_t) return launch_layout<T, true, true>(g, num_sms, st);  // (a weight's gradient: both by steps)
-    return g.b_t ? launch_layout<T, false, true>(g, num_sms, st) : launch_layout<T, false, false>(g, num_sms, st);
-}
-
 }  // namespace
 
-cudaError_t launch_gemm_simt(const GemmArgs& g, fe_dtype dtype, int num_sms, cudaStream_t st) {
-    return dtype == FE_F32 ? launch_type<float>(g, num_sms, st) : launch_type<bf16_t>(g, num_sms, st);
+cudaError_t launch_gemm_simt(const GemmArgs& g, int num_sms, cudaStream_t st) {
+    if (g.a_t) return launch_layout<float, true, true>(g, num_sms, st);  // (a weight's gradient: both by steps)
+    return g.b_t ? launch_layout<float, false, true>(g, num_sms, st) : launch_layout<float, false, false>(g, num_sms, st);
 }
 
 }  // namespace fe

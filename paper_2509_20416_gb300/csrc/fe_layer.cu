@@ -56,7 +56,7 @@ bool project_ok(const fe_target* t, const fe_project_args* a) {
     if (!t || !a || !sizes_ok(a->M, a->N, a->K) || !act_ok(a->act)) return false;
     const int es = elem(t);
     return in_ok(a->x, es) && in_ok(a->w, es) && opt_ptr(a->bias, es) && opt_in(a->residual, es) &&
-           out_ok(a->out, a->M, a->N, es) && opt_out(a->pre, a->M, a->N, es);
+           out_ok(a->out, a->M, a->N, es) && opt_out(a->pre, a->M, a->N, 4);
 }
 
 bool project_backward_ok(const fe_target* t, const fe_project_backward_args* a) {
@@ -64,7 +64,7 @@ bool project_backward_ok(const fe_target* t, const fe_project_backward_args* a) 
     const int es = elem(t);
     if (!a->dx.p && !a->dw.p && !a->dbias) return false;
     if ((a->dx.p && !a->w.p) || (a->dw.p && !a->x.p) || (a->act != FE_ACT_NONE && !a->pre.p)) return false;
-    return in_ok(a->dout, es) && opt_in(a->x, es) && opt_in(a->w, es) && opt_in(a->pre, es) && opt_ptr(a->dbias, es) &&
+    return in_ok(a->dout, es) && opt_in(a->x, es) && opt_in(a->w, es) && opt_in(a->pre, 4) && opt_ptr(a->dbias, es) &&
            opt_out(a->dx, a->M, a->K, es) && opt_out(a->dw, a->N, a->K, es);
 }
 
@@ -72,24 +72,46 @@ bool gated_ok(const fe_target* t, const fe_gated_ffn_args* a) {
     if (!t || !a || !sizes_ok(a->M, a->F, a->K) || !act_ok(a->act)) return false;
     const int es = elem(t);
     return in_ok(a->x, es) && in_ok(a->w_gate, es) && in_ok(a->w_up, es) && out_ok(a->out, a->M, a->F, es) &&
-           !a->gate_pre.p == !a->up_pre.p && opt_out(a->gate_pre, a->M, a->F, es) && opt_out(a->up_pre, a->M, a->F, es);
+           !a->gate_pre.p == !a->up_pre.p && opt_out(a->gate_pre, a->M, a->F, 4) && opt_out(a->up_pre, a->M, a->F, 4);
 }
 
 bool gated_backward_ok(const fe_target* t, const fe_gated_ffn_backward_args* a) {
     if (!t || !a || !sizes_ok(a->M, a->F, a->K) || !act_ok(a->act)) return false;
     const int es = elem(t);
-    if (!a->dw_gate.p != !a->dw_up.p || (!a->dx.p && !a->dw_gate.p)) return false;
+    if (a->w_down.p && (a->N < 1 || a->N > kMaxCols)) return false;
+    if (a->dw_down.p && !a->w_down.p) return false;
+    if (!a->dw_gate.p != !a->dw_up.p || (!a->dx.p && !a->dw_gate.p && !a->dw_down.p)) return false;
     if ((a->dx.p && (!a->w_gate.p || !a->w_up.p)) || (a->dw_gate.p && !a->x.p)) return false;
-    return in_ok(a->dout, es) && in_ok(a->gate_pre, es) && in_ok(a->up_pre, es) && opt_in(a->x, es) && opt_in(a->w_gate, es) &&
-           opt_in(a->w_up, es) && opt_out(a->dx, a->M, a->K, es) && opt_out(a->dw_gate, a->F, a->K, es) &&
-           opt_out(a->dw_up, a->F, a->K, es);
+    return in_ok(a->dout, es) && in_ok(a->gate_pre, 4) && in_ok(a->up_pre, 4) && opt_in(a->x, es) && opt_in(a->w_gate, es) &&
+           opt_in(a->w_up, es) && opt_in(a->w_down, es) && opt_out(a->dx, a->M, a->K, es) && opt_out(a->dw_gate, a->F, a->K, es) &&
+           opt_out(a->dw_up, a->F, a->K, es) && opt_out(a->dw_down, a->N, a->F, es);
 }
 
-// what a call does once its arguments are checked; st is not looked at where work is only counted
-fe_status gemm(const fe_target* t, GemmArgs& g, Workspace&, bool count, cudaStream_t st) {
-    if (count) return FE_OK;
+// What a call does once its arguments are checked; where its work is only counted nothing is launched
+// and st is not looked at.
+fe_status gemm(const fe_target* t, GemmArgs& g, Workspace& w, bool count, cudaStream_t st) {
     g.status = t->status;
-    FE_TRY(launch_gemm_simt(g, t->cfg.dtype, t->num_sms, st));
+    if (t->cfg.dtype == FE_F32) {
+        if (!count) FE_TRY(launch_gemm_simt(g, t->num_sms, st));
+        return FE_OK;
+    }
+    // rows off 16-byte boundaries are copied: the copy costs what the operand's bytes do, products on the
+    // CUDA cores would cost some twenty times the tensor cores' time
+    const auto readable = [&](fe_mat& m, int64_t rows, int64_t cols) -> fe_status {
+        if (gemm_tc_reads(m, rows, cols)) return FE_OK;
+        const fe_mat to = take_rows(w, rows, cols, 2);
+        if (!count) FE_TRY(launch_pack_rows(m, to, rows, cols, t->num_sms, st));
+        m = to;
+        return FE_OK;
+    };
+    for (int i = 0; i < 2; ++i) {
+        fe_status s = FE_OK;
+        if (i == 0 || g.segs == 2 || g.twice) s = g.a_t ? readable(g.a[i], g.K, g.M) : readable(g.a[i], g.M, g.K);
+        if (s == FE_OK && (i == 0 || g.segs == 2 || g.e.kind == FINISH_GATED))
+            s = g.b_t ? readable(g.b[i], g.K, g.N) : readable(g.b[i], g.N, g.K);
+        if (s != FE_OK) return s;
+    }
+    if (!count) FE_TRY(launch_gemm_tc(g, t->num_sms, st));
     return FE_OK;
 }
 
@@ -109,9 +131,9 @@ fe_status project(const fe_target* t, const fe_project_args* a, Workspace& w, bo
     g.e.res_row = a->residual.row;
     g.e.out = a->out.p;
     g.e.out_row = a->out.row;
-    g.e.pre = a->pre.p;
+    g.e.pre = (float*)a->pre.p;
     g.e.pre_row = a->pre.row;
-    g.e.vec = (!a->bias || on16(a->bias)) && on16(a->residual, es) && on16(a->out, es) && on16(a->pre, es);
+    g.e.vec = (!a->bias || on16(a->bias)) && on16(a->residual, es) && on16(a->out, es) && on16(a->pre, 4);
     return gemm(t, g, w, count, st);
 }
 
@@ -155,8 +177,8 @@ fe_status product_gradients(const fe_target* t, int64_t M, int N, int K, const f
         g.e.out_row = dw[0].row;
         g.e.vec = on16(dw[0], es) && (n == 1 || on16(dw[1], es));
         if (n == 2) {
-            g.out2 = dw[1].p;
-            g.out2_row = dw[1].row;
+            g.e.out2 = dw[1].p;
+            g.e.out2_row = dw[1].row;
         }
         return gemm(t, g, ws, count, st);
     }
@@ -184,7 +206,7 @@ fe_status project_backward(const fe_target* t, const fe_project_backward_args* a
         if (make) g.d1 = dz;
         g.parts = act_grad_parts(a->M, a->N, t->cfg.dtype, t->num_sms);
         if (a->dbias) g.part = (float*)w.take((int64_t)g.parts * a->N * sizeof(float));
-        g.vec = on16(g.dout, es) && on16(g.pre, es);
+        g.vec = on16(g.dout, es) && on16(g.pre, 4);
         if (!count) {
             FE_TRY(launch_act_grad(g, t->cfg.dtype, st));
             if (a->dbias) FE_TRY(launch_sum_parts(g.part, g.parts, 1, a->N, a->dbias, a->N, t->cfg.dtype, st));
@@ -201,18 +223,18 @@ fe_status gated(const fe_target* t, const fe_gated_ffn_args* a, Workspace& w, bo
     g.N = a->F;
     g.K = a->K;
     g.segs = 1;
-    g.gated = 1;
+    g.e.kind = FINISH_GATED;
     g.a[0] = a->x;
     g.b[0] = a->w_gate;
     g.b[1] = a->w_up;
     g.e.act = a->act;
     g.e.out = a->out.p;
     g.e.out_row = a->out.row;
-    g.e.pre = a->gate_pre.p;
+    g.e.pre = (float*)a->gate_pre.p;
     g.e.pre_row = a->gate_pre.row;
-    g.e.pre2 = a->up_pre.p;
+    g.e.pre2 = (float*)a->up_pre.p;
     g.e.pre2_row = a->up_pre.row;
-    g.e.vec = on16(a->out, es) && on16(a->gate_pre, es) && on16(a->up_pre, es);
+    g.e.vec = on16(a->out, es) && on16(a->gate_pre, 4) && on16(a->up_pre, 4);
     return gemm(t, g, w, count, st);
 }
 
@@ -220,26 +242,55 @@ fe_status gated_backward(const fe_target* t, const fe_gated_ffn_backward_args* a
     const int es = elem(t);
     const fe_mat dw[2] = {a->dw_gate, a->dw_up}, weights[2] = {a->w_gate, a->w_up};
     if (a->M == 0) {
-        for (int i = 0; i < 2 && !count; ++i) {
+        if (count) return FE_OK;
+        for (int i = 0; i < 2; ++i) {
             const fe_status s = zero_rows(dw[i], a->F, a->K, es, st);
             if (s != FE_OK) return s;
         }
-        return FE_OK;
+        return zero_rows(a->dw_down, a->N, a->F, es, st);
     }
     const fe_mat dz[2] = {take_rows(w, a->M, a->F, es), take_rows(w, a->M, a->F, es)};
-    ActGradArgs g{};
-    g.M = a->M;
-    g.N = a->F;
-    g.act = a->act;
-    g.gated = 1;
-    g.dout = a->dout;
-    g.pre = a->gate_pre;
-    g.pre2 = a->up_pre;
-    g.d1 = dz[0];
-    g.d2 = dz[1];
-    g.parts = act_grad_parts(a->M, a->F, t->cfg.dtype, t->num_sms);
-    g.vec = on16(g.dout, es) && on16(g.pre, es) && on16(g.pre2, es);
-    if (!count) FE_TRY(launch_act_grad(g, t->cfg.dtype, st));
+    if (a->w_down.p) {  // dh = dout w_down is finished before it is rounded
+        const fe_mat h = take_rows(w, a->M, a->F, es);
+        GemmArgs g{};
+        g.M = a->M;
+        g.N = a->F;
+        g.K = a->N;
+        g.segs = 1;
+        g.a[0] = a->dout;
+        g.b[0] = a->w_down;
+        g.b_t = 1;
+        g.e.kind = FINISH_GATED_GRAD;
+        g.e.act = a->act;
+        g.e.pre = (float*)a->gate_pre.p;
+        g.e.pre_row = a->gate_pre.row;
+        g.e.pre2 = (float*)a->up_pre.p;
+        g.e.pre2_row = a->up_pre.row;
+        g.e.out = dz[0].p;
+        g.e.out2 = dz[1].p;
+        g.e.out3 = h.p;
+        g.e.out_row = g.e.out2_row = g.e.out3_row = h.row;
+        g.e.vec = on16(a->gate_pre, 4) && on16(a->up_pre, 4);
+        fe_status s = gemm(t, g, w, count, st);
+        if (s != FE_OK) return s;
+        const fe_mat none{};
+        s = product_gradients(t, a->M, a->N, a->F, h, &a->w_down, &a->dout, 1, none, &a->dw_down, w, count, st);
+        if (s != FE_OK) return s;
+    } else {
+        ActGradArgs g{};
+        g.M = a->M;
+        g.N = a->F;
+        g.act = a->act;
+        g.gated = 1;
+        g.dout = a->dout;
+        g.pre = a->gate_pre;
+        g.pre2 = a->up_pre;
+        g.d1 = dz[0];
+        g.d2 = dz[1];
+        g.parts = act_grad_parts(a->M, a->F, t->cfg.dtype, t->num_sms);
+        g.vec = on16(g.dout, es) && on16(g.pre, 4) && on16(g.pre2, 4);
+        if (!count) FE_TRY(launch_act_grad(g, t->cfg.dtype, st));
+    }
     return product_gradients(t, a->M, a->F, a->K, a->x, weights, dz, 2, a->dx, dw, w, count, st);
 }
 

@@ -94,7 +94,7 @@ __device__ __forceinline__ void epilogue_plain(const Finish& e, int64_t m, int n
 #pragma unroll
         for (int i = 0; i < NV; ++i) z[i] += t[i];
     }
-    if (e.pre) store_row<T, NV>((T*)e.pre + m * e.pre_row + n, have, e.vec, z);
+    if (e.pre) store_row<float, NV>(e.pre + m * e.pre_row + n, have, e.vec, z);
     if (e.act != FE_ACT_NONE) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) z[i] = act_value(e.act, z[i]);
@@ -113,22 +113,40 @@ __device__ __forceinline__ void epilogue_gated(const Finish& e, int64_t m, int n
     const int have = N - n;
     if (have <= 0) return;
     if (e.pre) {
-        store_row<T, NV>((T*)e.pre + m * e.pre_row + n, have, e.vec, g);
-        store_row<T, NV>((T*)e.pre2 + m * e.pre2_row + n, have, e.vec, u);
+        store_row<float, NV>(e.pre + m * e.pre_row + n, have, e.vec, g);
+        store_row<float, NV>(e.pre2 + m * e.pre2_row + n, have, e.vec, u);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) g[i] = act_value(e.act, g[i]) * u[i];
     store_row<T, NV>((T*)e.out + m * e.out_row + n, have, e.vec, g);
 }
 
-// the sum of v over the CTA's threads, in the same order every time; buf: a float per warp
-__device__ __forceinline__ float cta_sum(float v, float* buf) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    v = warp_sum(v);
-    if (lane == 0) buf[warp] = v;
-    __syncthreads();
-    v = lane < warps ? buf[lane] : 0.f;
-    return warp_sum(v);
+// the gradients of a gated pair for the product z = dh, and the pair's own result
+template <typename T, int NV>
+__device__ __forceinline__ void epilogue_gated_grad(const Finish& e, int64_t m, int n, int N, float* z) {
+    const int have = N - n;
+    if (have <= 0) return;
+    float g[NV], u[NV];
+    load_row<float, NV>(e.pre + m * e.pre_row + n, have, e.vec, g);
+    load_row<float, NV>(e.pre2 + m * e.pre2_row + n, have, e.vec, u);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float v, dv;
+        act_both(e.act, g[i], v, dv);
+        g[i] = z[i] * v;
+        dv *= z[i] * u[i];
+        u[i] *= v;
+        z[i] = dv;
+    }
+    store_row<T, NV>((T*)e.out + m * e.out_row + n, have, e.vec, z);
+    store_row<T, NV>((T*)e.out2 + m * e.out2_row + n, have, e.vec, g);
+    store_row<T, NV>((T*)e.out3 + m * e.out3_row + n, have, e.vec, u);
+}
+
+template <typename T, int NV>
+__device__ __forceinline__ void epilogue_one(const Finish& e, int64_t m, int n, int N, float* z) {
+    if (e.kind == FINISH_GATED_GRAD) epilogue_gated_grad<T, NV>(e, m, n, N, z);
+    else epilogue_plain<T, NV>(e, m, n, N, z);
 }
 
 }  // namespace fe

@@ -6,29 +6,32 @@
 
 namespace fe {
 
-// What becomes of a matrix product z (and, gated, of the second product u):
-//   out = act(z + bias) + res, pre = z + bias          gated: out = act(z) u, pre = z, pre2 = u
+// What becomes of a matrix product z (and, GATED, of the second product u):
+//   PLAIN       out = act(z + bias) + res, pre = z + bias
+//   GATED       out = act(z) u, pre = z, pre2 = u
+//   GATED_GRAD  of pre and pre2, as they were stored: out = z pre2 act'(pre), out2 = z act(pre), out3 = act(pre) pre2
+enum FinishKind : int { FINISH_PLAIN = 0, FINISH_GATED = 1, FINISH_GATED_GRAD = 2 };
 struct Finish {
-    int act;
+    int kind, act;
     const void *bias, *res;
     int64_t res_row;
-    void *out, *pre, *pre2;
-    int64_t out_row, pre_row, pre2_row;
+    void *out, *out2, *out3;
+    int64_t out_row, out2_row, out3_row;
+    float *pre, *pre2;
+    int64_t pre_row, pre2_row;
     int vec;  // bias and all rows on 16-byte boundaries
 };
 
 // C [M, N] = sum over segments s of A_s [M, K] B_s [N, K]^T. An operand is stored as it is written
-// here, or (t) with its K index as rows. gated: B_0 and B_1 belong to two products of A_0. twice: a
-// second result A_1 B_0^T goes to out2.
+// here, or (t) with its K index as rows. FINISH_GATED: B_0 and B_1 belong to two products of A_0.
+// twice: a second result A_1 B_0^T goes to e.out2.
 struct GemmArgs {
     int64_t M;
     int N, K;
-    int segs, twice, gated;
+    int segs, twice;
     fe_mat a[2], b[2];
     int a_t, b_t;
     Finish e;
-    void* out2;
-    int64_t out2_row;
     int* status;
 };
 
@@ -77,7 +80,12 @@ struct LogprobArgs {
     int* status;
 };
 
-cudaError_t launch_gemm_simt(const GemmArgs& a, fe_dtype dtype, int num_sms, cudaStream_t st);
+cudaError_t launch_gemm_simt(const GemmArgs& a, int num_sms, cudaStream_t st);  // float32
+cudaError_t launch_gemm_tc(const GemmArgs& a, int num_sms, cudaStream_t st);    // bfloat16
+// whether launch_gemm_tc can read a matrix where it lies, and a copy that it can read
+bool gemm_tc_reads(const fe_mat& m, int64_t rows, int64_t cols);
+cudaError_t launch_pack_rows(const fe_mat& src, const fe_mat& dst, int64_t rows, int64_t cols, int num_sms, cudaStream_t st);
+cudaError_t gemm_tc_prepare();
 // parts of the rows that fe_project_backward's sums and the activation's gradient are split into
 int act_grad_parts(int64_t M, int N, fe_dtype dtype, int num_sms);
 cudaError_t launch_act_grad(const ActGradArgs& a, fe_dtype dtype, cudaStream_t st);
@@ -90,6 +98,6 @@ int64_t norm_backward_plan(NormArgs& a, fe_dtype dtype, int num_sms);
 cudaError_t launch_block_norm_backward(const NormArgs& a, fe_dtype dtype, cudaStream_t st);
 cudaError_t launch_token_logprobs(const LogprobArgs& a, fe_dtype dtype, int num_sms, cudaStream_t st);
 cudaError_t launch_token_logprobs_backward(const LogprobArgs& a, fe_dtype dtype, int num_sms, cudaStream_t st);
-cudaError_t layer_prepare();
+cudaError_t logprobs_prepare();
 
 }  // namespace fe

@@ -486,7 +486,7 @@ cudaError_t launch_token_logprobs_backward(const LogprobArgs& a, fe_dtype dtype,
     return dtype == FE_F32 ? backward<float>(a, num_sms, st) : backward<bf16_t>(a, num_sms, st);
 }
 
-cudaError_t layer_prepare() {
+cudaError_t logprobs_prepare() {
     cudaError_t e;
     const auto wide = [](auto kern) { return cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); };
     if ((e = wide(logprob_kernel<float, true>)) != cudaSuccess || (e = wide(logprob_kernel<float, false>)) != cudaSuccess) return e;

@@ -1,5 +1,6 @@
 // Attention of a draft tree's nodes (or of consecutive tokens) over the cache
 // (fe_tree_attention): the variants and their launches.
+#include "fe_tensor_map.h"
 #include "fe_tree_attn_join.cuh"
 #include "fe_tree_attn_simt.cuh"
 #include "fe_tree_attn_tc.cuh"
@@ -24,20 +25,6 @@ cudaError_t launch_simt(const TreeAttnArgs& args, int num_sms, cudaStream_t st) 
     const cudaError_t e = launch_k(tree_attn_simt_kernel<HD, NI>, dim3(grid), dim3(kSimtThreads), sizeof(SM), st, false, a);
     if (e != cudaSuccess) return e;
     return launch_join<float, HD, 16 * NI>(a, grid, st);
-}
-
-// cuTensorMapEncodeTiled, looked up once (the library does not link the driver)
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled encode_tiled() {
-    static const EncodeTiled fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess) return (EncodeTiled) nullptr;
-        return r == cudaDriverEntryPointSuccess ? (EncodeTiled)p : nullptr;
-    }();
-    return fn;
 }
 
 // Rows of a TMA box: a bfloat16 cache's tiles of 128 slots come in boxes that lie inside one page

@@ -28,7 +28,7 @@ _ARGS = {
     "fe_project": "qii" + 2 * _M + "P" + 3 * _M + "i4xPq",
     "fe_project_backward": "qii" + 6 * _M + "Pi4xPq",
     "fe_gated_ffn": "qii" + 6 * _M + "i4xPq",
-    "fe_gated_ffn_backward": "qii" + 9 * _M + "i4xPq",
+    "fe_gated_ffn_backward": "qiii4x" + 11 * _M + "i4xPq",
     "fe_block_norm": "qii" + 3 * _M + "qPPfff4x" + 2 * _M,
     "fe_block_norm_backward": "qii" + 3 * _M + "qPPfff4x" + 5 * _M + "PPPq",
     "fe_token_logprobs": "qiii4x" + _M + "if" + 7 * "P",
@@ -151,8 +151,8 @@ def _shaped(x, n: int) -> torch.Size:
 
 def fe_project(t: Target, x, w, bias=None, act: str = "none", residual=None, out=None, pre=None, stream=None):
     """act(x w^T + bias) + residual (include/fe_layer.h): x [..., K], w [N, K], bias [N], residual
-    [..., N]; act: "none", "relu", "silu" or "gelu". out may be the residual itself; pre [..., N] takes
-    x w^T + bias, for fe_project_backward."""
+    [..., N]; act: "none", "relu", "silu" or "gelu". out may be the residual itself; pre [..., N], float32,
+    takes x w^T + bias, for fe_project_backward."""
     if _recorded(stream, (out, pre), (x, w, bias, residual)):
         return _Project.apply(t, act, x, w, bias, residual)
     N, K = w.shape
@@ -160,7 +160,7 @@ def fe_project(t: Target, x, w, bias=None, act: str = "none", residual=None, out
     args = (M, N, K, *_mat(x, t.dtype, _shaped(x, K)), *_mat(w, t.dtype, (N, K)), _vec(bias, t.dtype, N),
             *_mat(residual, t.dtype, shape))
     out = _out(out, shape, x, side)
-    args += (*_mat(out, t.dtype, shape), *_mat(pre, t.dtype, shape), _act(act))
+    args += (*_mat(out, t.dtype, shape), *_mat(pre, torch.float32, shape), _act(act))
     if M:
         _call("fe_project", t, side, (x, w, bias, residual, out, pre), args, x.device)
     return out
@@ -179,7 +179,7 @@ def fe_project_backward(t: Target, dout, x=None, w=None, pre=None, act: str = "n
     gw = _out(None, (N, K), like, side) if dw else None
     gb = _out(None, (N,), like, side) if dbias else None
     args = (M, N, K, *_mat(x if dw else None, t.dtype, _shaped(dout, K)), *_mat(w if dx else None, t.dtype, (N, K)),
-            *_mat(dout, t.dtype, _shaped(dout, N)), *_mat(pre, t.dtype, dout.shape), *_mat(gx, t.dtype, _shaped(dout, K)),
+            *_mat(dout, t.dtype, _shaped(dout, N)), *_mat(pre, torch.float32, dout.shape), *_mat(gx, t.dtype, _shaped(dout, K)),
             *_mat(gw, t.dtype, (N, K)), _vec(gb, t.dtype, N), _act(act))
     if M and (dx or dw or dbias):
         _call("fe_project_backward", t, side, (dout, x, w, pre, gx, gw, gb), args, dout.device)
@@ -200,7 +200,7 @@ class _Project(torch.autograd.Function):
     @staticmethod
     def forward(ctx, t, act, x, w, bias, residual):
         need = any(ctx.needs_input_grad[2:5])
-        pre = torch.empty(_shaped(x, w.shape[0]), dtype=x.dtype, device=x.device) if need and act != "none" else None
+        pre = torch.empty(_shaped(x, w.shape[0]), device=x.device) if need and act != "none" else None
         out = fe_project(t, x, w, bias, act, residual, pre=pre)
         ctx.t, ctx.act = t, act
         ctx.save_for_backward(x if ctx.needs_input_grad[3] else None, w if ctx.needs_input_grad[2] else None, pre)
@@ -224,64 +224,67 @@ def fe_gated_ffn(t: Target, x, w_gate, w_up, w_down=None, act: str = "silu", res
                  up_pre=None, stream=None):
     """A gated feed-forward block (include/fe_layer.h): h = act(x w_gate^T) * (x w_up^T) for x [..., K] and
     w_gate, w_up [F, K]; with w_down [N, F] the whole block, h w_down^T + residual (fe_project). gate_pre
-    and up_pre [..., F] take the two products, for fe_gated_ffn_backward."""
+    and up_pre [..., F], float32, take the two products, for fe_gated_ffn_backward."""
+    if w_down is None and residual is not None:
+        raise ValueError("a residual needs w_down")
+    if _recorded(stream, (out, gate_pre, up_pre), (x, w_gate, w_up, w_down, residual)):
+        return _Gated.apply(t, act, x, w_gate, w_up, w_down, residual)
     if w_down is not None:
         h = fe_gated_ffn(t, x, w_gate, w_up, act=act, gate_pre=gate_pre, up_pre=up_pre, stream=stream)
         return fe_project(t, h, w_down, residual=residual, out=out, stream=stream)
-    if residual is not None:
-        raise ValueError("a residual needs w_down")
-    if _recorded(stream, (out, gate_pre, up_pre), (x, w_gate, w_up)):
-        return _Gated.apply(t, act, x, w_gate, w_up)
     F, K = w_gate.shape
     side, shape, M = _side(stream), _shaped(x, F), _rows_of(x)
     args = (M, F, K, *_mat(x, t.dtype, _shaped(x, K)), *_mat(w_gate, t.dtype, (F, K)), *_mat(w_up, t.dtype, (F, K)))
     out = _out(out, shape, x, side)
-    args += (*_mat(out, t.dtype, shape), *_mat(gate_pre, t.dtype, shape), *_mat(up_pre, t.dtype, shape), _act(act))
+    args += (*_mat(out, t.dtype, shape), *_mat(gate_pre, torch.float32, shape), *_mat(up_pre, torch.float32, shape), _act(act))
     if M:
         _call("fe_gated_ffn", t, side, (x, w_gate, w_up, out, gate_pre, up_pre), args, x.device)
     return out
 
 
-def fe_gated_ffn_backward(t: Target, dout, gate_pre, up_pre, x=None, w_gate=None, w_up=None, act: str = "silu", dx: bool = True,
-                          dw: bool = True, stream=None) -> tuple:
-    """Gradients (dx, dw_gate, dw_up) of fe_gated_ffn without w_down for dout [..., F]. The weights are
-    needed for dx, x for dw."""
-    if (dx and (w_gate is None or w_up is None)) or (dw and x is None):
-        raise ValueError("dx needs w_gate and w_up, dw needs x")
-    if not (dx or dw):
-        return None, None, None
-    F, M = dout.shape[-1], _rows_of(dout)
-    K = w_gate.shape[1] if dx else x.shape[-1]
-    side, shape = _side(stream), dout.shape
+def fe_gated_ffn_backward(t: Target, dout, gate_pre, up_pre, x=None, w_gate=None, w_up=None, w_down=None, act: str = "silu",
+                          dx: bool = True, dw: bool = True, dw_down: bool | None = None, stream=None) -> tuple:
+    """Gradients (dx, dw_gate, dw_up, dw_down) of fe_gated_ffn for dout, [..., F] or with w_down [..., N], None for
+    those not asked for (dw_down: by default with w_down). w_gate and w_up are needed for dx, x for dw."""
+    dw_down = w_down is not None if dw_down is None else dw_down
+    if (dx and (w_gate is None or w_up is None)) or (dw and x is None) or (dw_down and w_down is None):
+        raise ValueError("dx needs w_gate and w_up, dw needs x, dw_down needs w_down")
+    if not (dx or dw or dw_down):
+        return None, None, None, None
+    F, M, N = gate_pre.shape[-1], _rows_of(dout), dout.shape[-1]
+    K = w_gate.shape[1] if dx else x.shape[-1] if dw else 1
+    side, shape = _side(stream), _shaped(dout, F)
     gx = _out(None, _shaped(dout, K), dout, side) if dx else None
     gg, gu = (_out(None, (F, K), dout, side) if dw else None for _ in range(2))
-    args = (M, F, K, *_mat(x if dw else None, t.dtype, _shaped(dout, K)), *_mat(w_gate if dx else None, t.dtype, (F, K)),
-            *_mat(w_up if dx else None, t.dtype, (F, K)), *_mat(dout, t.dtype, shape), *_mat(gate_pre, t.dtype, shape),
-            *_mat(up_pre, t.dtype, shape), *_mat(gx, t.dtype, _shaped(dout, K)), *_mat(gg, t.dtype, (F, K)),
-            *_mat(gu, t.dtype, (F, K)), _act(act))
+    gd = _out(None, (N, F), dout, side) if dw_down else None
+    args = (M, F, K, N, *_mat(x if dw else None, t.dtype, _shaped(dout, K)), *_mat(w_gate if dx else None, t.dtype, (F, K)),
+            *_mat(w_up if dx else None, t.dtype, (F, K)), *_mat(w_down, t.dtype, (N, F)),
+            *_mat(dout, t.dtype, shape if w_down is None else dout.shape), *_mat(gate_pre, torch.float32, shape),
+            *_mat(up_pre, torch.float32, shape), *_mat(gx, t.dtype, _shaped(dout, K)), *_mat(gg, t.dtype, (F, K)),
+            *_mat(gu, t.dtype, (F, K)), *_mat(gd, t.dtype, (N, F)), _act(act))
     if M:
-        _call("fe_gated_ffn_backward", t, side, (dout, x, w_gate, w_up, gate_pre, up_pre, gx, gg, gu), args, dout.device)
+        _call("fe_gated_ffn_backward", t, side, (dout, x, w_gate, w_up, w_down, gate_pre, up_pre, gx, gg, gu, gd), args, dout.device)
     else:
-        _zero(side, gg, gu)
-    return gx, gg, gu
+        _zero(side, gg, gu, gd)
+    return gx, gg, gu, gd
 
 
 class _Gated(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, t, act, x, w_gate, w_up):
-        g, u = (torch.empty(_shaped(x, w_gate.shape[0]), dtype=x.dtype, device=x.device) for _ in range(2))
+    def forward(ctx, t, act, x, w_gate, w_up, w_down, residual):
+        g, u = (torch.empty(_shaped(x, w_gate.shape[0]), device=x.device) for _ in range(2))
         ctx.t, ctx.act = t, act
-        _, _, nx, ng, nu = ctx.needs_input_grad
-        ctx.save_for_backward(g, u, x if ng or nu else None, w_gate if nx else None, w_up if nx else None)
-        return fe_gated_ffn(t, x, w_gate, w_up, act=act, gate_pre=g, up_pre=u)
+        _, _, nx, ng, nu, _, _ = ctx.needs_input_grad
+        ctx.save_for_backward(g, u, x if ng or nu else None, w_gate if nx else None, w_up if nx else None, w_down)
+        return fe_gated_ffn(t, x, w_gate, w_up, w_down, act, residual, gate_pre=g, up_pre=u)
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
-        g, u, x, w_gate, w_up = ctx.saved_tensors
-        _, _, nx, ng, nu = ctx.needs_input_grad
-        gx, gg, gu = fe_gated_ffn_backward(ctx.t, _dense(dout), g, u, x, w_gate, w_up, ctx.act, nx, ng or nu)
-        return None, None, gx, gg if ng else None, gu if nu else None
+        g, u, x, w_gate, w_up, w_down = ctx.saved_tensors
+        _, _, nx, ng, nu, nd, nr = ctx.needs_input_grad
+        gx, gg, gu, gd = fe_gated_ffn_backward(ctx.t, _dense(dout), g, u, x, w_gate, w_up, w_down, ctx.act, nx, ng or nu, nd)
+        return None, None, gx, gg if ng else None, gu if nu else None, gd, dout if nr else None
 
 
 # ---- fe_block_norm --------------------------------------------------------------------------

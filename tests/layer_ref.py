@@ -69,8 +69,8 @@ def project(c, x, w, bias, residual, dout=None):
         g = dout.double()
         grad = g * da
         eg = torch.zeros_like(grad)
-        if c["act"] != "none":  # from the stored z, and rounded
-            _, ed = act_slack(c["act"], z, dz + u * (z.abs() + dz))
+        if c["act"] != "none":  # rounded
+            _, ed = act_slack(c["act"], z, dz)
             eg = g.abs() * ed
             er = eg + u * (grad.abs() + eg)
         else:
@@ -84,21 +84,26 @@ def project(c, x, w, bias, residual, dout=None):
     return got
 
 
-def gated(c, x, wg, wu, dout=None):
+def gated(c, x, wg, wu, dout=None, wd=None):
+    """With wd [N, F], dout [M, N] is the gradient of the block's result behind it."""
     u = c["unit"]
     pg, pu = Product(x, wg), Product(x, wu)
     a, da = act(c["act"], pg.v)
-    ea, _ = act_slack(c["act"], pg.v, pg.err)
+    ea, ed = act_slack(c["act"], pg.v, pg.err)
     h = a * pu.v
     eh = ea * (pu.v.abs() + pu.err) + a.abs() * pu.err + 2.0 ** -23 * h.abs()
-    got = {"out": (h, eh + u * (h.abs() + eh)), "hidden": (h, eh)}
+    eh = eh + u * (h.abs() + eh)
+    got = {"out": (h, eh)}
     if dout is not None:
-        g = dout.double()
-        sg, su = pg.err + u * (pg.v.abs() + pg.err), pu.err + u * (pu.v.abs() + pu.err)  # the stored products
-        va, vd = act_slack(c["act"], pg.v, sg)
+        g, e0 = dout.double(), 0.0
+        if wd is not None:
+            q = Product(g, wd.double().T)
+            p = Product(g.T, h.T, db=eh.T)
+            got["dw_down"] = (p.v, p.err + u * (p.v.abs() + p.err))
+            g, e0 = q.v, q.err
         dg, du = g * pu.v * da, g * a
-        eg = g.abs() * ((pu.v.abs() + su) * vd + su * da.abs()) + 2.0 ** -22 * dg.abs()
-        eu = g.abs() * va + 2.0 ** -23 * du.abs()
+        eg = (g.abs() + e0) * ((pu.v.abs() + pu.err) * ed + pu.err * da.abs()) + e0 * (pu.v * da).abs() + 2.0 ** -22 * dg.abs()
+        eu = (g.abs() + e0) * ea + e0 * a.abs() + 2.0 ** -23 * du.abs()
         eg, eu = eg + u * (dg.abs() + eg), eu + u * (du.abs() + eu)
         q = Product(torch.cat([dg, du], 1), torch.cat([wg, wu], 0).double().T, torch.cat([eg, eu], 1))
         got["dx"] = (q.v, q.err + u * (q.v.abs() + q.err))

@@ -57,6 +57,11 @@ def test_gated_gradients(act):
     agrees(lambda v: f(x=v), x, got["dx"][0], g)
     agrees(lambda v: f(wg=v), wg, got["dw_gate"][0], g)
     agrees(lambda v: f(wu=v), wu, got["dw_up"][0], g)
+    wd, do = normal(g, 3, 6), normal(g, 5, 3)  # the whole block
+    f = lambda **k: (ref.gated(c, k.get("x", x), wg, wu)["out"][0] @ k.get("wd", wd).T * do).sum()
+    got = ref.gated(c, x, wg, wu, do, wd)
+    agrees(lambda v: f(x=v), x, got["dx"][0], g)
+    agrees(lambda v: f(wd=v), wd, got["dw_down"][0], g)
 
 
 def test_relu_gradient_away_from_its_kink():
@@ -119,8 +124,8 @@ MEMBERS = {  # each with the format characters before it
     "fe_project": dict(M=0, N=1, K=2, x=3, w=5, bias=7, residual=8, out=10, pre=12, act=14, work=16, work_bytes=17),
     "fe_project_backward": dict(M=0, N=1, K=2, x=3, w=5, dout=7, pre=9, dx=11, dw=13, dbias=15, act=16, work=18, work_bytes=19),
     "fe_gated_ffn": dict(M=0, F=1, K=2, x=3, w_gate=5, w_up=7, out=9, gate_pre=11, up_pre=13, act=15, work=17, work_bytes=18),
-    "fe_gated_ffn_backward": dict(M=0, F=1, K=2, x=3, w_gate=5, w_up=7, dout=9, gate_pre=11, up_pre=13, dx=15, dw_gate=17, dw_up=19,
-                                  act=21, work=23, work_bytes=24),
+    "fe_gated_ffn_backward": dict(M=0, F=1, K=2, N=3, x=5, w_gate=7, w_up=9, w_down=11, dout=13, gate_pre=15, up_pre=17, dx=19, dw_gate=21,
+                                  dw_up=23, dw_down=25, act=27, work=29, work_bytes=30),
     "fe_block_norm": dict(R=0, d=1, post=2, x=3, z=5, gate=7, gate_rows=9, post_w=10, pre_w=11, scale=12, offset=13, eps=14, y=16, n=18),
     "fe_block_norm_backward": dict(R=0, d=1, post=2, x=3, z=5, gate=7, gate_rows=9, post_w=10, pre_w=11, scale=12, offset=13, eps=14,
                                    dy=16, dn=18, dx=20, dz=22, dgate=24, dpost_w=26, dpre_w=27, work=28, work_bytes=29),
@@ -176,7 +181,7 @@ def good(name):
         "fe_project": [8, 64, 64, *m(), *m(), P, *m(), *m(), *none, 1, 0, 0],
         "fe_project_backward": [8, 64, 64, *m(), *m(), *m(), *m(), *m(), *m(), P, 1, P, 1 << 30],
         "fe_gated_ffn": [8, 64, 64, *m(), *m(), *m(), *m(), *none, *none, 2, 0, 0],
-        "fe_gated_ffn_backward": [8, 64, 64, *(m() * 9), 2, P, 1 << 30],
+        "fe_gated_ffn_backward": [8, 64, 64, 64, *(m() * 11), 2, P, 1 << 30],
         "fe_block_norm": [8, 64, 1, *m(), *m(), *m(), 4, P, P, 1.0, 0.0, 1e-5, *m(), *m()],
         "fe_block_norm_backward": [8, 64, 1, *m(), *m(), *m(), 4, P, P, 1.0, 0.0, 1e-5, *(m() * 5), P, P, P, 1 << 30],
         "fe_token_logprobs": [8, 64, 2, 3, *m(), 0, 1.0, P, P, P, P, P, P, P],
@@ -202,7 +207,8 @@ SPOILT = {
     "fe_project_backward": [("dout", 0), ("w", 0), ("x", 0), ("pre", 0), ("dx", (P, 63)), ("dw", (P, 0)), ("dbias", P + 2), ("N", 0),
                             ("work", 0), ("work", P + 16), ("work_bytes", 100), ("act", 9)],
     "fe_gated_ffn": [("gate_pre", P), ("up_pre", P), ("out", (P, 10)), ("w_up", 0), ("w_gate", 0), ("F", 0), ("act", 7), ("M", -5)],
-    "fe_gated_ffn_backward": [("dw_up", 0), ("dw_gate", 0), ("w_up", 0), ("x", 0), ("gate_pre", 0), ("up_pre", 0), ("work_bytes", 0),
+    "fe_gated_ffn_backward": [("dw_up", 0), ("dw_gate", 0), ("w_up", 0), ("x", 0), ("gate_pre", 0), ("up_pre", 0), ("work_bytes", 0), ("w_down", 0), ("N", 0),
+                              ("dw_down", (P, 63)),
                               ("dx", (P, 1)), ("dout", 0)],
     "fe_block_norm": [("R", -1), ("d", 0), ("z", 0), ("gate_rows", 0), ("scale", math.nan), ("offset", math.inf), ("eps", -1.0),
                       ("eps", math.nan), ("y", (P, 63)), ("n", (P, 1)), ("x", 0), ("post_w", P + 1), ("x", P + 1)],
