@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kGradWarps * 32) act_grad_kernel(const __grid_
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     float v, dv;
-                    act_both(a.act, z[i], v, dv);
+                    act_both<kCoarse<T>>(a.act, z[i], v, dv);
                     z[i] = d[i] * v;
                     d[i] = d[i] * u[i] * dv;
                 }
@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kGradWarps * 32) act_grad_kernel(const __grid_
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     float v, dv;
-                    act_both(a.act, z[i], v, dv);
+                    act_both<kCoarse<T>>(a.act, z[i], v, dv);
                     d[i] *= dv;
                 }
             }

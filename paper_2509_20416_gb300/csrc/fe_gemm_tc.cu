@@ -3,7 +3,7 @@
 //
 // Persistent pairs of CTAs (cta_group::2) make tiles of 256 x BN: each CTA brings, by TMA, 128 rows of A
 // and BN / 2 of B in slices of 64 of the summed index, so that an SM reads half of what a CTA of its own
-// would for the same products. Warp 0 copies, warp 1 of the first CTA issues the products, warps 2 to 5
+// would for the same products. Warp 0 copies, warp 1 of the first CTA issues the products, warps 2 to 9
 // finish a tile (bias, activation, residual, gate, rounding) while the next one is summed in the
 // other half of tensor memory. The MN-major operand forms spare the gradients every transpose:
 // dx = dz w reads w by columns, dw = dz^T x both operands.
@@ -14,16 +14,19 @@ namespace fe {
 
 namespace {
 
-constexpr int kTcThreads = 192;
+constexpr int kFinishWarps = 8;
+constexpr int kTcThreads = 64 + 32 * kFinishWarps;
 constexpr int kTileM = 256, kSliceK = 64;
 
 template <int BN>
 struct TcTile {
     static constexpr int kA = 128 * kSliceK * 2, kB = BN / 2 * kSliceK * 2;
-    static constexpr int kStages = BN == 256 ? 6 : 8;
+    static constexpr int kStages = BN == 256 ? 5 : 7;
     static constexpr int kRing = kStages * (kA + kB);
+    static constexpr int kStaging = kFinishWarps * 4096;  // a warp's 32 x 32 floats
     static constexpr int kTmem = 2 * BN;  // two accumulators
-    static constexpr int kSmem = kRing + 1024 /* alignment */ + 512;
+    static constexpr int kSmem = kRing + kStaging + 1024 /* alignment */ + 512;
+    static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
 };
 
 struct TcBarriers {
@@ -53,13 +56,217 @@ struct TileWalk {
     }
 };
 
+// four consecutive columns of bfloat16 as they are stored, and of float32
+__device__ __forceinline__ uint2 load4(const bf16_t* p, int have, bool vec) {
+    if (vec && have >= 4) return *reinterpret_cast<const uint2*>(p);
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = i < have ? p[i].bits : 0u;
+    return make_uint2(x[0] | x[1] << 16, x[2] | x[3] << 16);
+}
+__device__ __forceinline__ float4 load4(const float* p, int have, bool vec) {
+    if (vec && have >= 4) return *reinterpret_cast<const float4*>(p);
+    return make_float4(have > 0 ? p[0] : 0.f, have > 1 ? p[1] : 0.f, have > 2 ? p[2] : 0.f, have > 3 ? p[3] : 0.f);
+}
+__device__ __forceinline__ void widen4(const uint2& x, float* f) {
+    f[0] = __uint_as_float(x.x << 16), f[1] = __uint_as_float(x.x & 0xFFFF0000u);
+    f[2] = __uint_as_float(x.y << 16), f[3] = __uint_as_float(x.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void store4(bf16_t* p, int have, bool vec, const float* f) {
+    if (vec && have >= 4) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) store_one(p + i, f[i]);
+    }
+}
+__device__ __forceinline__ void store4(float* p, int have, bool vec, const float* f) {
+    if (vec && have >= 4) {
+        *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < have) p[i] = f[i];
+    }
+}
+
+// A warp's 32 x 32 block turned from a row a lane (as tensor memory gives it) to four columns a lane, 8
+// lanes a row, so that rows meet global memory in whole sectors. 16-byte chunk c of row r lies at c ^ (r & 7).
+__device__ __forceinline__ void stage_rows(float* buf, uint32_t d, int lane) {
+    float z[32];
+    tc_ld32(d, z);
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        *reinterpret_cast<float4*>(buf + lane * 32 + ((c ^ (lane & 7)) << 2)) = make_float4(z[4 * c], z[4 * c + 1], z[4 * c + 2], z[4 * c + 3]);
+    __syncwarp();
+}
+__device__ __forceinline__ void staged(const float* buf, int row, int chunk, float* f) {
+    const float4 x = *reinterpret_cast<const float4*>(buf + row * 32 + ((chunk ^ (row & 7)) << 2));
+    f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w;
+}
+
+// A warp's part of a tile: 32 rows from m0 on, of which it takes columns n0 + 32 half, + 64, ... below n0 +
+// width. A lane has four columns of every fourth row; the rows are `left` (none: 0).
+struct WarpTile {
+    const Finish& e;
+    uint32_t d, d2;  // tensor memory: the product, and the gated pair's second
+    int64_t m0;
+    int left, n0, width, N, lane;
+    float* buf;
+    __device__ __forceinline__ int row(int i) const { return 4 * i + (lane >> 3); }
+    __device__ __forceinline__ int chunk() const { return lane & 7; }
+    __device__ __forceinline__ bool inside(int c) const { return c < width && n0 + c < N; }
+    __device__ __forceinline__ int have(int c) const { return N - n0 - c - 4 * chunk(); }
+    template <typename T>
+    __device__ __forceinline__ T* at(void* base, int64_t stride, int c) const {
+        return (T*)base + (m0 + row(0)) * stride + n0 + c + 4 * chunk();
+    }
+};
+
+// act(z + bias) + res. What the next block reads of the residual is in flight while a block is finished.
+__device__ __forceinline__ void residual_rows(const WarpTile& w, int c, uint2* r) {
+    const bf16_t* p = w.at<bf16_t>((void*)w.e.res, w.e.res_row, c);
+    const int have = w.inside(c) ? w.have(c) : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = load4(p + 4 * i * w.e.res_row, w.row(i) < w.left ? have : 0, w.e.vec);
+}
+template <typename Wait>
+__device__ __forceinline__ bool finish_plain(const WarpTile& w, int half, const Wait& wait) {
+    const Finish& e = w.e;
+    uint2 next[8], r[8];
+    if (e.res) residual_rows(w, half * 32, next);
+    if (!wait()) return false;
+    for (int c = half * 32; w.inside(c); c += 64) {
+        const int have = w.have(c);
+        float b[4] = {0.f, 0.f, 0.f, 0.f};
+        if (e.bias) widen4(load4((const bf16_t*)e.bias + w.n0 + c + 4 * w.chunk(), have, e.vec), b);
+        if (e.res) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[i] = next[i];
+            residual_rows(w, c + 64, next);
+        }
+        stage_rows(w.buf, w.d + c, w.lane);
+        float* pre = w.at<float>(e.pre, e.pre_row, c);
+        bf16_t* out = w.at<bf16_t>(e.out, e.out_row, c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float z[4];
+            staged(w.buf, w.row(i), w.chunk(), z);
+            if (w.row(i) >= w.left) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] += b[j];
+            if (e.pre) store4(pre + 4 * i * e.pre_row, have, e.vec, z);
+            if (e.act != FE_ACT_NONE) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] = act_value<true>(e.act, z[j]);
+            }
+            if (e.res) {
+                float t[4];
+                widen4(r[i], t);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[j] += t[j];
+            }
+            store4(out + 4 * i * e.out_row, have, e.vec, z);
+        }
+        __syncwarp();  // (the buffer's next block)
+    }
+    return true;
+}
+
+// act(z) u
+__device__ __forceinline__ void finish_gated(const WarpTile& w, int half) {
+    const Finish& e = w.e;
+    for (int c = half * 32; w.inside(c); c += 64) {
+        const int have = w.have(c);
+        float u[8][4];
+        stage_rows(w.buf, w.d2 + c, w.lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) staged(w.buf, w.row(i), w.chunk(), u[i]);
+        __syncwarp();
+        stage_rows(w.buf, w.d + c, w.lane);
+        float *pre = w.at<float>(e.pre, e.pre_row, c), *pre2 = w.at<float>(e.pre2, e.pre2_row, c);
+        bf16_t* out = w.at<bf16_t>(e.out, e.out_row, c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float g[4];
+            staged(w.buf, w.row(i), w.chunk(), g);
+            if (w.row(i) >= w.left) continue;
+            if (e.pre) {
+                store4(pre + 4 * i * e.pre_row, have, e.vec, g);
+                store4(pre2 + 4 * i * e.pre2_row, have, e.vec, u[i]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[j] = act_value<true>(e.act, g[j]) * u[i][j];
+            store4(out + 4 * i * e.out_row, have, e.vec, g);
+        }
+        __syncwarp();
+    }
+}
+
+// The gradients of a gated pair: half a block's (16 rows') stored products are in flight while the half before
+// is finished.
+__device__ __forceinline__ void pair_rows(const WarpTile& w, int c, int h, float4* g, float4* u) {
+    const float *p = w.at<float>(w.e.pre, w.e.pre_row, c), *q = w.at<float>(w.e.pre2, w.e.pre2_row, c);
+    const int have = w.inside(c) ? w.have(c) : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 4 * h + i, k = w.row(r) < w.left ? have : 0;
+        g[i] = load4(p + 4 * r * w.e.pre_row, k, w.e.vec);
+        u[i] = load4(q + 4 * r * w.e.pre2_row, k, w.e.vec);
+    }
+}
+template <typename Wait>
+__device__ __forceinline__ bool finish_gated_grad(const WarpTile& w, int half, const Wait& wait) {
+    const Finish& e = w.e;
+    float4 ng[4], nu[4];
+    pair_rows(w, half * 32, 0, ng, nu);
+    if (!wait()) return false;
+    for (int c = half * 32; w.inside(c); c += 64) {
+        const int have = w.have(c);
+        stage_rows(w.buf, w.d + c, w.lane);
+        bf16_t *out = w.at<bf16_t>(e.out, e.out_row, c), *out2 = w.at<bf16_t>(e.out2, e.out2_row, c),
+               *out3 = w.at<bf16_t>(e.out3, e.out3_row, c);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float4 cg[4], cu[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                cg[i] = ng[i];
+                cu[i] = nu[i];
+            }
+            pair_rows(w, h ? c + 64 : c, h ^ 1, ng, nu);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = 4 * h + i;
+                float z[4], g[4] = {cg[i].x, cg[i].y, cg[i].z, cg[i].w}, u[4] = {cu[i].x, cu[i].y, cu[i].z, cu[i].w};
+                staged(w.buf, w.row(r), w.chunk(), z);
+                if (w.row(r) >= w.left) continue;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float v, dv;
+                    act_both<true>(e.act, g[j], v, dv);
+                    g[j] = z[j] * v;
+                    z[j] *= u[j] * dv;
+                    u[j] *= v;
+                }
+                store4(out + 4 * r * e.out_row, have, e.vec, z);
+                store4(out2 + 4 * r * e.out2_row, have, e.vec, g);
+                store4(out3 + 4 * r * e.out3_row, have, e.vec, u);
+            }
+        }
+        __syncwarp();
+    }
+    return true;
+}
+
 template <int BN, bool AT, bool BT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
     gemm_tc_kernel(const __grid_constant__ GemmArgs g, const __grid_constant__ TcMaps maps) {
     using S = TcTile<BN>;
     extern __shared__ unsigned char raw[];
     unsigned char* const ring = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-    TcBarriers& bar = *reinterpret_cast<TcBarriers*>(ring + S::kRing);
+    TcBarriers& bar = *reinterpret_cast<TcBarriers*>(ring + S::kRing + S::kStaging);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
     const bool gated = g.e.kind == FINISH_GATED;
@@ -75,7 +282,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bar.done[i], 1);
-            mbar_init(&bar.free[i], 8);  // the finishing warps of both CTAs
+            mbar_init(&bar.free[i], 2 * kFinishWarps);  // the finishing warps of both CTAs
         }
         mbar_init(&bar.drain, 1);
         mbar_fence_init();
@@ -156,35 +363,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
         }
         __syncwarp();
     } else if (warp >= 2) {  // ---- results
-        const int quarter = warp & 3;
+        const int quarter = warp & 3, half = (warp - 2) >> 2;  // a quarter of the rows, every second 32 columns
+        float* const buf_rows = (float*)(ring + S::kRing) + (warp - 2) * 1024;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        Finish e = g.e;
         uint32_t i = 0;
         for (int64_t t = first; t < walk.all; t += step, ++i) {
             int prob;
             int64_t mt, nt;
             walk.at(t, prob, mt, nt);
             const uint32_t buf = i & 1, use = i >> 1, d = tmem + buf * BN + lanes;
-            bool ok = true;
-            if (lane == 0) ok = mbar_wait(&bar.done[buf], use & 1, g.status);
-            if (!__shfl_sync(0xffffffffu, ok, 0)) break;
-            tc_fence_after();
-            const int64_t m = mt * kTileM + rank * 128 + quarter * 32 + lane;
-            const int n0 = (int)(nt * width);
-            Finish e = g.e;
+            const auto wait = [&] {
+                bool ok = true;
+                if (lane == 0) ok = mbar_wait(&bar.done[buf], use & 1, g.status);
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                tc_fence_after();
+                return ok;
+            };
             if (prob) {
-                e.out = e.out2;
-                e.out_row = e.out2_row;
+                e.out = g.e.out2;
+                e.out_row = g.e.out2_row;
             }
-            for (int c = 0; c < width && n0 + c < g.N; c += 32) {
-                float z[32];
-                tc_ld32(d + c, z);
-                if (gated) {
-                    float u[32];
-                    tc_ld32(d + BN / 2 + c, u);
-                    if (m < g.M) epilogue_gated<bf16_t, 32>(e, m, n0 + c, g.N, z, u);
-                } else if (m < g.M) {
-                    epilogue_one<bf16_t, 32>(e, m, n0 + c, g.N, z);
-                }
+            const int64_t m0 = mt * kTileM + rank * 128 + quarter * 32;
+            const WarpTile w{e, d, d + BN / 2, m0, (int)(m0 < g.M ? min((int64_t)32, g.M - m0) : 0), (int)(nt * width), width, g.N, lane, buf_rows};
+            if (gated) {
+                if (!wait()) break;
+                finish_gated(w, half);
+            } else if (e.kind == FINISH_GATED_GRAD) {
+                if (!finish_gated_grad(w, half, wait)) break;
+            } else if (!finish_plain(w, half, wait)) {
+                break;
             }
             tc_fence_before();
             __syncwarp();
@@ -196,17 +404,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
     if (warp == 2) tc2_dealloc(tmem, S::kTmem);
 }
 
-// A matrix [rows, cols] of bfloat16 in boxes of 64 columns
-bool make_map(CUtensorMap* map, const fe_mat& m, int64_t rows, int64_t cols, int box_rows) {
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? m.row : (cols + 7) / 8 * 8) * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
-    const EncodeTiled encode = encode_tiled();
-    return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, m.p, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int BN, bool AT, bool BT>
 cudaError_t launch_pairs(const GemmArgs& g, int num_sms, cudaStream_t st) {
     using S = TcTile<BN>;
@@ -214,10 +411,10 @@ cudaError_t launch_pairs(const GemmArgs& g, int num_sms, cudaStream_t st) {
     const bool gated = g.e.kind == FINISH_GATED;
     for (int i = 0; i < 2; ++i) {
         if (i == 0 || g.segs == 2 || g.twice) {
-            if (!(AT ? make_map(&maps.a[i], g.a[i], g.K, g.M, 64) : make_map(&maps.a[i], g.a[i], g.M, g.K, 128))) return cudaErrorInvalidValue;
+            if (!(AT ? tensor_map_bf16(&maps.a[i], g.a[i], g.K, g.M, 64) : tensor_map_bf16(&maps.a[i], g.a[i], g.M, g.K, 128))) return cudaErrorInvalidValue;
         }
         if (i == 0 || g.segs == 2 || gated) {
-            if (!(BT ? make_map(&maps.b[i], g.b[i], g.K, g.N, 64) : make_map(&maps.b[i], g.b[i], g.N, g.K, BN / 2))) return cudaErrorInvalidValue;
+            if (!(BT ? tensor_map_bf16(&maps.b[i], g.b[i], g.K, g.N, 64) : tensor_map_bf16(&maps.b[i], g.b[i], g.N, g.K, BN / 2))) return cudaErrorInvalidValue;
         }
     }
     const int width = gated ? BN / 2 : BN;

@@ -111,7 +111,7 @@ fe_status gemm(const fe_target* t, GemmArgs& g, Workspace& w, bool count, cudaSt
             s = g.b_t ? readable(g.b[i], g.K, g.N) : readable(g.b[i], g.N, g.K);
         if (s != FE_OK) return s;
     }
-    if (!count) FE_TRY(launch_gemm_tc(g, t->num_sms, st));
+    if (!count) FE_TRY(gemm_few_takes(g) ? launch_gemm_few(g, t->num_sms, st) : launch_gemm_tc(g, t->num_sms, st));
     return FE_OK;
 }
 

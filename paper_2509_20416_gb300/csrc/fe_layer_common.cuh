@@ -9,21 +9,27 @@ namespace fe {
 __device__ __forceinline__ float load_one(const float* p) { return *p; }
 __device__ __forceinline__ float load_one(const bf16_t* p) { return bf16_to_f32(p->bits); }
 
-// 1 / (1 + e^-x); 0 and 1 at the ends
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+// 1 / (1 + e^-x); 0 and 1 at the ends. FAST: by the hardware's approximations, off by some 2^-21, for
+// results that are rounded to bfloat16 (a tile of 128 x 256 is finished while the next is summed only with them)
+template <bool FAST>
+__device__ __forceinline__ float sigmoid(float x) {
+    if (FAST) return __fdividef(1.0f, 1.0f + ex2_approx(-kLog2e * x));
+    return 1.0f / (1.0f + expf(-x));
+}
 
 constexpr float kGeluA = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 constexpr float kGeluB = 0.07135481627260025f;  // kGeluA * 0.044715
 
 // (1 + tanh(u)) / 2 = sigmoid(2 u). Past |z| = 12 the cube adds nothing to a sigmoid that is 0 or 1
 // in float32, and a square that overflows would make the gradient's 0 times it NaN.
+template <bool FAST>
 __device__ __forceinline__ float act_value(int act, float z) {
     switch (act) {
         case FE_ACT_RELU: return z < 0.f ? 0.f : z;
-        case FE_ACT_SILU: return z * sigmoid(z);
+        case FE_ACT_SILU: return z * sigmoid<FAST>(z);
         case FE_ACT_GELU: {
             const float c = fminf(fmaxf(z, -12.f), 12.f);
-            const float s = sigmoid(c * (kGeluA + kGeluB * c * c));
+            const float s = sigmoid<FAST>(c * (kGeluA + kGeluB * c * c));
             return (z < -12.f && z > -INFINITY) ? 0.f : z * s;
         }
         default: return z;
@@ -31,6 +37,7 @@ __device__ __forceinline__ float act_value(int act, float z) {
 }
 
 // act(z) and act'(z)
+template <bool FAST>
 __device__ __forceinline__ void act_both(int act, float z, float& v, float& dv) {
     switch (act) {
         case FE_ACT_RELU:
@@ -38,14 +45,14 @@ __device__ __forceinline__ void act_both(int act, float z, float& v, float& dv) 
             dv = z > 0.f ? 1.f : (z <= 0.f ? 0.f : z);
             return;
         case FE_ACT_SILU: {
-            const float s = sigmoid(z);
+            const float s = sigmoid<FAST>(z);
             v = z * s;
             dv = s * (1.f + z * (1.f - s));
             return;
         }
         case FE_ACT_GELU: {
             const float c = fminf(fmaxf(z, -12.f), 12.f);
-            const float s = sigmoid(c * (kGeluA + kGeluB * c * c));
+            const float s = sigmoid<FAST>(c * (kGeluA + kGeluB * c * c));
             v = (z < -12.f && z > -INFINITY) ? 0.f : z * s;
             dv = s + c * s * (1.f - s) * (kGeluA + 3.f * kGeluB * c * c);
             if (z != z) dv = z;
@@ -56,6 +63,9 @@ __device__ __forceinline__ void act_both(int act, float z, float& v, float& dv) 
             dv = 1.f;
     }
 }
+
+// a template parameter for the type whose results are rounded coarsely
+template <typename T> constexpr bool kCoarse = sizeof(T) == 2;
 
 // N consecutive elements of a row (N a multiple of 16 bytes where vec, else any) from and to floats;
 // elements from `have` on are left out
@@ -97,7 +107,7 @@ __device__ __forceinline__ void epilogue_plain(const Finish& e, int64_t m, int n
     if (e.pre) store_row<float, NV>(e.pre + m * e.pre_row + n, have, e.vec, z);
     if (e.act != FE_ACT_NONE) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) z[i] = act_value(e.act, z[i]);
+        for (int i = 0; i < NV; ++i) z[i] = act_value<false>(e.act, z[i]);
     }
     if (e.res) {
         load_row<T, NV>((const T*)e.res + m * e.res_row + n, have, e.vec, t);
@@ -117,7 +127,7 @@ __device__ __forceinline__ void epilogue_gated(const Finish& e, int64_t m, int n
         store_row<float, NV>(e.pre2 + m * e.pre2_row + n, have, e.vec, u);
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i) g[i] = act_value(e.act, g[i]) * u[i];
+    for (int i = 0; i < NV; ++i) g[i] = act_value<false>(e.act, g[i]) * u[i];
     store_row<T, NV>((T*)e.out + m * e.out_row + n, have, e.vec, g);
 }
 
@@ -132,7 +142,7 @@ __device__ __forceinline__ void epilogue_gated_grad(const Finish& e, int64_t m, 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         float v, dv;
-        act_both(e.act, g[i], v, dv);
+        act_both<false>(e.act, g[i], v, dv);
         g[i] = z[i] * v;
         dv *= z[i] * u[i];
         u[i] *= v;

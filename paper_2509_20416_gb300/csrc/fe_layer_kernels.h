@@ -86,6 +86,10 @@ cudaError_t launch_gemm_tc(const GemmArgs& a, int num_sms, cudaStream_t st);    
 bool gemm_tc_reads(const fe_mat& m, int64_t rows, int64_t cols);
 cudaError_t launch_pack_rows(const fe_mat& src, const fe_mat& dst, int64_t rows, int64_t cols, int num_sms, cudaStream_t st);
 cudaError_t gemm_tc_prepare();
+// the same for few rows of A: whether the kernel takes a product
+bool gemm_few_takes(const GemmArgs& a);
+cudaError_t launch_gemm_few(const GemmArgs& a, int num_sms, cudaStream_t st);
+cudaError_t gemm_few_prepare();
 // parts of the rows that fe_project_backward's sums and the activation's gradient are split into
 int act_grad_parts(int64_t M, int N, fe_dtype dtype, int num_sms);
 cudaError_t launch_act_grad(const ActGradArgs& a, fe_dtype dtype, cudaStream_t st);
