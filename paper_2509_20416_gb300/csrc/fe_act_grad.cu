@@ -19,32 +19,42 @@ __global__ void __launch_bounds__(kGradWarps * 32) act_grad_kernel(const __grid_
     const int64_t r0 = a.M * blockIdx.y / a.parts, r1 = a.M * (blockIdx.y + 1) / a.parts;
     float sum[V] = {};
     if (have > 0) {
-#pragma unroll 2
-        for (int64_t r = r0 + warp; r < r1; r += kGradWarps) {
-            float d[V], z[V], u[V];
-            load_row<T, V>((const T*)a.dout.p + r * a.dout.row + n, have, a.vec, d);
-            if (a.pre.p) load_row<float, V>((const float*)a.pre.p + r * a.pre.row + n, have, a.vec, z);
-            if (a.gated) {
-                load_row<float, V>((const float*)a.pre2.p + r * a.pre2.row + n, have, a.vec, u);
+        constexpr int F = 4;  // rows of a warp in flight
+        for (int64_t r = r0 + warp; r < r1; r += F * kGradWarps) {
+            float d[F][V], z[F][V], u[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float v, dv;
-                    act_both<kCoarse<T>>(a.act, z[i], v, dv);
-                    z[i] = d[i] * v;
-                    d[i] = d[i] * u[i] * dv;
-                }
-                store_row<T, V>((T*)a.d2.p + r * a.d2.row + n, have, a.vec, z);
-            } else if (a.act != FE_ACT_NONE) {
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float v, dv;
-                    act_both<kCoarse<T>>(a.act, z[i], v, dv);
-                    d[i] *= dv;
-                }
+            for (int f = 0; f < F; ++f) {
+                const int64_t m = r + f * kGradWarps;
+                const int k = m < r1 ? have : 0;
+                load_row<T, V>((const T*)a.dout.p + m * a.dout.row + n, k, a.vec, d[f]);
+                if (a.pre.p) load_row<float, V>((const float*)a.pre.p + m * a.pre.row + n, k, a.vec, z[f]);
             }
-            if (a.d1.p) store_row<T, V>((T*)a.d1.p + r * a.d1.row + n, have, a.vec, d);
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] += d[i];
+            for (int f = 0; f < F; ++f) {
+                const int64_t m = r + f * kGradWarps;
+                if (m >= r1) break;
+                if (a.gated) {
+                    load_row<float, V>((const float*)a.pre2.p + m * a.pre2.row + n, have, a.vec, u);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float v, dv;
+                        act_both<kCoarse<T>>(a.act, z[f][i], v, dv);
+                        z[f][i] = d[f][i] * v;
+                        d[f][i] = d[f][i] * u[i] * dv;
+                    }
+                    store_row<T, V>((T*)a.d2.p + m * a.d2.row + n, have, a.vec, z[f]);
+                } else if (a.act != FE_ACT_NONE) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        float v, dv;
+                        act_both<kCoarse<T>>(a.act, z[f][i], v, dv);
+                        d[f][i] *= dv;
+                    }
+                }
+                if (a.d1.p) store_row<T, V>((T*)a.d1.p + m * a.d1.row + n, have, a.vec, d[f]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] += d[f][i];
+            }
         }
     }
     if (!a.part) return;

@@ -61,41 +61,69 @@ __device__ __forceinline__ void weights(const void* w, int c, int have, bool vec
     for (int i = 0; i < V; ++i) f[i] += offset;
 }
 
-template <typename T, int VPT, bool WARP, int MAXT>
-__global__ void __launch_bounds__(MAXT) norm_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int V = Vec16<T>::kN;
+// Rows on their way: a thread's vectors of the next rows, copied behind its back (cp.async) into slots that it
+// alone writes and reads. NA arrays, DEPTH rows.
+template <typename T, int NA, int VPT, int DEPTH>
+struct RowRing {
+    uint4* mine;  // [DEPTH][NA][VPT] vectors, `threads` apart
+    int threads;
+    __device__ __forceinline__ uint4* at(int slot, int array, int j) const { return mine + ((slot * NA + array) * VPT + j) * threads; }
+    __device__ __forceinline__ void fetch(int slot, int array, const fe_mat& m, int64_t row, int c, int have, int j, bool vec) const {
+        uint4* dst = at(slot, array, j);
+        if (!m.p || have <= 0) return;
+        const T* src = (const T*)m.p + row * m.row + c;
+        if (vec && have >= Vec16<T>::kN) cp_async16(smem_u32(dst), src, true);
+        else *dst = load_raw<T>(src, 0, have, false);
+    }
+};
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+constexpr int forward_depth(int vpt) { return vpt == 1 ? 4 : 3; }
+constexpr int backward_depth(int vpt) { return vpt == 1 ? 3 : 2; }
+
+template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
+__global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant__ NormArgs a) {
+    constexpr int V = Vec16<T>::kN, D = forward_depth(VPT);
+    extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
     const int nt = WARP ? 32 : blockDim.x, tid = WARP ? threadIdx.x % 32 : threadIdx.x;
     const int64_t step = WARP ? (int64_t)gridDim.x * (blockDim.x / 32) : gridDim.x;
     int64_t r = WARP ? (int64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32 : blockIdx.x;
     const float inv_d = 1.f / (float)a.d;
-    uint4 rx[VPT], rz[VPT];
-    const auto fetch = [&](int64_t row) {
+    const RowRing<T, 2, VPT, D> ring{ring_mem + threadIdx.x, (int)blockDim.x};
+    const auto fetch = [&](int64_t row, int slot) {
+        if (row < a.R) {
+#pragma unroll
+            for (int j = 0; j < VPT; ++j) {
+                const int c = (j * nt + tid) * V, have = a.d - c;
+                ring.fetch(slot, 0, a.x, row, c, have, j, a.vec);
+                ring.fetch(slot, 1, a.z, row, c, have, j, a.vec);
+            }
+        }
+        cp_commit();
+    };
+    for (int i = 0; i < D - 1; ++i) fetch(r + i * step, i);
+    int slot = 0;
+    for (; r < a.R; r += step, slot = slot + 1 == D ? 0 : slot + 1) {
+        cp_wait<D - 2>();
+        float y[VPT][V], z[VPT][V];
+        float scale_z = 1.f;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int c = (j * nt + tid) * V, have = a.d - c;
-            if (have <= 0) {
-                rx[j] = rz[j] = make_uint4(0, 0, 0, 0);
-                continue;
-            }
-            rx[j] = load_raw<T>(a.x.p, row * a.x.row + c, have, a.vec);
-            if (a.z.p) rz[j] = load_raw<T>(a.z.p, row * a.z.row + c, have, a.vec);
+            const bool has = (j * nt + tid) * V < a.d;
+            Vec16<T>::widen(has ? *ring.at(slot, 0, j) : make_uint4(0, 0, 0, 0), y[j]);
+            Vec16<T>::widen(has && a.z.p ? *ring.at(slot, 1, j) : make_uint4(0, 0, 0, 0), z[j]);
         }
-    };
-    if (r < a.R) fetch(r);
-    for (; r < a.R; r += step) {
-        float y[VPT][V];
-        float scale_z = 1.f;
+        // (the slot that was read last: its row's outputs, which may be the inputs themselves, are rows before)
+        fetch(r + (D - 1) * step, slot == 0 ? D - 1 : slot - 1);
         if (a.post) {
             float s[1] = {0.f};
 #pragma unroll
-            for (int j = 0; j < VPT; ++j) {
-                float z[V];
-                Vec16<T>::widen(rz[j], z);
+            for (int j = 0; j < VPT; ++j)
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[0] += z[i] * z[i];
-            }
+                for (int i = 0; i < V; ++i) s[0] += z[j][i] * z[j][i];
             worker_sum<WARP, 1>(s, buf, turn);
             scale_z = rsqrtf(s[0] * inv_d + a.eps);
         }
@@ -103,33 +131,24 @@ __global__ void __launch_bounds__(MAXT) norm_kernel(const __grid_constant__ Norm
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int c = (j * nt + tid) * V, have = a.d - c;
-            Vec16<T>::widen(rx[j], y[j]);
             if (have > 0 && a.z.p) {
-                float z[V], w[V];
-                Vec16<T>::widen(rz[j], z);
+                float w[V];
                 if (a.post) {
                     weights<T>(a.post_w, c, have, a.vec, a.offset, w);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) z[i] *= scale_z * w[i];
+                    for (int i = 0; i < V; ++i) z[j][i] *= scale_z * w[i];
                 }
                 if (a.gate.p) {
                     load_row<T, V>((const T*)a.gate.p + r / a.gate_rows * a.gate.row + c, have, a.vec, w);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) z[i] *= w[i];
+                    for (int i = 0; i < V; ++i) z[j][i] *= w[i];
                 }
 #pragma unroll
-                for (int i = 0; i < V; ++i) y[j][i] = fmaf(a.scale, z[i], y[j][i]);
+                for (int i = 0; i < V; ++i) y[j][i] = fmaf(a.scale, z[j][i], y[j][i]);
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) s[0] += y[j][i] * y[j][i];
-        }
-        if (r + step < a.R) fetch(r + step);  // (a row is never both: outputs may be the inputs themselves)
-        if (a.y.p) {
-#pragma unroll
-            for (int j = 0; j < VPT; ++j) {
-                const int c = (j * nt + tid) * V;
-                store_row<T, V>((T*)a.y.p + r * a.y.row + c, a.d - c, a.vec, y[j]);
-            }
+            if (a.y.p) store_row<T, V>((T*)a.y.p + r * a.y.row + c, have, a.vec, y[j]);
         }
         if (!a.n.p) continue;
         worker_sum<WARP, 1>(s, buf, turn);
@@ -145,6 +164,7 @@ __global__ void __launch_bounds__(MAXT) norm_kernel(const __grid_constant__ Norm
             store_row<T, V>((T*)a.n.p + r * a.n.row + c, have, a.vec, w);
         }
     }
+    cp_wait<0>();
 }
 
 // Rows of any length: the statistics in passes of their own over the row (which the caches hold).
@@ -223,9 +243,47 @@ __device__ __forceinline__ void worker_rows(const NormArgs& a, int64_t w, int64_
     }
 }
 
-template <typename T, int VPT, bool WARP, int MAXT>
-__global__ void __launch_bounds__(MAXT) norm_backward_kernel(const __grid_constant__ NormArgs a, int64_t workers) {
-    constexpr int V = Vec16<T>::kN;
+// Pairs of neighbouring columns, and a thread's vector of them
+template <typename T>
+struct Pairs {
+    static constexpr int N = Vec16<T>::kN / 2;
+    uint64_t v[N];
+    __device__ __forceinline__ void widen(const uint4& x) {
+        if (sizeof(T) == 4) {
+            v[0] = pair_f32(x.x, x.y);
+            v[1] = pair_f32(x.z, x.w);
+        } else {
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = pair_f32(w[i] << 16, w[i] & 0xFFFF0000u);
+        }
+    }
+    __device__ __forceinline__ void floats(const float* f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = pair_f32(__float_as_uint(f[2 * i]), __float_as_uint(f[2 * i + 1]));
+    }
+    __device__ __forceinline__ void to(float* f) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            f[2 * i] = low_f32(v[i]);
+            f[2 * i + 1] = high_f32(v[i]);
+        }
+    }
+};
+__device__ __forceinline__ float pair_sum(uint64_t a) { return low_f32(a) + high_f32(a); }
+
+// a thread's weights (w + offset; 1 without) or gates as they were loaded
+template <typename T>
+__device__ __forceinline__ void pair_weights(const uint4& raw, bool given, float offset, Pairs<T>& p) {
+    p.widen(raw);
+#pragma unroll
+    for (int i = 0; i < Pairs<T>::N; ++i) p.v[i] = given ? add_x2(p.v[i], pair_f32(offset)) : pair_f32(1.f);
+}
+
+template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
+__global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a, int64_t workers) {
+    constexpr int V = Vec16<T>::kN, N = V / 2, D = backward_depth(VPT);
+    extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
     const int nt = WARP ? 32 : blockDim.x, tid = WARP ? threadIdx.x % 32 : threadIdx.x;
@@ -234,157 +292,218 @@ __global__ void __launch_bounds__(MAXT) norm_backward_kernel(const __grid_consta
     const float inv_d = 1.f / (float)a.d;
     int64_t r, r1;
     worker_rows(a, worker, r, r1);
-    uint4 rx[VPT], rz[VPT], ry[VPT], rn[VPT];
-    const auto fetch = [&](int64_t row) {
+    const RowRing<T, 4, VPT, D> ring{ring_mem + threadIdx.x, (int)blockDim.x};
+    const auto fetch = [&](int64_t row, int slot) {
+        if (row < r1) {
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int c = (j * nt + tid) * V, have = a.d - c;
-            rx[j] = rz[j] = ry[j] = rn[j] = make_uint4(0, 0, 0, 0);
-            if (have <= 0) continue;
-            rx[j] = load_raw<T>(a.x.p, row * a.x.row + c, have, a.vec);
-            if (a.z.p) rz[j] = load_raw<T>(a.z.p, row * a.z.row + c, have, a.vec);
-            if (a.dy.p) ry[j] = load_raw<T>(a.dy.p, row * a.dy.row + c, have, a.vec);
-            if (a.dn.p) rn[j] = load_raw<T>(a.dn.p, row * a.dn.row + c, have, a.vec);
+            for (int j = 0; j < VPT; ++j) {
+                const int c = (j * nt + tid) * V, have = a.d - c;
+                ring.fetch(slot, 0, a.x, row, c, have, j, a.vec);
+                ring.fetch(slot, 1, a.z, row, c, have, j, a.vec);
+                ring.fetch(slot, 2, a.dy, row, c, have, j, a.vec);
+                ring.fetch(slot, 3, a.dn, row, c, have, j, a.vec);
+            }
         }
+        cp_commit();
     };
-    float spre[VPT][V] = {}, spost[VPT][V] = {}, sgate[VPT][V] = {};
+    uint64_t spre[VPT][N] = {}, spost[VPT][N] = {}, sgate[VPT][N] = {};
     int64_t group = 0, group_end = a.R;  // rows of the current gate
     if (a.gate.p) {
         group = r / a.gate_rows;
         group_end = (group + 1) * a.gate_rows;
     }
-    if (r < r1) fetch(r);
-    for (; r < r1; ++r) {
+    // one vector a thread: weights and gates stay in registers; more: they are read again, from the first cache
+    constexpr bool HOLD = VPT == 1;
+    const int c0 = tid * V;
+    uint4 hold_post = make_uint4(0, 0, 0, 0), hold_pre = hold_post, hold_gate = hold_post;
+    const auto read_gate = [&] {
+        if (HOLD && a.gate.p && c0 < a.d && r < r1) hold_gate = load_raw<T>(a.gate.p, group * a.gate.row + c0, a.d - c0, a.vec);
+    };
+    if (HOLD && c0 < a.d) {
+        if (a.post_w) hold_post = load_raw<T>(a.post_w, c0, a.d - c0, a.vec);
+        if (a.pre_w) hold_pre = load_raw<T>(a.pre_w, c0, a.d - c0, a.vec);
+    }
+    read_gate();
+    const auto post_of = [&](int c, int have, Pairs<T>& w) {
+        pair_weights<T>(HOLD || !a.post_w ? hold_post : load_raw<T>(a.post_w, c, have, a.vec), a.post_w, a.offset, w);
+    };
+    const auto pre_of = [&](int c, int have, Pairs<T>& w) {
+        pair_weights<T>(HOLD || !a.pre_w ? hold_pre : load_raw<T>(a.pre_w, c, have, a.vec), a.pre_w, a.offset, w);
+    };
+    const auto gate_of = [&](int c, int have, Pairs<T>& w) {
+        w.widen(HOLD ? hold_gate : load_raw<T>(a.gate.p, group * a.gate.row + c, have, a.vec));
+    };
+    for (int i = 0; i < D - 1; ++i) fetch(r + i, i);
+    int slot = 0;
+    for (; r < r1; ++r, slot = slot + 1 == D ? 0 : slot + 1) {
+        cp_wait<D - 2>();
         float scale_z = 1.f;
         if (a.post) {
             float s[1] = {0.f};
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
-                float z[V];
-                Vec16<T>::widen(rz[j], z);
+                if ((j * nt + tid) * V >= a.d) continue;
+                Pairs<T> z;
+                z.widen(*ring.at(slot, 1, j));
+                uint64_t q = 0;
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[0] += z[i] * z[i];
+                for (int i = 0; i < N; ++i) q = fma_x2(z.v[i], z.v[i], q);
+                s[0] += pair_sum(q);
             }
             worker_sum<WARP, 1>(s, buf, turn);
             scale_z = rsqrtf(s[0] * inv_d + a.eps);
         }
-        // y (in dx's place), p and a = dn (w_pre + o)
-        float y[VPT][V], p[VPT][V], dn[VPT][V], t[2] = {0.f, 0.f};
+        // y, its square and (dn (w_pre + o)) y
+        Pairs<T> y[VPT];
+        float t[2] = {0.f, 0.f};
+        const uint64_t sz = pair_f32(scale_z), sc = pair_f32(a.scale);
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int c = (j * nt + tid) * V, have = a.d - c;
-            float w[V];
-            Vec16<T>::widen(rx[j], y[j]);
-            Vec16<T>::widen(rz[j], p[j]);
-            Vec16<T>::widen(rn[j], dn[j]);
-            if (have > 0 && a.z.p) {
+            if (have <= 0) continue;
+            Pairs<T> w;
+            y[j].widen(*ring.at(slot, 0, j));
+            if (a.z.p) {
+                Pairs<T> p;
+                p.widen(*ring.at(slot, 1, j));
                 if (a.post) {
-                    weights<T>(a.post_w, c, have, a.vec, a.offset, w);
+                    post_of(c, have, w);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) p[j][i] *= scale_z * w[i];
+                    for (int i = 0; i < N; ++i) p.v[i] = mul_x2(mul_x2(p.v[i], sz), w.v[i]);
+                }
+                if (a.gate.p) {
+                    gate_of(c, have, w);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) p.v[i] = mul_x2(p.v[i], w.v[i]);
                 }
 #pragma unroll
-                for (int i = 0; i < V; ++i) w[i] = 1.f;
-                if (a.gate.p) load_row<T, V>((const T*)a.gate.p + group * a.gate.row + c, have, a.vec, w);
-#pragma unroll
-                for (int i = 0; i < V; ++i) y[j][i] = fmaf(a.scale, p[j][i] * w[i], y[j][i]);
+                for (int i = 0; i < N; ++i) y[j].v[i] = fma_x2(sc, p.v[i], y[j].v[i]);
             }
-            if (have > 0 && a.dn.p) {
-                weights<T>(a.pre_w, c, have, a.vec, a.offset, w);
+            if (a.dn.p) {
+                Pairs<T> dn;
+                dn.widen(*ring.at(slot, 3, j));
+                pre_of(c, have, w);
+                uint64_t q0 = 0, q1 = 0;
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    t[0] += y[j][i] * y[j][i];
-                    t[1] += dn[j][i] * w[i] * y[j][i];
+                for (int i = 0; i < N; ++i) {
+                    q0 = fma_x2(y[j].v[i], y[j].v[i], q0);
+                    q1 = fma_x2(mul_x2(dn.v[i], w.v[i]), y[j].v[i], q1);
                 }
+                t[0] += pair_sum(q0);
+                t[1] += pair_sum(q1);
             }
         }
         float scale_y = 0.f, back = 0.f;
         if (a.dn.p) {
             worker_sum<WARP, 2>(t, buf, turn);
             scale_y = rsqrtf(t[0] * inv_d + a.eps);
-            back = t[1] * inv_d * scale_y * scale_y * scale_y;
+            back = -t[1] * inv_d * scale_y * scale_y * scale_y;
         }
+        const uint64_t sy = pair_f32(scale_y), by = pair_f32(back);
         float u[1] = {0.f};
-        float dp[VPT][V];
+        Pairs<T> b[VPT];  // dp (w_post + o)
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int c = (j * nt + tid) * V, have = a.d - c;
-            float w[V], dx[V];
-            Vec16<T>::widen(ry[j], dx);
             if (have <= 0) continue;
+            Pairs<T> w, dx;
+            if (a.dy.p) {
+                dx.widen(*ring.at(slot, 2, j));
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) dx.v[i] = 0;
+            }
             if (a.dn.p) {
-                weights<T>(a.pre_w, c, have, a.vec, a.offset, w);
+                Pairs<T> dn;
+                dn.widen(*ring.at(slot, 3, j));
+                pre_of(c, have, w);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    dx[i] += scale_y * dn[j][i] * w[i] - back * y[j][i];
-                    spre[j][i] = fmaf(dn[j][i], y[j][i] * scale_y, spre[j][i]);
+                for (int i = 0; i < N; ++i) {
+                    const uint64_t ry = mul_x2(dn.v[i], sy);
+                    spre[j][i] = fma_x2(ry, y[j].v[i], spre[j][i]);
+                    dx.v[i] = fma_x2(by, y[j].v[i], fma_x2(ry, w.v[i], dx.v[i]));
                 }
             }
-            if (a.dx.p) store_row<T, V>((T*)a.dx.p + r * a.dx.row + c, have, a.vec, dx);
+            if (a.dx.p) {
+                float f[V];
+                dx.to(f);
+                store_row<T, V>((T*)a.dx.p + r * a.dx.row + c, have, a.vec, f);
+            }
             if (!a.z.p) continue;
+            Pairs<T> z, g;
+            z.widen(*ring.at(slot, 1, j));
+            if (a.post) post_of(c, have, w);
+            if (a.gate.p) gate_of(c, have, g);
+            uint64_t q = 0;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                dp[j][i] = a.scale * dx[i];
-                sgate[j][i] = fmaf(dp[j][i], p[j][i], sgate[j][i]);
-            }
-            if (a.gate.p) {
-                load_row<T, V>((const T*)a.gate.p + group * a.gate.row + c, have, a.vec, w);
-#pragma unroll
-                for (int i = 0; i < V; ++i) dp[j][i] *= w[i];
-            }
-            if (a.post) {
-                float z[V];
-                Vec16<T>::widen(rz[j], z);
-                weights<T>(a.post_w, c, have, a.vec, a.offset, w);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    spost[j][i] = fmaf(dp[j][i], z[i] * scale_z, spost[j][i]);
-                    dp[j][i] *= w[i];
-                    u[0] += dp[j][i] * z[i];
-                    p[j][i] = z[i];  // (p has been used)
+            for (int i = 0; i < N; ++i) {
+                uint64_t dp = mul_x2(dx.v[i], sc);
+                const uint64_t zh = a.post ? mul_x2(z.v[i], sz) : z.v[i];
+                if (a.gate.p) {
+                    sgate[j][i] = fma_x2(dp, a.post ? mul_x2(zh, w.v[i]) : zh, sgate[j][i]);
+                    dp = mul_x2(dp, g.v[i]);
                 }
+                if (a.post) {
+                    spost[j][i] = fma_x2(dp, zh, spost[j][i]);
+                    dp = mul_x2(dp, w.v[i]);
+                    q = fma_x2(dp, z.v[i], q);
+                }
+                b[j].v[i] = dp;
             }
+            u[0] += pair_sum(q);
         }
-        if (r + 1 < r1) fetch(r + 1);
         if (a.post) worker_sum<WARP, 1>(u, buf, turn);
         if (a.dz.p) {
-            const float back_z = u[0] * inv_d * scale_z * scale_z * scale_z;
+            const uint64_t bz = pair_f32(-u[0] * inv_d * scale_z * scale_z * scale_z);
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
                 const int c = (j * nt + tid) * V, have = a.d - c;
                 if (have <= 0) continue;
+                float f[V];
                 if (a.post) {
+                    Pairs<T> z;
+                    z.widen(*ring.at(slot, 1, j));
 #pragma unroll
-                    for (int i = 0; i < V; ++i) dp[j][i] = scale_z * dp[j][i] - back_z * p[j][i];
+                    for (int i = 0; i < N; ++i) b[j].v[i] = fma_x2(bz, z.v[i], mul_x2(sz, b[j].v[i]));
                 }
-                store_row<T, V>((T*)a.dz.p + r * a.dz.row + c, have, a.vec, dp[j]);
+                b[j].to(f);
+                store_row<T, V>((T*)a.dz.p + r * a.dz.row + c, have, a.vec, f);
             }
         }
+        fetch(r + D - 1, slot == 0 ? D - 1 : slot - 1);
         if (r + 1 == group_end || (r + 1 == r1 && !a.parts)) {  // the last row of a gate
             if (a.dgate.p && !a.part_gate) {
 #pragma unroll
                 for (int j = 0; j < VPT; ++j) {
                     const int c = (j * nt + tid) * V;
-                    store_row<T, V>((T*)a.dgate.p + group * a.dgate.row + c, a.d - c, a.vec, sgate[j]);
+                    float f[V];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) sgate[j][i] = 0.f;
+                    for (int i = 0; i < N; ++i) {
+                        f[2 * i] = low_f32(sgate[j][i]);
+                        f[2 * i + 1] = high_f32(sgate[j][i]);
+                        sgate[j][i] = 0;
+                    }
+                    store_row<T, V>((T*)a.dgate.p + group * a.dgate.row + c, a.d - c, a.vec, f);
                 }
             }
             if (a.gate.p) {
                 ++group;
                 group_end += a.gate_rows;
+                if (r + 1 < r1) read_gate();
             }
         }
     }
+    cp_wait<0>();
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int c = (j * nt + tid) * V;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (c + i >= a.d) continue;
-            if (a.part_pre) a.part_pre[worker * a.d + c + i] = spre[j][i];
-            if (a.part_post) a.part_post[worker * a.d + c + i] = spost[j][i];
-            if (a.part_gate) a.part_gate[worker * a.d + c + i] = sgate[j][i];
+            const auto part = [&](const uint64_t* s) { return i & 1 ? high_f32(s[i / 2]) : low_f32(s[i / 2]); };
+            if (a.part_pre) a.part_pre[worker * a.d + c + i] = part(spre[j]);
+            if (a.part_post) a.part_post[worker * a.d + c + i] = part(spost[j]);
+            if (a.part_gate) a.part_gate[worker * a.d + c + i] = part(sgate[j]);
         }
     }
 }
@@ -512,72 +631,104 @@ __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const __grid_c
 // threads of a CTA for a row of nv vectors, VPT a thread
 int cta_threads(int64_t nv, int vpt) { return (int)(((nv + vpt - 1) / vpt + 31) / 32 * 32); }
 
+constexpr int kNormWarps = 4;  // warps of a CTA where warps are workers
+
 template <typename K>
-cudaError_t resident(K kern, int threads, int num_sms, int64_t rows, unsigned& grid) {
+cudaError_t resident(K kern, int threads, size_t smem, int num_sms, int64_t units, unsigned& grid) {
     int per = 0;
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, threads, 0);
+    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, threads, smem);
     const int64_t all = (int64_t)num_sms * (per > 0 ? per : 1);
-    grid = (unsigned)(rows < all ? rows : all);
+    grid = (unsigned)(units < all ? units : all);
     return e;
 }
 
-template <typename T, int VPT, bool WARP, int MAXT>
+template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
 cudaError_t launch_forward(const NormArgs& a, int threads, int num_sms, cudaStream_t st) {
     unsigned grid;
-    const auto kern = norm_kernel<T, VPT, WARP, MAXT>;
+    const auto kern = norm_kernel<T, VPT, WARP, MAXT, CTAS>;
+    const size_t smem = (size_t)forward_depth(VPT) * 2 * VPT * threads * sizeof(uint4);
     const int64_t units = WARP ? (a.R + threads / 32 - 1) / (threads / 32) : a.R;
-    const cudaError_t e = resident(kern, threads, num_sms, units, grid);
+    const cudaError_t e = resident(kern, threads, smem, num_sms, units, grid);
     if (e != cudaSuccess) return e;
-    return launch_k(kern, dim3(grid), dim3(threads), 0, st, false, a);
+    return launch_k(kern, dim3(grid), dim3(threads), smem, st, false, a);
 }
 
-constexpr int kNormWarps = 4;  // warps of a CTA where warps are workers
+// vectors of a row: a warp's at most, a CTA's with one or two a thread, and more
+constexpr int kWarpVecs = 32, kNarrow = 640, kOne = 1024, kTwo = 2048;
 
 template <typename T>
 cudaError_t forward(const NormArgs& a, int num_sms, cudaStream_t st) {
     const int64_t nv = (a.d + Vec16<T>::kN - 1) / Vec16<T>::kN;
-    if (nv <= 32) return launch_forward<T, 1, true, kNormWarps * 32>(a, kNormWarps * 32, num_sms, st);
-    if (nv <= 512) return launch_forward<T, 1, false, 512>(a, cta_threads(nv, 1), num_sms, st);
-    if (nv <= 1024) return launch_forward<T, 1, false, 1024>(a, cta_threads(nv, 1), num_sms, st);
-    if (nv <= 2048) return launch_forward<T, 2, false, 1024>(a, cta_threads(nv, 2), num_sms, st);
+    if (nv <= kWarpVecs) return launch_forward<T, 1, true, kNormWarps * 32, 8>(a, kNormWarps * 32, num_sms, st);
+    if (nv <= kNarrow) return launch_forward<T, 1, false, kNarrow, 2>(a, cta_threads(nv, 1), num_sms, st);
+    if (nv <= kOne) return launch_forward<T, 1, false, kOne, 1>(a, cta_threads(nv, 1), num_sms, st);
+    if (nv <= kTwo) return launch_forward<T, 2, false, kOne, 1>(a, cta_threads(nv, 2), num_sms, st);
     unsigned grid;
-    const cudaError_t e = resident(norm_long_kernel<T>, 1024, num_sms, a.R, grid);
+    const cudaError_t e = resident(norm_long_kernel<T>, 1024, 0, num_sms, a.R, grid);
     if (e != cudaSuccess) return e;
     return launch_k(norm_long_kernel<T>, dim3(grid), dim3(1024), 0, st, false, a);
 }
 
 // how a row of d elements is held in the backward pass: by a warp, by a CTA (one or two vectors a thread), in passes
 enum NormForm { BY_WARP, BY_CTA, BY_CTA_2, IN_PASSES };
-NormForm backward_form(int d, fe_dtype dtype) {
-    const int64_t v = dtype == FE_F32 ? 4 : 8, nv = (d + v - 1) / v;
-    return nv <= 32 ? BY_WARP : nv <= 640 ? BY_CTA : nv <= 1024 ? BY_CTA_2 : IN_PASSES;
+NormForm backward_form(int64_t nv) { return nv <= kWarpVecs ? BY_WARP : nv <= kNarrow ? BY_CTA : nv <= kOne ? BY_CTA_2 : IN_PASSES; }
+int form_threads(NormForm f, int64_t nv) {
+    return f == BY_WARP ? kNormWarps * 32 : f == IN_PASSES ? 1024 : cta_threads(nv, f == BY_CTA ? 1 : 2);
 }
+int64_t row_vecs(int d, fe_dtype dtype) { return dtype == FE_F32 ? ((int64_t)d + 3) / 4 : ((int64_t)d + 7) / 8; }
 
 template <typename T>
 cudaError_t backward(const NormArgs& a, fe_dtype dtype, cudaStream_t st) {
-    const int64_t nv = (a.d + Vec16<T>::kN - 1) / Vec16<T>::kN;
+    const int64_t nv = row_vecs(a.d, dtype);
+    const NormForm form = backward_form(nv);
+    const int threads = form_threads(form, nv);
     const int64_t workers = a.parts ? a.groups * a.parts : (a.groups + a.step - 1) / a.step;
+    const int vpt = form == BY_CTA_2 ? 2 : 1;
+    const size_t smem = (size_t)backward_depth(vpt) * 4 * vpt * threads * sizeof(uint4);
     const dim3 grid((unsigned)workers);
-    switch (backward_form(a.d, dtype)) {
+    switch (form) {
         case BY_WARP:
-            return launch_k(norm_backward_kernel<T, 1, true, kNormWarps * 32>, dim3((unsigned)((workers + kNormWarps - 1) / kNormWarps)),
-                            dim3(kNormWarps * 32), 0, st, false, a, workers);
+            return launch_k(norm_backward_kernel<T, 1, true, kNormWarps * 32, 4>, dim3((unsigned)((workers + kNormWarps - 1) / kNormWarps)),
+                            dim3(threads), smem, st, false, a, workers);
         case BY_CTA:
-            return launch_k(norm_backward_kernel<T, 1, false, 640>, grid, dim3(cta_threads(nv, 1)), 0, st, false, a, workers);
+            if (threads <= 320) return launch_k(norm_backward_kernel<T, 1, false, 320, 2>, grid, dim3(threads), smem, st, false, a, workers);
+            return launch_k(norm_backward_kernel<T, 1, false, kNarrow, 1>, grid, dim3(threads), smem, st, false, a, workers);
         case BY_CTA_2:
-            return launch_k(norm_backward_kernel<T, 2, false, 512>, grid, dim3(cta_threads(nv, 2)), 0, st, false, a, workers);
-        default: return launch_k(norm_backward_long_kernel<T>, grid, dim3(1024), 0, st, false, a);
+            return launch_k(norm_backward_kernel<T, 2, false, 512, 1>, grid, dim3(threads), smem, st, false, a, workers);
+        default: return launch_k(norm_backward_long_kernel<T>, grid, dim3(threads), 0, st, false, a);
     }
+}
+
+template <typename K>
+cudaError_t allow(K kern, size_t bytes) {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+template <typename T>
+cudaError_t prepare() {
+    cudaError_t e;
+    const size_t f = forward_depth(1) * 2 * sizeof(uint4), f2 = forward_depth(2) * 4 * sizeof(uint4), b = backward_depth(1) * 4 * sizeof(uint4);
+    if ((e = allow(norm_kernel<T, 1, false, kNarrow, 2>, f * kNarrow)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 1, false, kOne, 1>, f * kOne)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 2, false, kOne, 1>, f2 * kOne)) != cudaSuccess) return e;
+    if ((e = allow(norm_backward_kernel<T, 1, false, 320, 2>, b * 320)) != cudaSuccess) return e;
+    if ((e = allow(norm_backward_kernel<T, 1, false, kNarrow, 1>, b * kNarrow)) != cudaSuccess) return e;
+    return allow(norm_backward_kernel<T, 2, false, 512, 1>, backward_depth(2) * 8 * sizeof(uint4) * 512);
 }
 
 }  // namespace
 
+cudaError_t norm_prepare() {
+    const cudaError_t e = prepare<float>();
+    return e != cudaSuccess ? e : prepare<bf16_t>();
+}
+
 int64_t norm_backward_plan(NormArgs& a, fe_dtype dtype, int num_sms) {
-    const int64_t v = dtype == FE_F32 ? 4 : 8, nv = (a.d + v - 1) / v;
-    const NormForm form = backward_form(a.d, dtype);
-    const int threads = form == BY_CTA_2 ? cta_threads(nv, 2) : cta_threads(nv, 1);
-    // workers that fill the GPU once
-    const int64_t want = form == BY_WARP ? (int64_t)num_sms * 16 : form == IN_PASSES ? num_sms : num_sms * (640 / threads > 0 ? 640 / threads : 1);
+    const int64_t nv = row_vecs(a.d, dtype);
+    const NormForm form = backward_form(nv);
+    // workers that fill the GPU once: 16 warps an SM, or the CTAs of some 640 threads
+    const int ctas = 640 / form_threads(form, nv);
+    const int64_t want = (int64_t)num_sms * (form == BY_WARP ? 16 : ctas > 0 ? ctas : 1);
     const int64_t size = a.gate.p ? (a.gate_rows < a.R ? a.gate_rows : a.R) : a.R;
     a.gate_part = 1;
     a.groups = a.gate.p ? (a.R + a.gate_rows - 1) / a.gate_rows : 1;

@@ -92,6 +92,7 @@ fe_status build(fe_target* t, cudaStream_t st) {
     FE_TRY(tree_attn_prepare());
     FE_TRY(gemm_tc_prepare());
     FE_TRY(gemm_few_prepare());
+    FE_TRY(norm_prepare());
     FE_TRY(logprobs_prepare());
     const int pairs = c.rope_dim / 2;
     const size_t rows = (size_t)t->num_sms * 2 * kAttnItemRows;
