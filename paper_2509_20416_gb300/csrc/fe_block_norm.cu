@@ -4,9 +4,9 @@
 //
 //   forward   p = z rz (w_post + o), y = x + s g p, n = y ry (w_pre + o), r = 1 / sqrt(mean of squares + eps)
 //   backward  with a = dn (w_pre + o):
-//             dx = dy + ry a - y ry^3 mean(a y)
-//             dp = s g dx, b = dp (w_post + o):  dz = rz b - z rz^3 mean(b z)
-//             dw_pre = sum dn y ry,  dw_post = sum dp z rz,  dg = sum s p dx
+//             dx = dy + ry a - y ry^3 mean(a y),  dw_pre = sum dn y ry
+//             with b = dx s g (w_post + o):  dz = rz b - z rz^3 mean(b z)
+//             with t = sum dx z rz over the rows of a gate:  dg = s (w_post + o) t,  dw_post = sum s g t
 //             (y is computed again from x and z, so nothing rounded stands in for it)
 //
 // A worker is a CTA, or a warp where a row is at most 32 vectors of 16 bytes; its threads own
@@ -47,6 +47,18 @@ __device__ __forceinline__ void worker_sum(float* v, float (*buf)[32 * 2], int& 
     for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < warps ? b[i * 32 + lane] : 0.f);
 }
 
+// a thread's vector of a row; FULL: rows are whole vectors on their boundaries
+template <typename T, bool FULL>
+__device__ __forceinline__ uint4 load_vec(const T* p, int have, bool vec) {
+    if (FULL) return *reinterpret_cast<const uint4*>(p);
+    return load_raw<T>(p, 0, have, vec);
+}
+template <typename T, bool FULL>
+__device__ __forceinline__ void store_vec(T* p, int have, bool vec, const float* f) {
+    if (FULL) *reinterpret_cast<uint4*>(p) = pack16<T>(f);
+    else store_row<T, Vec16<T>::kN>(p, have, vec, f);
+}
+
 // w + offset for a thread's columns; 1 without weights
 template <typename T>
 __device__ __forceinline__ void weights(const void* w, int c, int have, bool vec, float offset, float* f) {
@@ -61,18 +73,45 @@ __device__ __forceinline__ void weights(const void* w, int c, int have, bool vec
     for (int i = 0; i < V; ++i) f[i] += offset;
 }
 
+// Pairs of neighbouring columns, and a thread's vector of them
+template <typename T>
+struct Pairs {
+    static constexpr int N = Vec16<T>::kN / 2;
+    uint64_t v[N];
+    __device__ __forceinline__ void widen(const uint4& x) {
+        if (sizeof(T) == 4) {
+            v[0] = pair_f32(x.x, x.y);
+            v[1] = pair_f32(x.z, x.w);
+        } else {
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = pair_f32(w[i] << 16, w[i] & 0xFFFF0000u);
+        }
+    }
+    __device__ __forceinline__ void floats(const float* f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = pair_f32(__float_as_uint(f[2 * i]), __float_as_uint(f[2 * i + 1]));
+    }
+    __device__ __forceinline__ void to(float* f) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            f[2 * i] = low_f32(v[i]);
+            f[2 * i + 1] = high_f32(v[i]);
+        }
+    }
+};
+__device__ __forceinline__ float pair_sum(uint64_t a) { return low_f32(a) + high_f32(a); }
+
 // Rows on their way: a thread's vectors of the next rows, copied behind its back (cp.async) into slots that it
 // alone writes and reads. NA arrays, DEPTH rows.
-template <typename T, int NA, int VPT, int DEPTH>
+template <typename T, int NA, int VPT, bool FULL>
 struct RowRing {
     uint4* mine;  // [DEPTH][NA][VPT] vectors, `threads` apart
     int threads;
     __device__ __forceinline__ uint4* at(int slot, int array, int j) const { return mine + ((slot * NA + array) * VPT + j) * threads; }
-    __device__ __forceinline__ void fetch(int slot, int array, const fe_mat& m, int64_t row, int c, int have, int j, bool vec) const {
+    __device__ __forceinline__ void fetch(int slot, int array, int j, const T* src, int have, bool vec) const {
         uint4* dst = at(slot, array, j);
-        if (!m.p || have <= 0) return;
-        const T* src = (const T*)m.p + row * m.row + c;
-        if (vec && have >= Vec16<T>::kN) cp_async16(smem_u32(dst), src, true);
+        if (FULL || (vec && have >= Vec16<T>::kN)) cp_async16(smem_u32(dst), src, true);
         else *dst = load_raw<T>(src, 0, have, false);
     }
 };
@@ -80,11 +119,16 @@ __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_grou
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 constexpr int forward_depth(int vpt) { return vpt == 1 ? 4 : 3; }
-constexpr int backward_depth(int vpt) { return vpt == 1 ? 3 : 2; }
+constexpr int kBackwardDepth = 2;
 
-template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
+// the group of rows that share a gate (rows are below 2^30)
+__device__ __forceinline__ int64_t group_of(const NormArgs& a, int64_t r) {
+    return a.gate_rows >= a.R ? 0 : (uint32_t)r / (uint32_t)a.gate_rows;
+}
+
+template <typename T, int VPT, bool WARP, int MAXT, int CTAS, bool FULL>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int V = Vec16<T>::kN, D = forward_depth(VPT);
+    constexpr int V = Vec16<T>::kN, N = V / 2, D = forward_depth(VPT);
     extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
@@ -92,77 +136,111 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
     const int64_t step = WARP ? (int64_t)gridDim.x * (blockDim.x / 32) : gridDim.x;
     int64_t r = WARP ? (int64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32 : blockIdx.x;
     const float inv_d = 1.f / (float)a.d;
-    const RowRing<T, 2, VPT, D> ring{ring_mem + threadIdx.x, (int)blockDim.x};
-    const auto fetch = [&](int64_t row, int slot) {
-        if (row < a.R) {
+    const RowRing<T, 2, VPT, FULL> ring{ring_mem + threadIdx.x, (int)blockDim.x};
+    const T *px = (const T*)a.x.p + r * a.x.row, *pz = (const T*)a.z.p + r * a.z.row;  // the next row to fetch
+    const int64_t sx = step * a.x.row, sz_ = step * a.z.row;
+    int64_t next = r;
+    const auto fetch = [&](int slot) {
+        if (next < a.R) {
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
                 const int c = (j * nt + tid) * V, have = a.d - c;
-                ring.fetch(slot, 0, a.x, row, c, have, j, a.vec);
-                ring.fetch(slot, 1, a.z, row, c, have, j, a.vec);
+                if (have <= 0) continue;
+                ring.fetch(slot, 0, j, px + c, have, a.vec);
+                if (a.z.p) ring.fetch(slot, 1, j, pz + c, have, a.vec);
             }
         }
         cp_commit();
+        px += sx;
+        pz += sz_;
+        next += step;
     };
-    for (int i = 0; i < D - 1; ++i) fetch(r + i * step, i);
+    // one vector a thread: the weights stay in registers
+    constexpr bool HOLD = VPT == 1;
+    uint4 hold_post = make_uint4(0, 0, 0, 0), hold_pre = hold_post;
+    if (HOLD && tid * V < a.d) {
+        if (a.post_w) hold_post = load_vec<T, FULL>((const T*)a.post_w + tid * V, a.d - tid * V, a.vec);
+        if (a.pre_w) hold_pre = load_vec<T, FULL>((const T*)a.pre_w + tid * V, a.d - tid * V, a.vec);
+    }
+    const auto held = [&](const void* w, const uint4& hold, int c, int have, Pairs<T>& p) {
+        p.widen(HOLD || !w ? hold : load_vec<T, FULL>((const T*)w + c, have, a.vec));
+#pragma unroll
+        for (int i = 0; i < N; ++i) p.v[i] = w ? add_x2(p.v[i], pair_f32(a.offset)) : pair_f32(1.f);
+    };
+    T *py = (T*)a.y.p + r * a.y.row, *pn = (T*)a.n.p + r * a.n.row;
+    const uint64_t sc = pair_f32(a.scale);
+    for (int i = 0; i < D - 1; ++i) fetch(i);
     int slot = 0;
     for (; r < a.R; r += step, slot = slot + 1 == D ? 0 : slot + 1) {
         cp_wait<D - 2>();
-        float y[VPT][V], z[VPT][V];
-        float scale_z = 1.f;
+        Pairs<T> y[VPT], z[VPT];
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const bool has = (j * nt + tid) * V < a.d;
-            Vec16<T>::widen(has ? *ring.at(slot, 0, j) : make_uint4(0, 0, 0, 0), y[j]);
-            Vec16<T>::widen(has && a.z.p ? *ring.at(slot, 1, j) : make_uint4(0, 0, 0, 0), z[j]);
+            y[j].widen(has ? *ring.at(slot, 0, j) : make_uint4(0, 0, 0, 0));
+            z[j].widen(has && a.z.p ? *ring.at(slot, 1, j) : make_uint4(0, 0, 0, 0));
         }
-        // (the slot that was read last: its row's outputs, which may be the inputs themselves, are rows before)
-        fetch(r + (D - 1) * step, slot == 0 ? D - 1 : slot - 1);
+        // (into the slot that was read last; outputs may be the inputs themselves: rows that were read before)
+        fetch(slot == 0 ? D - 1 : slot - 1);
+        float scale_z = 1.f;
         if (a.post) {
-            float s[1] = {0.f};
+            uint64_t q = 0;
 #pragma unroll
             for (int j = 0; j < VPT; ++j)
 #pragma unroll
-                for (int i = 0; i < V; ++i) s[0] += z[j][i] * z[j][i];
+                for (int i = 0; i < N; ++i) q = fma_x2(z[j].v[i], z[j].v[i], q);
+            float s[1] = {pair_sum(q)};
             worker_sum<WARP, 1>(s, buf, turn);
             scale_z = rsqrtf(s[0] * inv_d + a.eps);
         }
-        float s[1] = {0.f};
-#pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int c = (j * nt + tid) * V, have = a.d - c;
-            if (have > 0 && a.z.p) {
-                float w[V];
-                if (a.post) {
-                    weights<T>(a.post_w, c, have, a.vec, a.offset, w);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) z[j][i] *= scale_z * w[i];
-                }
-                if (a.gate.p) {
-                    load_row<T, V>((const T*)a.gate.p + r / a.gate_rows * a.gate.row + c, have, a.vec, w);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) z[j][i] *= w[i];
-                }
-#pragma unroll
-                for (int i = 0; i < V; ++i) y[j][i] = fmaf(a.scale, z[j][i], y[j][i]);
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[0] += y[j][i] * y[j][i];
-            if (a.y.p) store_row<T, V>((T*)a.y.p + r * a.y.row + c, have, a.vec, y[j]);
-        }
-        if (!a.n.p) continue;
-        worker_sum<WARP, 1>(s, buf, turn);
-        const float scale_y = rsqrtf(s[0] * inv_d + a.eps);
+        uint64_t q = 0;
+        const T* gate = (const T*)a.gate.p + (a.gate.p ? group_of(a, r) * a.gate.row : 0);
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int c = (j * nt + tid) * V, have = a.d - c;
             if (have <= 0) continue;
-            float w[V];
-            weights<T>(a.pre_w, c, have, a.vec, a.offset, w);
+            if (a.z.p) {
+                Pairs<T> w;
+                if (a.post) {
+                    held(a.post_w, hold_post, c, have, w);
+                    const uint64_t sz = pair_f32(scale_z);
 #pragma unroll
-            for (int i = 0; i < V; ++i) w[i] *= y[j][i] * scale_y;
-            store_row<T, V>((T*)a.n.p + r * a.n.row + c, have, a.vec, w);
+                    for (int i = 0; i < N; ++i) z[j].v[i] = mul_x2(mul_x2(z[j].v[i], sz), w.v[i]);
+                }
+                if (a.gate.p) {
+                    w.widen(load_vec<T, FULL>(gate + c, have, a.vec));
+#pragma unroll
+                    for (int i = 0; i < N; ++i) z[j].v[i] = mul_x2(z[j].v[i], w.v[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) y[j].v[i] = fma_x2(sc, z[j].v[i], y[j].v[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) q = fma_x2(y[j].v[i], y[j].v[i], q);
+            if (a.y.p) {
+                float f[V];
+                y[j].to(f);
+                store_vec<T, FULL>(py + c, have, a.vec, f);
+            }
         }
+        py += step * a.y.row;
+        if (!a.n.p) continue;
+        float s[1] = {pair_sum(q)};
+        worker_sum<WARP, 1>(s, buf, turn);
+        const uint64_t sy = pair_f32(rsqrtf(s[0] * inv_d + a.eps));
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int c = (j * nt + tid) * V, have = a.d - c;
+            if (have <= 0) continue;
+            Pairs<T> w;
+            held(a.pre_w, hold_pre, c, have, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) w.v[i] = mul_x2(mul_x2(y[j].v[i], sy), w.v[i]);
+            float f[V];
+            w.to(f);
+            store_vec<T, FULL>(pn + c, have, a.vec, f);
+        }
+        pn += step * a.n.row;
     }
     cp_wait<0>();
 }
@@ -243,46 +321,56 @@ __device__ __forceinline__ void worker_rows(const NormArgs& a, int64_t w, int64_
     }
 }
 
-// Pairs of neighbouring columns, and a thread's vector of them
+// Half a vector: two pairs of bfloat16 columns, or one of float32. The backward pass works through halves, so
+// that little more than the sums over rows and a row's y is in registers at any time.
 template <typename T>
-struct Pairs {
-    static constexpr int N = Vec16<T>::kN / 2;
+struct Half {
+    static constexpr int N = Vec16<T>::kN / 4;
     uint64_t v[N];
-    __device__ __forceinline__ void widen(const uint4& x) {
+    __device__ __forceinline__ void widen(const uint4* p, int h) {
+        const uint2 x = reinterpret_cast<const uint2*>(p)[h];
         if (sizeof(T) == 4) {
             v[0] = pair_f32(x.x, x.y);
-            v[1] = pair_f32(x.z, x.w);
         } else {
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = pair_f32(w[i] << 16, w[i] & 0xFFFF0000u);
+            v[0] = pair_f32(x.x << 16, x.x & 0xFFFF0000u);
+            v[N - 1] = pair_f32(x.y << 16, x.y & 0xFFFF0000u);
         }
     }
-    __device__ __forceinline__ void floats(const float* f) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = pair_f32(__float_as_uint(f[2 * i]), __float_as_uint(f[2 * i + 1]));
-    }
-    __device__ __forceinline__ void to(float* f) const {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            f[2 * i] = low_f32(v[i]);
-            f[2 * i + 1] = high_f32(v[i]);
-        }
+    __device__ __forceinline__ uint2 pack() const {
+        if (sizeof(T) == 4) return make_uint2((uint32_t)v[0], (uint32_t)(v[0] >> 32));
+        return make_uint2(pack_bf16(low_f32(v[0]), high_f32(v[0])), pack_bf16(low_f32(v[N - 1]), high_f32(v[N - 1])));
     }
 };
-__device__ __forceinline__ float pair_sum(uint64_t a) { return low_f32(a) + high_f32(a); }
-
-// a thread's weights (w + offset; 1 without) or gates as they were loaded
+// a thread's weights as held: w + offset, or 1
 template <typename T>
-__device__ __forceinline__ void pair_weights(const uint4& raw, bool given, float offset, Pairs<T>& p) {
-    p.widen(raw);
+__device__ __forceinline__ void half_weights(const uint4* held, int h, bool given, uint64_t offset, Half<T>& p) {
+    if (given) {
+        p.widen(held, h);
 #pragma unroll
-    for (int i = 0; i < Pairs<T>::N; ++i) p.v[i] = given ? add_x2(p.v[i], pair_f32(offset)) : pair_f32(1.f);
+        for (int i = 0; i < Half<T>::N; ++i) p.v[i] = add_x2(p.v[i], offset);
+    } else {
+#pragma unroll
+        for (int i = 0; i < Half<T>::N; ++i) p.v[i] = pair_f32(1.f);
+    }
 }
+template <typename T, bool FULL>
+__device__ __forceinline__ void store_packed(T* p, int have, bool vec, const uint2& lo, const uint2& hi) {
+    const uint4 x = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    if (FULL || (vec && have >= Vec16<T>::kN)) {
+        *reinterpret_cast<uint4*>(p) = x;
+    } else {
+        const T* e = reinterpret_cast<const T*>(&x);
+#pragma unroll
+        for (int i = 0; i < Vec16<T>::kN; ++i)
+            if (i < have) p[i] = e[i];
+    }
+}
+// (the compiler is not to gather loads of later halves in front: their registers would not be there)
+__device__ __forceinline__ void in_turn() { asm volatile("" ::: "memory"); }
 
-template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
+template <typename T, int VPT, bool WARP, int MAXT, int CTAS, bool FULL>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a, int64_t workers) {
-    constexpr int V = Vec16<T>::kN, N = V / 2, D = backward_depth(VPT);
+    constexpr int V = Vec16<T>::kN, N = V / 2, HN = N / 2, D = kBackwardDepth;
     extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
@@ -292,166 +380,210 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
     const float inv_d = 1.f / (float)a.d;
     int64_t r, r1;
     worker_rows(a, worker, r, r1);
-    const RowRing<T, 4, VPT, D> ring{ring_mem + threadIdx.x, (int)blockDim.x};
+    const RowRing<T, 4, VPT, FULL> ring{ring_mem + threadIdx.x, (int)blockDim.x};
     const auto fetch = [&](int64_t row, int slot) {
         if (row < r1) {
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
                 const int c = (j * nt + tid) * V, have = a.d - c;
-                ring.fetch(slot, 0, a.x, row, c, have, j, a.vec);
-                ring.fetch(slot, 1, a.z, row, c, have, j, a.vec);
-                ring.fetch(slot, 2, a.dy, row, c, have, j, a.vec);
-                ring.fetch(slot, 3, a.dn, row, c, have, j, a.vec);
+                if (have <= 0) continue;
+                ring.fetch(slot, 0, j, (const T*)a.x.p + row * a.x.row + c, have, a.vec);
+                if (a.z.p) ring.fetch(slot, 1, j, (const T*)a.z.p + row * a.z.row + c, have, a.vec);
+                if (a.dy.p) ring.fetch(slot, 2, j, (const T*)a.dy.p + row * a.dy.row + c, have, a.vec);
+                if (a.dn.p) ring.fetch(slot, 3, j, (const T*)a.dn.p + row * a.dn.row + c, have, a.vec);
             }
         }
         cp_commit();
     };
-    uint64_t spre[VPT][N] = {}, spost[VPT][N] = {}, sgate[VPT][N] = {};
+    uint64_t spre[VPT][N] = {}, sdx[VPT][N] = {};  // sums of dn y ry, and over a gate's rows of dx zh
     int64_t group = 0, group_end = a.R;  // rows of the current gate
     if (a.gate.p) {
-        group = r / a.gate_rows;
+        group = group_of(a, r);
         group_end = (group + 1) * a.gate_rows;
     }
-    // one vector a thread: weights and gates stay in registers; more: they are read again, from the first cache
-    constexpr bool HOLD = VPT == 1;
-    const int c0 = tid * V;
-    uint4 hold_post = make_uint4(0, 0, 0, 0), hold_pre = hold_post, hold_gate = hold_post;
-    const auto read_gate = [&] {
-        if (HOLD && a.gate.p && c0 < a.d && r < r1) hold_gate = load_raw<T>(a.gate.p, group * a.gate.row + c0, a.d - c0, a.vec);
+    // a thread's w_pre as it is stored, and s g (w_post + o) of the current gate in float32, behind the rows
+    const auto hold = [&](int array, int j) { return ring_mem + threadIdx.x + ((D * 4 + array) * VPT + j) * blockDim.x; };
+    const auto factor = [&](int j, int h) { return reinterpret_cast<uint64_t*>(hold(sizeof(T) == 2 ? 1 + h : 1, j)) + (sizeof(T) == 2 ? 0 : h); };
+    // gates and post weights of a vector's columns, and what they are multiplied with
+    const auto gates_of = [&](int j, float* g, float* w) {
+        const int c = (j * nt + tid) * V, have = a.d - c;
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = a.scale;
+        if (a.gate.p) {
+            load_row<T, V>((const T*)a.gate.p + group * a.gate.row + c, have, a.vec, g);
+#pragma unroll
+            for (int i = 0; i < V; ++i) g[i] *= a.scale;
+        }
+        weights<T>(a.post_w, c, have, a.vec, a.offset, w);
     };
-    if (HOLD && c0 < a.d) {
-        if (a.post_w) hold_post = load_raw<T>(a.post_w, c0, a.d - c0, a.vec);
-        if (a.pre_w) hold_pre = load_raw<T>(a.pre_w, c0, a.d - c0, a.vec);
+    const auto read_gate = [&] {
+        if (!a.z.p || r >= r1) return;
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            if ((j * nt + tid) * V >= a.d) continue;
+            float g[V], w[V];
+            gates_of(j, g, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                factor(j, i / HN)[i % HN] = pair_f32(__float_as_uint(g[2 * i] * w[2 * i]), __float_as_uint(g[2 * i + 1] * w[2 * i + 1]));
+        }
+    };
+    // At the end of a gate's rows: dgate = s (w_post + o) sum dx zh, dw_post += s g sum dx zh. A worker of several
+    // gates adds dw_post up in its own part of memory.
+    bool begun = false;
+    const auto end_gate = [&] {
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int c = (j * nt + tid) * V, have = a.d - c;
+            if (have <= 0) continue;
+            float g[V], w[V], t[V];
+            gates_of(j, g, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                t[2 * i] = low_f32(sdx[j][i]);
+                t[2 * i + 1] = high_f32(sdx[j][i]);
+                sdx[j][i] = 0;
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                g[i] *= t[i];
+                w[i] *= a.scale * t[i];
+            }
+            if (a.part_gate) store_row<float, V>(a.part_gate + worker * a.d + c, have, false, w);
+            else if (a.dgate.p) store_row<T, V>((T*)a.dgate.p + group * a.dgate.row + c, have, a.vec, w);
+            if (a.part_post) {
+                float* p = a.part_post + worker * a.d + c;
+                if (begun) {
+                    load_row<float, V>(p, have, false, t);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) g[i] += t[i];
+                }
+                store_row<float, V>(p, have, false, g);
+            }
+        }
+        begun = true;
+    };
+#pragma unroll
+    for (int j = 0; j < VPT; ++j) {
+        const int c = (j * nt + tid) * V;
+        if (a.pre_w && c < a.d) *hold(0, j) = load_vec<T, FULL>((const T*)a.pre_w + c, a.d - c, a.vec);
     }
     read_gate();
-    const auto post_of = [&](int c, int have, Pairs<T>& w) {
-        pair_weights<T>(HOLD || !a.post_w ? hold_post : load_raw<T>(a.post_w, c, have, a.vec), a.post_w, a.offset, w);
-    };
-    const auto pre_of = [&](int c, int have, Pairs<T>& w) {
-        pair_weights<T>(HOLD || !a.pre_w ? hold_pre : load_raw<T>(a.pre_w, c, have, a.vec), a.pre_w, a.offset, w);
-    };
-    const auto gate_of = [&](int c, int have, Pairs<T>& w) {
-        w.widen(HOLD ? hold_gate : load_raw<T>(a.gate.p, group * a.gate.row + c, have, a.vec));
-    };
-    for (int i = 0; i < D - 1; ++i) fetch(r + i, i);
+    if (r >= r1) {  // (more workers than rows in a short last group)
+#pragma unroll
+        for (int j = 0; j < VPT; ++j) {
+            const int c = (j * nt + tid) * V;
+            for (int i = 0; i < V && c + i < a.d; ++i) {
+                if (a.part_gate) a.part_gate[worker * a.d + c + i] = 0.f;
+                if (a.part_post) a.part_post[worker * a.d + c + i] = 0.f;
+            }
+        }
+    }
+    const auto pre_of = [&](int j, int h, Half<T>& w) { half_weights<T>(hold(0, j), h, a.pre_w, pair_f32(a.offset), w); };
+    for (int i = 0; i < D; ++i) fetch(r + i, i);
     int slot = 0;
     for (; r < r1; ++r, slot = slot + 1 == D ? 0 : slot + 1) {
-        cp_wait<D - 2>();
+        cp_wait<D - 1>();
         float scale_z = 1.f;
         if (a.post) {
-            float s[1] = {0.f};
+            uint64_t q = 0;
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
                 if ((j * nt + tid) * V >= a.d) continue;
                 Pairs<T> z;
                 z.widen(*ring.at(slot, 1, j));
-                uint64_t q = 0;
 #pragma unroll
                 for (int i = 0; i < N; ++i) q = fma_x2(z.v[i], z.v[i], q);
-                s[0] += pair_sum(q);
             }
+            float s[1] = {pair_sum(q)};
             worker_sum<WARP, 1>(s, buf, turn);
             scale_z = rsqrtf(s[0] * inv_d + a.eps);
         }
         // y, its square and (dn (w_pre + o)) y
-        Pairs<T> y[VPT];
-        float t[2] = {0.f, 0.f};
-        const uint64_t sz = pair_f32(scale_z), sc = pair_f32(a.scale);
+        uint64_t y[VPT][N], q0 = 0, q1 = 0;
+        const uint64_t sz = pair_f32(scale_z);
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
-            const int c = (j * nt + tid) * V, have = a.d - c;
-            if (have <= 0) continue;
-            Pairs<T> w;
-            y[j].widen(*ring.at(slot, 0, j));
-            if (a.z.p) {
-                Pairs<T> p;
-                p.widen(*ring.at(slot, 1, j));
-                if (a.post) {
-                    post_of(c, have, w);
+            if ((j * nt + tid) * V >= a.d) continue;
 #pragma unroll
-                    for (int i = 0; i < N; ++i) p.v[i] = mul_x2(mul_x2(p.v[i], sz), w.v[i]);
+            for (int h = 0; h < 2; ++h) {
+                Half<T> f, w;
+                f.widen(ring.at(slot, 0, j), h);
+                if (a.z.p) {
+                    Half<T> p;
+                    p.widen(ring.at(slot, 1, j), h);
+#pragma unroll
+                    for (int i = 0; i < HN; ++i) f.v[i] = fma_x2(mul_x2(p.v[i], sz), factor(j, h)[i], f.v[i]);
                 }
-                if (a.gate.p) {
-                    gate_of(c, have, w);
+                if (a.dn.p) {
+                    Half<T> dn;
+                    dn.widen(ring.at(slot, 3, j), h);
+                    pre_of(j, h, w);
 #pragma unroll
-                    for (int i = 0; i < N; ++i) p.v[i] = mul_x2(p.v[i], w.v[i]);
+                    for (int i = 0; i < HN; ++i) {
+                        q0 = fma_x2(f.v[i], f.v[i], q0);
+                        q1 = fma_x2(mul_x2(dn.v[i], w.v[i]), f.v[i], q1);
+                    }
                 }
 #pragma unroll
-                for (int i = 0; i < N; ++i) y[j].v[i] = fma_x2(sc, p.v[i], y[j].v[i]);
-            }
-            if (a.dn.p) {
-                Pairs<T> dn;
-                dn.widen(*ring.at(slot, 3, j));
-                pre_of(c, have, w);
-                uint64_t q0 = 0, q1 = 0;
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    q0 = fma_x2(y[j].v[i], y[j].v[i], q0);
-                    q1 = fma_x2(mul_x2(dn.v[i], w.v[i]), y[j].v[i], q1);
-                }
-                t[0] += pair_sum(q0);
-                t[1] += pair_sum(q1);
+                for (int i = 0; i < HN; ++i) y[j][h * HN + i] = f.v[i];
+                in_turn();
             }
         }
         float scale_y = 0.f, back = 0.f;
         if (a.dn.p) {
+            float t[2] = {pair_sum(q0), pair_sum(q1)};
             worker_sum<WARP, 2>(t, buf, turn);
             scale_y = rsqrtf(t[0] * inv_d + a.eps);
             back = -t[1] * inv_d * scale_y * scale_y * scale_y;
         }
         const uint64_t sy = pair_f32(scale_y), by = pair_f32(back);
-        float u[1] = {0.f};
-        Pairs<T> b[VPT];  // dp (w_post + o)
+        uint64_t q = 0;
+        // y becomes dx s g (w_post + o)
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             const int c = (j * nt + tid) * V, have = a.d - c;
             if (have <= 0) continue;
-            Pairs<T> w, dx;
-            if (a.dy.p) {
-                dx.widen(*ring.at(slot, 2, j));
-            } else {
+            uint2 out[2];
 #pragma unroll
-                for (int i = 0; i < N; ++i) dx.v[i] = 0;
-            }
-            if (a.dn.p) {
-                Pairs<T> dn;
-                dn.widen(*ring.at(slot, 3, j));
-                pre_of(c, have, w);
+            for (int h = 0; h < 2; ++h) {
+                Half<T> w, dx;
+                if (a.dy.p) {
+                    dx.widen(ring.at(slot, 2, j), h);
+                } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const uint64_t ry = mul_x2(dn.v[i], sy);
-                    spre[j][i] = fma_x2(ry, y[j].v[i], spre[j][i]);
-                    dx.v[i] = fma_x2(by, y[j].v[i], fma_x2(ry, w.v[i], dx.v[i]));
+                    for (int i = 0; i < HN; ++i) dx.v[i] = 0;
                 }
-            }
-            if (a.dx.p) {
-                float f[V];
-                dx.to(f);
-                store_row<T, V>((T*)a.dx.p + r * a.dx.row + c, have, a.vec, f);
-            }
-            if (!a.z.p) continue;
-            Pairs<T> z, g;
-            z.widen(*ring.at(slot, 1, j));
-            if (a.post) post_of(c, have, w);
-            if (a.gate.p) gate_of(c, have, g);
-            uint64_t q = 0;
+                if (a.dn.p) {
+                    Half<T> dn;
+                    dn.widen(ring.at(slot, 3, j), h);
+                    pre_of(j, h, w);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                uint64_t dp = mul_x2(dx.v[i], sc);
-                const uint64_t zh = a.post ? mul_x2(z.v[i], sz) : z.v[i];
-                if (a.gate.p) {
-                    sgate[j][i] = fma_x2(dp, a.post ? mul_x2(zh, w.v[i]) : zh, sgate[j][i]);
-                    dp = mul_x2(dp, g.v[i]);
+                    for (int i = 0; i < HN; ++i) {
+                        const int k = h * HN + i;
+                        const uint64_t ry = mul_x2(dn.v[i], sy);
+                        spre[j][k] = fma_x2(ry, y[j][k], spre[j][k]);
+                        dx.v[i] = fma_x2(by, y[j][k], fma_x2(ry, w.v[i], dx.v[i]));
+                    }
                 }
-                if (a.post) {
-                    spost[j][i] = fma_x2(dp, zh, spost[j][i]);
-                    dp = mul_x2(dp, w.v[i]);
-                    q = fma_x2(dp, z.v[i], q);
+                out[h] = dx.pack();
+                if (a.z.p) {
+                    Half<T> z;
+                    z.widen(ring.at(slot, 1, j), h);
+#pragma unroll
+                    for (int i = 0; i < HN; ++i) {
+                        const int k = h * HN + i;
+                        const uint64_t dp = mul_x2(dx.v[i], factor(j, h)[i]);
+                        sdx[j][k] = fma_x2(dx.v[i], mul_x2(z.v[i], sz), sdx[j][k]);
+                        q = fma_x2(dp, z.v[i], q);
+                        y[j][k] = dp;
+                    }
                 }
-                b[j].v[i] = dp;
+                in_turn();
             }
-            u[0] += pair_sum(q);
+            if (a.dx.p) store_packed<T, FULL>((T*)a.dx.p + r * a.dx.row + c, have, a.vec, out[0], out[1]);
         }
+        float u[1] = {pair_sum(q)};
         if (a.post) worker_sum<WARP, 1>(u, buf, turn);
         if (a.dz.p) {
             const uint64_t bz = pair_f32(-u[0] * inv_d * scale_z * scale_z * scale_z);
@@ -459,37 +591,28 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
             for (int j = 0; j < VPT; ++j) {
                 const int c = (j * nt + tid) * V, have = a.d - c;
                 if (have <= 0) continue;
-                float f[V];
-                if (a.post) {
-                    Pairs<T> z;
-                    z.widen(*ring.at(slot, 1, j));
+                uint2 out[2];
 #pragma unroll
-                    for (int i = 0; i < N; ++i) b[j].v[i] = fma_x2(bz, z.v[i], mul_x2(sz, b[j].v[i]));
+                for (int h = 0; h < 2; ++h) {
+                    Half<T> z, dz;
+                    z.widen(ring.at(slot, 1, j), h);
+#pragma unroll
+                    for (int i = 0; i < HN; ++i) {
+                        const uint64_t b = y[j][h * HN + i];
+                        dz.v[i] = a.post ? fma_x2(bz, z.v[i], mul_x2(sz, b)) : b;
+                    }
+                    out[h] = dz.pack();
                 }
-                b[j].to(f);
-                store_row<T, V>((T*)a.dz.p + r * a.dz.row + c, have, a.vec, f);
+                store_packed<T, FULL>((T*)a.dz.p + r * a.dz.row + c, have, a.vec, out[0], out[1]);
             }
         }
-        fetch(r + D - 1, slot == 0 ? D - 1 : slot - 1);
-        if (r + 1 == group_end || (r + 1 == r1 && !a.parts)) {  // the last row of a gate
-            if (a.dgate.p && !a.part_gate) {
-#pragma unroll
-                for (int j = 0; j < VPT; ++j) {
-                    const int c = (j * nt + tid) * V;
-                    float f[V];
-#pragma unroll
-                    for (int i = 0; i < N; ++i) {
-                        f[2 * i] = low_f32(sgate[j][i]);
-                        f[2 * i + 1] = high_f32(sgate[j][i]);
-                        sgate[j][i] = 0;
-                    }
-                    store_row<T, V>((T*)a.dgate.p + group * a.dgate.row + c, a.d - c, a.vec, f);
-                }
-            }
-            if (a.gate.p) {
+        fetch(r + D, slot);
+        if (r + 1 == group_end || r + 1 == r1) {  // the last of a gate's rows here
+            end_gate();
+            if (a.gate.p && r + 1 < r1) {
                 ++group;
                 group_end += a.gate_rows;
-                if (r + 1 < r1) read_gate();
+                read_gate();
             }
         }
     }
@@ -497,14 +620,14 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int c = (j * nt + tid) * V;
+        if (!a.part_pre || c >= a.d) continue;
+        float f[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (c + i >= a.d) continue;
-            const auto part = [&](const uint64_t* s) { return i & 1 ? high_f32(s[i / 2]) : low_f32(s[i / 2]); };
-            if (a.part_pre) a.part_pre[worker * a.d + c + i] = part(spre[j]);
-            if (a.part_post) a.part_post[worker * a.d + c + i] = part(spost[j]);
-            if (a.part_gate) a.part_gate[worker * a.d + c + i] = part(sgate[j]);
+        for (int i = 0; i < N; ++i) {
+            f[2 * i] = low_f32(spre[j][i]);
+            f[2 * i + 1] = high_f32(spre[j][i]);
         }
+        store_row<float, V>(a.part_pre + worker * a.d + c, a.d - c, false, f);
     }
 }
 
@@ -642,10 +765,13 @@ cudaError_t resident(K kern, int threads, size_t smem, int num_sms, int64_t unit
     return e;
 }
 
+// rows that are whole vectors on 16-byte boundaries
+template <typename T> bool whole(const NormArgs& a) { return a.vec && a.d % Vec16<T>::kN == 0; }
+
 template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
 cudaError_t launch_forward(const NormArgs& a, int threads, int num_sms, cudaStream_t st) {
     unsigned grid;
-    const auto kern = norm_kernel<T, VPT, WARP, MAXT, CTAS>;
+    const auto kern = whole<T>(a) ? norm_kernel<T, VPT, WARP, MAXT, CTAS, true> : norm_kernel<T, VPT, WARP, MAXT, CTAS, false>;
     const size_t smem = (size_t)forward_depth(VPT) * 2 * VPT * threads * sizeof(uint4);
     const int64_t units = WARP ? (a.R + threads / 32 - 1) / (threads / 32) : a.R;
     const cudaError_t e = resident(kern, threads, smem, num_sms, units, grid);
@@ -671,7 +797,7 @@ cudaError_t forward(const NormArgs& a, int num_sms, cudaStream_t st) {
 
 // how a row of d elements is held in the backward pass: by a warp, by a CTA (one or two vectors a thread), in passes
 enum NormForm { BY_WARP, BY_CTA, BY_CTA_2, IN_PASSES };
-NormForm backward_form(int64_t nv) { return nv <= kWarpVecs ? BY_WARP : nv <= kNarrow ? BY_CTA : nv <= kOne ? BY_CTA_2 : IN_PASSES; }
+NormForm backward_form(int64_t nv) { return nv <= kWarpVecs ? BY_WARP : nv <= 320 ? BY_CTA : nv <= kOne ? BY_CTA_2 : IN_PASSES; }
 int form_threads(NormForm f, int64_t nv) {
     return f == BY_WARP ? kNormWarps * 32 : f == IN_PASSES ? 1024 : cta_threads(nv, f == BY_CTA ? 1 : 2);
 }
@@ -684,17 +810,21 @@ cudaError_t backward(const NormArgs& a, fe_dtype dtype, cudaStream_t st) {
     const int threads = form_threads(form, nv);
     const int64_t workers = a.parts ? a.groups * a.parts : (a.groups + a.step - 1) / a.step;
     const int vpt = form == BY_CTA_2 ? 2 : 1;
-    const size_t smem = (size_t)backward_depth(vpt) * 4 * vpt * threads * sizeof(uint4);
+    const size_t smem = (size_t)(kBackwardDepth * 4 + 3) * vpt * threads * sizeof(uint4);
     const dim3 grid((unsigned)workers);
     switch (form) {
         case BY_WARP:
-            return launch_k(norm_backward_kernel<T, 1, true, kNormWarps * 32, 4>, dim3((unsigned)((workers + kNormWarps - 1) / kNormWarps)),
+            return launch_k(whole<T>(a) ? norm_backward_kernel<T, 1, true, kNormWarps * 32, 4, true> : norm_backward_kernel<T, 1, true, kNormWarps * 32, 4, false>, dim3((unsigned)((workers + kNormWarps - 1) / kNormWarps)),
                             dim3(threads), smem, st, false, a, workers);
         case BY_CTA:
-            if (threads <= 320) return launch_k(norm_backward_kernel<T, 1, false, 320, 2>, grid, dim3(threads), smem, st, false, a, workers);
-            return launch_k(norm_backward_kernel<T, 1, false, kNarrow, 1>, grid, dim3(threads), smem, st, false, a, workers);
+            return launch_k(whole<T>(a) ? norm_backward_kernel<T, 1, false, 320, 2, true> : norm_backward_kernel<T, 1, false, 320, 2, false>, grid,
+                            dim3(threads), smem, st, false, a, workers);
         case BY_CTA_2:
-            return launch_k(norm_backward_kernel<T, 2, false, 512, 1>, grid, dim3(threads), smem, st, false, a, workers);
+            if (threads <= 320)
+                return launch_k(whole<T>(a) ? norm_backward_kernel<T, 2, false, 320, 2, true> : norm_backward_kernel<T, 2, false, 320, 2, false>,
+                                grid, dim3(threads), smem, st, false, a, workers);
+            return launch_k(whole<T>(a) ? norm_backward_kernel<T, 2, false, 512, 1, true> : norm_backward_kernel<T, 2, false, 512, 1, false>, grid,
+                            dim3(threads), smem, st, false, a, workers);
         default: return launch_k(norm_backward_long_kernel<T>, grid, dim3(threads), 0, st, false, a);
     }
 }
@@ -704,23 +834,25 @@ cudaError_t allow(K kern, size_t bytes) {
     return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T>
+template <typename T, bool FULL>
 cudaError_t prepare() {
     cudaError_t e;
-    const size_t f = forward_depth(1) * 2 * sizeof(uint4), f2 = forward_depth(2) * 4 * sizeof(uint4), b = backward_depth(1) * 4 * sizeof(uint4);
-    if ((e = allow(norm_kernel<T, 1, false, kNarrow, 2>, f * kNarrow)) != cudaSuccess) return e;
-    if ((e = allow(norm_kernel<T, 1, false, kOne, 1>, f * kOne)) != cudaSuccess) return e;
-    if ((e = allow(norm_kernel<T, 2, false, kOne, 1>, f2 * kOne)) != cudaSuccess) return e;
-    if ((e = allow(norm_backward_kernel<T, 1, false, 320, 2>, b * 320)) != cudaSuccess) return e;
-    if ((e = allow(norm_backward_kernel<T, 1, false, kNarrow, 1>, b * kNarrow)) != cudaSuccess) return e;
-    return allow(norm_backward_kernel<T, 2, false, 512, 1>, backward_depth(2) * 8 * sizeof(uint4) * 512);
+    const size_t f = forward_depth(1) * 2 * sizeof(uint4), f2 = forward_depth(2) * 4 * sizeof(uint4), b = (kBackwardDepth * 4 + 3) * sizeof(uint4);
+    if ((e = allow(norm_kernel<T, 1, false, kNarrow, 2, FULL>, f * kNarrow)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 1, false, kOne, 1, FULL>, f * kOne)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 2, false, kOne, 1, FULL>, f2 * kOne)) != cudaSuccess) return e;
+    if ((e = allow(norm_backward_kernel<T, 1, false, 320, 2, FULL>, b * 320)) != cudaSuccess) return e;
+    if ((e = allow(norm_backward_kernel<T, 2, false, 320, 2, FULL>, b * 2 * 320)) != cudaSuccess) return e;
+    return allow(norm_backward_kernel<T, 2, false, 512, 1, FULL>, b * 2 * 512);
 }
 
 }  // namespace
 
 cudaError_t norm_prepare() {
-    const cudaError_t e = prepare<float>();
-    return e != cudaSuccess ? e : prepare<bf16_t>();
+    cudaError_t e;
+    if ((e = prepare<float, true>()) != cudaSuccess || (e = prepare<float, false>()) != cudaSuccess) return e;
+    if ((e = prepare<bf16_t, true>()) != cudaSuccess) return e;
+    return prepare<bf16_t, false>();
 }
 
 int64_t norm_backward_plan(NormArgs& a, fe_dtype dtype, int num_sms) {

@@ -24,6 +24,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kTopMax = 32, kTokMax = 64;
 constexpr int kNotes = 512;
+constexpr int kLpThreads = 256;  // four CTAs an SM, each thread with up to eight vectors on their way or at hand
 constexpr float kLn2 = 0.6931471805599453f;
 
 // order of (value, index): larger first by value (NaN above all, -0 equal to 0), then smaller index
@@ -77,6 +78,20 @@ struct RowShare {
 struct Stats {
     float m, s, u;
 };
+
+// the largest element of a vector (NaN counts as nothing)
+template <typename T>
+__device__ __forceinline__ float largest(const uint4& x) {
+    if (sizeof(T) == 4)
+        return fmaxf(fmaxf(__uint_as_float(x.x), __uint_as_float(x.y)), fmaxf(__uint_as_float(x.z), __uint_as_float(x.w)));
+    const auto max2 = [](uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    };
+    const uint32_t m = max2(max2(x.x, x.y), max2(x.z, x.w));
+    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+}
 
 // d = (x - m) c against a larger maximum M: e^d becomes 2^t e^d with t = (m - M) c
 __device__ __forceinline__ void rebase(Stats& a, float M, float c) {
@@ -207,7 +222,7 @@ __device__ __forceinline__ void cta_top(const RowShare<T>& r, uint64_t best, int
 }
 
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(512) logprob_kernel(const __grid_constant__ LogprobArgs a, float c, float inv_t) {
+__global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_constant__ LogprobArgs a, float c, float inv_t) {
     constexpr int V = Vec16<T>::kN;
     __shared__ LogprobShared sh;
     cg::cluster_group cluster = cg::this_cluster();
@@ -219,19 +234,29 @@ __global__ void __launch_bounds__(512) logprob_kernel(const __grid_constant__ Lo
         Stats st{-3.402823466e38f, 0.f, 0.f};
         float bx = -INFINITY;  // the largest element and its index
         int bi = -1;
-        const auto take = [&](const float* x, int n, int index) {
-            float top = x[0];
-#pragma unroll
-            for (int i = 1; i < V; ++i)
-                if (i < n) top = fmaxf(top, x[i]);
+        // n elements (a whole vector, or one)
+        const auto take = [&](const uint4& raw, int n, int index) {
+            float x[V];
+            Vec16<T>::widen(raw, x);
+            const float top = n == V ? largest<T>(raw) : x[0];
             if (top > st.m) rebase(st, top, c);
+            if (n == V) {
+                const uint64_t cc = pair_f32(c), mm = pair_f32(-st.m);  // (-m c could be infinite where m is the lowest value)
+                uint64_t s = 0, u = 0;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (i < n) {
-                    const float d = (x[i] - st.m) * c, e = ex2_approx(d);
-                    st.s += e;
-                    st.u = fmaf(e, fmaxf(d, -1e4f), st.u);
+                for (int i = 0; i < V / 2; ++i) {
+                    const uint64_t d = mul_x2(add_x2(pair_f32(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1])), mm), cc);
+                    const float dl = low_f32(d), dh = high_f32(d);
+                    const uint64_t e = pair_f32(__float_as_uint(ex2_approx(dl)), __float_as_uint(ex2_approx(dh)));
+                    s = add_x2(s, e);
+                    u = fma_x2(e, pair_f32(__float_as_uint(fmaxf(dl, -1e4f)), __float_as_uint(fmaxf(dh, -1e4f))), u);
                 }
+                st.s += low_f32(s) + high_f32(s);
+                st.u += low_f32(u) + high_f32(u);
+            } else {
+                const float d = (x[0] - st.m) * c, e = ex2_approx(d);
+                st.s += e;
+                st.u = fmaf(e, fmaxf(d, -1e4f), st.u);
             }
             if (TOP && (top > bx || bi < 0)) {
                 bx = top;
@@ -242,28 +267,26 @@ __global__ void __launch_bounds__(512) logprob_kernel(const __grid_constant__ Lo
             }
         };
         const int step = blockDim.x;
-        const auto one = [&](int i) {
-            float x[V] = {load_one(r.p + i)};
-            take(x, 1, i);
-        };
+        const auto one = [&](int i) { take(make_uint4(sizeof(T) == 2 ? (uint32_t) reinterpret_cast<const uint16_t*>(r.p)[i]
+                                                                     : reinterpret_cast<const uint32_t*>(r.p)[i], 0, 0, 0), 1, i); };
         r.each_before(one);  // (by growing index, so that the first of equal elements is kept)
-        // four vectors of a thread in flight
+        // four vectors of a thread in flight, the next four requested before these are looked at
         int v = r.v0 + tid;
-        for (; v + 3 * step < r.v1; v += 4 * step) {
+        uint4 next[4];
+        const auto request = [&](int w) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (w + j * step < r.v1) next[j] = r.load(w + j * step);
+        };
+        request(v);
+        for (; v < r.v1; v += 4 * step) {
             uint4 raw[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) raw[j] = r.load(v + j * step);
+            for (int j = 0; j < 4; ++j) raw[j] = next[j];
+            request(v + 4 * step);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float x[V];
-                Vec16<T>::widen(raw[j], x);
-                take(x, V, r.index(v + j * step));
-            }
-        }
-        for (; v < r.v1; v += step) {
-            float x[V];
-            Vec16<T>::widen(r.load(v), x);
-            take(x, V, r.index(v));
+            for (int j = 0; j < 4; ++j)
+                if (v + j * step < r.v1) take(raw[j], V, r.index(v + j * step));
         }
         r.each_behind(one);
         uint64_t best = 0;
@@ -344,7 +367,7 @@ __global__ void __launch_bounds__(512) logprob_kernel(const __grid_constant__ Lo
 // One CTA a share of a row: dl = (1 / T) p (A - dH (log p + H)) + (1 / T) (what the row's tokens get),
 // A = dlse - sum of the tokens' gradients.
 template <typename T>
-__global__ void __launch_bounds__(512) logprob_backward_kernel(const __grid_constant__ LogprobArgs a, float c, float inv_t, int shares) {
+__global__ void __launch_bounds__(kLpThreads, 4) logprob_backward_kernel(const __grid_constant__ LogprobArgs a, float c, float inv_t, int shares) {
     constexpr int V = Vec16<T>::kN;
     __shared__ int id[kTokMax + kTopMax];
     __shared__ float coef[kTokMax + kTopMax];
@@ -356,6 +379,16 @@ __global__ void __launch_bounds__(512) logprob_backward_kernel(const __grid_cons
         const T* x0 = (const T*)a.logits.p + row * a.logits.row;
         T* g0 = (T*)a.dlogits.p + row * a.dlogits.row;
         const RowShare<T> r(x0, a.V, (int)(unit % shares), shares);
+        // the first vectors are on their way while the row's tokens are read
+        const int step = blockDim.x;
+        int v = r.v0 + tid;
+        uint4 next[4];
+        const auto request = [&](int w) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (w + j * step < r.v1) next[j] = r.load(w + j * step);
+        };
+        request(v);
         __syncthreads();
         if (tid < n) {
             int t;
@@ -408,13 +441,20 @@ __global__ void __launch_bounds__(512) logprob_backward_kernel(const __grid_cons
         }
         __syncthreads();
         const bool aligned = (((uintptr_t)(g0 + r.head)) & 15) == 0;
-        const int step = blockDim.x;
-        int v = r.v0 + tid;
         const auto put = [&](int w, const uint4& raw) {
             float x[V];
             Vec16<T>::widen(raw, x);
+            const uint64_t cc = pair_f32(c), mm = pair_f32(-base), lc = pair_f32(-logs2), A2 = pair_f32(A), B2 = pair_f32(B);
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = grad(x[i]);
+            for (int i = 0; i < V; i += 2) {
+                const uint64_t d = fma_x2(add_x2(pair_f32(__float_as_uint(x[i]), __float_as_uint(x[i + 1])), mm), cc, lc);
+                const float dl = low_f32(d), dh = high_f32(d);
+                const uint64_t p = pair_f32(__float_as_uint(ex2_approx(dl)), __float_as_uint(ex2_approx(dh)));
+                const uint64_t q = fma_x2(B2, pair_f32(__float_as_uint(fmaxf(dl, -1e4f)), __float_as_uint(fmaxf(dh, -1e4f))), A2);
+                const uint64_t y = mul_x2(p, q);
+                x[i] = low_f32(y);
+                x[i + 1] = high_f32(y);
+            }
             T* g = g0 + r.index(w);
             if (aligned) {
                 __stcs(reinterpret_cast<uint4*>(g), pack16<T>(x));
@@ -423,14 +463,15 @@ __global__ void __launch_bounds__(512) logprob_backward_kernel(const __grid_cons
                 for (int i = 0; i < V; ++i) store_one(g + i, x[i]);
             }
         };
-        for (; v + 3 * step < r.v1; v += 4 * step) {
+        for (; v < r.v1; v += 4 * step) {
             uint4 raw[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) raw[j] = r.load(v + j * step);
+            for (int j = 0; j < 4; ++j) raw[j] = next[j];
+            request(v + 4 * step);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) put(v + j * step, raw[j]);
+            for (int j = 0; j < 4; ++j)
+                if (v + j * step < r.v1) put(v + j * step, raw[j]);
         }
-        for (; v < r.v1; v += step) put(v, r.load(v));
         const auto one = [&](int i) { store_one(g0 + i, grad(load_one(x0 + i))); };
         r.each_before(one);
         r.each_behind(one);
@@ -443,12 +484,12 @@ template <typename T, bool TOP>
 cudaError_t forward(const LogprobArgs& a, int num_sms, cudaStream_t st) {
     const int64_t vecs = a.V / Vec16<T>::kN;
     // CTAs of a row: as many as still leave a thread four vectors, until the GPU has four CTAs an SM
-    int ranks = 1, threads = 512;
+    int ranks = 1, threads = kLpThreads;
     while (ranks < 16 && a.R * ranks * 2 <= num_sms * 4 && vecs >= (int64_t)ranks * 2 * threads) ranks *= 2;
     while (threads > 128 && ranks == 1 && vecs < threads * 2) threads /= 2;
     const auto kern = logprob_kernel<T, TOP>;
     const float inv_t = 1.f / a.temperature;
-    int64_t rows = (int64_t)num_sms * (2048 / threads);  // as many CTAs as fit at once
+    int64_t rows = (int64_t)num_sms * (1024 / threads);  // as many CTAs as fit at once
     if (rows > a.R) rows = a.R;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * ranks));
@@ -466,10 +507,10 @@ cudaError_t forward(const LogprobArgs& a, int num_sms, cudaStream_t st) {
 template <typename T>
 cudaError_t backward(const LogprobArgs& a, int num_sms, cudaStream_t st) {
     const int64_t vecs = a.V / Vec16<T>::kN;
-    int shares = 1, threads = 512;
+    int shares = 1, threads = kLpThreads;
     while (a.R * shares * 2 <= num_sms * 4 && vecs >= (int64_t)shares * 2 * threads) shares *= 2;
     while (threads > 128 && vecs < (int64_t)shares * threads * 2) threads /= 2;
-    const int64_t units = a.R * shares, most = (int64_t)num_sms * (2048 / threads);
+    const int64_t units = a.R * shares, most = (int64_t)num_sms * (1024 / threads);
     const float inv_t = 1.f / a.temperature;
     return launch_k(logprob_backward_kernel<T>, dim3((unsigned)(units < most ? units : most)), dim3(threads), 0, st, false, a,
                     kLog2e * inv_t, inv_t, shares);

@@ -270,7 +270,8 @@ def test_block_norm(fe, handles, dtype, R, d, form):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("R,d,rows", [(1000, 96, 1), (1000, 96, 7), (900, 1024, 2), (3000, 16, 1500), (400, 17000, 3), (400, 17000, 390)])
+@pytest.mark.parametrize("R,d,rows", [(1000, 96, 1), (1000, 96, 7), (900, 1024, 2), (3000, 16, 1500), (400, 17000, 3), (400, 17000, 390),
+                                      (1001, 1024, 500), (1201, 5120, 600), (701, 96, 700), (801, 8000, 400), (500, 2000, 1)])
 def test_gate_groups(fe, handles, dtype, R, d, rows):
     """From a gate for each row to one for nearly all, more and fewer groups than the GPU has SMs, and a
     last group that is short."""
