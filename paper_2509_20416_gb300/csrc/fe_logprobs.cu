@@ -2,13 +2,14 @@
 // (fe_token_logprobs). Bound by memory traffic: a row of logits is read once; with c = log2(e) / T
 // and d = (x - m) c a thread keeps, of its elements,
 //   m, S = sum 2^d, U = sum d 2^d,   so that   lse = m / T + log S,   H = log S - ln 2 U / S,
-// rescaled when a vector of 16 bytes raises m, and the largest (value, index) that it saw.
+// against the largest m that its warp has seen, which four vectors of 16 bytes are compared with at a time.
 //
 // The K largest: of the threads' largest elements 32 groups are made; the K-th largest group maximum
-// is no larger than the K-th largest element of the row, so the few threads whose maximum reaches it
-// look through their elements again and note those that do. Rank among the notes is place in the
-// result. Where more elements reach it than there is room for (a row whose large elements all fall
-// to few threads), the CTA takes out its largest element K times instead.
+// is no larger than the K-th largest element of the row, so the elements of the few threads whose maximum
+// reaches it are looked through again, a warp a thread's share, and those that reach it are noted. Rank
+// among the notes is place in the result. Where more elements reach it than there is room for (equal
+// logits, or a row whose large elements all fall to few threads), the CTA takes out its largest element
+// K times instead.
 //
 // A cluster of 1 to 16 CTAs shares a row where there are too few rows to fill the GPU; its first CTA
 // joins the others' results through distributed shared memory.
@@ -61,16 +62,12 @@ struct RowShare {
         v1 = (int)((int64_t)vecs * (rank + 1) / ranks);
         loose = rank == 0 ? n - body : 0;
     }
-    // f(index) for a thread's loose elements, those before the body and those behind it; every pass over a
-    // share gives a thread the same elements
+    // f(index) for a thread's loose elements; every pass over a share gives a thread the same elements
     template <typename F>
-    __device__ __forceinline__ void each_before(const F& f) const {
-        for (int i = threadIdx.x; i < min(head, loose); i += blockDim.x) f(i);
+    __device__ __forceinline__ void each_loose(const F& f) const {
+        for (int i = threadIdx.x; i < loose; i += blockDim.x) f(loose_at(i));
     }
-    template <typename F>
-    __device__ __forceinline__ void each_behind(const F& f) const {
-        for (int i = head + threadIdx.x; i < loose; i += blockDim.x) f(i + body);
-    }
+    __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : i + body; }
     __device__ __forceinline__ int index(int v) const { return head + v * V; }
     __device__ __forceinline__ uint4 load(int v) const { return __ldcs(reinterpret_cast<const uint4*>(p + head) + v); }
 };
@@ -93,28 +90,28 @@ __device__ __forceinline__ float largest(const uint4& x) {
     return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
 }
 
-// d = (x - m) c against a larger maximum M: e^d becomes 2^t e^d with t = (m - M) c
-__device__ __forceinline__ void rebase(Stats& a, float M, float c) {
+// what a sum of 2^d and of d 2^d with d = (x - m) c becomes against a larger maximum M: (u + t s) f and s f with
+// t = (m - M) c, f = 2^t
+__device__ __forceinline__ Stats rebased(Stats a, float M, float c) {
     const float t = (a.m - M) * c, f = ex2_approx(t);
-    a.u = f * fmaf(a.s, fmaxf(t, -1e4f), a.u);
-    a.s *= f;
-    a.m = M;
+    return Stats{M, a.s * f, f * fmaf(a.s, fmaxf(t, -1e4f), a.u)};
 }
-__device__ __forceinline__ void join(Stats& a, Stats b, float c) {
-    const float M = fmaxf(a.m, b.m);
-    rebase(a, M, c);
-    rebase(b, M, c);
-    a.s += b.s;
-    a.u += b.u;
+// the sum over a warp's lanes
+__device__ __forceinline__ Stats warp_join(Stats a, float c) {
+    a = rebased(a, warp_max(a.m), c);
+    a.s = warp_sum(a.s);
+    a.u = warp_sum(a.u);
+    return a;
 }
+constexpr float kLowest = -3.402823466e38f;
 
 // Room that a row's passes share.
 struct LogprobShared {
     Stats stats[32];
-    uint64_t best[32][32];  // threads' largest keys, by warp
+    uint32_t best[32][32];  // order of the threads' largest elements, by warp
     uint64_t notes[kNotes];
     uint64_t top[kTopMax];
-    uint64_t floor;
+    uint32_t floor;
     int count;
     Stats total;
 };
@@ -136,77 +133,64 @@ __device__ __forceinline__ uint64_t largest_below(const RowShare<T>& r, uint64_t
         const uint64_t k = key_of(load_one(r.p + i), i);
         if (k < under && k > best) best = k;
     };
-    r.each_before(one);
-    r.each_behind(one);
+    r.each_loose(one);
     return best;
 }
 
-// The K largest keys of a CTA's share, sorted, into sh.top (0 where the share has fewer).
+// The K largest keys of a CTA's share, sorted, into sh.top (0 where the share has fewer). best: the order of
+// the thread's largest element, 0 if it has none.
 template <typename T>
-__device__ __forceinline__ void cta_top(const RowShare<T>& r, uint64_t best, int K, LogprobShared& sh) {
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = blockDim.x / 32;
+__device__ __forceinline__ void cta_top(const RowShare<T>& r, uint32_t best, int K, LogprobShared& sh) {
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = blockDim.x / 32, step = blockDim.x;
     sh.best[warp][lane] = best;
     if (tid == 0) sh.count = 0;
     __syncthreads();
     if (warp == 0) {
-        uint64_t k = 0;
+        uint32_t k = 0;
         for (int w = 0; w < warps; ++w) k = max(k, sh.best[w][lane]);
-        // rank of a group's maximum among the 32 (equal ones, of empty groups, by lane)
+        // rank of a group's maximum among the 32 (equal ones by lane)
         int rank = 0;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            const uint64_t o = __shfl_sync(0xffffffffu, k, i);
+            const uint32_t o = __shfl_sync(0xffffffffu, k, i);
             rank += o > k || (o == k && i < lane);
         }
-        if (rank == K - 1) sh.floor = k;
+        if (rank == K - 1) sh.floor = max(k, 1u);
         sh.top[lane] = 0;
     }
     __syncthreads();
-    const uint64_t floor = max(sh.floor, (uint64_t)1);
-    if (best >= floor) {
-        const auto note = [&](float x, int index) {
-            const uint64_t k = key_of(x, index);
-            if (k >= floor) {
-                const int at = atomicAdd(&sh.count, 1);
-                if (at < kNotes) sh.notes[at] = k;
-            }
-        };
-        const int step = blockDim.x;
-        int v = r.v0 + tid;
-        for (; v + 3 * step < r.v1; v += 4 * step) {
-            uint4 raw[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) raw[j] = r.load(v + j * step);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float x[RowShare<T>::V];
-                Vec16<T>::widen(raw[j], x);
-#pragma unroll
-                for (int i = 0; i < RowShare<T>::V; ++i) note(x[i], r.index(v + j * step) + i);
-            }
+    const uint32_t floor = sh.floor;
+    const auto note = [&](float x, int index) {
+        if (order_of(x) >= floor) {
+            const int at = atomicAdd(&sh.count, 1);
+            if (at < kNotes) sh.notes[at] = key_of(x, index);
         }
-        for (; v < r.v1; v += step) {
+    };
+    for (uint32_t left = __ballot_sync(0xffffffffu, best >= floor); left; left &= left - 1) {
+        const int owner = warp * 32 + __ffs(left) - 1;  // this thread's vectors, a lane each
+#pragma unroll 4
+        for (int v = r.v0 + owner + lane * step; v < r.v1; v += 32 * step) {
             float x[RowShare<T>::V];
             Vec16<T>::widen(r.load(v), x);
 #pragma unroll
             for (int i = 0; i < RowShare<T>::V; ++i) note(x[i], r.index(v) + i);
         }
+    }
+    if (best >= floor) {
         const auto one = [&](int i) { note(load_one(r.p + i), i); };
-        r.each_before(one);
-        r.each_behind(one);
+        r.each_loose(one);
     }
     __syncthreads();
     const int count = sh.count;
     if (count <= kNotes) {
-        for (int i = tid; i < count; i += blockDim.x) {
+        for (int i = tid; i < count; i += step) {
             const uint64_t k = sh.notes[i];
             int rank = 0;
             for (int j = 0; j < count; ++j) rank += sh.notes[j] > k;
             if (rank < K) sh.top[rank] = k;
         }
     } else {
-        uint64_t under = ~(uint64_t)0;  // (no key: an index is below 2^30)
-        uint64_t mine = best;
+        uint64_t under = ~(uint64_t)0, mine = under;  // (no key is that)
         for (int i = 0; i < K; ++i) {
             if (mine >= under) mine = largest_below(r, under);
             const uint64_t w = warp_max_key(mine);
@@ -223,99 +207,108 @@ __device__ __forceinline__ void cta_top(const RowShare<T>& r, uint64_t best, int
 
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_constant__ LogprobArgs a, float c, float inv_t) {
-    constexpr int V = Vec16<T>::kN;
+    constexpr int V = Vec16<T>::kN, B = 4;  // vectors of a thread that are looked at together
     __shared__ LogprobShared sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks();
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = blockDim.x / 32;
-    for (int64_t row = blockIdx.x / ranks; row < a.R; row += gridDim.x / ranks) {
-        const T* x0 = (const T*)a.logits.p + row * a.logits.row;
-        const RowShare<T> r(x0, a.V, rank, ranks);
-        Stats st{-3.402823466e38f, 0.f, 0.f};
-        float bx = -INFINITY;  // the largest element and its index
-        int bi = -1;
-        // n elements (a whole vector, or one)
-        const auto take = [&](const uint4& raw, int n, int index) {
-            float x[V];
-            Vec16<T>::widen(raw, x);
-            const float top = n == V ? largest<T>(raw) : x[0];
-            if (top > st.m) rebase(st, top, c);
-            if (n == V) {
-                const uint64_t cc = pair_f32(c), mm = pair_f32(-st.m);  // (-m c could be infinite where m is the lowest value)
-                uint64_t s = 0, u = 0;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = blockDim.x / 32, step = blockDim.x;
+    const uint32_t nothing = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;  // minus infinity
+    const int64_t row_step = gridDim.x / ranks;
+    uint4 next[B];
+    const auto request = [&](const RowShare<T>& r, int v) {
 #pragma unroll
-                for (int i = 0; i < V / 2; ++i) {
-                    const uint64_t d = mul_x2(add_x2(pair_f32(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1])), mm), cc);
+        for (int j = 0; j < B; ++j)
+            next[j] = v + j * step < r.v1 ? r.load(v + j * step) : make_uint4(nothing, nothing, nothing, nothing);
+    };
+    const auto share = [&](int64_t row) { return RowShare<T>((const T*)a.logits.p + row * a.logits.row, a.V, rank, ranks); };
+    int64_t row = blockIdx.x / ranks;
+    if (row < a.R) {
+        const RowShare<T> r = share(row);
+        request(r, r.v0 + tid);
+    }
+    for (; row < a.R; row += row_step) {
+        const T* x0 = (const T*)a.logits.p + row * a.logits.row;
+        const RowShare<T> r = share(row);
+        // a token that is asked for, and its logit, are read ahead
+        int id = -1;
+        float xt = 0.f;
+        if (rank == 0 && tid < a.J) {
+            id = a.tokens[row * a.J + tid];
+            if (id >= 0 && id < a.V) xt = load_one(x0 + id);
+        }
+        float m = kLowest, bx = -INFINITY;
+        uint64_t s = 0, u = 0;  // by even and odd columns
+        const uint64_t cc = pair_f32(c);
+        const auto look = [&](const uint4* raw, int n) {
+            float top = largest<T>(raw[0]);
+#pragma unroll
+            for (int j = 1; j < B; ++j)
+                if (j < n) top = fmaxf(top, largest<T>(raw[j]));
+            if (TOP) bx = fmaxf(bx, top);
+            if (__any_sync(0xffffffffu, top > m)) {
+                const float M = warp_max(fmaxf(top, m)), t = (m - M) * c;
+                const uint64_t f = pair_f32(ex2_approx(t));
+                u = mul_x2(f, fma_x2(s, pair_f32(fmaxf(t, -1e4f)), u));
+                s = mul_x2(f, s);
+                m = M;
+            }
+            const uint64_t mm = pair_f32(-m);  // (-m c could be infinite where m is the lowest value)
+#pragma unroll
+            for (int j = 0; j < B; ++j) {
+                if (j >= n) break;
+                float x[V];
+                Vec16<T>::widen(raw[j], x);
+#pragma unroll
+                for (int i = 0; i < V; i += 2) {
+                    const uint64_t d = mul_x2(add_x2(pair_f32(__float_as_uint(x[i]), __float_as_uint(x[i + 1])), mm), cc);
                     const float dl = low_f32(d), dh = high_f32(d);
                     const uint64_t e = pair_f32(__float_as_uint(ex2_approx(dl)), __float_as_uint(ex2_approx(dh)));
                     s = add_x2(s, e);
                     u = fma_x2(e, pair_f32(__float_as_uint(fmaxf(dl, -1e4f)), __float_as_uint(fmaxf(dh, -1e4f))), u);
                 }
-                st.s += low_f32(s) + high_f32(s);
-                st.u += low_f32(u) + high_f32(u);
-            } else {
-                const float d = (x[0] - st.m) * c, e = ex2_approx(d);
-                st.s += e;
-                st.u = fmaf(e, fmaxf(d, -1e4f), st.u);
-            }
-            if (TOP && (top > bx || bi < 0)) {
-                bx = top;
-                bi = index;
-#pragma unroll
-                for (int i = V - 1; i >= 0; --i)
-                    if (i < n && x[i] == top) bi = index + i;
             }
         };
-        const int step = blockDim.x;
-        const auto one = [&](int i) { take(make_uint4(sizeof(T) == 2 ? (uint32_t) reinterpret_cast<const uint16_t*>(r.p)[i]
-                                                                     : reinterpret_cast<const uint32_t*>(r.p)[i], 0, 0, 0), 1, i); };
-        r.each_before(one);  // (by growing index, so that the first of equal elements is kept)
-        // four vectors of a thread in flight, the next four requested before these are looked at
-        int v = r.v0 + tid;
-        uint4 next[4];
-        const auto request = [&](int w) {
+        // (whole warps: the turns of a warp are its first lane's)
+        for (int v = r.v0 + warp * 32; v < r.v1; v += B * step) {
+            uint4 raw[B];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (w + j * step < r.v1) next[j] = r.load(w + j * step);
-        };
-        request(v);
-        for (; v < r.v1; v += 4 * step) {
-            uint4 raw[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) raw[j] = next[j];
-            request(v + 4 * step);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (v + j * step < r.v1) take(raw[j], V, r.index(v + j * step));
+            for (int j = 0; j < B; ++j) raw[j] = next[j];
+            if (v + B * step < r.v1) request(r, v + lane + B * step);
+            look(raw, B);
         }
-        r.each_behind(one);
-        uint64_t best = 0;
+        for (int i = tid - lane; i < r.loose; i += step) {
+            uint4 raw[1] = {make_uint4(nothing, nothing, nothing, nothing)};
+            if (i + lane < r.loose) {
+                const int at = r.loose_at(i + lane);
+                raw[0].x = sizeof(T) == 2 ? (uint32_t) reinterpret_cast<const uint16_t*>(r.p)[at] | 0xFF800000u
+                                          : reinterpret_cast<const uint32_t*>(r.p)[at];
+            }
+            look(raw, 1);
+        }
+        if (row + row_step < a.R) {  // the next row's first vectors, while this row's sums are joined
+            const RowShare<T> q = share(row + row_step);
+            request(q, q.v0 + tid);
+        }
+        Stats st{m, warp_sum(low_f32(s) + high_f32(s)), warp_sum(low_f32(u) + high_f32(u))};
         if (TOP) {
-            if (bi >= 0) best = key_of(bx, bi);
-            if (st.s != st.s) best = largest_below(r, ~(uint64_t)0);  // NaN among a thread's elements: its first one
+            const bool any = r.v0 + tid < r.v1 || tid < r.loose;
+            uint32_t best = any ? order_of(bx) : 0;
+            const float mine = low_f32(s) + high_f32(s);
+            if (mine != mine) best = (uint32_t)(largest_below(r, ~(uint64_t)0) >> 32);  // NaN, or infinity, among its elements
             cta_top(r, best, a.K, sh);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            Stats b;
-            b.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-            b.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-            b.u = __shfl_xor_sync(0xffffffffu, st.u, o);
-            join(st, b, c);
         }
         if (lane == 0) sh.stats[warp] = st;
         __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < warps; ++w) join(st, sh.stats[w], c);
-            sh.total = st;
+        if (warp == 0) {
+            st = warp_join(lane < warps ? sh.stats[lane] : Stats{kLowest, 0.f, 0.f}, c);
+            if (lane == 0) sh.total = st;
         }
         if (ranks > 1) cluster.sync();
         else __syncthreads();
         if (rank == 0) {
-            if (tid == 0 && ranks > 1) {
-                st = sh.total;
-                for (int k = 1; k < ranks; ++k) join(st, cluster.map_shared_rank(&sh, k)->total, c);
-                sh.stats[0] = st;
+            if (warp == 0 && ranks > 1) {
+                st = warp_join(lane < ranks ? cluster.map_shared_rank(&sh, lane)->total : Stats{kLowest, 0.f, 0.f}, c);
+                if (lane == 0) sh.stats[0] = st;
             }
             if (ranks > 1) {
                 if (TOP) {  // the CTAs' lists, each of K sorted keys
@@ -346,10 +339,9 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_con
             }
             const bool bad = st.s != st.s;
             if (tid < a.J) {
-                const int id = a.tokens[row * a.J + tid];
                 float lp = 0.f;
                 if (id >= a.V) atomicOr(a.status, ST_DEVICE);
-                else if (id >= 0) lp = bad ? NAN : logp(load_one(x0 + id));
+                else if (id >= 0) lp = bad ? NAN : logp(xt);
                 a.logprob[row * a.J + tid] = lp;
             }
             if (TOP && tid < a.K) {
@@ -473,8 +465,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_backward_kernel(const _
                 if (v + j * step < r.v1) put(v + j * step, raw[j]);
         }
         const auto one = [&](int i) { store_one(g0 + i, grad(load_one(x0 + i))); };
-        r.each_before(one);
-        r.each_behind(one);
+        r.each_loose(one);
         __syncthreads();
         if (mine) store_one(g0 + id[tid], extra);
     }
@@ -483,13 +474,23 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_backward_kernel(const _
 template <typename T, bool TOP>
 cudaError_t forward(const LogprobArgs& a, int num_sms, cudaStream_t st) {
     const int64_t vecs = a.V / Vec16<T>::kN;
-    // CTAs of a row: as many as still leave a thread four vectors, until the GPU has four CTAs an SM
+    // CTAs of a row: the fewest rounds of CTAs (four an SM), counted in a thread's turns of four vectors, with some
+    // four turns' time for a row's end and two for a cluster's
     int ranks = 1, threads = kLpThreads;
-    while (ranks < 16 && a.R * ranks * 2 <= num_sms * 4 && vecs >= (int64_t)ranks * 2 * threads) ranks *= 2;
+    int64_t best = 0;
+    for (int r = 1; r <= 16 && (r == 1 || vecs >= (int64_t)r * threads); r *= 2) {
+        const int64_t rounds = (a.R * r + num_sms * 4 - 1) / (num_sms * 4);
+        const int64_t cost = rounds * ((vecs + r * threads * 4 - 1) / (r * threads * 4) + (r > 1 ? 6 : 4));
+        if (!best || cost < best) {
+            best = cost;
+            ranks = r;
+        }
+    }
     while (threads > 128 && ranks == 1 && vecs < threads * 2) threads /= 2;
     const auto kern = logprob_kernel<T, TOP>;
     const float inv_t = 1.f / a.temperature;
-    int64_t rows = (int64_t)num_sms * (1024 / threads);  // as many CTAs as fit at once
+    // CTAs that keep to one row each come and go; whole rows' CTAs stay, and have the next row on its way
+    int64_t rows = ranks > 1 ? (int64_t)1 << 26 : (int64_t)num_sms * (1024 / threads);
     if (rows > a.R) rows = a.R;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * ranks));
