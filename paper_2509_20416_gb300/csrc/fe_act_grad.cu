@@ -70,27 +70,28 @@ __global__ void __launch_bounds__(kGradWarps * 32) act_grad_kernel(const __grid_
     }
 }
 
-// a warp's lanes take neighbouring columns, the warps of a CTA every eighth part
+// a warp's lanes take neighbouring columns, the warps of a CTA every 32nd part
+constexpr int kSumWarps = 32;
 template <typename T>
-__global__ void __launch_bounds__(kGradWarps * 32)
-    sum_parts_kernel(const float* part, int64_t parts, int64_t groups, int64_t n, T* out, int64_t out_row) {
-    __shared__ float sums[kGradWarps][32];
+__global__ void __launch_bounds__(kSumWarps * 32) sum_parts_kernel(const __grid_constant__ SumJobs a) {
+    __shared__ float sums[kSumWarps][32];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
-    for (int64_t g = blockIdx.y; g < groups; g += gridDim.y) {
+    const SumJob& job = a.job[blockIdx.z];
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane, n = a.n;
+    for (int64_t g = blockIdx.y; g < job.groups; g += gridDim.y) {
         float s = 0.f;
         if (c < n) {
-            const float* p = part + g * parts * n + c;
+            const float* p = job.part + g * job.parts * n + c;
 #pragma unroll 8
-            for (int64_t i = warp; i < parts; i += kGradWarps) s += p[i * n];
+            for (int64_t i = warp; i < job.parts; i += kSumWarps) s += p[i * n];
         }
         sums[warp][lane] = s;
         __syncthreads();
         if (warp == 0 && c < n) {
             s = 0.f;
 #pragma unroll
-            for (int w = 0; w < kGradWarps; ++w) s += sums[w][lane];
-            store_one(out + g * out_row + c, s);
+            for (int w = 0; w < kSumWarps; ++w) s += sums[w][lane];
+            store_one((T*)job.out + g * job.out_row + c, s);
         }
         __syncthreads();
     }
@@ -115,12 +116,12 @@ cudaError_t launch_act_grad(const ActGradArgs& a, fe_dtype dtype, cudaStream_t s
     return dtype == FE_F32 ? launch_grad<float>(a, st) : launch_grad<bf16_t>(a, st);
 }
 
-cudaError_t launch_sum_parts(const float* part, int64_t parts, int64_t groups, int64_t n, void* out, int64_t out_row,
-                             fe_dtype dtype, cudaStream_t st) {
-    const dim3 grid((unsigned)((n + 31) / 32), (unsigned)(groups < 65535 ? groups : 65535)), block(kGradWarps * 32);
-    if (dtype == FE_F32)
-        return launch_k(sum_parts_kernel<float>, grid, block, 0, st, false, part, parts, groups, n, (float*)out, out_row);
-    return launch_k(sum_parts_kernel<bf16_t>, grid, block, 0, st, false, part, parts, groups, n, (bf16_t*)out, out_row);
+cudaError_t launch_sum_parts(const SumJobs& a, fe_dtype dtype, cudaStream_t st) {
+    int64_t groups = 1;
+    for (int i = 0; i < a.jobs; ++i) groups = a.job[i].groups > groups ? a.job[i].groups : groups;
+    if (!a.jobs) return cudaSuccess;
+    const dim3 grid((unsigned)((a.n + 31) / 32), (unsigned)(groups < 65535 ? groups : 65535), a.jobs), block(kSumWarps * 32);
+    return launch_k(dtype == FE_F32 ? sum_parts_kernel<float> : sum_parts_kernel<bf16_t>, grid, block, 0, st, false, a);
 }
 
 }  // namespace fe

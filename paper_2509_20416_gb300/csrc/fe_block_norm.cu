@@ -12,6 +12,8 @@
 // A worker is a CTA, or a warp where a row is at most 32 vectors of 16 bytes; its threads own
 // columns, so that the sums over rows stay in registers. The next row's loads are in flight while
 // a row's statistics are reduced.
+#include <atomic>
+
 #include "fe_layer_common.cuh"
 
 namespace fe {
@@ -756,13 +758,21 @@ int cta_threads(int64_t nv, int vpt) { return (int)(((nv + vpt - 1) / vpt + 31) 
 
 constexpr int kNormWarps = 4;  // warps of a CTA where warps are workers
 
+// A grid of the CTAs that fit at once, no more than `units`. How many fit an SM is asked once for each kernel and
+// size of a CTA (`known`, by warps).
+using Known = std::atomic<int>[33];
 template <typename K>
-cudaError_t resident(K kern, int threads, size_t smem, int num_sms, int64_t units, unsigned& grid) {
-    int per = 0;
-    const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, threads, smem);
-    const int64_t all = (int64_t)num_sms * (per > 0 ? per : 1);
+cudaError_t resident(K kern, Known& known, int threads, size_t smem, int num_sms, int64_t units, unsigned& grid) {
+    int per = known[threads / 32].load(std::memory_order_relaxed);
+    if (!per) {
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, threads, smem);
+        if (e != cudaSuccess) return e;
+        if (per < 1) per = 1;
+        known[threads / 32].store(per, std::memory_order_relaxed);
+    }
+    const int64_t all = (int64_t)num_sms * per;
     grid = (unsigned)(units < all ? units : all);
-    return e;
+    return cudaSuccess;
 }
 
 // rows that are whole vectors on 16-byte boundaries
@@ -774,7 +784,8 @@ cudaError_t launch_forward(const NormArgs& a, int threads, int num_sms, cudaStre
     const auto kern = whole<T>(a) ? norm_kernel<T, VPT, WARP, MAXT, CTAS, true> : norm_kernel<T, VPT, WARP, MAXT, CTAS, false>;
     const size_t smem = (size_t)forward_depth(VPT) * 2 * VPT * threads * sizeof(uint4);
     const int64_t units = WARP ? (a.R + threads / 32 - 1) / (threads / 32) : a.R;
-    const cudaError_t e = resident(kern, threads, smem, num_sms, units, grid);
+    static Known known[2];
+    const cudaError_t e = resident(kern, known[whole<T>(a)], threads, smem, num_sms, units, grid);
     if (e != cudaSuccess) return e;
     return launch_k(kern, dim3(grid), dim3(threads), smem, st, false, a);
 }
@@ -790,7 +801,8 @@ cudaError_t forward(const NormArgs& a, int num_sms, cudaStream_t st) {
     if (nv <= kOne) return launch_forward<T, 1, false, kOne, 1>(a, cta_threads(nv, 1), num_sms, st);
     if (nv <= kTwo) return launch_forward<T, 2, false, kOne, 1>(a, cta_threads(nv, 2), num_sms, st);
     unsigned grid;
-    const cudaError_t e = resident(norm_long_kernel<T>, 1024, 0, num_sms, a.R, grid);
+    static Known known;
+    const cudaError_t e = resident(norm_long_kernel<T>, known, 1024, 0, num_sms, a.R, grid);
     if (e != cudaSuccess) return e;
     return launch_k(norm_long_kernel<T>, dim3(grid), dim3(1024), 0, st, false, a);
 }

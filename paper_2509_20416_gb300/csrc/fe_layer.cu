@@ -209,7 +209,10 @@ fe_status project_backward(const fe_target* t, const fe_project_backward_args* a
         g.vec = on16(g.dout, es) && on16(g.pre, 4);
         if (!count) {
             FE_TRY(launch_act_grad(g, t->cfg.dtype, st));
-            if (a->dbias) FE_TRY(launch_sum_parts(g.part, g.parts, 1, a->N, a->dbias, a->N, t->cfg.dtype, st));
+            SumJobs sums{};
+            sums.n = a->N;
+            if (a->dbias) sums.add(g.part, g.parts, 1, a->dbias, a->N);
+            FE_TRY(launch_sum_parts(sums, t->cfg.dtype, st));
         }
     }
     return product_gradients(t, a->M, a->N, a->K, a->x, &a->w, &dz, 1, a->dx, &a->dw, w, count, st);
@@ -361,9 +364,12 @@ fe_status norm_backward(const fe_target* t, const fe_block_norm_backward_args* a
     if (a->dgate.p && n.gate_part) n.part_gate = (float*)w.take(bytes);
     if (count) return FE_OK;
     FE_TRY(launch_block_norm_backward(n, dt, st));
-    if (a->dpre_w) FE_TRY(launch_sum_parts(n.part_pre, workers, 1, a->d, a->dpre_w, a->d, dt, st));
-    if (a->dpost_w) FE_TRY(launch_sum_parts(n.part_post, workers, 1, a->d, a->dpost_w, a->d, dt, st));
-    if (a->dgate.p && n.parts) FE_TRY(launch_sum_parts(n.part_gate, n.parts, n.groups, a->d, a->dgate.p, a->dgate.row, dt, st));
+    SumJobs sums{};
+    sums.n = a->d;
+    if (a->dpre_w) sums.add(n.part_pre, workers, 1, a->dpre_w, a->d);
+    if (a->dpost_w) sums.add(n.part_post, workers, 1, a->dpost_w, a->d);
+    if (a->dgate.p && n.parts) sums.add(n.part_gate, n.parts, n.groups, a->dgate.p, a->dgate.row);
+    FE_TRY(launch_sum_parts(sums, dt, st));
     return FE_OK;
 }
 

@@ -94,8 +94,21 @@ cudaError_t gemm_few_prepare();
 int act_grad_parts(int64_t M, int N, fe_dtype dtype, int num_sms);
 cudaError_t launch_act_grad(const ActGradArgs& a, fe_dtype dtype, cudaStream_t st);
 // row g of out [groups, n] = sum over i < parts of part[g][i][n], in order, rounded to the type
-cudaError_t launch_sum_parts(const float* part, int64_t parts, int64_t groups, int64_t n, void* out, int64_t out_row,
-                             fe_dtype dtype, cudaStream_t st);
+struct SumJob {
+    const float* part;
+    int64_t parts, groups;
+    void* out;
+    int64_t out_row;
+};
+struct SumJobs {
+    SumJob job[3];
+    int jobs;
+    int64_t n;
+    void add(const float* part, int64_t parts, int64_t groups, void* out, int64_t out_row) {
+        job[jobs++] = SumJob{part, parts, groups, out, out_row};
+    }
+};
+cudaError_t launch_sum_parts(const SumJobs& a, fe_dtype dtype, cudaStream_t st);
 cudaError_t norm_prepare();
 cudaError_t launch_block_norm(const NormArgs& a, fe_dtype dtype, int num_sms, cudaStream_t st);
 // fills in how the rows are divided, and returns the number of workers: rows of part_post and part_pre

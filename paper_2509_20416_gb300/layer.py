@@ -35,36 +35,37 @@ _ARGS = {
     "fe_token_logprobs_backward": "qiii4x" + _M + "if" + 8 * "P" + _M,
 }
 _PACK = {name: struct.Struct("@" + fmt).pack for name, fmt in _ARGS.items()}
-_WORK = {}
+_CALL, _WORK = {}, {}
 for _name in _ARGS:
-    _f = getattr(_lib, _name)
+    _f = _CALL[_name] = getattr(_lib, _name)
     _f.argtypes = [_vp, ctypes.c_char_p, _vp]
     _f.restype = ctypes.c_int
     if hasattr(_lib, _name + "_work"):
-        _WORK[_name] = getattr(_lib, _name + "_work")
-        _WORK[_name].argtypes = [_vp, ctypes.c_char_p]
-        _WORK[_name].restype = ctypes.c_int64
+        _f = _WORK[_name] = getattr(_lib, _name + "_work")
+        _f.argtypes = [_vp, ctypes.c_char_p]
+        _f.restype = ctypes.c_int64
 _NONE = (0, 0)
-
-
-def _here(x) -> None:
-    if not x.is_cuda:
-        raise ValueError("buffers the kernels access must be CUDA tensors")
-    if x.get_device() != torch.cuda.current_device():
-        raise ValueError("buffers the kernels access must be on the current device")
 
 
 def _mat(x, dtype, shape) -> tuple:
     """The address and row stride of [..., columns] as a matrix; (0, 0) for None."""
     if x is None:
         return _NONE
-    _here(x)
-    if x.dtype != dtype or x.shape != shape:
-        raise ValueError(f"expected a {dtype} tensor of shape {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
+    if x.dtype != dtype or x.shape != shape or not x.is_cuda:
+        _wrong(x, dtype, shape)
+    if x.is_contiguous():
+        n = shape[-1]
+        return x.data_ptr(), n if x.numel() > n else 0
     row = _row(x)
     if row is None:
         raise ValueError(f"columns must be contiguous and rows one stride apart, got strides {tuple(x.stride())} of {tuple(x.shape)}")
     return x.data_ptr(), row
+
+
+def _wrong(x, dtype, shape) -> None:
+    if not x.is_cuda:
+        raise ValueError("buffers the kernels access must be CUDA tensors")
+    raise ValueError(f"expected a {dtype} tensor of shape {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
 
 
 def _row(x):
@@ -86,15 +87,16 @@ def _row(x):
 
 def _dense(x):
     """x, copied where it has no single row stride (gradients may come in any layout)."""
-    return x if _row(x) is not None else x.contiguous()
+    return x if x.is_contiguous() or _row(x) is not None else x.contiguous()
 
 
 def _vec(x, dtype, n) -> int:
     """The address of a contiguous vector of n elements (0 for None)."""
     if x is None:
         return 0
-    _here(x)
-    if x.dtype != dtype or x.shape != (n,) or not x.is_contiguous():
+    if x.dtype != dtype or x.shape != (n,) or not x.is_contiguous() or not x.is_cuda:
+        if not x.is_cuda:
+            raise ValueError("buffers the kernels access must be CUDA tensors")
         raise ValueError(f"expected a contiguous {dtype} tensor of {n} elements, got {x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
 
@@ -105,8 +107,15 @@ def _rows_of(x) -> int:
     return x.numel() // x.shape[-1]
 
 
+def _new(shape, like, side, dtype=None):
+    """A new output of a call (on `side`: allocated there)."""
+    if side is None:
+        return like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
+    return _empty(shape, like.dtype if dtype is None else dtype, like.device, side)
+
+
 def _out(x, shape, like, side):
-    return _empty(shape, like.dtype, like.device, side) if x is None else x
+    return _new(shape, like, side) if x is None else x
 
 
 def _act(act: str) -> int:
@@ -115,35 +124,47 @@ def _act(act: str) -> int:
     return _ACTS[act]
 
 
-def _call(name: str, t: Target, side, tensors, args: tuple, device=None) -> None:
-    """Pack the arguments (without the workspace) and call the library on the current stream or on `side`."""
-    if side is None:
-        raw = _raw_stream(torch.cuda.current_device()) if _raw_stream is not None else _stream(None)
-    else:
-        raw = side.cuda_stream
-        for x in tensors:
-            if x is not None:
+def _call(name: str, t: Target, side, tensors: tuple, args: tuple) -> None:
+    """Pack the arguments (without the workspace) and call the library on the current stream or on `side`; the
+    given `tensors` must lie on the current device."""
+    dev = torch.cuda.current_device()
+    like = None
+    for x in tensors:
+        if x is not None:
+            like = x
+            if x.get_device() != dev:
+                raise ValueError("buffers the kernels access must be on the current device")
+            if side is not None:
                 x.record_stream(side)
-    if name in _WORK:
-        need = _WORK[name](t.ptr, _PACK[name](*args, 0, 0))
+    raw = side.cuda_stream if side is not None else _raw_stream(dev) if _raw_stream is not None else _stream(None)
+    pack, size = _PACK[name], _WORK.get(name)
+    if size is not None:
+        packed = pack(*args, 0, 0)
+        need = size(t.ptr, packed)
         if need > 0:
-            work = _empty((need,), torch.uint8, device, side)
-            args += (work.data_ptr(), need)
-        else:
-            args += _NONE
-    code = getattr(_lib, name)(t.ptr, _PACK[name](*args), raw)
+            work = _new((need,), like, side, torch.uint8)
+            packed = pack(*args, work.data_ptr(), need)
+    else:
+        packed = pack(*args)
+    code = _CALL[name](t.ptr, packed, raw)
     if code:
         _check(code, name)
 
 
-def _recorded(stream, outs, inputs) -> bool:
-    """Whether a call takes part in autograd."""
-    return torch.is_grad_enabled() and all(x is None for x in outs) and _side(stream) is None and \
-        any(x is not None and x.requires_grad for x in inputs)
+def _recorded(stream) -> bool:
+    """Whether a call without outputs given takes part in autograd, if an input does."""
+    return torch.is_grad_enabled() and _side(stream) is None
+
+
+def _wants(*inputs) -> bool:
+    for x in inputs:
+        if x is not None and x.requires_grad:
+            return True
+    return False
 
 
 def _shaped(x, n: int) -> torch.Size:
-    return x.shape[:-1] + (n,)
+    return x.shape if x.shape[-1] == n else x.shape[:-1] + (n,)
 
 
 # ---- fe_project ---------------------------------------------------------------------------
@@ -153,7 +174,7 @@ def fe_project(t: Target, x, w, bias=None, act: str = "none", residual=None, out
     """act(x w^T + bias) + residual (include/fe_layer.h): x [..., K], w [N, K], bias [N], residual
     [..., N]; act: "none", "relu", "silu" or "gelu". out may be the residual itself; pre [..., N], float32,
     takes x w^T + bias, for fe_project_backward."""
-    if _recorded(stream, (out, pre), (x, w, bias, residual)):
+    if out is None and pre is None and _recorded(stream) and _wants(x, w, bias, residual):
         return _Project.apply(t, act, x, w, bias, residual)
     N, K = w.shape
     side, shape, M = _side(stream), _shaped(x, N), _rows_of(x)
@@ -162,7 +183,7 @@ def fe_project(t: Target, x, w, bias=None, act: str = "none", residual=None, out
     out = _out(out, shape, x, side)
     args += (*_mat(out, t.dtype, shape), *_mat(pre, torch.float32, shape), _act(act))
     if M:
-        _call("fe_project", t, side, (x, w, bias, residual, out, pre), args, x.device)
+        _call("fe_project", t, side, (x, w, bias, residual, out, pre), args)
     return out
 
 
@@ -182,7 +203,7 @@ def fe_project_backward(t: Target, dout, x=None, w=None, pre=None, act: str = "n
             *_mat(dout, t.dtype, _shaped(dout, N)), *_mat(pre, torch.float32, dout.shape), *_mat(gx, t.dtype, _shaped(dout, K)),
             *_mat(gw, t.dtype, (N, K)), _vec(gb, t.dtype, N), _act(act))
     if M and (dx or dw or dbias):
-        _call("fe_project_backward", t, side, (dout, x, w, pre, gx, gw, gb), args, dout.device)
+        _call("fe_project_backward", t, side, (dout, x, w, pre, gx, gw, gb), args)
     elif not M:
         _zero(side, gw, gb)
     return gx, gw, gb
@@ -200,7 +221,7 @@ class _Project(torch.autograd.Function):
     @staticmethod
     def forward(ctx, t, act, x, w, bias, residual):
         need = any(ctx.needs_input_grad[2:5])
-        pre = torch.empty(_shaped(x, w.shape[0]), device=x.device) if need and act != "none" else None
+        pre = _new(_shaped(x, w.shape[0]), x, None, torch.float32) if need and act != "none" else None
         out = fe_project(t, x, w, bias, act, residual, pre=pre)
         ctx.t, ctx.act = t, act
         ctx.save_for_backward(x if ctx.needs_input_grad[3] else None, w if ctx.needs_input_grad[2] else None, pre)
@@ -227,7 +248,7 @@ def fe_gated_ffn(t: Target, x, w_gate, w_up, w_down=None, act: str = "silu", res
     and up_pre [..., F], float32, take the two products, for fe_gated_ffn_backward."""
     if w_down is None and residual is not None:
         raise ValueError("a residual needs w_down")
-    if _recorded(stream, (out, gate_pre, up_pre), (x, w_gate, w_up, w_down, residual)):
+    if out is None and gate_pre is None and up_pre is None and _recorded(stream) and _wants(x, w_gate, w_up, w_down, residual):
         return _Gated.apply(t, act, x, w_gate, w_up, w_down, residual)
     if w_down is not None:
         h = fe_gated_ffn(t, x, w_gate, w_up, act=act, gate_pre=gate_pre, up_pre=up_pre, stream=stream)
@@ -238,7 +259,7 @@ def fe_gated_ffn(t: Target, x, w_gate, w_up, w_down=None, act: str = "silu", res
     out = _out(out, shape, x, side)
     args += (*_mat(out, t.dtype, shape), *_mat(gate_pre, torch.float32, shape), *_mat(up_pre, torch.float32, shape), _act(act))
     if M:
-        _call("fe_gated_ffn", t, side, (x, w_gate, w_up, out, gate_pre, up_pre), args, x.device)
+        _call("fe_gated_ffn", t, side, (x, w_gate, w_up, out, gate_pre, up_pre), args)
     return out
 
 
@@ -263,7 +284,7 @@ def fe_gated_ffn_backward(t: Target, dout, gate_pre, up_pre, x=None, w_gate=None
             *_mat(up_pre, torch.float32, shape), *_mat(gx, t.dtype, _shaped(dout, K)), *_mat(gg, t.dtype, (F, K)),
             *_mat(gu, t.dtype, (F, K)), *_mat(gd, t.dtype, (N, F)), _act(act))
     if M:
-        _call("fe_gated_ffn_backward", t, side, (dout, x, w_gate, w_up, w_down, gate_pre, up_pre, gx, gg, gu, gd), args, dout.device)
+        _call("fe_gated_ffn_backward", t, side, (dout, x, w_gate, w_up, w_down, gate_pre, up_pre, gx, gg, gu, gd), args)
     else:
         _zero(side, gg, gu, gd)
     return gx, gg, gu, gd
@@ -272,7 +293,7 @@ def fe_gated_ffn_backward(t: Target, dout, gate_pre, up_pre, x=None, w_gate=None
 class _Gated(torch.autograd.Function):
     @staticmethod
     def forward(ctx, t, act, x, w_gate, w_up, w_down, residual):
-        g, u = (torch.empty(_shaped(x, w_gate.shape[0]), device=x.device) for _ in range(2))
+        g, u = (_new(_shaped(x, w_gate.shape[0]), x, None, torch.float32) for _ in range(2))
         ctx.t, ctx.act = t, act
         _, _, nx, ng, nu, _, _ = ctx.needs_input_grad
         ctx.save_for_backward(g, u, x if ng or nu else None, w_gate if nx else None, w_up if nx else None, w_down)
@@ -306,7 +327,7 @@ def fe_block_norm(t: Target, x, z=None, post: bool | None = None, post_weight=No
     R, d = _rows_of(x), x.shape[-1]
     gate_rows = _gate_rows(gate, gate_rows, R)
     opts = (bool(post), gate_rows, float(scale), float(offset), float(eps))
-    if _recorded(stream, (y, n), (x, z, post_weight, gate, pre_weight)):
+    if y is None and n is None and _recorded(stream) and _wants(x, z, post_weight, gate, pre_weight):
         return _BlockNorm.apply(t, opts, x, z, post_weight, gate, pre_weight)
     side = _side(stream)
     y, n = _out(y, x.shape, x, side), _out(n, x.shape, x, side)
@@ -362,7 +383,7 @@ def fe_block_norm_backward(t: Target, x, z=None, post: bool | None = None, post_
         (*_mat(dy, t.dtype, x.shape), *_mat(dn, t.dtype, x.shape), *_mat(dx, t.dtype, x.shape), *_mat(dz, t.dtype, x.shape),
          *_mat(dg, t.dtype, shapes[3]), _vec(dp, t.dtype, d), _vec(dw, t.dtype, d))
     if R:
-        _call("fe_block_norm_backward", t, side, (x, z, post_weight, gate, pre_weight, dy, dn, dx, dz, dp, dg, dw), args, x.device)
+        _call("fe_block_norm_backward", t, side, (x, z, post_weight, gate, pre_weight, dy, dn, dx, dz, dp, dg, dw), args)
     else:
         _zero(side, dp, dg, dw)
     return dx, dz, dp, dg, dw
@@ -398,7 +419,8 @@ def _tokens(x, lead) -> tuple:
     """tokens [..., J] or [...] (one a row) as [..., J], and J."""
     if x is None:
         return None, 0
-    _here(x)
+    if not x.is_cuda:
+        raise ValueError("buffers the kernels access must be CUDA tensors")
     x = x[..., None] if x.shape == lead else x
     if x.dtype != torch.int32 or x.shape[:-1] != lead:
         raise ValueError(f"tokens must be int32 of shape {tuple(lead)} or {tuple(lead)} + (J,), got {x.dtype} {tuple(x.shape)}")
@@ -411,17 +433,17 @@ def fe_token_logprobs(t: Target, logits, tokens=None, top: int = 0, temperature:
     entropy [...]; lse [...]; top_id [..., top] int32; top_logprob [..., top]): the `top` most probable
     tokens, in order. logprob is None without tokens. stats [..., 2] takes what fe_token_logprobs_backward
     needs of a row."""
-    if _recorded(stream, (stats,), (logits,)):
+    if stats is None and _recorded(stream) and logits.requires_grad:
         out = _Logprobs.apply(t, logits, tokens, top, temperature)
         return (None, *out[1:]) if tokens is None else out
     lead, V = logits.shape[:-1], logits.shape[-1]
     tok, J = _tokens(tokens, lead)
     if logits.dtype not in _LOGITS:
         raise ValueError(f"logits must be float32 or bfloat16, got {logits.dtype}")
-    side, dev = _side(stream), logits.device
-    new = lambda shape, dtype=torch.float32: _empty(shape, dtype, dev, side)
-    logprob = None if tokens is None else new(tokens.shape)
-    entropy, lse, ids, lps = new(lead), new(lead), new(lead + (top,), torch.int32), new(lead + (top,))
+    side, f32 = _side(stream), torch.float32
+    logprob = None if tokens is None else _new(tokens.shape, logits, side, f32)
+    entropy, lse = _new(lead, logits, side, f32), _new(lead, logits, side, f32)
+    ids, lps = _new(lead + (top,), logits, side, torch.int32), _new(lead + (top,), logits, side, f32)
     if stats is not None and (stats.dtype != torch.float32 or stats.shape != lead + (2,) or not stats.is_contiguous() or not stats.is_cuda):
         raise ValueError(f"stats must be a contiguous float32 CUDA tensor of shape {tuple(lead) + (2,)}")
     p = lambda x: 0 if x is None else x.data_ptr()
@@ -449,7 +471,8 @@ def fe_token_logprobs_backward(t: Target, logits, stats, tokens=None, dlogprob=N
     def flat(x, shape, dtype=torch.float32):
         if x is None:
             return None
-        _here(x)
+        if not x.is_cuda:
+            raise ValueError("buffers the kernels access must be CUDA tensors")
         if x.dtype != dtype or x.shape != shape:
             raise ValueError(f"expected {dtype} of shape {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
         return x.contiguous()
@@ -471,7 +494,7 @@ def fe_token_logprobs_backward(t: Target, logits, stats, tokens=None, dlogprob=N
 class _Logprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, t, logits, tokens, top, temperature):
-        stats = torch.empty(logits.shape[:-1] + (2,), device=logits.device)
+        stats = _new(logits.shape[:-1] + (2,), logits, None, torch.float32)
         out = fe_token_logprobs(t, logits, tokens, top, temperature, stats)
         logprob, entropy, _, ids, _ = out
         ctx.t, ctx.temperature = t, temperature
