@@ -1,12 +1,15 @@
 // Matrix products of bfloat16 on the tensor cores (fe_layer.h's products and their gradients): C = A B^T
 // with either operand stored by rows or by its summed index, float32 sums in tensor memory.
 //
-// Persistent pairs of CTAs (cta_group::2) make tiles of 256 x BN: each CTA brings, by TMA, 128 rows of A
-// and BN / 2 of B in slices of 64 of the summed index, so that an SM reads half of what a CTA of its own
-// would for the same products. Warp 0 copies, warp 1 of the first CTA issues the products, warps 2 to 9
-// finish a tile (bias, activation, residual, gate, rounding) while the next one is summed in the
+// Persistent pairs of CTAs (cta_group::2) make tiles of 256 x BN, BN 128 to 256: each CTA brings, by TMA, 128
+// rows of A and BN / 2 of B in slices of 64 of the summed index, so that an SM reads half of what a CTA of
+// its own would for the same products. Warp 0 copies, warp 1 of the first CTA issues the products, warps 2
+// to 9 finish a tile (bias, activation, residual, gate, rounding) while the next one is summed in the
 // other half of tensor memory. The MN-major operand forms spare the gradients every transpose:
 // dx = dz w reads w by columns, dw = dz^T x both operands.
+//
+// BN is the width whose rounds of tiles over the pairs are shortest: 16 x 16 tiles of 256 take 76 pairs 4
+// rounds where 3.4 would hold them, 16 x 19 of 224 take 4 rounds of 7/8.
 #include "fe_gemm_tc.cuh"
 #include "fe_tensor_map.h"
 
@@ -18,19 +21,19 @@ constexpr int kFinishWarps = 8;
 constexpr int kTcThreads = 64 + 32 * kFinishWarps;
 constexpr int kTileM = 256, kSliceK = 64;
 
-template <int BN>
-struct TcTile {
-    static constexpr int kA = 128 * kSliceK * 2, kB = BN / 2 * kSliceK * 2;
-    static constexpr int kStages = BN == 256 ? 5 : 7;
-    static constexpr int kRing = kStages * (kA + kB);
-    static constexpr int kStaging = kFinishWarps * 4096;  // a warp's 32 x 32 floats
-    static constexpr int kTmem = 2 * BN;  // two accumulators
-    static constexpr int kSmem = kRing + kStaging + 1024 /* alignment */ + 512;
-    static_assert(kSmem <= 227 * 1024, "shared memory of a CTA");
+constexpr int kSliceA = 128 * kSliceK * 2;
+constexpr int kStaging = kFinishWarps * 4096;  // a warp's 32 x 32 floats
+constexpr int kTcRing = 188 * 1024, kTcStages = 8;
+constexpr int kTcSmem = kTcRing + kStaging + 1024 /* alignment */ + 512;
+static_assert(kTcSmem <= 227 * 1024, "shared memory of a CTA");
+
+// the tile's width and what follows from it
+struct TcWidth {
+    int bn, b_bytes, stages;  // B's bytes of a slice in a CTA, slices in flight
 };
 
 struct TcBarriers {
-    uint64_t full[8], empty[8], done[2], free[2], drain;
+    uint64_t full[kTcStages], empty[kTcStages], done[2], free[2], drain;
     uint32_t tmem;
 };
 
@@ -112,12 +115,12 @@ struct WarpTile {
     const Finish& e;
     uint32_t d, d2;  // tensor memory: the product, and the gated pair's second
     int64_t m0;
-    int left, n0, width, N, lane;
+    int left, n0, end, lane;  // end: the first column behind the tile
     float* buf;
     __device__ __forceinline__ int row(int i) const { return 4 * i + (lane >> 3); }
     __device__ __forceinline__ int chunk() const { return lane & 7; }
-    __device__ __forceinline__ bool inside(int c) const { return c < width && n0 + c < N; }
-    __device__ __forceinline__ int have(int c) const { return N - n0 - c - 4 * chunk(); }
+    __device__ __forceinline__ bool inside(int c) const { return n0 + c < end; }
+    __device__ __forceinline__ int have(int c) const { return end - n0 - c - 4 * chunk(); }
     template <typename T>
     __device__ __forceinline__ T* at(void* base, int64_t stride, int c) const {
         return (T*)base + (m0 + row(0)) * stride + n0 + c + 4 * chunk();
@@ -260,13 +263,13 @@ __device__ __forceinline__ bool finish_gated_grad(const WarpTile& w, int half, c
     return true;
 }
 
-template <int BN, bool AT, bool BT>
+template <bool AT, bool BT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
-    gemm_tc_kernel(const __grid_constant__ GemmArgs g, const __grid_constant__ TcMaps maps) {
-    using S = TcTile<BN>;
+    gemm_tc_kernel(const __grid_constant__ GemmArgs g, const __grid_constant__ TcMaps maps, const TcWidth shape) {
+    const int BN = shape.bn, stages = shape.stages, stage_bytes = kSliceA + shape.b_bytes;
     extern __shared__ unsigned char raw[];
     unsigned char* const ring = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
-    TcBarriers& bar = *reinterpret_cast<TcBarriers*>(ring + S::kRing + S::kStaging);
+    TcBarriers& bar = *reinterpret_cast<TcBarriers*>(ring + kTcRing + kStaging);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = cluster_rank();
     const bool gated = g.e.kind == FINISH_GATED;
@@ -276,7 +279,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
     const int slices = (g.K + kSliceK - 1) / kSliceK, all = slices * g.segs;
 
     if (warp == 0 && lane == 0) {
-        for (int i = 0; i < S::kStages; ++i) {
+        for (int i = 0; i < stages; ++i) {
             mbar_init(&bar.full[i], 1);
             mbar_init(&bar.empty[i], 1);
         }
@@ -287,7 +290,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
         mbar_init(&bar.drain, 1);
         mbar_fence_init();
     }
-    if (warp == 2) tc2_alloc(&bar.tmem, S::kTmem);
+    if (warp == 2) tc2_alloc(&bar.tmem, 512);  // two accumulators of up to 256 columns
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();
@@ -297,6 +300,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
     if (warp == 0) {  // ---- copies
         if (one_lane()) {
             int64_t n = 0;  // slices so far
+            int slot = 0;
+            uint32_t phase = 0;  // of the slot's current use
             bool ok = true;
             for (int64_t t = first; t < walk.all && ok; t += step) {
                 int prob;
@@ -305,13 +310,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
                 const int m0 = (int)(mt * kTileM + rank * 128);
                 const int n0 = (int)(nt * width) + (gated ? 0 : (int)rank * (BN / 2));
                 for (int c = 0; c < all; ++c, ++n) {
-                    const int slot = (int)(n % S::kStages);
-                    const uint32_t use = (uint32_t)(n / S::kStages);
-                    if (use > 0 && !(ok = mbar_wait(&bar.empty[slot], (use - 1) & 1, g.status))) break;
+                    if (n >= stages && !(ok = mbar_wait(&bar.empty[slot], phase ^ 1, g.status))) break;
                     const int seg = c >= slices, k = (c - seg * slices) * kSliceK;
-                    unsigned char* const a = ring + slot * (S::kA + S::kB);
-                    unsigned char* const b = a + S::kA;
-                    if (rank == 0) mbar_arrive_expect_tx(&bar.full[slot], 2 * (S::kA + S::kB));
+                    unsigned char* const a = ring + slot * stage_bytes;
+                    unsigned char* const b = a + kSliceA;
+                    if (rank == 0) mbar_arrive_expect_tx(&bar.full[slot], 2 * stage_bytes);
                     const uint32_t full = peer_u32(&bar.full[slot], 0);
                     const CUtensorMap* const am = &maps.a[seg + prob];
                     const CUtensorMap* const bm = &maps.b[gated ? (int)rank : seg];
@@ -320,39 +323,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
                     } else {
                         tma_box_pair(a, am, k, m0, full);
                     }
-                    if (BT) {
-                        for (int i = 0; i < BN / 128; ++i) tma_box_pair(b + i * 8192, bm, n0 + 64 * i, k, full);
+                    if (BT) {  // (whole groups of 64 columns: of the last one the product reads what it needs)
+                        for (int i = 0; i < shape.b_bytes / 8192; ++i) tma_box_pair(b + i * 8192, bm, n0 + 64 * i, k, full);
                     } else {
                         tma_box_pair(b, bm, k, n0, full);
                     }
+                    if (++slot == stages) slot = 0, phase ^= 1;
                 }
             }
             if (!ok && rank == 0) {  // (what is in flight lands before the CTA ends)
-                for (int64_t i = n > S::kStages ? n - S::kStages : 0; i < n; ++i)
-                    mbar_wait(&bar.full[i % S::kStages], (uint32_t)(i / S::kStages) & 1, g.status, 50000000LL);
+                for (int64_t i = n > stages ? n - stages : 0; i < n; ++i)
+                    mbar_wait(&bar.full[i % stages], (uint32_t)(i / stages) & 1, g.status, 50000000LL);
             }
         }
         __syncwarp();
     } else if (warp == 1 && rank == 0) {  // ---- products
         const uint32_t id = idesc_bf16_f32(256, BN) | (AT ? 1u << 15 : 0) | (BT ? 1u << 16 : 0);
         if (one_lane()) {
-            int64_t n = 0;
             uint32_t i = 0;  // tiles so far
+            int slot = 0;
+            uint32_t phase = 0;
             bool ok = true;
             for (int64_t t = first; t < walk.all && ok; t += step, ++i) {
-                const uint32_t buf = i & 1, use = i >> 1, d = tmem + buf * BN;
+                const uint32_t buf = i & 1, use = i >> 1, d = tmem + buf * 256;
                 if (use > 0 && !(ok = mbar_wait(&bar.free[buf], (use - 1) & 1, g.status))) break;
                 tc_fence_after();
-                for (int c = 0; c < all; ++c, ++n) {
-                    const int slot = (int)(n % S::kStages);
-                    if (!(ok = mbar_wait(&bar.full[slot], (uint32_t)(n / S::kStages) & 1, g.status))) break;
+                for (int c = 0; c < all; ++c) {
+                    if (!(ok = mbar_wait(&bar.full[slot], phase, g.status))) break;
                     tc_fence_after();
-                    const uint32_t at = smem_u32(ring + slot * (S::kA + S::kB));
-                    const uint64_t ad = operand_desc(at, AT), bd = operand_desc(at + S::kA, BT);
+                    const uint32_t at = smem_u32(ring + slot * stage_bytes);
+                    const uint64_t ad = operand_desc(at, AT), bd = operand_desc(at + kSliceA, BT);
 #pragma unroll
                     for (int k = 0; k < kSliceK / 16; ++k)
                         tc2_mma(d, ad + k * (AT ? 128 : 2), bd + k * (BT ? 128 : 2), id, c > 0 || k > 0);
                     tc2_commit(&bar.empty[slot]);
+                    if (++slot == stages) slot = 0, phase ^= 1;
                 }
                 tc2_commit(&bar.done[buf]);
             }
@@ -364,7 +369,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
         __syncwarp();
     } else if (warp >= 2) {  // ---- results
         const int quarter = warp & 3, half = (warp - 2) >> 2;  // a quarter of the rows, every second 32 columns
-        float* const buf_rows = (float*)(ring + S::kRing) + (warp - 2) * 1024;
+        float* const buf_rows = (float*)(ring + kTcRing) + (warp - 2) * 1024;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         Finish e = g.e;
         uint32_t i = 0;
@@ -372,7 +377,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
             int prob;
             int64_t mt, nt;
             walk.at(t, prob, mt, nt);
-            const uint32_t buf = i & 1, use = i >> 1, d = tmem + buf * BN + lanes;
+            const uint32_t buf = i & 1, use = i >> 1, d = tmem + buf * 256 + lanes;
             const auto wait = [&] {
                 bool ok = true;
                 if (lane == 0) ok = mbar_wait(&bar.done[buf], use & 1, g.status);
@@ -385,7 +390,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
                 e.out_row = g.e.out2_row;
             }
             const int64_t m0 = mt * kTileM + rank * 128 + quarter * 32;
-            const WarpTile w{e, d, d + BN / 2, m0, (int)(m0 < g.M ? min((int64_t)32, g.M - m0) : 0), (int)(nt * width), width, g.N, lane, buf_rows};
+            const WarpTile w{e, d, d + BN / 2, m0, (int)(m0 < g.M ? min((int64_t)32, g.M - m0) : 0), (int)(nt * width), (int)min((int64_t)g.N, (nt + 1) * width), lane, buf_rows};
             if (gated) {
                 if (!wait()) break;
                 finish_gated(w, half);
@@ -401,36 +406,43 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
     }
     __syncthreads();
     cluster_sync_all();
-    if (warp == 2) tc2_dealloc(tmem, S::kTmem);
+    if (warp == 2) tc2_dealloc(tmem, 512);
 }
 
-template <int BN, bool AT, bool BT>
-cudaError_t launch_pairs(const GemmArgs& g, int num_sms, cudaStream_t st) {
-    using S = TcTile<BN>;
-    TcMaps maps{};
+template <bool AT, bool BT>
+cudaError_t launch_tiles(const GemmArgs& g, int num_sms, cudaStream_t st) {
     const bool gated = g.e.kind == FINISH_GATED;
+    const int64_t mt = (g.M + kTileM - 1) / kTileM * (g.twice ? 2 : 1), pairs = num_sms / 2;
+    const auto tiles = [&](int bn) { return mt * ((g.N + (gated ? bn / 2 : bn) - 1) / (gated ? bn / 2 : bn)); };
+    // The width: rounds of tiles, each of its columns' time, or of its copies' where that is more (a column's products
+    // of a slice take as long as the copy of 134 bytes), and of some 16 columns' for its start. B by its summed
+    // index comes in whole groups of 64 columns: there a width of 160 (5120 x 5120 from 4093 rows, 9 rounds)
+    // took 174 us and 256 (6 rounds) 128 us.
+    TcWidth shape{};
+    int64_t best = 0;
+    for (int w = 256; w >= 128; w -= 32) {
+        const int b_bytes = BT ? (w / 2 + 63) / 64 * 8192 : w / 2 * 128, copies = (kSliceA + b_bytes) / 134;
+        const int64_t cost = (tiles(w) + pairs - 1) / pairs * ((w > copies ? w : copies) + 16);
+        if (!best || cost < best) {
+            best = cost;
+            shape.bn = w;
+            shape.b_bytes = b_bytes;
+        }
+    }
+    const int bn = shape.bn;
+    shape.stages = kTcRing / (kSliceA + shape.b_bytes);
+    if (shape.stages > kTcStages) shape.stages = kTcStages;
+    TcMaps maps{};
     for (int i = 0; i < 2; ++i) {
         if (i == 0 || g.segs == 2 || g.twice) {
             if (!(AT ? tensor_map_bf16(&maps.a[i], g.a[i], g.K, g.M, 64) : tensor_map_bf16(&maps.a[i], g.a[i], g.M, g.K, 128))) return cudaErrorInvalidValue;
         }
         if (i == 0 || g.segs == 2 || gated) {
-            if (!(BT ? tensor_map_bf16(&maps.b[i], g.b[i], g.K, g.N, 64) : tensor_map_bf16(&maps.b[i], g.b[i], g.N, g.K, BN / 2))) return cudaErrorInvalidValue;
+            if (!(BT ? tensor_map_bf16(&maps.b[i], g.b[i], g.K, g.N, 64) : tensor_map_bf16(&maps.b[i], g.b[i], g.N, g.K, bn / 2))) return cudaErrorInvalidValue;
         }
     }
-    const int width = gated ? BN / 2 : BN;
-    const int64_t tiles = (g.M + kTileM - 1) / kTileM * ((g.N + width - 1) / width) * (g.twice ? 2 : 1);
-    const int64_t pairs = tiles < num_sms / 2 ? tiles : num_sms / 2;
-    return launch_k(gemm_tc_kernel<BN, AT, BT>, dim3((unsigned)(2 * pairs)), dim3(kTcThreads), S::kSmem, st, false, g, maps);
-}
-
-template <bool AT, bool BT>
-cudaError_t launch_tiles(const GemmArgs& g, int num_sms, cudaStream_t st) {
-    const int64_t mt = (g.M + kTileM - 1) / kTileM * (g.twice ? 2 : 1), pairs = num_sms / 2;
-    const int w = g.e.kind == FINISH_GATED ? 2 : 1;
-    const auto rounds = [&](int bn) { return (mt * ((g.N + bn / w - 1) / (bn / w)) + pairs - 1) / pairs; };
-    // narrow tiles where they take less than the wide ones' rounds: a narrow tile costs some 0.6 of a wide one
-    if (rounds(128) * 6 < rounds(256) * 10) return launch_pairs<128, AT, BT>(g, num_sms, st);
-    return launch_pairs<256, AT, BT>(g, num_sms, st);
+    const int64_t n = tiles(bn) < pairs ? tiles(bn) : pairs;
+    return launch_k(gemm_tc_kernel<AT, BT>, dim3((unsigned)(2 * n)), dim3(kTcThreads), kTcSmem, st, false, g, maps, shape);
 }
 
 // Rows that TMA cannot read (off 16-byte boundaries, repeated) as rows that it can
@@ -442,19 +454,17 @@ __global__ void __launch_bounds__(256) pack_rows_kernel(const bf16_t* src, int64
     }
 }
 
-template <int BN, bool AT, bool BT>
+template <bool AT, bool BT>
 cudaError_t allow() {
-    return cudaFuncSetAttribute(gemm_tc_kernel<BN, AT, BT>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcTile<BN>::kSmem);
+    return cudaFuncSetAttribute(gemm_tc_kernel<AT, BT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem);
 }
 
 }  // namespace
 
 cudaError_t gemm_tc_prepare() {
     cudaError_t e;
-    if ((e = allow<256, false, false>()) != cudaSuccess || (e = allow<256, false, true>()) != cudaSuccess) return e;
-    if ((e = allow<256, true, true>()) != cudaSuccess || (e = allow<128, false, false>()) != cudaSuccess) return e;
-    if ((e = allow<128, false, true>()) != cudaSuccess) return e;
-    return allow<128, true, true>();
+    if ((e = allow<false, false>()) != cudaSuccess || (e = allow<false, true>()) != cudaSuccess) return e;
+    return allow<true, true>();
 }
 
 bool gemm_tc_reads(const fe_mat& m, int64_t rows, int64_t cols) {
