@@ -8,52 +8,71 @@ namespace fe {
 
 namespace {
 
-constexpr int kGradWarps = 8;
+constexpr int kGradWarps = 8, kGradRows = 4;
 
+// a row's columns of a lane, as loaded
 template <typename T>
-__global__ void __launch_bounds__(kGradWarps * 32) act_grad_kernel(const __grid_constant__ ActGradArgs a) {
+struct GradRow {
+    uint4 d;
+    float z[Vec16<T>::kN], u[Vec16<T>::kN];
+};
+template <typename T, bool FULL, bool GATED>
+__device__ __forceinline__ void load_grad_row(const ActGradArgs& a, int64_t m, int n, int have, GradRow<T>& x) {
+    constexpr int V = Vec16<T>::kN;
+    const T* d = (const T*)a.dout.p + m * a.dout.row + n;
+    if (FULL) {
+        x.d = *reinterpret_cast<const uint4*>(d);
+    } else {
+        float f[V];
+        load_row<T, V>(d, have, false, f);
+        x.d = pack16<T>(f);
+    }
+    if (a.pre.p) load_row<float, V>((const float*)a.pre.p + m * a.pre.row + n, FULL ? V : have, FULL, x.z);
+    if (GATED) load_row<float, V>((const float*)a.pre2.p + m * a.pre2.row + n, FULL ? V : have, FULL, x.u);
+}
+
+template <typename T, bool FULL, bool GATED>
+__global__ void __launch_bounds__(kGradWarps * 32, 2) act_grad_kernel(const __grid_constant__ ActGradArgs a) {
     constexpr int V = Vec16<T>::kN;
     __shared__ float sums[kGradWarps][32][V + 1];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int n = (blockIdx.x * 32 + lane) * V, have = a.N - n;
-    const int64_t r0 = a.M * blockIdx.y / a.parts, r1 = a.M * (blockIdx.y + 1) / a.parts;
+    const int64_t r0 = (int64_t)a.part_rows * blockIdx.y, r1 = min(r0 + a.part_rows, a.M);
     float sum[V] = {};
     if (have > 0) {
-        constexpr int F = 4;  // rows of a warp in flight
+        constexpr int F = GATED ? kGradRows / 2 : kGradRows;  // rows of a warp in flight
         for (int64_t r = r0 + warp; r < r1; r += F * kGradWarps) {
-            float d[F][V], z[F][V], u[V];
+            GradRow<T> x[F];
 #pragma unroll
-            for (int f = 0; f < F; ++f) {
-                const int64_t m = r + f * kGradWarps;
-                const int k = m < r1 ? have : 0;
-                load_row<T, V>((const T*)a.dout.p + m * a.dout.row + n, k, a.vec, d[f]);
-                if (a.pre.p) load_row<float, V>((const float*)a.pre.p + m * a.pre.row + n, k, a.vec, z[f]);
-            }
+            for (int f = 0; f < F; ++f)
+                if (r + f * kGradWarps < r1) load_grad_row<T, FULL, GATED>(a, r + f * kGradWarps, n, have, x[f]);
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 const int64_t m = r + f * kGradWarps;
                 if (m >= r1) break;
-                if (a.gated) {
-                    load_row<float, V>((const float*)a.pre2.p + m * a.pre2.row + n, have, a.vec, u);
+                float d[V], e[V];
+                Vec16<T>::widen(x[f].d, d);
+                const float(&z)[V] = x[f].z, (&u)[V] = x[f].u;
+                if (GATED) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         float v, dv;
-                        act_both<kCoarse<T>>(a.act, z[f][i], v, dv);
-                        z[f][i] = d[f][i] * v;
-                        d[f][i] = d[f][i] * u[i] * dv;
+                        act_both<kCoarse<T>>(a.act, z[i], v, dv);
+                        e[i] = d[i] * v;
+                        d[i] = d[i] * u[i] * dv;
                     }
-                    store_row<T, V>((T*)a.d2.p + m * a.d2.row + n, have, a.vec, z[f]);
+                    store_row<T, V>((T*)a.d2.p + m * a.d2.row + n, FULL ? V : have, FULL, e);
                 } else if (a.act != FE_ACT_NONE) {
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         float v, dv;
-                        act_both<kCoarse<T>>(a.act, z[f][i], v, dv);
-                        d[f][i] *= dv;
+                        act_both<kCoarse<T>>(a.act, z[i], v, dv);
+                        d[i] *= dv;
                     }
                 }
-                if (a.d1.p) store_row<T, V>((T*)a.d1.p + m * a.d1.row + n, have, a.vec, d[f]);
+                if (a.d1.p) store_row<T, V>((T*)a.d1.p + m * a.d1.row + n, FULL ? V : have, FULL, d);
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum[i] += d[f][i];
+                for (int i = 0; i < V; ++i) sum[i] += d[i];
             }
         }
     }
@@ -99,17 +118,23 @@ __global__ void __launch_bounds__(kSumWarps * 32) sum_parts_kernel(const __grid_
 
 template <typename T>
 cudaError_t launch_grad(const ActGradArgs& a, cudaStream_t st) {
-    const int strip = 32 * Vec16<T>::kN;
-    return launch_k(act_grad_kernel<T>, dim3((a.N + strip - 1) / strip, a.parts), dim3(kGradWarps * 32), 0, st, false, a);
+    constexpr int V = Vec16<T>::kN, strip = 32 * V;
+    const bool full = a.vec && a.N % V == 0;
+    const auto kern = a.gated ? (full ? act_grad_kernel<T, true, true> : act_grad_kernel<T, false, true>)
+                              : (full ? act_grad_kernel<T, true, false> : act_grad_kernel<T, false, false>);
+    return launch_k(kern, dim3((a.N + strip - 1) / strip, a.parts), dim3(kGradWarps * 32), 0, st, false, a);
 }
 
 }  // namespace
 
-int act_grad_parts(int64_t M, int N, fe_dtype dtype, int num_sms) {
+// A part's rows fill its warps' turns; parts as many as give an SM some eight CTAs, within a grid's bounds.
+void act_grad_plan(ActGradArgs& a, fe_dtype dtype, int num_sms) {
     const int strip = dtype == FE_F32 ? 128 : 256;
-    const int64_t strips = (N + strip - 1) / strip, most = (M + kGradWarps - 1) / kGradWarps;
-    const int64_t want = (num_sms * 8 + strips - 1) / strips;  // eight CTAs an SM
-    return (int)(want < most ? want : most);
+    const int64_t strips = (a.N + strip - 1) / strip, turn = kGradWarps * kGradRows, turns = (a.M + turn - 1) / turn;
+    const int64_t want = (num_sms * 8 + strips - 1) / strips;
+    int64_t k = (turns + want - 1) / want;
+    a.part_rows = (int)(k * turn);
+    a.parts = (int)((a.M + a.part_rows - 1) / a.part_rows);
 }
 
 cudaError_t launch_act_grad(const ActGradArgs& a, fe_dtype dtype, cudaStream_t st) {

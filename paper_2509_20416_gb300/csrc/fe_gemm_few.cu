@@ -46,6 +46,14 @@ __global__ void __launch_bounds__(kFewThreads)
     int cols = 32;
     while (cols < f.nt) cols *= 2;
 
+    const auto copy = [&](int k, int slot) {
+        unsigned char* const w = ring + slot * f.stage_bytes;
+        mbar_arrive_expect_tx(&bar.full[slot], 16384 + f.nt * 128);
+        tma_box(w, &wmap0, k * 64, n0, &bar.full[slot]);
+        if (gated) tma_box(w + 8192, &wmap1, k * 64, n0, &bar.full[slot]);
+        tma_box(w + 16384, &xmap, k * 64, 0, &bar.full[slot]);
+    };
+    const int ahead = min(f.stages, k1 - k0);
     if (warp == 0 && lane == 0) {
         for (int i = 0; i < f.stages; ++i) {
             mbar_init(&bar.full[i], 1);
@@ -53,6 +61,7 @@ __global__ void __launch_bounds__(kFewThreads)
         }
         mbar_init(&bar.done, 1);
         mbar_fence_init();
+        for (int i = 0; i < ahead; ++i) copy(k0 + i, i);  // (before the CTA is set up)
     }
     if (warp == 1) tc_alloc(&bar.tmem, cols);
     tc_fence_before();
@@ -61,18 +70,13 @@ __global__ void __launch_bounds__(kFewThreads)
     const uint32_t tmem = bar.tmem;
 
     if (warp == 0) {  // ---- copies
-        if (one_lane()) {
-            int slot = 0;
-            uint32_t phase = 0;
+        if (lane == 0) {
+            int slot = ahead == f.stages ? 0 : ahead, n = ahead;
+            uint32_t phase = 0;  // of the slot's use before
             bool ok = true;
-            int n = 0;
-            for (int k = k0; k < k1; ++k, ++n) {
-                if (n >= f.stages && !(ok = mbar_wait(&bar.empty[slot], phase ^ 1, g.status))) break;
-                unsigned char* const w = ring + slot * f.stage_bytes;
-                mbar_arrive_expect_tx(&bar.full[slot], 16384 + f.nt * 128);
-                tma_box(w, &wmap0, k * 64, n0, &bar.full[slot]);
-                tma_box(w + 8192, &wmap1, k * 64, gated ? n0 : n0 + 64, &bar.full[slot]);
-                tma_box(w + 16384, &xmap, k * 64, 0, &bar.full[slot]);
+            for (int k = k0 + ahead; k < k1; ++k, ++n) {
+                if (!(ok = mbar_wait(&bar.empty[slot], phase, g.status))) break;
+                copy(k, slot);
                 if (++slot == f.stages) slot = 0, phase ^= 1;
             }
             if (!ok) {  // (what is in flight lands before the CTA ends)
@@ -205,7 +209,7 @@ cudaError_t launch_gemm_few(const GemmArgs& g, int num_sms, cudaStream_t st) {
     smem = (smem > part ? smem : part) + 1024;
     CUtensorMap w0, w1, x;
     const auto map = [](CUtensorMap* m, const fe_mat& a, int64_t r, int64_t c, int box_rows) { return tensor_map_bf16(m, a, r, c, box_rows); };
-    if (!map(&w0, g.b[0], g.N, g.K, 64) || !map(&w1, g.b[gated ? 1 : 0], g.N, g.K, 64) || !map(&x, g.a[0], g.M, g.K, f.nt)) return cudaErrorInvalidValue;
+    if (!map(&w0, g.b[0], g.N, g.K, rows) || !map(&w1, g.b[gated ? 1 : 0], g.N, g.K, rows) || !map(&x, g.a[0], g.M, g.K, f.nt)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(blocks * f.ranks));
     cfg.blockDim = dim3(kFewThreads);

@@ -4,7 +4,8 @@
 // A CTA of 256 threads makes a BM x BN tile, a thread BM/16 x BN/16 of it in registers: per step of
 // the summed index it reads (BM + BN) / 16 floats from shared memory for BM BN / 256 products. The
 // products go in pairs of columns (fma.rn.f32x2). Slices of 16 steps alternate between two buffers;
-// the next slice's loads are in flight while a slice is multiplied.
+// the next slice's loads, or the next four's of a small tile, whose products are done before a load comes
+// back, are in flight while a slice is multiplied.
 #include "fe_layer_common.cuh"
 
 namespace fe {
@@ -84,7 +85,7 @@ __device__ __forceinline__ void read_run(const float* s, float* f) {
     }
 }
 
-template <typename T, int BM, int BN, bool AT, bool BT>
+template <typename T, int BM, int BN, bool AT, bool BT, int P>
 __global__ void __launch_bounds__(256) gemm_simt_kernel(const __grid_constant__ GemmArgs g, int a_vec, int b_vec) {
     constexpr int HM = BM / 32, HN = BN / 32;  // a thread's rows and columns: HM and HN in each half of the tile
     __shared__ float As[2][kBK][BM + 4], Bs[2][kBK][BN + 4];
@@ -102,41 +103,50 @@ __global__ void __launch_bounds__(256) gemm_simt_kernel(const __grid_constant__ 
 #pragma unroll
         for (int j = 0; j < HN; ++j) acc[i][j] = 0;
     const int slices = (g.K + kBK - 1) / kBK, all = slices * g.segs;
-    Slice<T, BM, AT> a;
-    Slice<T, BN, BT> b;
-    const auto fetch = [&](int s) {
+    Slice<T, BM, AT> a[P];  // slices i + 1 to i + P, on their way while slice i is multiplied
+    Slice<T, BN, BT> b[P];
+    const auto fetch = [&](int s, int p) {
+        if (s >= all) return;
         const int seg = s >= slices;
         const int k0 = (s - seg * slices) * kBK;
-        a.load(g.a[seg + prob], m0, g.M, k0, g.K, a_vec, 0, g.a[0]);
-        b.load(g.b[seg], n0, g.N, k0, g.K, b_vec, g.e.kind == FINISH_GATED ? width : 0, g.b[1]);
+        a[p].load(g.a[seg + prob], m0, g.M, k0, g.K, a_vec, 0, g.a[0]);
+        b[p].load(g.b[seg], n0, g.N, k0, g.K, b_vec, g.e.kind == FINISH_GATED ? width : 0, g.b[1]);
     };
-    fetch(0);
-    a.store(As[0]);
-    b.store(Bs[0]);
+#pragma unroll
+    for (int p = 0; p < P; ++p) fetch(p, p);
+    a[0].store(As[0]);
+    b[0].store(Bs[0]);
+    fetch(P, 0);
     __syncthreads();
-    for (int s = 0; s < all; ++s) {
-        if (s + 1 < all) fetch(s + 1);
-        const float(*sa)[BM + 4] = As[s & 1];
-        const float(*sb)[BN + 4] = Bs[s & 1];
+    for (int s0 = 0; s0 < all; s0 += P) {
 #pragma unroll
-        for (int k = 0; k < kBK; ++k) {
-            float av[2 * HM], bv[2 * HN];
-            read_run<HM>(&sa[k][ty * HM], av);
-            read_run<HM>(&sa[k][BM / 2 + ty * HM], av + HM);
-            read_run<HN>(&sb[k][tx * HN], bv);
-            read_run<HN>(&sb[k][BN / 2 + tx * HN], bv + HN);
+        for (int p = 0; p < P; ++p) {
+            const int s = s0 + p;
+            if (s >= all) break;
+            const float(*sa)[BM + 4] = As[s & 1];
+            const float(*sb)[BN + 4] = Bs[s & 1];
 #pragma unroll
-            for (int i = 0; i < 2 * HM; ++i) {
-                const uint64_t ai = pair_f32(av[i]);
+            for (int k = 0; k < kBK; ++k) {
+                float av[2 * HM], bv[2 * HN];
+                read_run<HM>(&sa[k][ty * HM], av);
+                read_run<HM>(&sa[k][BM / 2 + ty * HM], av + HM);
+                read_run<HN>(&sb[k][tx * HN], bv);
+                read_run<HN>(&sb[k][BN / 2 + tx * HN], bv + HN);
 #pragma unroll
-                for (int j = 0; j < HN; ++j)
-                    acc[i][j] = fma_x2(ai, pair_f32(__float_as_uint(bv[2 * j]), __float_as_uint(bv[2 * j + 1])), acc[i][j]);
+                for (int i = 0; i < 2 * HM; ++i) {
+                    const uint64_t ai = pair_f32(av[i]);
+#pragma unroll
+                    for (int j = 0; j < HN; ++j)
+                        acc[i][j] = fma_x2(ai, pair_f32(__float_as_uint(bv[2 * j]), __float_as_uint(bv[2 * j + 1])), acc[i][j]);
+                }
             }
-        }
-        if (s + 1 < all) {
-            a.store(As[(s + 1) & 1]);
-            b.store(Bs[(s + 1) & 1]);
-            __syncthreads();
+            if (s + 1 < all) {
+                const int q = (p + 1) % P;
+                a[q].store(As[(s + 1) & 1]);
+                b[q].store(Bs[(s + 1) & 1]);
+                fetch(s + 1 + P, q);
+                __syncthreads();
+            }
         }
     }
     Finish e = g.e;
@@ -175,7 +185,7 @@ cudaError_t launch_tile(const GemmArgs& g, cudaStream_t st) {
     bool av = true, bv = true;
     for (int i = 0; i < na; ++i) av = av && runs_of_4(g.a[i], es);
     for (int i = 0; i < nb; ++i) bv = bv && runs_of_4(g.b[i], es);
-    return launch_k(gemm_simt_kernel<T, BM, BN, AT, BT>, dim3((unsigned)tiles), dim3(256), 0, st, false, g, (int)av, (int)bv);
+    return launch_k(gemm_simt_kernel<T, BM, BN, AT, BT, BM == 64 ? 4 : 1>, dim3((unsigned)tiles), dim3(256), 0, st, false, g, (int)av, (int)bv);
 }
 
 template <typename T, bool AT, bool BT>

@@ -204,7 +204,7 @@ fe_status project_backward(const fe_target* t, const fe_project_backward_args* a
         g.dout = a->dout;
         if (a->act != FE_ACT_NONE) g.pre = a->pre;
         if (make) g.d1 = dz;
-        g.parts = act_grad_parts(a->M, a->N, t->cfg.dtype, t->num_sms);
+        act_grad_plan(g, t->cfg.dtype, t->num_sms);
         if (a->dbias) g.part = (float*)w.take((int64_t)g.parts * a->N * sizeof(float));
         g.vec = on16(g.dout, es) && on16(g.pre, 4);
         if (!count) {
@@ -290,7 +290,7 @@ fe_status gated_backward(const fe_target* t, const fe_gated_ffn_backward_args* a
         g.pre2 = a->up_pre;
         g.d1 = dz[0];
         g.d2 = dz[1];
-        g.parts = act_grad_parts(a->M, a->F, t->cfg.dtype, t->num_sms);
+        act_grad_plan(g, t->cfg.dtype, t->num_sms);
         g.vec = on16(g.dout, es) && on16(g.pre, 4) && on16(g.pre2, 4);
         if (!count) FE_TRY(launch_act_grad(g, t->cfg.dtype, st));
     }

@@ -42,7 +42,7 @@ struct ActGradArgs {
     fe_mat dout, pre, pre2;   // pre2, d2: gated only
     fe_mat d1, d2;            // d1 may be absent
     float* part;              // [parts][N] sums over the rows of each part, or NULL
-    int parts;
+    int parts, part_rows;
     int vec;
 };
 
@@ -90,8 +90,8 @@ cudaError_t gemm_tc_prepare();
 bool gemm_few_takes(const GemmArgs& a);
 cudaError_t launch_gemm_few(const GemmArgs& a, int num_sms, cudaStream_t st);
 cudaError_t gemm_few_prepare();
-// parts of the rows that fe_project_backward's sums and the activation's gradient are split into
-int act_grad_parts(int64_t M, int N, fe_dtype dtype, int num_sms);
+// divides the rows into parts
+void act_grad_plan(ActGradArgs& a, fe_dtype dtype, int num_sms);
 cudaError_t launch_act_grad(const ActGradArgs& a, fe_dtype dtype, cudaStream_t st);
 // row g of out [groups, n] = sum over i < parts of part[g][i][n], in order, rounded to the type
 struct SumJob {
