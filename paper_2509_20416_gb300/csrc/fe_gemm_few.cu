@@ -24,12 +24,6 @@ struct FewBarriers {
     uint32_t tmem;
 };
 
-__device__ __forceinline__ float load_peer(uint32_t addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-
 __global__ void __launch_bounds__(kFewThreads)
     gemm_few_kernel(const __grid_constant__ GemmArgs g, const __grid_constant__ CUtensorMap wmap0, const __grid_constant__ CUtensorMap wmap1,
                     const __grid_constant__ CUtensorMap xmap, const __grid_constant__ FewArgs f) {
