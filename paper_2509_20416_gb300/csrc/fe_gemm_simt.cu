@@ -108,7 +108,9 @@ __global__ void __launch_bounds__(256, BM == 128 ? 2 : 3)
     if (prob) t -= nt * mt;
     const int64_t m0 = t / nt * BM;
     const int n0 = (int)(t % nt) * width;
-    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    // a warp's lanes are 4 x 8 threads of the tile, so that each of its reads of a slice is one turn of the banks
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int tx = warp % 2 * 8 + lane % 8, ty = warp / 2 * 4 + lane / 8;
     uint64_t acc[2 * HM][HN];
 #pragma unroll
     for (int i = 0; i < 2 * HM; ++i)
