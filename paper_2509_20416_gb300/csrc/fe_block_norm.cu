@@ -120,8 +120,7 @@ struct RowRing {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-constexpr int forward_depth(int vpt) { return vpt == 1 ? 4 : 3; }
-constexpr int kBackwardDepth = 2;
+constexpr int kNormDepth = 2;  // rows of a worker on their way
 
 // the group of rows that share a gate (rows are below 2^30)
 __device__ __forceinline__ int64_t group_of(const NormArgs& a, int64_t r) {
@@ -130,7 +129,7 @@ __device__ __forceinline__ int64_t group_of(const NormArgs& a, int64_t r) {
 
 template <typename T, int VPT, bool WARP, int MAXT, int CTAS, bool FULL>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant__ NormArgs a) {
-    constexpr int V = Vec16<T>::kN, N = V / 2, D = forward_depth(VPT);
+    constexpr int V = Vec16<T>::kN, N = V / 2, D = kNormDepth;
     extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
@@ -157,24 +156,30 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
         pz += sz_;
         next += step;
     };
-    // one vector a thread: the weights stay in registers
-    constexpr bool HOLD = VPT == 1;
-    uint4 hold_post = make_uint4(0, 0, 0, 0), hold_pre = hold_post;
-    if (HOLD && tid * V < a.d) {
-        if (a.post_w) hold_post = load_vec<T, FULL>((const T*)a.post_w + tid * V, a.d - tid * V, a.vec);
-        if (a.pre_w) hold_pre = load_vec<T, FULL>((const T*)a.pre_w + tid * V, a.d - tid * V, a.vec);
-    }
-    const auto held = [&](const void* w, const uint4& hold, int c, int have, Pairs<T>& p) {
-        p.widen(HOLD || !w ? hold : load_vec<T, FULL>((const T*)w + c, have, a.vec));
+    // a thread's weights as they are stored, behind the rows
+    const auto hold = [&](int array, int j) { return ring_mem + threadIdx.x + ((D * 2 + array) * VPT + j) * blockDim.x; };
 #pragma unroll
-        for (int i = 0; i < N; ++i) p.v[i] = w ? add_x2(p.v[i], pair_f32(a.offset)) : pair_f32(1.f);
+    for (int j = 0; j < VPT; ++j) {
+        const int c = (j * nt + tid) * V, have = a.d - c;
+        if (a.post_w && have > 0) *hold(0, j) = load_vec<T, FULL>((const T*)a.post_w + c, have, a.vec);
+        if (a.pre_w && have > 0) *hold(1, j) = load_vec<T, FULL>((const T*)a.pre_w + c, have, a.vec);
+    }
+    const auto held = [&](const void* w, int array, int j, Pairs<T>& p) {
+        if (!w) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) p.v[i] = pair_f32(1.f);
+            return;
+        }
+        p.widen(*hold(array, j));
+#pragma unroll
+        for (int i = 0; i < N; ++i) p.v[i] = add_x2(p.v[i], pair_f32(a.offset));
     };
     T *py = (T*)a.y.p + r * a.y.row, *pn = (T*)a.n.p + r * a.n.row;
     const uint64_t sc = pair_f32(a.scale);
-    for (int i = 0; i < D - 1; ++i) fetch(i);
+    for (int i = 0; i < D; ++i) fetch(i);
     int slot = 0;
     for (; r < a.R; r += step, slot = slot + 1 == D ? 0 : slot + 1) {
-        cp_wait<D - 2>();
+        cp_wait<D - 1>();
         Pairs<T> y[VPT], z[VPT];
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
@@ -182,8 +187,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
             y[j].widen(has ? *ring.at(slot, 0, j) : make_uint4(0, 0, 0, 0));
             z[j].widen(has && a.z.p ? *ring.at(slot, 1, j) : make_uint4(0, 0, 0, 0));
         }
-        // (into the slot that was read last; outputs may be the inputs themselves: rows that were read before)
-        fetch(slot == 0 ? D - 1 : slot - 1);
+        fetch(slot);  // (outputs may be the inputs themselves: rows that have been read)
         float scale_z = 1.f;
         if (a.post) {
             uint64_t q = 0;
@@ -204,7 +208,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
             if (a.z.p) {
                 Pairs<T> w;
                 if (a.post) {
-                    held(a.post_w, hold_post, c, have, w);
+                    held(a.post_w, 0, j, w);
                     const uint64_t sz = pair_f32(scale_z);
 #pragma unroll
                     for (int i = 0; i < N; ++i) z[j].v[i] = mul_x2(mul_x2(z[j].v[i], sz), w.v[i]);
@@ -235,7 +239,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
             const int c = (j * nt + tid) * V, have = a.d - c;
             if (have <= 0) continue;
             Pairs<T> w;
-            held(a.pre_w, hold_pre, c, have, w);
+            held(a.pre_w, 1, j, w);
 #pragma unroll
             for (int i = 0; i < N; ++i) w.v[i] = mul_x2(mul_x2(y[j].v[i], sy), w.v[i]);
             float f[V];
@@ -372,7 +376,7 @@ __device__ __forceinline__ void in_turn() { asm volatile("" ::: "memory"); }
 
 template <typename T, int VPT, bool WARP, int MAXT, int CTAS, bool FULL>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a, int64_t workers) {
-    constexpr int V = Vec16<T>::kN, N = V / 2, HN = N / 2, D = kBackwardDepth;
+    constexpr int V = Vec16<T>::kN, N = V / 2, HN = N / 2, D = kNormDepth;
     extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
@@ -782,7 +786,7 @@ template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
 cudaError_t launch_forward(const NormArgs& a, int threads, int num_sms, cudaStream_t st) {
     unsigned grid;
     const auto kern = whole<T>(a) ? norm_kernel<T, VPT, WARP, MAXT, CTAS, true> : norm_kernel<T, VPT, WARP, MAXT, CTAS, false>;
-    const size_t smem = (size_t)forward_depth(VPT) * 2 * VPT * threads * sizeof(uint4);
+    const size_t smem = (size_t)(kNormDepth + 1) * 2 * VPT * threads * sizeof(uint4);
     const int64_t units = WARP ? (a.R + threads / 32 - 1) / (threads / 32) : a.R;
     static Known known[2];
     const cudaError_t e = resident(kern, known[whole<T>(a)], threads, smem, num_sms, units, grid);
@@ -791,14 +795,15 @@ cudaError_t launch_forward(const NormArgs& a, int threads, int num_sms, cudaStre
 }
 
 // vectors of a row: a warp's at most, a CTA's with one or two a thread, and more
-constexpr int kWarpVecs = 32, kNarrow = 640, kOne = 1024, kTwo = 2048;
+constexpr int kWarpVecs = 32, kOne = 1024, kTwo = 2048;
 
 template <typename T>
 cudaError_t forward(const NormArgs& a, int num_sms, cudaStream_t st) {
     const int64_t nv = (a.d + Vec16<T>::kN - 1) / Vec16<T>::kN;
     if (nv <= kWarpVecs) return launch_forward<T, 1, true, kNormWarps * 32, 8>(a, kNormWarps * 32, num_sms, st);
-    if (nv <= kNarrow) return launch_forward<T, 1, false, kNarrow, 2>(a, cta_threads(nv, 1), num_sms, st);
-    if (nv <= kOne) return launch_forward<T, 1, false, kOne, 1>(a, cta_threads(nv, 1), num_sms, st);
+    if (nv <= 256) return launch_forward<T, 1, false, 256, 4>(a, cta_threads(nv, 1), num_sms, st);
+    if (nv <= 640) return launch_forward<T, 2, false, 320, 3>(a, cta_threads(nv, 2), num_sms, st);
+    if (nv <= kOne) return launch_forward<T, 2, false, 512, 2>(a, cta_threads(nv, 2), num_sms, st);
     if (nv <= kTwo) return launch_forward<T, 2, false, kOne, 1>(a, cta_threads(nv, 2), num_sms, st);
     unsigned grid;
     static Known known;
@@ -822,7 +827,7 @@ cudaError_t backward(const NormArgs& a, fe_dtype dtype, cudaStream_t st) {
     const int threads = form_threads(form, nv);
     const int64_t workers = a.parts ? a.groups * a.parts : (a.groups + a.step - 1) / a.step;
     const int vpt = form == BY_CTA_2 ? 2 : 1;
-    const size_t smem = (size_t)(kBackwardDepth * 4 + 3) * vpt * threads * sizeof(uint4);
+    const size_t smem = (size_t)(kNormDepth * 4 + 3) * vpt * threads * sizeof(uint4);
     const dim3 grid((unsigned)workers);
     switch (form) {
         case BY_WARP:
@@ -849,9 +854,10 @@ cudaError_t allow(K kern, size_t bytes) {
 template <typename T, bool FULL>
 cudaError_t prepare() {
     cudaError_t e;
-    const size_t f = forward_depth(1) * 2 * sizeof(uint4), f2 = forward_depth(2) * 4 * sizeof(uint4), b = (kBackwardDepth * 4 + 3) * sizeof(uint4);
-    if ((e = allow(norm_kernel<T, 1, false, kNarrow, 2, FULL>, f * kNarrow)) != cudaSuccess) return e;
-    if ((e = allow(norm_kernel<T, 1, false, kOne, 1, FULL>, f * kOne)) != cudaSuccess) return e;
+    const size_t f = (kNormDepth + 1) * 2 * sizeof(uint4), f2 = 2 * f, b = (kNormDepth * 4 + 3) * sizeof(uint4);
+    if ((e = allow(norm_kernel<T, 1, false, 256, 4, FULL>, f * 256)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 2, false, 320, 3, FULL>, f2 * 320)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 2, false, 512, 2, FULL>, f2 * 512)) != cudaSuccess) return e;
     if ((e = allow(norm_kernel<T, 2, false, kOne, 1, FULL>, f2 * kOne)) != cudaSuccess) return e;
     if ((e = allow(norm_backward_kernel<T, 1, false, 320, 2, FULL>, b * 320)) != cudaSuccess) return e;
     if ((e = allow(norm_backward_kernel<T, 2, false, 320, 2, FULL>, b * 2 * 320)) != cudaSuccess) return e;
