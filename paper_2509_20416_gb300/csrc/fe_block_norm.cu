@@ -371,9 +371,6 @@ __device__ __forceinline__ void store_packed(T* p, int have, bool vec, const uin
             if (i < have) p[i] = e[i];
     }
 }
-// (the compiler is not to gather loads of later halves in front: their registers would not be there)
-__device__ __forceinline__ void in_turn() { asm volatile("" ::: "memory"); }
-
 template <typename T, int VPT, bool WARP, int MAXT, int CTAS, bool FULL>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a, int64_t workers) {
     constexpr int V = Vec16<T>::kN, N = V / 2, HN = N / 2, D = kNormDepth;
@@ -533,7 +530,6 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
                 }
 #pragma unroll
                 for (int i = 0; i < HN; ++i) y[j][h * HN + i] = f.v[i];
-                in_turn();
             }
         }
         float scale_y = 0.f, back = 0.f;
@@ -585,7 +581,6 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
                         y[j][k] = dp;
                     }
                 }
-                in_turn();
             }
             if (a.dx.p) store_packed<T, FULL>((T*)a.dx.p + r * a.dx.row + c, have, a.vec, out[0], out[1]);
         }
