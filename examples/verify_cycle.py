@@ -1,8 +1,9 @@
 """Greedy speculative decoding end to end on the GPU: the drafter's trees verified by a small
-attention-only target whose layers run on the target-side operators (Sec. 2.4 of FastEagle,
-"Parallel Verification" and "Update and Iterate"). Random weights stand in for trained ones.
+target whose layers run on the target-side operators (Sec. 2.4 of FastEagle, "Parallel
+Verification" and "Update and Iterate"): attention alone with PyTorch's matrix products, or whole
+layers on the dense operators. Random weights stand in for trained ones.
 
-    python examples/verify_cycle.py [--cache f32|bf16|e4m3] [--steps N]
+    python examples/verify_cycle.py [--cache f32|bf16|e4m3] [--target attention|layers] [--steps N]
 
 prints the accepted tokens per cycle and checks that the text equals token-by-token decoding.
 """
@@ -59,6 +60,46 @@ class ToyTarget:
         u = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-5)
         feat = torch.cat([states[0], states[len(states) // 2], states[-1]], -1)
         return (u @ self.head.T).argmax(-1).to(torch.int32), feat
+
+
+class LayerTarget(ToyTarget):
+    """Whole layers: attention and a gated feed-forward block, each with a norm before it and the
+    attention's with one behind it, and a head whose most probable token is the next."""
+
+    def __init__(self, cfg: dict, W: dict, cache: str, batch: int, max_seq: int, n_layers: int = 2, page_size: int = 16,
+                 seed: int = 1):
+        super().__init__(cfg, W, cache, batch, max_seq, n_layers, page_size, seed)
+        g = torch.Generator().manual_seed(seed + 1)
+        mat = lambda *s: (torch.randn(*s, generator=g) / s[-1] ** 0.5).to(self.dt).cuda()
+        gain = lambda: (1 + 0.1 * torch.randn(self.d, generator=g)).to(self.dt).cuda()
+        for L in self.layers:
+            L.update(attn_norm=gain(), post_norm=gain(), mlp_norm=gain(), gate=mat(cfg["ffn"], self.d), up=mat(cfg["ffn"], self.d),
+                     down=mat(self.d, cfg["ffn"]))
+        self.final_norm = gain()
+        self.embed, self.head = self.embed.to(self.dt), self.head.to(self.dt)
+
+    def forward(self, tok, pos, start, n_rows=None, mask=None):
+        B, T = tok.shape
+        t = self.t
+        x = self.embed[tok.long()] * 50.0
+        states = [x]
+        for i, L in enumerate(self.layers):
+            _, u = fe.fe_block_norm(t, x, pre_weight=L["attn_norm"])
+            qkv = fe.fe_project(t, u, L["qkv"]).view(B, T, self.H + 2 * self.Hkv, self.hd)
+            q, k, v = qkv.split([self.H, self.Hkv, self.Hkv], 2)
+            q = fe.fe_cache_write(t, self.cache, i, k, v, start, n_rows=n_rows, pos=pos, q=q)
+            a, _ = fe.fe_tree_attention(t, self.cache, i, q, start, mask=mask, n_nodes=n_rows)
+            o = fe.fe_project(t, a.reshape(B, T, -1), L["o"])
+            x, u = fe.fe_block_norm(t, x, o, post_weight=L["post_norm"], pre_weight=L["mlp_norm"])
+            x = fe.fe_gated_ffn(t, u, L["gate"], L["up"], w_down=L["down"], residual=x)
+            states.append(x)
+        _, u = fe.fe_block_norm(t, x, pre_weight=self.final_norm)
+        top = fe.fe_token_logprobs(t, fe.fe_project(t, u, self.head), top=1)[3]
+        feat = torch.cat([states[0], states[len(states) // 2], states[-1]], -1).float()
+        return top[..., 0].contiguous(), feat
+
+
+TARGETS = {"attention": ToyTarget, "layers": LayerTarget}
 
 
 def decode_plain(target: ToyTarget, prompts, steps: int):
@@ -138,24 +179,26 @@ def decode_drafted(target: ToyTarget, h, cfg: dict, prompts, steps: int, top_k: 
     return [t[:steps] for t in text], accepted
 
 
-def run(cache: str = "f32", steps: int = 24, batch: int = 3, seed: int = 0):
+def run(cache: str = "f32", steps: int = 24, batch: int = 3, seed: int = 0, target: str = "attention"):
     """Both decodings on fresh caches; returns (drafted text, plain text, accepted per cycle)."""
+    make = TARGETS[target]
     cfg = wl.make_config("tiny", B=batch, max_seq=128)
     W = wl.make_weights(cfg)
     h = fe.fe_draft_init(dict(cfg, max_batch=batch), W)
     g = torch.Generator().manual_seed(seed)
     prompts = [torch.randint(0, cfg["vocab"], (5 + 4 * b,), generator=g).tolist() for b in range(batch)]
-    plain = decode_plain(ToyTarget(cfg, W, cache, batch, 128), prompts, steps)
-    text, accepted = decode_drafted(ToyTarget(cfg, W, cache, batch, 128), h, cfg, prompts, steps, forced=plain)
+    plain = decode_plain(make(cfg, W, cache, batch, 128), prompts, steps)
+    text, accepted = decode_drafted(make(cfg, W, cache, batch, 128), h, cfg, prompts, steps, forced=plain)
     return text, plain.tolist(), accepted
 
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--cache", default="f32", choices=["f32", "bf16", "e4m3"])
+    ap.add_argument("--target", default="attention", choices=list(TARGETS))
     ap.add_argument("--steps", type=int, default=24)
     a = ap.parse_args()
-    text, plain, accepted = run(a.cache, a.steps)
+    text, plain, accepted = run(a.cache, a.steps, target=a.target)
     print("accepted per cycle:", accepted)
     print("equal to token-by-token decoding:", text == plain)
 
