@@ -269,7 +269,6 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_con
             }
         };
         // (whole warps: the turns of a warp are its first lane's)
-#pragma unroll 2
         for (int v = r.v0 + warp * 32; v < r.v1; v += B * step) {
             uint4 raw[B];
 #pragma unroll
@@ -456,7 +455,6 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_backward_kernel(const _
                 for (int i = 0; i < V; ++i) store_one(g + i, x[i]);
             }
         };
-#pragma unroll 2
         for (; v < r.v1; v += 4 * step) {
             uint4 raw[4];
 #pragma unroll
