@@ -6,7 +6,7 @@
 //
 // The K largest: of the threads' largest elements 32 groups are made; the K-th largest group maximum
 // is no larger than the K-th largest element of the row, so the elements of the few threads whose maximum
-// reaches it are looked through again, a warp a thread's share, and those that reach it are noted. Rank
+// reaches it are looked through again by all threads, and those that reach it are noted. Rank
 // among the notes is place in the result. Where more elements reach it than there is room for (equal
 // logits, or a row whose large elements all fall to few threads), the CTA takes out its largest element
 // K times instead.
@@ -25,7 +25,7 @@ namespace cg = cooperative_groups;
 
 constexpr int kTopMax = 32, kTokMax = 64;
 constexpr int kNotes = 512;
-constexpr int kLpThreads = 256;  // four CTAs an SM, each thread with up to eight vectors on their way or at hand
+constexpr int kLpThreads = 256;  // that read a row (four CTAs an SM)
 constexpr float kLn2 = 0.6931471805599453f;
 
 // order of (value, index): larger first by value (NaN above all, -0 equal to 0), then smaller index
@@ -36,6 +36,11 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t index) { return (uint64_t)order_of(x) << 32 | (uint32_t)~index; }
 __device__ __forceinline__ uint32_t key_index(uint64_t k) { return ~(uint32_t)k; }
+// the element (not NaN) that a key was made of
+__device__ __forceinline__ float key_value(uint64_t k) {
+    const uint32_t u = (uint32_t)(k >> 32);
+    return __uint_as_float((u & 0x80000000u) ? u & 0x7FFFFFFFu : ~u);
+}
 
 __device__ __forceinline__ uint64_t warp_max_key(uint64_t k) {
 #pragma unroll
@@ -65,11 +70,12 @@ struct RowShare {
     // f(index) for a thread's loose elements; every pass over a share gives a thread the same elements
     template <typename F>
     __device__ __forceinline__ void each_loose(const F& f) const {
-        for (int i = threadIdx.x; i < loose; i += blockDim.x) f(loose_at(i));
+        for (int i = threadIdx.x; i < loose; i += kLpThreads) f(loose_at(i));
     }
     __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : i + body; }
     __device__ __forceinline__ int index(int v) const { return head + v * V; }
-    __device__ __forceinline__ uint4 load(int v) const { return __ldcs(reinterpret_cast<const uint4*>(p + head) + v); }
+    __device__ __forceinline__ uint4 load(int v) const { return reinterpret_cast<const uint4*>(p + head)[v]; }
+    __device__ __forceinline__ uint4 load_once(int v) const { return __ldcs(reinterpret_cast<const uint4*>(p + head) + v); }
 };
 
 struct Stats {
@@ -107,12 +113,13 @@ constexpr float kLowest = -3.402823466e38f;
 
 // Room that a row's passes share.
 struct LogprobShared {
-    Stats stats[32];
-    uint32_t best[32][32];  // order of the threads' largest elements, by warp
+    Stats stats[kLpThreads / 32];
+    uint32_t best[kLpThreads / 32][32];  // order of the threads' largest elements, by warp
     uint64_t notes[kNotes];
     uint64_t top[kTopMax];
+    int owner[kLpThreads];  // threads whose largest element may be among the row's
     uint32_t floor;
-    int count;
+    int count, owners;
     Stats total;
 };
 
@@ -120,7 +127,7 @@ struct LogprobShared {
 template <typename T>
 __device__ __forceinline__ uint64_t largest_below(const RowShare<T>& r, uint64_t under) {
     uint64_t best = 0;
-    for (int v = r.v0 + threadIdx.x; v < r.v1; v += blockDim.x) {
+    for (int v = r.v0 + threadIdx.x; v < r.v1; v += kLpThreads) {
         float x[RowShare<T>::V];
         Vec16<T>::widen(r.load(v), x);
 #pragma unroll
@@ -137,14 +144,16 @@ __device__ __forceinline__ uint64_t largest_below(const RowShare<T>& r, uint64_t
     return best;
 }
 
+__device__ __forceinline__ void lp_sync() { named_sync(1, kLpThreads); }  // the reading warps
+
 // The K largest keys of a CTA's share, sorted, into sh.top (0 where the share has fewer). best: the order of
 // the thread's largest element, 0 if it has none.
 template <typename T>
 __device__ __forceinline__ void cta_top(const RowShare<T>& r, uint32_t best, int K, LogprobShared& sh) {
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = blockDim.x / 32, step = blockDim.x;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = kLpThreads / 32, step = kLpThreads;
     sh.best[warp][lane] = best;
-    if (tid == 0) sh.count = 0;
-    __syncthreads();
+    if (tid == 0) sh.count = sh.owners = 0;
+    lp_sync();
     if (warp == 0) {
         uint32_t k = 0;
         for (int w = 0; w < warps; ++w) k = max(k, sh.best[w][lane]);
@@ -158,7 +167,7 @@ __device__ __forceinline__ void cta_top(const RowShare<T>& r, uint32_t best, int
         if (rank == K - 1) sh.floor = max(k, 1u);
         sh.top[lane] = 0;
     }
-    __syncthreads();
+    lp_sync();
     const uint32_t floor = sh.floor;
     const auto note = [&](float x, int index) {
         if (order_of(x) >= floor) {
@@ -166,21 +175,25 @@ __device__ __forceinline__ void cta_top(const RowShare<T>& r, uint32_t best, int
             if (at < kNotes) sh.notes[at] = key_of(x, index);
         }
     };
-    for (uint32_t left = __ballot_sync(0xffffffffu, best >= floor); left; left &= left - 1) {
-        const int owner = warp * 32 + __ffs(left) - 1;  // this thread's vectors, a lane each
-#pragma unroll 4
-        for (int v = r.v0 + owner + lane * step; v < r.v1; v += 32 * step) {
+    if (best >= floor) sh.owner[atomicAdd(&sh.owners, 1)] = tid;
+    lp_sync();
+    // those threads' vectors, divided among all
+    const int each = max(r.v1 - r.v0 + step - 1, 0) / step, all = sh.owners * each;
+#pragma unroll 8
+    for (int i = tid; i < all; i += step) {
+        const int v = r.v0 + sh.owner[i / each] + i % each * step;
+        if (v < r.v1) {
             float x[RowShare<T>::V];
             Vec16<T>::widen(r.load(v), x);
 #pragma unroll
-            for (int i = 0; i < RowShare<T>::V; ++i) note(x[i], r.index(v) + i);
+            for (int j = 0; j < RowShare<T>::V; ++j) note(x[j], r.index(v) + j);
         }
     }
     if (best >= floor) {
         const auto one = [&](int i) { note(load_one(r.p + i), i); };
         r.each_loose(one);
     }
-    __syncthreads();
+    lp_sync();
     const int count = sh.count;
     if (count <= kNotes) {
         for (int i = tid; i < count; i += step) {
@@ -194,39 +207,71 @@ __device__ __forceinline__ void cta_top(const RowShare<T>& r, uint32_t best, int
         for (int i = 0; i < K; ++i) {
             if (mine >= under) mine = largest_below(r, under);
             const uint64_t w = warp_max_key(mine);
-            __syncthreads();
+            lp_sync();
             if (lane == 0) sh.notes[warp] = w;
-            __syncthreads();
+            lp_sync();
             under = warp_max_key(lane < warps ? sh.notes[lane] : 0);
             if (tid == 0) sh.top[i] = under;
             if (under == 0) break;
         }
     }
-    __syncthreads();
+    lp_sync();
 }
 
+// Slices of a row share on their way, by bulk copies of a warp that does nothing else: three of 16 KB a CTA, so
+// that an SM's four CTAs have up to 192 KB outstanding, and the next row's first while a row is joined.
+constexpr int kLpSlices = 3, kLpSlice = 4 * kLpThreads;  // vectors of a slice: four a thread
+struct SliceBarriers {
+    uint64_t full[kLpSlices], empty[kLpSlices];
+};
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_constant__ LogprobArgs a, float c, float inv_t) {
-    constexpr int V = Vec16<T>::kN, B = 4;  // vectors of a thread that are looked at together
+__global__ void __launch_bounds__(kLpThreads + 32, 4) logprob_kernel(const __grid_constant__ LogprobArgs a, float c, float inv_t) {
+    constexpr int V = Vec16<T>::kN, B = kLpSlice / kLpThreads;
+    extern __shared__ __align__(128) uint4 slices[];
     __shared__ LogprobShared sh;
+    __shared__ SliceBarriers bar;
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), ranks = (int)cluster.num_blocks();
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = blockDim.x / 32, step = blockDim.x;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = kLpThreads / 32, step = kLpThreads;
     const uint32_t nothing = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;  // minus infinity
     const int64_t row_step = gridDim.x / ranks;
-    uint4 next[B];
-    const auto request = [&](const RowShare<T>& r, int v) {
-#pragma unroll
-        for (int j = 0; j < B; ++j)
-            next[j] = v + j * step < r.v1 ? r.load(v + j * step) : make_uint4(nothing, nothing, nothing, nothing);
-    };
     const auto share = [&](int64_t row) { return RowShare<T>((const T*)a.logits.p + row * a.logits.row, a.V, rank, ranks); };
-    int64_t row = blockIdx.x / ranks;
-    if (row < a.R) {
-        const RowShare<T> r = share(row);
-        request(r, r.v0 + tid);
+    if (tid == 0) {
+        for (int i = 0; i < kLpSlices; ++i) {
+            mbar_init(&bar.full[i], 1);
+            mbar_init(&bar.empty[i], kLpThreads / 32);
+        }
+        mbar_fence_init();
     }
-    for (; row < a.R; row += row_step) {
+    __syncthreads();
+    int slot = 0;
+    uint32_t phase = 0;  // of the slot's current use
+    bool ok = true;      // (a wait that runs out is the last one: the kernel ends, its status says so)
+    if (warp == warps) {  // ---- copies
+        int n = 0;
+        for (int64_t row = blockIdx.x / ranks; row < a.R; row += row_step) {
+            if (lane == 0) {
+                const RowShare<T> r = share(row);
+                for (int v = r.v0; v < r.v1 && ok; v += kLpSlice, ++n) {
+                    if (n >= kLpSlices && !(ok = mbar_wait(&bar.empty[slot], phase ^ 1, a.status))) break;
+                    const uint32_t bytes = (uint32_t)min(kLpSlice, r.v1 - v) * 16;
+                    mbar_arrive_expect_tx(&bar.full[slot], bytes);
+                    bulk_g2s(slices + slot * kLpSlice, r.p + r.index(v), bytes, &bar.full[slot]);
+                    if (++slot == kLpSlices) slot = 0, phase ^= 1;
+                }
+            }
+            __syncwarp();
+            if (ranks > 1) {
+                cluster.sync();
+                cluster.sync();
+            }
+        }
+        if (lane == 0 && !ok) {  // (what is in flight lands before the CTA ends)
+            for (int i = max(n - kLpSlices, 0); i < n; ++i) mbar_wait(&bar.full[i % kLpSlices], (uint32_t)(i / kLpSlices) & 1, a.status, 50000000LL);
+        }
+        return;
+    }
+    for (int64_t row = blockIdx.x / ranks; row < a.R; row += row_step) {
         const T* x0 = (const T*)a.logits.p + row * a.logits.row;
         const RowShare<T> r = share(row);
         // a token that is asked for, and its logit, are read ahead
@@ -268,12 +313,16 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_con
                 }
             }
         };
-        // (whole warps: the turns of a warp are its first lane's)
-        for (int v = r.v0 + warp * 32; v < r.v1; v += B * step) {
+        for (int v = r.v0; v < r.v1; v += kLpSlice) {
+            if (ok) ok = mbar_wait(&bar.full[slot], phase, a.status);
+            const uint4* p = slices + slot * kLpSlice + tid;
+            const int have = r.v1 - v - tid;
             uint4 raw[B];
 #pragma unroll
-            for (int j = 0; j < B; ++j) raw[j] = next[j];
-            if (v + B * step < r.v1) request(r, v + lane + B * step);
+            for (int j = 0; j < B; ++j) raw[j] = j * step < have ? p[j * step] : make_uint4(nothing, nothing, nothing, nothing);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar.empty[slot]);
+            if (++slot == kLpSlices) slot = 0, phase ^= 1;
             look(raw, B);
         }
         for (int i = tid - lane; i < r.loose; i += step) {
@@ -285,10 +334,6 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_con
             }
             look(raw, 1);
         }
-        if (row + row_step < a.R) {  // the next row's first vectors, while this row's sums are joined
-            const RowShare<T> q = share(row + row_step);
-            request(q, q.v0 + tid);
-        }
         Stats st{m, warp_sum(low_f32(s) + high_f32(s)), warp_sum(low_f32(u) + high_f32(u))};
         if (TOP) {
             const bool any = r.v0 + tid < r.v1 || tid < r.loose;
@@ -298,13 +343,13 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_con
             cta_top(r, best, a.K, sh);
         }
         if (lane == 0) sh.stats[warp] = st;
-        __syncthreads();
+        lp_sync();
         if (warp == 0) {
             st = warp_join(lane < warps ? sh.stats[lane] : Stats{kLowest, 0.f, 0.f}, c);
             if (lane == 0) sh.total = st;
         }
         if (ranks > 1) cluster.sync();
-        else __syncthreads();
+        else lp_sync();
         if (rank == 0) {
             if (warp == 0 && ranks > 1) {
                 st = warp_join(lane < ranks ? cluster.map_shared_rank(&sh, lane)->total : Stats{kLowest, 0.f, 0.f}, c);
@@ -314,7 +359,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_con
                 if (TOP) {  // the CTAs' lists, each of K sorted keys
                     const int all = ranks * a.K;
                     for (int i = tid; i < all; i += step) sh.notes[i] = cluster.map_shared_rank(&sh, i / a.K)->top[i % a.K];
-                    __syncthreads();
+                    lp_sync();
                     for (int i = tid; i < all; i += step) {
                         const uint64_t k = sh.notes[i];
                         int at = 0;
@@ -322,7 +367,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_con
                         if (at < a.K && k) sh.top[at] = k;
                     }
                 }
-                __syncthreads();
+                lp_sync();
             }
             st = ranks > 1 ? sh.stats[0] : sh.total;
             // a row of nothing but -inf: S = 0
@@ -345,14 +390,12 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_kernel(const __grid_con
                 a.logprob[row * a.J + tid] = lp;
             }
             if (TOP && tid < a.K) {
-                const int id = (int)key_index(sh.top[tid]);
-                const bool there = id >= 0 && id < a.V;  // (always)
-                a.top_id[row * a.K + tid] = id;
-                a.top_logprob[row * a.K + tid] = bad || !there ? NAN : logp(load_one(x0 + id));
+                a.top_id[row * a.K + tid] = (int)key_index(sh.top[tid]);
+                a.top_logprob[row * a.K + tid] = bad ? NAN : logp(key_value(sh.top[tid]));
             }
         }
         if (ranks > 1) cluster.sync();  // (the others' shared memory has been read)
-        else __syncthreads();
+        else lp_sync();
     }
 }
 
@@ -378,7 +421,7 @@ __global__ void __launch_bounds__(kLpThreads, 4) logprob_backward_kernel(const _
         const auto request = [&](int w) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (w + j * step < r.v1) next[j] = r.load(w + j * step);
+                if (w + j * step < r.v1) next[j] = r.load_once(w + j * step);
         };
         request(v);
         __syncthreads();
@@ -476,7 +519,8 @@ cudaError_t forward(const LogprobArgs& a, int num_sms, cudaStream_t st) {
     const int64_t vecs = a.V / Vec16<T>::kN;
     // CTAs of a row: the fewest rounds of CTAs (four an SM), counted in a thread's turns of four vectors, with some
     // four turns' time for a row's end and two for a cluster's
-    int ranks = 1, threads = kLpThreads;
+    const int threads = kLpThreads;
+    int ranks = 1;
     int64_t best = 0;
     for (int r = 1; r <= 16 && (r == 1 || vecs >= (int64_t)r * threads); r *= 2) {
         const int64_t rounds = (a.R * r + num_sms * 4 - 1) / (num_sms * 4);
@@ -486,15 +530,15 @@ cudaError_t forward(const LogprobArgs& a, int num_sms, cudaStream_t st) {
             ranks = r;
         }
     }
-    while (threads > 128 && ranks == 1 && vecs < threads * 2) threads /= 2;
     const auto kern = logprob_kernel<T, TOP>;
     const float inv_t = 1.f / a.temperature;
     // CTAs that keep to one row each come and go; whole rows' CTAs stay, and have the next row on its way
-    int64_t rows = ranks > 1 ? (int64_t)1 << 26 : (int64_t)num_sms * (1024 / threads);
+    int64_t rows = ranks > 1 ? (int64_t)1 << 26 : (int64_t)num_sms * 4;
     if (rows > a.R) rows = a.R;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows * ranks));
-    cfg.blockDim = dim3(threads);
+    cfg.blockDim = dim3(threads + 32);
+    cfg.dynamicSmemBytes = kLpSlices * kLpSlice * sizeof(uint4);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -508,10 +552,10 @@ cudaError_t forward(const LogprobArgs& a, int num_sms, cudaStream_t st) {
 template <typename T>
 cudaError_t backward(const LogprobArgs& a, int num_sms, cudaStream_t st) {
     const int64_t vecs = a.V / Vec16<T>::kN;
-    int shares = 1, threads = kLpThreads;
+    const int threads = kLpThreads;
+    int shares = 1;
     while (a.R * shares * 2 <= num_sms * 4 && vecs >= (int64_t)shares * 2 * threads) shares *= 2;
-    while (threads > 128 && vecs < (int64_t)shares * threads * 2) threads /= 2;
-    const int64_t units = a.R * shares, most = (int64_t)num_sms * (1024 / threads);
+    const int64_t units = a.R * shares, most = (int64_t)num_sms * 4;
     const float inv_t = 1.f / a.temperature;
     return launch_k(logprob_backward_kernel<T>, dim3((unsigned)(units < most ? units : most)), dim3(threads), 0, st, false, a,
                     kLog2e * inv_t, inv_t, shares);
@@ -530,7 +574,10 @@ cudaError_t launch_token_logprobs_backward(const LogprobArgs& a, fe_dtype dtype,
 
 cudaError_t logprobs_prepare() {
     cudaError_t e;
-    const auto wide = [](auto kern) { return cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1); };
+    const auto wide = [](auto kern) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kLpSlices * kLpSlice * sizeof(uint4)));
+    };
     if ((e = wide(logprob_kernel<float, true>)) != cudaSuccess || (e = wide(logprob_kernel<float, false>)) != cudaSuccess) return e;
     if ((e = wide(logprob_kernel<bf16_t, true>)) != cudaSuccess) return e;
     return wide(logprob_kernel<bf16_t, false>);
