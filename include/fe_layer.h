@@ -118,7 +118,7 @@ FE_API fe_status fe_gated_ffn_backward(fe_target *t, const fe_gated_ffn_backward
  *               gate_rows is 1 for a gate of each row, the tokens of a sequence for a gate of each
  *               sequence, and R for a gate of each channel
  *  y, n         either may be absent; y may be x or z itself, n may be z itself (the same p and row)
- * scale and offset finite, eps finite and >= 0; R >= 0, d in 1..2^24. */
+ * scale and offset finite, eps finite and >= 0; R in 0..2^30, d in 1..2^20. */
 typedef struct {
     int64_t R;
     int32_t d, post;

@@ -12,7 +12,7 @@ using namespace fe;
 namespace {
 
 constexpr int64_t kMaxRows = 1 << 30;
-constexpr int kMaxCols = 1 << 24;
+constexpr int kMaxCols = 1 << 24, kMaxNorm = 1 << 20;
 
 int elem(const fe_target* t) { return t->cfg.dtype == FE_F32 ? 4 : 2; }
 
@@ -299,7 +299,7 @@ fe_status gated_backward(const fe_target* t, const fe_gated_ffn_backward_args* a
 
 template <typename A>
 bool norm_sizes_ok(const fe_target* t, const A* a) {
-    if (!t || !a || a->R < 0 || a->R > kMaxRows || a->d < 1 || a->d > kMaxCols) return false;
+    if (!t || !a || a->R < 0 || a->R > kMaxRows || a->d < 1 || a->d > kMaxNorm) return false;
     if (!isfinite(a->scale) || !isfinite(a->offset) || !isfinite(a->eps) || a->eps < 0.f) return false;
     const int es = elem(t);
     if (!in_ok(a->x, es) || !opt_in(a->z, es) || !opt_in(a->gate, es) || !opt_ptr(a->post_w, es) || !opt_ptr(a->pre_w, es)) return false;

@@ -415,7 +415,15 @@ class _BlockNorm(torch.autograd.Function):
 _LOGITS = {torch.float32: FE_F32, torch.bfloat16: FE_BF16}
 
 
-def _tokens(x, lead) -> tuple:
+def _contiguous(x, side):
+    """x, copied on the call's stream where it is not contiguous."""
+    if x.is_contiguous() or side is None:
+        return x.contiguous()
+    with torch.cuda.stream(side):
+        return x.contiguous()
+
+
+def _tokens(x, lead, side) -> tuple:
     """tokens [..., J] or [...] (one a row) as [..., J], and J."""
     if x is None:
         return None, 0
@@ -424,7 +432,7 @@ def _tokens(x, lead) -> tuple:
     x = x[..., None] if x.shape == lead else x
     if x.dtype != torch.int32 or x.shape[:-1] != lead:
         raise ValueError(f"tokens must be int32 of shape {tuple(lead)} or {tuple(lead)} + (J,), got {x.dtype} {tuple(x.shape)}")
-    return x.contiguous(), x.shape[-1]
+    return _contiguous(x, side), x.shape[-1]
 
 
 def fe_token_logprobs(t: Target, logits, tokens=None, top: int = 0, temperature: float = 1.0, stats=None, stream=None) -> tuple:
@@ -436,11 +444,10 @@ def fe_token_logprobs(t: Target, logits, tokens=None, top: int = 0, temperature:
     if stats is None and _recorded(stream) and logits.requires_grad:
         out = _Logprobs.apply(t, logits, tokens, top, temperature)
         return (None, *out[1:]) if tokens is None else out
-    lead, V = logits.shape[:-1], logits.shape[-1]
-    tok, J = _tokens(tokens, lead)
+    lead, V, side, f32 = logits.shape[:-1], logits.shape[-1], _side(stream), torch.float32
+    tok, J = _tokens(tokens, lead, side)
     if logits.dtype not in _LOGITS:
         raise ValueError(f"logits must be float32 or bfloat16, got {logits.dtype}")
-    side, f32 = _side(stream), torch.float32
     logprob = None if tokens is None else _new(tokens.shape, logits, side, f32)
     entropy, lse = _new(lead, logits, side, f32), _new(lead, logits, side, f32)
     ids, lps = _new(lead + (top,), logits, side, torch.int32), _new(lead + (top,), logits, side, f32)
@@ -459,14 +466,13 @@ def fe_token_logprobs_backward(t: Target, logits, stats, tokens=None, dlogprob=N
                                dtop_logprob=None, temperature: float = 1.0, dlogits=None, stream=None):
     """dlogits [..., V] of fe_token_logprobs, for the gradients of its results (None: zero); stats, entropy
     and top_id are the forward call's. dlogits may be the logits themselves."""
-    lead, V = logits.shape[:-1], logits.shape[-1]
-    tok, J = _tokens(tokens, lead)
+    lead, V, side = logits.shape[:-1], logits.shape[-1], _side(stream)
+    tok, J = _tokens(tokens, lead, side)
     if logits.dtype not in _LOGITS:
         raise ValueError(f"logits must be float32 or bfloat16, got {logits.dtype}")
     if (dlogprob is not None and tok is None) or (dentropy is not None and entropy is None) or \
             (dtop_logprob is not None and top_id is None):
         raise ValueError("dlogprob needs tokens, dentropy needs entropy, and dtop_logprob needs top_id")
-    side = _side(stream)
 
     def flat(x, shape, dtype=torch.float32):
         if x is None:
@@ -475,7 +481,7 @@ def fe_token_logprobs_backward(t: Target, logits, stats, tokens=None, dlogprob=N
             raise ValueError("buffers the kernels access must be CUDA tensors")
         if x.dtype != dtype or x.shape != shape:
             raise ValueError(f"expected {dtype} of shape {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
-        return x.contiguous()
+        return _contiguous(x, side)
 
     K = 0 if top_id is None else top_id.shape[-1]
     given = (flat(stats, lead + (2,)), flat(entropy, lead), flat(dlogprob, None if tokens is None else tokens.shape), flat(dentropy, lead),

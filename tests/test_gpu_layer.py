@@ -310,6 +310,26 @@ def test_block_norm_strides_and_in_place(fe, handles, dtype, d, left, right):
         ref.check(v, want[name], name)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,d", [(50, 64), (50, 1000), (40, 5120), (30, 8000), (20, 20000)])
+def test_block_norm_gradients_in_place(fe, handles, dtype, R, d):
+    """dx and dz in the place of dy and dn, either way round."""
+    t, g = handles[dtype], gen(d)
+    x, z, dy, dn = (normal(g, dtype, R, d) for _ in range(4))
+    pw, qw = normal(g, dtype, d), normal(g, dtype, d)
+    want = fe.fe_block_norm_backward(t, x, z, None, pw, pre_weight=qw, dy=dy, dn=dn)
+    from paper_2509_20416_gb300 import layer
+    for swap in (False, True):
+        a, b = dy.clone(), dn.clone()
+        dx, dz = (b, a) if swap else (a, b)
+        dp, dq = torch.empty_like(pw), torch.empty_like(qw)
+        m = lambda v: (v.data_ptr(), d)
+        args = layer._norm_args(t, (True, 0, 1.0, 0.0, 1e-5), x, z, pw, None, qw) + (*m(a), *m(b), *m(dx), *m(dz), 0, 0, dp.data_ptr(), dq.data_ptr())
+        layer._call("fe_block_norm_backward", t, None, (x, z, pw, qw, a, b, dp, dq), args)
+        for got, w in zip((dx, dz, dp, dq), (want[0], want[1], want[2], want[4])):
+            assert torch.equal(got, w)
+
+
 def test_norm_alone(fe, handles):
     """Without a block's output: the first norm of a model."""
     t, g = handles["bf16"], gen(2)
@@ -553,7 +573,14 @@ def test_other_streams(fe, handles, dtype):
     z = fe.fe_block_norm(t, r, y, post_weight=pw, stream=s)
     lp = fe.fe_token_logprobs(t, z[1], tok, top=3, stream=s.cuda_stream)
     got = fe.fe_project_backward(t, z[1], late, w, dbias=True, stream=s)
+    wide = torch.zeros(40, 2, dtype=torch.int32, device="cuda")  # tokens that are not contiguous, and made late
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(50_000_000)
+        wide[:, 0] = 5
+    late_lp = fe.fe_token_logprobs(t, z[1], wide[:, :1], stream=s)[0]
     s.synchronize()
+    assert torch.equal(late_lp, fe.fe_token_logprobs(t, z[1], wide[:, :1].contiguous())[0])
     for a, b in zip((y, *z, *lp, *got), (want, *norm, *logp, dx, dw, db)):
         assert torch.equal(a, b)
 
