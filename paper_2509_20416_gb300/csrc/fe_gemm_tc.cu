@@ -23,7 +23,8 @@ constexpr int kTileM = 256, kSliceK = 64;
 
 constexpr int kSliceA = 128 * kSliceK * 2;
 constexpr int kStaging = kFinishWarps * 4096;  // a warp's 32 x 32 floats
-constexpr int kTcRing = 188 * 1024, kTcStages = 8;
+constexpr int kTcRing = 192 * 1024, kTcStages = 8;
+constexpr int kPairs = kFinishWarps * 8192;  // of the ring, for a gated gradient's products on their way
 constexpr int kTcSmem = kTcRing + kStaging + 1024 /* alignment */ + 512;
 static_assert(kTcSmem <= 227 * 1024, "shared memory of a CTA");
 
@@ -207,60 +208,60 @@ __device__ __forceinline__ void finish_gated(const WarpTile& w, int half) {
     }
 }
 
-// The gradients of a gated pair: half a block's (16 rows') stored products are in flight while the half before
-// is finished.
-__device__ __forceinline__ void pair_rows(const WarpTile& w, int c, int h, float4* g, float4* u) {
-    const float *p = w.at<float>(w.e.pre, w.e.pre_row, c), *q = w.at<float>(w.e.pre2, w.e.pre2_row, c);
-    const int have = w.inside(c) ? w.have(c) : 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = 4 * h + i, k = w.row(r) < w.left ? have : 0;
-        g[i] = load4(p + 4 * r * w.e.pre_row, k, w.e.vec);
-        u[i] = load4(q + 4 * r * w.e.pre2_row, k, w.e.vec);
+// The gradients of a gated pair. A lane's stored products of a row of the next block are copied (cp.async) into the
+// place of the row that it has just read, which it alone writes and reads: 8 KB a warp, 64 KB an SM in flight.
+__device__ __forceinline__ void pair_row(const WarpTile& w, int c, int i, float4* slot) {
+    const int have = w.inside(c) && w.row(i) < w.left ? w.have(c) : 0;
+    if (have > 0) {
+        const float* g = w.at<float>(w.e.pre, w.e.pre_row, c) + 4 * i * w.e.pre_row;
+        const float* u = w.at<float>(w.e.pre2, w.e.pre2_row, c) + 4 * i * w.e.pre2_row;
+        if (w.e.vec && have >= 4) {
+            cp_async16(smem_u32(slot + 64 * i), g, true);
+            cp_async16(smem_u32(slot + 64 * i + 32), u, true);
+        } else {
+            slot[64 * i] = load4(g, have, false);
+            slot[64 * i + 32] = load4(u, have, false);
+        }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
 }
 template <typename Wait>
-__device__ __forceinline__ bool finish_gated_grad(const WarpTile& w, int half, const Wait& wait) {
+__device__ __forceinline__ bool finish_gated_grad(const WarpTile& w, int half, const Wait& wait, float4* slots) {
     const Finish& e = w.e;
-    float4 ng[4], nu[4];
-    pair_rows(w, half * 32, 0, ng, nu);
-    if (!wait()) return false;
-    for (int c = half * 32; w.inside(c); c += 64) {
+    float4* const slot = slots + w.lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pair_row(w, half * 32, i, slot);
+    const bool ok = wait();
+    for (int c = half * 32; ok && w.inside(c); c += 64) {
         const int have = w.have(c);
         stage_rows(w.buf, w.d + c, w.lane);
         bf16_t *out = w.at<bf16_t>(e.out, e.out_row, c), *out2 = w.at<bf16_t>(e.out2, e.out2_row, c),
                *out3 = w.at<bf16_t>(e.out3, e.out3_row, c);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float4 cg[4], cu[4];
+        for (int i = 0; i < 8; ++i) {
+            float z[4];
+            asm volatile("cp.async.wait_group 7;" ::: "memory");
+            const float4 cg = slot[64 * i], cu = slot[64 * i + 32];
+            float g[4] = {cg.x, cg.y, cg.z, cg.w}, u[4] = {cu.x, cu.y, cu.z, cu.w};
+            pair_row(w, c + 64, i, slot);
+            staged(w.buf, w.row(i), w.chunk(), z);
+            if (w.row(i) >= w.left || have <= 0) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                cg[i] = ng[i];
-                cu[i] = nu[i];
+            for (int j = 0; j < 4; ++j) {
+                float v, dv;
+                act_both<true>(e.act, g[j], v, dv);
+                g[j] = z[j] * v;
+                z[j] *= u[j] * dv;
+                u[j] *= v;
             }
-            pair_rows(w, h ? c + 64 : c, h ^ 1, ng, nu);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 4 * h + i;
-                float z[4], g[4] = {cg[i].x, cg[i].y, cg[i].z, cg[i].w}, u[4] = {cu[i].x, cu[i].y, cu[i].z, cu[i].w};
-                staged(w.buf, w.row(r), w.chunk(), z);
-                if (w.row(r) >= w.left) continue;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float v, dv;
-                    act_both<true>(e.act, g[j], v, dv);
-                    g[j] = z[j] * v;
-                    z[j] *= u[j] * dv;
-                    u[j] *= v;
-                }
-                store4(out + 4 * r * e.out_row, have, e.vec, z);
-                store4(out2 + 4 * r * e.out2_row, have, e.vec, g);
-                store4(out3 + 4 * r * e.out3_row, have, e.vec, u);
-            }
+            store4(out + 4 * i * e.out_row, have, e.vec, z);
+            store4(out2 + 4 * i * e.out2_row, have, e.vec, g);
+            store4(out3 + 4 * i * e.out3_row, have, e.vec, u);
         }
         __syncwarp();
     }
-    return true;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return ok;
 }
 
 template <bool AT, bool BT>
@@ -395,7 +396,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
                 if (!wait()) break;
                 finish_gated(w, half);
             } else if (e.kind == FINISH_GATED_GRAD) {
-                if (!finish_gated_grad(w, half, wait)) break;
+                if (!finish_gated_grad(w, half, wait, (float4*)(ring + kTcRing - kPairs) + (warp - 2) * 512)) break;
             } else if (!finish_plain(w, half, wait)) {
                 break;
             }
@@ -430,7 +431,7 @@ cudaError_t launch_tiles(const GemmArgs& g, int num_sms, cudaStream_t st) {
         }
     }
     const int bn = shape.bn;
-    shape.stages = kTcRing / (kSliceA + shape.b_bytes);
+    shape.stages = (kTcRing - (g.e.kind == FINISH_GATED_GRAD ? kPairs : 0)) / (kSliceA + shape.b_bytes);
     if (shape.stages > kTcStages) shape.stages = kTcStages;
     TcMaps maps{};
     for (int i = 0; i < 2; ++i) {
