@@ -4,12 +4,11 @@
 //   m, S = sum 2^d, U = sum d 2^d,   so that   lse = m / T + log S,   H = log S - ln 2 U / S,
 // against the largest m that its warp has seen, which four vectors of 16 bytes are compared with at a time.
 //
-// The K largest: of the threads' largest elements 32 groups are made; the K-th largest group maximum
-// is no larger than the K-th largest element of the row, so the elements of the few threads whose maximum
-// reaches it are looked through again by all threads, and those that reach it are noted. Rank
-// among the notes is place in the result. Where more elements reach it than there is room for (equal
-// logits, or a row whose large elements all fall to few threads), the CTA takes out its largest element
-// K times instead.
+// The K largest: of the threads' largest elements so far 32 groups are made; the K-th largest group maximum
+// is no larger than the K-th largest element of the row, so elements that reach it are noted, and the few
+// others are out. It is raised after 1, 3, 9, ... slices of a row. Rank among the notes is place in the
+// result. Where there is not room for the notes (equal logits, or growing ones) the row is looked at again, by the
+// final maxima, or the CTA takes out its largest element K times.
 //
 // A cluster of 1 to 16 CTAs shares a row where there are too few rows to fill the GPU; its first CTA
 // joins the others' results through distributed shared memory.
@@ -117,9 +116,8 @@ struct LogprobShared {
     uint32_t best[kLpThreads / 32][32];  // order of the threads' largest elements, by warp
     uint64_t notes[kNotes];
     uint64_t top[kTopMax];
-    int owner[kLpThreads];  // threads whose largest element may be among the row's
     uint32_t floor;
-    int count, owners;
+    int count, odd;
     Stats total;
 };
 
@@ -146,63 +144,66 @@ __device__ __forceinline__ uint64_t largest_below(const RowShare<T>& r, uint64_t
 
 __device__ __forceinline__ void lp_sync() { named_sync(1, kLpThreads); }  // the reading warps
 
-// The K largest keys of a CTA's share, sorted, into sh.top (0 where the share has fewer). best: the order of
-// the thread's largest element, 0 if it has none.
-template <typename T>
-__device__ __forceinline__ void cta_top(const RowShare<T>& r, uint32_t best, int K, LogprobShared& sh) {
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = kLpThreads / 32, step = kLpThreads;
+// The K-th largest of 32 groups' maxima (best: the order of the thread's largest element so far, 0 for none), which
+// no more than K - 1 of the share's elements need exceed; 1, below every order, where fewer groups have any.
+__device__ __forceinline__ uint32_t cta_floor(uint32_t best, int K, LogprobShared& sh) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     sh.best[warp][lane] = best;
-    if (tid == 0) sh.count = sh.owners = 0;
     lp_sync();
     if (warp == 0) {
         uint32_t k = 0;
-        for (int w = 0; w < warps; ++w) k = max(k, sh.best[w][lane]);
-        // rank of a group's maximum among the 32 (equal ones by lane)
-        int rank = 0;
+#pragma unroll
+        for (int w = 0; w < kLpThreads / 32; ++w) k = max(k, sh.best[w][lane]);
+        int rank = 0;  // among the 32 (equal ones by lane)
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             const uint32_t o = __shfl_sync(0xffffffffu, k, i);
             rank += o > k || (o == k && i < lane);
         }
         if (rank == K - 1) sh.floor = max(k, 1u);
-        sh.top[lane] = 0;
     }
     lp_sync();
-    const uint32_t floor = sh.floor;
-    const auto note = [&](float x, int index) {
-        if (order_of(x) >= floor) {
-            const int at = atomicAdd(&sh.count, 1);
-            if (at < kNotes) sh.notes[at] = key_of(x, index);
-        }
-    };
-    if (best >= floor) sh.owner[atomicAdd(&sh.owners, 1)] = tid;
-    lp_sync();
-    // those threads' vectors, divided among all
-    const int each = max(r.v1 - r.v0 + step - 1, 0) / step, all = sh.owners * each;
-#pragma unroll 8
-    for (int i = tid; i < all; i += step) {
-        const int v = r.v0 + sh.owner[i / each] + i % each * step;
-        if (v < r.v1) {
+    return sh.floor;
+}
+__device__ __forceinline__ void note(float x, int index, uint32_t floor, LogprobShared& sh) {
+    if (order_of(x) >= floor) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < kNotes) sh.notes[at] = key_of(x, index);
+    }
+}
+// The K largest of the notes, sorted, into sh.top; false if there was not room for all.
+__device__ __forceinline__ bool rank_notes(int K, LogprobShared& sh) {
+    const int count = sh.count;
+    if (count > kNotes) return false;
+    for (int i = threadIdx.x; i < count; i += kLpThreads) {
+        const uint64_t k = sh.notes[i];
+        int rank = 0;
+        for (int j = 0; j < count; ++j) rank += sh.notes[j] > k;
+        if (rank < K) sh.top[rank] = k;
+    }
+    return true;
+}
+
+// The K largest keys of a CTA's share from a second look: at the threads whose largest element (best) reaches the
+// floor of all, or, where that leaves too many, by taking out the largest K times.
+template <typename T>
+__device__ __forceinline__ void cta_top(const RowShare<T>& r, uint32_t best, int K, LogprobShared& sh) {
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, warps = kLpThreads / 32, step = kLpThreads;
+    lp_sync();  // (the notes have been read)
+    if (tid == 0) sh.count = 0;
+    const uint32_t floor = cta_floor(best, K, sh);
+    if (best >= floor) {
+        for (int v = r.v0 + tid; v < r.v1; v += step) {
             float x[RowShare<T>::V];
             Vec16<T>::widen(r.load(v), x);
 #pragma unroll
-            for (int j = 0; j < RowShare<T>::V; ++j) note(x[j], r.index(v) + j);
+            for (int j = 0; j < RowShare<T>::V; ++j) note(x[j], r.index(v) + j, floor, sh);
         }
-    }
-    if (best >= floor) {
-        const auto one = [&](int i) { note(load_one(r.p + i), i); };
+        const auto one = [&](int i) { note(load_one(r.p + i), i, floor, sh); };
         r.each_loose(one);
     }
     lp_sync();
-    const int count = sh.count;
-    if (count <= kNotes) {
-        for (int i = tid; i < count; i += step) {
-            const uint64_t k = sh.notes[i];
-            int rank = 0;
-            for (int j = 0; j < count; ++j) rank += sh.notes[j] > k;
-            if (rank < K) sh.top[rank] = k;
-        }
-    } else {
+    if (!rank_notes(K, sh)) {
         uint64_t under = ~(uint64_t)0, mine = under;  // (no key is that)
         for (int i = 0; i < K; ++i) {
             if (mine >= under) mine = largest_below(r, under);
@@ -215,7 +216,6 @@ __device__ __forceinline__ void cta_top(const RowShare<T>& r, uint32_t best, int
             if (under == 0) break;
         }
     }
-    lp_sync();
 }
 
 // Slices of a row share on their way, by bulk copies of a warp that does nothing else: three of 16 KB a CTA, so
@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kLpThreads + 32, 4) logprob_kernel(const __gri
         float m = kLowest, bx = -INFINITY;
         uint64_t s = 0, u = 0;  // by even and odd columns
         const uint64_t cc = pair_f32(c);
-        const auto look = [&](const uint4* raw, int n) {
+        const auto look = [&](const uint4* raw, int n) -> float {
             float top = largest<T>(raw[0]);
 #pragma unroll
             for (int j = 1; j < B; ++j)
@@ -312,8 +312,17 @@ __global__ void __launch_bounds__(kLpThreads + 32, 4) logprob_kernel(const __gri
                     u = fma_x2(e, pair_f32(__float_as_uint(fmaxf(dl, -1e4f)), __float_as_uint(fmaxf(dh, -1e4f))), u);
                 }
             }
+            return top;
         };
-        for (int v = r.v0; v < r.v1; v += kLpSlice) {
+        uint32_t floor = 1;
+        float reach = -INFINITY;  // the floor's value
+        if (TOP) {
+            if (tid == 0) sh.count = sh.odd = 0;
+            if (tid < kTopMax) sh.top[tid] = 0;
+            if (r.v0 >= r.v1) lp_sync();
+        }
+        int turn = 0, raise = 0;
+        for (int v = r.v0; v < r.v1; v += kLpSlice, ++turn) {
             if (ok) ok = mbar_wait(&bar.full[slot], phase, a.status);
             const uint4* p = slices + slot * kLpSlice + tid;
             const int have = r.v1 - v - tid;
@@ -323,24 +332,46 @@ __global__ void __launch_bounds__(kLpThreads + 32, 4) logprob_kernel(const __gri
             __syncwarp();
             if (lane == 0) mbar_arrive(&bar.empty[slot]);
             if (++slot == kLpSlices) slot = 0, phase ^= 1;
-            look(raw, B);
+            const float top = look(raw, B);
+            if (TOP) {
+                if (turn == raise) {  // the floor, from the slices 0, 0 to 2, 0 to 8, ...
+                    floor = cta_floor(r.v0 + tid < r.v1 ? order_of(bx) : 0, a.K, sh);
+                    reach = floor < 0x00800000u ? -INFINITY : key_value((uint64_t)floor << 32);
+                    raise = 3 * raise + 2;
+                }
+                if (top >= reach) {
+#pragma unroll
+                    for (int j = 0; j < B; ++j) {
+                        if (j * step >= have) break;
+                        float x[V];
+                        Vec16<T>::widen(raw[j], x);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) note(x[i], r.index(v + tid + j * step) + i, floor, sh);
+                    }
+                }
+            }
         }
         for (int i = tid - lane; i < r.loose; i += step) {
             uint4 raw[1] = {make_uint4(nothing, nothing, nothing, nothing)};
+            int at = -1;
             if (i + lane < r.loose) {
-                const int at = r.loose_at(i + lane);
+                at = r.loose_at(i + lane);
                 raw[0].x = sizeof(T) == 2 ? (uint32_t) reinterpret_cast<const uint16_t*>(r.p)[at] | 0xFF800000u
                                           : reinterpret_cast<const uint32_t*>(r.p)[at];
             }
-            look(raw, 1);
+            const float top = look(raw, 1);
+            if (TOP && at >= 0) note(top, at, floor, sh);
         }
         Stats st{m, warp_sum(low_f32(s) + high_f32(s)), warp_sum(low_f32(u) + high_f32(u))};
         if (TOP) {
-            const bool any = r.v0 + tid < r.v1 || tid < r.loose;
-            uint32_t best = any ? order_of(bx) : 0;
             const float mine = low_f32(s) + high_f32(s);
-            if (mine != mine) best = (uint32_t)(largest_below(r, ~(uint64_t)0) >> 32);  // NaN, or infinity, among its elements
-            cta_top(r, best, a.K, sh);
+            if (mine != mine) sh.odd = 1;  // NaN, or infinity, among a thread's elements
+            lp_sync();
+            if (sh.odd || !rank_notes(a.K, sh)) {
+                uint32_t best = r.v0 + tid < r.v1 || tid < r.loose ? order_of(bx) : 0;
+                if (mine != mine) best = (uint32_t)(largest_below(r, ~(uint64_t)0) >> 32);
+                cta_top(r, best, a.K, sh);
+            }
         }
         if (lane == 0) sh.stats[warp] = st;
         lp_sync();
