@@ -9,6 +9,10 @@
 //             with t = sum dx z rz over the rows of a gate:  dg = s (w_post + o) t,  dw_post = sum s g t
 //             (y is computed again from x and z, so nothing rounded stands in for it)
 //
+// Measured (GB300, 16379 rows of 5120 bfloat16, gate, both norms): forward 114 us (5.9 TB/s; with one vector a thread
+// 134, loads in registers ahead instead of copies 143 to 193), gradient 223 us over 148 us of bytes, bound by
+// instruction issue (with CTAs of 640 threads 325; separate sums for gate and weight 30 % more registers and work).
+//
 // A worker is a CTA, or a warp where a row is at most 32 vectors of 16 bytes; its threads own
 // columns, so that the sums over rows stay in registers. The next row's loads are in flight while
 // a row's statistics are reduced.

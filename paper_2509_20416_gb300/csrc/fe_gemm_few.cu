@@ -5,6 +5,11 @@
 // 1 to 8 CTAs shares a block of 128 rows and divides the summed index; the parts are added in
 // their order through distributed shared memory, each CTA finishing its share of the tokens. A gated
 // pair's block is 64 rows of either matrix.
+//
+// Measured (GB300): one token through a gated pair of 14336 x 4096 38 to 40 us (86 to 90 % of the copy rate; 109 us
+// as tiles of 256 rows), 71 rows through 28672 x 8192 151 us (92 %), 49 rows to 128256 172 us (91 %), one token
+// through 6144 x 4096 13.4 us, where a CTA's start, its first copies and the join are half. The first copies
+// go out before tensor memory is allocated.
 #include "fe_gemm_tc.cuh"
 #include "fe_tensor_map.h"
 

@@ -8,6 +8,11 @@
 // other half of tensor memory. The MN-major operand forms spare the gradients every transpose:
 // dx = dz w reads w by columns, dw = dz^T x both operands.
 //
+// Measured (GB300): 4093 x 5120 x 5120 119 to 124 us (1730 to 1810 TFLOP/s; cuBLAS 119 to 126 on the same boxes),
+// with gelu, bias, residual and the float32 pre-activation 136; a gated pair of 14336 x 4096 from 4093 rows 482 us
+// (1990 TFLOP/s), 523 with both products stored; the gradients' products 1650 to 1910 TFLOP/s. Long steps are bound by
+// the card's power (1550 TFLOP/s over a block's forward and backward pass). Five slices in flight instead of six cost 4 %.
+//
 // BN is the width whose rounds of tiles over the pairs are shortest: 16 x 16 tiles of 256 take 76 pairs 4
 // rounds where 3.4 would hold them, 16 x 19 of 224 take 4 rounds of 7/8.
 #include "fe_gemm_tc.cuh"

@@ -10,6 +10,9 @@
 // result. Where there is not room for the notes (equal logits, or growing ones) the row is looked at again, by the
 // final maxima, or the CTA takes out its largest element K times.
 //
+// Measured (GB300): 1568 rows of 128256 float32 logits with the ten largest 134 us (6.0 TB/s), 8189 rows of 32000
+// bfloat16 102 us (5.1 TB/s; some 11 instructions an element), their gradient 152 us (6.9 TB/s).
+//
 // A cluster of 1 to 16 CTAs shares a row where there are too few rows to fill the GPU; its first CTA
 // joins the others' results through distributed shared memory.
 #include <cooperative_groups.h>
