@@ -8,8 +8,10 @@ with contiguous columns and rows one stride apart, such as column slices of a fu
 `stream` (a torch stream or a raw handle) is where a call runs, the current stream unless given;
 ordering it with others is the caller's. Where autograd records and neither outputs nor a stream
 are given, the results are differentiable (once); the _backward functions are the same gradients
-as plain calls, for a captured step or a training loop of one's own. Workspaces are allocated for
-each call, so that calls and captured graphs do not share them.
+as plain calls, for a captured step or a training loop of one's own. (PyTorch's engine joins the
+streams of a leaf's graphs: a backward pass is captured while no eager graph of the same leaves lives,
+or with the _backward functions.) Workspaces are allocated for each call, so that calls and captured
+graphs do not share them.
 """
 from __future__ import annotations
 
@@ -312,29 +314,35 @@ class _Gated(torch.autograd.Function):
 
 
 def fe_block_norm(t: Target, x, z=None, post: bool | None = None, post_weight=None, gate=None, gate_rows: int | None = None,
-                  scale: float = 1.0, pre_weight=None, offset: float = 0.0, eps: float = 1e-5, y=None, n=None, stream=None) -> tuple:
+                  scale: float = 1.0, pre_weight=None, offset: float = 0.0, eps: float = 1e-5, y=None, n=None, pre: bool = True,
+                  stream=None) -> tuple:
     """The norms around a block (include/fe_layer.h): y = x + scale gate p with p the block's output z
     [..., d], normed if post (the default where post_weight is given), and n = norm(y), which the next
     block takes. gate is [groups, d] for groups of gate_rows rows (default: rows / groups, rounded up),
-    or [d] for all. Without z, y is x. Returns (y, n); outputs given may be z, or y x, themselves."""
+    or [d] for all. Without z, y is x (returned as it is unless an output is given). Returns (y, n), n None
+    if not pre; outputs given may be z, or y x, themselves."""
     post = post_weight is not None if post is None else post
     if post_weight is not None and not post:
         raise ValueError("post_weight without post")
     if z is None and (post or gate is not None):
         raise ValueError("a norm or a gate of the block's output needs z")
+    if not pre and (pre_weight is not None or n is not None or (z is None and y is None)):
+        raise ValueError("without a norm before the next block there is no pre_weight or n, and z or y is needed")
     if gate is not None and gate.dim() == 1:
         gate = gate[None]
     R, d = _rows_of(x), x.shape[-1]
     gate_rows = _gate_rows(gate, gate_rows, R)
     opts = (bool(post), gate_rows, float(scale), float(offset), float(eps))
     if y is None and n is None and _recorded(stream) and _wants(x, z, post_weight, gate, pre_weight):
-        return _BlockNorm.apply(t, opts, x, z, post_weight, gate, pre_weight)
+        out = _BlockNorm.apply(t, opts, pre, x, z, post_weight, gate, pre_weight)
+        return (x, out) if z is None else out if pre else (out, None)
     side = _side(stream)
-    y, n = _out(y, x.shape, x, side), _out(n, x.shape, x, side)
+    y = None if y is None and z is None else _out(y, x.shape, x, side)
+    n = _out(n, x.shape, x, side) if pre else None
     args = _norm_args(t, opts, x, z, post_weight, gate, pre_weight) + (*_mat(y, t.dtype, x.shape), *_mat(n, t.dtype, x.shape))
     if R:
         _call("fe_block_norm", t, side, (x, z, post_weight, gate, pre_weight, y, n), args)
-    return y, n
+    return x if y is None else y, n
 
 
 def _gate_rows(gate, rows, R: int) -> int:
@@ -390,24 +398,28 @@ def fe_block_norm_backward(t: Target, x, z=None, post: bool | None = None, post_
 
 
 class _BlockNorm(torch.autograd.Function):
+    """(y, n), or the one of them that is wanted: without z y is x, without pre there is no n."""
+
     @staticmethod
-    def forward(ctx, t, opts, x, z, post_weight, gate, pre_weight):
-        ctx.t, ctx.opts = t, opts
+    def forward(ctx, t, opts, pre, x, z, post_weight, gate, pre_weight):
+        ctx.t, ctx.opts, ctx.pre = t, opts, pre
         ctx.save_for_backward(x, z, post_weight, gate, pre_weight)
         ctx.set_materialize_grads(False)
         post, rows, scale, offset, eps = opts
-        return fe_block_norm(t, x, z, post, post_weight, gate, rows, scale, pre_weight, offset, eps)
+        y, n = fe_block_norm(t, x, z, post, post_weight, gate, rows, scale, pre_weight, offset, eps, pre=pre)
+        return n if z is None else (y, n) if pre else y
 
     @staticmethod
     @once_differentiable
-    def backward(ctx, dy, dn):
-        if dy is None and dn is None:
-            return (None,) * 7
+    def backward(ctx, *grads):
+        if all(g is None for g in grads):
+            return (None,) * 8
         x, z, post_weight, gate, pre_weight = ctx.saved_tensors
         post, rows, scale, offset, eps = ctx.opts
-        dy, dn = (None if g is None else _dense(g) for g in (dy, dn))
-        return None, None, *fe_block_norm_backward(ctx.t, x, z, post, post_weight, gate, rows, scale, pre_weight, offset, eps, dy, dn,
-                                                   ctx.needs_input_grad[2:])
+        grads = tuple(None if g is None else _dense(g) for g in grads)
+        dy, dn = grads if len(grads) == 2 else (None, *grads) if z is None else (*grads, None)
+        return None, None, None, *fe_block_norm_backward(ctx.t, x, z, post, post_weight, gate, rows, scale, pre_weight, offset, eps, dy,
+                                                         dn, ctx.needs_input_grad[3:])
 
 
 # ---- fe_token_logprobs -----------------------------------------------------------------------

@@ -337,9 +337,37 @@ def test_norm_alone(fe, handles):
     want = ref.norm(dict(post=False, rows=0, scale=1.0, offset=0.0, eps=1e-5, unit=2.0 ** -8), x, None, None, None, w, None, dn)
     (y, n), (dx, dw) = both(lambda x, w: fe.fe_block_norm(t, x, pre_weight=w), [x, w], [None, dn])
     assert torch.equal(y, x)
+    assert fe.fe_block_norm(t, x, pre_weight=w)[0] is x  # nothing is written
+    copy = torch.empty_like(x)
+    assert torch.equal(fe.fe_block_norm(t, x, pre_weight=w, y=copy)[1], n) and torch.equal(copy, x)
+    leaf = x.detach().requires_grad_()  # the residual's gradient joins the norm's
+    y, n2 = fe.fe_block_norm(t, leaf, pre_weight=w)
+    d, = torch.autograd.grad([y * 1.0, n2], [leaf], [torch.ones_like(x), dn])
+    assert torch.equal(d, (dx.float() + 1.0).bfloat16())
     ref.check(n, want["n"], "n")
     ref.check(dx, want["dx"], "dx")
     ref.check(dw, want["dpre"], "dw")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,d", [(20, 100), (9, 5120), (3, 20000)])
+def test_norm_behind_a_block_alone(fe, handles, dtype, R, d):
+    """The last block of a model: its norm, gate and residual, and no block behind it."""
+    t, g = handles[dtype], gen(d)
+    x, z, dy, pw, gate = (normal(g, dtype, *s) for s in ((R, d), (R, d), (R, d), (d,), (d,)))
+    want = ref.norm(dict(post=True, rows=R, scale=0.5, offset=1.0, eps=1e-5, unit=ref.UNIT[dtype]), x, z, pw, gate[None], None, dy, None)
+
+    def call(x, z, pw, gate):
+        y, n = fe.fe_block_norm(t, x, z, post_weight=pw, gate=gate, scale=0.5, offset=1.0, pre=False)
+        assert n is None
+        return y
+    (y,), got = both(call, [x, z, pw, gate], [dy])
+    ref.check(y, want["y"], "y")
+    for name, v in zip(("dx", "dz", "dpost"), got):
+        ref.check(v, want[name], name)
+    ref.check(got[3][None], want["dgate"], "dgate")
+    with pytest.raises(ValueError, match="pre_weight"):
+        fe.fe_block_norm(t, x, z, pre_weight=pw, pre=False)
 
 
 # ---- fe_token_logprobs ------------------------------------------------------------------------------
@@ -549,6 +577,32 @@ def test_captured_step(fe, handles, dtype):
         leaves[0].mul_(0.5)
     graphs[0].replay()
     assert all(torch.equal(x, y) for x, y in zip(results[0], run()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_captured_gradients_beside_a_living_graph(fe, handles, dtype):
+    """Gradients by plain calls are captured while an eager graph of the same leaves lives, and that graph's
+    own backward pass gives the same afterwards."""
+    t, g = handles[dtype], gen(12)
+    x, wg, wu, wd = normal(g, dtype, 150, 96), normal(g, dtype, 200, 96), normal(g, dtype, 200, 96), normal(g, dtype, 96, 200)
+    do = normal(g, dtype, 150, 96)
+    leaves = [v.detach().requires_grad_() for v in (x, wg, wu, wd)]
+    alive = fe.fe_gated_ffn(t, *leaves)
+
+    def step():
+        gp, up = torch.empty(150, 200, device="cuda"), torch.empty(150, 200, device="cuda")
+        fe.fe_gated_ffn(t, x, wg, wu, wd, gate_pre=gp, up_pre=up)
+        return fe.fe_gated_ffn_backward(t, do, gp, up, x, wg, wu, wd)
+    want = step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for v in got:
+        v.zero_()
+    graph.replay()
+    eager = torch.autograd.grad([alive], leaves, [do])
+    for a, b, c in zip(got, want, eager):
+        assert torch.equal(a, b) and torch.equal(a, c)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
