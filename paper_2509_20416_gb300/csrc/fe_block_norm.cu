@@ -10,8 +10,9 @@
 //             (y is computed again from x and z, so nothing rounded stands in for it)
 //
 // Measured (GB300, 16379 rows of 5120 bfloat16, gate, both norms): forward 114 us (5.9 TB/s; with one vector a thread
-// 134, loads in registers ahead instead of copies 143 to 193), gradient 223 us over 148 us of bytes, bound by
-// instruction issue (with CTAs of 640 threads 325; separate sums for gate and weight 30 % more registers and work).
+// 134, loads in registers ahead instead of copies 143 to 193), gradient 198 us over 148 us of bytes, bound by
+// instruction issue (with CTAs of 640 threads 325; separate sums for gate and weight 30 % more registers and work;
+// with the ring's stride in a register, not a constant of the kernel, 223).
 //
 // A worker is a CTA, or a warp where a row is at most 32 vectors of 16 bytes; its threads own
 // columns, so that the sums over rows stay in registers. The next row's loads are in flight while
@@ -110,11 +111,10 @@ __device__ __forceinline__ float pair_sum(uint64_t a) { return low_f32(a) + high
 
 // Rows on their way: a thread's vectors of the next rows, copied behind its back (cp.async) into slots that it
 // alone writes and reads. NA arrays, DEPTH rows.
-template <typename T, int NA, int VPT, bool FULL>
+template <typename T, int NA, int VPT, bool FULL, int S>
 struct RowRing {
-    uint4* mine;  // [DEPTH][NA][VPT] vectors, `threads` apart
-    int threads;
-    __device__ __forceinline__ uint4* at(int slot, int array, int j) const { return mine + ((slot * NA + array) * VPT + j) * threads; }
+    uint4* mine;  // [DEPTH][NA][VPT] vectors, S apart
+    __device__ __forceinline__ uint4* at(int slot, int array, int j) const { return mine + ((slot * NA + array) * VPT + j) * S; }
     __device__ __forceinline__ void fetch(int slot, int array, int j, const T* src, int have, bool vec) const {
         uint4* dst = at(slot, array, j);
         if (FULL || (vec && have >= Vec16<T>::kN)) cp_async16(smem_u32(dst), src, true);
@@ -125,6 +125,7 @@ __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_grou
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 constexpr int kNormDepth = 2;  // rows of a worker on their way
+constexpr int back_depth(int room) { return room <= 512 ? kNormDepth : 1; }  // in the backward pass: what 227 KB hold
 
 // the group of rows that share a gate (rows are below 2^30)
 __device__ __forceinline__ int64_t group_of(const NormArgs& a, int64_t r) {
@@ -141,7 +142,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
     const int64_t step = WARP ? (int64_t)gridDim.x * (blockDim.x / 32) : gridDim.x;
     int64_t r = WARP ? (int64_t)blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32 : blockIdx.x;
     const float inv_d = 1.f / (float)a.d;
-    const RowRing<T, 2, VPT, FULL> ring{ring_mem + threadIdx.x, (int)blockDim.x};
+    const RowRing<T, 2, VPT, FULL, MAXT> ring{ring_mem + threadIdx.x};
     const T *px = (const T*)a.x.p + r * a.x.row, *pz = (const T*)a.z.p + r * a.z.row;  // the next row to fetch
     const int64_t sx = step * a.x.row, sz_ = step * a.z.row;
     int64_t next = r;
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
         next += step;
     };
     // a thread's weights as they are stored, behind the rows
-    const auto hold = [&](int array, int j) { return ring_mem + threadIdx.x + ((D * 2 + array) * VPT + j) * blockDim.x; };
+    const auto hold = [&](int array, int j) { return ring_mem + threadIdx.x + ((D * 2 + array) * VPT + j) * MAXT; };
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int c = (j * nt + tid) * V, have = a.d - c;
@@ -377,7 +378,7 @@ __device__ __forceinline__ void store_packed(T* p, int have, bool vec, const uin
 }
 template <typename T, int VPT, bool WARP, int MAXT, int CTAS, bool FULL>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a, int64_t workers) {
-    constexpr int V = Vec16<T>::kN, N = V / 2, HN = N / 2, D = kNormDepth;
+    constexpr int V = Vec16<T>::kN, N = V / 2, HN = N / 2, D = back_depth(MAXT);
     extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
@@ -387,7 +388,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
     const float inv_d = 1.f / (float)a.d;
     int64_t r, r1;
     worker_rows(a, worker, r, r1);
-    const RowRing<T, 4, VPT, FULL> ring{ring_mem + threadIdx.x, (int)blockDim.x};
+    const RowRing<T, 4, VPT, FULL, MAXT> ring{ring_mem + threadIdx.x};
     const auto fetch = [&](int64_t row, int slot) {
         if (row < r1) {
 #pragma unroll
@@ -409,7 +410,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
         group_end = (group + 1) * a.gate_rows;
     }
     // a thread's w_pre as it is stored, and s g (w_post + o) of the current gate in float32, behind the rows
-    const auto hold = [&](int array, int j) { return ring_mem + threadIdx.x + ((D * 4 + array) * VPT + j) * blockDim.x; };
+    const auto hold = [&](int array, int j) { return ring_mem + threadIdx.x + ((D * 4 + array) * VPT + j) * MAXT; };
     const auto factor = [&](int j, int h) { return reinterpret_cast<uint64_t*>(hold(sizeof(T) == 2 ? 1 + h : 1, j)) + (sizeof(T) == 2 ? 0 : h); };
     // gates and post weights of a vector's columns, and what they are multiplied with
     const auto gates_of = [&](int j, float* g, float* w) {
@@ -785,7 +786,7 @@ template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
 cudaError_t launch_forward(const NormArgs& a, int threads, int num_sms, cudaStream_t st) {
     unsigned grid;
     const auto kern = whole<T>(a) ? norm_kernel<T, VPT, WARP, MAXT, CTAS, true> : norm_kernel<T, VPT, WARP, MAXT, CTAS, false>;
-    const size_t smem = (size_t)(kNormDepth + 1) * 2 * VPT * threads * sizeof(uint4);
+    const size_t smem = (size_t)(kNormDepth + 1) * 2 * VPT * MAXT * sizeof(uint4);
     const int64_t units = WARP ? (a.R + threads / 32 - 1) / (threads / 32) : a.R;
     static Known known[2];
     const cudaError_t e = resident(kern, known[whole<T>(a)], threads, smem, num_sms, units, grid);
@@ -800,7 +801,9 @@ template <typename T>
 cudaError_t forward(const NormArgs& a, int num_sms, cudaStream_t st) {
     const int64_t nv = (a.d + Vec16<T>::kN - 1) / Vec16<T>::kN;
     if (nv <= kWarpVecs) return launch_forward<T, 1, true, kNormWarps * 32, 8>(a, kNormWarps * 32, num_sms, st);
+    if (nv <= 128) return launch_forward<T, 1, false, 128, 8>(a, cta_threads(nv, 1), num_sms, st);
     if (nv <= 256) return launch_forward<T, 1, false, 256, 4>(a, cta_threads(nv, 1), num_sms, st);
+    if (nv <= 384) return launch_forward<T, 2, false, 192, 5>(a, cta_threads(nv, 2), num_sms, st);
     if (nv <= 640) return launch_forward<T, 2, false, 320, 3>(a, cta_threads(nv, 2), num_sms, st);
     if (nv <= kOne) return launch_forward<T, 2, false, 512, 2>(a, cta_threads(nv, 2), num_sms, st);
     if (nv <= kTwo) return launch_forward<T, 2, false, kOne, 1>(a, cta_threads(nv, 2), num_sms, st);
@@ -813,11 +816,47 @@ cudaError_t forward(const NormArgs& a, int num_sms, cudaStream_t st) {
 
 // how a row of d elements is held in the backward pass: by a warp, by a CTA (one or two vectors a thread), in passes
 enum NormForm { BY_WARP, BY_CTA, BY_CTA_2, IN_PASSES };
-NormForm backward_form(int64_t nv) { return nv <= kWarpVecs ? BY_WARP : nv <= 320 ? BY_CTA : nv <= kOne ? BY_CTA_2 : IN_PASSES; }
+NormForm backward_form(int64_t nv) { return nv <= kWarpVecs ? BY_WARP : nv <= 64 ? BY_CTA : nv <= kTwo ? BY_CTA_2 : IN_PASSES; }
 int form_threads(NormForm f, int64_t nv) {
     return f == BY_WARP ? kNormWarps * 32 : f == IN_PASSES ? 1024 : cta_threads(nv, f == BY_CTA ? 1 : 2);
 }
+// The kernels of the backward pass that hold a row: vectors a thread, threads at most (and room for them in the
+// ring), whether warps are workers, and the CTAs of an SM that registers are kept for. Two vectors a thread wherever
+// a row has enough: half the reductions' work for each element (128 MB of x, gradient without a gate: rows of 1024
+// float32 143 us, with one vector 192; 2048 bfloat16 161, 221; 2560 bfloat16 170, 205). Long rows keep one row on
+// its way and still beat passes over memory (5120 float32 211 us, 557; 8192 float32 190, 421).
+struct BackKernel {
+    int vpt, room;
+    bool warp;
+    int ctas;
+    int ctas_f32 = ctas;  // (a third CTA of 192 threads: float32 rows of 1536 149 us, 165 without; bfloat16 of 2880 214, 202)
+};
+constexpr BackKernel kBack[] = {{1, kNormWarps * 32, true, 5}, {1, 64, false, 9},  {2, 64, false, 9},  {2, 128, false, 5},
+                                {2, 160, false, 4},            {2, 192, false, 2, 3}, {2, 320, false, 2}, {2, 512, false, 1},
+                                {2, 768, false, 1},            {2, 1024, false, 1}};
+constexpr int kBacks = sizeof(kBack) / sizeof(kBack[0]);
+constexpr size_t back_smem(int i) { return (size_t)(back_depth(kBack[i].room) * 4 + 3) * kBack[i].vpt * kBack[i].room * sizeof(uint4); }
+int back_kernel(NormForm f, int threads) {
+    if (f == BY_WARP) return 0;
+    if (f == BY_CTA) return 1;
+    int i = 2;
+    while (kBack[i].room < threads) ++i;
+    return i;
+}
+// CTAs of each that fit an SM, as the device says when a handle is made
+std::atomic<int> back_fit[2][kBacks];
 int64_t row_vecs(int d, fe_dtype dtype) { return dtype == FE_F32 ? ((int64_t)d + 3) / 4 : ((int64_t)d + 7) / 8; }
+
+// f(i, FULL, kernel) for every kernel of the backward pass
+template <typename T, int I, typename F>
+void each_back(const F& f) {
+    if constexpr (I < kBacks) {
+        constexpr BackKernel k = kBack[I];
+        f(I, true, norm_backward_kernel<T, k.vpt, k.warp, k.room, sizeof(T) == 4 ? k.ctas_f32 : k.ctas, true>);
+        f(I, false, norm_backward_kernel<T, k.vpt, k.warp, k.room, sizeof(T) == 4 ? k.ctas_f32 : k.ctas, false>);
+        each_back<T, I + 1>(f);
+    }
+}
 
 template <typename T>
 cudaError_t backward(const NormArgs& a, fe_dtype dtype, cudaStream_t st) {
@@ -825,24 +864,14 @@ cudaError_t backward(const NormArgs& a, fe_dtype dtype, cudaStream_t st) {
     const NormForm form = backward_form(nv);
     const int threads = form_threads(form, nv);
     const int64_t workers = a.parts ? a.groups * a.parts : (a.groups + a.step - 1) / a.step;
-    const int vpt = form == BY_CTA_2 ? 2 : 1;
-    const size_t smem = (size_t)(kNormDepth * 4 + 3) * vpt * threads * sizeof(uint4);
-    const dim3 grid((unsigned)workers);
-    switch (form) {
-        case BY_WARP:
-            return launch_k(whole<T>(a) ? norm_backward_kernel<T, 1, true, kNormWarps * 32, 4, true> : norm_backward_kernel<T, 1, true, kNormWarps * 32, 4, false>, dim3((unsigned)((workers + kNormWarps - 1) / kNormWarps)),
-                            dim3(threads), smem, st, false, a, workers);
-        case BY_CTA:
-            return launch_k(whole<T>(a) ? norm_backward_kernel<T, 1, false, 320, 2, true> : norm_backward_kernel<T, 1, false, 320, 2, false>, grid,
-                            dim3(threads), smem, st, false, a, workers);
-        case BY_CTA_2:
-            if (threads <= 320)
-                return launch_k(whole<T>(a) ? norm_backward_kernel<T, 2, false, 320, 2, true> : norm_backward_kernel<T, 2, false, 320, 2, false>,
-                                grid, dim3(threads), smem, st, false, a, workers);
-            return launch_k(whole<T>(a) ? norm_backward_kernel<T, 2, false, 512, 1, true> : norm_backward_kernel<T, 2, false, 512, 1, false>, grid,
-                            dim3(threads), smem, st, false, a, workers);
-        default: return launch_k(norm_backward_long_kernel<T>, grid, dim3(threads), 0, st, false, a);
-    }
+    if (form == IN_PASSES) return launch_k(norm_backward_long_kernel<T>, dim3((unsigned)workers), dim3(threads), 0, st, false, a);
+    const int i = back_kernel(form, threads);
+    const int64_t ctas = form == BY_WARP ? (workers + kNormWarps - 1) / kNormWarps : workers;
+    cudaError_t e = cudaSuccess;
+    each_back<T, 0>([&](int k, bool full, auto kern) {
+        if (k == i && full == whole<T>(a)) e = launch_k(kern, dim3((unsigned)ctas), dim3(threads), back_smem(i), st, false, a, workers);
+    });
+    return e;
 }
 
 template <typename K>
@@ -853,14 +882,25 @@ cudaError_t allow(K kern, size_t bytes) {
 template <typename T, bool FULL>
 cudaError_t prepare() {
     cudaError_t e;
-    const size_t f = (kNormDepth + 1) * 2 * sizeof(uint4), f2 = 2 * f, b = (kNormDepth * 4 + 3) * sizeof(uint4);
+    const size_t f = (kNormDepth + 1) * 2 * sizeof(uint4), f2 = 2 * f;
     if ((e = allow(norm_kernel<T, 1, false, 256, 4, FULL>, f * 256)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 2, false, 192, 5, FULL>, f2 * 192)) != cudaSuccess) return e;
     if ((e = allow(norm_kernel<T, 2, false, 320, 3, FULL>, f2 * 320)) != cudaSuccess) return e;
     if ((e = allow(norm_kernel<T, 2, false, 512, 2, FULL>, f2 * 512)) != cudaSuccess) return e;
-    if ((e = allow(norm_kernel<T, 2, false, kOne, 1, FULL>, f2 * kOne)) != cudaSuccess) return e;
-    if ((e = allow(norm_backward_kernel<T, 1, false, 320, 2, FULL>, b * 320)) != cudaSuccess) return e;
-    if ((e = allow(norm_backward_kernel<T, 2, false, 320, 2, FULL>, b * 2 * 320)) != cudaSuccess) return e;
-    return allow(norm_backward_kernel<T, 2, false, 512, 1, FULL>, b * 2 * 512);
+    return allow(norm_kernel<T, 2, false, kOne, 1, FULL>, f2 * kOne);
+}
+
+template <typename T>
+cudaError_t prepare_backward() {
+    cudaError_t e = cudaSuccess;
+    each_back<T, 0>([&](int i, bool full, auto kern) {
+        if (e != cudaSuccess || (e = allow(kern, back_smem(i))) != cudaSuccess) return;
+        int per = 0;
+        if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, kBack[i].room, back_smem(i))) != cudaSuccess) return;
+        std::atomic<int>& fit = back_fit[sizeof(T) == 4][i];
+        if (full || per < fit.load(std::memory_order_relaxed)) fit.store(per, std::memory_order_relaxed);
+    });
+    return e;
 }
 
 }  // namespace
@@ -869,15 +909,17 @@ cudaError_t norm_prepare() {
     cudaError_t e;
     if ((e = prepare<float, true>()) != cudaSuccess || (e = prepare<float, false>()) != cudaSuccess) return e;
     if ((e = prepare<bf16_t, true>()) != cudaSuccess) return e;
-    return prepare<bf16_t, false>();
+    if ((e = prepare<bf16_t, false>()) != cudaSuccess || (e = prepare_backward<float>()) != cudaSuccess) return e;
+    return prepare_backward<bf16_t>();
 }
 
 int64_t norm_backward_plan(NormArgs& a, fe_dtype dtype, int num_sms) {
     const int64_t nv = row_vecs(a.d, dtype);
     const NormForm form = backward_form(nv);
-    // workers that fill the GPU once: 16 warps an SM, or the CTAs of some 640 threads
-    const int ctas = 640 / form_threads(form, nv);
-    const int64_t want = (int64_t)num_sms * (form == BY_WARP ? 16 : ctas > 0 ? ctas : 1);
+    // workers that fill the GPU once
+    const int i = form == IN_PASSES ? 0 : back_kernel(form, form_threads(form, nv));
+    const int fit = form == IN_PASSES ? 1 : back_fit[dtype == FE_F32][i].load(std::memory_order_relaxed);
+    const int64_t want = (int64_t)num_sms * (fit > 0 ? fit : kBack[i].ctas) * (form == BY_WARP ? kNormWarps : 1);
     const int64_t size = a.gate.p ? (a.gate_rows < a.R ? a.gate_rows : a.R) : a.R;
     a.gate_part = 1;
     a.groups = a.gate.p ? (a.R + a.gate_rows - 1) / a.gate_rows : 1;

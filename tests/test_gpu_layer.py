@@ -285,6 +285,25 @@ def test_gate_groups(fe, handles, dtype, R, d, rows):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [132, 300, 512, 1021, 1284, 1536, 2104, 2560, 2880, 2976, 4092, 5112, 6140, 8184, 12280, 12296, 16377])
+@pytest.mark.parametrize("rows", [None, 1, 3])
+def test_block_norm_forms(fe, handles, dtype, d, rows):
+    """Both edges of every form in which a row is held, with several rows for each worker."""
+    t, g = handles[dtype], gen(d)
+    R = 1 + min(3000, (1 << 22) // d)
+    x, z, dy, dn = (normal(g, dtype, R, d) for _ in range(4))
+    gate, pw, qw = normal(g, dtype, -(-R // rows), d) if rows else None, normal(g, dtype, d), normal(g, dtype, d)
+    want = ref.norm(dict(post=True, rows=rows or 0, scale=0.5, offset=1.0, eps=1e-5, unit=ref.UNIT[dtype]), x, z, pw, gate, qw, dy, dn)
+    y, n = fe.fe_block_norm(t, x, z, None, pw, gate, rows, 0.5, qw, 1.0)
+    ref.check(y, want["y"], "y")
+    ref.check(n, want["n"], "n")
+    got = fe.fe_block_norm_backward(t, x, z, None, pw, gate, rows, 0.5, qw, 1.0, dy=dy, dn=dn)
+    for name, v in zip(("dx", "dz", "dpost", "dgate", "dpre"), got):
+        if v is not None:
+            ref.check(v, want[name], name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [72, 1000, 9000, 20000])
 @pytest.mark.parametrize("left,right", [(8, 0), (1, 2)])
 def test_block_norm_strides_and_in_place(fe, handles, dtype, d, left, right):
