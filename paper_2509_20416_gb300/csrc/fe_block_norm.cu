@@ -10,7 +10,7 @@
 //             (y is computed again from x and z, so nothing rounded stands in for it)
 //
 // Measured (GB300, 16379 rows of 5120 bfloat16, gate, both norms): forward 114 us (5.9 TB/s; with one vector a thread
-// 134, loads in registers ahead instead of copies 143 to 193), gradient 198 us over 148 us of bytes, bound by
+// 134, loads in registers ahead instead of copies 143 to 193), gradient 174 us over 148 us of bytes, bound by
 // instruction issue (with CTAs of 640 threads 325; separate sums for gate and weight 30 % more registers and work;
 // with the ring's stride in a register, not a constant of the kernel, 223).
 //
@@ -376,9 +376,15 @@ __device__ __forceinline__ void store_packed(T* p, int have, bool vec, const uin
             if (i < have) p[i] = e[i];
     }
 }
-template <typename T, int VPT, bool WARP, int MAXT, int CTAS, bool FULL>
+// what a kernel of the backward pass may take for granted: nothing; rows that are whole vectors on their boundaries;
+// and with them every operand but the gate and w_post, which are read outside the loop over the rows
+// (16379 x 5120 bfloat16 with a gate 174 us, 198 with the questions asked in the loop).
+enum Given { ANY, WHOLE, ALL_GIVEN };
+template <typename T, int VPT, bool WARP, int MAXT, int CTAS, int KIND>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a, int64_t workers) {
     constexpr int V = Vec16<T>::kN, N = V / 2, HN = N / 2, D = back_depth(MAXT);
+    constexpr bool FULL = KIND >= WHOLE, ALL = KIND == ALL_GIVEN;
+    const bool has_z = ALL || a.z.p, has_dy = ALL || a.dy.p, has_dn = ALL || a.dn.p, has_post = ALL || a.post;
     extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
@@ -388,6 +394,10 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
     const float inv_d = 1.f / (float)a.d;
     int64_t r, r1;
     worker_rows(a, worker, r, r1);
+    // The half of a vector that a thread takes first: lanes 8 to 15 of every 16 the upper one, so that the 8-byte
+    // reads of 16 lanes, 16 bytes apart, meet every bank once. y, sdx and spre are in a thread's own order. (float32 rows
+    // of 5120 184 us, 206 without; bfloat16 in order: the selections cost more than the banks, 150 us against 156.)
+    const int flip = sizeof(T) == 4 ? threadIdx.x >> 3 & 1 : 0;
     const RowRing<T, 4, VPT, FULL, MAXT> ring{ring_mem + threadIdx.x};
     const auto fetch = [&](int64_t row, int slot) {
         if (row < r1) {
@@ -396,9 +406,9 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
                 const int c = (j * nt + tid) * V, have = a.d - c;
                 if (have <= 0) continue;
                 ring.fetch(slot, 0, j, (const T*)a.x.p + row * a.x.row + c, have, a.vec);
-                if (a.z.p) ring.fetch(slot, 1, j, (const T*)a.z.p + row * a.z.row + c, have, a.vec);
-                if (a.dy.p) ring.fetch(slot, 2, j, (const T*)a.dy.p + row * a.dy.row + c, have, a.vec);
-                if (a.dn.p) ring.fetch(slot, 3, j, (const T*)a.dn.p + row * a.dn.row + c, have, a.vec);
+                if (has_z) ring.fetch(slot, 1, j, (const T*)a.z.p + row * a.z.row + c, have, a.vec);
+                if (has_dy) ring.fetch(slot, 2, j, (const T*)a.dy.p + row * a.dy.row + c, have, a.vec);
+                if (has_dn) ring.fetch(slot, 3, j, (const T*)a.dn.p + row * a.dn.row + c, have, a.vec);
             }
         }
         cp_commit();
@@ -425,7 +435,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
         weights<T>(a.post_w, c, have, a.vec, a.offset, w);
     };
     const auto read_gate = [&] {
-        if (!a.z.p || r >= r1) return;
+        if (!has_z || r >= r1) return;
 #pragma unroll
         for (int j = 0; j < VPT; ++j) {
             if ((j * nt + tid) * V >= a.d) continue;
@@ -448,10 +458,12 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
             gates_of(j, g, w);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                t[2 * i] = low_f32(sdx[j][i]);
-                t[2 * i + 1] = high_f32(sdx[j][i]);
-                sdx[j][i] = 0;
+                const uint64_t v = flip ? sdx[j][i ^ HN] : sdx[j][i];
+                t[2 * i] = low_f32(v);
+                t[2 * i + 1] = high_f32(v);
             }
+#pragma unroll
+            for (int i = 0; i < N; ++i) sdx[j][i] = 0;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 g[i] *= t[i];
@@ -487,13 +499,13 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
             }
         }
     }
-    const auto pre_of = [&](int j, int h, Half<T>& w) { half_weights<T>(hold(0, j), h, a.pre_w, pair_f32(a.offset), w); };
+    const auto pre_of = [&](int j, int h, Half<T>& w) { half_weights<T>(hold(0, j), h ^ flip, ALL || a.pre_w, pair_f32(a.offset), w); };
     for (int i = 0; i < D; ++i) fetch(r + i, i);
     int slot = 0;
     for (; r < r1; ++r, slot = slot + 1 == D ? 0 : slot + 1) {
         cp_wait<D - 1>();
         float scale_z = 1.f;
-        if (a.post) {
+        if (has_post) {
             uint64_t q = 0;
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
@@ -516,16 +528,16 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 Half<T> f, w;
-                f.widen(ring.at(slot, 0, j), h);
-                if (a.z.p) {
+                f.widen(ring.at(slot, 0, j), h ^ flip);
+                if (has_z) {
                     Half<T> p;
-                    p.widen(ring.at(slot, 1, j), h);
+                    p.widen(ring.at(slot, 1, j), h ^ flip);
 #pragma unroll
-                    for (int i = 0; i < HN; ++i) f.v[i] = fma_x2(mul_x2(p.v[i], sz), factor(j, h)[i], f.v[i]);
+                    for (int i = 0; i < HN; ++i) f.v[i] = fma_x2(mul_x2(p.v[i], sz), factor(j, h ^ flip)[i], f.v[i]);
                 }
-                if (a.dn.p) {
+                if (has_dn) {
                     Half<T> dn;
-                    dn.widen(ring.at(slot, 3, j), h);
+                    dn.widen(ring.at(slot, 3, j), h ^ flip);
                     pre_of(j, h, w);
 #pragma unroll
                     for (int i = 0; i < HN; ++i) {
@@ -538,7 +550,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
             }
         }
         float scale_y = 0.f, back = 0.f;
-        if (a.dn.p) {
+        if (has_dn) {
             float t[2] = {pair_sum(q0), pair_sum(q1)};
             worker_sum<WARP, 2>(t, buf, turn);
             scale_y = rsqrtf(t[0] * inv_d + a.eps);
@@ -555,15 +567,15 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 Half<T> w, dx;
-                if (a.dy.p) {
-                    dx.widen(ring.at(slot, 2, j), h);
+                if (has_dy) {
+                    dx.widen(ring.at(slot, 2, j), h ^ flip);
                 } else {
 #pragma unroll
                     for (int i = 0; i < HN; ++i) dx.v[i] = 0;
                 }
-                if (a.dn.p) {
+                if (has_dn) {
                     Half<T> dn;
-                    dn.widen(ring.at(slot, 3, j), h);
+                    dn.widen(ring.at(slot, 3, j), h ^ flip);
                     pre_of(j, h, w);
 #pragma unroll
                     for (int i = 0; i < HN; ++i) {
@@ -574,24 +586,24 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
                     }
                 }
                 out[h] = dx.pack();
-                if (a.z.p) {
+                if (has_z) {
                     Half<T> z;
-                    z.widen(ring.at(slot, 1, j), h);
+                    z.widen(ring.at(slot, 1, j), h ^ flip);
 #pragma unroll
                     for (int i = 0; i < HN; ++i) {
                         const int k = h * HN + i;
-                        const uint64_t dp = mul_x2(dx.v[i], factor(j, h)[i]);
+                        const uint64_t dp = mul_x2(dx.v[i], factor(j, h ^ flip)[i]);
                         sdx[j][k] = fma_x2(dx.v[i], mul_x2(z.v[i], sz), sdx[j][k]);
                         q = fma_x2(dp, z.v[i], q);
                         y[j][k] = dp;
                     }
                 }
             }
-            if (a.dx.p) store_packed<T, FULL>((T*)a.dx.p + r * a.dx.row + c, have, a.vec, out[0], out[1]);
+            if (ALL || a.dx.p) store_packed<T, FULL>((T*)a.dx.p + r * a.dx.row + c, have, a.vec, flip ? out[1] : out[0], flip ? out[0] : out[1]);
         }
         float u[1] = {pair_sum(q)};
-        if (a.post) worker_sum<WARP, 1>(u, buf, turn);
-        if (a.dz.p) {
+        if (has_post) worker_sum<WARP, 1>(u, buf, turn);
+        if (ALL || a.dz.p) {
             const uint64_t bz = pair_f32(-u[0] * inv_d * scale_z * scale_z * scale_z);
 #pragma unroll
             for (int j = 0; j < VPT; ++j) {
@@ -601,15 +613,15 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     Half<T> z, dz;
-                    z.widen(ring.at(slot, 1, j), h);
+                    z.widen(ring.at(slot, 1, j), h ^ flip);
 #pragma unroll
                     for (int i = 0; i < HN; ++i) {
                         const uint64_t b = y[j][h * HN + i];
-                        dz.v[i] = a.post ? fma_x2(bz, z.v[i], mul_x2(sz, b)) : b;
+                        dz.v[i] = has_post ? fma_x2(bz, z.v[i], mul_x2(sz, b)) : b;
                     }
                     out[h] = dz.pack();
                 }
-                store_packed<T, FULL>((T*)a.dz.p + r * a.dz.row + c, have, a.vec, out[0], out[1]);
+                store_packed<T, FULL>((T*)a.dz.p + r * a.dz.row + c, have, a.vec, flip ? out[1] : out[0], flip ? out[0] : out[1]);
             }
         }
         fetch(r + D, slot);
@@ -630,8 +642,9 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_
         float f[V];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            f[2 * i] = low_f32(spre[j][i]);
-            f[2 * i + 1] = high_f32(spre[j][i]);
+            const uint64_t v = flip ? spre[j][i ^ HN] : spre[j][i];
+            f[2 * i] = low_f32(v);
+            f[2 * i + 1] = high_f32(v);
         }
         store_row<float, V>(a.part_pre + worker * a.d + c, a.d - c, false, f);
     }
@@ -814,31 +827,32 @@ cudaError_t forward(const NormArgs& a, int num_sms, cudaStream_t st) {
     return launch_k(norm_long_kernel<T>, dim3(grid), dim3(1024), 0, st, false, a);
 }
 
-// how a row of d elements is held in the backward pass: by a warp, by a CTA (one or two vectors a thread), in passes
-enum NormForm { BY_WARP, BY_CTA, BY_CTA_2, IN_PASSES };
-NormForm backward_form(int64_t nv) { return nv <= kWarpVecs ? BY_WARP : nv <= 64 ? BY_CTA : nv <= kTwo ? BY_CTA_2 : IN_PASSES; }
+// how a row of d elements is held in the backward pass: by a warp (one or two vectors a lane), by a CTA, in passes
+enum NormForm { BY_WARP, BY_WARP_2, BY_CTA, IN_PASSES };
+NormForm backward_form(int64_t nv) { return nv <= kWarpVecs ? BY_WARP : nv <= 2 * kWarpVecs ? BY_WARP_2 : nv <= kTwo ? BY_CTA : IN_PASSES; }
 int form_threads(NormForm f, int64_t nv) {
-    return f == BY_WARP ? kNormWarps * 32 : f == IN_PASSES ? 1024 : cta_threads(nv, f == BY_CTA ? 1 : 2);
+    return f <= BY_WARP_2 ? kNormWarps * 32 : f == IN_PASSES ? 1024 : cta_threads(nv, 2);
 }
 // The kernels of the backward pass that hold a row: vectors a thread, threads at most (and room for them in the
 // ring), whether warps are workers, and the CTAs of an SM that registers are kept for. Two vectors a thread wherever
 // a row has enough: half the reductions' work for each element (128 MB of x, gradient without a gate: rows of 1024
-// float32 143 us, with one vector 192; 2048 bfloat16 161, 221; 2560 bfloat16 170, 205). Long rows keep one row on
-// its way and still beat passes over memory (5120 float32 211 us, 557; 8192 float32 190, 421).
+// float32 143 us, with one vector 192; 2048 bfloat16 161, 221; 2560 bfloat16 170, 205), and a warp with two vectors
+// a lane before a CTA of 64 threads (rows of 320 bfloat16 214 us, 240; 512 alike). Long rows keep one row on its way
+// and still beat passes over memory (5120 float32 211 us, 557; 8192 float32 190, 421).
 struct BackKernel {
     int vpt, room;
     bool warp;
     int ctas;
     int ctas_f32 = ctas;  // (a third CTA of 192 threads: float32 rows of 1536 149 us, 165 without; bfloat16 of 2880 214, 202)
 };
-constexpr BackKernel kBack[] = {{1, kNormWarps * 32, true, 5}, {1, 64, false, 9},  {2, 64, false, 9},  {2, 128, false, 5},
-                                {2, 160, false, 4},            {2, 192, false, 2, 3}, {2, 320, false, 2}, {2, 512, false, 1},
-                                {2, 768, false, 1},            {2, 1024, false, 1}};
+constexpr BackKernel kBack[] = {{1, kNormWarps * 32, true, 5}, {2, kNormWarps * 32, true, 5}, {2, 64, false, 9},
+                                {2, 128, false, 5},            {2, 160, false, 4},            {2, 192, false, 2, 3},
+                                {2, 320, false, 2},            {2, 512, false, 1},            {2, 768, false, 1},
+                                {2, 1024, false, 1}};
 constexpr int kBacks = sizeof(kBack) / sizeof(kBack[0]);
 constexpr size_t back_smem(int i) { return (size_t)(back_depth(kBack[i].room) * 4 + 3) * kBack[i].vpt * kBack[i].room * sizeof(uint4); }
 int back_kernel(NormForm f, int threads) {
-    if (f == BY_WARP) return 0;
-    if (f == BY_CTA) return 1;
+    if (f <= BY_WARP_2) return f;
     int i = 2;
     while (kBack[i].room < threads) ++i;
     return i;
@@ -847,15 +861,21 @@ int back_kernel(NormForm f, int threads) {
 std::atomic<int> back_fit[2][kBacks];
 int64_t row_vecs(int d, fe_dtype dtype) { return dtype == FE_F32 ? ((int64_t)d + 3) / 4 : ((int64_t)d + 7) / 8; }
 
-// f(i, FULL, kernel) for every kernel of the backward pass
+// f(i, what it takes for granted, kernel) for every kernel of the backward pass
 template <typename T, int I, typename F>
 void each_back(const F& f) {
     if constexpr (I < kBacks) {
         constexpr BackKernel k = kBack[I];
-        f(I, true, norm_backward_kernel<T, k.vpt, k.warp, k.room, sizeof(T) == 4 ? k.ctas_f32 : k.ctas, true>);
-        f(I, false, norm_backward_kernel<T, k.vpt, k.warp, k.room, sizeof(T) == 4 ? k.ctas_f32 : k.ctas, false>);
+        constexpr int ctas = sizeof(T) == 4 ? k.ctas_f32 : k.ctas;
+        f(I, ANY, norm_backward_kernel<T, k.vpt, k.warp, k.room, ctas, ANY>);
+        f(I, WHOLE, norm_backward_kernel<T, k.vpt, k.warp, k.room, ctas, WHOLE>);
+        f(I, ALL_GIVEN, norm_backward_kernel<T, k.vpt, k.warp, k.room, ctas, ALL_GIVEN>);
         each_back<T, I + 1>(f);
     }
+}
+template <typename T>
+Given given(const NormArgs& a) {
+    return !whole<T>(a) ? ANY : a.z.p && a.dy.p && a.dn.p && a.post && a.dx.p && a.dz.p && a.pre_w ? ALL_GIVEN : WHOLE;
 }
 
 template <typename T>
@@ -866,10 +886,11 @@ cudaError_t backward(const NormArgs& a, fe_dtype dtype, cudaStream_t st) {
     const int64_t workers = a.parts ? a.groups * a.parts : (a.groups + a.step - 1) / a.step;
     if (form == IN_PASSES) return launch_k(norm_backward_long_kernel<T>, dim3((unsigned)workers), dim3(threads), 0, st, false, a);
     const int i = back_kernel(form, threads);
-    const int64_t ctas = form == BY_WARP ? (workers + kNormWarps - 1) / kNormWarps : workers;
+    const int64_t ctas = form <= BY_WARP_2 ? (workers + kNormWarps - 1) / kNormWarps : workers;
     cudaError_t e = cudaSuccess;
-    each_back<T, 0>([&](int k, bool full, auto kern) {
-        if (k == i && full == whole<T>(a)) e = launch_k(kern, dim3((unsigned)ctas), dim3(threads), back_smem(i), st, false, a, workers);
+    const Given g = given<T>(a);
+    each_back<T, 0>([&](int k, Given of, auto kern) {
+        if (k == i && of == g) e = launch_k(kern, dim3((unsigned)ctas), dim3(threads), back_smem(i), st, false, a, workers);
     });
     return e;
 }
@@ -893,12 +914,12 @@ cudaError_t prepare() {
 template <typename T>
 cudaError_t prepare_backward() {
     cudaError_t e = cudaSuccess;
-    each_back<T, 0>([&](int i, bool full, auto kern) {
+    each_back<T, 0>([&](int i, Given of, auto kern) {
         if (e != cudaSuccess || (e = allow(kern, back_smem(i))) != cudaSuccess) return;
         int per = 0;
         if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, kBack[i].room, back_smem(i))) != cudaSuccess) return;
         std::atomic<int>& fit = back_fit[sizeof(T) == 4][i];
-        if (full || per < fit.load(std::memory_order_relaxed)) fit.store(per, std::memory_order_relaxed);
+        if (of == ANY || per < fit.load(std::memory_order_relaxed)) fit.store(per, std::memory_order_relaxed);
     });
     return e;
 }
@@ -919,7 +940,7 @@ int64_t norm_backward_plan(NormArgs& a, fe_dtype dtype, int num_sms) {
     // workers that fill the GPU once
     const int i = form == IN_PASSES ? 0 : back_kernel(form, form_threads(form, nv));
     const int fit = form == IN_PASSES ? 1 : back_fit[dtype == FE_F32][i].load(std::memory_order_relaxed);
-    const int64_t want = (int64_t)num_sms * (fit > 0 ? fit : kBack[i].ctas) * (form == BY_WARP ? kNormWarps : 1);
+    const int64_t want = (int64_t)num_sms * (fit > 0 ? fit : kBack[i].ctas) * (form <= BY_WARP_2 ? kNormWarps : 1);
     const int64_t size = a.gate.p ? (a.gate_rows < a.R ? a.gate_rows : a.R) : a.R;
     a.gate_part = 1;
     a.groups = a.gate.p ? (a.R + a.gate_rows - 1) / a.gate_rows : 1;
