@@ -9,9 +9,9 @@
 //             with t = sum dx z rz over the rows of a gate:  dg = s (w_post + o) t,  dw_post = sum s g t
 //             (y is computed again from x and z, so nothing rounded stands in for it)
 //
-// Measured (GB300, 16379 rows of 5120 bfloat16, gate, both norms): forward 114 us (5.9 TB/s; with one vector a thread
+// Measured (GB300, 16379 rows of 5120 bfloat16, gate, both norms): forward 105 us (6.4 TB/s; with one vector a thread
 // 134, loads in registers ahead instead of copies 143 to 193), gradient 174 us over 148 us of bytes, bound by
-// instruction issue (with CTAs of 640 threads 325; separate sums for gate and weight 30 % more registers and work;
+// the latency of shared memory and by issue (57 % of the slots; with CTAs of 640 threads 325; separate sums for gate and weight 30 % more registers and work;
 // with the ring's stride in a register, not a constant of the kernel, 223).
 //
 // A worker is a CTA, or a warp where a row is at most 32 vectors of 16 bytes; its threads own
@@ -132,9 +132,15 @@ __device__ __forceinline__ int64_t group_of(const NormArgs& a, int64_t r) {
     return a.gate_rows >= a.R ? 0 : (uint32_t)r / (uint32_t)a.gate_rows;
 }
 
-template <typename T, int VPT, bool WARP, int MAXT, int CTAS, bool FULL>
+// What a kernel may take for granted: nothing; rows that are whole vectors on their boundaries; and with them every
+// operand but the gate and, in the backward pass, w_post, which are read outside its loop over the rows
+// (16379 x 5120 bfloat16 with a gate: gradient 174 us, 198 with the questions asked in the loop, forward 105, 112).
+enum Given { ANY, WHOLE, ALL_GIVEN };
+template <typename T, int VPT, bool WARP, int MAXT, int CTAS, int KIND>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant__ NormArgs a) {
     constexpr int V = Vec16<T>::kN, N = V / 2, D = kNormDepth;
+    constexpr bool FULL = KIND >= WHOLE, ALL = KIND == ALL_GIVEN;
+    const bool has_z = ALL || a.z.p, has_post = ALL || a.post;
     extern __shared__ uint4 ring_mem[];
     __shared__ float buf[2][64];
     int turn = 0;
@@ -153,7 +159,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
                 const int c = (j * nt + tid) * V, have = a.d - c;
                 if (have <= 0) continue;
                 ring.fetch(slot, 0, j, px + c, have, a.vec);
-                if (a.z.p) ring.fetch(slot, 1, j, pz + c, have, a.vec);
+                if (has_z) ring.fetch(slot, 1, j, pz + c, have, a.vec);
             }
         }
         cp_commit();
@@ -170,7 +176,7 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
         if (a.pre_w && have > 0) *hold(1, j) = load_vec<T, FULL>((const T*)a.pre_w + c, have, a.vec);
     }
     const auto held = [&](const void* w, int array, int j, Pairs<T>& p) {
-        if (!w) {
+        if (!ALL && !w) {
 #pragma unroll
             for (int i = 0; i < N; ++i) p.v[i] = pair_f32(1.f);
             return;
@@ -190,11 +196,11 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
         for (int j = 0; j < VPT; ++j) {
             const bool has = (j * nt + tid) * V < a.d;
             y[j].widen(has ? *ring.at(slot, 0, j) : make_uint4(0, 0, 0, 0));
-            z[j].widen(has && a.z.p ? *ring.at(slot, 1, j) : make_uint4(0, 0, 0, 0));
+            z[j].widen(has && has_z ? *ring.at(slot, 1, j) : make_uint4(0, 0, 0, 0));
         }
         fetch(slot);  // (outputs may be the inputs themselves: rows that have been read)
         float scale_z = 1.f;
-        if (a.post) {
+        if (has_post) {
             uint64_t q = 0;
 #pragma unroll
             for (int j = 0; j < VPT; ++j)
@@ -210,9 +216,9 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
         for (int j = 0; j < VPT; ++j) {
             const int c = (j * nt + tid) * V, have = a.d - c;
             if (have <= 0) continue;
-            if (a.z.p) {
+            if (has_z) {
                 Pairs<T> w;
-                if (a.post) {
+                if (has_post) {
                     held(a.post_w, 0, j, w);
                     const uint64_t sz = pair_f32(scale_z);
 #pragma unroll
@@ -228,14 +234,14 @@ __global__ void __launch_bounds__(MAXT, CTAS) norm_kernel(const __grid_constant_
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) q = fma_x2(y[j].v[i], y[j].v[i], q);
-            if (a.y.p) {
+            if (ALL || a.y.p) {
                 float f[V];
                 y[j].to(f);
                 store_vec<T, FULL>(py + c, have, a.vec, f);
             }
         }
         py += step * a.y.row;
-        if (!a.n.p) continue;
+        if (!ALL && !a.n.p) continue;
         float s[1] = {pair_sum(q)};
         worker_sum<WARP, 1>(s, buf, turn);
         const uint64_t sy = pair_f32(rsqrtf(s[0] * inv_d + a.eps));
@@ -376,10 +382,6 @@ __device__ __forceinline__ void store_packed(T* p, int have, bool vec, const uin
             if (i < have) p[i] = e[i];
     }
 }
-// what a kernel of the backward pass may take for granted: nothing; rows that are whole vectors on their boundaries;
-// and with them every operand but the gate and w_post, which are read outside the loop over the rows
-// (16379 x 5120 bfloat16 with a gate 174 us, 198 with the questions asked in the loop).
-enum Given { ANY, WHOLE, ALL_GIVEN };
 template <typename T, int VPT, bool WARP, int MAXT, int CTAS, int KIND>
 __global__ void __launch_bounds__(MAXT, CTAS) norm_backward_kernel(const __grid_constant__ NormArgs a, int64_t workers) {
     constexpr int V = Vec16<T>::kN, N = V / 2, HN = N / 2, D = back_depth(MAXT);
@@ -798,11 +800,15 @@ template <typename T> bool whole(const NormArgs& a) { return a.vec && a.d % Vec1
 template <typename T, int VPT, bool WARP, int MAXT, int CTAS>
 cudaError_t launch_forward(const NormArgs& a, int threads, int num_sms, cudaStream_t st) {
     unsigned grid;
-    const auto kern = whole<T>(a) ? norm_kernel<T, VPT, WARP, MAXT, CTAS, true> : norm_kernel<T, VPT, WARP, MAXT, CTAS, false>;
+    const bool all = a.z.p && a.post && a.post_w && a.pre_w && a.y.p && a.n.p;
+    const int kind = !whole<T>(a) ? ANY : all ? ALL_GIVEN : WHOLE;
+    const auto kern = kind == ANY     ? norm_kernel<T, VPT, WARP, MAXT, CTAS, ANY>
+                      : kind == WHOLE ? norm_kernel<T, VPT, WARP, MAXT, CTAS, WHOLE>
+                                      : norm_kernel<T, VPT, WARP, MAXT, CTAS, ALL_GIVEN>;
     const size_t smem = (size_t)(kNormDepth + 1) * 2 * VPT * MAXT * sizeof(uint4);
     const int64_t units = WARP ? (a.R + threads / 32 - 1) / (threads / 32) : a.R;
-    static Known known[2];
-    const cudaError_t e = resident(kern, known[whole<T>(a)], threads, smem, num_sms, units, grid);
+    static Known known[3];
+    const cudaError_t e = resident(kern, known[kind], threads, smem, num_sms, units, grid);
     if (e != cudaSuccess) return e;
     return launch_k(kern, dim3(grid), dim3(threads), smem, st, false, a);
 }
@@ -814,6 +820,7 @@ template <typename T>
 cudaError_t forward(const NormArgs& a, int num_sms, cudaStream_t st) {
     const int64_t nv = (a.d + Vec16<T>::kN - 1) / Vec16<T>::kN;
     if (nv <= kWarpVecs) return launch_forward<T, 1, true, kNormWarps * 32, 8>(a, kNormWarps * 32, num_sms, st);
+    if (nv <= 2 * kWarpVecs) return launch_forward<T, 2, true, kNormWarps * 32, 8>(a, kNormWarps * 32, num_sms, st);
     if (nv <= 128) return launch_forward<T, 1, false, 128, 8>(a, cta_threads(nv, 1), num_sms, st);
     if (nv <= 256) return launch_forward<T, 1, false, 256, 4>(a, cta_threads(nv, 1), num_sms, st);
     if (nv <= 384) return launch_forward<T, 2, false, 192, 5>(a, cta_threads(nv, 2), num_sms, st);
@@ -900,15 +907,15 @@ cudaError_t allow(K kern, size_t bytes) {
     return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T, bool FULL>
+template <typename T, int KIND>
 cudaError_t prepare() {
     cudaError_t e;
     const size_t f = (kNormDepth + 1) * 2 * sizeof(uint4), f2 = 2 * f;
-    if ((e = allow(norm_kernel<T, 1, false, 256, 4, FULL>, f * 256)) != cudaSuccess) return e;
-    if ((e = allow(norm_kernel<T, 2, false, 192, 5, FULL>, f2 * 192)) != cudaSuccess) return e;
-    if ((e = allow(norm_kernel<T, 2, false, 320, 3, FULL>, f2 * 320)) != cudaSuccess) return e;
-    if ((e = allow(norm_kernel<T, 2, false, 512, 2, FULL>, f2 * 512)) != cudaSuccess) return e;
-    return allow(norm_kernel<T, 2, false, kOne, 1, FULL>, f2 * kOne);
+    if ((e = allow(norm_kernel<T, 1, false, 256, 4, KIND>, f * 256)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 2, false, 192, 5, KIND>, f2 * 192)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 2, false, 320, 3, KIND>, f2 * 320)) != cudaSuccess) return e;
+    if ((e = allow(norm_kernel<T, 2, false, 512, 2, KIND>, f2 * 512)) != cudaSuccess) return e;
+    return allow(norm_kernel<T, 2, false, kOne, 1, KIND>, f2 * kOne);
 }
 
 template <typename T>
@@ -928,9 +935,10 @@ cudaError_t prepare_backward() {
 
 cudaError_t norm_prepare() {
     cudaError_t e;
-    if ((e = prepare<float, true>()) != cudaSuccess || (e = prepare<float, false>()) != cudaSuccess) return e;
-    if ((e = prepare<bf16_t, true>()) != cudaSuccess) return e;
-    if ((e = prepare<bf16_t, false>()) != cudaSuccess || (e = prepare_backward<float>()) != cudaSuccess) return e;
+    if ((e = prepare<float, ANY>()) != cudaSuccess || (e = prepare<float, WHOLE>()) != cudaSuccess) return e;
+    if ((e = prepare<float, ALL_GIVEN>()) != cudaSuccess || (e = prepare<bf16_t, ANY>()) != cudaSuccess) return e;
+    if ((e = prepare<bf16_t, WHOLE>()) != cudaSuccess || (e = prepare<bf16_t, ALL_GIVEN>()) != cudaSuccess) return e;
+    if ((e = prepare_backward<float>()) != cudaSuccess) return e;
     return prepare_backward<bf16_t>();
 }
 
