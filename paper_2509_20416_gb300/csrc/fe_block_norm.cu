@@ -11,10 +11,11 @@
 //
 // Measured (GB300, 16379 rows of 5120 bfloat16, gate, both norms): forward 105 us (6.4 TB/s; with one vector a thread
 // 134, loads in registers ahead instead of copies 143 to 193), gradient 174 us over 148 us of bytes, bound by
-// the latency of shared memory and by issue (57 % of the slots; with CTAs of 640 threads 325; separate sums for gate and weight 30 % more registers and work;
-// with the ring's stride in a register, not a constant of the kernel, 223).
+// the latency of shared memory and by issue (57 % of the slots; with CTAs of 640 threads 325; separate sums for
+// gate and weight 30 % more registers and work; with the ring's stride in a register, not a constant of the
+// kernel, 223).
 //
-// A worker is a CTA, or a warp where a row is at most 32 vectors of 16 bytes; its threads own
+// A worker is a CTA, or a warp where a row is at most 64 vectors of 16 bytes; its threads own
 // columns, so that the sums over rows stay in registers. The next row's loads are in flight while
 // a row's statistics are reduced.
 #include <atomic>
