@@ -922,13 +922,16 @@ cudaError_t prepare() {
 template <typename T>
 cudaError_t prepare_backward() {
     cudaError_t e = cudaSuccess;
+    int fit[kBacks] = {};
     each_back<T, 0>([&](int i, Given of, auto kern) {
         if (e != cudaSuccess || (e = allow(kern, back_smem(i))) != cudaSuccess) return;
         int per = 0;
         if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kern, kBack[i].room, back_smem(i))) != cudaSuccess) return;
-        std::atomic<int>& fit = back_fit[sizeof(T) == 4][i];
-        if (of == ANY || per < fit.load(std::memory_order_relaxed)) fit.store(per, std::memory_order_relaxed);
+        fit[i] = of == ANY || per < fit[i] ? per : fit[i];
     });
+    if (e == cudaSuccess) {  // (the same numbers for every handle)
+        for (int i = 0; i < kBacks; ++i) back_fit[sizeof(T) == 4][i].store(fit[i], std::memory_order_relaxed);
+    }
     return e;
 }
 
