@@ -110,9 +110,9 @@ def _rows_of(x) -> int:
 
 
 def _new(shape, like, side, dtype=None):
-    """A new output of a call (on `side`: allocated there)."""
+    """A new output of a call (on `side`: allocated there). (torch.empty: half the time of Tensor.new_empty.)"""
     if side is None:
-        return like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
+        return torch.empty(shape, dtype=like.dtype if dtype is None else dtype, device=like.device)
     return _empty(shape, like.dtype if dtype is None else dtype, like.device, side)
 
 
@@ -330,16 +330,16 @@ def fe_block_norm(t: Target, x, z=None, post: bool | None = None, post_weight=No
         raise ValueError("without a norm before the next block there is no pre_weight or n, and z or y is needed")
     if gate is not None and gate.dim() == 1:
         gate = gate[None]
-    R, d = _rows_of(x), x.shape[-1]
+    R, shape = _rows_of(x), x.shape
     gate_rows = _gate_rows(gate, gate_rows, R)
     opts = (bool(post), gate_rows, float(scale), float(offset), float(eps))
     if y is None and n is None and _recorded(stream) and _wants(x, z, post_weight, gate, pre_weight):
         out = _BlockNorm.apply(t, opts, pre, x, z, post_weight, gate, pre_weight)
         return (x, out) if z is None else out if pre else (out, None)
     side = _side(stream)
-    y = None if y is None and z is None else _out(y, x.shape, x, side)
-    n = _out(n, x.shape, x, side) if pre else None
-    args = _norm_args(t, opts, x, z, post_weight, gate, pre_weight) + (*_mat(y, t.dtype, x.shape), *_mat(n, t.dtype, x.shape))
+    y = None if y is None and z is None else _out(y, shape, x, side)
+    n = _out(n, shape, x, side) if pre else None
+    args = _norm_args(t, opts, x, z, post_weight, gate, pre_weight) + (*_mat(y, t.dtype, shape), *_mat(n, t.dtype, shape))
     if R:
         _call("fe_block_norm", t, side, (x, z, post_weight, gate, pre_weight, y, n), args)
     return x if y is None else y, n
@@ -361,10 +361,11 @@ def _gate_rows(gate, rows, R: int) -> int:
 
 def _norm_args(t, opts, x, z, post_weight, gate, pre_weight) -> tuple:
     post, rows, scale, offset, eps = opts
-    d = x.shape[-1]
-    return (_rows_of(x), d, int(post), *_mat(x, t.dtype, x.shape), *_mat(z, t.dtype, x.shape),
-            *_mat(gate, t.dtype, None if gate is None else (gate.shape[0], d)), rows, _vec(post_weight, t.dtype, d),
-            _vec(pre_weight, t.dtype, d), scale, offset, eps)
+    shape, dtype = x.shape, t.dtype
+    d = shape[-1]
+    return (_rows_of(x), d, int(post), *_mat(x, dtype, shape), *_mat(z, dtype, shape),
+            *_mat(gate, dtype, None if gate is None else (gate.shape[0], d)), rows, _vec(post_weight, dtype, d),
+            _vec(pre_weight, dtype, d), scale, offset, eps)
 
 
 def fe_block_norm_backward(t: Target, x, z=None, post: bool | None = None, post_weight=None, gate=None, gate_rows: int | None = None,
