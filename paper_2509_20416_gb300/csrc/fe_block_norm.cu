@@ -953,7 +953,7 @@ int64_t norm_backward_plan(NormArgs& a, fe_dtype dtype, int num_sms) {
     const int i = form == IN_PASSES ? 0 : back_kernel(form, form_threads(form, nv));
     const int fit = form == IN_PASSES ? 1 : back_fit[dtype == FE_F32][i].load(std::memory_order_relaxed);
     const int64_t want = (int64_t)num_sms * (fit > 0 ? fit : kBack[i].ctas) * (form <= BY_WARP_2 ? kNormWarps : 1);
-    const int64_t size = a.gate.p ? (a.gate_rows < a.R ? a.gate_rows : a.R) : a.R;
+    const int64_t size = a.gate.p ? a.gate_rows : a.R;
     a.gate_part = 1;
     a.groups = a.gate.p ? (a.R + a.gate_rows - 1) / a.gate_rows : 1;
     if (a.groups >= want) {

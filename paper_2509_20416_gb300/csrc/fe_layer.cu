@@ -297,6 +297,9 @@ fe_status gated_backward(const fe_target* t, const fe_gated_ffn_backward_args* a
     return product_gradients(t, a->M, a->F, a->K, a->x, weights, dz, 2, a->dx, dw, w, count, st);
 }
 
+// Groups of rows that share gates (gate_rows may be any positive number).
+int64_t gate_groups(int64_t R, int64_t gate_rows) { return R ? (R - 1) / gate_rows + 1 : 0; }
+
 template <typename A>
 bool norm_sizes_ok(const fe_target* t, const A* a) {
     if (!t || !a || a->R < 0 || a->R > kMaxRows || a->d < 1 || a->d > kMaxNorm) return false;
@@ -318,7 +321,7 @@ bool norm_backward_ok(const fe_target* t, const fe_block_norm_backward_args* a) 
     const int es = elem(t);
     if ((!a->z.p && a->dz.p) || (!a->gate.p && a->dgate.p) || (!a->post && a->dpost_w)) return false;
     if (!a->dx.p && !a->dz.p && !a->dgate.p && !a->dpost_w && !a->dpre_w) return false;
-    const int64_t groups = a->gate.p ? (a->R + a->gate_rows - 1) / a->gate_rows : 0;
+    const int64_t groups = a->gate.p ? gate_groups(a->R, a->gate_rows) : 0;
     return opt_in(a->dy, es) && opt_in(a->dn, es) && opt_out(a->dx, a->R, a->d, es) && opt_out(a->dz, a->R, a->d, es) &&
            opt_out(a->dgate, groups, a->d, es) && opt_ptr(a->dpost_w, es) && opt_ptr(a->dpre_w, es);
 }
@@ -332,7 +335,7 @@ NormArgs norm_args(const A* a) {
     n.x = a->x;
     n.z = a->z;
     n.gate = a->gate;
-    n.gate_rows = a->gate.p ? a->gate_rows : a->R;
+    n.gate_rows = a->gate.p && a->gate_rows < a->R ? a->gate_rows : a->R;  // (what follows counts with sums of it and R)
     n.post_w = a->post ? a->post_w : nullptr;
     n.pre_w = a->pre_w;
     n.scale = a->scale;

@@ -52,7 +52,7 @@ struct NormArgs {
     int64_t R;
     int d, post;
     fe_mat x, z, gate;
-    int64_t gate_rows;
+    int64_t gate_rows;            // at most R
     const void *post_w, *pre_w;
     float scale, offset, eps;
     fe_mat y, n;                  // forward

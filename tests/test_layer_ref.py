@@ -242,6 +242,19 @@ def test_library_refuses_bad_arguments(fe, handle, name):
         assert size(handle[0], packed) >= 0
 
 
+def test_gates_of_more_rows_than_there_are(fe, handle):
+    """A gate's rows may be any positive number: from R on they are one group."""
+    from paper_2509_20416_gb300 import layer
+    size = lambda rows, R: layer._WORK["fe_block_norm_backward"](
+        handle[0], layer._PACK["fe_block_norm_backward"](*[R if i == 0 else v for i, v in enumerate(spoil("fe_block_norm_backward", "gate_rows", rows))]))
+    for R in (1, 8, 5000):
+        want = size(R, R)
+        assert want > 0
+        for rows in (R + 1, 1 << 31, 1 << 62, (1 << 63) - R, (1 << 63) - 1):
+            assert size(rows, R) == want, (R, rows)
+    assert size((1 << 63) - 1, 0) == 0
+
+
 def test_binding_refuses_what_is_no_cuda_tensor(fe):
     t = fe.Target(0, dict(n_heads=1, n_kv_heads=1, head_dim=64, max_seq=16, dtype="f32", rope_theta=1e4))
     x, w = torch.zeros(2, 8), torch.zeros(4, 8)
