@@ -429,9 +429,10 @@ _LOGITS = {torch.float32: FE_F32, torch.bfloat16: FE_BF16}
 
 
 def _contiguous(x, side):
-    """x, copied on the call's stream where it is not contiguous."""
+    """x, copied on the call's stream where it is not contiguous; there x is in use until the copy has run."""
     if x.is_contiguous() or side is None:
         return x.contiguous()
+    x.record_stream(side)
     with torch.cuda.stream(side):
         return x.contiguous()
 

@@ -24,3 +24,33 @@ def test_gates_of_more_rows_than_there_are(fe, handles, dtype, d):  # noqa: F811
         got = fe.fe_block_norm_backward(t, x, z, None, pw, gate, rows, dy=dy, dn=dn)
         for name, v in zip(("dx", "dz", "dpost", "dgate"), got):
             ref.check(v, want[name], name)
+
+
+def test_dropped_inputs_of_another_stream(fe, handles):  # noqa: F811
+    """Inputs that are not contiguous are copied on the call's stream. A caller may drop them at once: memory that
+    is then handed out on the current stream is not theirs while the copy waits."""
+    t, g, R, V = handles["f32"], gen(3), 4096, 64
+    logits = normal(g, "f32", R, V)
+    tok = torch.randint(0, V, (R, 2), generator=g, device="cuda", dtype=torch.int32)
+    grads = torch.randn(R, 2, generator=g, device="cuda")
+    stats = torch.empty(R, 2, device="cuda")
+    want = fe.fe_token_logprobs(t, logits, tok[:, :1].contiguous(), stats=stats)[0]
+    want_d = fe.fe_token_logprobs_backward(t, logits, stats, tok[:, :1].contiguous(), grads[:, :1].contiguous())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    fe.fe_token_logprobs(t, logits, tok[:, :1], stream=s)  # (kernels loaded before the pause)
+    torch.cuda.synchronize()
+    for call in range(2):
+        ids, dl = tok.clone(), grads.clone()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(100_000_000)
+        if call == 0:
+            got = fe.fe_token_logprobs(t, logits, ids[:, :1], stream=s)[0]
+        else:
+            got = fe.fe_token_logprobs_backward(t, logits, stats, ids[:, :1], dl[:, :1], stream=s)
+        del ids, dl
+        others = [torch.full((R, 2), 7, dtype=torch.int32, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        assert torch.equal(got, want if call == 0 else want_d), call
+        assert all((o == 7).all() for o in others)

@@ -273,6 +273,37 @@ def test_binding_refuses_what_is_no_cuda_tensor(fe):
         fe.fe_block_norm(t, x, x, gate=x[:1], gate_rows=1)
 
 
+def test_a_copy_on_a_stream_notes_its_source(fe, monkeypatch):
+    """What a call copies on its stream is noted as in use there before the copy is queued: its memory may not be
+    handed out again until the copy has run. Contiguous inputs are noted by the call itself."""
+    from contextlib import nullcontext
+
+    from paper_2509_20416_gb300 import layer
+    monkeypatch.setattr(torch.cuda, "stream", lambda side: nullcontext())
+
+    class Input:
+        def __init__(self, contiguous):
+            self.events, self._c = [], contiguous
+
+        def is_contiguous(self):
+            return self._c
+
+        def record_stream(self, side):
+            self.events.append(("in use", side))
+
+        def contiguous(self):
+            self.events.append("copy")
+            return self
+    x = Input(False)
+    layer._contiguous(x, "side")
+    assert x.events == [("in use", "side"), "copy"]
+    x = Input(False)
+    layer._contiguous(x, None)
+    assert x.events == ["copy"]
+    x = Input(True)
+    assert layer._contiguous(x, "side") is x and not any(e != "copy" for e in x.events)
+
+
 def test_row_strides(fe):
     from paper_2509_20416_gb300.layer import _row
     x = torch.zeros(4, 6, 10)
