@@ -102,8 +102,10 @@ __device__ __forceinline__ void store4(float* p, int have, bool vec, const float
 
 // A warp's 32 x 32 block turned from a row a lane (as tensor memory gives it) to four columns a lane, 8
 // lanes a row, so that rows meet global memory in whole sectors. 16-byte chunk c of row r lies at c ^ (r & 7).
+// What comes before it branches by lane at ragged edges; the load from tensor memory is the warp's as one.
 __device__ __forceinline__ void stage_rows(float* buf, uint32_t d, int lane) {
     float z[32];
+    __syncwarp();
     tc_ld32(d, z);
 #pragma unroll
     for (int c = 0; c < 8; ++c)

@@ -145,7 +145,15 @@ __device__ __forceinline__ uint64_t largest_below(const RowShare<T>& r, uint64_t
     return best;
 }
 
-__device__ __forceinline__ void lp_sync() { named_sync(1, kLpThreads); }  // the reading warps
+// the reading warps, and the cluster; their lanes have to arrive as one, whatever branches lie before
+__device__ __forceinline__ void lp_sync() {
+    __syncwarp();
+    named_sync(1, kLpThreads);
+}
+__device__ __forceinline__ void lp_cluster_sync(const cg::cluster_group& cluster) {
+    __syncwarp();
+    cluster.sync();
+}
 
 // The K-th largest of 32 groups' maxima (best: the order of the thread's largest element so far, 0 for none), which
 // no more than K - 1 of the share's elements need exceed; 1, below every order, where fewer groups have any.
@@ -265,8 +273,8 @@ __global__ void __launch_bounds__(kLpThreads + 32, 4) logprob_kernel(const __gri
             }
             __syncwarp();
             if (ranks > 1) {
-                cluster.sync();
-                cluster.sync();
+                lp_cluster_sync(cluster);
+                lp_cluster_sync(cluster);
             }
         }
         if (lane == 0 && !ok) {  // (what is in flight lands before the CTA ends)
@@ -382,7 +390,7 @@ __global__ void __launch_bounds__(kLpThreads + 32, 4) logprob_kernel(const __gri
             st = warp_join(lane < warps ? sh.stats[lane] : Stats{kLowest, 0.f, 0.f}, c);
             if (lane == 0) sh.total = st;
         }
-        if (ranks > 1) cluster.sync();
+        if (ranks > 1) lp_cluster_sync(cluster);
         else lp_sync();
         if (rank == 0) {
             if (warp == 0 && ranks > 1) {
@@ -428,7 +436,7 @@ __global__ void __launch_bounds__(kLpThreads + 32, 4) logprob_kernel(const __gri
                 a.top_logprob[row * a.K + tid] = bad ? NAN : logp(key_value(sh.top[tid]));
             }
         }
-        if (ranks > 1) cluster.sync();  // (the others' shared memory has been read)
+        if (ranks > 1) lp_cluster_sync(cluster);  // (the others' shared memory has been read)
         else lp_sync();
     }
 }

@@ -54,3 +54,24 @@ def test_dropped_inputs_of_another_stream(fe, handles):  # noqa: F811
         torch.cuda.synchronize()
         assert torch.equal(got, want if call == 0 else want_d), call
         assert all((o == 7).all() for o in others)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(3, 900, 333), (90, 1500, 131), (300, 200, 77), (1501, 136, 4099), (2817, 72, 2050)])
+def test_ragged_edges(fe, handles, dtype, M, K, N):  # noqa: F811
+    """Edges at which the lanes of a warp have different numbers of columns and rows to read, in one tile and in
+    several of a CTA, with all that a product's end reads and writes."""
+    t, g = handles[dtype], gen(M + N)
+    x, w = normal(g, dtype, M, K), normal(g, dtype, N, K, std=K ** -0.5)
+    b, r = normal(g, dtype, N), normal(g, dtype, M, N)
+    pre = torch.empty(M, N, device="cuda")
+    c = dict(act="silu", unit=ref.UNIT[dtype])
+    out = fe.fe_project(t, x, w, b, "silu", r, pre=pre)
+    ref.check(out, ref.project(c, x, w, b, r)["out"], "out")
+    ref.check(pre, ref.project(dict(act="none", unit=0.0), x, w, b, None)["out"], "pre")
+    if N % 2:
+        want = ref.logprobs(out.float(), torch.zeros(M, 1, dtype=torch.int32, device="cuda"), 1.0, 5)
+        ent, lse, ids = fe.fe_token_logprobs(t, out.float(), top=5)[1:4]
+        ref.check(ent, want["entropy"], "entropy")
+        ref.check(lse, want["lse"], "lse")
+        assert torch.equal(ids, want["top_id"])
