@@ -26,6 +26,10 @@ constexpr int kFinishWarps = 8;
 constexpr int kTcThreads = 64 + 32 * kFinishWarps;
 constexpr int kTileM = 256, kSliceK = 64;
 
+// How long a finishing warp waits for a tile, besides what any wait gets: a weight's gradient sums up to 2^24 slices
+// in one tile, at 230 ns each where a pair works alone, 750 where the copies of all pairs come from memory.
+constexpr int64_t kSliceBudgetNs = 2000;
+
 constexpr int kSliceA = 128 * kSliceK * 2;
 constexpr int kStaging = kFinishWarps * 4096;  // a warp's 32 x 32 floats
 constexpr int kTcRing = 192 * 1024, kTcStages = 8;
@@ -388,7 +392,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
             const uint32_t buf = i & 1, use = i >> 1, d = tmem + buf * 256 + lanes;
             const auto wait = [&] {
                 bool ok = true;
-                if (lane == 0) ok = mbar_wait(&bar.done[buf], use & 1, g.status);
+                if (lane == 0) ok = mbar_wait(&bar.done[buf], use & 1, g.status, kWaitBudgetNs + all * kSliceBudgetNs);
                 ok = __shfl_sync(0xffffffffu, ok, 0);
                 tc_fence_after();
                 return ok;

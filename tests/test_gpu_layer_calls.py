@@ -75,3 +75,19 @@ def test_ragged_edges(fe, handles, dtype, M, K, N):  # noqa: F811
         ref.check(ent, want["entropy"], "entropy")
         ref.check(lse, want["lse"], "lse")
         assert torch.equal(ids, want["top_id"])
+
+
+def test_weight_gradient_of_the_most_rows(fe, handles):  # noqa: F811
+    """2^30 rows, which one pair of CTAs sums in seconds: nothing gives up on it. Most rows are zeros, so that the
+    few others' sum is known."""
+    t, g, M, N, K = handles["bf16"], gen(30), 1 << 30, 8, 16
+    dout, x = (torch.zeros(M, n, dtype=torch.bfloat16, device="cuda") for n in (N, K))
+    at = torch.randint(0, M, (1000,), generator=g, device="cuda").unique()
+    at = torch.cat([at, torch.tensor([M - 1], device="cuda")]).unique()
+    dout[at], x[at] = normal(g, "bf16", len(at), N), normal(g, "bf16", len(at), K)
+    _, dw, _ = fe.fe_project_backward(t, dout, x, dx=False)
+    assert fe.fe_target_status(t) == fe.FE_OK
+    q = ref.Product(dout[at].T, x[at].T)
+    ref.check(dw, (q.v, q.err + 2.0 ** -8 * (q.v.abs() + q.err)), "dw")
+    del dout, x
+    torch.cuda.empty_cache()
