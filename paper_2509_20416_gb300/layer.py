@@ -253,8 +253,9 @@ def fe_gated_ffn(t: Target, x, w_gate, w_up, w_down=None, act: str = "silu", res
     if out is None and gate_pre is None and up_pre is None and _recorded(stream) and _wants(x, w_gate, w_up, w_down, residual):
         return _Gated.apply(t, act, x, w_gate, w_up, w_down, residual)
     if w_down is not None:
-        h = fe_gated_ffn(t, x, w_gate, w_up, act=act, gate_pre=gate_pre, up_pre=up_pre, stream=stream)
-        return fe_project(t, h, w_down, residual=residual, out=out, stream=stream)
+        with torch.no_grad():  # (not recorded as a whole: neither of its parts is)
+            h = fe_gated_ffn(t, x, w_gate, w_up, act=act, gate_pre=gate_pre, up_pre=up_pre, stream=stream)
+            return fe_project(t, h, w_down, residual=residual, out=out, stream=stream)
     F, K = w_gate.shape
     side, shape, M = _side(stream), _shaped(x, F), _rows_of(x)
     args = (M, F, K, *_mat(x, t.dtype, _shaped(x, K)), *_mat(w_gate, t.dtype, (F, K)), *_mat(w_up, t.dtype, (F, K)))

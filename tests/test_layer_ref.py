@@ -304,6 +304,24 @@ def test_a_copy_on_a_stream_notes_its_source(fe, monkeypatch):
     assert layer._contiguous(x, "side") is x and not any(e != "copy" for e in x.events)
 
 
+def test_a_block_with_outputs_given_is_not_recorded_in_part(fe, monkeypatch):
+    """Outputs given keep a call out of autograd: its result must not carry the graph of the last product alone."""
+    from paper_2509_20416_gb300 import layer
+    seen = []
+    monkeypatch.setattr(layer, "_mat", lambda x, dtype, shape: (0, 0))
+    monkeypatch.setattr(layer, "_call", lambda name, t, side, tensors, args: seen.append((name, tensors)))
+    t = fe.Target(0, dict(n_heads=1, n_kv_heads=1, head_dim=64, max_seq=16, dtype="f32", rope_theta=1e4))
+    x, wg, wu, wd, r = (torch.zeros(8, 8, requires_grad=True) for _ in range(5))
+    for given in (dict(gate_pre=torch.empty(8, 8), up_pre=torch.empty(8, 8)), dict(out=torch.empty(8, 8)),
+                  dict(out=torch.empty(8, 8), gate_pre=torch.empty(8, 8), up_pre=torch.empty(8, 8))):
+        seen.clear()
+        y = fe.fe_gated_ffn(t, x, wg, wu, wd, residual=r, **given)
+        assert not y.requires_grad, list(given)
+        assert [name for name, _ in seen] == ["fe_gated_ffn", "fe_project"]
+        assert not seen[1][1][0].requires_grad, list(given)  # (h)
+    assert fe.fe_gated_ffn(t, x, wg, wu, wd, residual=r).requires_grad
+
+
 def test_row_strides(fe):
     from paper_2509_20416_gb300.layer import _row
     x = torch.zeros(4, 6, 10)
