@@ -7,11 +7,11 @@ handle's type (fe_token_logprobs: float32 or bfloat16 logits, whatever the handl
 with contiguous columns and rows one stride apart, such as column slices of a fused projection.
 `stream` (a torch stream or a raw handle) is where a call runs, the current stream unless given;
 ordering it with others is the caller's. Where autograd records and neither outputs nor a stream
-are given, the results are differentiable (once); the _backward functions are the same gradients
-as plain calls, for a captured step or a training loop of one's own. (PyTorch's engine joins the
-streams of a leaf's graphs: a backward pass is captured while no eager graph of the same leaves lives,
-or with the _backward functions.) Workspaces are allocated for each call, so that calls and captured
-graphs do not share them.
+are given, the results are differentiable (once); outputs given carry no graph, and count as changed in
+place. The _backward functions are the same gradients as plain calls, for a captured step or a training
+loop of one's own. (PyTorch's engine joins the streams of a leaf's graphs: a backward pass is captured
+while no eager graph of the same leaves lives, or with the _backward functions.) Workspaces are
+allocated for each call, so that calls and captured graphs do not share them.
 """
 from __future__ import annotations
 
@@ -22,7 +22,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import _check, _lib, _stream, _vp, FE_BF16, FE_F32
-from .target import Target, _empty, _raw_stream, _side
+from .target import Target, _empty, _raw_stream, _side, _written
 
 _ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 _M = "Pq"  # fe_mat
@@ -182,10 +182,12 @@ def fe_project(t: Target, x, w, bias=None, act: str = "none", residual=None, out
     side, shape, M = _side(stream), _shaped(x, N), _rows_of(x)
     args = (M, N, K, *_mat(x, t.dtype, _shaped(x, K)), *_mat(w, t.dtype, (N, K)), _vec(bias, t.dtype, N),
             *_mat(residual, t.dtype, shape))
+    given = out, pre
     out = _out(out, shape, x, side)
     args += (*_mat(out, t.dtype, shape), *_mat(pre, torch.float32, shape), _act(act))
     if M:
         _call("fe_project", t, side, (x, w, bias, residual, out, pre), args)
+    _written(*given)
     return out
 
 
@@ -259,10 +261,12 @@ def fe_gated_ffn(t: Target, x, w_gate, w_up, w_down=None, act: str = "silu", res
     F, K = w_gate.shape
     side, shape, M = _side(stream), _shaped(x, F), _rows_of(x)
     args = (M, F, K, *_mat(x, t.dtype, _shaped(x, K)), *_mat(w_gate, t.dtype, (F, K)), *_mat(w_up, t.dtype, (F, K)))
+    given = out, gate_pre, up_pre
     out = _out(out, shape, x, side)
     args += (*_mat(out, t.dtype, shape), *_mat(gate_pre, torch.float32, shape), *_mat(up_pre, torch.float32, shape), _act(act))
     if M:
         _call("fe_gated_ffn", t, side, (x, w_gate, w_up, out, gate_pre, up_pre), args)
+    _written(*given)
     return out
 
 
@@ -337,12 +341,13 @@ def fe_block_norm(t: Target, x, z=None, post: bool | None = None, post_weight=No
     if y is None and n is None and _recorded(stream) and _wants(x, z, post_weight, gate, pre_weight):
         out = _BlockNorm.apply(t, opts, pre, x, z, post_weight, gate, pre_weight)
         return (x, out) if z is None else out if pre else (out, None)
-    side = _side(stream)
+    side, given = _side(stream), (y, n)
     y = None if y is None and z is None else _out(y, shape, x, side)
     n = _out(n, shape, x, side) if pre else None
     args = _norm_args(t, opts, x, z, post_weight, gate, pre_weight) + (*_mat(y, t.dtype, shape), *_mat(n, t.dtype, shape))
     if R:
         _call("fe_block_norm", t, side, (x, z, post_weight, gate, pre_weight, y, n), args)
+    _written(*given)
     return x if y is None else y, n
 
 
@@ -474,6 +479,7 @@ def fe_token_logprobs(t: Target, logits, tokens=None, top: int = 0, temperature:
             p(entropy), p(lse), p(stats), p(ids), p(lps))
     if R:
         _call("fe_token_logprobs", t, side, (logits, tok, logprob, entropy, lse, stats, ids, lps), args)
+    _written(stats)
     return logprob, entropy, lse, ids, lps
 
 
@@ -502,6 +508,7 @@ def fe_token_logprobs_backward(t: Target, logits, stats, tokens=None, dlogprob=N
     given = (flat(stats, lead + (2,)), flat(entropy, lead), flat(dlogprob, None if tokens is None else tokens.shape), flat(dentropy, lead),
              flat(dlse, lead), flat(dtop_logprob, lead + (K,)))
     top_id = flat(top_id, lead + (K,), torch.int32)
+    out = dlogits
     dlogits = _out(dlogits, logits.shape, logits, side)
     p = lambda x: 0 if x is None else x.data_ptr()
     R = _rows_of(logits)
@@ -509,6 +516,7 @@ def fe_token_logprobs_backward(t: Target, logits, stats, tokens=None, dlogprob=N
             *(p(x) for x in given), *_mat(dlogits, logits.dtype, logits.shape))
     if R:
         _call("fe_token_logprobs_backward", t, side, (logits, tok, top_id, *given, dlogits), args)
+    _written(out)
     return dlogits
 
 

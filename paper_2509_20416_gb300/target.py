@@ -6,7 +6,8 @@ keys, values, outputs) are CUDA tensors [B, T, heads, head_dim] of the handle's 
 strides whose innermost dimension is contiguous, such as views of a fused projection; integer
 inputs are contiguous CUDA int32 tensors. `stream` (a torch stream or a raw handle) is where a call
 runs, the current stream unless given; ordering it with others is the caller's. fe_rope takes part
-in autograd; the results of the cache and the attention over it, which serve, carry no graph.
+in autograd; the results of the cache and the attention over it, which serve, carry no graph. Outputs
+given count as changed in place.
 """
 from __future__ import annotations
 
@@ -230,6 +231,14 @@ def _empty(shape, dtype, device, side):
     return x
 
 
+def _written(*outputs) -> None:
+    """Tell autograd of outputs that the caller gave (None: not given): a graph that has saved one of them then refuses
+    to go back with the new values, as after PyTorch's own in-place operations."""
+    for x in outputs:
+        if x is not None and not x.is_inference():
+            torch.autograd.graph.increment_version(x)
+
+
 def _call(name: str, t: Target, side, tensors, *args) -> None:
     """Pack the arguments and call the library, on the current stream or on `side`: there, the
     allocator is told that `tensors` are in use."""
@@ -254,7 +263,7 @@ def fe_rope(t: Target, q, k, pos, backward: bool = False, q_out=None, k_out=None
             and any(x is not None and x.requires_grad for x in (q, k)):
         return _Rotation.apply(t, pos, backward, q, k)
     B, T = pos.shape
-    side = _side(stream)
+    side, given = _side(stream), (q_out, k_out)
     qr = kr = qo = ko = _NONE
     if q is not None:
         shape = (B, T, t.H, t.hd)
@@ -268,6 +277,7 @@ def fe_rope(t: Target, q, k, pos, backward: bool = False, q_out=None, k_out=None
         ko = _rows(t, k_out, shape)
     _call("fe_rope", t, side, lambda: (q, k, q_out, k_out, pos), B, T, *qr, *kr, *qo, *ko, _ints(pos, (B, T)),
           1 if backward else 0)
+    _written(*given)
     return q_out, k_out
 
 
@@ -297,7 +307,7 @@ def fe_cache_write(t: Target, cache: Cache, layer: int, k, v, start, n_rows=None
     queries into q_out, which is returned."""
     B, T = k.shape[:2]
     shape = (B, T, t.Hkv, t.hd)
-    side = _side(stream)
+    side, given = _side(stream), q_out
     qr = qo = _NONE
     if q is not None:
         qshape = (B, T, t.H, t.hd)
@@ -307,6 +317,7 @@ def fe_cache_write(t: Target, cache: Cache, layer: int, k, v, start, n_rows=None
     _call("fe_cache_write", t, side, lambda: (k, v, start, n_rows, pos, q, q_out, *cache.tensors()), B, T,
           *_rows(t, k, shape), *_rows(t, v, shape), *qr, *qo, _ints(pos, (B, T)), _ints(start, (B,)), _ints(n_rows, (B,)),
           *cache._layer(layer, B))
+    _written(given)
     return q_out
 
 
@@ -315,12 +326,13 @@ def fe_cache_read(t: Target, cache: Cache, layer: int, start, n_rows, L: int, k_
     """Slots start[b] .. start[b] + n_rows[b] - 1 of a layer's cache as rows k, v [B, L, Hkv, hd]
     of the handle's type; rows past n_rows[b] are zero."""
     B = start.shape[0]
-    side = _side(stream)
+    side, given = _side(stream), (k_out, v_out)
     shape = (B, L, t.Hkv, t.hd)
     k_out = _empty(shape, t.dtype, start.device, side) if k_out is None else k_out
     v_out = _empty(shape, t.dtype, start.device, side) if v_out is None else v_out
     _call("fe_cache_read", t, side, lambda: (start, n_rows, k_out, v_out, *cache.tensors()), B, L, _ints(start, (B,)),
           _ints(n_rows, (B,)), *cache._layer(layer, B), *_rows(t, k_out, shape), *_rows(t, v_out, shape))
+    _written(*given)
     return k_out, v_out
 
 
@@ -333,7 +345,7 @@ def fe_tree_attention(t: Target, cache: Cache, layer: int, q, prefix_len, mask=N
     B, T = q.shape[:2]
     shape = (B, T, t.H, t.hd)
     qr = _rows(t, q, shape)
-    side = _side(stream)
+    side, given = _side(stream), (out, lse)
     if out is None:
         out = _empty(shape, t.dtype, q.device, side)
     if lse is None:
@@ -346,6 +358,7 @@ def fe_tree_attention(t: Target, cache: Cache, layer: int, q, prefix_len, mask=N
     _call("fe_tree_attention", t, side, lambda: (q, prefix_len, n_nodes, mask, out, lse, *cache.tensors()), B, T, *qr,
           *_rows(t, out, shape), lse.data_ptr(), _ints(prefix_len, (B,)), _ints(n_nodes, (B,)),
           0 if mask is None else mask.data_ptr(), t.scale if scale is None else float(scale), *cache._layer(layer, B))
+    _written(*given)
     return out, lse
 
 

@@ -91,3 +91,26 @@ def test_weight_gradient_of_the_most_rows(fe, handles):  # noqa: F811
     ref.check(dw, (q.v, q.err + 2.0 ** -8 * (q.v.abs() + q.err)), "dw")
     del dout, x
     torch.cuda.empty_cache()
+
+
+def test_saved_tensors_that_are_overwritten(fe, handles):  # noqa: F811
+    """A graph whose saved tensor has been taken as an output refuses to go back, as it does after PyTorch's own
+    in-place operations."""
+    t, g = handles["f32"], gen(11)
+    x, z, w = normal(g, "f32", 12, 64), normal(g, "f32", 12, 64), normal(g, "f32", 64, 64)
+    leaf = w.detach().requires_grad_()
+    for write in (lambda s: fe.fe_project(t, x, w, out=s), lambda s: fe.fe_project(t, x, w, pre=s), lambda s: fe.fe_block_norm(t, x, z, y=s),
+                  lambda s: fe.fe_block_norm(t, x, z, n=s), lambda s: fe.fe_gated_ffn(t, x, w, w, gate_pre=s, up_pre=torch.empty_like(s)),
+                  lambda s: fe.fe_gated_ffn(t, x, w, w, w, out=s),
+                  lambda s: fe.fe_token_logprobs_backward(t, x, torch.zeros(12, 2, device="cuda"), dlogits=s)):
+        s = z.clone()
+        for y in (s @ leaf.T, fe.fe_project(t, s, leaf)):
+            write(s)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                y.sum().backward()
+        y = fe.fe_project(t, s, leaf)  # (saved as it is now)
+        torch.autograd.grad([y], [leaf], [x])
+    stats = torch.empty(12, 2, device="cuda")
+    before = stats._version
+    fe.fe_token_logprobs(t, x, stats=stats)
+    assert stats._version > before

@@ -322,6 +322,41 @@ def test_a_block_with_outputs_given_is_not_recorded_in_part(fe, monkeypatch):
     assert fe.fe_gated_ffn(t, x, wg, wu, wd, residual=r).requires_grad
 
 
+def test_outputs_given_count_as_changed(fe, monkeypatch):
+    """Autograd learns of what the kernels write into a caller's tensors, by their versions."""
+    from paper_2509_20416_gb300 import layer, target
+    monkeypatch.setattr(layer, "_mat", lambda x, dtype, shape: (0, 0))
+    monkeypatch.setattr(layer, "_call", lambda name, t, side, tensors, args: None)
+    for f in ("_rows", "_ints"):
+        monkeypatch.setattr(target, f, lambda *a: (0, 0, 0, 0) if len(a) == 3 else 0)
+    monkeypatch.setattr(target, "_call", lambda *a: None)
+    t = fe.Target(0, dict(n_heads=1, n_kv_heads=1, head_dim=8, max_seq=16, dtype="f32", rope_theta=1e4))
+    x, w = torch.zeros(8, 8), torch.zeros(8, 8)
+    q, pos = torch.zeros(2, 4, 1, 8), torch.zeros(2, 4, dtype=torch.int32)
+
+    class Flat:  # (a cache)
+        def _layer(self, i, B):
+            return ()
+    new = lambda like=x: torch.zeros_like(like)
+    calls = [lambda a, b: fe.fe_project(t, x, w, out=a, pre=b), lambda a, b: fe.fe_gated_ffn(t, x, w, w, gate_pre=a, up_pre=b),
+             lambda a, b: (fe.fe_gated_ffn(t, x, w, w, w, out=a), fe.fe_gated_ffn(t, x, w, w, out=b)),
+             lambda a, b: fe.fe_block_norm(t, a, x, y=a, n=b)]
+    for i, call in enumerate(calls):
+        a, b = new(), new()
+        call(a, b)
+        assert a._version > 0 and b._version > 0, i
+    assert x._version == 0 and w._version == 0
+    for i, call in enumerate([lambda a, b: fe.fe_rope(t, a, b, pos, q_out=a, k_out=b),
+                              lambda a, b: (fe.fe_cache_write(t, Flat(), 0, q, q, pos[:, 0], q=q, q_out=a), fe.fe_rope(t, b, None, pos, q_out=b)),
+                              lambda a, b: fe.fe_cache_read(t, Flat(), 0, pos[:, 0], None, 4, a, b)]):
+        a, b = new(q), new(q)
+        call(a, b)
+        assert a._version > 0 and b._version > 0, i
+    with torch.inference_mode():
+        y = torch.zeros(8, 8)
+    fe.fe_project(t, x, w, out=y)  # (has no version)
+
+
 def test_row_strides(fe):
     from paper_2509_20416_gb300.layer import _row
     x = torch.zeros(4, 6, 10)
