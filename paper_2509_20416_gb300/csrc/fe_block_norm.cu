@@ -865,7 +865,7 @@ int back_kernel(NormForm f, int threads) {
     while (kBack[i].room < threads) ++i;
     return i;
 }
-// CTAs of each that fit an SM, as the device says when a handle is made
+// CTAs of each that fit an SM, as the device says when a handle's first gradient is prepared
 std::atomic<int> back_fit[2][kBacks];
 int64_t row_vecs(int d, fe_dtype dtype) { return dtype == FE_F32 ? ((int64_t)d + 3) / 4 : ((int64_t)d + 7) / 8; }
 
@@ -935,16 +935,17 @@ cudaError_t prepare_backward() {
     return e;
 }
 
+template <typename T>
+cudaError_t prepare_forward() {
+    cudaError_t e = prepare<T, ANY>();
+    if (e == cudaSuccess) e = prepare<T, WHOLE>();
+    return e == cudaSuccess ? prepare<T, ALL_GIVEN>() : e;
+}
+
 }  // namespace
 
-cudaError_t norm_prepare() {
-    cudaError_t e;
-    if ((e = prepare<float, ANY>()) != cudaSuccess || (e = prepare<float, WHOLE>()) != cudaSuccess) return e;
-    if ((e = prepare<float, ALL_GIVEN>()) != cudaSuccess || (e = prepare<bf16_t, ANY>()) != cudaSuccess) return e;
-    if ((e = prepare<bf16_t, WHOLE>()) != cudaSuccess || (e = prepare<bf16_t, ALL_GIVEN>()) != cudaSuccess) return e;
-    if ((e = prepare_backward<float>()) != cudaSuccess) return e;
-    return prepare_backward<bf16_t>();
-}
+cudaError_t norm_prepare(fe_dtype dtype) { return dtype == FE_F32 ? prepare_forward<float>() : prepare_forward<bf16_t>(); }
+cudaError_t norm_backward_prepare(fe_dtype dtype) { return dtype == FE_F32 ? prepare_backward<float>() : prepare_backward<bf16_t>(); }
 
 int64_t norm_backward_plan(NormArgs& a, fe_dtype dtype, int num_sms) {
     const int64_t nv = row_vecs(a.d, dtype);

@@ -111,8 +111,11 @@ fe_status gemm(const fe_target* t, GemmArgs& g, Workspace& w, bool count, cudaSt
             s = g.b_t ? readable(g.b[i], g.K, g.N) : readable(g.b[i], g.N, g.K);
         if (s != FE_OK) return s;
     }
-    if (!count) FE_TRY(gemm_few_takes(g) ? launch_gemm_few(g, t->num_sms, st) : launch_gemm_tc(g, t->num_sms, st));
-    return FE_OK;
+    if (count) return FE_OK;
+    const bool few = gemm_few_takes(g);
+    const fe_status s = few ? set_up(t, GEMM_FEW, gemm_few_prepare) : set_up(t, GEMM_TC, gemm_tc_prepare);
+    if (s == FE_OK) FE_TRY(few ? launch_gemm_few(g, t->num_sms, st) : launch_gemm_tc(g, t->num_sms, st));
+    return s;
 }
 
 fe_status project(const fe_target* t, const fe_project_args* a, Workspace& w, bool count, cudaStream_t st) {
@@ -361,6 +364,9 @@ fe_status norm_backward(const fe_target* t, const fe_block_norm_backward_args* a
     n.dgate = a->dgate;
     n.vec = on16(n.x, es) && on16(n.z, es) && on16(n.gate, es) && on16(n.post_w) && on16(n.pre_w) && on16(n.dy, es) &&
             on16(n.dn, es) && on16(n.dx, es) && on16(n.dz, es) && on16(n.dgate, es);
+    // (where there is no GPU the work can be counted all the same)
+    const fe_status s = set_up(t, NORM_BACKWARD, [&] { return norm_backward_prepare(dt); });
+    if (s != FE_OK && !count) return s;
     const int64_t workers = norm_backward_plan(n, dt, t->num_sms), bytes = workers * a->d * (int64_t)sizeof(float);
     if (a->dpre_w) n.part_pre = (float*)w.take(bytes);
     if (a->dpost_w) n.part_post = (float*)w.take(bytes);
@@ -454,6 +460,8 @@ fe_status fe_block_norm(fe_target* t, const fe_block_norm_args* a, void* stream)
     n.y = a->y;
     n.n = a->n;
     n.vec = on16(n.x, es) && on16(n.z, es) && on16(n.gate, es) && on16(n.post_w) && on16(n.pre_w) && on16(n.y, es) && on16(n.n, es);
+    const fe_status s = set_up(t, NORM, [&] { return norm_prepare(t->cfg.dtype); });
+    if (s != FE_OK) return s;
     FE_TRY(launch_block_norm(n, t->cfg.dtype, t->num_sms, (cudaStream_t)stream));
     return FE_OK;
 }
@@ -478,6 +486,8 @@ fe_status fe_token_logprobs(fe_target* t, const fe_token_logprobs_args* a, void*
     r.stats = a->stats;
     r.top_id = a->top_id;
     r.top_logprob = a->top_logprob;
+    const fe_status s = set_up(t, a->dtype == FE_F32 ? LOGPROBS_F32 : LOGPROBS_BF16, [&] { return logprobs_prepare(a->dtype); });
+    if (s != FE_OK) return s;
     FE_TRY(launch_token_logprobs(r, a->dtype, t->num_sms, (cudaStream_t)stream));
     return FE_OK;
 }

@@ -109,13 +109,15 @@ struct SumJobs {
     }
 };
 cudaError_t launch_sum_parts(const SumJobs& a, fe_dtype dtype, cudaStream_t st);
-cudaError_t norm_prepare();
+cudaError_t norm_prepare(fe_dtype dtype);
 cudaError_t launch_block_norm(const NormArgs& a, fe_dtype dtype, int num_sms, cudaStream_t st);
-// fills in how the rows are divided, and returns the number of workers: rows of part_post and part_pre
+// fills in how the rows are divided (by what norm_backward_prepare has asked of the device, or a guess where there is
+// none), and returns the number of workers: rows of part_post and part_pre
 int64_t norm_backward_plan(NormArgs& a, fe_dtype dtype, int num_sms);
+cudaError_t norm_backward_prepare(fe_dtype dtype);
 cudaError_t launch_block_norm_backward(const NormArgs& a, fe_dtype dtype, cudaStream_t st);
 cudaError_t launch_token_logprobs(const LogprobArgs& a, fe_dtype dtype, int num_sms, cudaStream_t st);
 cudaError_t launch_token_logprobs_backward(const LogprobArgs& a, fe_dtype dtype, int num_sms, cudaStream_t st);
-cudaError_t logprobs_prepare();
+cudaError_t logprobs_prepare(fe_dtype dtype);
 
 }  // namespace fe

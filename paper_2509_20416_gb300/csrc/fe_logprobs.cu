@@ -614,15 +614,17 @@ cudaError_t launch_token_logprobs_backward(const LogprobArgs& a, fe_dtype dtype,
     return dtype == FE_F32 ? backward<float>(a, num_sms, st) : backward<bf16_t>(a, num_sms, st);
 }
 
-cudaError_t logprobs_prepare() {
-    cudaError_t e;
+cudaError_t logprobs_prepare(fe_dtype dtype) {
     const auto wide = [](auto kern) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         return e != cudaSuccess ? e : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kLpSlices * kLpSlice * sizeof(uint4)));
     };
-    if ((e = wide(logprob_kernel<float, true>)) != cudaSuccess || (e = wide(logprob_kernel<float, false>)) != cudaSuccess) return e;
-    if ((e = wide(logprob_kernel<bf16_t, true>)) != cudaSuccess) return e;
-    return wide(logprob_kernel<bf16_t, false>);
+    const auto both = [&](auto a, auto b) {
+        const cudaError_t e = wide(a);
+        return e != cudaSuccess ? e : wide(b);
+    };
+    return dtype == FE_F32 ? both(logprob_kernel<float, true>, logprob_kernel<float, false>)
+                           : both(logprob_kernel<bf16_t, true>, logprob_kernel<bf16_t, false>);
 }
 
 }  // namespace fe

@@ -6,7 +6,6 @@
 #include <new>
 #include <vector>
 
-#include "fe_layer_kernels.h"
 #include "fe_target_handle.h"
 
 #define FE_SOURCE "fe_target.cu"
@@ -90,10 +89,6 @@ fe_status build(fe_target* t, cudaStream_t st) {
     FE_TRY(cudaGetDevice(&t->device));
     FE_TRY(cudaDeviceGetAttribute(&t->num_sms, cudaDevAttrMultiProcessorCount, t->device));
     FE_TRY(tree_attn_prepare());
-    FE_TRY(gemm_tc_prepare());
-    FE_TRY(gemm_few_prepare());
-    FE_TRY(norm_prepare());
-    FE_TRY(logprobs_prepare());
     const int pairs = c.rope_dim / 2;
     const size_t rows = (size_t)t->num_sms * 2 * kAttnItemRows;
     FE_TRY(cudaMalloc((void**)&t->rope, (size_t)c.max_seq * pairs * sizeof(float2)));

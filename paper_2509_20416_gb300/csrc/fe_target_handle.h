@@ -3,6 +3,8 @@
 
 #include <stdio.h>
 
+#include <atomic>
+
 #include "fe_target_kernels.h"
 
 struct fe_target {
@@ -12,6 +14,7 @@ struct fe_target {
     float *part_o = nullptr, *part_ml = nullptr;
     int* status = nullptr;
     fe::SplitDesc* split = nullptr;
+    mutable std::atomic<unsigned> ready{0};  // kernels of the dense operators that are set up (fe::Kernels)
 };
 
 namespace fe {
@@ -39,6 +42,20 @@ inline fe_status check_device(const fe_target* t) {
     snprintf(buf, sizeof(buf), "the current CUDA device (%d) is not the handle's device (%d)", dev, t->device);
     set_error_detail(buf);
     return FE_ERR_INVALID_ARG;
+}
+
+// What the dense operators need of the device before their kernels run (shared memory above 48 KB, large clusters, how
+// many CTAs fit) is asked for when a handle first uses them: it loads some hundred kernels, 17 ms in a process, which a
+// handle that only rotates and attends need not pay. Twice, from two threads, does no harm.
+enum Kernels : unsigned { GEMM_TC = 1, GEMM_FEW = 2, NORM = 4, NORM_BACKWARD = 8, LOGPROBS_F32 = 16, LOGPROBS_BF16 = 32 };
+template <typename F>
+fe_status set_up(const fe_target* t, Kernels which, const F& prepare) {
+    if (t->ready.load(std::memory_order_acquire) & which) return FE_OK;
+    int dev = -1;
+    FE_TRY(cudaGetDevice(&dev));
+    FE_TRY(prepare());
+    if (dev == t->device) t->ready.fetch_or(which, std::memory_order_release);
+    return FE_OK;
 }
 #undef FE_SOURCE
 

@@ -1,5 +1,9 @@
 """Calls of the dense operators that programs may make at the edge of what include/fe_layer.h and the binding
 allow."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -114,3 +118,63 @@ def test_saved_tensors_that_are_overwritten(fe, handles):  # noqa: F811
     before = stats._version
     fe.fe_token_logprobs(t, x, stats=stats)
     assert stats._version > before
+
+
+FIRST_CALLS = """
+import ctypes, sys
+import torch
+import paper_2509_20416_gb300 as fe
+
+class Handle(ctypes.Structure):  # the start of the library's handle
+    _fields_ = [("cfg", fe.target.fe_target_config), ("device", ctypes.c_int), ("num_sms", ctypes.c_int), ("buffers", ctypes.c_void_p * 5),
+                ("ready", ctypes.c_uint)]
+ready = lambda: Handle.from_address(t.ptr).ready
+dtype = sys.argv[1]
+T = dict(f32=torch.float32, bf16=torch.bfloat16)[dtype]
+t = fe.fe_target_init(dict(n_heads=2, n_kv_heads=1, head_dim=64, max_seq=16, dtype=dtype, rope_theta=1e4))
+g = torch.Generator(device="cuda").manual_seed(1)
+n = lambda *s: torch.randn(s, generator=g, device="cuda").to(T)
+pos = torch.zeros(1, 4, dtype=torch.int32, device="cuda")
+fe.fe_rope(t, n(1, 4, 2, 64), None, pos)
+assert ready() == 0  # (rotating and attending need none of the dense operators' kernels)
+x, w, z, v, do = n(200, 640), n(640, 640) / 25, n(200, 640), n(640), n(200, 640)
+logits, tok = n(200, 33000), torch.zeros(200, 1, dtype=torch.int32, device="cuda")
+
+def step():
+    y, u = fe.fe_block_norm(t, x, z, post_weight=v, pre_weight=v)
+    out = fe.fe_project(t, u, w, residual=y)
+    one = fe.fe_gated_ffn(t, u[:3], w, w)
+    stats = torch.empty(200, 2, device="cuda")
+    lp = fe.fe_token_logprobs(t, logits, tok, top=3, stats=stats)
+    back = fe.fe_token_logprobs_backward(t, logits, stats, tok, torch.ones_like(lp[0]))
+    return [y, u, out, one, *lp, back, *fe.fe_project_backward(t, do, u, w, dbias=True),
+            *[r for r in fe.fe_block_norm_backward(t, x, z, None, v, pre_weight=v, dy=do, dn=do) if r is not None]]
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):  # the first calls of the process
+    got = step()
+assert ready() != 0
+for r in got:
+    r.zero_()
+graph.replay()
+want = step()
+torch.cuda.synchronize()
+assert fe.fe_target_status(t) == fe.FE_OK
+for i, (a, b) in enumerate(zip(got, want)):
+    assert torch.equal(a, b), i
+other = fe.fe_target_init(dict(n_heads=1, n_kv_heads=1, head_dim=64, max_seq=16, dtype=dtype, rope_theta=1e4))
+assert torch.equal(fe.fe_project(other, u := want[1], w, residual=want[0]), want[2])
+print("first calls captured")
+"""
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_first_calls_of_a_process(tmp_path, dtype):
+    """A handle sets up the dense operators' kernels when they are first used, and that may be while a graph is
+    captured."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    script = tmp_path / "first_calls.py"
+    script.write_text(FIRST_CALLS)
+    r = subprocess.run([sys.executable, str(script), dtype], cwd=root, env=dict(os.environ, PYTHONPATH=root), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "first calls captured" in r.stdout, r.stdout + r.stderr
