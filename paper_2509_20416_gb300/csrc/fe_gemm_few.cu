@@ -10,6 +10,7 @@
 // as tiles of 256 rows), 71 rows through 28672 x 8192 151 us (92 %), 49 rows to 128256 172 us (91 %), one token
 // through 6144 x 4096 13.4 us, where a CTA's start, its first copies and the join are half. The first copies
 // go out before tensor memory is allocated.
+#include "fe_gemm_plan.h"
 #include "fe_gemm_tc.cuh"
 #include "fe_tensor_map.h"
 
@@ -17,12 +18,7 @@ namespace fe {
 
 namespace {
 
-constexpr int kFewThreads = 128, kFewRows = 128, kFewStages = 12, kFewMost = 8;
-constexpr int kPartRow = kFewRows + 4;  // floats of a token's sums in shared memory
-
-struct FewArgs {
-    int nt, stages, stage_bytes, ranks;
-};
+constexpr int kFewThreads = 128;
 
 struct FewBarriers {
     uint64_t full[kFewStages], empty[kFewStages], done;
@@ -167,8 +163,6 @@ __global__ void __launch_bounds__(kFewThreads)
     if (f.ranks > 1) cluster_sync_all();  // (the others have read this CTA's sums)
 }
 
-constexpr int kFewSmem = 224 * 1024;  // of an SM, for its CTAs' rings
-
 }  // namespace
 
 cudaError_t gemm_few_prepare() {
@@ -181,31 +175,10 @@ bool gemm_few_takes(const GemmArgs& g) {
 
 cudaError_t launch_gemm_few(const GemmArgs& g, int num_sms, cudaStream_t st) {
     const bool gated = g.e.kind == FINISH_GATED;
-    const int rows = gated ? 64 : 128, slices = (g.K + 63) / 64;
+    const int rows = gated ? 64 : 128;
     const int64_t blocks = ((int64_t)g.N + rows - 1) / rows;
-    FewArgs f{};
-    f.nt = (int)(g.M + 15) / 16 * 16;
-    // How many CTAs share a block: the busiest SM's CTAs, each with its slices and some four slices' time
-    // for its start and the join
-    int64_t best = 0;
-    for (int r = 1; r <= kFewMost && r <= slices; r *= 2) {
-        const int64_t per = (blocks * r + num_sms - 1) / num_sms, cost = per * ((slices + r - 1) / r + 4);
-        if (!best || cost < best) {
-            best = cost;
-            f.ranks = r;
-        }
-    }
-    f.stage_bytes = 16384 + (f.nt * 128 + 1023) / 1024 * 1024;
-    // the rings of the CTAs that an SM holds at once, up to four, share its memory
-    const int64_t per = (blocks * f.ranks + num_sms - 1) / num_sms;
-    const int held = per < 4 ? (int)per : 4, mine = (slices + f.ranks - 1) / f.ranks;
-    const int part = (int)g.M * kPartRow * 4;
-    f.stages = (kFewSmem / held - 4096) / f.stage_bytes;
-    if (f.stages > kFewStages) f.stages = kFewStages;
-    if (f.stages > mine) f.stages = mine;
-    if (f.stages < 2) f.stages = 2;
-    int smem = f.stages * f.stage_bytes;
-    smem = (smem > part ? smem : part) + 1024;
+    int smem = 0;
+    const FewArgs f = few_plan(g.M, g.N, g.K, gated, num_sms, &smem);
     CUtensorMap w0, w1, x;
     const auto map = [](CUtensorMap* m, const fe_mat& a, int64_t r, int64_t c, int box_rows) { return tensor_map_bf16(m, a, r, c, box_rows); };
     if (!map(&w0, g.b[0], g.N, g.K, rows) || !map(&w1, g.b[gated ? 1 : 0], g.N, g.K, rows) || !map(&x, g.a[0], g.M, g.K, f.nt)) return cudaErrorInvalidValue;

@@ -10,6 +10,7 @@
 //
 // Bound by issue and shared memory: 4096 cubed 2.5 ms (55 TFLOP/s, 70 % of the float32 units), 331 x 688 x 257 15 us
 // (41 us without clusters). At most 8 rows: one row to 6144 of 4096 16 us (92 % of the copy rate).
+#include "fe_gemm_plan.h"
 #include "fe_gemm_tc.cuh"
 
 namespace fe {
@@ -341,10 +342,8 @@ cudaError_t launch_tile(const GemmArgs& g, int num_sms, cudaStream_t st) {
 
 template <typename T, bool AT, bool BT>
 cudaError_t launch_layout(const GemmArgs& g, int num_sms, cudaStream_t st) {
-    const int64_t big = ((g.M + 127) / 128) * ((g.N + (g.e.kind == FINISH_GATED ? 63 : 127)) / (g.e.kind == FINISH_GATED ? 64 : 128)) * (g.twice ? 2 : 1);
-    // too few large tiles to occupy the GPU: a quarter of the size
-    if (big < num_sms || g.M <= 64) return launch_tile<T, 64, 64, AT, BT>(g, num_sms, st);
-    return launch_tile<T, 128, 128, AT, BT>(g, num_sms, st);
+    if (simt_large(g.M, g.N, g.e.kind == FINISH_GATED, g.twice, num_sms)) return launch_tile<T, 128, 128, AT, BT>(g, num_sms, st);
+    return launch_tile<T, 64, 64, AT, BT>(g, num_sms, st);
 }
 
 }  // namespace

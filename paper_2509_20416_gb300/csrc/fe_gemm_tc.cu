@@ -13,8 +13,9 @@
 // (1990 TFLOP/s), 523 with both products stored; the gradients' products 1650 to 1910 TFLOP/s. Long steps are bound by
 // the card's power (1550 TFLOP/s over a block's forward and backward pass). Five slices in flight instead of six cost 4 %.
 //
-// BN is the width whose rounds of tiles over the pairs are shortest: 16 x 16 tiles of 256 take 76 pairs 4
+// BN is the width whose rounds of tiles over the pairs are shortest (fe_gemm_plan.h): 16 x 16 tiles of 256 take 76 pairs 4
 // rounds where 3.4 would hold them, 16 x 19 of 224 take 4 rounds of 7/8.
+#include "fe_gemm_plan.h"
 #include "fe_gemm_tc.cuh"
 #include "fe_tensor_map.h"
 
@@ -22,25 +23,15 @@ namespace fe {
 
 namespace {
 
-constexpr int kFinishWarps = 8;
 constexpr int kTcThreads = 64 + 32 * kFinishWarps;
-constexpr int kTileM = 256, kSliceK = 64;
 
 // How long a finishing warp waits for a tile, besides what any wait gets: a weight's gradient sums up to 2^24 slices
 // in one tile, at 230 ns each where a pair works alone, 750 where the copies of all pairs come from memory.
 constexpr int64_t kSliceBudgetNs = 2000;
 
-constexpr int kSliceA = 128 * kSliceK * 2;
 constexpr int kStaging = kFinishWarps * 4096;  // a warp's 32 x 32 floats
-constexpr int kTcRing = 192 * 1024, kTcStages = 8;
-constexpr int kPairs = kFinishWarps * 8192;  // of the ring, for a gated gradient's products on their way
 constexpr int kTcSmem = kTcRing + kStaging + 1024 /* alignment */ + 512;
 static_assert(kTcSmem <= 227 * 1024, "shared memory of a CTA");
-
-// the tile's width and what follows from it
-struct TcWidth {
-    int bn, b_bytes, stages;  // B's bytes of a slice in a CTA, slices in flight
-};
 
 struct TcBarriers {
     uint64_t full[kTcStages], empty[kTcStages], done[2], free[2], drain;
@@ -424,26 +415,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
 template <bool AT, bool BT>
 cudaError_t launch_tiles(const GemmArgs& g, int num_sms, cudaStream_t st) {
     const bool gated = g.e.kind == FINISH_GATED;
-    const int64_t mt = (g.M + kTileM - 1) / kTileM * (g.twice ? 2 : 1), pairs = num_sms / 2;
-    const auto tiles = [&](int bn) { return mt * ((g.N + (gated ? bn / 2 : bn) - 1) / (gated ? bn / 2 : bn)); };
-    // The width: rounds of tiles, each of its columns' time, or of its copies' where that is more (a column's products
-    // of a slice take as long as the copy of 134 bytes), and of some 16 columns' for its start. B by its summed
-    // index comes in whole groups of 64 columns: there a width of 160 (5120 x 5120 from 4093 rows, 9 rounds)
-    // took 174 us and 256 (6 rounds) 128 us.
-    TcWidth shape{};
-    int64_t best = 0;
-    for (int w = 256; w >= 128; w -= 32) {
-        const int b_bytes = BT ? (w / 2 + 63) / 64 * 8192 : w / 2 * 128, copies = (kSliceA + b_bytes) / 134;
-        const int64_t cost = (tiles(w) + pairs - 1) / pairs * ((w > copies ? w : copies) + 16);
-        if (!best || cost < best) {
-            best = cost;
-            shape.bn = w;
-            shape.b_bytes = b_bytes;
-        }
-    }
+    const TcWidth shape = tc_width(g.M, g.N, gated, g.twice, g.e.kind == FINISH_GATED_GRAD, BT, num_sms);
     const int bn = shape.bn;
-    shape.stages = (kTcRing - (g.e.kind == FINISH_GATED_GRAD ? kPairs : 0)) / (kSliceA + shape.b_bytes);
-    if (shape.stages > kTcStages) shape.stages = kTcStages;
     TcMaps maps{};
     for (int i = 0; i < 2; ++i) {
         if (i == 0 || g.segs == 2 || g.twice) {
@@ -453,7 +426,7 @@ cudaError_t launch_tiles(const GemmArgs& g, int num_sms, cudaStream_t st) {
             if (!(BT ? tensor_map_bf16(&maps.b[i], g.b[i], g.K, g.N, 64) : tensor_map_bf16(&maps.b[i], g.b[i], g.N, g.K, bn / 2))) return cudaErrorInvalidValue;
         }
     }
-    const int64_t n = tiles(bn) < pairs ? tiles(bn) : pairs;
+    const int64_t tiles = tc_tiles(g.M, g.N, gated, g.twice, bn), pairs = num_sms / 2, n = tiles < pairs ? tiles : pairs;
     return launch_k(gemm_tc_kernel<AT, BT>, dim3((unsigned)(2 * n)), dim3(kTcThreads), kTcSmem, st, false, g, maps, shape);
 }
 

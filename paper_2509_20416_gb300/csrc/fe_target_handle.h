@@ -45,8 +45,8 @@ inline fe_status check_device(const fe_target* t) {
 }
 
 // What the dense operators need of the device before their kernels run (shared memory above 48 KB, large clusters, how
-// many CTAs fit) is asked for when a handle first uses them: it loads some hundred kernels, 17 ms in a process, which a
-// handle that only rotates and attends need not pay. Twice, from two threads, does no harm.
+// many CTAs fit) is asked for when a handle first uses them: it loads their modules, 17 ms in a process (16 of them the
+// norms'), which a handle that only rotates and attends need not pay. Twice, from two threads, does no harm.
 enum Kernels : unsigned { GEMM_TC = 1, GEMM_FEW = 2, NORM = 4, NORM_BACKWARD = 8, LOGPROBS_F32 = 16, LOGPROBS_BF16 = 32 };
 template <typename F>
 fe_status set_up(const fe_target* t, Kernels which, const F& prepare) {
