@@ -21,13 +21,13 @@ constexpr int kBK = 16;
 
 // One operand's slice of R rows (tile rows) x 16 steps. Stored by rows (summed index contiguous) a
 // thread takes runs of 4 steps of a row, stored by steps (T) runs of 4 rows of a step.
-template <typename T, int R, bool STEPS>
+template <int R, bool STEPS>
 struct Slice {
     static constexpr int kRuns = R * kBK / 4 / 256;
     float v[kRuns][4];
 
-    // row_of(i): the row of the stored matrix for tile row i, -1 outside (BY ROWS); for STEPS tile rows
-    // are columns from r0 on, rows of them
+    // Steps k0 on, of K, of the R rows from r0 on, of `rows` (STEPS: columns of the stored matrix); what lies
+    // outside is 0. By rows, a tile of a gated pair (split > 0) takes its rows from `split` on from the second matrix.
     __device__ __forceinline__ void load(const fe_mat& m, int64_t r0, int64_t rows, int k0, int K, bool vec, int split,
                                          const fe_mat& second) {
 #pragma unroll
@@ -35,32 +35,25 @@ struct Slice {
             const int u = threadIdx.x + i * 256;
             if (!STEPS) {
                 const int r = u / (kBK / 4), k = k0 + u % (kBK / 4) * 4;
-                // gated tiles: their second half takes the same rows of the second matrix
                 const bool two = split > 0 && r >= split;
                 const int64_t row = r0 + (two ? r - split : r);
-                const T* p = (const T*)(two ? second.p : m.p) + row * (two ? second.row : m.row) + k;
+                const float* p = (const float*)(two ? second.p : m.p) + row * (two ? second.row : m.row) + k;
                 run(p, row < rows ? K - k : 0, vec, v[i]);
             } else {
                 const int k = u / (R / 4), r = u % (R / 4) * 4;
-                const T* p = (const T*)m.p + (int64_t)(k0 + k) * m.row + r0 + r;
+                const float* p = (const float*)m.p + (int64_t)(k0 + k) * m.row + r0 + r;
                 const int64_t left = rows - r0 - r;
                 run(p, k0 + k < K ? (left < 4 ? (int)left : 4) : 0, vec, v[i]);
             }
         }
     }
-    __device__ __forceinline__ static void run(const T* p, int have, bool vec, float* f) {
+    __device__ __forceinline__ static void run(const float* p, int have, bool vec, float* f) {
         if (vec && have >= 4) {
-            if (sizeof(T) == 4) {
-                const float4 x = *reinterpret_cast<const float4*>(p);
-                f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w;
-            } else {
-                const uint2 x = *reinterpret_cast<const uint2*>(p);
-                f[0] = __uint_as_float(x.x << 16), f[1] = __uint_as_float(x.x & 0xFFFF0000u);
-                f[2] = __uint_as_float(x.y << 16), f[3] = __uint_as_float(x.y & 0xFFFF0000u);
-            }
+            const float4 x = *reinterpret_cast<const float4*>(p);
+            f[0] = x.x, f[1] = x.y, f[2] = x.z, f[3] = x.w;
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f[i] = i < have ? load_one(p + i) : 0.f;
+            for (int i = 0; i < 4; ++i) f[i] = i < have ? p[i] : 0.f;
         }
     }
     __device__ __forceinline__ void store(float (*s)[R + 4]) const {
@@ -90,7 +83,7 @@ __device__ __forceinline__ void read_run(const float* s, float* f) {
     }
 }
 
-template <typename T, int BM, int BN, bool AT, bool BT, int P>
+template <int BM, int BN, bool AT, bool BT, int P>
 __global__ void __launch_bounds__(256, BM == 128 ? 2 : 3)
     gemm_simt_kernel(const __grid_constant__ GemmArgs g, int a_vec, int b_vec, int ranks) {
     constexpr int HM = BM / 32, HN = BN / 32;  // a thread's rows and columns: HM and HN in each half of the tile
@@ -122,8 +115,8 @@ __global__ void __launch_bounds__(256, BM == 128 ? 2 : 3)
         for (int j = 0; j < HN; ++j) acc[i][j] = 0;
     const int slices = (g.K + kBK - 1) / kBK, total = slices * g.segs;
     const int first = (int)((int64_t)total * rank / ranks), all = (int)((int64_t)total * (rank + 1) / ranks) - first;
-    Slice<T, BM, AT> a[P];  // slices i + 1 to i + P, on their way while slice i is multiplied
-    Slice<T, BN, BT> b[P];
+    Slice<BM, AT> a[P];  // slices i + 1 to i + P, on their way while slice i is multiplied
+    Slice<BN, BT> b[P];
     const auto fetch = [&](int s, int p) {
         if (s >= all) return;
         s += first;
@@ -176,10 +169,10 @@ __global__ void __launch_bounds__(256, BM == 128 ? 2 : 3)
     }
     const auto finish = [&](int64_t m, float* z) {
         if (e.kind == FINISH_GATED) {
-            epilogue_gated<T, HN>(e, m, n0 + tx * HN, g.N, z, z + HN);
+            epilogue_gated<HN>(e, m, n0 + tx * HN, g.N, z, z + HN);
         } else {
-            epilogue_one<T, HN>(e, m, n0 + tx * HN, g.N, z);
-            epilogue_one<T, HN>(e, m, n0 + BN / 2 + tx * HN, g.N, z + HN);
+            epilogue_one<HN>(e, m, n0 + tx * HN, g.N, z);
+            epilogue_one<HN>(e, m, n0 + BN / 2 + tx * HN, g.N, z + HN);
         }
     };
     const auto row_of = [&](int i) { return i < HM ? ty * HM + i : BM / 2 + ty * HM + i - HM; };
@@ -296,27 +289,26 @@ __global__ void __launch_bounds__(kDotWarps * 32) dot_kernel(const __grid_consta
     };
     if (gated) {
         float z = total(r % 2), u = total(2 + r % 2);
-        if (r < 2) epilogue_gated<float, 1>(g.e, m, (int)n0 + r, g.N, &z, &u);
+        if (r < 2) epilogue_gated<1>(g.e, m, (int)n0 + r, g.N, &z, &u);
     } else {
         float z = total(r);
-        epilogue_plain<float, 1>(g.e, m, (int)n0 + r, g.N, &z);
+        epilogue_plain<1>(g.e, m, (int)n0 + r, g.N, &z);
     }
 }
+
+// runs of 4 elements on their own boundary
+bool runs_of_4(const fe_mat& m) { return ((uintptr_t)m.p & 15) == 0 && m.row % 4 == 0; }
 
 template <int MT>
 cudaError_t launch_dot(const GemmArgs& g, cudaStream_t st) {
     const int per = g.e.kind == FINISH_GATED ? 2 : 4;
-    const auto on16 = [](const fe_mat& m) { return ((uintptr_t)m.p & 15) == 0 && m.row % 4 == 0; };
-    const bool vec = g.K % 4 == 0 && on16(g.a[0]) && on16(g.b[0]) && (per == 4 || on16(g.b[1]));
+    const bool vec = g.K % 4 == 0 && runs_of_4(g.a[0]) && runs_of_4(g.b[0]) && (per == 4 || runs_of_4(g.b[1]));
     return launch_k(vec ? dot_kernel<MT, true> : dot_kernel<MT, false>, dim3((unsigned)((g.N + per - 1) / per)), dim3(kDotWarps * 32), 0, st, false, g);
 }
 
-// runs of 4 elements on their own boundary
-bool runs_of_4(const fe_mat& m, int es) { return ((uintptr_t)m.p & (4 * es - 1)) == 0 && m.row % 4 == 0; }
-
-template <typename T, int BM, int BN, bool AT, bool BT>
+template <int BM, int BN, bool AT, bool BT>
 cudaError_t launch_tile(const GemmArgs& g, int num_sms, cudaStream_t st) {
-    const int es = sizeof(T), width = g.e.kind == FINISH_GATED ? BN / 2 : BN;
+    const int width = g.e.kind == FINISH_GATED ? BN / 2 : BN;
     const int64_t tiles = ((g.M + BM - 1) / BM) * ((g.N + width - 1) / width) * (g.twice ? 2 : 1);
     // CTAs of a tile: as many as two an SM hold, with eight slices each at least
     const int64_t slices = ((int64_t)g.K + kBK - 1) / kBK * g.segs;
@@ -325,8 +317,8 @@ cudaError_t launch_tile(const GemmArgs& g, int num_sms, cudaStream_t st) {
     if (tiles > 0x7FFFFFFF) return cudaErrorInvalidConfiguration;
     const int na = g.segs == 2 || g.twice ? 2 : 1, nb = g.segs == 2 || g.e.kind == FINISH_GATED ? 2 : 1;
     bool av = true, bv = true;
-    for (int i = 0; i < na; ++i) av = av && runs_of_4(g.a[i], es);
-    for (int i = 0; i < nb; ++i) bv = bv && runs_of_4(g.b[i], es);
+    for (int i = 0; i < na; ++i) av = av && runs_of_4(g.a[i]);
+    for (int i = 0; i < nb; ++i) bv = bv && runs_of_4(g.b[i]);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * ranks));
     cfg.blockDim = dim3(256);
@@ -337,13 +329,13 @@ cudaError_t launch_tile(const GemmArgs& g, int num_sms, cudaStream_t st) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = ranks > 1;
-    return cudaLaunchKernelEx(&cfg, gemm_simt_kernel<T, BM, BN, AT, BT, BM == 64 ? 2 : 1>, g, (int)av, (int)bv, ranks);
+    return cudaLaunchKernelEx(&cfg, gemm_simt_kernel<BM, BN, AT, BT, BM == 64 ? 2 : 1>, g, (int)av, (int)bv, ranks);
 }
 
-template <typename T, bool AT, bool BT>
+template <bool AT, bool BT>
 cudaError_t launch_layout(const GemmArgs& g, int num_sms, cudaStream_t st) {
-    if (simt_large(g.M, g.N, g.e.kind == FINISH_GATED, g.twice, num_sms)) return launch_tile<T, 128, 128, AT, BT>(g, num_sms, st);
-    return launch_tile<T, 64, 64, AT, BT>(g, num_sms, st);
+    if (simt_large(g.M, g.N, g.e.kind == FINISH_GATED, g.twice, num_sms)) return launch_tile<128, 128, AT, BT>(g, num_sms, st);
+    return launch_tile<64, 64, AT, BT>(g, num_sms, st);
 }
 
 }  // namespace
@@ -351,8 +343,8 @@ cudaError_t launch_layout(const GemmArgs& g, int num_sms, cudaStream_t st) {
 cudaError_t launch_gemm_simt(const GemmArgs& g, int num_sms, cudaStream_t st) {
     if (!g.a_t && !g.b_t && g.segs == 1 && g.M <= 8 && g.e.kind != FINISH_GATED_GRAD)
         return g.M == 1 ? launch_dot<1>(g, st) : g.M == 2 ? launch_dot<2>(g, st) : g.M <= 4 ? launch_dot<4>(g, st) : launch_dot<8>(g, st);
-    if (g.a_t) return launch_layout<float, true, true>(g, num_sms, st);  // (a weight's gradient: both by steps)
-    return g.b_t ? launch_layout<float, false, true>(g, num_sms, st) : launch_layout<float, false, false>(g, num_sms, st);
+    if (g.a_t) return launch_layout<true, true>(g, num_sms, st);  // (a weight's gradient: both by steps)
+    return g.b_t ? launch_layout<false, true>(g, num_sms, st) : launch_layout<false, false>(g, num_sms, st);
 }
 
 }  // namespace fe

@@ -93,14 +93,14 @@ __device__ __forceinline__ void store_row(T* p, int have, bool vec, const float*
     }
 }
 
-// NV columns of row m from column n on, of a plain product z (overwritten)
-template <typename T, int NV>
+// What becomes of a float32 product: NV columns of row m from column n on, of a plain product z (overwritten)
+template <int NV>
 __device__ __forceinline__ void epilogue_plain(const Finish& e, int64_t m, int n, int N, float* z) {
     const int have = N - n;
     if (have <= 0) return;
     float t[NV];
     if (e.bias) {
-        load_row<T, NV>((const T*)e.bias + n, have, e.vec, t);
+        load_row<float, NV>((const float*)e.bias + n, have, e.vec, t);
 #pragma unroll
         for (int i = 0; i < NV; ++i) z[i] += t[i];
     }
@@ -110,15 +110,15 @@ __device__ __forceinline__ void epilogue_plain(const Finish& e, int64_t m, int n
         for (int i = 0; i < NV; ++i) z[i] = act_value<false>(e.act, z[i]);
     }
     if (e.res) {
-        load_row<T, NV>((const T*)e.res + m * e.res_row + n, have, e.vec, t);
+        load_row<float, NV>((const float*)e.res + m * e.res_row + n, have, e.vec, t);
 #pragma unroll
         for (int i = 0; i < NV; ++i) z[i] += t[i];
     }
-    store_row<T, NV>((T*)e.out + m * e.out_row + n, have, e.vec, z);
+    store_row<float, NV>((float*)e.out + m * e.out_row + n, have, e.vec, z);
 }
 
 // the same of a gated pair of products g and u (g is overwritten)
-template <typename T, int NV>
+template <int NV>
 __device__ __forceinline__ void epilogue_gated(const Finish& e, int64_t m, int n, int N, float* g, const float* u) {
     const int have = N - n;
     if (have <= 0) return;
@@ -128,11 +128,11 @@ __device__ __forceinline__ void epilogue_gated(const Finish& e, int64_t m, int n
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) g[i] = act_value<false>(e.act, g[i]) * u[i];
-    store_row<T, NV>((T*)e.out + m * e.out_row + n, have, e.vec, g);
+    store_row<float, NV>((float*)e.out + m * e.out_row + n, have, e.vec, g);
 }
 
 // the gradients of a gated pair for the product z = dh, and the pair's own result
-template <typename T, int NV>
+template <int NV>
 __device__ __forceinline__ void epilogue_gated_grad(const Finish& e, int64_t m, int n, int N, float* z) {
     const int have = N - n;
     if (have <= 0) return;
@@ -148,15 +148,15 @@ __device__ __forceinline__ void epilogue_gated_grad(const Finish& e, int64_t m, 
         u[i] *= v;
         z[i] = dv;
     }
-    store_row<T, NV>((T*)e.out + m * e.out_row + n, have, e.vec, z);
-    store_row<T, NV>((T*)e.out2 + m * e.out2_row + n, have, e.vec, g);
-    store_row<T, NV>((T*)e.out3 + m * e.out3_row + n, have, e.vec, u);
+    store_row<float, NV>((float*)e.out + m * e.out_row + n, have, e.vec, z);
+    store_row<float, NV>((float*)e.out2 + m * e.out2_row + n, have, e.vec, g);
+    store_row<float, NV>((float*)e.out3 + m * e.out3_row + n, have, e.vec, u);
 }
 
-template <typename T, int NV>
+template <int NV>
 __device__ __forceinline__ void epilogue_one(const Finish& e, int64_t m, int n, int N, float* z) {
-    if (e.kind == FINISH_GATED_GRAD) epilogue_gated_grad<T, NV>(e, m, n, N, z);
-    else epilogue_plain<T, NV>(e, m, n, N, z);
+    if (e.kind == FINISH_GATED_GRAD) epilogue_gated_grad<NV>(e, m, n, N, z);
+    else epilogue_plain<NV>(e, m, n, N, z);
 }
 
 }  // namespace fe
